@@ -156,6 +156,9 @@ def _prepare_norm(case, seed, gen):
     # a residual stream: a mean of its own in each channel, a few channels far larger than the rest
     x = _normal(gen, rows, H).mul_(1 + 10 * (torch.rand(H, generator=gen, device="cuda") < 0.01)).add_(0.3 * _normal(gen, H) + 0.2)
     s = {"case": case, "x": _rows(x, dt, case["pad"]), "gamma": (1 + 0.1 * _normal(gen, H)).to(DT[case["w"]])}
+    if own:
+        from paper_2602_22445_b200 import binding as B
+        s["lib"], s["desc"] = B, B.make_norm_desc(H, dt, DT[case["w"]], P=case.get("P", 1), k=case.get("k", H), eps=NORM_EPS)
     if case["op"] == "fwd":
         s["beta"] = (0.1 * _normal(gen, H)).to(DT[case["w"]])
         s["y"] = torch.zeros(rows, H, dtype=dt, device="cuda")
@@ -173,8 +176,7 @@ def _prepare_norm(case, seed, gen):
     s["dx"] = torch.zeros(rows, H, dtype=dt, device="cuda")
     s["dgamma"], s["dbeta"] = torch.zeros(S, P, case["k"], device="cuda"), torch.zeros(S, P, case["k"], device="cuda")
     if own:
-        from paper_2602_22445_b200 import binding as B
-        s["workspace"] = torch.empty(max(16, B.ftc_layernorm_workspace_bytes(_norm_desc(case), rows)), dtype=torch.uint8, device="cuda")
+        s["workspace"] = torch.empty(max(16, B.ftc_layernorm_workspace_bytes(s["desc"], rows)), dtype=torch.uint8, device="cuda")
     return s
 
 
@@ -224,6 +226,7 @@ def _prepare_tensors(case, seed, gen):
         s["scale"] = torch.tensor([0.75], device="cuda")         # the clip factor, where the norm left it
     if own:
         from paper_2602_22445_b200 import binding as B
+        s["lib"] = B
         s["table"] = B.make_param_table([
             B.make_param(s["param"][i] if case["op"] == "adamw" else None, g, master=s["master"][i] if case["op"] == "adamw" else None,
                          status=s["status"][i], k=case["k"], weight_decay=s["decay"][i] if case["op"] == "adamw" else 0.0)
@@ -244,36 +247,27 @@ def run(s):
     return {"fwd": _plain_fwd, "bwd": _plain_bwd, "gnorm": _plain_gnorm, "adamw": _plain_adamw}[op](s)
 
 
-def _norm_desc(case):
-    from paper_2602_22445_b200 import binding as B
-    return B.make_norm_desc(case["H"], DT[case["x"]], DT[case["w"]], P=case.get("P", 1), k=case.get("k", case["H"]), eps=NORM_EPS)
-
-
 def _own_fwd(s):
-    from paper_2602_22445_b200 import binding as B
-    B.ftc_layernorm_forward(_norm_desc(s["case"]), s["x"], s["gamma"], s["beta"], s["y"], s["mean"], s["rstd"])
+    s["lib"].ftc_layernorm_forward(s["desc"], s["x"], s["gamma"], s["beta"], s["y"], s["mean"], s["rstd"])
     return s["y"], s["mean"], s["rstd"]
 
 
 def _own_bwd(s):
-    from paper_2602_22445_b200 import binding as B
-    B.ftc_layernorm_backward(_norm_desc(s["case"]), s["dy"], s["x"], s["gamma"], s["mean"], s["rstd"], s["splits"],
-                             s["dx"], s["dgamma"], s["dbeta"], s["workspace"])
+    s["lib"].ftc_layernorm_backward(s["desc"], s["dy"], s["x"], s["gamma"], s["mean"], s["rstd"], s["splits"],
+                                    s["dx"], s["dgamma"], s["dbeta"], s["workspace"])
     return s["dx"], s["dgamma"], s["dbeta"]
 
 
 def _own_gnorm(s):
-    from paper_2602_22445_b200 import binding as B
-    B.ftc_grad_norm(s["table"], MAX_NORM, s["norm"], s["norms"], s["workspace"])
+    s["lib"].ftc_grad_norm(s["table"], MAX_NORM, s["norm"], s["norms"], s["workspace"])
     return s["norm"], s["norms"]
 
 
 def _own_adamw(s):
-    from paper_2602_22445_b200 import binding as B
-    B.ftc_adamw_step(s["hyper"], s["table"], s["m"], s["v"], s["m_scale"], s["v_scale"], s["scale"])
+    s["lib"].ftc_adamw_step(s["hyper"], s["table"], s["m"], s["v"], s["m_scale"], s["v_scale"], s["scale"])
     if s["case"]["bits"] == 32:
         return s["flat"], s["flat32"], s["m"], s["v"]
-    B.ftc_adamw_states(s["table"], s["m"], s["v"], s["m_scale"], s["v_scale"], s["m_out"], s["v_out"])
+    s["lib"].ftc_adamw_states(s["table"], s["m"], s["v"], s["m_scale"], s["v_scale"], s["m_out"], s["v_out"])
     return s["flat"], s["flat32"], s["m_out"], s["v_out"]
 
 
