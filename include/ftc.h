@@ -63,7 +63,8 @@ extern "C" {
 #define FTC_VERSION 0x00010000u
 
 /* element types and reduction functions (section "Reduce": associative and commutative) */
-enum { FTC_I32 = 0, FTC_I64 = 1, FTC_U64 = 2, FTC_F32 = 3 };
+enum { FTC_I32 = 0, FTC_I64 = 1, FTC_U64 = 2, FTC_F32 = 3,
+       FTC_BF16 = 4, FTC_F16 = 5 };           /* the training operators below only; the batch calls refuse them */
 enum { FTC_SUM = 0, FTC_MAX = 1, FTC_XOR = 2 };   /* integer sums wrap; FTC_F32 supports FTC_SUM only */
 
 /* call-level return codes */
@@ -334,6 +335,132 @@ FTC_API const char* ftc_kernel_variant(const ftc_desc_t* desc, int is_allreduce)
  * kernel for scenarios of a few KB hands out short runs of consecutive scenarios the same way); a batch keeps the whole
  * GPU busy when S is a few times this number. Needs a device. Launches nothing. */
 FTC_API int ftc_launch_blocks(const ftc_desc_t* desc, uint64_t S, int is_allreduce, uint32_t* blocks);
+
+/*
+ * Training operators around the collectives (not part of the paper's method): the operators of a data-parallel training
+ * step that make the messages a corrected allreduce sends, and that consume what it delivers together with the status
+ * records. All arithmetic is in float32 whatever the element types; sums over long axes keep float32 or float64 partial
+ * sums in a fixed order (no atomic additions: the same call on the same GPU model gives the same bits).
+ *
+ * Layer norm over rows of H elements, as P processes of a data-parallel job see it.
+ */
+typedef struct {
+    uint32_t H;         /* elements of a row, 1 .. 2^24 */
+    uint32_t P;         /* processes the rows are divided over (backward), 1 .. 2^20; 1: the ordinary weight gradient */
+    uint32_t k;         /* elements of a message (backward): the weight gradients are [ceil(H/k)][P][k]; k = H and P = 1: [H] */
+    uint32_t dtype;     /* x, y, dy, dx: FTC_F32, FTC_BF16 or FTC_F16 */
+    uint32_t wdtype;    /* gamma, beta: FTC_F32 or dtype */
+    float    eps;       /* >= 0 */
+} ftc_norm_t;
+
+/*
+ * y = (x - mean) * rstd * gamma + beta with mean = sum(x) / H, rstd = 1 / sqrt(sum((x - mean)^2) / H + eps), for each row.
+ *   d_x     [rows] rows of H elements, row r at element r * x_stride; d_y likewise (x_stride, y_stride >= H); d_y may be d_x
+ *           (with the same stride)
+ *   d_gamma, d_beta  [H] of wdtype; NULL: ones, zeros
+ *   d_mean, d_rstd   [rows] float32 for the backward pass; either may be NULL
+ * Pointers are aligned to their element size; rows that begin on 16-byte boundaries (pointer and stride) with H a multiple
+ * of 16 bytes are the fast case. rows = 0 is valid and does nothing. FTC_EUNSUPPORTED: another dtype or wdtype.
+ */
+FTC_API int ftc_layernorm_forward(const ftc_norm_t* desc, uint64_t rows, const void* d_x, uint64_t x_stride, const void* d_gamma,
+                                  const void* d_beta, void* d_y, uint64_t y_stride, float* d_mean, float* d_rstd, void* cuda_stream);
+
+/*
+ * Gradients of the above. With xh = (x - mean) * rstd and a = dy * gamma:
+ *   dx = rstd * (a - sum(a)/H - xh * sum(a * xh)/H) for each row, dgamma = sum of dy * xh and dbeta = sum of dy over the rows
+ *   that a process holds.
+ *   d_mean, d_rstd  [rows], as the forward pass left them
+ *   d_row_splits    [P+1] uint64, ascending: process p holds rows d_row_splits[p] .. d_row_splits[p+1]-1 (values beyond `rows`
+ *                   count as `rows`; none: its gradients are zero). NULL: process p holds rows p*rows/P .. (p+1)*rows/P-1
+ *   d_dx            rows of H elements, or NULL; may be d_dy or d_x (with the same stride)
+ *   d_dgamma, d_dbeta  float32 [ceil(H/k)][P][k] -- the inputs of ceil(H/k) scenarios for ftc_allreduce_batch (FTC_F32, FTC_SUM):
+ *                   column h of process p is element h % k of message h / k; the last message is filled up with zeros; NULL: not
+ *                   computed
+ *   d_workspace     ftc_layernorm_workspace_bytes(desc, rows) bytes (0 when neither weight gradient is wanted), 16-byte aligned
+ * rows = 0 writes zeros to the weight gradients.
+ */
+FTC_API int ftc_layernorm_backward(const ftc_norm_t* desc, uint64_t rows, const void* d_dy, uint64_t dy_stride, const void* d_x,
+                                   uint64_t x_stride, const void* d_gamma, const float* d_mean, const float* d_rstd,
+                                   const uint64_t* d_row_splits, void* d_dx, uint64_t dx_stride, float* d_dgamma, float* d_dbeta,
+                                   void* d_workspace, size_t workspace_bytes, void* cuda_stream);
+FTC_API size_t ftc_layernorm_workspace_bytes(const ftc_norm_t* desc, uint64_t rows);   /* 0 for an invalid descriptor */
+
+/*
+ * Many tensors at once: a table of a model's tensors, built on the host, kept by the caller on the host and (a copy) on the
+ * device, and given to the calls below. Each call is one pass over all tensors.
+ */
+typedef struct {
+    void* param;                /* [n] of param_dtype: the weights (may be NULL in tables that only ftc_grad_norm gets) */
+    float* master;              /* [n]: the weights in 32 bits, which the update works on; param is then the rounded copy, written
+                                   only. NULL: param itself is updated (rounded to nearest) */
+    const void* grad;           /* [n] of grad_dtype: the gradient, or (with status) the sums that an allreduce delivered, its d_out
+                                   [ceil(n/k)][k] of which the first n elements count */
+    const uint32_t* status;     /* [ceil(n/k)][FTC_STATUS_WORDS]: the status records of those messages, 16-byte aligned. The gradient
+                                   is the sum divided by the processes included in it; a message with another outcome than FTC_ST_OK
+                                   (or nobody included) was not delivered: its elements keep their weights and states and count
+                                   nothing in the norm. NULL: the gradient is taken as it is */
+    uint64_t n;                 /* elements, 0 .. 2^40 */
+    uint32_t k;                 /* elements of a message, 1 .. 2^30; read only with status */
+    uint32_t param_dtype;       /* FTC_F32, FTC_BF16, FTC_F16 */
+    uint32_t grad_dtype;
+    float    lr_scale;          /* this tensor's learning rate is lr * lr_scale */
+    float    weight_decay;
+    uint32_t reserved;          /* 0 */
+} ftc_param_t;
+
+#define FTC_STATE_BLOCK 256u    /* the optimizer states are laid out in blocks of so many elements of one tensor: tensor i begins at
+                                   the sum of ceil(n/256) over the tensors before it (in blocks), its last block filled up */
+
+FTC_API size_t ftc_param_table_bytes(const ftc_param_t* h_params, uint32_t n_params);  /* 0 for invalid entries */
+/* Checks the entries and writes the table to h_table (8-byte aligned host memory of that many bytes). The caller copies it to
+ * the device as it is (256-byte aligned); it holds the tensors' addresses, so tensors that move need a new table.
+ * FTC_EINVAL: NULL grad with n > 0, misaligned pointers (element size), k = 0 with status, n or n_params out of range. */
+FTC_API int ftc_param_table_build(const ftc_param_t* h_params, uint32_t n_params, void* h_table, size_t table_bytes);
+/* Blocks of FTC_STATE_BLOCK elements that the table's tensors take up; 0 for anything that is no table. */
+FTC_API uint64_t ftc_param_table_blocks(const void* h_table);
+
+/*
+ * The 2-norm of all gradients together, the factor that clips it, and the norm of each tensor's gradient.
+ *   d_norm   [2] float32: the norm over all tensors; max_norm / norm where the norm exceeds max_norm, else 1, NaN where the norm is
+ *            not finite (which makes ftc_adamw_step do nothing)
+ *   d_norms  [n_params] float32: each tensor's norm, or NULL
+ *   d_workspace  ftc_grad_norm_workspace_bytes(h_table) bytes, 16-byte aligned
+ * Squares are added up in float64. max_norm > 0 (infinity: no clipping).
+ */
+FTC_API int ftc_grad_norm(const void* h_table, const void* d_table, float max_norm, float* d_norm, float* d_norms,
+                          void* d_workspace, size_t workspace_bytes, void* cuda_stream);
+FTC_API size_t ftc_grad_norm_workspace_bytes(const void* h_table);
+
+/* One AdamW step (decoupled weight decay). */
+typedef struct {
+    double lr, beta1, beta2, eps;   /* lr >= 0 finite, 0 <= beta < 1, eps >= 0 */
+    uint64_t step;                  /* 1 for the first step (bias corrections 1 - beta^step) */
+    uint32_t state_bits;            /* 32 or 8 */
+    uint32_t reserved;              /* 0 */
+} ftc_adamw_t;
+
+/*
+ * For every element, in float32 with each operation rounded (no fused multiply-add), c1 = 1/(1-beta1^step), c2 = 1/sqrt(1-beta2^step),
+ * l = lr * lr_scale:
+ *   g = grad * (1 / included) * *d_grad_scale;  m = m*beta1 + g*(1-beta1);  v = v*beta2 + (g*g)*(1-beta2)
+ *   p = p * (1 - l*weight_decay) - (m / (sqrt(v)*c2 + eps)) * (l*c1)
+ *   d_m, d_v  states of ftc_param_table_blocks() blocks of FTC_STATE_BLOCK elements: float32, or with state_bits = 8 int8 and
+ *             uint8; zero bytes before the first step; 32-byte aligned
+ *   d_m_scale, d_v_scale  float32, one for each block (state_bits = 8; else NULL)
+ *   d_grad_scale  one float32 (d_norm + 1 of ftc_grad_norm), or NULL for 1; where it is not finite the call changes nothing
+ * States in 8 bits: with s = max |m| of the block (at least 2^-126), m is held as the whole number c nearest to 127*sqrt(|m|/s),
+ * signed, and stands for c*|c|*s/127^2. v is held through its root r = sqrt(v): s = max r, c nearest to 255*sqrt(r/s) and at
+ * least 1 where r > 0; it stands for (c^2*s/255^2)^2. The update itself uses the new m and v before they are rounded. A block of which no
+ * element's message was delivered stays as it is; a block that meets NaN or an infinity stands for NaN afterwards.
+ * param must not be NULL for tensors with n > 0 (FTC_EINVAL).
+ */
+FTC_API int ftc_adamw_step(const ftc_adamw_t* hyper, const void* h_table, const void* d_table, void* d_m, void* d_v,
+                           float* d_m_scale, float* d_v_scale, const float* d_grad_scale, void* cuda_stream);
+
+/* What states in 8 bits stand for, in the same layout: d_m_out, d_v_out float32 [blocks][FTC_STATE_BLOCK], 32-byte aligned (for
+ * checkpoints, inspection, or going on in 32 bits). `blocks` blocks of d_m, d_v and the scales are read. */
+FTC_API int ftc_adamw_states(uint64_t blocks, const void* d_m, const void* d_v, const float* d_m_scale, const float* d_v_scale,
+                             float* d_m_out, float* d_v_out, void* cuda_stream);
 
 FTC_API const char* ftc_strerror(int code);
 FTC_API uint32_t ftc_version(void);

@@ -15,6 +15,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libftc.so")
 
 FTC_I32, FTC_I64, FTC_U64, FTC_F32 = 0, 1, 2, 3
+FTC_BF16, FTC_F16 = 4, 5                 # training operators only
 FTC_SUM, FTC_MAX, FTC_XOR = 0, 1, 2
 FTC_OK, FTC_EINVAL, FTC_EUNSUPPORTED, FTC_EWORKSPACE, FTC_ECUDA, FTC_ETOOLARGE = 0, -1, -2, -3, -4, -5
 FTC_NOALLOC_SCRATCH_BYTES = 8 << 20
@@ -42,7 +43,11 @@ OPS = {"sum": FTC_SUM, "max": FTC_MAX, "xor": FTC_XOR}
 EXPORTS = ["ftc_reduce_batch", "ftc_allreduce_batch", "ftc_reduce_batch_noalloc", "ftc_candidates_batch",
            "ftc_candidates_workspace_bytes", "ftc_candidates_kernel_name", "ftc_message_counts_batch", "ftc_failed_list_batch", "ftc_workspace_bytes", "ftc_reduce_batch_host",
            "ftc_allreduce_batch_host", "ftc_host_staging_bytes", "ftc_schedule_info", "ftc_fill_inputs",
-           "ftc_kernel_name", "ftc_kernel_variant", "ftc_launch_blocks", "ftc_read_bandwidth_probe", "ftc_strerror", "ftc_version"]
+           "ftc_kernel_name", "ftc_kernel_variant", "ftc_launch_blocks", "ftc_read_bandwidth_probe", "ftc_strerror", "ftc_version",
+           "ftc_layernorm_forward", "ftc_layernorm_backward", "ftc_layernorm_workspace_bytes", "ftc_param_table_bytes",
+           "ftc_param_table_build", "ftc_param_table_blocks", "ftc_grad_norm", "ftc_grad_norm_workspace_bytes", "ftc_adamw_step",
+           "ftc_adamw_states"]
+FTC_STATE_BLOCK = 256
 
 
 class ftc_desc_t(C.Structure):
@@ -53,6 +58,22 @@ class ftc_desc_t(C.Structure):
 class ftc_sched_t(C.Structure):
     _fields_ = [("q", C.c_uint32), ("r", C.c_uint32), ("H", C.c_uint32), ("rounds_reduce", C.c_uint32),
                 ("rounds_attempt", C.c_uint32), ("msgs_upcorrection", C.c_uint64), ("msgs_tree", C.c_uint64)]
+
+
+class ftc_norm_t(C.Structure):
+    _fields_ = [("H", C.c_uint32), ("P", C.c_uint32), ("k", C.c_uint32), ("dtype", C.c_uint32), ("wdtype", C.c_uint32),
+                ("eps", C.c_float)]
+
+
+class ftc_param_t(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("master", C.c_void_p), ("grad", C.c_void_p), ("status", C.c_void_p), ("n", C.c_uint64),
+                ("k", C.c_uint32), ("param_dtype", C.c_uint32), ("grad_dtype", C.c_uint32), ("lr_scale", C.c_float),
+                ("weight_decay", C.c_float), ("reserved", C.c_uint32)]
+
+
+class ftc_adamw_t(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_uint64),
+                ("state_bits", C.c_uint32), ("reserved", C.c_uint32)]
 
 
 class FtcError(RuntimeError):
@@ -107,6 +128,27 @@ def load():
     lib.ftc_launch_blocks.argtypes = [dp, u64, C.c_int, C.POINTER(u32)]
     lib.ftc_read_bandwidth_probe.restype = C.c_int
     lib.ftc_read_bandwidth_probe.argtypes = [u32, vp, u64, vp, vp]
+    np_, ap = C.POINTER(ftc_norm_t), C.POINTER(ftc_adamw_t)
+    lib.ftc_layernorm_forward.restype = C.c_int
+    lib.ftc_layernorm_forward.argtypes = [np_, u64, vp, u64, vp, vp, vp, u64, vp, vp, vp]
+    lib.ftc_layernorm_backward.restype = C.c_int
+    lib.ftc_layernorm_backward.argtypes = [np_, u64, vp, u64, vp, u64, vp, vp, vp, vp, vp, u64, vp, vp, vp, sz, vp]
+    lib.ftc_layernorm_workspace_bytes.restype = sz
+    lib.ftc_layernorm_workspace_bytes.argtypes = [np_, u64]
+    lib.ftc_param_table_bytes.restype = sz
+    lib.ftc_param_table_bytes.argtypes = [vp, u32]
+    lib.ftc_param_table_build.restype = C.c_int
+    lib.ftc_param_table_build.argtypes = [vp, u32, vp, sz]
+    lib.ftc_param_table_blocks.restype = u64
+    lib.ftc_param_table_blocks.argtypes = [vp]
+    lib.ftc_grad_norm.restype = C.c_int
+    lib.ftc_grad_norm.argtypes = [vp, vp, C.c_float, vp, vp, vp, sz, vp]
+    lib.ftc_grad_norm_workspace_bytes.restype = sz
+    lib.ftc_grad_norm_workspace_bytes.argtypes = [vp]
+    lib.ftc_adamw_step.restype = C.c_int
+    lib.ftc_adamw_step.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.ftc_adamw_states.restype = C.c_int
+    lib.ftc_adamw_states.argtypes = [u64, vp, vp, vp, vp, vp, vp, vp]
     lib.ftc_strerror.restype = C.c_char_p
     lib.ftc_strerror.argtypes = [C.c_int]
     lib.ftc_version.restype = u32
@@ -299,4 +341,171 @@ def ftc_fill_inputs(kind, seed, first_scenario, S, P, k, d_out, stream=None) -> 
                                 _stream(stream))
     if rc != FTC_OK:
         raise FtcError(rc, "ftc_fill_inputs")
+    return rc
+
+
+# ---- training operators: layer norm, many-tensor gradient norm and AdamW ----
+
+def _float_code(dt) -> int:
+    """FTC_* code of the floating types the training operators take."""
+    name = str(dt).replace("torch.", "")
+    codes = {"float32": FTC_F32, "bfloat16": FTC_BF16, "float16": FTC_F16}
+    if name not in codes:
+        raise ValueError(f"float32, bfloat16 or float16 wanted, got {name}")
+    return codes[name]
+
+
+def make_norm_desc(H, dtype, wdtype=None, P=1, k=None, eps=1e-5) -> ftc_norm_t:
+    """Rows of H elements of `dtype`, weights of `wdtype` (default: `dtype`); P and k: processes and message length of the weight
+    gradients (default: one process, one message of H elements)."""
+    dtype = dtype if isinstance(dtype, int) else _float_code(dtype)
+    wdtype = dtype if wdtype is None else wdtype if isinstance(wdtype, int) else _float_code(wdtype)
+    return ftc_norm_t(H, P, H if k is None else k, dtype, wdtype, eps)
+
+
+def _rows_ptr(desc, t, what, rows):
+    """Address and row stride of a [rows][H] tensor of the descriptor's type whose rows are contiguous."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != desc.H or (desc.H > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: a CUDA tensor [{rows}][{desc.H}] with contiguous rows is wanted")
+    if _float_code(t.dtype) != desc.dtype:
+        raise ValueError(f"{what}: its type is not the descriptor's")
+    stride = t.stride(0)
+    if rows <= 1 and stride < desc.H:
+        stride = desc.H
+    return t.data_ptr(), stride
+
+
+def _vector_ptr(t, what, n, code=FTC_F32):
+    if t is None:
+        return None
+    if t.numel() != n or _float_code(t.dtype) != code:
+        raise ValueError(f"{what}: {n} elements of the right type are wanted")
+    return _dev_ptr(t)
+
+
+def ftc_layernorm_forward(desc, d_x, d_gamma, d_beta, d_y, d_mean, d_rstd, stream=None, check=True) -> int:
+    rows = d_x.shape[0]
+    x, xs = _rows_ptr(desc, d_x, "d_x", rows)
+    y, ys = _rows_ptr(desc, d_y, "d_y", rows)
+    rc = load().ftc_layernorm_forward(C.byref(desc), rows, x, xs, _vector_ptr(d_gamma, "d_gamma", desc.H, desc.wdtype),
+                                      _vector_ptr(d_beta, "d_beta", desc.H, desc.wdtype), y, ys,
+                                      _vector_ptr(d_mean, "d_mean", rows), _vector_ptr(d_rstd, "d_rstd", rows), _stream(stream))
+    if check and rc != FTC_OK:
+        raise FtcError(rc, "ftc_layernorm_forward")
+    return rc
+
+
+def ftc_layernorm_workspace_bytes(desc, rows) -> int:
+    return load().ftc_layernorm_workspace_bytes(C.byref(desc), rows)
+
+
+def ftc_layernorm_backward(desc, d_dy, d_x, d_gamma, d_mean, d_rstd, d_row_splits, d_dx, d_dgamma, d_dbeta, d_workspace,
+                           stream=None, check=True) -> int:
+    rows = d_x.shape[0]
+    dy, dys = _rows_ptr(desc, d_dy, "d_dy", rows)
+    x, xs = _rows_ptr(desc, d_x, "d_x", rows)
+    dx, dxs = _rows_ptr(desc, d_dx, "d_dx", rows)
+    n = -(-desc.H // desc.k) * desc.P * desc.k
+    if d_row_splits is not None and (d_row_splits.numel() != desc.P + 1 or d_row_splits.element_size() != 8 or d_row_splits.is_floating_point()):
+        raise ValueError("d_row_splits: P + 1 whole numbers of 64 bits are wanted")
+    ws_bytes = 0 if d_workspace is None else d_workspace.numel() * d_workspace.element_size()
+    rc = load().ftc_layernorm_backward(C.byref(desc), rows, dy, dys, x, xs, _vector_ptr(d_gamma, "d_gamma", desc.H, desc.wdtype),
+                                       _vector_ptr(d_mean, "d_mean", rows), _vector_ptr(d_rstd, "d_rstd", rows),
+                                       _dev_ptr(d_row_splits), dx, dxs, _vector_ptr(d_dgamma, "d_dgamma", n),
+                                       _vector_ptr(d_dbeta, "d_dbeta", n), _dev_ptr(d_workspace), ws_bytes, _stream(stream))
+    if check and rc != FTC_OK:
+        raise FtcError(rc, "ftc_layernorm_backward")
+    return rc
+
+
+def make_param(param, grad, master=None, status=None, k=0, lr_scale=1.0, weight_decay=0.0):
+    """One tensor of a table: the arguments of ftc_param_t, as tensors. A table keeps them alive."""
+    n = grad.numel()
+    for t, what in ((param, "param"), (master, "master")):
+        if t is not None and t.numel() != n:
+            raise ValueError(f"{what}: {n} elements are wanted, as in grad")
+    if master is not None and _float_code(master.dtype) != FTC_F32:
+        raise ValueError("master: float32 is wanted")
+    if status is not None and (k < 1 or status.numel() != -(-n // k) * FTC_STATUS_WORDS or status.element_size() != 4):
+        raise ValueError("status: one record of 4 words of 32 bits for each message of k elements is wanted")
+    entry = ftc_param_t(_dev_ptr(param), _dev_ptr(master), _dev_ptr(grad), _dev_ptr(status), n, k if status is not None else 0,
+                        FTC_F32 if param is None else _float_code(param.dtype), _float_code(grad.dtype), lr_scale, weight_decay, 0)
+    return entry, (param, grad, master, status)
+
+
+class ParamTable:
+    """A table of tensors (ftc_param_table_build) on the host and on the device, with the tensors that it points to."""
+
+    def __init__(self, params, device="cuda"):
+        torch = _torch()
+        entries = (ftc_param_t * max(1, len(params)))(*[p[0] for p in params])
+        size = load().ftc_param_table_bytes(entries, len(params))
+        self.host = np.zeros(max(size, 8) // 8, dtype=np.uint64)
+        rc = load().ftc_param_table_build(entries, len(params), self.host.ctypes.data, size)
+        if rc != FTC_OK:
+            raise FtcError(rc, "ftc_param_table_build")
+        self.keeps = [p[1] for p in params]
+        self.n_params = len(params)
+        self.h_ptr = self.host.ctypes.data
+        self.blocks = load().ftc_param_table_blocks(self.h_ptr)
+        self.device = torch.from_numpy(self.host.view(np.int64)).to(device)
+        self.d_ptr = self.device.data_ptr()
+
+
+def make_param_table(params, device="cuda") -> ParamTable:
+    """The table of a list of make_param()s. Tensors that move need a new one."""
+    return ParamTable(params, device)
+
+
+def ftc_grad_norm_workspace_bytes(table) -> int:
+    return load().ftc_grad_norm_workspace_bytes(table.h_ptr)
+
+
+def ftc_grad_norm(table, max_norm, d_norm, d_norms, d_workspace, stream=None, check=True) -> int:
+    ws_bytes = 0 if d_workspace is None else d_workspace.numel() * d_workspace.element_size()
+    rc = load().ftc_grad_norm(table.h_ptr, table.d_ptr, max_norm, _vector_ptr(d_norm, "d_norm", 2),
+                              _vector_ptr(d_norms, "d_norms", table.n_params), _dev_ptr(d_workspace), ws_bytes, _stream(stream))
+    if check and rc != FTC_OK:
+        raise FtcError(rc, "ftc_grad_norm")
+    return rc
+
+
+def make_adamw(lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1) -> ftc_adamw_t:
+    return ftc_adamw_t(lr, beta1, beta2, eps, step, 32, 0)
+
+
+def _states(table, d_m, d_v, d_m_scale, d_v_scale):
+    """The states' bits and addresses, sizes checked."""
+    n = table.blocks * FTC_STATE_BLOCK
+    bits = 8 * d_m.element_size()
+    if bits != 8 * d_v.element_size() or d_m.numel() != n or d_v.numel() != n or (bits != 8 and d_m.dtype != d_v.dtype):
+        raise ValueError(f"states: {n} elements each, float32 or 8-bit, are wanted")
+    if bits == 8 and (d_m_scale is None or d_v_scale is None):
+        raise ValueError("states in 8 bits: scales are wanted")
+    if bits != 8 and _float_code(d_m.dtype) != FTC_F32:
+        raise ValueError("states: float32 or 8-bit elements are wanted")
+    scales = [_vector_ptr(t, "scales", table.blocks) if bits == 8 else None for t in (d_m_scale, d_v_scale)]
+    return bits, [_dev_ptr(d_m), _dev_ptr(d_v), *scales]
+
+
+def ftc_adamw_step(hyper, table, d_m, d_v, d_m_scale=None, d_v_scale=None, d_grad_scale=None, stream=None, check=True) -> int:
+    hyper.state_bits, states = _states(table, d_m, d_v, d_m_scale, d_v_scale)
+    rc = load().ftc_adamw_step(C.byref(hyper), table.h_ptr, table.d_ptr, *states, _vector_ptr(d_grad_scale, "d_grad_scale", 1),
+                               _stream(stream))
+    if check and rc != FTC_OK:
+        raise FtcError(rc, "ftc_adamw_step")
+    return rc
+
+
+def ftc_adamw_states(table, d_m, d_v, d_m_scale, d_v_scale, d_m_out, d_v_out, stream=None, check=True) -> int:
+    bits, states = _states(table, d_m, d_v, d_m_scale, d_v_scale)
+    if bits != 8:
+        raise ValueError("states in 8 bits are wanted")
+    n = table.blocks * FTC_STATE_BLOCK
+    rc = load().ftc_adamw_states(table.blocks, *states, _vector_ptr(d_m_out, "d_m_out", n), _vector_ptr(d_v_out, "d_v_out", n),
+                                 _stream(stream))
+    if check and rc != FTC_OK:
+        raise FtcError(rc, "ftc_adamw_states")
     return rc
