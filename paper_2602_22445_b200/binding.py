@@ -346,13 +346,18 @@ def ftc_fill_inputs(kind, seed, first_scenario, S, P, k, d_out, stream=None) -> 
 
 # ---- training operators: layer norm, many-tensor gradient norm and AdamW ----
 
+_FLOAT_CODES = {"float32": FTC_F32, "bfloat16": FTC_BF16, "float16": FTC_F16}
+
+
 def _float_code(dt) -> int:
-    """FTC_* code of the floating types the training operators take."""
-    name = str(dt).replace("torch.", "")
-    codes = {"float32": FTC_F32, "bfloat16": FTC_BF16, "float16": FTC_F16}
-    if name not in codes:
-        raise ValueError(f"float32, bfloat16 or float16 wanted, got {name}")
-    return codes[name]
+    """FTC_* code of the floating types the training operators take (torch's types are added to the names as they are met)."""
+    code = _FLOAT_CODES.get(dt)
+    if code is None:
+        code = _FLOAT_CODES.get(str(dt).replace("torch.", ""))
+        if code is None:
+            raise ValueError(f"float32, bfloat16 or float16 wanted, got {dt}")
+        _FLOAT_CODES[dt] = code
+    return code
 
 
 def make_norm_desc(H, dtype, wdtype=None, P=1, k=None, eps=1e-5) -> ftc_norm_t:
