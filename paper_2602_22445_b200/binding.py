@@ -193,9 +193,27 @@ def _host_ptr(a):
     return a.data_ptr()
 
 
+_raw_stream = None
+
+
+def _find_raw_stream():
+    """How to ask torch for the current stream's handle: its own short way (a tenth of the public call's microseconds) where this
+    version has it."""
+    torch = _torch()
+    try:
+        device, stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    except AttributeError:
+        return lambda: torch.cuda.current_stream().cuda_stream
+    torch.cuda.current_stream()                       # torch's CUDA state exists from here on
+    return lambda: stream(device())
+
+
 def _stream(stream):
+    global _raw_stream
     if stream is None:
-        return _torch().cuda.current_stream().cuda_stream
+        if _raw_stream is None:
+            _raw_stream = _find_raw_stream()
+        return _raw_stream()
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 

@@ -1,11 +1,12 @@
-// Layer norm forward and backward, with the weight gradients of each process of a data-parallel job.
+// Layer norm forward and backward, with the weight gradients of each process of a data-parallel job: choice of kernels, and the
+// kernels for rows that do not fit the registers of a thread block (the others: ftc_norm_impl.cuh).
 //
-// A thread block walks rows; the sums over a row are taken by the whole block. The weight gradients are sums over rows: block
-// b walks the rows [b*R, (b+1)*R) in order and keeps one partial sum per column, which it leaves in the workspace whenever
-// the row's process changes and at its end. Block b and process p share slot b + p: going on by one row either the block or
-// the process grows, so no two (block, process) pairs that have rows in common meet in one slot, and blocks + P slots are enough
-// however the rows are divided. A second kernel adds the slots of each process in ascending order and lays the sums out as messages.
-#include "ftc_train.cuh"
+// Weight gradients are sums over rows: a group of threads walks the rows [b*R, (b+1)*R) in order and keeps one partial sum per column,
+// which it leaves in the workspace whenever the row's process changes and at its end. Group b and process p share slot b + p: going on
+// by one row either the group or the process grows, so no two (group, process) pairs that have rows in common meet in one slot, and
+// groups + P slots are enough however the rows are divided. A second kernel adds the slots of each process in ascending order and lays
+// the sums out as messages.
+#include "ftc_norm_impl.cuh"
 
 namespace ftc {
 
@@ -21,8 +22,9 @@ __device__ __forceinline__ float block_sum(float v, float* scratch) {
     return s;
 }
 
+// A block walks a row three times; rows come back from the caches.
 template <typename T, typename W>
-__global__ void __launch_bounds__(kThreads) norm_forward_kernel(NormArgs a) {
+__global__ void __launch_bounds__(kThreads) norm_forward_long_kernel(NormArgs a) {
     __shared__ float scratch[kThreads / 32];
     const W* gamma = static_cast<const W*>(a.gamma);
     const W* beta = static_cast<const W*>(a.beta);
@@ -44,48 +46,21 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(NormArgs a) {
     }
 }
 
-// First row of process p, at most `rows`.
-__device__ __forceinline__ uint64_t first_row(const NormArgs& a, uint64_t p) {
-    if (!a.splits) return p * a.rows / a.P;
-    const uint64_t s = a.splits[p];
-    return s < a.rows ? s : a.rows;
-}
-
-// The process that holds row r: the first one that ends behind it (P if none does).
-__device__ __forceinline__ uint32_t holder(const NormArgs& a, uint64_t r) {
-    uint32_t lo = 0, hi = a.P;
-    while (lo < hi) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (first_row(a, (uint64_t)mid + 1) > r) hi = mid; else lo = mid + 1;
-    }
-    return lo;
-}
-
+// dx alone.
 template <typename T, typename W>
-__global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a) {
+__global__ void __launch_bounds__(kThreads) norm_backward_long_kernel(NormArgs a) {
     __shared__ float scratch[kThreads / 32];
     const W* gamma = static_cast<const W*>(a.gamma);
-    const uint64_t r0 = blockIdx.x * a.rows_per_block, r1 = r0 + a.rows_per_block < a.rows ? r0 + a.rows_per_block : a.rows;
-    uint32_t p = a.slots ? holder(a, r0) : 0;
-    uint64_t end = a.slots && p < a.P ? first_row(a, (uint64_t)p + 1) : 0;
-    bool fresh = true;
-    for (uint64_t r = r0; r < r1; ++r) {
-        while (p < a.P && a.slots && r >= end) { ++p; fresh = true; end = p < a.P ? first_row(a, (uint64_t)p + 1) : 0; }
-        const bool counts = a.slots && p < a.P && r >= first_row(a, p);
+    for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const T* x = static_cast<const T*>(a.x) + r * a.x_stride;
         const T* dy = static_cast<const T*>(a.dy) + r * a.dy_stride;
         T* dx = static_cast<T*>(a.dx) + r * a.dx_stride;
-        float* dg = a.slots + ((uint64_t)blockIdx.x + p) * 2 * a.H;
-        float* db = dg + a.H;
         const float mean = a.mean[r], rstd = a.rstd[r];
         float s1 = 0.f, s2 = 0.f;
         for (uint32_t h = threadIdx.x; h < a.H; h += kThreads) {
-            const float g = to_f32(dy[h]), xh = (to_f32(x[h]) - mean) * rstd, u = g * (gamma ? to_f32(gamma[h]) : 1.f);
+            const float xh = (to_f32(x[h]) - mean) * rstd, u = to_f32(dy[h]) * (gamma ? to_f32(gamma[h]) : 1.f);
             s1 += u; s2 = fmaf(u, xh, s2);
-            if (counts) { dg[h] = fresh ? g * xh : dg[h] + g * xh; db[h] = fresh ? g : db[h] + g; }
         }
-        if (counts) fresh = false;
-        if (!a.dx) continue;
         const float c1 = block_sum(s1, scratch) / a.H, c2 = block_sum(s2, scratch) / a.H;
         for (uint32_t h = threadIdx.x; h < a.H; h += kThreads) {
             const float xh = (to_f32(x[h]) - mean) * rstd, u = to_f32(dy[h]) * (gamma ? to_f32(gamma[h]) : 1.f);
@@ -94,56 +69,158 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormArgs a) {
     }
 }
 
-// dgamma[s][p][e], dbeta[s][p][e] from the slots: a thread for each element.
-__global__ void __launch_bounds__(kThreads) norm_messages_kernel(NormArgs a) {
-    const uint64_t S = (a.H + a.k - 1) / a.k, n = S * a.P * a.k;
-    for (uint64_t i = blockIdx.x * (uint64_t)kThreads + threadIdx.x; i < n; i += (uint64_t)gridDim.x * kThreads) {
-        const uint64_t e = i % a.k, p = i / a.k % a.P, h = i / a.k / a.P * a.k + e;
-        float g = 0.f, b = 0.f;
-        const uint64_t lo = first_row(a, p), hi = first_row(a, p + 1);
-        if (h < a.H && lo < hi)
-            for (uint64_t blk = lo / a.rows_per_block; blk <= (hi - 1) / a.rows_per_block; ++blk) {
-                g += a.slots[(blk + p) * 2 * a.H + h];
-                b += a.slots[(blk + p) * 2 * a.H + a.H + h];
+// The weight gradients alone: a thread owns N neighbouring columns and walks its group's rows, four rows' loads out at once. No
+// sum over a row is needed.
+template <typename T, int VB>
+__global__ void __launch_bounds__(kThreads) norm_columns_kernel(NormArgs a) {
+    constexpr int N = VB / (int)sizeof(T), AHEAD = 4;
+    using V = Pack<T, VB>;
+    const uint32_t c = (blockIdx.x * kThreads + threadIdx.x) * N;
+    if (c >= a.H) return;                                            // N divides H
+    RowWalk walk(a, blockIdx.y);
+    float dg[N] = {}, db[N] = {};
+    for (uint64_t r = walk.r0; r < walk.r1; r += AHEAD) {
+        V x[AHEAD], dy[AHEAD];
+        float mean[AHEAD], rstd[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (r + i < walk.r1) {
+                x[i].load(static_cast<const T*>(a.x) + (r + i) * a.x_stride + c);
+                dy[i].load(static_cast<const T*>(a.dy) + (r + i) * a.dy_stride + c);
+                mean[i] = a.mean[r + i]; rstd[i] = a.rstd[r + i];
             }
-        if (a.dgamma) a.dgamma[i] = g;
-        if (a.dbeta) a.dbeta[i] = b;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (r + i < walk.r1) {
+                if (walk.leaves(r + i)) {
+                    if (walk.any) store_slot<N>(a, walk.slot(), c, dg, db);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) dg[j] = db[j] = 0.f;
+                    walk.go_to(r + i);
+                }
+                if (walk.counts(r + i)) {
+                    walk.any = true;
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        const float g = dy[i].get(j);
+                        dg[j] = fmaf(g, (x[i].get(j) - mean[i]) * rstd[i], dg[j]);
+                        db[j] += g;
+                    }
+                }
+            }
     }
+    if (walk.any) store_slot<N>(a, walk.slot(), c, dg, db);
 }
 
-template <typename F> static cudaError_t by_type(uint32_t dtype, uint32_t wdtype, F f) {
-    if (dtype == FTC_F32) f(float(), float());
-    else if (dtype == FTC_BF16) { if (wdtype == FTC_F32) f(__nv_bfloat16(), float()); else f(__nv_bfloat16(), __nv_bfloat16()); }
-    else { if (wdtype == FTC_F32) f(__half(), float()); else f(__half(), __half()); }
+// dgamma[s][p][e], dbeta[s][p][e] from the slots: a warp adds the slots of one process for 32 columns (Q = 1), or the 8 warps of a block
+// take every eighth slot each and their sums are added in order (Q = 8, for processes with many slots).
+template <int Q>
+__global__ void __launch_bounds__(256) norm_messages_kernel(NormArgs a, uint32_t tiles) {
+    __shared__ float part[2][8][32];
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint64_t item = Q == 8 ? blockIdx.x : blockIdx.x * 8ull + warp, p = item / tiles;
+    const uint32_t h = (uint32_t)(item % tiles) * 32 + lane;
+    float g = 0.f, b = 0.f;
+    if (p < a.P && h < a.H) {
+        const uint64_t lo = first_row(a, p), hi = first_row(a, p + 1);
+        if (lo < hi) {
+            const uint64_t last = (hi - 1) / a.rows_per_group;
+#pragma unroll 4
+            for (uint64_t grp = lo / a.rows_per_group + (Q == 8 ? warp : 0); grp <= last; grp += Q) {
+                const float* slot = a.slots + (grp + p) * 2 * a.H + h;
+                g += slot[0];
+                b += slot[a.H];
+            }
+        }
+    }
+    if (Q == 8) {
+        part[0][warp][lane] = g; part[1][warp][lane] = b;
+        __syncthreads();
+        if (warp) return;
+        g = b = 0.f;
+        for (int i = 0; i < 8; ++i) { g += part[0][i][lane]; b += part[1][i][lane]; }
+    }
+    const uint32_t S = (a.H + a.k - 1) / a.k, s = h / a.k;
+    if (p >= a.P || s >= S) return;                                  // h beyond H: the last message's fill, zeros
+    const uint64_t o = ((uint64_t)s * a.P + p) * a.k + h % a.k;
+    if (a.dgamma) a.dgamma[o] = g;
+    if (a.dbeta) a.dbeta[o] = b;
+}
+
+static bool on(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+// Bytes of the widest load that all rows begin on and that divides a row: 16, or 4 or 2 (the element) where that does not fit.
+static uint32_t row_vector(const NormArgs& a) {
+    const uint32_t e = a.dtype == FTC_F32 ? 4 : 2;
+    const uint64_t strides = (a.x_stride | a.y_stride | a.dy_stride | a.dx_stride | a.H) * e;
+    const auto fits = [&](uint32_t v) { return strides % v == 0 && on(a.x, v) && on(a.y, v) && on(a.dy, v) && on(a.dx, v); };
+    if (fits(16) && on(a.gamma, 16) && on(a.beta, 16)) return 16;
+    return fits(4) && on(a.gamma, 8) && on(a.beta, 8) ? 4 : e;
+}
+
+template <typename T, typename W> static cudaError_t forward(const NormArgs& a, int sms, cudaStream_t st) {
+    const cudaError_t e = forward_rows<T, W>(a, row_vector(a), sms, st);
+    if (e != cudaErrorNotSupported) return e;
+    const uint64_t cap = (uint64_t)sms * 8;
+    norm_forward_long_kernel<T, W><<<(uint32_t)(a.rows < cap ? a.rows : cap), kThreads, 0, st>>>(a);
     return cudaGetLastError();
 }
 
-cudaError_t launch_norm_forward(const NormArgs& a, int sm_count, cudaStream_t st) {
-    const uint64_t cap = (uint64_t)sm_count * 8;
-    const uint32_t grid = (uint32_t)(a.rows < cap ? a.rows : cap);
-    return by_type(a.dtype, a.wdtype, [&](auto t, auto w) { norm_forward_kernel<decltype(t), decltype(w)><<<grid, kThreads, 0, st>>>(a); });
+cudaError_t launch_norm_forward(const NormArgs& a, int sms, cudaStream_t st) {
+    if (a.dtype == FTC_F32) return forward<float, float>(a, sms, st);
+    if (a.dtype == FTC_BF16) return a.wdtype == FTC_F32 ? forward<__nv_bfloat16, float>(a, sms, st) : forward<__nv_bfloat16, __nv_bfloat16>(a, sms, st);
+    return a.wdtype == FTC_F32 ? forward<__half, float>(a, sms, st) : forward<__half, __half>(a, sms, st);
 }
 
-// As many blocks as the GPU holds, fewer where their partial sums would take up more than 2 GiB.
-uint32_t norm_backward_blocks(uint32_t H, uint64_t rows, int sm_count) {
-    uint64_t b = (uint64_t)sm_count * 4;
-    const uint64_t room = (1ull << 28) / H;
-    if (b > room) b = room ? room : 1;
-    if (b > rows) b = rows;
-    if (b == 0) return 0;
-    const uint64_t each = (rows + b - 1) / b;
+// Groups that share the rows in the backward pass: as many as the GPU runs at once, at least 16 rows each where there are rows enough
+// (each group writes and the second kernel reads 8 bytes a column: 16 rows keep that under a sixth of the rows' own 96 bytes and more),
+// fewer where their partial sums would take up more than 2 GiB.
+uint32_t norm_backward_groups(uint32_t H, uint64_t rows, int sms) {
+    const uint64_t per_sm = H <= 256 ? 16 : H <= 1024 ? 8 : H <= 2048 ? 4 : 2;
+    uint64_t n = (uint64_t)sms * per_sm;
+    const uint64_t few = rows / 16 > (uint64_t)sms ? rows / 16 : (uint64_t)sms, room = (1ull << 28) / H;
+    if (n > few) n = few;
+    if (n > room) n = room ? room : 1;
+    if (n > rows) n = rows;
+    if (n == 0) return 0;
+    const uint64_t each = (rows + n - 1) / n;
     return (uint32_t)((rows + each - 1) / each);
 }
 
-cudaError_t launch_norm_backward(NormArgs a, cudaStream_t st) {
-    cudaError_t e;
-    if (a.blocks) {
-        e = by_type(a.dtype, a.wdtype, [&](auto t, auto w) { norm_backward_kernel<decltype(t), decltype(w)><<<a.blocks, kThreads, 0, st>>>(a); });
+template <typename T> static cudaError_t columns(const NormArgs& a, cudaStream_t st) {
+    constexpr int e = sizeof(T);
+    const uint32_t v = row_vector(a), threads = (a.H * e / v + kThreads - 1) / kThreads;
+    const dim3 grid(threads, a.groups);
+    if (v == 16) norm_columns_kernel<T, 16><<<grid, kThreads, 0, st>>>(a);
+    else if (v == 4) norm_columns_kernel<T, 4><<<grid, kThreads, 0, st>>>(a);
+    else norm_columns_kernel<T, e><<<grid, kThreads, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+template <typename T, typename W> static cudaError_t backward(const NormArgs& a, int sms, cudaStream_t st) {
+    const cudaError_t e = backward_rows<T, W>(a, row_vector(a), st);
+    if (e != cudaErrorNotSupported) return e;
+    if (a.slots) { const cudaError_t c = columns<T>(a, st); if (c != cudaSuccess || !a.dx) return c; }
+    const uint64_t cap = (uint64_t)sms * 8;
+    norm_backward_long_kernel<T, W><<<(uint32_t)(a.rows < cap ? a.rows : cap), kThreads, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_norm_backward(const NormArgs& a, int sms, cudaStream_t st) {
+    if (a.rows) {
+        cudaError_t e;
+        if (a.dtype == FTC_F32) e = backward<float, float>(a, sms, st);
+        else if (a.dtype == FTC_BF16) e = a.wdtype == FTC_F32 ? backward<__nv_bfloat16, float>(a, sms, st) : backward<__nv_bfloat16, __nv_bfloat16>(a, sms, st);
+        else e = a.wdtype == FTC_F32 ? backward<__half, float>(a, sms, st) : backward<__half, __half>(a, sms, st);
         if (e != cudaSuccess) return e;
     }
     if (!a.slots) return cudaSuccess;
-    const uint64_t n = (uint64_t)((a.H + a.k - 1) / a.k) * a.P * a.k, want = (n + kThreads - 1) / kThreads;
-    norm_messages_kernel<<<(uint32_t)(want < 65536 ? want : 65536), kThreads, 0, st>>>(a);
+    const uint32_t S = (a.H + a.k - 1) / a.k;
+    const uint64_t filled = (uint64_t)S * a.k;                       // columns with the last message's fill
+    const uint32_t tiles = (uint32_t)((filled + 31) / 32);
+    const uint64_t items = (uint64_t)tiles * a.P;
+    if (a.groups / a.P >= 16) norm_messages_kernel<8><<<(uint32_t)items, 256, 0, st>>>(a, tiles);
+    else norm_messages_kernel<1><<<(uint32_t)((items + 7) / 8), 256, 0, st>>>(a, tiles);
     return cudaGetLastError();
 }
 

@@ -49,14 +49,14 @@ struct NormArgs {
     const float *mean, *rstd;
     const uint64_t* splits;
     float *dgamma, *dbeta, *slots;
-    uint64_t rows, x_stride, y_stride, dy_stride, dx_stride, rows_per_block;
-    uint32_t H, P, k, dtype, wdtype, blocks;
+    uint64_t rows, x_stride, y_stride, dy_stride, dx_stride, rows_per_group;
+    uint32_t H, P, k, dtype, wdtype, groups;
     float eps;
 };
 cudaError_t launch_norm_forward(const NormArgs& a, int sm_count, cudaStream_t st);
-cudaError_t launch_norm_backward(NormArgs a, cudaStream_t st);
-// Blocks that the backward pass over the weights takes; each leaves its partial sums in the workspace.
-uint32_t norm_backward_blocks(uint32_t H, uint64_t rows, int sm_count);
+cudaError_t launch_norm_backward(const NormArgs& a, int sm_count, cudaStream_t st);
+// Groups that share the rows in the backward pass; each leaves its partial sums of the weight gradients in the workspace.
+uint32_t norm_backward_groups(uint32_t H, uint64_t rows, int sm_count);
 
 struct AdamArgs {
     const void* table; uint32_t n_params; uint64_t n_blocks;

@@ -26,7 +26,7 @@ int check_norm(const ftc_norm_t* d, uint64_t rows) {
 }
 
 size_t norm_workspace(const ftc_norm_t* d, uint64_t rows, int sms) {
-    return ((size_t)norm_backward_blocks(d->H, rows, sms) + d->P) * d->H * 2 * sizeof(float);
+    return ((size_t)norm_backward_groups(d->H, rows, sms) + d->P) * d->H * 2 * sizeof(float);
 }
 
 const TableHead* head_of(const void* h_table) {
@@ -102,9 +102,9 @@ int ftc_layernorm_backward(const ftc_norm_t* desc, uint64_t rows, const void* d_
     a.dgamma = d_dgamma; a.dbeta = d_dbeta; a.slots = weights ? static_cast<float*>(d_workspace) : nullptr;
     a.rows = rows; a.x_stride = x_stride; a.dy_stride = dy_stride; a.dx_stride = dx_stride;
     a.H = desc->H; a.P = desc->P; a.k = desc->k; a.dtype = desc->dtype; a.wdtype = desc->wdtype; a.eps = desc->eps;
-    a.blocks = norm_backward_blocks(desc->H, rows, sms);
-    a.rows_per_block = a.blocks ? (rows + a.blocks - 1) / a.blocks : 0;
-    return status(launch_norm_backward(a, static_cast<cudaStream_t>(cuda_stream)));
+    a.groups = norm_backward_groups(desc->H, rows, sms);
+    a.rows_per_group = a.groups ? (rows + a.groups - 1) / a.groups : 0;
+    return status(launch_norm_backward(a, sms, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 size_t ftc_param_table_bytes(const ftc_param_t* h_params, uint32_t n_params) {
