@@ -176,7 +176,7 @@ cudaError_t launch_norm_forward(const NormArgs& a, int sms, cudaStream_t st) {
 // (each group writes and the second kernel reads 8 bytes a column: 16 rows keep that under a sixth of the rows' own 96 bytes and more),
 // fewer where their partial sums would take up more than 2 GiB.
 uint32_t norm_backward_groups(uint32_t H, uint64_t rows, int sms) {
-    const uint64_t per_sm = H <= 256 ? 16 : H <= 1024 ? 8 : H <= 2048 ? 4 : 2;
+    const uint32_t g = group_threads(H), per_sm = g < 640 ? 640 / g : 1;
     uint64_t n = (uint64_t)sms * per_sm;
     const uint64_t few = rows / 16 > (uint64_t)sms ? rows / 16 : (uint64_t)sms, room = (1ull << 28) / H;
     if (n > few) n = few;

@@ -1,9 +1,14 @@
 // Layer norm on rows that fit the registers of a thread block.
 //
-// A group of G threads (a warp, or a block of up to 1024) holds a row: vector i of thread t is vector i*G + t of the row, so every
-// load and store of a warp is one contiguous run. Statistics are taken in two steps from the registers (mean, then squared distances),
-// which no common offset of the row can spoil. A group walks many rows with gamma, beta and the column sums in registers, and has the next
-// row's loads out while it works on the present one.
+// A group of G threads (a warp, or a block of up to 512) holds a row, 16 elements a thread: vector i of thread t is vector i*G + t of
+// the row, so every load and store of a warp is one contiguous run. Statistics are taken in two steps from the registers (mean, then
+// squared distances), which no common offset of the row can spoil. A group walks many rows with gamma, beta and the column sums in registers.
+//
+// Rows come in through a ring of D rows in shared memory, filled by asynchronous copies (16 or 4 bytes a thread) that run D - 1 rows
+// ahead: what an SM has under way no longer depends on registers. Each thread copies what it reads itself, so the ring needs no barrier. The
+// exception is 16-bit rows that begin between two 4-byte words (ODD: an odd H or stride): their words are copied whole, and a thread
+// shifts its pair of elements out of two neighbouring words, which takes one barrier a row. The word that reaches over the
+// first row's beginning or the last row's end is put together from its one element.
 #pragma once
 #include "ftc_train.cuh"
 
@@ -119,68 +124,154 @@ template <int N> __device__ __forceinline__ void store_slot(const NormArgs& a, u
     }
 }
 
-// Sums over the group. With more than one warp a pair of values goes through shared memory; `turn` alternates between two places, so
-// that one barrier a call is enough (a place is written again only behind the barrier of the call in between).
-__device__ __forceinline__ float2 group_sum(float2 v, float2 (*scratch)[32], uint32_t& turn) {
+// Sums over the group. With more than one warp they go through shared memory; `turn` alternates between two places, so that one
+// barrier a call is enough (a place is written again only behind the barrier of the call in between). Places of warps that do not
+// exist hold zeros.
+constexpr int kMaxGroup = 512, kMaxWarps = kMaxGroup / 32;
+struct Scratch { float4 pair[2][kMaxWarps / 2]; };
+
+__device__ __forceinline__ void clear_scratch(Scratch& s) {
+    const uint32_t t = threadIdx.y * blockDim.x + threadIdx.x;
+    if (t < kMaxWarps) (&s.pair[0][0])[t] = make_float4(0.f, 0.f, 0.f, 0.f);
+    __syncthreads();
+}
+__device__ __forceinline__ float2 group_sum(float2 v, Scratch& scratch, uint32_t& turn) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) { v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o); v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o); }
     if (blockDim.x == 32) return v;
-    const uint32_t warps = blockDim.x / 32;
-    if ((threadIdx.x & 31) == 0) scratch[turn][threadIdx.x >> 5] = v;
+    float4* place = scratch.pair[turn];
+    if ((threadIdx.x & 31) == 0) reinterpret_cast<float2*>(place)[threadIdx.x >> 5] = v;
     __syncthreads();
-    float2 s = scratch[turn][0];
-    for (uint32_t i = 1; i < warps; ++i) { s.x += scratch[turn][i].x; s.y += scratch[turn][i].y; }
+    float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kMaxWarps / 2; ++i) { const float4 q = place[i]; s.x += q.x + q.z; s.y += q.y + q.w; }
     turn ^= 1u;
     return s;
 }
-__device__ __forceinline__ float group_sum(float v, float2 (*scratch)[32], uint32_t& turn) {
+__device__ __forceinline__ float group_sum(float v, Scratch& scratch, uint32_t& turn) {
     v = warp_sum(v);
     if (blockDim.x == 32) return v;
-    const uint32_t warps = blockDim.x / 32;
-    if ((threadIdx.x & 31) == 0) scratch[turn][threadIdx.x >> 5].x = v;
+    float4* place = scratch.pair[turn];
+    if ((threadIdx.x & 31) == 0) reinterpret_cast<float*>(place)[threadIdx.x >> 5] = v;
     __syncthreads();
-    float s = scratch[turn][0].x;
-    for (uint32_t i = 1; i < warps; ++i) s += scratch[turn][i].x;
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kMaxWarps / 4; ++i) { const float4 q = place[i]; s += (q.x + q.y) + (q.z + q.w); }
     turn ^= 1u;
     return s;
 }
+__device__ __forceinline__ void group_barrier() { if (blockDim.x == 32) __syncwarp(); else __syncthreads(); }
 
-// blockDim = (G, groups in the block). HOLD: gamma and beta stay in registers and the next row is loaded ahead.
-template <typename T, typename W, int VB, int NV, bool HOLD, int MAXT>
-__global__ void __launch_bounds__(MAXT) norm_forward_kernel(NormArgs a) {
+template <int VB> __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+    if constexpr (VB == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" :: "r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_end_batch() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(PENDING) : "memory"); }
+
+// The rows of one array in the ring: NV vectors of VB bytes for each thread, n elements in a row, `rows` rows.
+template <typename T, int VB, int NV, bool ODD> struct RingRows {
+    static constexpr int N = VB / (int)sizeof(T);
+    const T* base;
+    uint64_t stride, rows;
+    uint32_t n, vecs;
+    // Bytes that one row takes up in the ring.
+    static __host__ __device__ uint32_t bytes(uint32_t G) { return NV * G * VB + (ODD ? 16 : 0); }
+    __device__ __forceinline__ uint32_t odd(uint64_t r) const { return ODD ? (uint32_t)(reinterpret_cast<uintptr_t>(base + r * stride) >> 1) & 1u : 0u; }
+    __device__ __forceinline__ void fetch(char* place, uint64_t r) const {
+        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(place);
+        if constexpr (!ODD) {
+            const T* p = base + r * stride;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const uint32_t q = i * blockDim.x + threadIdx.x;
+                if (q < vecs) copy_async<VB>(dst + q * VB, p + q * N);
+            }
+        } else {
+            const uint32_t s = odd(r), words = (s + n + 1) / 2;
+            const T* p = base + r * stride - s;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const uint32_t q = i * blockDim.x + threadIdx.x;
+                if (q >= words) continue;
+                if (q == 0 && s && r == 0) reinterpret_cast<uint32_t*>(place)[0] = (uint32_t)reinterpret_cast<const uint16_t*>(p)[1] << 16;
+                else if (q == words - 1 && ((s + n) & 1u) && r + 1 == rows) reinterpret_cast<uint32_t*>(place)[q] = reinterpret_cast<const uint16_t*>(p)[2 * q];
+                else copy_async<4>(dst + q * 4, p + q * 2);
+            }
+        }
+    }
+    // Vector i of this thread; zeros behind the row's end.
+    __device__ __forceinline__ void read(Pack<T, VB>& v, const char* place, int i, uint32_t s) const {
+        const uint32_t q = i * blockDim.x + threadIdx.x;
+        if (q >= vecs) { v.clear(); return; }
+        if constexpr (VB == 16) { const uint4 w = reinterpret_cast<const uint4*>(place)[q]; v.r[0] = w.x; v.r[1] = w.y; v.r[2] = w.z; v.r[3] = w.w; }
+        else if constexpr (!ODD) v.r[0] = reinterpret_cast<const uint32_t*>(place)[q];
+        else {
+            const uint32_t* w = reinterpret_cast<const uint32_t*>(place) + q;
+            v.r[0] = s ? __funnelshift_r(w[0], w[1], 16) : w[0];
+            if (2 * q + 1 >= n) v.r[0] &= 0xFFFFu;                   // an odd row's last element stands alone
+        }
+    }
+};
+
+// A vector of results to column c of a row (ODD: a pair that may begin between words, or be one element).
+template <typename T, int VB, bool ODD> __device__ __forceinline__ void store_vector(T* row, uint32_t c, uint32_t n, const float* v) {
+    if constexpr (!ODD) Pack<T, VB>::store(row + c, v);
+    else {
+        if (c + 1 < n && (reinterpret_cast<uintptr_t>(row) & 3u) == 0) { Pack<T, 4>::store(row + c, v); return; }
+        row[c] = from_f32<T>(v[0]);
+        if (c + 1 < n) row[c + 1] = from_f32<T>(v[1]);
+    }
+}
+
+// Weights of a thread's vector; ODD: of a pair of which the second may not exist.
+template <typename W, int N, bool ODD> __device__ __forceinline__ void vector_weights(float* v, const W* w, uint32_t c, uint32_t n, float other) {
+    if constexpr (!ODD) load_weights<W, N>(v, w, c, other);
+    else { v[0] = w ? to_f32(w[c]) : other; v[1] = w && c + 1 < n ? to_f32(w[c + 1]) : other; }
+}
+
+// blockDim = (G, groups in the block).
+template <typename T, typename W, int VB, int NV, bool ODD, int D>
+__global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
     using V = Pack<T, VB>;
+    using Rows = RingRows<T, VB, NV, ODD>;
     constexpr int N = V::N;
-    __shared__ float2 scratch[2][32];
+    extern __shared__ uint4 ring_memory[];
+    __shared__ Scratch scratch;
     uint32_t turn = 0;
-    const uint32_t G = blockDim.x, vecs = a.H / N;
-    const W* gamma = static_cast<const W*>(a.gamma);
-    const W* beta = static_cast<const W*>(a.beta);
+    const uint32_t G = blockDim.x, vecs = (a.H + N - 1) / N, bytes = Rows::bytes(G);
+    char* ring = reinterpret_cast<char*>(ring_memory) + threadIdx.y * D * bytes;
+    const Rows in{static_cast<const T*>(a.x), a.x_stride, a.rows, a.H, vecs};
     const float inv = 1.f / (float)a.H;
     const uint64_t step = (uint64_t)gridDim.x * blockDim.y;
     uint64_t r = (uint64_t)blockIdx.x * blockDim.y + threadIdx.y;
-    V next[NV];
-    float g[HOLD ? NV * N : N], b[HOLD ? NV * N : N];
-    const auto fetch = [&](uint64_t row) {
-        const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t q = i * G + threadIdx.x;
-            if (q < vecs) next[i].load(x + q * N); else next[i].clear();
-        }
-    };
-    if (r < a.rows) fetch(r);
-    if (HOLD) {
+    for (int d = 0; d < D - 1; ++d) {
+        if (r + d * step < a.rows) in.fetch(ring + d * bytes, r + d * step);
+        copies_end_batch();
+    }
+    float g[NV * N], b[NV * N];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t q = i * G + threadIdx.x;
-            if (q < vecs) { load_weights<W, N>(g + i * N, gamma, q * N, 1.f); load_weights<W, N>(b + i * N, beta, q * N, 0.f); }
+    for (int i = 0; i < NV; ++i) {
+        const uint32_t q = i * G + threadIdx.x;
+        if (q < vecs) {
+            vector_weights<W, N, ODD>(g + i * N, static_cast<const W*>(a.gamma), q * N, a.H, 1.f);
+            vector_weights<W, N, ODD>(b + i * N, static_cast<const W*>(a.beta), q * N, a.H, 0.f);
         }
     }
+    clear_scratch(scratch);
+    uint32_t stage = 0;
     for (; r < a.rows; r += step) {
+        copies_wait<D - 2>();
+        if (ODD) group_barrier();
         V x[NV];
+        const uint32_t s0 = in.odd(r);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) x[i] = next[i];
-        if (HOLD && r + step < a.rows) fetch(r + step);
+        for (int i = 0; i < NV; ++i) in.read(x[i], ring + stage * bytes, i, s0);
+        const uint32_t last = stage == 0 ? D - 1 : stage - 1;
+        if (r + (D - 1) * step < a.rows) in.fetch(ring + last * bytes, r + (D - 1) * step);
+        copies_end_batch();
+        stage = stage + 1 == D ? 0 : stage + 1;
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
@@ -190,9 +281,11 @@ __global__ void __launch_bounds__(MAXT) norm_forward_kernel(NormArgs a) {
         s = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (i * G + threadIdx.x < vecs) {
 #pragma unroll
-                for (int j = 0; j < N; ++j) { const float d = x[i].get(j) - mean; s = fmaf(d, d, s); }
+            for (int j = 0; j < N; ++j) {
+                const float d = x[i].get(j) - mean;
+                const uint32_t c = (i * G + threadIdx.x) * N + (ODD ? j : 0);
+                if (c < a.H) s = fmaf(d, d, s);
             }
         const float rstd = 1.f / sqrtf(group_sum(s, scratch, turn) * inv + a.eps);
         T* y = static_cast<T*>(a.y) + r * a.y_stride;
@@ -200,67 +293,76 @@ __global__ void __launch_bounds__(MAXT) norm_forward_kernel(NormArgs a) {
         for (int i = 0; i < NV; ++i) {
             const uint32_t q = i * G + threadIdx.x;
             if (q < vecs) {
-                if (!HOLD) { load_weights<W, N>(g, gamma, q * N, 1.f); load_weights<W, N>(b, beta, q * N, 0.f); }
                 float o[N];
 #pragma unroll
-                for (int j = 0; j < N; ++j) o[j] = fmaf((x[i].get(j) - mean) * rstd, g[HOLD ? i * N + j : j], b[HOLD ? i * N + j : j]);
-                V::store(y + q * N, o);
+                for (int j = 0; j < N; ++j) o[j] = fmaf((x[i].get(j) - mean) * rstd, g[i * N + j], b[i * N + j]);
+                store_vector<T, VB, ODD>(y, q * N, a.H, o);
             }
         }
         if (threadIdx.x == 0) {
             if (a.mean_out) a.mean_out[r] = mean;
             if (a.rstd_out) a.rstd_out[r] = rstd;
         }
-        if (!HOLD && r + step < a.rows) fetch(r + step);
     }
 }
 
-// blockDim = (G, groups in the block); a group of threads walks the rows of one RowWalk. AHEAD: the next row is loaded ahead.
-template <typename T, typename W, int VB, int NV, bool AHEAD, int MAXT>
-__global__ void __launch_bounds__(MAXT) norm_backward_kernel(NormArgs a) {
+// blockDim = (G, groups in the block); a group of threads walks the rows of one RowWalk.
+template <typename T, typename W, int VB, int NV, bool ODD, int D>
+__global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
     using V = Pack<T, VB>;
+    using Rows = RingRows<T, VB, NV, ODD>;
     constexpr int N = V::N, E = NV * N;
-    __shared__ float2 scratch[2][32];
+    extern __shared__ uint4 ring_memory[];
+    __shared__ Scratch scratch;
     uint32_t turn = 0;
-    const uint32_t G = blockDim.x, vecs = a.H / N, group = blockIdx.x * blockDim.y + threadIdx.y;
-    if (group >= a.groups) return;                                   // whole groups; a group of several warps is a whole block
+    const uint32_t G = blockDim.x, vecs = (a.H + N - 1) / N, bytes = Rows::bytes(G), group = blockIdx.x * blockDim.y + threadIdx.y;
+    char* ring = reinterpret_cast<char*>(ring_memory) + threadIdx.y * D * 2 * bytes;
+    const Rows xs{static_cast<const T*>(a.x), a.x_stride, a.rows, a.H, vecs}, ys{static_cast<const T*>(a.dy), a.dy_stride, a.rows, a.H, vecs};
+    clear_scratch(scratch);
+    if (group >= a.groups) return;                                   // whole warps, and in blocks of one group nobody
     RowWalk walk(a, group);
     const float inv = 1.f / (float)a.H;
-    V nx[NV], ny[NV];
-    float nmean = 0.f, nrstd = 0.f;
-    const auto fetch = [&](uint64_t row) {
-        const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
-        const T* dy = static_cast<const T*>(a.dy) + row * a.dy_stride;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t q = i * G + threadIdx.x;
-            if (q < vecs) { nx[i].load(x + q * N); ny[i].load(dy + q * N); }
-            else { nx[i].clear(); ny[i].clear(); }                   // dy = 0: adds nothing to any sum
-        }
-        nmean = a.mean[row]; nrstd = a.rstd[row];
-    };
+    for (int d = 0; d < D - 1; ++d) {
+        if (walk.r0 + d < walk.r1) { xs.fetch(ring + 2 * d * bytes, walk.r0 + d); ys.fetch(ring + (2 * d + 1) * bytes, walk.r0 + d); }
+        copies_end_batch();
+    }
     float g[E], dg[E], db[E];
-    if (walk.r0 < walk.r1) fetch(walk.r0);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const uint32_t q = i * G + threadIdx.x;
 #pragma unroll
         for (int j = 0; j < N; ++j) g[i * N + j] = dg[i * N + j] = db[i * N + j] = 0.f;
-        if (q < vecs) load_weights<W, N>(g + i * N, static_cast<const W*>(a.gamma), q * N, 1.f);
+        if (q < vecs) vector_weights<W, N, ODD>(g + i * N, static_cast<const W*>(a.gamma), q * N, a.H, 1.f);
     }
     const auto leave = [&]() {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const uint32_t q = i * G + threadIdx.x;
-            if (q < vecs) store_slot<N>(a, walk.slot(), q * N, dg + i * N, db + i * N);
+            if (q >= vecs) continue;
+            if constexpr (!ODD) store_slot<N>(a, walk.slot(), q * N, dg + i * N, db + i * N);
+            else {
+                store_slot<1>(a, walk.slot(), q * 2, dg + i * N, db + i * N);
+                if (q * 2 + 1 < a.H) store_slot<1>(a, walk.slot(), q * 2 + 1, dg + i * N + 1, db + i * N + 1);
+            }
         }
     };
+    float nmean = 0.f, nrstd = 0.f;
+    if (walk.r0 < walk.r1) { nmean = a.mean[walk.r0]; nrstd = a.rstd[walk.r0]; }
+    uint32_t stage = 0;
     for (uint64_t r = walk.r0; r < walk.r1; ++r) {
+        copies_wait<D - 2>();
+        if (ODD) group_barrier();
         V x[NV], dy[NV];
-        const float mean = nmean, rstd = nrstd;
+        const uint32_t sx = xs.odd(r), sy = ys.odd(r);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) { x[i] = nx[i]; dy[i] = ny[i]; }
-        if (AHEAD && r + 1 < walk.r1) fetch(r + 1);
+        for (int i = 0; i < NV; ++i) { xs.read(x[i], ring + 2 * stage * bytes, i, sx); ys.read(dy[i], ring + (2 * stage + 1) * bytes, i, sy); }
+        const uint32_t last = stage == 0 ? D - 1 : stage - 1;
+        if (r + (D - 1) < walk.r1) { xs.fetch(ring + 2 * last * bytes, r + (D - 1)); ys.fetch(ring + (2 * last + 1) * bytes, r + (D - 1)); }
+        copies_end_batch();
+        stage = stage + 1 == D ? 0 : stage + 1;
+        const float mean = nmean, rstd = nrstd;
+        if (r + 1 < walk.r1) { nmean = a.mean[r + 1]; nrstd = a.rstd[r + 1]; }
         float2 s = make_float2(0.f, 0.f);
         if (a.slots && walk.leaves(r)) {
             if (walk.any) leave();
@@ -273,94 +375,80 @@ __global__ void __launch_bounds__(MAXT) norm_backward_kernel(NormArgs a) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
+            for (int j = 0; j < N; ++j) {                            // behind the row's end dy = 0 adds nothing
                 const float d = dy[i].get(j), xh = (x[i].get(j) - mean) * rstd, u = d * g[i * N + j];
                 s.x += u;
                 s.y = fmaf(u, xh, s.y);
                 if (counts) { dg[i * N + j] = fmaf(d, xh, dg[i * N + j]); db[i * N + j] += d; }
             }
-        if (a.dx) {
-            s = group_sum(s, scratch, turn);
-            const float c1 = s.x * inv, c2 = s.y * inv;
-            T* dx = static_cast<T*>(a.dx) + r * a.dx_stride;
+        if (!a.dx) continue;
+        s = group_sum(s, scratch, turn);
+        const float c1 = s.x * inv, c2 = s.y * inv;
+        T* dx = static_cast<T*>(a.dx) + r * a.dx_stride;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const uint32_t q = i * G + threadIdx.x;
-                if (q < vecs) {
-                    float o[N];
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t q = i * G + threadIdx.x;
+            if (q < vecs) {
+                float o[N];
 #pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const float xh = (x[i].get(j) - mean) * rstd;
-                        o[j] = rstd * (fmaf(dy[i].get(j), g[i * N + j], -c1) - xh * c2);
-                    }
-                    V::store(dx + q * N, o);
+                for (int j = 0; j < N; ++j) {
+                    const float xh = (x[i].get(j) - mean) * rstd;
+                    o[j] = rstd * (fmaf(dy[i].get(j), g[i * N + j], -c1) - xh * c2);
                 }
+                store_vector<T, VB, ODD>(dx, q * N, a.H, o);
             }
         }
-        if (!AHEAD && r + 1 < walk.r1) fetch(r + 1);
     }
     if (a.slots && walk.any) leave();
 }
 
-// Threads for a row of `vecs` vectors, NV each, and rows of a block of 128 threads where a warp is enough for one.
+// Threads that hold a row of H elements, 16 each, and rows of a block of 128 threads where a warp is enough for one.
+static inline uint32_t group_threads(uint32_t H) { return (H / 16 + 1 + 31) / 32 * 32; }
 static inline dim3 group_shape(uint32_t vecs, uint32_t nv) {
     const uint32_t g = ((vecs + nv - 1) / nv + 31) / 32 * 32;
     return dim3(g, g == 32 ? 4 : 1);
 }
 
-template <typename T, typename W, int VB, int NV, bool HOLD, int MAXT>
-static cudaError_t forward_run(const NormArgs& a, int sms, cudaStream_t st) {
-    const dim3 block = group_shape(a.H / (VB / (uint32_t)sizeof(T)), NV);
-    const uint64_t blocks = (a.rows + block.y - 1) / block.y, cap = (uint64_t)sms * (MAXT == 1024 ? 1024 : 768) / (block.x * block.y);
-    norm_forward_kernel<T, W, VB, NV, HOLD, MAXT><<<(uint32_t)(blocks < cap ? blocks : cap ? cap : 1), block, 0, st>>>(a);
+template <typename K> static cudaError_t allow_shared(K kernel, size_t bytes) {
+    return bytes <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+template <typename T, typename W, int VB, int NV, bool ODD, int D> static cudaError_t forward_run(const NormArgs& a, int sms, cudaStream_t st) {
+    constexpr uint32_t N = VB / (uint32_t)sizeof(T);
+    const dim3 block = group_shape((a.H + N - 1) / N + (ODD ? 1 : 0), NV);
+    const size_t smem = (size_t)block.y * D * RingRows<T, VB, NV, ODD>::bytes(block.x);
+    const cudaError_t e = allow_shared(norm_forward_kernel<T, W, VB, NV, ODD, D>, smem);
+    if (e != cudaSuccess) return e;
+    const uint64_t blocks = (a.rows + block.y - 1) / block.y, cap = (uint64_t)sms * (768 / (block.x * block.y) ? 768 / (block.x * block.y) : 1);
+    norm_forward_kernel<T, W, VB, NV, ODD, D><<<(uint32_t)(blocks < cap ? blocks : cap), block, smem, st>>>(a);
     return cudaGetLastError();
 }
 
 // cudaErrorNotSupported: the row does not fit.
 template <typename T, typename W> static cudaError_t forward_rows(const NormArgs& a, uint32_t v, int sms, cudaStream_t st) {
-    const uint32_t vecs = a.H * (uint32_t)sizeof(T) / v;
-    if (v == 16) {
-        constexpr int most = sizeof(T) == 2 ? 2 : 4;
-        if (vecs <= 256) return forward_run<T, W, 16, 1, true, 512>(a, sms, st);
-        if (vecs <= 512 * most) return forward_run<T, W, 16, most, true, 512>(a, sms, st);
-        if (vecs <= 8192) return forward_run<T, W, 16, 8, false, 1024>(a, sms, st);
-        return cudaErrorNotSupported;
-    }
-    constexpr int E = sizeof(T);
-    if constexpr (E == 2) if (v == 4) {
-        if (vecs <= 2048) return forward_run<T, W, 4, 4, true, 512>(a, sms, st);
-        if (vecs <= 16384) return forward_run<T, W, 4, 16, false, 1024>(a, sms, st);
-        return cudaErrorNotSupported;
-    }
-    if (vecs <= 2048) return forward_run<T, W, E, 4, true, 512>(a, sms, st);
-    if (vecs <= 16384) return forward_run<T, W, E, 16, false, 1024>(a, sms, st);
-    return cudaErrorNotSupported;
+    constexpr int E = sizeof(T), D = E == 2 ? 4 : 3;
+    if (a.H > 16 * kMaxGroup || (v == 2 && a.H > 16 * kMaxGroup - 2)) return cudaErrorNotSupported;
+    if (v == 16) return a.H <= 32 * 16 / E ? forward_run<T, W, 16, 1, false, D>(a, sms, st) : forward_run<T, W, 16, E, false, D>(a, sms, st);
+    if constexpr (E == 4) return forward_run<T, W, 4, 16, false, D>(a, sms, st);
+    else return v == 4 ? forward_run<T, W, 4, 8, false, D>(a, sms, st) : forward_run<T, W, 4, 8, true, D>(a, sms, st);
 }
 
-template <typename T, typename W, int VB, int NV>
-static cudaError_t backward_run(const NormArgs& a, cudaStream_t st) {
-    const dim3 block = group_shape(a.H / (VB / (uint32_t)sizeof(T)), NV);
-    norm_backward_kernel<T, W, VB, NV, NV * Pack<T, VB>::WORDS <= 8, 512><<<(a.groups + block.y - 1) / block.y, block, 0, st>>>(a);
+template <typename T, typename W, int VB, int NV, bool ODD, int D> static cudaError_t backward_run(const NormArgs& a, cudaStream_t st) {
+    constexpr uint32_t N = VB / (uint32_t)sizeof(T);
+    const dim3 block = group_shape((a.H + N - 1) / N + (ODD ? 1 : 0), NV);
+    const size_t smem = (size_t)block.y * D * 2 * RingRows<T, VB, NV, ODD>::bytes(block.x);
+    const cudaError_t e = allow_shared(norm_backward_kernel<T, W, VB, NV, ODD, D>, smem);
+    if (e != cudaSuccess) return e;
+    norm_backward_kernel<T, W, VB, NV, ODD, D><<<(a.groups + block.y - 1) / block.y, block, smem, st>>>(a);
     return cudaGetLastError();
 }
 
 template <typename T, typename W> static cudaError_t backward_rows(const NormArgs& a, uint32_t v, cudaStream_t st) {
-    const uint32_t vecs = a.H * (uint32_t)sizeof(T) / v;
-    if (v == 16) {
-        if (vecs <= 256) return backward_run<T, W, 16, 1>(a, st);
-        if (vecs <= 1024) return backward_run<T, W, 16, 2>(a, st);
-        if constexpr (sizeof(T) == 4) { if (vecs <= 2048) return backward_run<T, W, 16, 4>(a, st); }
-        return cudaErrorNotSupported;
-    }
-    constexpr int E = sizeof(T);
-    if constexpr (E == 2) if (v == 4) {
-        if (vecs <= 2048) return backward_run<T, W, 4, 4>(a, st);
-        if (vecs <= 4096) return backward_run<T, W, 4, 8>(a, st);
-        return cudaErrorNotSupported;
-    }
-    if (vecs <= 2048) return backward_run<T, W, E, 4>(a, st);
-    if (vecs <= 8192) return backward_run<T, W, E, 16>(a, st);
-    return cudaErrorNotSupported;
+    constexpr int E = sizeof(T), D = E == 2 ? 3 : 2;
+    if (a.H > 16 * kMaxGroup || (v == 2 && a.H > 16 * kMaxGroup - 2)) return cudaErrorNotSupported;
+    if (v == 16) return a.H <= 32 * 16 / E ? backward_run<T, W, 16, 1, false, D>(a, st) : backward_run<T, W, 16, E, false, D>(a, st);
+    if constexpr (E == 4) return backward_run<T, W, 4, 16, false, D>(a, st);
+    else return v == 4 ? backward_run<T, W, 4, 8, false, D>(a, st) : backward_run<T, W, 4, 8, true, D>(a, st);
 }
 
 }  // namespace ftc

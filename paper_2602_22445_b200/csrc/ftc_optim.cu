@@ -4,6 +4,7 @@
 // A block is read in one of two layouts. Wide: lane l holds the elements 8 l .. 8 l + 7, one load of 32 (or 16) bytes for each array;
 // it takes a full block of a tensor whose arrays all begin on such boundaries. Narrow: lane l holds the elements l, l + 32, ..., one
 // element a load, each load of the warp one contiguous run: for any alignment and for a tensor's last block.
+#include "ftc_f32x2.cuh"
 #include "ftc_train.cuh"
 
 namespace ftc {
@@ -49,33 +50,36 @@ template <bool WIDE> __device__ __forceinline__ void load_raw(Raw& x, const void
 
 __device__ __forceinline__ float half_f32(uint32_t bits) { return __half2float(__ushort_as_half((unsigned short)bits)); }
 
-template <bool WIDE> __device__ __forceinline__ void numbers(float* v, const Raw& x, uint32_t dtype) {
+template <bool WIDE> __device__ __forceinline__ void numbers(F2* v, const Raw& x, uint32_t dtype) {
     if (dtype == FTC_F32) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(x.r[j]);
+        for (int i = 0; i < 4; ++i) v[i] = pair(__uint_as_float(x.r[2 * i]), __uint_as_float(x.r[2 * i + 1]));
     } else if (dtype == FTC_BF16) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(WIDE ? (j & 1 ? x.r[j / 2] & 0xFFFF0000u : x.r[j / 2] << 16) : x.r[j] << 16);
+        for (int i = 0; i < 4; ++i)
+            v[i] = WIDE ? pair(__uint_as_float(x.r[i] << 16), __uint_as_float(x.r[i] & 0xFFFF0000u))
+                        : pair(__uint_as_float(x.r[2 * i] << 16), __uint_as_float(x.r[2 * i + 1] << 16));
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = half_f32(WIDE ? (j & 1 ? x.r[j / 2] >> 16 : x.r[j / 2] & 0xFFFFu) : x.r[j]);
+        for (int i = 0; i < 4; ++i)
+            v[i] = WIDE ? pair(half_f32(x.r[i] & 0xFFFFu), half_f32(x.r[i] >> 16)) : pair(half_f32(x.r[2 * i]), half_f32(x.r[2 * i + 1]));
     }
 }
 
 // Elements whose bit in `live` is set; all of them in the wide layout if all bits are.
-template <bool WIDE> __device__ __forceinline__ void store_numbers(void* base, uint32_t dtype, uint64_t e0, uint32_t lane, const float* v, uint32_t live) {
+template <bool WIDE> __device__ __forceinline__ void store_numbers(void* base, uint32_t dtype, uint64_t e0, uint32_t lane, const F2* v, uint32_t live) {
     uint32_t r[8];
     if (WIDE && live == 0xFFu) {
         if (dtype == FTC_F32) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) r[j] = __float_as_uint(v[j]);
+            for (int i = 0; i < 4; ++i) { r[2 * i] = __float_as_uint(lo(v[i])); r[2 * i + 1] = __float_as_uint(hi(v[i])); }
             store_32(static_cast<float*>(base) + e0 + lane * 8, r);
             return;
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (dtype == FTC_BF16) { const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]); r[j] = *reinterpret_cast<const uint32_t*>(&p); }
-            else { const __half2 p = __floats2half2_rn(v[2 * j], v[2 * j + 1]); r[j] = *reinterpret_cast<const uint32_t*>(&p); }
+        for (int i = 0; i < 4; ++i) {
+            if (dtype == FTC_BF16) { const __nv_bfloat162 p = __floats2bfloat162_rn(lo(v[i]), hi(v[i])); r[i] = *reinterpret_cast<const uint32_t*>(&p); }
+            else { const __half2 p = __floats2half2_rn(lo(v[i]), hi(v[i])); r[i] = *reinterpret_cast<const uint32_t*>(&p); }
         }
         *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + e0 + lane * 8) = make_uint4(r[0], r[1], r[2], r[3]);
         return;
@@ -83,10 +87,11 @@ template <bool WIDE> __device__ __forceinline__ void store_numbers(void* base, u
 #pragma unroll
     for (int j = 0; j < 8; ++j)
         if (live >> j & 1u) {
-            const uint64_t i = e0 + at<WIDE>(lane, j);
-            if (dtype == FTC_F32) static_cast<float*>(base)[i] = v[j];
-            else if (dtype == FTC_BF16) static_cast<__nv_bfloat16*>(base)[i] = from_f32<__nv_bfloat16>(v[j]);
-            else static_cast<__half*>(base)[i] = from_f32<__half>(v[j]);
+            const uint32_t i = at<WIDE>(lane, j);
+            const float x = j & 1 ? hi(v[j / 2]) : lo(v[j / 2]);
+            if (dtype == FTC_F32) (static_cast<float*>(base) + e0)[i] = x;
+            else if (dtype == FTC_BF16) (static_cast<__nv_bfloat16*>(base) + e0)[i] = from_f32<__nv_bfloat16>(x);
+            else (static_cast<__half*>(base) + e0)[i] = from_f32<__half>(x);
         }
 }
 
@@ -98,46 +103,69 @@ __device__ __forceinline__ float share_of(uint2 s) { return (s.x & 0xFFu) == FTC
 
 // What each of the lane's elements is multiplied with, and which were delivered (bits). One division where the lane's elements are
 // neighbours; elements and messages of more than 32 bits take the long one.
-template <bool WIDE> __device__ __forceinline__ uint32_t shares(float* w, const TableEntry& t, uint64_t e0, uint32_t lane, uint32_t left) {
+template <bool WIDE> __device__ __forceinline__ uint32_t shares(F2* w, const TableEntry& t, uint64_t e0, uint32_t lane, uint32_t left) {
     uint32_t live = 0;
-    if (!t.status) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) { w[j] = 1.f; live |= (WIDE || at<WIDE>(lane, j) < left ? 1u : 0u) << j; }
-        return live;
-    }
+    float f[8];
     const bool small = e0 + FTC_STATE_BLOCK <= 0xFFFFFFFFull;
     if (WIDE) {
         const uint64_t e = e0 + lane * 8;
         uint64_t q = small ? (uint32_t)e / t.k : e / t.k;
         uint32_t r = (uint32_t)(e - q * t.k);
         float s = share_of(record(t, q));
+        if (t.k - r >= 8) {                                          // one message has all eight
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = twice(s);
+            return s > 0.f ? 0xFFu : 0u;
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            w[j] = s;
+            f[j] = s;
             live |= (s > 0.f ? 1u : 0u) << j;
             if (j < 7 && ++r == t.k) { r = 0; s = share_of(record(t, ++q)); }
         }
-        return live;
-    }
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        w[j] = 0.f;
-        if (at<WIDE>(lane, j) < left) {
-            const uint64_t e = e0 + at<WIDE>(lane, j);
-            w[j] = share_of(record(t, small ? (uint32_t)e / t.k : e / t.k));
-            live |= (w[j] > 0.f ? 1u : 0u) << j;
+        for (int j = 0; j < 8; ++j) {
+            f[j] = 0.f;
+            if (at<WIDE>(lane, j) < left) {
+                const uint64_t e = e0 + at<WIDE>(lane, j);
+                f[j] = share_of(record(t, small ? (uint32_t)e / t.k : e / t.k));
+                live |= (f[j] > 0.f ? 1u : 0u) << j;
+            }
         }
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pair(f[2 * i], f[2 * i + 1]);
+    return live;
+}
+template <bool WIDE> __device__ __forceinline__ uint32_t inside(uint32_t lane, uint32_t left) {
+    if (WIDE) return 0xFFu;
+    uint32_t live = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) live |= (at<WIDE>(lane, j) < left ? 1u : 0u) << j;
     return live;
 }
 
-// The whole number c with (c - 1/2)^2 <= x < (c + 1/2)^2, at most `most`. The squares are exact in float32, so the result does not
-// depend on how the root is rounded.
-__device__ __forceinline__ float nearest_root(float x, float most) {
-    float c = floorf(sqrtf(x) + 0.5f);
-    if (c * c - c + 0.25f > x) c -= 1.f;
-    if (c * c + c + 0.25f <= x) c += 1.f;
-    return fminf(fmaxf(c, 0.f), most);
+// Byte j of the words x, and the numbers' low bytes back: a whole number c with |c| < 2^22 stands in the low bits of 3 * 2^22 + c
+// (no conversion instructions, which run at a quarter of the rate).
+constexpr float kWhole = 12582912.f;
+__device__ __forceinline__ F2 bytes_numbers(uint32_t a, uint32_t b, F2 less) {                     // a, b: one byte each
+    return add(pair(__uint_as_float(a | 0x4B000000u), __uint_as_float(b | 0x4B000000u)), less);
+}
+__device__ __forceinline__ uint32_t byte_of(uint32_t w, int j) { return __byte_perm(w, 0u, 0x4440 + j); }
+
+// The whole numbers c with (c - 1/2)^2 <= x < (c + 1/2)^2, at most `most`. A root with an error of some units in the last place gives c
+// or a neighbour; x - c^2 is exact in float32 (a multiple of x's last place, smaller than x), so the two comparisons decide exactly.
+__device__ __forceinline__ float fast_root(float x) { float r; asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ F2 nearest_roots(F2 x, float most) {
+    const F2 c = add(add(pair(fast_root(lo(x)), fast_root(hi(x))), twice(kWhole)), twice(-kWhole));
+    const F2 nc = mul(c, twice(-1.f)), d = fma(nc, c, x), up = add(c, twice(0.25f)), down = add(nc, twice(0.25f));
+    float a = lo(c), b = hi(c);
+    if (lo(d) >= lo(up)) a += 1.f;
+    if (hi(d) >= hi(up)) b += 1.f;
+    if (lo(d) < lo(down)) a -= 1.f;
+    if (hi(d) < hi(down)) b -= 1.f;
+    return pair(fminf(fmaxf(a, 0.f), most), fminf(fmaxf(b, 0.f), most));          // at c = 0 the lower comparison says nothing
 }
 
 // Largest of the warp's non-negative values, as bit patterns: infinities above all numbers, NaN above them.
@@ -152,11 +180,11 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const TableEntry&
     load_raw<WIDE>(pr, weights, pd, e0, lane, left);
     const uint64_t q = b * FTC_STATE_BLOCK;
     float ms = 0.f, vs = 0.f;
+    uint8_t *mp = static_cast<uint8_t*>(a.m) + q, *vp = static_cast<uint8_t*>(a.v) + q;
     if (BITS == 32) {
         load_raw<WIDE>(mr, a.m, FTC_F32, q, lane, FTC_STATE_BLOCK);
         load_raw<WIDE>(vr, a.v, FTC_F32, q, lane, FTC_STATE_BLOCK);
     } else {
-        const uint8_t *mp = static_cast<const uint8_t*>(a.m) + q, *vp = static_cast<const uint8_t*>(a.v) + q;
         if (WIDE) {
             const uint2 x = reinterpret_cast<const uint2*>(mp)[lane], y = reinterpret_cast<const uint2*>(vp)[lane];
             mr.r[0] = x.x; mr.r[1] = x.y; vr.r[0] = y.x; vr.r[1] = y.y;
@@ -166,30 +194,51 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const TableEntry&
         }
         ms = a.m_scale[b]; vs = a.v_scale[b];
     }
-    float w[8], g[8], p[8], m[8], v[8];
-    const uint32_t live = shares<WIDE>(w, t, e0, lane, left);
+    F2 g[4], p[4], m[4], v[4], root[4];
+    uint32_t live;
     numbers<WIDE>(g, gr, t.grad_dtype);
+    if (t.status) {
+        F2 w[4];
+        live = shares<WIDE>(w, t, e0, lane, left);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g[i] = mul(g[i], w[i]);
+    } else live = inside<WIDE>(lane, left);
     numbers<WIDE>(p, pr, pd);
     if (BITS == 32) { numbers<true>(m, mr, FTC_F32); numbers<true>(v, vr, FTC_F32); }
     else {
-        ms *= kInv127; vs *= kInv255;
+        const F2 mk = twice(ms * kInv127), vk = twice(vs * kInv255);
+        if (WIDE) { mr.r[0] ^= 0x80808080u; mr.r[1] ^= 0x80808080u; }           // signed bytes + 128
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t cm = WIDE ? mr.r[j / 4] >> (j % 4 * 8) & 0xFFu : mr.r[j], cv = WIDE ? vr.r[j / 4] >> (j % 4 * 8) & 0xFFu : vr.r[j];
-            const float c = (float)(int8_t)cm, d = (float)cv, r = d * d * vs;
-            m[j] = c * fabsf(c) * ms;
-            v[j] = r * r;
+        for (int i = 0; i < 4; ++i) {
+            const int j = i * 2 % 4;
+            const F2 c = WIDE ? bytes_numbers(byte_of(mr.r[i / 2], j), byte_of(mr.r[i / 2], j + 1), twice(-8388736.f))
+                              : bytes_numbers(mr.r[2 * i] ^ 0x80u, mr.r[2 * i + 1] ^ 0x80u, twice(-8388736.f));
+            const F2 d = WIDE ? bytes_numbers(byte_of(vr.r[i / 2], j), byte_of(vr.r[i / 2], j + 1), twice(-8388608.f))
+                              : bytes_numbers(vr.r[2 * i], vr.r[2 * i + 1], twice(-8388608.f));
+            const F2 r = mul(mul(d, d), vk);
+            m[i] = mul(mul(c, pair(fabsf(lo(c)), fabsf(hi(c)))), mk);
+            v[i] = mul(r, r);
         }
     }
-    const float lr = a.lr * t.lr_scale, keep = 1.f - lr * t.weight_decay, rate = lr * a.fix1;
-    float root[8];
+    const float lr = a.lr * t.lr_scale;
+    const F2 keep = twice(1.f - lr * t.weight_decay), rate = twice(-(lr * a.fix1)), sc = twice(scale);
+    const bool some = t.status && live != 0xFFu;                                // messages missing
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float gj = g[j] * w[j] * scale, mj = m[j] * a.beta1 + gj * a.rest1, vj = v[j] * a.beta2 + gj * gj * a.rest2;
-        root[j] = sqrtf(vj);
-        const float pj = p[j] * keep - mj / (root[j] * a.fix2 + a.eps) * rate;
-        if (live >> j & 1u) { m[j] = mj; v[j] = vj; p[j] = pj; }
-        else if (BITS == 8) root[j] = sqrtf(v[j]);
+    for (int i = 0; i < 4; ++i) {
+        g[i] = mul(g[i], sc);
+        const F2 mi = add_apart(mul(m[i], twice(a.beta1)), mul(g[i], twice(a.rest1)));
+        const F2 vi = add_apart(mul(v[i], twice(a.beta2)), mul(mul(g[i], g[i]), twice(a.rest2)));
+        root[i] = BITS == 8 ? pair(__fsqrt_rn(lo(vi)), __fsqrt_rn(hi(vi))) : pair(fast_root(lo(vi)), fast_root(hi(vi)));
+        const F2 den = add(mul(root[i], twice(a.fix2)), twice(a.eps));
+        const F2 ratio = pair(__fdividef(lo(mi), lo(den)), __fdividef(hi(mi), hi(den)));
+        const F2 pi = add(mul(p[i], keep), mul(ratio, rate));
+        if (some) {
+            const bool x = live >> (2 * i) & 1u, y = live >> (2 * i + 1) & 1u;
+            m[i] = pair(x ? lo(mi) : lo(m[i]), y ? hi(mi) : hi(m[i]));
+            if (BITS == 8) root[i] = pair(x ? lo(root[i]) : __fsqrt_rn(lo(v[i])), y ? hi(root[i]) : __fsqrt_rn(hi(v[i])));
+        } else m[i] = mi;
+        v[i] = vi;
+        p[i] = pi;                                                              // stored where live only, as v is
     }
     store_numbers<WIDE>(weights, pd, e0, lane, p, live);
     if (t.master) store_numbers<WIDE>(t.param, t.param_dtype, e0, lane, p, live);
@@ -198,29 +247,37 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const TableEntry&
         store_numbers<WIDE>(a.v, FTC_F32, q, lane, v, live);
         return;
     }
-    if (!__any_sync(0xFFFFFFFFu, live)) return;
-    uint32_t mm = 0, rm = 0;
+    if (t.status && !__any_sync(0xFFFFFFFFu, live)) return;
+    uint32_t mm = 0, rm = 0;                                                    // behind the tensor's end all is zero
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        mm = max(mm, __float_as_uint(m[j]) & 0x7FFFFFFFu);
-        rm = max(rm, __float_as_uint(root[j]) & 0x7FFFFFFFu);
+    for (int i = 0; i < 4; ++i) {
+        mm = max(mm, max(__float_as_uint(lo(m[i])) & 0x7FFFFFFFu, __float_as_uint(hi(m[i])) & 0x7FFFFFFFu));
+        rm = max(rm, max(__float_as_uint(lo(root[i])) & 0x7FFFFFFFu, __float_as_uint(hi(root[i])) & 0x7FFFFFFFu));
     }
     ms = warp_max_bits(mm); vs = warp_max_bits(rm);
-    ms = ms < kTiny ? kTiny : ms; vs = vs < kTiny ? kTiny : vs;             // NaN stays
-    const float mi = 1.f / ms, vi = 1.f / vs;
+    ms = ms <= 3.402823466e38f ? fmaxf(ms, kTiny) : __uint_as_float(0x7FC00000u);
+    vs = vs <= 3.402823466e38f ? fmaxf(vs, kTiny) : __uint_as_float(0x7FC00000u);
+    const float inv = 1.f / (lane & 1 ? vs : ms);                               // one division for both
+    const F2 mi = twice(__shfl_sync(0xFFFFFFFFu, inv, 0)), vi = twice(__shfl_sync(0xFFFFFFFFu, inv, 1));
     uint32_t cm[8], cv[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float c = nearest_root(fabsf(m[j]) * mi * 16129.f, 127.f);
-        float d = nearest_root(root[j] * vi * 65025.f, 255.f);
-        if (root[j] > 0.f) d = fmaxf(d, 1.f);
-        cm[j] = (uint32_t)(int)(m[j] < 0.f ? -c : c) & 0xFFu;
-        cv[j] = (uint32_t)d;
+    for (int i = 0; i < 4; ++i) {
+        const F2 c = nearest_roots(mul(mul(pair(fabsf(lo(m[i])), fabsf(hi(m[i]))), mi), twice(16129.f)), 127.f);
+        F2 d = nearest_roots(mul(mul(root[i], vi), twice(65025.f)), 255.f);
+        d = pair(lo(root[i]) > 0.f ? fmaxf(lo(d), 1.f) : lo(d), hi(root[i]) > 0.f ? fmaxf(hi(d), 1.f) : hi(d));
+        const F2 s = add(pair(copysignf(lo(c), lo(m[i])), copysignf(hi(c), hi(m[i]))), twice(kWhole)), u = add(d, twice(kWhole));
+        cm[2 * i] = __float_as_uint(lo(s)); cm[2 * i + 1] = __float_as_uint(hi(s));
+        cv[2 * i] = __float_as_uint(lo(u)); cv[2 * i + 1] = __float_as_uint(hi(u));
     }
-    uint8_t *mp = static_cast<uint8_t*>(a.m) + q, *vp = static_cast<uint8_t*>(a.v) + q;
     if (WIDE) {
-        reinterpret_cast<uint2*>(mp)[lane] = make_uint2(cm[0] | cm[1] << 8 | cm[2] << 16 | cm[3] << 24, cm[4] | cm[5] << 8 | cm[6] << 16 | cm[7] << 24);
-        reinterpret_cast<uint2*>(vp)[lane] = make_uint2(cv[0] | cv[1] << 8 | cv[2] << 16 | cv[3] << 24, cv[4] | cv[5] << 8 | cv[6] << 16 | cv[7] << 24);
+        uint32_t x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t* c = i < 2 ? cm + 4 * i : cv + 4 * (i - 2);
+            x[i] = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+        }
+        reinterpret_cast<uint2*>(mp)[lane] = make_uint2(x[0], x[1]);
+        reinterpret_cast<uint2*>(vp)[lane] = make_uint2(x[2], x[3]);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) { mp[j * 32 + lane] = (uint8_t)cm[j]; vp[j * 32 + lane] = (uint8_t)cv[j]; }
@@ -229,7 +286,7 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const TableEntry&
 }
 
 template <int BITS>
-__global__ void __launch_bounds__(kWarps * 32) adamw_kernel(AdamArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, 3) adamw_kernel(AdamArgs a) {
     const uint32_t lane = threadIdx.x & 31;
     const uint64_t b = blockIdx.x * (uint64_t)kWarps + (threadIdx.x >> 5);
     if (b >= a.n_blocks) return;
@@ -276,23 +333,37 @@ cudaError_t launch_adamw_states(uint64_t blocks, const void* m, const void* v, c
 
 constexpr int kAhead = 4;                                        // blocks whose loads a warp has out at once
 
-template <bool WIDE> __device__ __forceinline__ double block_squares(const Raw& x, const TableEntry& t, uint64_t e0, uint32_t lane, uint32_t left) {
-    float w[8], g[8];
-    numbers<WIDE>(g, x, t.grad_dtype);
-    double s = 0;
-    if (t.status) {
-        const uint32_t live = shares<WIDE>(w, t, e0, lane, left);
+// Sum of the squares of 8 numbers. In float32 where that neither overflows nor loses small squares (4 roundings at most one after the
+// other), else in float64.
+__device__ __forceinline__ double squares(const F2* g) {
+    const F2 s = add(fma(g[0], g[0], mul(g[1], g[1])), fma(g[2], g[2], mul(g[3], g[3])));
+    const float f = lo(s) + hi(s);
+    if (f >= 1e-30f && f <= 1e38f) return (double)f;
+    double d = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) g[j] = live >> j & 1u ? g[j] * w[j] : 0.f;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) s = fma((double)g[j], (double)g[j], s);       // elements behind the end were loaded as zeros
-    return s;
+    for (int i = 0; i < 4; ++i) d += (double)lo(g[i]) * lo(g[i]) + (double)hi(g[i]) * hi(g[i]);
+    return d;
 }
 
-__global__ void __launch_bounds__(kWarps * 32) grad_squares_kernel(const void* table, uint32_t n_params, uint64_t n_blocks, uint64_t span, double* slots) {
+template <bool WIDE> __device__ __forceinline__ double block_squares(const Raw& x, const TableEntry& t, uint64_t e0, uint32_t lane, uint32_t left) {
+    F2 g[4];
+    numbers<WIDE>(g, x, t.grad_dtype);
+    if (t.status) {
+        F2 w[4];
+        const uint32_t live = shares<WIDE>(w, t, e0, lane, left);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            g[i] = mul(g[i], w[i]);
+            g[i] = pair(live >> (2 * i) & 1u ? lo(g[i]) : 0.f, live >> (2 * i + 1) & 1u ? hi(g[i]) : 0.f);
+        }
+    }
+    return squares(g);                                               // elements behind the end were loaded as zeros
+}
+
+__global__ void __launch_bounds__(kWarps * 32) grad_squares_kernel(const void* table, uint32_t n_params, uint64_t n_blocks, uint64_t span, double* slots, uint32_t* ticket) {
     const uint32_t lane = threadIdx.x & 31;
     const uint64_t w = blockIdx.x * (uint64_t)kWarps + (threadIdx.x >> 5);
+    if (w == 0 && lane == 0) *ticket = 0;
     uint64_t b = w * span;
     const uint64_t b1 = b + span < n_blocks ? b + span : n_blocks;
     while (b < b1) {
@@ -300,14 +371,30 @@ __global__ void __launch_bounds__(kWarps * 32) grad_squares_kernel(const void* t
         const TableEntry t = table_entries(table)[ti];
         const uint64_t last = t.first_block + (t.n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK, end = last < b1 ? last : b1;
         const uint64_t whole = t.wide ? t.first_block + t.n / FTC_STATE_BLOCK : 0, end_wide = whole < end ? whole : end;
+        const bool plain = t.status && t.k % 8 == 0 && t.n <= 0xFFFFFFFFull;    // a lane's eight elements are of one message
         double s = 0;
         for (; b + kAhead <= end_wide; b += kAhead) {
             Raw x[kAhead];
             const uint64_t e0 = (b - t.first_block) * FTC_STATE_BLOCK;
+            uint2 st[kAhead];
+            if (plain) {
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) st[i] = record(t, ((uint32_t)e0 + i * FTC_STATE_BLOCK + lane * 8) / t.k);
+            }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) load_raw<true>(x[i], t.grad, t.grad_dtype, e0 + i * FTC_STATE_BLOCK, lane, FTC_STATE_BLOCK);
+            if (!plain) {
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) s += block_squares<true>(x[i], t, e0 + i * FTC_STATE_BLOCK, lane, FTC_STATE_BLOCK);
+                for (int i = 0; i < kAhead; ++i) s += block_squares<true>(x[i], t, e0 + i * FTC_STATE_BLOCK, lane, FTC_STATE_BLOCK);
+                continue;
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                F2 g[4];
+                numbers<true>(g, x[i], t.grad_dtype);
+                const float share = share_of(st[i]);
+                if (share > 0.f) s = ::fma((double)share * share, squares(g), s);
+            }
         }
         for (; b < end; ++b) {
             Raw x;
@@ -321,35 +408,46 @@ __global__ void __launch_bounds__(kWarps * 32) grad_squares_kernel(const void* t
     }
 }
 
-// One block: a warp for each tensor's sum, then the sum over tensors.
-__global__ void __launch_bounds__(1024) grad_norm_kernel(const void* table, uint32_t n_params, uint64_t span, float max_norm, const double* slots, double* sums,
-                                                         float* norm, float* norms) {
-    __shared__ double part[32];
-    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (uint32_t ti = warp; ti < n_params; ti += 32) {
+__device__ __forceinline__ double block_sum(double s, double* part) {          // 128 threads
+    s = warp_sum(s);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
+    __syncthreads();
+    s = (part[0] + part[1]) + (part[2] + part[3]);
+    __syncthreads();
+    return s;
+}
+
+// A block adds the slots of one tensor after the other; the block that is last to finish adds the tensors' sums. Every sum has an order of
+// its own that does not depend on which block comes last.
+__global__ void __launch_bounds__(128) grad_norm_kernel(const void* table, uint32_t n_params, uint64_t span, float max_norm, const double* slots, double* sums,
+                                                        uint32_t* ticket, float* norm, float* norms) {
+    __shared__ double part[4];
+    __shared__ bool mine;
+    for (uint32_t ti = blockIdx.x; ti < n_params; ti += gridDim.x) {
         const uint64_t n = table_entries(table)[ti].n, first = table_entries(table)[ti].first_block;
         double s = 0;
         if (n) {
-            const uint64_t last = first + (n - 1) / FTC_STATE_BLOCK;
+            const uint64_t last = (first + (n - 1) / FTC_STATE_BLOCK) / span;
 #pragma unroll 8
-            for (uint64_t w = first / span + lane; w <= last / span; w += 32) s += slots[w + ti];
+            for (uint64_t w = first / span + threadIdx.x; w <= last; w += 128) s += slots[w + ti];
         }
-        s = warp_sum(s);
-        if (lane == 0) { sums[ti] = s; if (norms) norms[ti] = (float)sqrt(s); }
+        s = block_sum(s, part);
+        if (threadIdx.x == 0) { sums[ti] = s; if (norms) norms[ti] = (float)sqrt(s); }
+    }
+    if (threadIdx.x == 0) {
+        __threadfence();                                             // this block's sums before its ticket
+        mine = atomicAdd(ticket, 1u) == gridDim.x - 1;
+        __threadfence();
     }
     __syncthreads();
+    if (!mine) return;
     double s = 0;
-    for (uint32_t ti = threadIdx.x; ti < n_params; ti += 1024) s += sums[ti];
-    s = warp_sum(s);
-    if (lane == 0) part[warp] = s;
-    __syncthreads();
-    if (warp == 0) {
-        s = warp_sum(part[lane]);
-        if (lane == 0) {
-            const float r = (float)sqrt(s);
-            norm[0] = r;
-            norm[1] = !isfinite(r) ? __uint_as_float(0x7FC00000u) : r > max_norm ? max_norm / r : 1.f;
-        }
+    for (uint32_t ti = threadIdx.x; ti < n_params; ti += 128) s += __ldcg(sums + ti);
+    s = block_sum(s, part);
+    if (threadIdx.x == 0) {
+        const float r = (float)sqrt(s);
+        norm[0] = r;
+        norm[1] = !isfinite(r) ? __uint_as_float(0x7FC00000u) : r > max_norm ? max_norm / r : 1.f;
     }
 }
 
@@ -361,15 +459,15 @@ uint32_t grad_norm_warps(uint64_t n_blocks, int sm_count) {
 
 cudaError_t launch_grad_norm(const void* table, uint32_t n_params, uint64_t n_blocks, float max_norm, float* norm, float* norms, double* ws, int sm_count,
                              cudaStream_t st) {
-    const uint32_t warps = grad_norm_warps(n_blocks, sm_count);
+    const uint32_t warps = grad_norm_warps(n_blocks, sm_count), squares_grid = warps ? (warps + kWarps - 1) / kWarps : 1;
     const uint64_t span = warps ? (n_blocks + warps - 1) / warps : 1;
-    double* sums = ws + warps + n_params;
-    if (warps) {
-        grad_squares_kernel<<<(warps + kWarps - 1) / kWarps, kWarps * 32, 0, st>>>(table, n_params, n_blocks, span, ws);
-        const cudaError_t e = cudaGetLastError();
-        if (e != cudaSuccess) return e;
-    }
-    grad_norm_kernel<<<1, 1024, 0, st>>>(table, n_params, span, max_norm, ws, sums, norm, norms);
+    double *slots = ws + 1, *sums = slots + warps + n_params;
+    uint32_t* ticket = reinterpret_cast<uint32_t*>(ws);
+    grad_squares_kernel<<<squares_grid, kWarps * 32, 0, st>>>(table, n_params, n_blocks, span, slots, ticket);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    const uint32_t cap = (uint32_t)sm_count * 8, grid = n_params < cap ? (n_params ? n_params : 1) : cap;
+    grad_norm_kernel<<<grid, 128, 0, st>>>(table, n_params, span, max_norm, slots, sums, ticket, norm, norms);
     return cudaGetLastError();
 }
 
