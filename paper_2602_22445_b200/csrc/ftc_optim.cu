@@ -154,22 +154,34 @@ __device__ __forceinline__ F2 bytes_numbers(uint32_t a, uint32_t b, F2 less) {  
 }
 __device__ __forceinline__ uint32_t byte_of(uint32_t w, int j) { return __byte_perm(w, 0u, 0x4440 + j); }
 
-// The whole numbers c with (c - 1/2)^2 <= x < (c + 1/2)^2, at most `most`. A root with an error of some units in the last place gives c
-// or a neighbour; x - c^2 is exact in float32 (a multiple of x's last place, smaller than x), so the two comparisons decide exactly.
-__device__ __forceinline__ float fast_root(float x) { float r; asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
-__device__ __forceinline__ F2 nearest_roots(F2 x, float most) {
-    const F2 c = add(add(pair(fast_root(lo(x)), fast_root(hi(x))), twice(kWhole)), twice(-kWhole));
-    const F2 nc = mul(c, twice(-1.f)), d = fma(nc, c, x), up = add(c, twice(0.25f)), down = add(nc, twice(0.25f));
-    float a = lo(c), b = hi(c);
-    if (lo(d) >= lo(up)) a += 1.f;
-    if (hi(d) >= hi(up)) b += 1.f;
-    if (lo(d) < lo(down)) a -= 1.f;
-    if (hi(d) < hi(down)) b -= 1.f;
-    return pair(fminf(fmaxf(a, 0.f), most), fminf(fmaxf(b, 0.f), most));          // at c = 0 the lower comparison says nothing
+// The whole numbers c nearest to sqrt(x), (c - 1/2)^2 <= x < (c + 1/2)^2, at most `most`, from an approximate root. The root and
+// x may be off by some units in the last place: `far` collects how far the root lies from its whole number, and where that comes
+// too near a half, c may be wrong. With a root good to 2^-23 and an exact x (m) the root is off by 127 * 2^-23 < 1.6e-5; with an x whose
+// own root was approximate and whose roundings may fall otherwise (v: 2^-23 + 2 * 2^-24), by 255 * 2^-22 < 6.1e-5.
+constexpr float kDoubtM = 2e-5f, kDoubtV = 6.5e-5f;
+__device__ __forceinline__ float fast_root(float x) { float r; asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ F2 likely_roots(F2 x, float& far) {
+    const F2 s = pair(fast_root(lo(x)), fast_root(hi(x))), c = add(add(s, twice(kWhole)), twice(-kWhole)), f = fma(c, twice(-1.f), s);
+    far = fmaxf(far, fmaxf(fabsf(lo(f)), fabsf(hi(f))));
+    return c;
+}
+// The same without doubt: x - c^2 is exact in float32 (a multiple of x's last place, smaller than x), so two comparisons decide.
+__device__ __noinline__ float nearest_root(float x, float most) {
+    float c = floorf(__fsqrt_rn(x) + 0.5f);
+    const float d = __fmaf_rn(-c, c, x);
+    if (d >= c + 0.25f) c += 1.f;
+    else if (d < 0.25f - c) c -= 1.f;
+    return fminf(fmaxf(c, 0.f), most);                               // at c = 0 the lower comparison says nothing
 }
 
 // Largest of the warp's non-negative values, as bit patterns: infinities above all numbers, NaN above them.
 __device__ __forceinline__ float warp_max_bits(uint32_t v) { return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, v)); }
+
+// Quotients by way of a reciprocal where eps keeps the divisor far above the smallest normal number.
+constexpr float kNoSmall = 1e-30f;
+__device__ __forceinline__ float fast_inverse(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+
+__device__ __noinline__ float slow_ratio(float m, float v, float fix2, float eps) { return m / (__fsqrt_rn(v) * fix2 + eps); }
 
 template <int BITS, bool WIDE>
 __device__ __forceinline__ void adamw_block(const AdamArgs& a, const TableEntry& t, uint64_t b, uint32_t lane, uint64_t e0, uint32_t left, float scale) {
@@ -194,7 +206,7 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const TableEntry&
         }
         ms = a.m_scale[b]; vs = a.v_scale[b];
     }
-    F2 g[4], p[4], m[4], v[4], root[4];
+    F2 g[4], p[4], m[4], v[4];
     uint32_t live;
     numbers<WIDE>(g, gr, t.grad_dtype);
     if (t.status) {
@@ -223,22 +235,25 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const TableEntry&
     const float lr = a.lr * t.lr_scale;
     const F2 keep = twice(1.f - lr * t.weight_decay), rate = twice(-(lr * a.fix1)), sc = twice(scale);
     const bool some = t.status && live != 0xFFu;                                // messages missing
+    F2 root[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         g[i] = mul(g[i], sc);
         const F2 mi = add_apart(mul(m[i], twice(a.beta1)), mul(g[i], twice(a.rest1)));
         const F2 vi = add_apart(mul(v[i], twice(a.beta2)), mul(mul(g[i], g[i]), twice(a.rest2)));
-        root[i] = BITS == 8 ? pair(__fsqrt_rn(lo(vi)), __fsqrt_rn(hi(vi))) : pair(fast_root(lo(vi)), fast_root(hi(vi)));
+        root[i] = pair(fast_root(lo(vi)), fast_root(hi(vi)));
         const F2 den = add(mul(root[i], twice(a.fix2)), twice(a.eps));
-        const F2 ratio = pair(__fdividef(lo(mi), lo(den)), __fdividef(hi(mi), hi(den)));
-        const F2 pi = add(mul(p[i], keep), mul(ratio, rate));
-        if (some) {
+        F2 ratio;
+        if (a.eps >= kNoSmall) ratio = mul(mi, pair(fast_inverse(lo(den)), fast_inverse(hi(den))));
+        else ratio = pair(slow_ratio(lo(mi), lo(vi), a.fix2, a.eps), slow_ratio(hi(mi), hi(vi), a.fix2, a.eps));
+        const F2 pi = fma(ratio, rate, mul(p[i], keep));
+        if (some) {                                                             // m, v: for the block's codes; else stored where live only
             const bool x = live >> (2 * i) & 1u, y = live >> (2 * i + 1) & 1u;
             m[i] = pair(x ? lo(mi) : lo(m[i]), y ? hi(mi) : hi(m[i]));
-            if (BITS == 8) root[i] = pair(x ? lo(root[i]) : __fsqrt_rn(lo(v[i])), y ? hi(root[i]) : __fsqrt_rn(hi(v[i])));
-        } else m[i] = mi;
-        v[i] = vi;
-        p[i] = pi;                                                              // stored where live only, as v is
+            v[i] = pair(x ? lo(vi) : lo(v[i]), y ? hi(vi) : hi(v[i]));
+            if (BITS == 8) root[i] = pair(fast_root(lo(v[i])), fast_root(hi(v[i])));
+        } else { m[i] = mi; v[i] = vi; }
+        p[i] = pi;
     }
     store_numbers<WIDE>(weights, pd, e0, lane, p, live);
     if (t.master) store_numbers<WIDE>(t.param, t.param_dtype, e0, lane, p, live);
@@ -248,24 +263,36 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const TableEntry&
         return;
     }
     if (t.status && !__any_sync(0xFFFFFFFFu, live)) return;
-    uint32_t mm = 0, rm = 0;                                                    // behind the tensor's end all is zero
+    uint32_t mm = 0, vm = 0;                                                    // behind the tensor's end all is zero
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         mm = max(mm, max(__float_as_uint(lo(m[i])) & 0x7FFFFFFFu, __float_as_uint(hi(m[i])) & 0x7FFFFFFFu));
-        rm = max(rm, max(__float_as_uint(lo(root[i])) & 0x7FFFFFFFu, __float_as_uint(hi(root[i])) & 0x7FFFFFFFu));
+        vm = max(vm, max(__float_as_uint(lo(v[i])) & 0x7FFFFFFFu, __float_as_uint(hi(v[i])) & 0x7FFFFFFFu));
     }
-    ms = warp_max_bits(mm); vs = warp_max_bits(rm);
+    ms = warp_max_bits(mm); vs = __fsqrt_rn(warp_max_bits(vm));                 // the root keeps the order: the largest root
     ms = ms <= 3.402823466e38f ? fmaxf(ms, kTiny) : __uint_as_float(0x7FC00000u);
     vs = vs <= 3.402823466e38f ? fmaxf(vs, kTiny) : __uint_as_float(0x7FC00000u);
     const float inv = 1.f / (lane & 1 ? vs : ms);                               // one division for both
-    const F2 mi = twice(__shfl_sync(0xFFFFFFFFu, inv, 0)), vi = twice(__shfl_sync(0xFFFFFFFFu, inv, 1));
+    const float mi = __shfl_sync(0xFFFFFFFFu, inv, 0), vi = __shfl_sync(0xFFFFFFFFu, inv, 1);
+    F2 c[4], d[4];
+    float far_m = 0.f, far_v = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        c[i] = likely_roots(mul(mul(pair(fabsf(lo(m[i])), fabsf(hi(m[i]))), twice(mi)), twice(16129.f)), far_m);
+        d[i] = likely_roots(mul(mul(root[i], twice(vi)), twice(65025.f)), far_v);
+    }
+    if (!(far_m < 0.5f - kDoubtM && far_v < 0.5f - kDoubtV)) {                  // one lane in a thousand, and NaN
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            c[i] = pair(nearest_root(fabsf(lo(m[i])) * mi * 16129.f, 127.f), nearest_root(fabsf(hi(m[i])) * mi * 16129.f, 127.f));
+            d[i] = pair(nearest_root(__fsqrt_rn(lo(v[i])) * vi * 65025.f, 255.f), nearest_root(__fsqrt_rn(hi(v[i])) * vi * 65025.f, 255.f));
+        }
+    }
     uint32_t cm[8], cv[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const F2 c = nearest_roots(mul(mul(pair(fabsf(lo(m[i])), fabsf(hi(m[i]))), mi), twice(16129.f)), 127.f);
-        F2 d = nearest_roots(mul(mul(root[i], vi), twice(65025.f)), 255.f);
-        d = pair(lo(root[i]) > 0.f ? fmaxf(lo(d), 1.f) : lo(d), hi(root[i]) > 0.f ? fmaxf(hi(d), 1.f) : hi(d));
-        const F2 s = add(pair(copysignf(lo(c), lo(m[i])), copysignf(hi(c), hi(m[i]))), twice(kWhole)), u = add(d, twice(kWhole));
+        const F2 e = pair(lo(v[i]) > 0.f ? fmaxf(lo(d[i]), 1.f) : lo(d[i]), hi(v[i]) > 0.f ? fmaxf(hi(d[i]), 1.f) : hi(d[i]));
+        const F2 s = add(pair(copysignf(lo(c[i]), lo(m[i])), copysignf(hi(c[i]), hi(m[i]))), twice(kWhole)), u = add(e, twice(kWhole));
         cm[2 * i] = __float_as_uint(lo(s)); cm[2 * i + 1] = __float_as_uint(hi(s));
         cv[2 * i] = __float_as_uint(lo(u)); cv[2 * i + 1] = __float_as_uint(hi(u));
     }
@@ -273,8 +300,8 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const TableEntry&
         uint32_t x[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t* c = i < 2 ? cm + 4 * i : cv + 4 * (i - 2);
-            x[i] = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+            const uint32_t* w = i < 2 ? cm + 4 * i : cv + 4 * (i - 2);
+            x[i] = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
         }
         reinterpret_cast<uint2*>(mp)[lane] = make_uint2(x[0], x[1]);
         reinterpret_cast<uint2*>(vp)[lane] = make_uint2(x[2], x[3]);
@@ -286,7 +313,7 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const TableEntry&
 }
 
 template <int BITS>
-__global__ void __launch_bounds__(kWarps * 32, 3) adamw_kernel(AdamArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, 4) adamw_kernel(AdamArgs a) {
     const uint32_t lane = threadIdx.x & 31;
     const uint64_t b = blockIdx.x * (uint64_t)kWarps + (threadIdx.x >> 5);
     if (b >= a.n_blocks) return;
