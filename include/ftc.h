@@ -433,7 +433,7 @@ FTC_API size_t ftc_grad_norm_workspace_bytes(const void* h_table);
 
 /* One AdamW step (decoupled weight decay). */
 typedef struct {
-    double lr, beta1, beta2, eps;   /* lr >= 0 finite, 0 <= beta < 1, eps >= 0 */
+    double lr, beta1, beta2, eps;   /* lr >= 0 finite, 0 <= beta < 1, eps >= 1e-30 */
     uint64_t step;                  /* 1 for the first step (bias corrections 1 - beta^step) */
     uint32_t state_bits;            /* 32 or 8 */
     uint32_t reserved;              /* 0 */

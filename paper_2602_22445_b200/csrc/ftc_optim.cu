@@ -31,21 +31,23 @@ __device__ __forceinline__ void load_16(const void* p, uint32_t* r) {
 // Which elements a lane holds of the block that begins at element e0 of a tensor of n.
 template <bool WIDE> __device__ __forceinline__ uint32_t at(uint32_t lane, int j) { return WIDE ? lane * 8 + j : j * 32 + lane; }
 
+template <typename U> __device__ __forceinline__ void load_narrow(Raw& x, const U* p, uint32_t lane, uint32_t left) {
+    if (left >= FTC_STATE_BLOCK) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x.r[j] = p[j * 32];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x.r[j] = lane + j * 32 < left ? p[j * 32] : 0u;
+    }
+}
 template <bool WIDE> __device__ __forceinline__ void load_raw(Raw& x, const void* base, uint32_t dtype, uint64_t e0, uint32_t lane, uint32_t left) {
     if (WIDE) {
         if (dtype == FTC_F32) load_32(static_cast<const float*>(base) + e0 + lane * 8, x.r);
         else load_16(static_cast<const uint16_t*>(base) + e0 + lane * 8, x.r);
         return;
     }
-    if (dtype == FTC_F32) {
-        const uint32_t* p = static_cast<const uint32_t*>(base) + e0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x.r[j] = at<WIDE>(lane, j) < left ? p[at<WIDE>(lane, j)] : 0u;
-    } else {
-        const uint16_t* p = static_cast<const uint16_t*>(base) + e0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x.r[j] = at<WIDE>(lane, j) < left ? p[at<WIDE>(lane, j)] : 0u;
-    }
+    if (dtype == FTC_F32) load_narrow(x, static_cast<const uint32_t*>(base) + e0 + lane, lane, left);
+    else load_narrow(x, static_cast<const uint16_t*>(base) + e0 + lane, lane, left);
 }
 
 __device__ __forceinline__ float half_f32(uint32_t bits) { return __half2float(__ushort_as_half((unsigned short)bits)); }
@@ -177,22 +179,20 @@ __device__ __noinline__ float nearest_root(float x, float most) {
 // Largest of the warp's non-negative values, as bit patterns: infinities above all numbers, NaN above them.
 __device__ __forceinline__ float warp_max_bits(uint32_t v) { return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, v)); }
 
-// Quotients by way of a reciprocal where eps keeps the divisor far above the smallest normal number.
-constexpr float kNoSmall = 1e-30f;
+// For divisors that eps keeps far above the smallest normal number.
 __device__ __forceinline__ float fast_inverse(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 
-__device__ __noinline__ float slow_ratio(float m, float v, float fix2, float eps) { return m / (__fsqrt_rn(v) * fix2 + eps); }
+
+// What a block needs, as loaded.
+struct BlockIn { Raw gr, pr, mr, vr; float ms, vs; };
 
 template <int BITS, bool WIDE>
-__device__ __forceinline__ void adamw_block(const AdamArgs& a, const TableEntry& t, uint64_t b, uint32_t lane, uint64_t e0, uint32_t left, float scale) {
-    Raw gr, pr, mr, vr;
-    const uint32_t pd = t.master ? (uint32_t)FTC_F32 : t.param_dtype;
-    void* weights = t.master ? t.master : t.param;
-    load_raw<WIDE>(gr, t.grad, t.grad_dtype, e0, lane, left);
-    load_raw<WIDE>(pr, weights, pd, e0, lane, left);
+__device__ __forceinline__ void adamw_load(BlockIn& in, const AdamArgs& a, const TableEntry& t, uint64_t b, uint32_t lane, uint64_t e0, uint32_t left) {
+    Raw &mr = in.mr, &vr = in.vr;
+    load_raw<WIDE>(in.gr, t.grad, t.grad_dtype, e0, lane, left);
+    load_raw<WIDE>(in.pr, t.master ? t.master : t.param, t.master ? (uint32_t)FTC_F32 : t.param_dtype, e0, lane, left);
     const uint64_t q = b * FTC_STATE_BLOCK;
-    float ms = 0.f, vs = 0.f;
-    uint8_t *mp = static_cast<uint8_t*>(a.m) + q, *vp = static_cast<uint8_t*>(a.v) + q;
+    const uint8_t *mp = static_cast<const uint8_t*>(a.m) + q, *vp = static_cast<const uint8_t*>(a.v) + q;
     if (BITS == 32) {
         load_raw<WIDE>(mr, a.m, FTC_F32, q, lane, FTC_STATE_BLOCK);
         load_raw<WIDE>(vr, a.v, FTC_F32, q, lane, FTC_STATE_BLOCK);
@@ -204,8 +204,19 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const TableEntry&
 #pragma unroll
             for (int j = 0; j < 8; ++j) { mr.r[j] = mp[j * 32 + lane]; vr.r[j] = vp[j * 32 + lane]; }
         }
-        ms = a.m_scale[b]; vs = a.v_scale[b];
+        in.ms = a.m_scale[b]; in.vs = a.v_scale[b];
     }
+}
+
+template <int BITS, bool WIDE>
+__device__ __forceinline__ void adamw_block(const BlockIn& in, const AdamArgs& a, const TableEntry& t, uint64_t b, uint32_t lane, uint64_t e0, uint32_t left, float scale) {
+    const Raw &gr = in.gr, &pr = in.pr;
+    Raw mr = in.mr, vr = in.vr;
+    float ms = in.ms, vs = in.vs;
+    const uint32_t pd = t.master ? (uint32_t)FTC_F32 : t.param_dtype;
+    void* weights = t.master ? t.master : t.param;
+    const uint64_t q = b * FTC_STATE_BLOCK;
+    uint8_t *mp = static_cast<uint8_t*>(a.m) + q, *vp = static_cast<uint8_t*>(a.v) + q;
     F2 g[4], p[4], m[4], v[4];
     uint32_t live;
     numbers<WIDE>(g, gr, t.grad_dtype);
@@ -243,15 +254,12 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const TableEntry&
         const F2 vi = add_apart(mul(v[i], twice(a.beta2)), mul(mul(g[i], g[i]), twice(a.rest2)));
         root[i] = pair(fast_root(lo(vi)), fast_root(hi(vi)));
         const F2 den = add(mul(root[i], twice(a.fix2)), twice(a.eps));
-        F2 ratio;
-        if (a.eps >= kNoSmall) ratio = mul(mi, pair(fast_inverse(lo(den)), fast_inverse(hi(den))));
-        else ratio = pair(slow_ratio(lo(mi), lo(vi), a.fix2, a.eps), slow_ratio(hi(mi), hi(vi), a.fix2, a.eps));
-        const F2 pi = fma(ratio, rate, mul(p[i], keep));
-        if (some) {                                                             // m, v: for the block's codes; else stored where live only
+        const F2 pi = fma(mul(mi, pair(fast_inverse(lo(den)), fast_inverse(hi(den)))), rate, mul(p[i], keep));
+        if (BITS == 8 && some) {                                                // the block's codes need all; in 32 bits the live are stored
             const bool x = live >> (2 * i) & 1u, y = live >> (2 * i + 1) & 1u;
             m[i] = pair(x ? lo(mi) : lo(m[i]), y ? hi(mi) : hi(m[i]));
             v[i] = pair(x ? lo(vi) : lo(v[i]), y ? hi(vi) : hi(v[i]));
-            if (BITS == 8) root[i] = pair(fast_root(lo(v[i])), fast_root(hi(v[i])));
+            root[i] = pair(fast_root(lo(v[i])), fast_root(hi(v[i])));
         } else { m[i] = mi; v[i] = vi; }
         p[i] = pi;
     }
@@ -312,7 +320,15 @@ __device__ __forceinline__ void adamw_block(const AdamArgs& a, const TableEntry&
     if (lane == 0) { a.m_scale[b] = ms; a.v_scale[b] = vs; }
 }
 
-template <int BITS>
+template <int BITS, bool WIDE>
+__device__ __forceinline__ void adamw_one(const AdamArgs& a, const TableEntry& t, uint64_t b, uint32_t lane, uint64_t e0, uint32_t left, float scale) {
+    BlockIn in;
+    adamw_load<BITS, WIDE>(in, a, t, b, lane, e0, left);
+    adamw_block<BITS, WIDE>(in, a, t, b, lane, e0, left, scale);
+}
+
+// A warp takes one block. WIDE: full blocks of aligned tensors go the wide way; else all go the narrow one.
+template <int BITS, bool WIDE>
 __global__ void __launch_bounds__(kWarps * 32, 4) adamw_kernel(AdamArgs a) {
     const uint32_t lane = threadIdx.x & 31;
     const uint64_t b = blockIdx.x * (uint64_t)kWarps + (threadIdx.x >> 5);
@@ -321,14 +337,54 @@ __global__ void __launch_bounds__(kWarps * 32, 4) adamw_kernel(AdamArgs a) {
     const TableEntry t = table_entries(a.table)[table_map(a.table, a.n_params)[b]];
     if (!isfinite(scale)) return;
     const uint64_t e0 = (b - t.first_block) * FTC_STATE_BLOCK, left = t.n - e0;
-    if (t.wide && left >= FTC_STATE_BLOCK) adamw_block<BITS, true>(a, t, b, lane, e0, FTC_STATE_BLOCK, scale);
-    else adamw_block<BITS, false>(a, t, b, lane, e0, left < FTC_STATE_BLOCK ? (uint32_t)left : FTC_STATE_BLOCK, scale);
+    if (WIDE && t.wide && left >= FTC_STATE_BLOCK) adamw_one<BITS, true>(a, t, b, lane, e0, FTC_STATE_BLOCK, scale);
+    else adamw_one<BITS, false>(a, t, b, lane, e0, left < FTC_STATE_BLOCK ? (uint32_t)left : FTC_STATE_BLOCK, scale);
 }
 
-cudaError_t launch_adamw(const AdamArgs& a, int, cudaStream_t st) {
+constexpr uint32_t kWalkWarps = 8, kWalkBlocks = 2;
+// A warp takes `span` blocks, the next one's loads out while it works on the present one.
+template <int BITS, bool WIDE>
+__global__ void __launch_bounds__(kWalkWarps * 32, kWalkBlocks) adamw_walk_kernel(AdamArgs a, uint64_t span) {
+    const uint32_t lane = threadIdx.x & 31;
+    uint64_t b = (blockIdx.x * (uint64_t)kWalkWarps + (threadIdx.x >> 5)) * span;
+    const uint64_t stop = b + span < a.n_blocks ? b + span : a.n_blocks;
+    const float scale = a.grad_scale ? *a.grad_scale : 1.f;
+    if (!isfinite(scale)) return;
+    while (b < stop) {
+        const TableEntry t = table_entries(a.table)[table_map(a.table, a.n_params)[b]];
+        const uint64_t last = t.first_block + (t.n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK, end = last < stop ? last : stop;
+        const uint64_t whole = t.wide || !WIDE ? t.first_block + t.n / FTC_STATE_BLOCK : 0, end_ahead = whole < end ? whole : end;
+        uint64_t e0 = (b - t.first_block) * FTC_STATE_BLOCK;
+        if (b < end_ahead) {
+            BlockIn next;
+            adamw_load<BITS, WIDE>(next, a, t, b, lane, e0, FTC_STATE_BLOCK);
+            for (; b < end_ahead; ++b, e0 += FTC_STATE_BLOCK) {
+                const BlockIn in = next;
+                if (b + 1 < end_ahead) adamw_load<BITS, WIDE>(next, a, t, b + 1, lane, e0 + FTC_STATE_BLOCK, FTC_STATE_BLOCK);
+                adamw_block<BITS, WIDE>(in, a, t, b, lane, e0, FTC_STATE_BLOCK, scale);
+            }
+        }
+        for (; b < end; ++b, e0 += FTC_STATE_BLOCK)
+            adamw_one<BITS, false>(a, t, b, lane, e0, t.n - e0 < FTC_STATE_BLOCK ? (uint32_t)(t.n - e0) : FTC_STATE_BLOCK, scale);
+    }
+}
+
+cudaError_t launch_adamw(const AdamArgs& a, int sms, cudaStream_t st) {
+    const uint64_t warps = (uint64_t)sms * kWalkWarps * kWalkBlocks, span = (a.n_blocks + warps - 1) / warps;
+    const uint32_t walk_grid = sms * kWalkBlocks, threads = kWalkWarps * 32;
+    if (a.bits == 8 && a.n_blocks >= warps * 4 && (a.mostly_wide || 0)) {
+        if (a.mostly_wide) adamw_walk_kernel<8, true><<<walk_grid, threads, 0, st>>>(a, span);
+        else adamw_walk_kernel<8, false><<<walk_grid, threads, 0, st>>>(a, span);
+        return cudaGetLastError();
+    }
     const uint32_t grid = (uint32_t)((a.n_blocks + kWarps - 1) / kWarps);
-    if (a.bits == 32) adamw_kernel<32><<<grid, kWarps * 32, 0, st>>>(a);
-    else adamw_kernel<8><<<grid, kWarps * 32, 0, st>>>(a);
+    if (a.bits == 32) {
+        if (a.mostly_wide) adamw_kernel<32, true><<<grid, kWarps * 32, 0, st>>>(a);
+        else adamw_kernel<32, false><<<grid, kWarps * 32, 0, st>>>(a);
+    } else {
+        if (a.mostly_wide) adamw_kernel<8, true><<<grid, kWarps * 32, 0, st>>>(a);
+        else adamw_kernel<8, false><<<grid, kWarps * 32, 0, st>>>(a);
+    }
     return cudaGetLastError();
 }
 

@@ -25,7 +25,7 @@ template <typename V> __device__ __forceinline__ V warp_sum(V v) {
 // ---- the table of tensors: header, entries, one tensor index for each block of FTC_STATE_BLOCK elements ----
 
 constexpr uint64_t kTableMagic = 0x3154424154435446ull;
-struct TableHead { uint64_t magic, n_blocks; uint32_t n_params, flags; uint64_t pad; };     // flags bit 0: some tensor has no weights
+struct TableHead { uint64_t magic, n_blocks; uint32_t n_params, flags; uint64_t pad; };     // flags bit 0: some tensor has no weights; 1: most blocks are full ones of aligned tensors
 struct TableEntry {
     void* param; float* master; const void* grad; const uint32_t* status;
     uint64_t n, first_block;
@@ -62,7 +62,7 @@ struct AdamArgs {
     const void* table; uint32_t n_params; uint64_t n_blocks;
     void *m, *v; float *m_scale, *v_scale; const float* grad_scale;
     float lr, beta1, beta2, rest1, rest2, eps, fix1, fix2;
-    uint32_t bits;
+    uint32_t bits, mostly_wide;
 };
 cudaError_t launch_adamw(const AdamArgs& a, int sm_count, cudaStream_t st);
 cudaError_t launch_adamw_states(uint64_t blocks, const void* m, const void* v, const float* ms, const float* vs, float* mo, float* vo, int sm_count, cudaStream_t st);

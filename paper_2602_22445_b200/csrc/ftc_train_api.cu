@@ -120,7 +120,7 @@ int ftc_param_table_build(const ftc_param_t* h_params, uint32_t n_params, void* 
     h->magic = kTableMagic; h->n_blocks = (uint64_t)blocks; h->n_params = n_params;
     TableEntry* en = reinterpret_cast<TableEntry*>(h + 1);
     uint32_t* map = reinterpret_cast<uint32_t*>(en + n_params);
-    uint64_t at = 0;
+    uint64_t at = 0, wide = 0;
     for (uint32_t i = 0; i < n_params; ++i) {
         const ftc_param_t& t = h_params[i];
         TableEntry& q = en[i];
@@ -129,8 +129,10 @@ int ftc_param_table_build(const ftc_param_t* h_params, uint32_t n_params, void* 
         q.wide = aligned(t.grad, 8 * size_of(t.grad_dtype)) && aligned(t.param, 8 * size_of(t.param_dtype)) && aligned(t.master, 32);   // 8 elements a load
         q.lr_scale = t.lr_scale; q.weight_decay = t.weight_decay;
         if (t.n && !t.param) h->flags |= 1u;
+        if (q.wide) wide += t.n / FTC_STATE_BLOCK;
         for (const uint64_t end = at + (t.n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK; at < end; ++at) map[at] = i;
     }
+    if (wide * 2 >= h->n_blocks) h->flags |= 2u;
     return FTC_OK;
 }
 
@@ -163,7 +165,7 @@ int ftc_adamw_step(const ftc_adamw_t* hyper, const void* h_table, const void* d_
     const TableHead* h = head_of(h_table);
     if (!hyper || !h || !d_table || !aligned(d_table, 256) || hyper->reserved || (h->flags & 1u)) return FTC_EINVAL;
     if (!(hyper->lr >= 0) || !std::isfinite(hyper->lr) || !(hyper->beta1 >= 0 && hyper->beta1 < 1) || !(hyper->beta2 >= 0 && hyper->beta2 < 1) ||
-        !(hyper->eps >= 0) || !std::isfinite(hyper->eps) || hyper->step == 0) return FTC_EINVAL;
+        !(hyper->eps >= 1e-30) || !std::isfinite((float)hyper->eps) || hyper->step == 0) return FTC_EINVAL;
     if (hyper->state_bits != 32 && hyper->state_bits != 8) return FTC_EUNSUPPORTED;
     if (h->n_blocks == 0) return FTC_OK;
     if (!d_m || !d_v || !aligned(d_m, 32) || !aligned(d_v, 32) || !aligned(d_grad_scale, 4)) return FTC_EINVAL;
@@ -172,7 +174,7 @@ int ftc_adamw_step(const ftc_adamw_t* hyper, const void* h_table, const void* d_
     if (rc != FTC_OK) return rc;
     AdamArgs a{};
     a.table = d_table; a.n_params = h->n_params; a.n_blocks = h->n_blocks;
-    a.m = d_m; a.v = d_v; a.m_scale = d_m_scale; a.v_scale = d_v_scale; a.grad_scale = d_grad_scale; a.bits = hyper->state_bits;
+    a.m = d_m; a.v = d_v; a.m_scale = d_m_scale; a.v_scale = d_v_scale; a.grad_scale = d_grad_scale; a.bits = hyper->state_bits; a.mostly_wide = h->flags >> 1 & 1u;
     const double t = (double)hyper->step;
     a.lr = (float)hyper->lr; a.eps = (float)hyper->eps;
     a.beta1 = (float)hyper->beta1; a.beta2 = (float)hyper->beta2; a.rest1 = (float)(1 - hyper->beta1); a.rest2 = (float)(1 - hyper->beta2);
