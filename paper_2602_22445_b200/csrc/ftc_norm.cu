@@ -159,7 +159,7 @@ static uint32_t row_vector(const NormArgs& a) {
 }
 
 template <typename T, typename W> static cudaError_t forward(const NormArgs& a, int sms, cudaStream_t st) {
-    const cudaError_t e = forward_rows<T, W>(a, row_vector(a), sms, st);
+    const cudaError_t e = forward_rows<T, W>(a, row_vector(a) == 16, sms, st);
     if (e != cudaErrorNotSupported) return e;
     const uint64_t cap = (uint64_t)sms * 8;
     norm_forward_long_kernel<T, W><<<(uint32_t)(a.rows < cap ? a.rows : cap), kThreads, 0, st>>>(a);
@@ -176,7 +176,7 @@ cudaError_t launch_norm_forward(const NormArgs& a, int sms, cudaStream_t st) {
 // (each group writes and the second kernel reads 8 bytes a column: 16 rows keep that under a sixth of the rows' own 96 bytes and more),
 // fewer where their partial sums would take up more than 2 GiB.
 uint32_t norm_backward_groups(uint32_t H, uint64_t rows, int sms) {
-    const uint32_t g = group_threads(H), per_sm = g < 640 ? 640 / g : 1;
+    const uint32_t g = group_threads(H), per_sm = g < 512 ? 512 / g : 1;
     uint64_t n = (uint64_t)sms * per_sm;
     const uint64_t few = rows / 16 > (uint64_t)sms ? rows / 16 : (uint64_t)sms, room = (1ull << 28) / H;
     if (n > few) n = few;
@@ -198,7 +198,7 @@ template <typename T> static cudaError_t columns(const NormArgs& a, cudaStream_t
 }
 
 template <typename T, typename W> static cudaError_t backward(const NormArgs& a, int sms, cudaStream_t st) {
-    const cudaError_t e = backward_rows<T, W>(a, row_vector(a), st);
+    const cudaError_t e = backward_rows<T, W>(a, row_vector(a) == 16, st);
     if (e != cudaErrorNotSupported) return e;
     if (a.slots) { const cudaError_t c = columns<T>(a, st); if (c != cudaSuccess || !a.dx) return c; }
     const uint64_t cap = (uint64_t)sms * 8;

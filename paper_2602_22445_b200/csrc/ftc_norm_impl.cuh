@@ -1,15 +1,17 @@
 // Layer norm on rows that fit the registers of a thread block.
 //
-// A group of G threads (a warp, or a block of up to 512) holds a row, 16 elements a thread: vector i of thread t is vector i*G + t of
-// the row, so every load and store of a warp is one contiguous run. Statistics are taken in two steps from the registers (mean, then
-// squared distances), which no common offset of the row can spoil. A group walks many rows with gamma, beta and the column sums in registers.
+// A group of G threads (a warp, or a block of up to 512) holds a row, 16 elements a thread (rows of at most 512 bytes: one vector), as
+// packed pairs. Vector i of thread t is vector i*G + t of the row, so every load and store of a warp is one contiguous run. Statistics
+// are taken in two steps from the registers (mean, then squared distances), which no common offset of the row can spoil. A group walks
+// many rows with gamma, beta and the column sums in registers.
 //
-// Rows come in through a ring of D rows in shared memory, filled by asynchronous copies (16 or 4 bytes a thread) that run D - 1 rows
-// ahead: what an SM has under way no longer depends on registers. Each thread copies what it reads itself, so the ring needs no barrier. The
-// exception is 16-bit rows that begin between two 4-byte words (ODD: an odd H or stride): their words are copied whole, and a thread
-// shifts its pair of elements out of two neighbouring words, which takes one barrier a row. The word that reaches over the
-// first row's beginning or the last row's end is put together from its one element.
+// Rows come in through a ring of D rows in shared memory, filled by asynchronous copies of 16 bytes that run D - 1 rows ahead: what an SM
+// has under way does not depend on registers. Where all rows begin on 16 bytes each thread copies what it reads itself and the ring
+// needs no barrier. Other rows (SHIFT) are copied with the 16-byte pieces that cover them, and threads read them from where they begin
+// in the ring (16-bit elements: pairs, out of two neighbouring words where a row begins between words), which takes one barrier a
+// row. A piece that reaches over the array's first or last element is put together from the elements inside.
 #pragma once
+#include "ftc_f32x2.cuh"
 #include "ftc_train.cuh"
 
 namespace ftc {
@@ -124,124 +126,192 @@ template <int N> __device__ __forceinline__ void store_slot(const NormArgs& a, u
     }
 }
 
-// Sums over the group. With more than one warp they go through shared memory; `turn` alternates between two places, so that one
-// barrier a call is enough (a place is written again only behind the barrier of the call in between). Places of warps that do not
-// exist hold zeros.
+// Sums over the group, for all its threads. With more than one warp they go through shared memory; `turn` alternates between two places,
+// so that one barrier a call is enough (a place is written again only behind the barrier of the call in between). Places of warps that
+// do not exist hold zeros.
 constexpr int kMaxGroup = 512, kMaxWarps = kMaxGroup / 32;
-struct Scratch { float4 pair[2][kMaxWarps / 2]; };
+struct Scratch { float one[2][2][kMaxWarps]; };
 
 __device__ __forceinline__ void clear_scratch(Scratch& s) {
     const uint32_t t = threadIdx.y * blockDim.x + threadIdx.x;
-    if (t < kMaxWarps) (&s.pair[0][0])[t] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (t < 4 * kMaxWarps) (&s.one[0][0][0])[t] = 0.f;              // blocks have at least 64 threads
     __syncthreads();
 }
-__device__ __forceinline__ float2 group_sum(float2 v, Scratch& scratch, uint32_t& turn) {
+__device__ __forceinline__ float half_warp_sum(float v) {            // of each 16 lanes
 #pragma unroll
-    for (int o = 16; o; o >>= 1) { v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o); v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o); }
-    if (blockDim.x == 32) return v;
-    float4* place = scratch.pair[turn];
-    if ((threadIdx.x & 31) == 0) reinterpret_cast<float2*>(place)[threadIdx.x >> 5] = v;
-    __syncthreads();
-    float2 s = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < kMaxWarps / 2; ++i) { const float4 q = place[i]; s.x += q.x + q.z; s.y += q.y + q.w; }
-    turn ^= 1u;
-    return s;
+    for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
 }
 __device__ __forceinline__ float group_sum(float v, Scratch& scratch, uint32_t& turn) {
-    v = warp_sum(v);
+    v = half_warp_sum(v);
+    v += __shfl_xor_sync(0xFFFFFFFFu, v, 16);
     if (blockDim.x == 32) return v;
-    float4* place = scratch.pair[turn];
-    if ((threadIdx.x & 31) == 0) reinterpret_cast<float*>(place)[threadIdx.x >> 5] = v;
+    float* place = scratch.one[turn][0];
+    if ((threadIdx.x & 31) == 0) place[threadIdx.x >> 5] = v;
     __syncthreads();
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < kMaxWarps / 4; ++i) { const float4 q = place[i]; s += (q.x + q.y) + (q.z + q.w); }
     turn ^= 1u;
-    return s;
+    return half_warp_sum(place[threadIdx.x & (kMaxWarps - 1)]);
+}
+// Two sums at once: after the first exchange the lower half of the warp goes on with x, the upper with y.
+__device__ __forceinline__ float2 group_sum(float2 v, Scratch& scratch, uint32_t& turn) {
+    const bool upper = threadIdx.x & 16;
+    float s = (upper ? v.y : v.x) + __shfl_xor_sync(0xFFFFFFFFu, upper ? v.x : v.y, 16);
+    s = half_warp_sum(s);
+    if (blockDim.x != 32) {
+        float(*place)[kMaxWarps] = scratch.one[turn];
+        if ((threadIdx.x & 15) == 0) place[upper][threadIdx.x >> 5] = s;
+        __syncthreads();
+        turn ^= 1u;
+        s = half_warp_sum(place[upper][threadIdx.x & (kMaxWarps - 1)]);
+    }
+    const float other = __shfl_xor_sync(0xFFFFFFFFu, s, 16);
+    return upper ? make_float2(other, s) : make_float2(s, other);
 }
 __device__ __forceinline__ void group_barrier() { if (blockDim.x == 32) __syncwarp(); else __syncthreads(); }
 
-template <int VB> __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
-    if constexpr (VB == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" :: "r"(dst), "l"(src) : "memory");
+// 1 / sqrt(x): the approximate one and a step of Newton's method (none at 0, infinity and NaN, where the first is right).
+__device__ __forceinline__ float inverse_root(float x) {
+    const float r = rsqrtf(x);
+    return x > 0.f && x < 3e38f ? fmaf(r, fmaf(-0.5f * x * r, r, 0.5f), r) : r;
+}
+
+__device__ __forceinline__ void copy_async_16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void copies_end_batch() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(PENDING) : "memory"); }
 
-// The rows of one array in the ring: NV vectors of VB bytes for each thread, n elements in a row, `rows` rows.
-template <typename T, int VB, int NV, bool ODD> struct RingRows {
-    static constexpr int N = VB / (int)sizeof(T);
-    const T* base;
-    uint64_t stride, rows;
-    uint32_t n, vecs;
+// A thread's part of a row: NV vectors of N elements, E in all, as pairs.
+template <typename T, bool SHIFT, int NV_> struct Part {
+    static constexpr int NV = NV_, N = SHIFT ? (sizeof(T) == 2 ? 2 : 1) : 16 / (int)sizeof(T), E = NV * N, VB = N * (int)sizeof(T);
+    static_assert(E % 2 == 0, "pairs");
     // Bytes that one row takes up in the ring.
-    static __host__ __device__ uint32_t bytes(uint32_t G) { return NV * G * VB + (ODD ? 16 : 0); }
-    __device__ __forceinline__ uint32_t odd(uint64_t r) const { return ODD ? (uint32_t)(reinterpret_cast<uintptr_t>(base + r * stride) >> 1) & 1u : 0u; }
+    static __host__ __device__ uint32_t bytes(uint32_t G) { return NV * G * VB + (SHIFT ? 32 : 0); }
+};
+__device__ __forceinline__ float element(const F2* v, int j) { return j & 1 ? hi(v[j / 2]) : lo(v[j / 2]); }
+
+template <typename T> __device__ __forceinline__ F2 pair_of_word(uint32_t w) {
+    if constexpr (IsBf16<T>::value) return pair(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+    else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w)); return pair(f.x, f.y); }
+}
+
+// The rows of one array on their way through the ring.
+template <typename T, bool SHIFT, int NV> struct RingRows {
+    using P = Part<T, SHIFT, NV>;
+    const T* base;
+    uint64_t stride;
+    uint32_t n, vecs;
+    uintptr_t first, behind;                                          // the array's first byte and the one behind its last
+    __device__ __forceinline__ RingRows(const void* p, uint64_t s, uint64_t rows, uint32_t elements, uint32_t vectors)
+        : base(static_cast<const T*>(p)), stride(s), n(elements), vecs(vectors), first(reinterpret_cast<uintptr_t>(p)),
+          behind(reinterpret_cast<uintptr_t>(base + (rows ? (rows - 1) * s + elements : 0))) {}
+    __device__ __forceinline__ uint32_t start(uint64_t r) const { return SHIFT ? (uint32_t)reinterpret_cast<uintptr_t>(base + r * stride) & 15u : 0u; }
     __device__ __forceinline__ void fetch(char* place, uint64_t r) const {
         const uint32_t dst = (uint32_t)__cvta_generic_to_shared(place);
-        if constexpr (!ODD) {
-            const T* p = base + r * stride;
+        const T* row = base + r * stride;
+        if constexpr (!SHIFT) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const uint32_t q = i * blockDim.x + threadIdx.x;
-                if (q < vecs) copy_async<VB>(dst + q * VB, p + q * N);
+                if (q < vecs) copy_async_16(dst + q * 16, row + q * P::N);
             }
         } else {
-            const uint32_t s = odd(r), words = (s + n + 1) / 2;
-            const T* p = base + r * stride - s;
+            const uint32_t pieces = (start(r) + n * (uint32_t)sizeof(T) + 15) / 16;
+            const uintptr_t from = reinterpret_cast<uintptr_t>(row) & ~(uintptr_t)15;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
+            for (int i = 0; i < NV * P::VB / 16 + 1; ++i) {           // at most that many: the ring row holds NV * G * VB bytes and 32
                 const uint32_t q = i * blockDim.x + threadIdx.x;
-                if (q >= words) continue;
-                if (q == 0 && s && r == 0) reinterpret_cast<uint32_t*>(place)[0] = (uint32_t)reinterpret_cast<const uint16_t*>(p)[1] << 16;
-                else if (q == words - 1 && ((s + n) & 1u) && r + 1 == rows) reinterpret_cast<uint32_t*>(place)[q] = reinterpret_cast<const uint16_t*>(p)[2 * q];
-                else copy_async<4>(dst + q * 4, p + q * 2);
+                if (q >= pieces) continue;
+                const uintptr_t at = from + q * 16;
+                if (at >= first && at + 16 <= behind) copy_async_16(dst + q * 16, reinterpret_cast<const void*>(at));
+                else
+                    for (uintptr_t e = at; e < at + 16; e += sizeof(T))
+                        if (e >= first && e < behind) *reinterpret_cast<T*>(place + q * 16 + (e - at)) = *reinterpret_cast<const T*>(e);
             }
         }
     }
-    // Vector i of this thread; zeros behind the row's end.
-    __device__ __forceinline__ void read(Pack<T, VB>& v, const char* place, int i, uint32_t s) const {
-        const uint32_t q = i * blockDim.x + threadIdx.x;
-        if (q >= vecs) { v.clear(); return; }
-        if constexpr (VB == 16) { const uint4 w = reinterpret_cast<const uint4*>(place)[q]; v.r[0] = w.x; v.r[1] = w.y; v.r[2] = w.z; v.r[3] = w.w; }
-        else if constexpr (!ODD) v.r[0] = reinterpret_cast<const uint32_t*>(place)[q];
-        else {
-            const uint32_t* w = reinterpret_cast<const uint32_t*>(place) + q;
-            v.r[0] = s ? __funnelshift_r(w[0], w[1], 16) : w[0];
-            if (2 * q + 1 >= n) v.r[0] &= 0xFFFFu;                   // an odd row's last element stands alone
+    // This thread's elements of the row in the ring; zeros behind the row's end.
+    __device__ __forceinline__ void read(F2* v, const char* place, uint32_t mis) const {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t q = i * blockDim.x + threadIdx.x;
+            const bool in = q < vecs;
+            if constexpr (!SHIFT) {
+                const uint4 w = in ? reinterpret_cast<const uint4*>(place)[q] : make_uint4(0u, 0u, 0u, 0u);
+                if constexpr (sizeof(T) == 4) {
+                    v[2 * i] = pair(__uint_as_float(w.x), __uint_as_float(w.y));
+                    v[2 * i + 1] = pair(__uint_as_float(w.z), __uint_as_float(w.w));
+                } else {
+                    v[4 * i] = pair_of_word<T>(w.x); v[4 * i + 1] = pair_of_word<T>(w.y);
+                    v[4 * i + 2] = pair_of_word<T>(w.z); v[4 * i + 3] = pair_of_word<T>(w.w);
+                }
+            } else if constexpr (sizeof(T) == 4) {
+                const float x = in ? reinterpret_cast<const float*>(place + mis)[q] : 0.f;
+                v[i / 2] = i & 1 ? pair(lo(v[i / 2]), x) : pair(x, 0.f);
+            } else {
+                const uint32_t* w = reinterpret_cast<const uint32_t*>(place + (mis & 12u)) + q;
+                uint32_t x = 0u;
+                if (in) {
+                    x = mis & 2u ? __funnelshift_r(w[0], w[1], 16) : w[0];
+                    if (2 * q + 1 >= n) x &= 0xFFFFu;                 // an odd row's last element stands alone
+                }
+                v[i] = pair_of_word<T>(x);
+            }
         }
     }
 };
 
-// A vector of results to column c of a row (ODD: a pair that may begin between words, or be one element).
-template <typename T, int VB, bool ODD> __device__ __forceinline__ void store_vector(T* row, uint32_t c, uint32_t n, const float* v) {
-    if constexpr (!ODD) Pack<T, VB>::store(row + c, v);
-    else {
-        if (c + 1 < n && (reinterpret_cast<uintptr_t>(row) & 3u) == 0) { Pack<T, 4>::store(row + c, v); return; }
-        row[c] = from_f32<T>(v[0]);
-        if (c + 1 < n) row[c + 1] = from_f32<T>(v[1]);
+// Vector i of a thread's results to its columns of a row.
+template <typename T, bool SHIFT, int NV> __device__ __forceinline__ void write_row(T* row, const F2* v, uint32_t n, uint32_t vecs) {
+    using P = Part<T, SHIFT, NV>;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint32_t q = i * blockDim.x + threadIdx.x;
+        if (q >= vecs) continue;
+        float o[P::N];
+#pragma unroll
+        for (int j = 0; j < P::N; ++j) o[j] = element(v, i * P::N + j);
+        if constexpr (SHIFT && sizeof(T) == 2) {
+            const uint32_t c = 2 * q;
+            if (c + 1 < n && (reinterpret_cast<uintptr_t>(row) & 3u) == 0) Pack<T, 4>::store(row + c, o);
+            else { row[c] = from_f32<T>(o[0]); if (c + 1 < n) row[c + 1] = from_f32<T>(o[1]); }
+        } else Pack<T, P::VB>::store(row + q * P::N, o);
     }
 }
 
-// Weights of a thread's vector; ODD: of a pair of which the second may not exist.
-template <typename W, int N, bool ODD> __device__ __forceinline__ void vector_weights(float* v, const W* w, uint32_t c, uint32_t n, float other) {
-    if constexpr (!ODD) load_weights<W, N>(v, w, c, other);
-    else { v[0] = w ? to_f32(w[c]) : other; v[1] = w && c + 1 < n ? to_f32(w[c + 1]) : other; }
+// A thread's weights; `other` where there are none or no columns.
+template <typename T, typename W, bool SHIFT, int NV> __device__ __forceinline__ void read_weights(F2* v, const void* weights, float other, uint32_t n, uint32_t vecs) {
+    using P = Part<T, SHIFT, NV>;
+    const W* w = static_cast<const W*>(weights);
+    float f[P::E];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint32_t q = i * blockDim.x + threadIdx.x;
+#pragma unroll
+        for (int j = 0; j < P::N; ++j) f[i * P::N + j] = other;
+        if (q >= vecs) continue;
+        if constexpr (!SHIFT) load_weights<W, P::N>(f + i * P::N, w, q * P::N, other);
+        else if (w) {
+#pragma unroll
+            for (int j = 0; j < P::N; ++j)
+                if (q * P::N + j < n) f[i * P::N + j] = to_f32(w[q * P::N + j]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < P::E / 2; ++j) v[j] = pair(f[2 * j], f[2 * j + 1]);
 }
 
 // blockDim = (G, groups in the block).
-template <typename T, typename W, int VB, int NV, bool ODD, int D>
+template <typename T, typename W, bool SHIFT, int NV, int D>
 __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
-    using V = Pack<T, VB>;
-    using Rows = RingRows<T, VB, NV, ODD>;
-    constexpr int N = V::N;
+    using P = Part<T, SHIFT, NV>;
+    constexpr int H2 = P::E / 2;
     extern __shared__ uint4 ring_memory[];
     __shared__ Scratch scratch;
     uint32_t turn = 0;
-    const uint32_t G = blockDim.x, vecs = (a.H + N - 1) / N, bytes = Rows::bytes(G);
+    const uint32_t G = blockDim.x, vecs = (a.H + P::N - 1) / P::N, bytes = P::bytes(G);
     char* ring = reinterpret_cast<char*>(ring_memory) + threadIdx.y * D * bytes;
-    const Rows in{static_cast<const T*>(a.x), a.x_stride, a.rows, a.H, vecs};
+    const RingRows<T, SHIFT, NV> in(a.x, a.x_stride, a.rows, a.H, vecs);
     const float inv = 1.f / (float)a.H;
     const uint64_t step = (uint64_t)gridDim.x * blockDim.y;
     uint64_t r = (uint64_t)blockIdx.x * blockDim.y + threadIdx.y;
@@ -250,55 +320,48 @@ __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
         if (r + d * step < a.rows) in.fetch(ring + d * bytes, r + d * step);
         copies_end_batch();
     }
-    float g[NV * N], b[NV * N];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const uint32_t q = i * G + threadIdx.x;
-        if (q < vecs) {
-            vector_weights<W, N, ODD>(g + i * N, static_cast<const W*>(a.gamma), q * N, a.H, 1.f);
-            vector_weights<W, N, ODD>(b + i * N, static_cast<const W*>(a.beta), q * N, a.H, 0.f);
-        }
-    }
+    F2 g[H2], b[H2];
+    read_weights<T, W, SHIFT, NV>(g, a.gamma, 1.f, a.H, vecs);
+    read_weights<T, W, SHIFT, NV>(b, a.beta, 0.f, a.H, vecs);
     clear_scratch(scratch);
     uint32_t stage = 0;
     for (; r < a.rows; r += step) {
         copies_wait<D - 2>();
-        if (ODD) group_barrier();
-        V x[NV];
-        const uint32_t s0 = in.odd(r);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) in.read(x[i], ring + stage * bytes, i, s0);
+        if (SHIFT) group_barrier();
+        F2 x[H2];
+        in.read(x, ring + stage * bytes, in.start(r));
         const uint32_t last = stage == 0 ? D - 1 : stage - 1;
         if (r + (D - 1) * step < a.rows) in.fetch(ring + last * bytes, r + (D - 1) * step);
         copies_end_batch();
         stage = stage + 1 == D ? 0 : stage + 1;
-        float s = 0.f;
+        F2 s = x[0];
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int j = 1; j < H2; ++j) s = add(s, x[j]);
+        const float mean = group_sum(lo(s) + hi(s), scratch, turn) * inv;
+        s = twice(0.f);
 #pragma unroll
-            for (int j = 0; j < N; ++j) s += x[i].get(j);
-        const float mean = group_sum(s, scratch, turn) * inv;
-        s = 0.f;
+        for (int j = 0; j < H2; ++j) x[j] = add(x[j], twice(-mean));
+        if constexpr (P::N > 1) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+            for (int i = 0; i < NV; ++i) {
+                const uint32_t q = i * G + threadIdx.x;
+                if (SHIFT && 2 * q + 1 == a.H) x[i] = pair(lo(x[i]), 0.f);
+                if (q < vecs) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const float d = x[i].get(j) - mean;
-                const uint32_t c = (i * G + threadIdx.x) * N + (ODD ? j : 0);
-                if (c < a.H) s = fmaf(d, d, s);
+                    for (int j = i * P::N / 2; j < (i + 1) * P::N / 2; ++j) s = fma(x[j], x[j], s);
+                }
             }
-        const float rstd = 1.f / sqrtf(group_sum(s, scratch, turn) * inv + a.eps);
-        T* y = static_cast<T*>(a.y) + r * a.y_stride;
+        } else {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t q = i * G + threadIdx.x;
-            if (q < vecs) {
-                float o[N];
-#pragma unroll
-                for (int j = 0; j < N; ++j) o[j] = fmaf((x[i].get(j) - mean) * rstd, g[i * N + j], b[i * N + j]);
-                store_vector<T, VB, ODD>(y, q * N, a.H, o);
+            for (int j = 0; j < H2; ++j) {                           // vectors of one element: two of them make a pair
+                if ((2 * j + 1) * G + threadIdx.x >= vecs) x[j] = pair(2 * j * G + threadIdx.x < vecs ? lo(x[j]) : 0.f, 0.f);
+                s = fma(x[j], x[j], s);
             }
         }
+        const float rstd = inverse_root(group_sum(lo(s) + hi(s), scratch, turn) * inv + a.eps);
+#pragma unroll
+        for (int j = 0; j < H2; ++j) x[j] = fma(mul(x[j], twice(rstd)), g[j], b[j]);
+        write_row<T, SHIFT, NV>(static_cast<T*>(a.y) + r * a.y_stride, x, a.H, vecs);
         if (threadIdx.x == 0) {
             if (a.mean_out) a.mean_out[r] = mean;
             if (a.rstd_out) a.rstd_out[r] = rstd;
@@ -307,17 +370,16 @@ __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
 }
 
 // blockDim = (G, groups in the block); a group of threads walks the rows of one RowWalk.
-template <typename T, typename W, int VB, int NV, bool ODD, int D>
+template <typename T, typename W, bool SHIFT, int NV, int D>
 __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
-    using V = Pack<T, VB>;
-    using Rows = RingRows<T, VB, NV, ODD>;
-    constexpr int N = V::N, E = NV * N;
+    using P = Part<T, SHIFT, NV>;
+    constexpr int H2 = P::E / 2;
     extern __shared__ uint4 ring_memory[];
     __shared__ Scratch scratch;
     uint32_t turn = 0;
-    const uint32_t G = blockDim.x, vecs = (a.H + N - 1) / N, bytes = Rows::bytes(G), group = blockIdx.x * blockDim.y + threadIdx.y;
+    const uint32_t G = blockDim.x, vecs = (a.H + P::N - 1) / P::N, bytes = P::bytes(G), group = blockIdx.x * blockDim.y + threadIdx.y;
     char* ring = reinterpret_cast<char*>(ring_memory) + threadIdx.y * D * 2 * bytes;
-    const Rows xs{static_cast<const T*>(a.x), a.x_stride, a.rows, a.H, vecs}, ys{static_cast<const T*>(a.dy), a.dy_stride, a.rows, a.H, vecs};
+    const RingRows<T, SHIFT, NV> xs(a.x, a.x_stride, a.rows, a.H, vecs), ys(a.dy, a.dy_stride, a.rows, a.H, vecs);
     clear_scratch(scratch);
     if (group >= a.groups) return;                                   // whole warps, and in blocks of one group nobody
     RowWalk walk(a, group);
@@ -327,23 +389,22 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
         if (walk.r0 + d < walk.r1) { xs.fetch(ring + 2 * d * bytes, walk.r0 + d); ys.fetch(ring + (2 * d + 1) * bytes, walk.r0 + d); }
         copies_end_batch();
     }
-    float g[E], dg[E], db[E];
+    F2 g[H2], dg[H2], db[H2];
+    read_weights<T, W, SHIFT, NV>(g, a.gamma, 1.f, a.H, vecs);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const uint32_t q = i * G + threadIdx.x;
-#pragma unroll
-        for (int j = 0; j < N; ++j) g[i * N + j] = dg[i * N + j] = db[i * N + j] = 0.f;
-        if (q < vecs) vector_weights<W, N, ODD>(g + i * N, static_cast<const W*>(a.gamma), q * N, a.H, 1.f);
-    }
+    for (int j = 0; j < H2; ++j) dg[j] = db[j] = twice(0.f);
     const auto leave = [&]() {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const uint32_t q = i * G + threadIdx.x;
             if (q >= vecs) continue;
-            if constexpr (!ODD) store_slot<N>(a, walk.slot(), q * N, dg + i * N, db + i * N);
+            float x[P::N], y[P::N];
+#pragma unroll
+            for (int j = 0; j < P::N; ++j) { x[j] = element(dg, i * P::N + j); y[j] = element(db, i * P::N + j); }
+            if constexpr (!SHIFT || sizeof(T) == 4) store_slot<P::N>(a, walk.slot(), q * P::N, x, y);
             else {
-                store_slot<1>(a, walk.slot(), q * 2, dg + i * N, db + i * N);
-                if (q * 2 + 1 < a.H) store_slot<1>(a, walk.slot(), q * 2 + 1, dg + i * N + 1, db + i * N + 1);
+                store_slot<1>(a, walk.slot(), q * 2, x, y);
+                if (q * 2 + 1 < a.H) store_slot<1>(a, walk.slot(), q * 2 + 1, x + 1, y + 1);
             }
         }
     };
@@ -352,60 +413,47 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
     uint32_t stage = 0;
     for (uint64_t r = walk.r0; r < walk.r1; ++r) {
         copies_wait<D - 2>();
-        if (ODD) group_barrier();
-        V x[NV], dy[NV];
-        const uint32_t sx = xs.odd(r), sy = ys.odd(r);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) { xs.read(x[i], ring + 2 * stage * bytes, i, sx); ys.read(dy[i], ring + (2 * stage + 1) * bytes, i, sy); }
+        if (SHIFT) group_barrier();
+        F2 x[H2], dy[H2];
+        xs.read(x, ring + 2 * stage * bytes, xs.start(r));
+        ys.read(dy, ring + (2 * stage + 1) * bytes, ys.start(r));
         const uint32_t last = stage == 0 ? D - 1 : stage - 1;
         if (r + (D - 1) < walk.r1) { xs.fetch(ring + 2 * last * bytes, r + (D - 1)); ys.fetch(ring + (2 * last + 1) * bytes, r + (D - 1)); }
         copies_end_batch();
         stage = stage + 1 == D ? 0 : stage + 1;
         const float mean = nmean, rstd = nrstd;
         if (r + 1 < walk.r1) { nmean = a.mean[r + 1]; nrstd = a.rstd[r + 1]; }
-        float2 s = make_float2(0.f, 0.f);
         if (a.slots && walk.leaves(r)) {
             if (walk.any) leave();
 #pragma unroll
-            for (int j = 0; j < E; ++j) dg[j] = db[j] = 0.f;
+            for (int j = 0; j < H2; ++j) dg[j] = db[j] = twice(0.f);
             walk.go_to(r);
         }
         const bool counts = a.slots && walk.counts(r);
         walk.any |= counts;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int j = 0; j < H2; ++j) x[j] = mul(add(x[j], twice(-mean)), twice(rstd));        // behind the row's end dy = 0 adds nothing
+        if (counts) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) {                            // behind the row's end dy = 0 adds nothing
-                const float d = dy[i].get(j), xh = (x[i].get(j) - mean) * rstd, u = d * g[i * N + j];
-                s.x += u;
-                s.y = fmaf(u, xh, s.y);
-                if (counts) { dg[i * N + j] = fmaf(d, xh, dg[i * N + j]); db[i * N + j] += d; }
-            }
-        if (!a.dx) continue;
-        s = group_sum(s, scratch, turn);
-        const float c1 = s.x * inv, c2 = s.y * inv;
-        T* dx = static_cast<T*>(a.dx) + r * a.dx_stride;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t q = i * G + threadIdx.x;
-            if (q < vecs) {
-                float o[N];
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const float xh = (x[i].get(j) - mean) * rstd;
-                    o[j] = rstd * (fmaf(dy[i].get(j), g[i * N + j], -c1) - xh * c2);
-                }
-                store_vector<T, VB, ODD>(dx, q * N, a.H, o);
-            }
+            for (int j = 0; j < H2; ++j) { dg[j] = fma(dy[j], x[j], dg[j]); db[j] = add(db[j], dy[j]); }
         }
+        if (!a.dx) continue;
+        F2 s1 = twice(0.f), s2 = twice(0.f);
+#pragma unroll
+        for (int j = 0; j < H2; ++j) { dy[j] = mul(dy[j], g[j]); s1 = add(s1, dy[j]); s2 = fma(dy[j], x[j], s2); }
+        const float2 s = group_sum(make_float2(lo(s1) + hi(s1), lo(s2) + hi(s2)), scratch, turn);
+        const F2 c1 = twice(-s.x * inv), c2 = twice(-s.y * inv);
+#pragma unroll
+        for (int j = 0; j < H2; ++j) x[j] = mul(fma(x[j], c2, add(dy[j], c1)), twice(rstd));
+        write_row<T, SHIFT, NV>(static_cast<T*>(a.dx) + r * a.dx_stride, x, a.H, vecs);
     }
     if (a.slots && walk.any) leave();
 }
 
 // Threads that hold a row of H elements, 16 each, and rows of a block of 128 threads where a warp is enough for one.
-static inline uint32_t group_threads(uint32_t H) { return (H / 16 + 1 + 31) / 32 * 32; }
+static inline uint32_t group_threads(uint32_t H) { return (H + 16 * 32 - 1) / (16 * 32) * 32; }
 static inline dim3 group_shape(uint32_t vecs, uint32_t nv) {
-    const uint32_t g = ((vecs + nv - 1) / nv + 31) / 32 * 32;
+    const uint32_t g = (vecs + nv * 32 - 1) / (nv * 32) * 32;
     return dim3(g, g == 32 ? 4 : 1);
 }
 
@@ -413,42 +461,41 @@ template <typename K> static cudaError_t allow_shared(K kernel, size_t bytes) {
     return bytes <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
-template <typename T, typename W, int VB, int NV, bool ODD, int D> static cudaError_t forward_run(const NormArgs& a, int sms, cudaStream_t st) {
-    constexpr uint32_t N = VB / (uint32_t)sizeof(T);
-    const dim3 block = group_shape((a.H + N - 1) / N + (ODD ? 1 : 0), NV);
-    const size_t smem = (size_t)block.y * D * RingRows<T, VB, NV, ODD>::bytes(block.x);
-    const cudaError_t e = allow_shared(norm_forward_kernel<T, W, VB, NV, ODD, D>, smem);
+template <typename T, typename W, bool SHIFT, int NV, int D> static cudaError_t forward_run(const NormArgs& a, int sms, cudaStream_t st) {
+    using P = Part<T, SHIFT, NV>;
+    const dim3 block = group_shape((a.H + P::N - 1) / P::N, NV);
+    const size_t smem = (size_t)block.y * D * P::bytes(block.x);
+    const cudaError_t e = allow_shared(norm_forward_kernel<T, W, SHIFT, NV, D>, smem);
     if (e != cudaSuccess) return e;
-    const uint64_t blocks = (a.rows + block.y - 1) / block.y, cap = (uint64_t)sms * (768 / (block.x * block.y) ? 768 / (block.x * block.y) : 1);
-    norm_forward_kernel<T, W, VB, NV, ODD, D><<<(uint32_t)(blocks < cap ? blocks : cap), block, smem, st>>>(a);
+    const uint32_t threads = block.x * block.y, per_sm = threads < 768 ? 768 / threads : 1;
+    const uint64_t blocks = (a.rows + block.y - 1) / block.y, cap = (uint64_t)sms * per_sm;
+    norm_forward_kernel<T, W, SHIFT, NV, D><<<(uint32_t)(blocks < cap ? blocks : cap), block, smem, st>>>(a);
     return cudaGetLastError();
 }
 
 // cudaErrorNotSupported: the row does not fit.
-template <typename T, typename W> static cudaError_t forward_rows(const NormArgs& a, uint32_t v, int sms, cudaStream_t st) {
-    constexpr int E = sizeof(T), D = E == 2 ? 4 : 3;
-    if (a.H > 16 * kMaxGroup || (v == 2 && a.H > 16 * kMaxGroup - 2)) return cudaErrorNotSupported;
-    if (v == 16) return a.H <= 32 * 16 / E ? forward_run<T, W, 16, 1, false, D>(a, sms, st) : forward_run<T, W, 16, E, false, D>(a, sms, st);
-    if constexpr (E == 4) return forward_run<T, W, 4, 16, false, D>(a, sms, st);
-    else return v == 4 ? forward_run<T, W, 4, 8, false, D>(a, sms, st) : forward_run<T, W, 4, 8, true, D>(a, sms, st);
+template <typename T, typename W> static cudaError_t forward_rows(const NormArgs& a, bool aligned, int sms, cudaStream_t st) {
+    constexpr int e = sizeof(T), D = e == 2 ? 4 : 3;
+    if (a.H > 16 * kMaxGroup) return cudaErrorNotSupported;
+    if (!aligned) return forward_run<T, W, true, e == 2 ? 8 : 16, D>(a, sms, st);
+    return a.H <= 32 * 16 / e ? forward_run<T, W, false, 1, D>(a, sms, st) : forward_run<T, W, false, e, D>(a, sms, st);
 }
 
-template <typename T, typename W, int VB, int NV, bool ODD, int D> static cudaError_t backward_run(const NormArgs& a, cudaStream_t st) {
-    constexpr uint32_t N = VB / (uint32_t)sizeof(T);
-    const dim3 block = group_shape((a.H + N - 1) / N + (ODD ? 1 : 0), NV);
-    const size_t smem = (size_t)block.y * D * 2 * RingRows<T, VB, NV, ODD>::bytes(block.x);
-    const cudaError_t e = allow_shared(norm_backward_kernel<T, W, VB, NV, ODD, D>, smem);
+template <typename T, typename W, bool SHIFT, int NV, int D> static cudaError_t backward_run(const NormArgs& a, cudaStream_t st) {
+    using P = Part<T, SHIFT, NV>;
+    const dim3 block = group_shape((a.H + P::N - 1) / P::N, NV);
+    const size_t smem = (size_t)block.y * D * 2 * P::bytes(block.x);
+    const cudaError_t e = allow_shared(norm_backward_kernel<T, W, SHIFT, NV, D>, smem);
     if (e != cudaSuccess) return e;
-    norm_backward_kernel<T, W, VB, NV, ODD, D><<<(a.groups + block.y - 1) / block.y, block, smem, st>>>(a);
+    norm_backward_kernel<T, W, SHIFT, NV, D><<<(a.groups + block.y - 1) / block.y, block, smem, st>>>(a);
     return cudaGetLastError();
 }
 
-template <typename T, typename W> static cudaError_t backward_rows(const NormArgs& a, uint32_t v, cudaStream_t st) {
-    constexpr int E = sizeof(T), D = E == 2 ? 3 : 2;
-    if (a.H > 16 * kMaxGroup || (v == 2 && a.H > 16 * kMaxGroup - 2)) return cudaErrorNotSupported;
-    if (v == 16) return a.H <= 32 * 16 / E ? backward_run<T, W, 16, 1, false, D>(a, st) : backward_run<T, W, 16, E, false, D>(a, st);
-    if constexpr (E == 4) return backward_run<T, W, 4, 16, false, D>(a, st);
-    else return v == 4 ? backward_run<T, W, 4, 8, false, D>(a, st) : backward_run<T, W, 4, 8, true, D>(a, st);
+template <typename T, typename W> static cudaError_t backward_rows(const NormArgs& a, bool aligned, cudaStream_t st) {
+    constexpr int e = sizeof(T), D = e == 2 ? 3 : 2;
+    if (a.H > 16 * kMaxGroup) return cudaErrorNotSupported;
+    if (!aligned) return backward_run<T, W, true, e == 2 ? 8 : 16, D>(a, st);
+    return a.H <= 32 * 16 / e ? backward_run<T, W, false, 1, D>(a, st) : backward_run<T, W, false, e, D>(a, st);
 }
 
 }  // namespace ftc
