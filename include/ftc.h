@@ -359,7 +359,7 @@ typedef struct {
  *           (with the same stride)
  *   d_gamma, d_beta  [H] of wdtype; NULL: ones, zeros
  *   d_mean, d_rstd   [rows] float32 for the backward pass; either may be NULL
- * Pointers are aligned to their element size; rows that begin on 16-byte boundaries (pointer and stride) with H a multiple
+ * rows is at most 2^31. Pointers are aligned to their element size; rows that begin on 16-byte boundaries (pointer and stride) with H a multiple
  * of 16 bytes are the fast case. rows = 0 is valid and does nothing. FTC_EUNSUPPORTED: another dtype or wdtype.
  */
 FTC_API int ftc_layernorm_forward(const ftc_norm_t* desc, uint64_t rows, const void* d_x, uint64_t x_stride, const void* d_gamma,

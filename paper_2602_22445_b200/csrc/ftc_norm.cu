@@ -79,14 +79,14 @@ __global__ void __launch_bounds__(kThreads) norm_columns_kernel(NormArgs a) {
     if (c >= a.H) return;                                            // N divides H
     RowWalk walk(a, blockIdx.y);
     float dg[N] = {}, db[N] = {};
-    for (uint64_t r = walk.r0; r < walk.r1; r += AHEAD) {
+    for (uint32_t r = walk.r0; r < walk.r1; r += AHEAD) {                // r1 + AHEAD stays below 2^32
         V x[AHEAD], dy[AHEAD];
         float mean[AHEAD], rstd[AHEAD];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)
             if (r + i < walk.r1) {
-                x[i].load(static_cast<const T*>(a.x) + (r + i) * a.x_stride + c);
-                dy[i].load(static_cast<const T*>(a.dy) + (r + i) * a.dy_stride + c);
+                x[i].load(static_cast<const T*>(a.x) + (uint64_t)(r + i) * a.x_stride + c);
+                dy[i].load(static_cast<const T*>(a.dy) + (uint64_t)(r + i) * a.dy_stride + c);
                 mean[i] = a.mean[r + i]; rstd[i] = a.rstd[r + i];
             }
 #pragma unroll
@@ -118,16 +118,16 @@ template <int Q>
 __global__ void __launch_bounds__(256) norm_messages_kernel(NormArgs a, uint32_t tiles) {
     __shared__ float part[2][8][32];
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint64_t item = Q == 8 ? blockIdx.x : blockIdx.x * 8ull + warp, p = item / tiles;
-    const uint32_t h = (uint32_t)(item % tiles) * 32 + lane;
+    const uint64_t item = Q == 8 ? blockIdx.x : blockIdx.x * 8ull + warp;
+    const uint32_t p = (uint32_t)(item / tiles), h = (uint32_t)(item % tiles) * 32 + lane;
     float g = 0.f, b = 0.f;
     if (p < a.P && h < a.H) {
-        const uint64_t lo = first_row(a, p), hi = first_row(a, p + 1);
+        const uint32_t lo = first_row(a, p), hi = first_row(a, p + 1);
         if (lo < hi) {
-            const uint64_t last = (hi - 1) / a.rows_per_group;
+            const uint32_t last = (hi - 1) / a.rows_per_group;
 #pragma unroll 4
-            for (uint64_t grp = lo / a.rows_per_group + (Q == 8 ? warp : 0); grp <= last; grp += Q) {
-                const float* slot = a.slots + (grp + p) * 2 * a.H + h;
+            for (uint32_t grp = lo / a.rows_per_group + (Q == 8 ? warp : 0); grp <= last; grp += Q) {
+                const float* slot = a.slots + ((uint64_t)grp + p) * 2 * a.H + h;
                 g += slot[0];
                 b += slot[a.H];
             }

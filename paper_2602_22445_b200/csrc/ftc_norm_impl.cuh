@@ -77,37 +77,37 @@ template <typename W, int N> __device__ __forceinline__ void load_weights(float*
 }
 
 // First row of process p, at most `rows`.
-__device__ __forceinline__ uint64_t first_row(const NormArgs& a, uint64_t p) {
-    if (!a.splits) return p * a.rows / a.P;
+__device__ __forceinline__ uint32_t first_row(const NormArgs& a, uint32_t p) {
+    if (!a.splits) return (uint32_t)((uint64_t)p * a.rows / a.P);
     const uint64_t s = a.splits[p];
-    return s < a.rows ? s : a.rows;
+    return s < a.rows ? (uint32_t)s : a.rows;
 }
 
 // The rows of group b, and the process that holds the present one.
 struct RowWalk {
     const NormArgs& a;
-    uint64_t r0, r1, start, end;
-    uint32_t b, p;
+    uint32_t r0, r1, start, end, b, p;
     bool any;                                   // the present process has rows here so far
     __device__ __forceinline__ RowWalk(const NormArgs& args, uint32_t group) : a(args), b(group), any(false) {
         r0 = group * a.rows_per_group;
-        r1 = r0 + a.rows_per_group < a.rows ? r0 + a.rows_per_group : a.rows;
-        if (r0 > r1) r0 = r1;
+        r1 = a.rows - r0 < a.rows_per_group ? a.rows : r0 + a.rows_per_group;
+        start = 0; end = ~0u; p = 0;
+        if (!a.slots) return;
         uint32_t lo = 0, hi = a.P;              // the first process that ends behind r0 (P if none does)
         while (lo < hi) {
             const uint32_t mid = (lo + hi) / 2;
-            if (first_row(a, (uint64_t)mid + 1) > r0) hi = mid; else lo = mid + 1;
+            if (first_row(a, mid + 1) > r0) hi = mid; else lo = mid + 1;
         }
         p = lo;
         bounds();
     }
     __device__ __forceinline__ void bounds() {
-        start = p < a.P ? first_row(a, p) : a.rows;
-        end = p < a.P ? first_row(a, (uint64_t)p + 1) : ~0ull;
+        start = p < a.P ? first_row(a, p) : ~0u;
+        end = p < a.P ? first_row(a, p + 1) : ~0u;
     }
-    __device__ __forceinline__ bool leaves(uint64_t r) const { return r >= end; }
-    __device__ __forceinline__ void go_to(uint64_t r) { while (r >= end) { ++p; bounds(); } any = false; }
-    __device__ __forceinline__ bool counts(uint64_t r) const { return r >= start && p < a.P; }
+    __device__ __forceinline__ bool leaves(uint32_t r) const { return r >= end; }
+    __device__ __forceinline__ void go_to(uint32_t r) { while (r >= end) { ++p; bounds(); } any = false; }
+    __device__ __forceinline__ bool counts(uint32_t r) const { return r >= start; }
     __device__ __forceinline__ uint64_t slot() const { return (uint64_t)b + p; }
 };
 
@@ -195,49 +195,56 @@ template <typename T> __device__ __forceinline__ F2 pair_of_word(uint32_t w) {
     else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w)); return pair(f.x, f.y); }
 }
 
-// The rows of one array on their way through the ring.
-template <typename T, bool SHIFT, int NV> struct RingRows {
+// The rows of one array on their way through the ring; FULL: every thread has all its vectors. `row`: the thread's first byte of the present
+// row (SHIFT: the row's first byte).
+template <typename T, bool SHIFT, bool FULL, int NV> struct RingRows {
     using P = Part<T, SHIFT, NV>;
-    const T* base;
-    uint64_t stride;
+    const char* row;
+    uint64_t step, ahead;                                             // bytes to the group's next row, and to the one that is fetched
     uint32_t n, vecs;
-    uintptr_t first, behind;                                          // the array's first byte and the one behind its last
-    __device__ __forceinline__ RingRows(const void* p, uint64_t s, uint64_t rows, uint32_t elements, uint32_t vectors)
-        : base(static_cast<const T*>(p)), stride(s), n(elements), vecs(vectors), first(reinterpret_cast<uintptr_t>(p)),
-          behind(reinterpret_cast<uintptr_t>(base + (rows ? (rows - 1) * s + elements : 0))) {}
-    __device__ __forceinline__ uint32_t start(uint64_t r) const { return SHIFT ? (uint32_t)reinterpret_cast<uintptr_t>(base + r * stride) & 15u : 0u; }
-    __device__ __forceinline__ void fetch(char* place, uint64_t r) const {
-        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(place);
-        const T* row = base + r * stride;
+    uintptr_t first, behind;                                          // SHIFT: the array's first byte and the one behind its last
+    __device__ __forceinline__ RingRows(const void* p, uint64_t stride, uint32_t rows, uint32_t elements, uint32_t vectors, uint32_t r, uint32_t row_step, int rows_ahead)
+        : row(static_cast<const char*>(p) + (r * stride * sizeof(T) + (SHIFT ? 0u : threadIdx.x * 16u))), step(row_step * stride * sizeof(T)),
+          ahead(rows_ahead * step), n(elements), vecs(vectors) {
+        if (SHIFT) {
+            first = reinterpret_cast<uintptr_t>(p);
+            behind = first + ((uint64_t)(rows - 1) * stride + elements) * sizeof(T);
+        }
+    }
+    __device__ __forceinline__ void next() { row += step; }
+    // Copies the row at `from` to `place` (byte offset in the ring).
+    __device__ __forceinline__ void fetch(char* ring, uint32_t place, const char* from) const {
         if constexpr (!SHIFT) {
+            const uint32_t dst = (uint32_t)__cvta_generic_to_shared(ring) + place + threadIdx.x * 16u;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const uint32_t q = i * blockDim.x + threadIdx.x;
-                if (q < vecs) copy_async_16(dst + q * 16, row + q * P::N);
-            }
+            for (int i = 0; i < NV; ++i)
+                if (FULL || i * blockDim.x + threadIdx.x < vecs) copy_async_16(dst + i * blockDim.x * 16u, from + i * blockDim.x * 16u);
         } else {
-            const uint32_t pieces = (start(r) + n * (uint32_t)sizeof(T) + 15) / 16;
-            const uintptr_t from = reinterpret_cast<uintptr_t>(row) & ~(uintptr_t)15;
+            const uint32_t pieces = (((uint32_t)reinterpret_cast<uintptr_t>(from) & 15u) + n * (uint32_t)sizeof(T) + 15) / 16;
+            const uintptr_t begin = reinterpret_cast<uintptr_t>(from) & ~(uintptr_t)15;
+            const uint32_t dst = (uint32_t)__cvta_generic_to_shared(ring) + place;
+            const bool inside = begin >= first && begin + pieces * 16u <= behind;      // all rows but the array's first and last
 #pragma unroll
             for (int i = 0; i < NV * P::VB / 16 + 1; ++i) {           // at most that many: the ring row holds NV * G * VB bytes and 32
                 const uint32_t q = i * blockDim.x + threadIdx.x;
                 if (q >= pieces) continue;
-                const uintptr_t at = from + q * 16;
-                if (at >= first && at + 16 <= behind) copy_async_16(dst + q * 16, reinterpret_cast<const void*>(at));
+                const uintptr_t at = begin + q * 16u;
+                if (inside || (at >= first && at + 16 <= behind)) copy_async_16(dst + q * 16u, reinterpret_cast<const void*>(at));
                 else
-                    for (uintptr_t e = at; e < at + 16; e += sizeof(T))
-                        if (e >= first && e < behind) *reinterpret_cast<T*>(place + q * 16 + (e - at)) = *reinterpret_cast<const T*>(e);
+                    for (uint32_t e = 0; e < 16; e += sizeof(T))
+                        if (at + e >= first && at + e < behind) *reinterpret_cast<T*>(ring + place + q * 16u + e) = *reinterpret_cast<const T*>(at + e);
             }
         }
     }
-    // This thread's elements of the row in the ring; zeros behind the row's end.
-    __device__ __forceinline__ void read(F2* v, const char* place, uint32_t mis) const {
+    // This thread's elements of the present row; zeros behind its end.
+    __device__ __forceinline__ void read(F2* v, const char* ring, uint32_t place) const {
+        const uint32_t mis = SHIFT ? (uint32_t)reinterpret_cast<uintptr_t>(row) & 15u : 0u;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const uint32_t q = i * blockDim.x + threadIdx.x;
-            const bool in = q < vecs;
+            const bool in = FULL || q < vecs;
             if constexpr (!SHIFT) {
-                const uint4 w = in ? reinterpret_cast<const uint4*>(place)[q] : make_uint4(0u, 0u, 0u, 0u);
+                const uint4 w = in ? *reinterpret_cast<const uint4*>(ring + place + q * 16u) : make_uint4(0u, 0u, 0u, 0u);
                 if constexpr (sizeof(T) == 4) {
                     v[2 * i] = pair(__uint_as_float(w.x), __uint_as_float(w.y));
                     v[2 * i + 1] = pair(__uint_as_float(w.z), __uint_as_float(w.w));
@@ -246,10 +253,10 @@ template <typename T, bool SHIFT, int NV> struct RingRows {
                     v[4 * i + 2] = pair_of_word<T>(w.z); v[4 * i + 3] = pair_of_word<T>(w.w);
                 }
             } else if constexpr (sizeof(T) == 4) {
-                const float x = in ? reinterpret_cast<const float*>(place + mis)[q] : 0.f;
+                const float x = in ? *reinterpret_cast<const float*>(ring + place + mis + q * 4u) : 0.f;
                 v[i / 2] = i & 1 ? pair(lo(v[i / 2]), x) : pair(x, 0.f);
             } else {
-                const uint32_t* w = reinterpret_cast<const uint32_t*>(place + (mis & 12u)) + q;
+                const uint32_t* w = reinterpret_cast<const uint32_t*>(ring + place + (mis & 12u) + q * 4u);
                 uint32_t x = 0u;
                 if (in) {
                     x = mis & 2u ? __funnelshift_r(w[0], w[1], 16) : w[0];
@@ -262,12 +269,12 @@ template <typename T, bool SHIFT, int NV> struct RingRows {
 };
 
 // Vector i of a thread's results to its columns of a row.
-template <typename T, bool SHIFT, int NV> __device__ __forceinline__ void write_row(T* row, const F2* v, uint32_t n, uint32_t vecs) {
+template <typename T, bool SHIFT, bool FULL, int NV> __device__ __forceinline__ void write_row(T* row, const F2* v, uint32_t n, uint32_t vecs) {
     using P = Part<T, SHIFT, NV>;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const uint32_t q = i * blockDim.x + threadIdx.x;
-        if (q >= vecs) continue;
+        if (!FULL && q >= vecs) continue;
         float o[P::N];
 #pragma unroll
         for (int j = 0; j < P::N; ++j) o[j] = element(v, i * P::N + j);
@@ -302,7 +309,7 @@ template <typename T, typename W, bool SHIFT, int NV> __device__ __forceinline__
 }
 
 // blockDim = (G, groups in the block).
-template <typename T, typename W, bool SHIFT, int NV, int D>
+template <typename T, typename W, bool SHIFT, bool FULL, int NV, int D>
 __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
     using P = Part<T, SHIFT, NV>;
     constexpr int H2 = P::E / 2;
@@ -311,29 +318,32 @@ __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
     uint32_t turn = 0;
     const uint32_t G = blockDim.x, vecs = (a.H + P::N - 1) / P::N, bytes = P::bytes(G);
     char* ring = reinterpret_cast<char*>(ring_memory) + threadIdx.y * D * bytes;
-    const RingRows<T, SHIFT, NV> in(a.x, a.x_stride, a.rows, a.H, vecs);
     const float inv = 1.f / (float)a.H;
-    const uint64_t step = (uint64_t)gridDim.x * blockDim.y;
-    uint64_t r = (uint64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    const uint32_t step = gridDim.x * blockDim.y, r0 = blockIdx.x * blockDim.y + threadIdx.y;
+    RingRows<T, SHIFT, FULL, NV> in(a.x, a.x_stride, a.rows, a.H, vecs, r0, step, D - 1);
+    T* y = static_cast<T*>(a.y) + r0 * a.y_stride;
+    uint32_t fetched = r0, put = 0, take = 0;
 #pragma unroll
     for (int d = 0; d < D - 1; ++d) {
-        if (r + d * step < a.rows) in.fetch(ring + d * bytes, r + d * step);
+        if (fetched < a.rows) in.fetch(ring, put, in.row + d * in.step);
         copies_end_batch();
+        fetched += step; put += bytes;                               // rows + grid stay below 2^32
     }
     F2 g[H2], b[H2];
     read_weights<T, W, SHIFT, NV>(g, a.gamma, 1.f, a.H, vecs);
     read_weights<T, W, SHIFT, NV>(b, a.beta, 0.f, a.H, vecs);
     clear_scratch(scratch);
-    uint32_t stage = 0;
-    for (; r < a.rows; r += step) {
+    for (uint32_t r = r0; r < a.rows; r += step) {
         copies_wait<D - 2>();
         if (SHIFT) group_barrier();
         F2 x[H2];
-        in.read(x, ring + stage * bytes, in.start(r));
-        const uint32_t last = stage == 0 ? D - 1 : stage - 1;
-        if (r + (D - 1) * step < a.rows) in.fetch(ring + last * bytes, r + (D - 1) * step);
+        in.read(x, ring, take);
+        if (fetched < a.rows) in.fetch(ring, put, in.row + in.ahead);
         copies_end_batch();
-        stage = stage + 1 == D ? 0 : stage + 1;
+        fetched += step;
+        put = take;
+        take = take + bytes == D * bytes ? 0 : take + bytes;
+        in.next();
         F2 s = x[0];
 #pragma unroll
         for (int j = 1; j < H2; ++j) s = add(s, x[j]);
@@ -346,7 +356,7 @@ __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
             for (int i = 0; i < NV; ++i) {
                 const uint32_t q = i * G + threadIdx.x;
                 if (SHIFT && 2 * q + 1 == a.H) x[i] = pair(lo(x[i]), 0.f);
-                if (q < vecs) {
+                if (FULL || q < vecs) {
 #pragma unroll
                     for (int j = i * P::N / 2; j < (i + 1) * P::N / 2; ++j) s = fma(x[j], x[j], s);
                 }
@@ -361,7 +371,8 @@ __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
         const float rstd = inverse_root(group_sum(lo(s) + hi(s), scratch, turn) * inv + a.eps);
 #pragma unroll
         for (int j = 0; j < H2; ++j) x[j] = fma(mul(x[j], twice(rstd)), g[j], b[j]);
-        write_row<T, SHIFT, NV>(static_cast<T*>(a.y) + r * a.y_stride, x, a.H, vecs);
+        write_row<T, SHIFT, FULL, NV>(y, x, a.H, vecs);
+        y += step * a.y_stride;
         if (threadIdx.x == 0) {
             if (a.mean_out) a.mean_out[r] = mean;
             if (a.rstd_out) a.rstd_out[r] = rstd;
@@ -370,7 +381,7 @@ __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
 }
 
 // blockDim = (G, groups in the block); a group of threads walks the rows of one RowWalk.
-template <typename T, typename W, bool SHIFT, int NV, int D>
+template <typename T, typename W, bool SHIFT, bool FULL, int NV, int D>
 __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
     using P = Part<T, SHIFT, NV>;
     constexpr int H2 = P::E / 2;
@@ -379,15 +390,18 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
     uint32_t turn = 0;
     const uint32_t G = blockDim.x, vecs = (a.H + P::N - 1) / P::N, bytes = P::bytes(G), group = blockIdx.x * blockDim.y + threadIdx.y;
     char* ring = reinterpret_cast<char*>(ring_memory) + threadIdx.y * D * 2 * bytes;
-    const RingRows<T, SHIFT, NV> xs(a.x, a.x_stride, a.rows, a.H, vecs), ys(a.dy, a.dy_stride, a.rows, a.H, vecs);
     clear_scratch(scratch);
     if (group >= a.groups) return;                                   // whole warps, and in blocks of one group nobody
     RowWalk walk(a, group);
+    RingRows<T, SHIFT, FULL, NV> xs(a.x, a.x_stride, a.rows, a.H, vecs, walk.r0, 1, D - 1), ys(a.dy, a.dy_stride, a.rows, a.H, vecs, walk.r0, 1, D - 1);
+    T* dx = static_cast<T*>(a.dx) + walk.r0 * a.dx_stride;
     const float inv = 1.f / (float)a.H;
+    uint32_t put = 0, take = 0;
 #pragma unroll
     for (int d = 0; d < D - 1; ++d) {
-        if (walk.r0 + d < walk.r1) { xs.fetch(ring + 2 * d * bytes, walk.r0 + d); ys.fetch(ring + (2 * d + 1) * bytes, walk.r0 + d); }
+        if (walk.r0 + d < walk.r1) { xs.fetch(ring, put, xs.row + d * xs.step); ys.fetch(ring, put + bytes, ys.row + d * ys.step); }
         copies_end_batch();
+        put += 2 * bytes;
     }
     F2 g[H2], dg[H2], db[H2];
     read_weights<T, W, SHIFT, NV>(g, a.gamma, 1.f, a.H, vecs);
@@ -397,7 +411,7 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const uint32_t q = i * G + threadIdx.x;
-            if (q >= vecs) continue;
+            if (!FULL && q >= vecs) continue;
             float x[P::N], y[P::N];
 #pragma unroll
             for (int j = 0; j < P::N; ++j) { x[j] = element(dg, i * P::N + j); y[j] = element(db, i * P::N + j); }
@@ -408,19 +422,18 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
             }
         }
     };
-    float nmean = 0.f, nrstd = 0.f;
-    if (walk.r0 < walk.r1) { nmean = a.mean[walk.r0]; nrstd = a.rstd[walk.r0]; }
-    uint32_t stage = 0;
-    for (uint64_t r = walk.r0; r < walk.r1; ++r) {
+    float nmean = a.mean[walk.r0], nrstd = a.rstd[walk.r0];
+    for (uint32_t r = walk.r0; r < walk.r1; ++r) {
         copies_wait<D - 2>();
         if (SHIFT) group_barrier();
         F2 x[H2], dy[H2];
-        xs.read(x, ring + 2 * stage * bytes, xs.start(r));
-        ys.read(dy, ring + (2 * stage + 1) * bytes, ys.start(r));
-        const uint32_t last = stage == 0 ? D - 1 : stage - 1;
-        if (r + (D - 1) < walk.r1) { xs.fetch(ring + 2 * last * bytes, r + (D - 1)); ys.fetch(ring + (2 * last + 1) * bytes, r + (D - 1)); }
+        xs.read(x, ring, take);
+        ys.read(dy, ring, take + bytes);
+        if (r + (D - 1) < walk.r1) { xs.fetch(ring, put, xs.row + xs.ahead); ys.fetch(ring, put + bytes, ys.row + ys.ahead); }
         copies_end_batch();
-        stage = stage + 1 == D ? 0 : stage + 1;
+        put = take;
+        take = take + 2 * bytes == D * 2 * bytes ? 0 : take + 2 * bytes;
+        xs.next(); ys.next();
         const float mean = nmean, rstd = nrstd;
         if (r + 1 < walk.r1) { nmean = a.mean[r + 1]; nrstd = a.rstd[r + 1]; }
         if (a.slots && walk.leaves(r)) {
@@ -445,7 +458,8 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
         const F2 c1 = twice(-s.x * inv), c2 = twice(-s.y * inv);
 #pragma unroll
         for (int j = 0; j < H2; ++j) x[j] = mul(fma(x[j], c2, add(dy[j], c1)), twice(rstd));
-        write_row<T, SHIFT, NV>(static_cast<T*>(a.dx) + r * a.dx_stride, x, a.H, vecs);
+        write_row<T, SHIFT, FULL, NV>(dx, x, a.H, vecs);
+        dx += a.dx_stride;
     }
     if (a.slots && walk.any) leave();
 }
@@ -461,16 +475,21 @@ template <typename K> static cudaError_t allow_shared(K kernel, size_t bytes) {
     return bytes <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
+template <typename T, typename W, bool SHIFT, bool FULL, int NV, int D> static cudaError_t forward_launch(const NormArgs& a, dim3 block, int sms, cudaStream_t st) {
+    const size_t smem = (size_t)block.y * D * Part<T, SHIFT, NV>::bytes(block.x);
+    const cudaError_t e = allow_shared(norm_forward_kernel<T, W, SHIFT, FULL, NV, D>, smem);
+    if (e != cudaSuccess) return e;
+    const uint32_t threads = block.x * block.y, per_sm = threads < 768 ? 768 / threads : 1;
+    const uint32_t blocks = (a.rows + block.y - 1) / block.y, cap = (uint32_t)sms * per_sm;
+    norm_forward_kernel<T, W, SHIFT, FULL, NV, D><<<blocks < cap ? blocks : cap, block, smem, st>>>(a);
+    return cudaGetLastError();
+}
 template <typename T, typename W, bool SHIFT, int NV, int D> static cudaError_t forward_run(const NormArgs& a, int sms, cudaStream_t st) {
     using P = Part<T, SHIFT, NV>;
     const dim3 block = group_shape((a.H + P::N - 1) / P::N, NV);
-    const size_t smem = (size_t)block.y * D * P::bytes(block.x);
-    const cudaError_t e = allow_shared(norm_forward_kernel<T, W, SHIFT, NV, D>, smem);
-    if (e != cudaSuccess) return e;
-    const uint32_t threads = block.x * block.y, per_sm = threads < 768 ? 768 / threads : 1;
-    const uint64_t blocks = (a.rows + block.y - 1) / block.y, cap = (uint64_t)sms * per_sm;
-    norm_forward_kernel<T, W, SHIFT, NV, D><<<(uint32_t)(blocks < cap ? blocks : cap), block, smem, st>>>(a);
-    return cudaGetLastError();
+    if constexpr (!SHIFT)
+        if (a.H == NV * P::N * block.x) return forward_launch<T, W, SHIFT, true, NV, D>(a, block, sms, st);
+    return forward_launch<T, W, SHIFT, false, NV, D>(a, block, sms, st);
 }
 
 // cudaErrorNotSupported: the row does not fit.
@@ -481,14 +500,19 @@ template <typename T, typename W> static cudaError_t forward_rows(const NormArgs
     return a.H <= 32 * 16 / e ? forward_run<T, W, false, 1, D>(a, sms, st) : forward_run<T, W, false, e, D>(a, sms, st);
 }
 
+template <typename T, typename W, bool SHIFT, bool FULL, int NV, int D> static cudaError_t backward_launch(const NormArgs& a, dim3 block, cudaStream_t st) {
+    const size_t smem = (size_t)block.y * D * 2 * Part<T, SHIFT, NV>::bytes(block.x);
+    const cudaError_t e = allow_shared(norm_backward_kernel<T, W, SHIFT, FULL, NV, D>, smem);
+    if (e != cudaSuccess) return e;
+    norm_backward_kernel<T, W, SHIFT, FULL, NV, D><<<(a.groups + block.y - 1) / block.y, block, smem, st>>>(a);
+    return cudaGetLastError();
+}
 template <typename T, typename W, bool SHIFT, int NV, int D> static cudaError_t backward_run(const NormArgs& a, cudaStream_t st) {
     using P = Part<T, SHIFT, NV>;
     const dim3 block = group_shape((a.H + P::N - 1) / P::N, NV);
-    const size_t smem = (size_t)block.y * D * 2 * P::bytes(block.x);
-    const cudaError_t e = allow_shared(norm_backward_kernel<T, W, SHIFT, NV, D>, smem);
-    if (e != cudaSuccess) return e;
-    norm_backward_kernel<T, W, SHIFT, NV, D><<<(a.groups + block.y - 1) / block.y, block, smem, st>>>(a);
-    return cudaGetLastError();
+    if constexpr (!SHIFT)
+        if (a.H == NV * P::N * block.x) return backward_launch<T, W, SHIFT, true, NV, D>(a, block, st);
+    return backward_launch<T, W, SHIFT, false, NV, D>(a, block, st);
 }
 
 template <typename T, typename W> static cudaError_t backward_rows(const NormArgs& a, bool aligned, cudaStream_t st) {

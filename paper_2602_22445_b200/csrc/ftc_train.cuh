@@ -49,8 +49,8 @@ struct NormArgs {
     const float *mean, *rstd;
     const uint64_t* splits;
     float *dgamma, *dbeta, *slots;
-    uint64_t rows, x_stride, y_stride, dy_stride, dx_stride, rows_per_group;
-    uint32_t H, P, k, dtype, wdtype, groups;
+    uint64_t x_stride, y_stride, dy_stride, dx_stride;
+    uint32_t rows, H, P, k, dtype, wdtype, groups, rows_per_group;
     float eps;
 };
 cudaError_t launch_norm_forward(const NormArgs& a, int sm_count, cudaStream_t st);

@@ -20,7 +20,7 @@ int status(cudaError_t e) { return e == cudaSuccess ? FTC_OK : FTC_ECUDA; }
 int check_norm(const ftc_norm_t* d, uint64_t rows) {
     if (!d) return FTC_EINVAL;
     if (!is_float(d->dtype) || (d->wdtype != FTC_F32 && d->wdtype != d->dtype)) return FTC_EUNSUPPORTED;
-    if (d->H == 0 || d->H > (1u << 24) || d->P == 0 || d->P > (1u << 20) || d->k == 0 || d->k > (1u << 24) || !(d->eps >= 0.f) || rows > (1ull << 40))
+    if (d->H == 0 || d->H > (1u << 24) || d->P == 0 || d->P > (1u << 20) || d->k == 0 || d->k > (1u << 24) || !(d->eps >= 0.f) || rows > (1ull << 31))
         return FTC_EINVAL;
     return FTC_OK;
 }
@@ -69,7 +69,7 @@ int ftc_layernorm_forward(const ftc_norm_t* desc, uint64_t rows, const void* d_x
     if ((rc = sm_count(sms)) != FTC_OK) return rc;
     NormArgs a{};
     a.x = d_x; a.gamma = d_gamma; a.beta = d_beta; a.y = d_y; a.mean_out = d_mean; a.rstd_out = d_rstd;
-    a.rows = rows; a.x_stride = x_stride; a.y_stride = y_stride;
+    a.rows = (uint32_t)rows; a.x_stride = x_stride; a.y_stride = y_stride;
     a.H = desc->H; a.dtype = desc->dtype; a.wdtype = desc->wdtype; a.eps = desc->eps;
     return status(launch_norm_forward(a, sms, static_cast<cudaStream_t>(cuda_stream)));
 }
@@ -100,10 +100,10 @@ int ftc_layernorm_backward(const ftc_norm_t* desc, uint64_t rows, const void* d_
     NormArgs a{};
     a.x = d_x; a.dy = d_dy; a.gamma = d_gamma; a.mean = d_mean; a.rstd = d_rstd; a.splits = d_row_splits; a.dx = d_dx;
     a.dgamma = d_dgamma; a.dbeta = d_dbeta; a.slots = weights ? static_cast<float*>(d_workspace) : nullptr;
-    a.rows = rows; a.x_stride = x_stride; a.dy_stride = dy_stride; a.dx_stride = dx_stride;
+    a.rows = (uint32_t)rows; a.x_stride = x_stride; a.dy_stride = dy_stride; a.dx_stride = dx_stride;
     a.H = desc->H; a.P = desc->P; a.k = desc->k; a.dtype = desc->dtype; a.wdtype = desc->wdtype; a.eps = desc->eps;
     a.groups = norm_backward_groups(desc->H, rows, sms);
-    a.rows_per_group = a.groups ? (rows + a.groups - 1) / a.groups : 0;
+    a.rows_per_group = a.groups ? (uint32_t)((rows + a.groups - 1) / a.groups) : 0;
     return status(launch_norm_backward(a, sms, static_cast<cudaStream_t>(cuda_stream)));
 }
 
