@@ -155,11 +155,11 @@ static uint32_t row_vector(const NormArgs& a) {
     const uint64_t strides = (a.x_stride | a.y_stride | a.dy_stride | a.dx_stride | a.H) * e;
     const auto fits = [&](uint32_t v) { return strides % v == 0 && on(a.x, v) && on(a.y, v) && on(a.dy, v) && on(a.dx, v); };
     if (fits(16) && on(a.gamma, 16) && on(a.beta, 16)) return 16;
-    return fits(4) && on(a.gamma, 8) && on(a.beta, 8) ? 4 : e;
+    return fits(4) ? 4 : e;
 }
 
 template <typename T, typename W> static cudaError_t forward(const NormArgs& a, int sms, cudaStream_t st) {
-    const cudaError_t e = forward_rows<T, W>(a, row_vector(a) == 16, sms, st);
+    const cudaError_t e = forward_rows<T, W>(a, row_vector(a), sms, st);
     if (e != cudaErrorNotSupported) return e;
     const uint64_t cap = (uint64_t)sms * 8;
     norm_forward_long_kernel<T, W><<<(uint32_t)(a.rows < cap ? a.rows : cap), kThreads, 0, st>>>(a);
@@ -198,7 +198,7 @@ template <typename T> static cudaError_t columns(const NormArgs& a, cudaStream_t
 }
 
 template <typename T, typename W> static cudaError_t backward(const NormArgs& a, int sms, cudaStream_t st) {
-    const cudaError_t e = backward_rows<T, W>(a, row_vector(a) == 16, st);
+    const cudaError_t e = backward_rows<T, W>(a, row_vector(a), st);
     if (e != cudaErrorNotSupported) return e;
     if (a.slots) { const cudaError_t c = columns<T>(a, st); if (c != cudaSuccess || !a.dx) return c; }
     const uint64_t cap = (uint64_t)sms * 8;

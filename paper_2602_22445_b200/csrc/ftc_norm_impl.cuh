@@ -7,9 +7,9 @@
 //
 // Rows come in through a ring of D rows in shared memory, filled by asynchronous copies of 16 bytes that run D - 1 rows ahead: what an SM
 // has under way does not depend on registers. Where all rows begin on 16 bytes each thread copies what it reads itself and the ring
-// needs no barrier. Other rows (SHIFT) are copied with the 16-byte pieces that cover them, and threads read them from where they begin
-// in the ring (16-bit elements: pairs, out of two neighbouring words where a row begins between words), which takes one barrier a
-// row. A piece that reaches over the array's first or last element is put together from the elements inside.
+// needs no barrier. Other rows are copied with the 16-byte pieces that cover them, and threads read them word by word from where they
+// begin in the ring (kWords), 16-bit elements that begin or end between words as pairs out of two neighbouring words (kOdd); this takes
+// one barrier a row. A piece that reaches over the array's first or last element is put together from the elements inside.
 #pragma once
 #include "ftc_f32x2.cuh"
 #include "ftc_train.cuh"
@@ -114,6 +114,13 @@ struct RowWalk {
 template <int N> __device__ __forceinline__ void store_slot(const NormArgs& a, uint64_t slot, uint32_t c, const float* dg, const float* db) {
     float* g = a.slots + slot * 2 * a.H + c;
     float* b = g + a.H;
+    if constexpr (N == 2) {                     // of an odd H every second slot begins between pairs
+        if ((a.H & 1u) == 0) {
+            *reinterpret_cast<float2*>(g) = make_float2(dg[0], dg[1]);
+            *reinterpret_cast<float2*>(b) = make_float2(db[0], db[1]);
+            return;
+        }
+    }
     if constexpr (N % 4 == 0) {                 // N divides H, the workspace begins on 16 bytes
 #pragma unroll
         for (int j = 0; j < N; j += 4) {
@@ -182,7 +189,10 @@ __device__ __forceinline__ void copies_end_batch() { asm volatile("cp.async.comm
 template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(PENDING) : "memory"); }
 
 // A thread's part of a row: NV vectors of N elements, E in all, as pairs.
-template <typename T, bool SHIFT, int NV_> struct Part {
+enum Mode { kAligned, kWords, kOdd };
+
+template <typename T, int MODE, int NV_> struct Part {
+    static constexpr bool SHIFT = MODE != kAligned;
     static constexpr int NV = NV_, N = SHIFT ? (sizeof(T) == 2 ? 2 : 1) : 16 / (int)sizeof(T), E = NV * N, VB = N * (int)sizeof(T);
     static_assert(E % 2 == 0, "pairs");
     // Bytes that one row takes up in the ring.
@@ -197,8 +207,9 @@ template <typename T> __device__ __forceinline__ F2 pair_of_word(uint32_t w) {
 
 // The rows of one array on their way through the ring; FULL: every thread has all its vectors. `row`: the thread's first byte of the present
 // row (SHIFT: the row's first byte).
-template <typename T, bool SHIFT, bool FULL, int NV> struct RingRows {
-    using P = Part<T, SHIFT, NV>;
+template <typename T, int MODE, bool FULL, int NV> struct RingRows {
+    using P = Part<T, MODE, NV>;
+    static constexpr bool SHIFT = MODE != kAligned;
     const char* row;
     uint64_t step, ahead;                                             // bytes to the group's next row, and to the one that is fetched
     uint32_t n, vecs;
@@ -259,8 +270,11 @@ template <typename T, bool SHIFT, bool FULL, int NV> struct RingRows {
                 const uint32_t* w = reinterpret_cast<const uint32_t*>(ring + place + (mis & 12u) + q * 4u);
                 uint32_t x = 0u;
                 if (in) {
-                    x = mis & 2u ? __funnelshift_r(w[0], w[1], 16) : w[0];
-                    if (2 * q + 1 >= n) x &= 0xFFFFu;                 // an odd row's last element stands alone
+                    x = w[0];
+                    if constexpr (MODE == kOdd) {
+                        if (mis & 2u) x = __funnelshift_r(x, w[1], 16);
+                        if (q == n / 2) x &= 0xFFFFu;                 // an odd row's last element stands alone
+                    }
                 }
                 v[i] = pair_of_word<T>(x);
             }
@@ -269,8 +283,9 @@ template <typename T, bool SHIFT, bool FULL, int NV> struct RingRows {
 };
 
 // Vector i of a thread's results to its columns of a row.
-template <typename T, bool SHIFT, bool FULL, int NV> __device__ __forceinline__ void write_row(T* row, const F2* v, uint32_t n, uint32_t vecs) {
-    using P = Part<T, SHIFT, NV>;
+template <typename T, int MODE, bool FULL, int NV> __device__ __forceinline__ void write_row(T* row, const F2* v, uint32_t n, uint32_t vecs) {
+    using P = Part<T, MODE, NV>;
+    const bool between = MODE == kOdd && (reinterpret_cast<uintptr_t>(row) & 2u);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const uint32_t q = i * blockDim.x + threadIdx.x;
@@ -278,18 +293,18 @@ template <typename T, bool SHIFT, bool FULL, int NV> __device__ __forceinline__ 
         float o[P::N];
 #pragma unroll
         for (int j = 0; j < P::N; ++j) o[j] = element(v, i * P::N + j);
-        if constexpr (SHIFT && sizeof(T) == 2) {
-            const uint32_t c = 2 * q;
-            if (c + 1 < n && (reinterpret_cast<uintptr_t>(row) & 3u) == 0) Pack<T, 4>::store(row + c, o);
-            else { row[c] = from_f32<T>(o[0]); if (c + 1 < n) row[c + 1] = from_f32<T>(o[1]); }
+        if (MODE == kOdd && (between || q == n / 2)) {
+            row[2 * q] = from_f32<T>(o[0]);
+            if (q != n / 2) row[2 * q + 1] = from_f32<T>(o[1 % P::N]);
         } else Pack<T, P::VB>::store(row + q * P::N, o);
     }
 }
 
 // A thread's weights; `other` where there are none or no columns.
-template <typename T, typename W, bool SHIFT, int NV> __device__ __forceinline__ void read_weights(F2* v, const void* weights, float other, uint32_t n, uint32_t vecs) {
-    using P = Part<T, SHIFT, NV>;
+template <typename T, typename W, int MODE, int NV> __device__ __forceinline__ void read_weights(F2* v, const void* weights, float other, uint32_t n, uint32_t vecs) {
+    using P = Part<T, MODE, NV>;
     const W* w = static_cast<const W*>(weights);
+    const bool pairs = P::N == 2 && (reinterpret_cast<uintptr_t>(w) & (2 * sizeof(W) - 1)) == 0;
     float f[P::E];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -297,11 +312,15 @@ template <typename T, typename W, bool SHIFT, int NV> __device__ __forceinline__
 #pragma unroll
         for (int j = 0; j < P::N; ++j) f[i * P::N + j] = other;
         if (q >= vecs) continue;
-        if constexpr (!SHIFT) load_weights<W, P::N>(f + i * P::N, w, q * P::N, other);
+        if constexpr (MODE == kAligned || P::N == 1) load_weights<W, P::N>(f + i * P::N, w, q * P::N, other);
         else if (w) {
-#pragma unroll
-            for (int j = 0; j < P::N; ++j)
-                if (q * P::N + j < n) f[i * P::N + j] = to_f32(w[q * P::N + j]);
+            if (pairs && (MODE != kOdd || q != n / 2)) {
+                if constexpr (sizeof(W) == 4) { const float2 x = *reinterpret_cast<const float2*>(w + 2 * q); f[2 * i] = x.x; f[2 * i + 1] = x.y; }
+                else { Pack<W, 4> x; x.load(w + 2 * q); f[2 * i] = x.get(0); f[2 * i + 1] = x.get(1); }
+            } else {
+                f[2 * i] = to_f32(w[2 * q]);
+                if (2 * q + 1 < n) f[2 * i + 1] = to_f32(w[2 * q + 1]);
+            }
         }
     }
 #pragma unroll
@@ -309,9 +328,10 @@ template <typename T, typename W, bool SHIFT, int NV> __device__ __forceinline__
 }
 
 // blockDim = (G, groups in the block).
-template <typename T, typename W, bool SHIFT, bool FULL, int NV, int D>
+template <typename T, typename W, int MODE, bool FULL, int NV, int D>
 __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
-    using P = Part<T, SHIFT, NV>;
+    using P = Part<T, MODE, NV>;
+    constexpr bool SHIFT = MODE != kAligned;
     constexpr int H2 = P::E / 2;
     extern __shared__ uint4 ring_memory[];
     __shared__ Scratch scratch;
@@ -320,7 +340,7 @@ __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
     char* ring = reinterpret_cast<char*>(ring_memory) + threadIdx.y * D * bytes;
     const float inv = 1.f / (float)a.H;
     const uint32_t step = gridDim.x * blockDim.y, r0 = blockIdx.x * blockDim.y + threadIdx.y;
-    RingRows<T, SHIFT, FULL, NV> in(a.x, a.x_stride, a.rows, a.H, vecs, r0, step, D - 1);
+    RingRows<T, MODE, FULL, NV> in(a.x, a.x_stride, a.rows, a.H, vecs, r0, step, D - 1);
     T* y = static_cast<T*>(a.y) + r0 * a.y_stride;
     uint32_t fetched = r0, put = 0, take = 0;
 #pragma unroll
@@ -330,8 +350,8 @@ __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
         fetched += step; put += bytes;                               // rows + grid stay below 2^32
     }
     F2 g[H2], b[H2];
-    read_weights<T, W, SHIFT, NV>(g, a.gamma, 1.f, a.H, vecs);
-    read_weights<T, W, SHIFT, NV>(b, a.beta, 0.f, a.H, vecs);
+    read_weights<T, W, MODE, NV>(g, a.gamma, 1.f, a.H, vecs);
+    read_weights<T, W, MODE, NV>(b, a.beta, 0.f, a.H, vecs);
     clear_scratch(scratch);
     for (uint32_t r = r0; r < a.rows; r += step) {
         copies_wait<D - 2>();
@@ -355,7 +375,7 @@ __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const uint32_t q = i * G + threadIdx.x;
-                if (SHIFT && 2 * q + 1 == a.H) x[i] = pair(lo(x[i]), 0.f);
+                if (MODE == kOdd && 2 * q + 1 == a.H) x[i] = pair(lo(x[i]), 0.f);
                 if (FULL || q < vecs) {
 #pragma unroll
                     for (int j = i * P::N / 2; j < (i + 1) * P::N / 2; ++j) s = fma(x[j], x[j], s);
@@ -371,7 +391,7 @@ __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
         const float rstd = inverse_root(group_sum(lo(s) + hi(s), scratch, turn) * inv + a.eps);
 #pragma unroll
         for (int j = 0; j < H2; ++j) x[j] = fma(mul(x[j], twice(rstd)), g[j], b[j]);
-        write_row<T, SHIFT, FULL, NV>(y, x, a.H, vecs);
+        write_row<T, MODE, FULL, NV>(y, x, a.H, vecs);
         y += step * a.y_stride;
         if (threadIdx.x == 0) {
             if (a.mean_out) a.mean_out[r] = mean;
@@ -381,9 +401,10 @@ __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
 }
 
 // blockDim = (G, groups in the block); a group of threads walks the rows of one RowWalk.
-template <typename T, typename W, bool SHIFT, bool FULL, int NV, int D>
+template <typename T, typename W, int MODE, bool FULL, int NV, int D>
 __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
-    using P = Part<T, SHIFT, NV>;
+    using P = Part<T, MODE, NV>;
+    constexpr bool SHIFT = MODE != kAligned;
     constexpr int H2 = P::E / 2;
     extern __shared__ uint4 ring_memory[];
     __shared__ Scratch scratch;
@@ -393,7 +414,7 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
     clear_scratch(scratch);
     if (group >= a.groups) return;                                   // whole warps, and in blocks of one group nobody
     RowWalk walk(a, group);
-    RingRows<T, SHIFT, FULL, NV> xs(a.x, a.x_stride, a.rows, a.H, vecs, walk.r0, 1, D - 1), ys(a.dy, a.dy_stride, a.rows, a.H, vecs, walk.r0, 1, D - 1);
+    RingRows<T, MODE, FULL, NV> xs(a.x, a.x_stride, a.rows, a.H, vecs, walk.r0, 1, D - 1), ys(a.dy, a.dy_stride, a.rows, a.H, vecs, walk.r0, 1, D - 1);
     T* dx = static_cast<T*>(a.dx) + walk.r0 * a.dx_stride;
     const float inv = 1.f / (float)a.H;
     uint32_t put = 0, take = 0;
@@ -404,7 +425,7 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
         put += 2 * bytes;
     }
     F2 g[H2], dg[H2], db[H2];
-    read_weights<T, W, SHIFT, NV>(g, a.gamma, 1.f, a.H, vecs);
+    read_weights<T, W, MODE, NV>(g, a.gamma, 1.f, a.H, vecs);
 #pragma unroll
     for (int j = 0; j < H2; ++j) dg[j] = db[j] = twice(0.f);
     const auto leave = [&]() {
@@ -415,11 +436,8 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
             float x[P::N], y[P::N];
 #pragma unroll
             for (int j = 0; j < P::N; ++j) { x[j] = element(dg, i * P::N + j); y[j] = element(db, i * P::N + j); }
-            if constexpr (!SHIFT || sizeof(T) == 4) store_slot<P::N>(a, walk.slot(), q * P::N, x, y);
-            else {
-                store_slot<1>(a, walk.slot(), q * 2, x, y);
-                if (q * 2 + 1 < a.H) store_slot<1>(a, walk.slot(), q * 2 + 1, x + 1, y + 1);
-            }
+            if (MODE == kOdd && q == a.H / 2) store_slot<1>(a, walk.slot(), q * 2, x, y);
+            else store_slot<P::N>(a, walk.slot(), q * P::N, x, y);
         }
     };
     float nmean = a.mean[walk.r0], nrstd = a.rstd[walk.r0];
@@ -458,7 +476,7 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
         const F2 c1 = twice(-s.x * inv), c2 = twice(-s.y * inv);
 #pragma unroll
         for (int j = 0; j < H2; ++j) x[j] = mul(fma(x[j], c2, add(dy[j], c1)), twice(rstd));
-        write_row<T, SHIFT, FULL, NV>(dx, x, a.H, vecs);
+        write_row<T, MODE, FULL, NV>(dx, x, a.H, vecs);
         dx += a.dx_stride;
     }
     if (a.slots && walk.any) leave();
@@ -475,51 +493,55 @@ template <typename K> static cudaError_t allow_shared(K kernel, size_t bytes) {
     return bytes <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
-template <typename T, typename W, bool SHIFT, bool FULL, int NV, int D> static cudaError_t forward_launch(const NormArgs& a, dim3 block, int sms, cudaStream_t st) {
-    const size_t smem = (size_t)block.y * D * Part<T, SHIFT, NV>::bytes(block.x);
-    const cudaError_t e = allow_shared(norm_forward_kernel<T, W, SHIFT, FULL, NV, D>, smem);
+template <typename T, typename W, int MODE, bool FULL, int NV, int D> static cudaError_t forward_launch(const NormArgs& a, dim3 block, int sms, cudaStream_t st) {
+    const size_t smem = (size_t)block.y * D * Part<T, MODE, NV>::bytes(block.x);
+    const cudaError_t e = allow_shared(norm_forward_kernel<T, W, MODE, FULL, NV, D>, smem);
     if (e != cudaSuccess) return e;
     const uint32_t threads = block.x * block.y, per_sm = threads < 768 ? 768 / threads : 1;
     const uint32_t blocks = (a.rows + block.y - 1) / block.y, cap = (uint32_t)sms * per_sm;
-    norm_forward_kernel<T, W, SHIFT, FULL, NV, D><<<blocks < cap ? blocks : cap, block, smem, st>>>(a);
+    norm_forward_kernel<T, W, MODE, FULL, NV, D><<<blocks < cap ? blocks : cap, block, smem, st>>>(a);
     return cudaGetLastError();
 }
-template <typename T, typename W, bool SHIFT, int NV, int D> static cudaError_t forward_run(const NormArgs& a, int sms, cudaStream_t st) {
-    using P = Part<T, SHIFT, NV>;
+template <typename T, typename W, int MODE, int NV, int D> static cudaError_t forward_run(const NormArgs& a, int sms, cudaStream_t st) {
+    using P = Part<T, MODE, NV>;
     const dim3 block = group_shape((a.H + P::N - 1) / P::N, NV);
-    if constexpr (!SHIFT)
-        if (a.H == NV * P::N * block.x) return forward_launch<T, W, SHIFT, true, NV, D>(a, block, sms, st);
-    return forward_launch<T, W, SHIFT, false, NV, D>(a, block, sms, st);
+    if constexpr (MODE == kAligned)
+        if (a.H == NV * P::N * block.x) return forward_launch<T, W, MODE, true, NV, D>(a, block, sms, st);
+    return forward_launch<T, W, MODE, false, NV, D>(a, block, sms, st);
 }
 
 // cudaErrorNotSupported: the row does not fit.
-template <typename T, typename W> static cudaError_t forward_rows(const NormArgs& a, bool aligned, int sms, cudaStream_t st) {
+template <typename T, typename W> static cudaError_t forward_rows(const NormArgs& a, uint32_t v, int sms, cudaStream_t st) {
     constexpr int e = sizeof(T), D = e == 2 ? 4 : 3;
     if (a.H > 16 * kMaxGroup) return cudaErrorNotSupported;
-    if (!aligned) return forward_run<T, W, true, e == 2 ? 8 : 16, D>(a, sms, st);
-    return a.H <= 32 * 16 / e ? forward_run<T, W, false, 1, D>(a, sms, st) : forward_run<T, W, false, e, D>(a, sms, st);
+    if (v == 16) return a.H <= 32 * 16 / e ? forward_run<T, W, kAligned, 1, D>(a, sms, st) : forward_run<T, W, kAligned, e, D>(a, sms, st);
+    if constexpr (e == 2)
+        if (v == 2) return forward_run<T, W, kOdd, 8, D>(a, sms, st);
+    return forward_run<T, W, kWords, 4 * e, D>(a, sms, st);
 }
 
-template <typename T, typename W, bool SHIFT, bool FULL, int NV, int D> static cudaError_t backward_launch(const NormArgs& a, dim3 block, cudaStream_t st) {
-    const size_t smem = (size_t)block.y * D * 2 * Part<T, SHIFT, NV>::bytes(block.x);
-    const cudaError_t e = allow_shared(norm_backward_kernel<T, W, SHIFT, FULL, NV, D>, smem);
+template <typename T, typename W, int MODE, bool FULL, int NV, int D> static cudaError_t backward_launch(const NormArgs& a, dim3 block, cudaStream_t st) {
+    const size_t smem = (size_t)block.y * D * 2 * Part<T, MODE, NV>::bytes(block.x);
+    const cudaError_t e = allow_shared(norm_backward_kernel<T, W, MODE, FULL, NV, D>, smem);
     if (e != cudaSuccess) return e;
-    norm_backward_kernel<T, W, SHIFT, FULL, NV, D><<<(a.groups + block.y - 1) / block.y, block, smem, st>>>(a);
+    norm_backward_kernel<T, W, MODE, FULL, NV, D><<<(a.groups + block.y - 1) / block.y, block, smem, st>>>(a);
     return cudaGetLastError();
 }
-template <typename T, typename W, bool SHIFT, int NV, int D> static cudaError_t backward_run(const NormArgs& a, cudaStream_t st) {
-    using P = Part<T, SHIFT, NV>;
+template <typename T, typename W, int MODE, int NV, int D> static cudaError_t backward_run(const NormArgs& a, cudaStream_t st) {
+    using P = Part<T, MODE, NV>;
     const dim3 block = group_shape((a.H + P::N - 1) / P::N, NV);
-    if constexpr (!SHIFT)
-        if (a.H == NV * P::N * block.x) return backward_launch<T, W, SHIFT, true, NV, D>(a, block, st);
-    return backward_launch<T, W, SHIFT, false, NV, D>(a, block, st);
+    if constexpr (MODE == kAligned)
+        if (a.H == NV * P::N * block.x) return backward_launch<T, W, MODE, true, NV, D>(a, block, st);
+    return backward_launch<T, W, MODE, false, NV, D>(a, block, st);
 }
 
-template <typename T, typename W> static cudaError_t backward_rows(const NormArgs& a, bool aligned, cudaStream_t st) {
+template <typename T, typename W> static cudaError_t backward_rows(const NormArgs& a, uint32_t v, cudaStream_t st) {
     constexpr int e = sizeof(T), D = e == 2 ? 3 : 2;
     if (a.H > 16 * kMaxGroup) return cudaErrorNotSupported;
-    if (!aligned) return backward_run<T, W, true, e == 2 ? 8 : 16, D>(a, st);
-    return a.H <= 32 * 16 / e ? backward_run<T, W, false, 1, D>(a, st) : backward_run<T, W, false, e, D>(a, st);
+    if (v == 16) return a.H <= 32 * 16 / e ? backward_run<T, W, kAligned, 1, D>(a, st) : backward_run<T, W, kAligned, e, D>(a, st);
+    if constexpr (e == 2)
+        if (v == 2) return backward_run<T, W, kOdd, 8, D>(a, st);
+    return backward_run<T, W, kWords, 4 * e, D>(a, st);
 }
 
 }  // namespace ftc
