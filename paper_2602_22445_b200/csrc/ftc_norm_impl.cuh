@@ -1,15 +1,17 @@
 // Layer norm on rows that fit the registers of a thread block.
 //
-// A group of G threads (a warp, or a block of up to 512) holds a row, 16 elements a thread (rows of at most 512 bytes: one vector), as
-// packed pairs. Vector i of thread t is vector i*G + t of the row, so every load and store of a warp is one contiguous run. Statistics
-// are taken in two steps from the registers (mean, then squared distances), which no common offset of the row can spoil. A group walks
-// many rows with gamma, beta and the column sums in registers.
+// A group of threads (a warp, or a block of up to 16 warps) holds a row, 16 elements a thread (rows of at most 512 bytes: one vector),
+// as packed pairs. A warp has one contiguous stretch of the row, vector i of lane l its vector 32 i + l: every load and store of a warp
+// is one contiguous run, all at fixed offsets, and only the last warp may have vectors that do not exist. Statistics are taken in two
+// steps from the registers (mean, then squared distances), which no common offset of the row can spoil. A group walks many rows with
+// gamma, beta and the column sums in registers.
 //
 // Rows come in through a ring of D rows in shared memory, filled by asynchronous copies of 16 bytes that run D - 1 rows ahead: what an SM
-// has under way does not depend on registers. Where all rows begin on 16 bytes each thread copies what it reads itself and the ring
-// needs no barrier. Other rows are copied with the 16-byte pieces that cover them, and threads read them word by word from where they
-// begin in the ring (kWords), 16-bit elements that begin or end between words as pairs out of two neighbouring words (kOdd); this takes
-// one barrier a row. A piece that reaches over the array's first or last element is put together from the elements inside.
+// has under way does not depend on registers. A warp copies what it reads itself, so the ring needs no barrier of the block. Where all
+// rows begin on 16 bytes (kAligned) each thread copies its own vectors. Other stretches are copied with the 16-byte pieces that cover
+// them, and threads read them word by word from where they begin in the ring (kWords), 16-bit elements that begin or end between words
+// as pairs out of two neighbouring words (kOdd). A piece that reaches over the array's first or last element is put together from the
+// elements inside.
 #pragma once
 #include "ftc_f32x2.cuh"
 #include "ftc_train.cuh"
@@ -174,8 +176,6 @@ __device__ __forceinline__ float2 group_sum(float2 v, Scratch& scratch, uint32_t
     const float other = __shfl_xor_sync(0xFFFFFFFFu, s, 16);
     return upper ? make_float2(other, s) : make_float2(s, other);
 }
-__device__ __forceinline__ void group_barrier() { if (blockDim.x == 32) __syncwarp(); else __syncthreads(); }
-
 // 1 / sqrt(x): the approximate one and a step of Newton's method (none at 0, infinity and NaN, where the first is right).
 __device__ __forceinline__ float inverse_root(float x) {
     const float r = rsqrtf(x);
@@ -195,8 +195,10 @@ template <typename T, int MODE, int NV_> struct Part {
     static constexpr bool SHIFT = MODE != kAligned;
     static constexpr int NV = NV_, N = SHIFT ? (sizeof(T) == 2 ? 2 : 1) : 16 / (int)sizeof(T), E = NV * N, VB = N * (int)sizeof(T);
     static_assert(E % 2 == 0, "pairs");
-    // Bytes that one row takes up in the ring.
-    static __host__ __device__ uint32_t bytes(uint32_t G) { return NV * G * VB + (SHIFT ? 32 : 0); }
+    static constexpr uint32_t WARP = 32 * NV, STRETCH = WARP * VB, PLACE = STRETCH + (SHIFT ? 32 : 0);   // a warp's vectors, their bytes, its room in a ring row
+    static __device__ __forceinline__ uint32_t first_vector() { return (threadIdx.x >> 5) * WARP + (threadIdx.x & 31); }
+    // Does every lane of this warp have all its vectors, of whole pairs?
+    static __device__ __forceinline__ bool whole(uint32_t n) { return ((threadIdx.x >> 5) + 1) * WARP * N <= n; }
 };
 __device__ __forceinline__ float element(const F2* v, int j) { return j & 1 ? hi(v[j / 2]) : lo(v[j / 2]); }
 
@@ -205,57 +207,75 @@ template <typename T> __device__ __forceinline__ F2 pair_of_word(uint32_t w) {
     else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w)); return pair(f.x, f.y); }
 }
 
-// The rows of one array on their way through the ring; FULL: every thread has all its vectors. `row`: the thread's first byte of the present
-// row (SHIFT: the row's first byte).
-template <typename T, int MODE, bool FULL, int NV> struct RingRows {
+// The rows of one array on their way through the ring. `row`: this thread's first byte of the present row (SHIFT: the warp's first byte);
+// `place`: where the warp's stretch of a row is in the ring. ALL: every warp of the group is whole.
+template <typename T, int MODE, bool ALL, int NV> struct RingRows {
     using P = Part<T, MODE, NV>;
-    static constexpr bool SHIFT = MODE != kAligned;
+    static constexpr bool SHIFT = P::SHIFT;
+    static constexpr int PIECES = P::STRETCH / 512;                   // rounds of 32 pieces that cover a stretch which begins on 16 bytes
     const char* row;
     uint64_t step, ahead;                                             // bytes to the group's next row, and to the one that is fetched
-    uint32_t n, vecs;
+    uint32_t n, vecs, bytes;                                          // elements and vectors of a row, bytes of the warp's stretch
+    bool whole;
     uintptr_t first, behind;                                          // SHIFT: the array's first byte and the one behind its last
-    __device__ __forceinline__ RingRows(const void* p, uint64_t stride, uint32_t rows, uint32_t elements, uint32_t vectors, uint32_t r, uint32_t row_step, int rows_ahead)
-        : row(static_cast<const char*>(p) + (r * stride * sizeof(T) + (SHIFT ? 0u : threadIdx.x * 16u))), step(row_step * stride * sizeof(T)),
-          ahead(rows_ahead * step), n(elements), vecs(vectors) {
+    __device__ __forceinline__ RingRows(const void* p, uint64_t stride, uint32_t rows, uint32_t elements, uint32_t r, uint32_t row_step, int rows_ahead)
+        : step(row_step * stride * sizeof(T)), ahead(rows_ahead * step), n(elements), vecs((elements + P::N - 1) / P::N), whole(ALL || P::whole(elements)) {
+        const uint32_t begin = (threadIdx.x >> 5) * P::STRETCH;
+        row = static_cast<const char*>(p) + r * stride * sizeof(T) + begin + (SHIFT ? 0u : (threadIdx.x & 31) * 16u);
         if (SHIFT) {
+            bytes = whole ? P::STRETCH : n * (uint32_t)sizeof(T) - begin;
             first = reinterpret_cast<uintptr_t>(p);
             behind = first + ((uint64_t)(rows - 1) * stride + elements) * sizeof(T);
         }
     }
     __device__ __forceinline__ void next() { row += step; }
-    // Copies the row at `from` to `place` (byte offset in the ring).
-    __device__ __forceinline__ void fetch(char* ring, uint32_t place, const char* from) const {
+    // Copies this warp's stretch that begins (SHIFT; else this thread's part of it) at `from`.
+    __device__ __forceinline__ void fetch(char* place, const char* from) const {
+        const uint32_t lane = threadIdx.x & 31, dst = (uint32_t)__cvta_generic_to_shared(place) + lane * 16u;
         if constexpr (!SHIFT) {
-            const uint32_t dst = (uint32_t)__cvta_generic_to_shared(ring) + place + threadIdx.x * 16u;
+            if (ALL || whole) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (FULL || i * blockDim.x + threadIdx.x < vecs) copy_async_16(dst + i * blockDim.x * 16u, from + i * blockDim.x * 16u);
+                for (int i = 0; i < NV; ++i) copy_async_16(dst + i * 512, from + i * 512);
+            } else {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if (P::first_vector() + i * 32 < vecs) copy_async_16(dst + i * 512, from + i * 512);
+            }
         } else {
-            const uint32_t pieces = (((uint32_t)reinterpret_cast<uintptr_t>(from) & 15u) + n * (uint32_t)sizeof(T) + 15) / 16;
+            const uint32_t pieces = (((uint32_t)reinterpret_cast<uintptr_t>(from) & 15u) + bytes + 15) / 16;
             const uintptr_t begin = reinterpret_cast<uintptr_t>(from) & ~(uintptr_t)15;
-            const uint32_t dst = (uint32_t)__cvta_generic_to_shared(ring) + place;
-            const bool inside = begin >= first && begin + pieces * 16u <= behind;      // all rows but the array's first and last
+            if (begin < first || begin + pieces * 16u > behind) { fetch_edge(place, begin, pieces); return; }
+            const char* at = reinterpret_cast<const char*>(begin) + lane * 16u;
+            if (whole) {
 #pragma unroll
-            for (int i = 0; i < NV * P::VB / 16 + 1; ++i) {           // at most that many: the ring row holds NV * G * VB bytes and 32
-                const uint32_t q = i * blockDim.x + threadIdx.x;
-                if (q >= pieces) continue;
-                const uintptr_t at = begin + q * 16u;
-                if (inside || (at >= first && at + 16 <= behind)) copy_async_16(dst + q * 16u, reinterpret_cast<const void*>(at));
-                else
-                    for (uint32_t e = 0; e < 16; e += sizeof(T))
-                        if (at + e >= first && at + e < behind) *reinterpret_cast<T*>(ring + place + q * 16u + e) = *reinterpret_cast<const T*>(at + e);
+                for (int i = 0; i < PIECES; ++i) copy_async_16(dst + i * 512, at + i * 512);
+                if (lane + PIECES * 32 < pieces) copy_async_16(dst + PIECES * 512, at + PIECES * 512);
+            } else {
+#pragma unroll
+                for (int i = 0; i <= PIECES; ++i)
+                    if (lane + i * 32 < pieces) copy_async_16(dst + i * 512, at + i * 512);
             }
         }
     }
+    // The same at the array's first and last row.
+    __device__ __noinline__ void fetch_edge(char* place, uintptr_t begin, uint32_t pieces) const {
+        for (uint32_t q = threadIdx.x & 31; q < pieces; q += 32) {
+            const uintptr_t at = begin + q * 16u;
+            if (at >= first && at + 16 <= behind) copy_async_16((uint32_t)__cvta_generic_to_shared(place) + q * 16u, reinterpret_cast<const void*>(at));
+            else
+                for (uint32_t e = 0; e < 16; e += sizeof(T))
+                    if (at + e >= first && at + e < behind) *reinterpret_cast<T*>(place + q * 16u + e) = *reinterpret_cast<const T*>(at + e);
+        }
+    }
     // This thread's elements of the present row; zeros behind its end.
-    __device__ __forceinline__ void read(F2* v, const char* ring, uint32_t place) const {
-        const uint32_t mis = SHIFT ? (uint32_t)reinterpret_cast<uintptr_t>(row) & 15u : 0u;
+    template <bool WHOLE> __device__ __forceinline__ void read_as(F2* v, const char* place) const {
+        const uint32_t lane = threadIdx.x & 31, mis = SHIFT ? (uint32_t)reinterpret_cast<uintptr_t>(row) & 15u : 0u;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint32_t q = i * blockDim.x + threadIdx.x;
-            const bool in = FULL || q < vecs;
+            const uint32_t q = P::first_vector() + i * 32;
+            const bool in = WHOLE || q < vecs;
             if constexpr (!SHIFT) {
-                const uint4 w = in ? *reinterpret_cast<const uint4*>(ring + place + q * 16u) : make_uint4(0u, 0u, 0u, 0u);
+                const uint4 w = in ? reinterpret_cast<const uint4*>(place)[i * 32 + lane] : make_uint4(0u, 0u, 0u, 0u);
                 if constexpr (sizeof(T) == 4) {
                     v[2 * i] = pair(__uint_as_float(w.x), __uint_as_float(w.y));
                     v[2 * i + 1] = pair(__uint_as_float(w.z), __uint_as_float(w.w));
@@ -264,54 +284,59 @@ template <typename T, int MODE, bool FULL, int NV> struct RingRows {
                     v[4 * i + 2] = pair_of_word<T>(w.z); v[4 * i + 3] = pair_of_word<T>(w.w);
                 }
             } else if constexpr (sizeof(T) == 4) {
-                const float x = in ? *reinterpret_cast<const float*>(ring + place + mis + q * 4u) : 0.f;
+                const float x = in ? reinterpret_cast<const float*>(place + mis)[i * 32 + lane] : 0.f;
                 v[i / 2] = i & 1 ? pair(lo(v[i / 2]), x) : pair(x, 0.f);
             } else {
-                const uint32_t* w = reinterpret_cast<const uint32_t*>(ring + place + (mis & 12u) + q * 4u);
+                const uint32_t* w = reinterpret_cast<const uint32_t*>(place + (mis & 12u)) + (i * 32 + lane);
                 uint32_t x = 0u;
                 if (in) {
                     x = w[0];
                     if constexpr (MODE == kOdd) {
-                        if (mis & 2u) x = __funnelshift_r(x, w[1], 16);
-                        if (q == n / 2) x &= 0xFFFFu;                 // an odd row's last element stands alone
+                        x = __funnelshift_r(x, w[1], (mis & 2u) * 8u);
+                        if (!WHOLE && q == n / 2) x &= 0xFFFFu;       // an odd row's last element stands alone
                     }
                 }
                 v[i] = pair_of_word<T>(x);
             }
         }
     }
+    __device__ __forceinline__ void read(F2* v, const char* place) const { if (ALL || whole) read_as<true>(v, place); else read_as<false>(v, place); }
 };
 
-// Vector i of a thread's results to its columns of a row.
-template <typename T, int MODE, bool FULL, int NV> __device__ __forceinline__ void write_row(T* row, const F2* v, uint32_t n, uint32_t vecs) {
+// A thread's results to its columns of a row.
+template <typename T, int MODE, int NV, bool WHOLE> __device__ __forceinline__ void write_row_as(T* row, const F2* v, uint32_t n) {
     using P = Part<T, MODE, NV>;
     const bool between = MODE == kOdd && (reinterpret_cast<uintptr_t>(row) & 2u);
+    T* at = row + P::first_vector() * P::N;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const uint32_t q = i * blockDim.x + threadIdx.x;
-        if (!FULL && q >= vecs) continue;
+        const uint32_t q = P::first_vector() + i * 32;
+        if (!WHOLE && q * P::N >= n) continue;
         float o[P::N];
 #pragma unroll
         for (int j = 0; j < P::N; ++j) o[j] = element(v, i * P::N + j);
-        if (MODE == kOdd && (between || q == n / 2)) {
-            row[2 * q] = from_f32<T>(o[0]);
-            if (q != n / 2) row[2 * q + 1] = from_f32<T>(o[1 % P::N]);
-        } else Pack<T, P::VB>::store(row + q * P::N, o);
+        if (MODE == kOdd && (between || (!WHOLE && q == n / 2))) {
+            at[i * 64] = from_f32<T>(o[0]);
+            if (WHOLE || q != n / 2) at[i * 64 + 1] = from_f32<T>(o[1 % P::N]);
+        } else Pack<T, P::VB>::store(at + i * 32 * P::N, o);
     }
+}
+template <typename T, int MODE, bool ALL, int NV> __device__ __forceinline__ void write_row(T* row, const F2* v, uint32_t n, bool whole) {
+    if (ALL || whole) write_row_as<T, MODE, NV, true>(row, v, n); else write_row_as<T, MODE, NV, false>(row, v, n);
 }
 
 // A thread's weights; `other` where there are none or no columns.
-template <typename T, typename W, int MODE, int NV> __device__ __forceinline__ void read_weights(F2* v, const void* weights, float other, uint32_t n, uint32_t vecs) {
+template <typename T, typename W, int MODE, int NV> __device__ __forceinline__ void read_weights(F2* v, const void* weights, float other, uint32_t n) {
     using P = Part<T, MODE, NV>;
     const W* w = static_cast<const W*>(weights);
     const bool pairs = P::N == 2 && (reinterpret_cast<uintptr_t>(w) & (2 * sizeof(W) - 1)) == 0;
     float f[P::E];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const uint32_t q = i * blockDim.x + threadIdx.x;
+        const uint32_t q = P::first_vector() + i * 32;
 #pragma unroll
         for (int j = 0; j < P::N; ++j) f[i * P::N + j] = other;
-        if (q >= vecs) continue;
+        if (q * P::N >= n) continue;
         if constexpr (MODE == kAligned || P::N == 1) load_weights<W, P::N>(f + i * P::N, w, q * P::N, other);
         else if (w) {
             if (pairs && (MODE != kOdd || q != n / 2)) {
@@ -328,37 +353,36 @@ template <typename T, typename W, int MODE, int NV> __device__ __forceinline__ v
 }
 
 // blockDim = (G, groups in the block).
-template <typename T, typename W, int MODE, bool FULL, int NV, int D>
+template <typename T, typename W, int MODE, bool ALL, int NV, int D>
 __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
     using P = Part<T, MODE, NV>;
-    constexpr bool SHIFT = MODE != kAligned;
     constexpr int H2 = P::E / 2;
     extern __shared__ uint4 ring_memory[];
     __shared__ Scratch scratch;
     uint32_t turn = 0;
-    const uint32_t G = blockDim.x, vecs = (a.H + P::N - 1) / P::N, bytes = P::bytes(G);
-    char* ring = reinterpret_cast<char*>(ring_memory) + threadIdx.y * D * bytes;
+    const uint32_t bytes = blockDim.x / 32 * P::PLACE;               // a row in the ring
+    char* ring = reinterpret_cast<char*>(ring_memory) + threadIdx.y * D * bytes + (threadIdx.x >> 5) * P::PLACE;
     const float inv = 1.f / (float)a.H;
     const uint32_t step = gridDim.x * blockDim.y, r0 = blockIdx.x * blockDim.y + threadIdx.y;
-    RingRows<T, MODE, FULL, NV> in(a.x, a.x_stride, a.rows, a.H, vecs, r0, step, D - 1);
+    RingRows<T, MODE, ALL, NV> in(a.x, a.x_stride, a.rows, a.H, r0, step, D - 1);
     T* y = static_cast<T*>(a.y) + r0 * a.y_stride;
     uint32_t fetched = r0, put = 0, take = 0;
 #pragma unroll
     for (int d = 0; d < D - 1; ++d) {
-        if (fetched < a.rows) in.fetch(ring, put, in.row + d * in.step);
+        if (fetched < a.rows) in.fetch(ring + put, in.row + d * in.step);
         copies_end_batch();
         fetched += step; put += bytes;                               // rows + grid stay below 2^32
     }
     F2 g[H2], b[H2];
-    read_weights<T, W, MODE, NV>(g, a.gamma, 1.f, a.H, vecs);
-    read_weights<T, W, MODE, NV>(b, a.beta, 0.f, a.H, vecs);
+    read_weights<T, W, MODE, NV>(g, a.gamma, 1.f, a.H);
+    read_weights<T, W, MODE, NV>(b, a.beta, 0.f, a.H);
     clear_scratch(scratch);
     for (uint32_t r = r0; r < a.rows; r += step) {
         copies_wait<D - 2>();
-        if (SHIFT) group_barrier();
+        if (P::SHIFT) __syncwarp();
         F2 x[H2];
-        in.read(x, ring, take);
-        if (fetched < a.rows) in.fetch(ring, put, in.row + in.ahead);
+        in.read(x, ring + take);
+        if (fetched < a.rows) in.fetch(ring + put, in.row + in.ahead);
         copies_end_batch();
         fetched += step;
         put = take;
@@ -371,27 +395,19 @@ __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
         s = twice(0.f);
 #pragma unroll
         for (int j = 0; j < H2; ++j) x[j] = add(x[j], twice(-mean));
-        if constexpr (P::N > 1) {
+        if (!ALL && !in.whole) {                                     // nothing behind the row's end
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const uint32_t q = i * G + threadIdx.x;
-                if (MODE == kOdd && 2 * q + 1 == a.H) x[i] = pair(lo(x[i]), 0.f);
-                if (FULL || q < vecs) {
-#pragma unroll
-                    for (int j = i * P::N / 2; j < (i + 1) * P::N / 2; ++j) s = fma(x[j], x[j], s);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < H2; ++j) {                           // vectors of one element: two of them make a pair
-                if ((2 * j + 1) * G + threadIdx.x >= vecs) x[j] = pair(2 * j * G + threadIdx.x < vecs ? lo(x[j]) : 0.f, 0.f);
-                s = fma(x[j], x[j], s);
+            for (int j = 0; j < H2; ++j) {
+                const uint32_t c = P::N == 1 ? P::first_vector() + 2 * j * 32 : (P::first_vector() + 2 * j / P::N * 32) * P::N + 2 * j % P::N;
+                if (c + (P::N == 1 ? 32 : 1) >= a.H) x[j] = pair(c < a.H ? lo(x[j]) : 0.f, 0.f);
             }
         }
+#pragma unroll
+        for (int j = 0; j < H2; ++j) s = fma(x[j], x[j], s);
         const float rstd = inverse_root(group_sum(lo(s) + hi(s), scratch, turn) * inv + a.eps);
 #pragma unroll
         for (int j = 0; j < H2; ++j) x[j] = fma(mul(x[j], twice(rstd)), g[j], b[j]);
-        write_row<T, MODE, FULL, NV>(y, x, a.H, vecs);
+        write_row<T, MODE, ALL, NV>(y, x, a.H, in.whole);
         y += step * a.y_stride;
         if (threadIdx.x == 0) {
             if (a.mean_out) a.mean_out[r] = mean;
@@ -401,38 +417,37 @@ __global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
 }
 
 // blockDim = (G, groups in the block); a group of threads walks the rows of one RowWalk.
-template <typename T, typename W, int MODE, bool FULL, int NV, int D>
+template <typename T, typename W, int MODE, bool ALL, int NV, int D>
 __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
     using P = Part<T, MODE, NV>;
-    constexpr bool SHIFT = MODE != kAligned;
     constexpr int H2 = P::E / 2;
     extern __shared__ uint4 ring_memory[];
     __shared__ Scratch scratch;
     uint32_t turn = 0;
-    const uint32_t G = blockDim.x, vecs = (a.H + P::N - 1) / P::N, bytes = P::bytes(G), group = blockIdx.x * blockDim.y + threadIdx.y;
-    char* ring = reinterpret_cast<char*>(ring_memory) + threadIdx.y * D * 2 * bytes;
+    const uint32_t bytes = blockDim.x / 32 * P::PLACE, group = blockIdx.x * blockDim.y + threadIdx.y;
+    char* ring = reinterpret_cast<char*>(ring_memory) + threadIdx.y * D * 2 * bytes + (threadIdx.x >> 5) * P::PLACE;
     clear_scratch(scratch);
     if (group >= a.groups) return;                                   // whole warps, and in blocks of one group nobody
     RowWalk walk(a, group);
-    RingRows<T, MODE, FULL, NV> xs(a.x, a.x_stride, a.rows, a.H, vecs, walk.r0, 1, D - 1), ys(a.dy, a.dy_stride, a.rows, a.H, vecs, walk.r0, 1, D - 1);
+    RingRows<T, MODE, ALL, NV> xs(a.x, a.x_stride, a.rows, a.H, walk.r0, 1, D - 1), ys(a.dy, a.dy_stride, a.rows, a.H, walk.r0, 1, D - 1);
     T* dx = static_cast<T*>(a.dx) + walk.r0 * a.dx_stride;
     const float inv = 1.f / (float)a.H;
     uint32_t put = 0, take = 0;
 #pragma unroll
     for (int d = 0; d < D - 1; ++d) {
-        if (walk.r0 + d < walk.r1) { xs.fetch(ring, put, xs.row + d * xs.step); ys.fetch(ring, put + bytes, ys.row + d * ys.step); }
+        if (walk.r0 + d < walk.r1) { xs.fetch(ring + put, xs.row + d * xs.step); ys.fetch(ring + put + bytes, ys.row + d * ys.step); }
         copies_end_batch();
         put += 2 * bytes;
     }
     F2 g[H2], dg[H2], db[H2];
-    read_weights<T, W, MODE, NV>(g, a.gamma, 1.f, a.H, vecs);
+    read_weights<T, W, MODE, NV>(g, a.gamma, 1.f, a.H);
 #pragma unroll
     for (int j = 0; j < H2; ++j) dg[j] = db[j] = twice(0.f);
     const auto leave = [&]() {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint32_t q = i * G + threadIdx.x;
-            if (!FULL && q >= vecs) continue;
+            const uint32_t q = P::first_vector() + i * 32;
+            if (!ALL && q * P::N >= a.H) continue;
             float x[P::N], y[P::N];
 #pragma unroll
             for (int j = 0; j < P::N; ++j) { x[j] = element(dg, i * P::N + j); y[j] = element(db, i * P::N + j); }
@@ -443,11 +458,11 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
     float nmean = a.mean[walk.r0], nrstd = a.rstd[walk.r0];
     for (uint32_t r = walk.r0; r < walk.r1; ++r) {
         copies_wait<D - 2>();
-        if (SHIFT) group_barrier();
+        if (P::SHIFT) __syncwarp();
         F2 x[H2], dy[H2];
-        xs.read(x, ring, take);
-        ys.read(dy, ring, take + bytes);
-        if (r + (D - 1) < walk.r1) { xs.fetch(ring, put, xs.row + xs.ahead); ys.fetch(ring, put + bytes, ys.row + ys.ahead); }
+        xs.read(x, ring + take);
+        ys.read(dy, ring + take + bytes);
+        if (r + (D - 1) < walk.r1) { xs.fetch(ring + put, xs.row + xs.ahead); ys.fetch(ring + put + bytes, ys.row + ys.ahead); }
         copies_end_batch();
         put = take;
         take = take + 2 * bytes == D * 2 * bytes ? 0 : take + 2 * bytes;
@@ -476,7 +491,7 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
         const F2 c1 = twice(-s.x * inv), c2 = twice(-s.y * inv);
 #pragma unroll
         for (int j = 0; j < H2; ++j) x[j] = mul(fma(x[j], c2, add(dy[j], c1)), twice(rstd));
-        write_row<T, MODE, FULL, NV>(dx, x, a.H, vecs);
+        write_row<T, MODE, ALL, NV>(dx, x, a.H, xs.whole);
         dx += a.dx_stride;
     }
     if (a.slots && walk.any) leave();
@@ -493,13 +508,14 @@ template <typename K> static cudaError_t allow_shared(K kernel, size_t bytes) {
     return bytes <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
-template <typename T, typename W, int MODE, bool FULL, int NV, int D> static cudaError_t forward_launch(const NormArgs& a, dim3 block, int sms, cudaStream_t st) {
-    const size_t smem = (size_t)block.y * D * Part<T, MODE, NV>::bytes(block.x);
-    const cudaError_t e = allow_shared(norm_forward_kernel<T, W, MODE, FULL, NV, D>, smem);
+template <typename T, typename W, int MODE, bool ALL, int NV, int D> static cudaError_t forward_launch(const NormArgs& a, dim3 block, int sms, cudaStream_t st) {
+    using P = Part<T, MODE, NV>;
+    const size_t smem = (size_t)block.y * D * (block.x / 32) * P::PLACE;
+    const cudaError_t e = allow_shared(norm_forward_kernel<T, W, MODE, ALL, NV, D>, smem);
     if (e != cudaSuccess) return e;
     const uint32_t threads = block.x * block.y, per_sm = threads < 768 ? 768 / threads : 1;
     const uint32_t blocks = (a.rows + block.y - 1) / block.y, cap = (uint32_t)sms * per_sm;
-    norm_forward_kernel<T, W, MODE, FULL, NV, D><<<blocks < cap ? blocks : cap, block, smem, st>>>(a);
+    norm_forward_kernel<T, W, MODE, ALL, NV, D><<<blocks < cap ? blocks : cap, block, smem, st>>>(a);
     return cudaGetLastError();
 }
 template <typename T, typename W, int MODE, int NV, int D> static cudaError_t forward_run(const NormArgs& a, int sms, cudaStream_t st) {
@@ -520,11 +536,12 @@ template <typename T, typename W> static cudaError_t forward_rows(const NormArgs
     return forward_run<T, W, kWords, 4 * e, D>(a, sms, st);
 }
 
-template <typename T, typename W, int MODE, bool FULL, int NV, int D> static cudaError_t backward_launch(const NormArgs& a, dim3 block, cudaStream_t st) {
-    const size_t smem = (size_t)block.y * D * 2 * Part<T, MODE, NV>::bytes(block.x);
-    const cudaError_t e = allow_shared(norm_backward_kernel<T, W, MODE, FULL, NV, D>, smem);
+template <typename T, typename W, int MODE, bool ALL, int NV, int D> static cudaError_t backward_launch(const NormArgs& a, dim3 block, cudaStream_t st) {
+    using P = Part<T, MODE, NV>;
+    const size_t smem = (size_t)block.y * D * 2 * (block.x / 32) * P::PLACE;
+    const cudaError_t e = allow_shared(norm_backward_kernel<T, W, MODE, ALL, NV, D>, smem);
     if (e != cudaSuccess) return e;
-    norm_backward_kernel<T, W, MODE, FULL, NV, D><<<(a.groups + block.y - 1) / block.y, block, smem, st>>>(a);
+    norm_backward_kernel<T, W, MODE, ALL, NV, D><<<(a.groups + block.y - 1) / block.y, block, smem, st>>>(a);
     return cudaGetLastError();
 }
 template <typename T, typename W, int MODE, int NV, int D> static cudaError_t backward_run(const NormArgs& a, cudaStream_t st) {
