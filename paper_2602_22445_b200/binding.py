@@ -390,32 +390,35 @@ def _rows_ptr(desc, t, what, rows):
     """Address and row stride of a [rows][H] tensor of the descriptor's type whose rows are contiguous."""
     if t is None:
         return None, 0
-    if not t.is_cuda or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != desc.H or (desc.H > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: a CUDA tensor [{rows}][{desc.H}] with contiguous rows is wanted")
-    if _float_code(t.dtype) != desc.dtype:
+    H = desc.H
+    if t.shape != (rows, H) or not t.is_cuda:
+        raise ValueError(f"{what}: a CUDA tensor [{rows}][{H}] is wanted")
+    if _FLOAT_CODES.get(t.dtype) != desc.dtype and _float_code(t.dtype) != desc.dtype:
         raise ValueError(f"{what}: its type is not the descriptor's")
-    stride = t.stride(0)
-    if rows <= 1 and stride < desc.H:
-        stride = desc.H
-    return t.data_ptr(), stride
+    stride, inner = t.stride()
+    if inner != 1 and H > 1:
+        raise ValueError(f"{what}: contiguous rows are wanted")
+    return t.data_ptr(), stride if rows > 1 or stride >= H else H
 
 
 def _vector_ptr(t, what, n, code=FTC_F32):
+    """Address of n contiguous elements of a floating type."""
     if t is None:
         return None
-    if t.numel() != n or _float_code(t.dtype) != code:
-        raise ValueError(f"{what}: {n} elements of the right type are wanted")
-    return _dev_ptr(t)
+    if t.numel() != n or not t.is_cuda or not t.is_contiguous() or (_FLOAT_CODES.get(t.dtype) != code and _float_code(t.dtype) != code):
+        raise ValueError(f"{what}: {n} contiguous CUDA elements of the right type are wanted")
+    return t.data_ptr()
 
 
 def ftc_layernorm_forward(desc, d_x, d_gamma, d_beta, d_y, d_mean, d_rstd, stream=None, check=True) -> int:
     rows = d_x.shape[0]
     x, xs = _rows_ptr(desc, d_x, "d_x", rows)
     y, ys = _rows_ptr(desc, d_y, "d_y", rows)
-    rc = load().ftc_layernorm_forward(C.byref(desc), rows, x, xs, _vector_ptr(d_gamma, "d_gamma", desc.H, desc.wdtype),
-                                      _vector_ptr(d_beta, "d_beta", desc.H, desc.wdtype), y, ys,
-                                      _vector_ptr(d_mean, "d_mean", rows), _vector_ptr(d_rstd, "d_rstd", rows), _stream(stream))
-    if check and rc != FTC_OK:
+    H, code = desc.H, desc.wdtype
+    rc = (_lib or load()).ftc_layernorm_forward(desc, rows, x, xs, _vector_ptr(d_gamma, "d_gamma", H, code),
+                                                _vector_ptr(d_beta, "d_beta", H, code), y, ys, _vector_ptr(d_mean, "d_mean", rows),
+                                                _vector_ptr(d_rstd, "d_rstd", rows), _stream(stream))
+    if rc and check:
         raise FtcError(rc, "ftc_layernorm_forward")
     return rc
 
@@ -434,7 +437,7 @@ def ftc_layernorm_backward(desc, d_dy, d_x, d_gamma, d_mean, d_rstd, d_row_split
     if d_row_splits is not None and (d_row_splits.numel() != desc.P + 1 or d_row_splits.element_size() != 8 or d_row_splits.is_floating_point()):
         raise ValueError("d_row_splits: P + 1 whole numbers of 64 bits are wanted")
     ws_bytes = 0 if d_workspace is None else d_workspace.numel() * d_workspace.element_size()
-    rc = load().ftc_layernorm_backward(C.byref(desc), rows, dy, dys, x, xs, _vector_ptr(d_gamma, "d_gamma", desc.H, desc.wdtype),
+    rc = (_lib or load()).ftc_layernorm_backward(desc, rows, dy, dys, x, xs, _vector_ptr(d_gamma, "d_gamma", desc.H, desc.wdtype),
                                        _vector_ptr(d_mean, "d_mean", rows), _vector_ptr(d_rstd, "d_rstd", rows),
                                        _dev_ptr(d_row_splits), dx, dxs, _vector_ptr(d_dgamma, "d_dgamma", n),
                                        _vector_ptr(d_dbeta, "d_dbeta", n), _dev_ptr(d_workspace), ws_bytes, _stream(stream))
@@ -488,7 +491,7 @@ def ftc_grad_norm_workspace_bytes(table) -> int:
 
 def ftc_grad_norm(table, max_norm, d_norm, d_norms, d_workspace, stream=None, check=True) -> int:
     ws_bytes = 0 if d_workspace is None else d_workspace.numel() * d_workspace.element_size()
-    rc = load().ftc_grad_norm(table.h_ptr, table.d_ptr, max_norm, _vector_ptr(d_norm, "d_norm", 2),
+    rc = (_lib or load()).ftc_grad_norm(table.h_ptr, table.d_ptr, max_norm, _vector_ptr(d_norm, "d_norm", 2),
                               _vector_ptr(d_norms, "d_norms", table.n_params), _dev_ptr(d_workspace), ws_bytes, _stream(stream))
     if check and rc != FTC_OK:
         raise FtcError(rc, "ftc_grad_norm")
@@ -515,7 +518,7 @@ def _states(table, d_m, d_v, d_m_scale, d_v_scale):
 
 def ftc_adamw_step(hyper, table, d_m, d_v, d_m_scale=None, d_v_scale=None, d_grad_scale=None, stream=None, check=True) -> int:
     hyper.state_bits, states = _states(table, d_m, d_v, d_m_scale, d_v_scale)
-    rc = load().ftc_adamw_step(C.byref(hyper), table.h_ptr, table.d_ptr, *states, _vector_ptr(d_grad_scale, "d_grad_scale", 1),
+    rc = (_lib or load()).ftc_adamw_step(hyper, table.h_ptr, table.d_ptr, *states, _vector_ptr(d_grad_scale, "d_grad_scale", 1),
                                _stream(stream))
     if check and rc != FTC_OK:
         raise FtcError(rc, "ftc_adamw_step")

@@ -76,8 +76,10 @@ __global__ void __launch_bounds__(kThreads) norm_columns_kernel(NormArgs a) {
     constexpr int N = VB / (int)sizeof(T), AHEAD = 4;
     using V = Pack<T, VB>;
     const uint32_t c = (blockIdx.x * kThreads + threadIdx.x) * N;
-    if (c >= a.H) return;                                            // N divides H
+    later_kernel_may_start();
     RowWalk walk(a, blockIdx.y);
+    walk.find();                                                     // by whole warps
+    if (c >= a.H) return;                                            // N divides H
     float dg[N] = {}, db[N] = {};
     for (uint32_t r = walk.r0; r < walk.r1; r += AHEAD) {                // r1 + AHEAD stays below 2^32
         V x[AHEAD], dy[AHEAD];
@@ -112,33 +114,33 @@ __global__ void __launch_bounds__(kThreads) norm_columns_kernel(NormArgs a) {
     if (walk.any) store_slot<N>(a, walk.slot(), c, dg, db);
 }
 
-// dgamma[s][p][e], dbeta[s][p][e] from the slots: a warp adds the slots of one process for 32 columns (Q = 1), or the 8 warps of a block
-// take every eighth slot each and their sums are added in order (Q = 8, for processes with many slots).
+// dgamma[s][p][e], dbeta[s][p][e] from the slots: Q warps add the slots of one process for 32 columns, each every Q-th slot, and their
+// sums are added in order.
 template <int Q>
-__global__ void __launch_bounds__(256) norm_messages_kernel(NormArgs a, uint32_t tiles) {
-    __shared__ float part[2][8][32];
-    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint64_t item = Q == 8 ? blockIdx.x : blockIdx.x * 8ull + warp;
+__global__ void __launch_bounds__(Q == 32 ? 1024 : 256) norm_messages_kernel(NormArgs a, uint32_t tiles) {
+    constexpr int WARPS = Q == 32 ? 32 : 8;
+    __shared__ float part[2][WARPS][32];
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, turn = warp % Q;
+    const uint64_t item = blockIdx.x * (uint64_t)(WARPS / Q) + warp / Q;
     const uint32_t p = (uint32_t)(item / tiles), h = (uint32_t)(item % tiles) * 32 + lane;
     float g = 0.f, b = 0.f;
-    if (p < a.P && h < a.H) {
-        const uint32_t lo = first_row(a, p), hi = first_row(a, p + 1);
-        if (lo < hi) {
-            const uint32_t last = (hi - 1) / a.rows_per_group;
+    const bool wanted = p < a.P && h < a.H;
+    const uint32_t lo = wanted ? first_row(a, p) : 0, hi = wanted ? first_row(a, p + 1) : 0;
+    wait_for_earlier_kernel();
+    if (lo < hi) {
+        const uint32_t last = (hi - 1) / a.rows_per_group;
 #pragma unroll 4
-            for (uint32_t grp = lo / a.rows_per_group + (Q == 8 ? warp : 0); grp <= last; grp += Q) {
-                const float* slot = a.slots + ((uint64_t)grp + p) * 2 * a.H + h;
-                g += slot[0];
-                b += slot[a.H];
-            }
+        for (uint32_t grp = lo / a.rows_per_group + turn; grp <= last; grp += Q) {
+            const float* slot = a.slots + ((uint64_t)grp + p) * 2 * a.H + h;
+            g += slot[0];
+            b += slot[a.H];
         }
     }
-    if (Q == 8) {
+    if (Q > 1) {
         part[0][warp][lane] = g; part[1][warp][lane] = b;
         __syncthreads();
-        if (warp) return;
-        g = b = 0.f;
-        for (int i = 0; i < 8; ++i) { g += part[0][i][lane]; b += part[1][i][lane]; }
+        if (turn) return;
+        for (int i = 1; i < Q; ++i) { g += part[0][warp + i][lane]; b += part[1][warp + i][lane]; }
     }
     const uint32_t S = (a.H + a.k - 1) / a.k, s = h / a.k;
     if (p >= a.P || s >= S) return;                                  // h beyond H: the last message's fill, zeros
@@ -219,9 +221,15 @@ cudaError_t launch_norm_backward(const NormArgs& a, int sms, cudaStream_t st) {
     const uint64_t filled = (uint64_t)S * a.k;                       // columns with the last message's fill
     const uint32_t tiles = (uint32_t)((filled + 31) / 32);
     const uint64_t items = (uint64_t)tiles * a.P;
-    if (a.groups / a.P >= 16) norm_messages_kernel<8><<<(uint32_t)items, 256, 0, st>>>(a, tiles);
-    else norm_messages_kernel<1><<<(uint32_t)((items + 7) / 8), 256, 0, st>>>(a, tiles);
-    return cudaGetLastError();
+    if (!a.rows) {                                                   // zeros; no earlier kernel of this call
+        norm_messages_kernel<1><<<(uint32_t)((items + 7) / 8), 256, 0, st>>>(a, tiles);
+        return cudaGetLastError();
+    }
+    const uint32_t slots = a.groups / a.P + 1;                       // of a process, on average
+    if (slots <= 2) return launch_second(norm_messages_kernel<1>, (uint32_t)((items + 7) / 8), 256, st, a, tiles);
+    if (slots <= 12) return launch_second(norm_messages_kernel<4>, (uint32_t)((items + 1) / 2), 256, st, a, tiles);
+    if (slots <= 64) return launch_second(norm_messages_kernel<8>, (uint32_t)items, 256, st, a, tiles);
+    return launch_second(norm_messages_kernel<32>, (uint32_t)items, 1024, st, a, tiles);
 }
 
 }  // namespace ftc

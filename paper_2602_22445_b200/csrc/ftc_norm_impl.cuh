@@ -85,24 +85,33 @@ __device__ __forceinline__ uint32_t first_row(const NormArgs& a, uint32_t p) {
     return s < a.rows ? (uint32_t)s : a.rows;
 }
 
-// The rows of group b, and the process that holds the present one.
+// The process that holds row r: the first one that ends behind it (P if none does); for a whole warp. Even shares: the last p with
+// p*rows/P <= r. Given splits: 32 of them at a time.
+__device__ __forceinline__ uint32_t holder(const NormArgs& a, uint32_t r) {
+    if (!a.splits) return (uint32_t)(((uint64_t)(r + 1) * a.P - 1) / a.rows);
+    uint32_t lo = 0, n = a.P;                                        // among lo .. lo + n - 1, or lo + n
+    while (n) {
+        const uint32_t each = (n + 31) / 32, at = (threadIdx.x & 31) * each, last = at + each < n ? at + each : n;   // a lane looks at the last of its share
+        const bool behind = at < n && first_row(a, lo + last) > r;
+        const uint32_t hits = __ballot_sync(0xFFFFFFFFu, behind);
+        if (!hits) return lo + n;
+        const uint32_t lane = __ffs(hits) - 1, from = lane * each;
+        lo += from;
+        n = (from + each < n ? each : n - from) - 1;                 // its last one is known to be behind
+    }
+    return lo;
+}
+
+// The rows of group b, and the process that holds the present one. A warp walks as one.
 struct RowWalk {
     const NormArgs& a;
     uint32_t r0, r1, start, end, b, p;
     bool any;                                   // the present process has rows here so far
-    __device__ __forceinline__ RowWalk(const NormArgs& args, uint32_t group) : a(args), b(group), any(false) {
+    __device__ __forceinline__ RowWalk(const NormArgs& args, uint32_t group) : a(args), start(0), end(~0u), b(group), p(0), any(false) {
         r0 = group * a.rows_per_group;
         r1 = a.rows - r0 < a.rows_per_group ? a.rows : r0 + a.rows_per_group;
-        start = 0; end = ~0u; p = 0;
-        if (!a.slots) return;
-        uint32_t lo = 0, hi = a.P;              // the first process that ends behind r0 (P if none does)
-        while (lo < hi) {
-            const uint32_t mid = (lo + hi) / 2;
-            if (first_row(a, mid + 1) > r0) hi = mid; else lo = mid + 1;
-        }
-        p = lo;
-        bounds();
     }
+    __device__ __forceinline__ void find() { p = holder(a, r0); bounds(); }
     __device__ __forceinline__ void bounds() {
         start = p < a.P ? first_row(a, p) : ~0u;
         end = p < a.P ? first_row(a, p + 1) : ~0u;
@@ -353,8 +362,8 @@ template <typename T, typename W, int MODE, int NV> __device__ __forceinline__ v
 }
 
 // blockDim = (G, groups in the block).
-template <typename T, typename W, int MODE, bool ALL, int NV, int D>
-__global__ void __launch_bounds__(kMaxGroup) norm_forward_kernel(NormArgs a) {
+template <typename T, typename W, int MODE, bool ALL, int NV, int D, int MAXT>
+__global__ void __launch_bounds__(MAXT, MAXT <= 256 ? 768 / MAXT : 1) norm_forward_kernel(NormArgs a) {
     using P = Part<T, MODE, NV>;
     constexpr int H2 = P::E / 2;
     extern __shared__ uint4 ring_memory[];
@@ -426,6 +435,7 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
     uint32_t turn = 0;
     const uint32_t bytes = blockDim.x / 32 * P::PLACE, group = blockIdx.x * blockDim.y + threadIdx.y;
     char* ring = reinterpret_cast<char*>(ring_memory) + threadIdx.y * D * 2 * bytes + (threadIdx.x >> 5) * P::PLACE;
+    later_kernel_may_start();
     clear_scratch(scratch);
     if (group >= a.groups) return;                                   // whole warps, and in blocks of one group nobody
     RowWalk walk(a, group);
@@ -439,6 +449,8 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
         copies_end_batch();
         put += 2 * bytes;
     }
+    float nmean = a.mean[walk.r0], nrstd = a.rstd[walk.r0];
+    if (a.slots) walk.find();
     F2 g[H2], dg[H2], db[H2];
     read_weights<T, W, MODE, NV>(g, a.gamma, 1.f, a.H);
 #pragma unroll
@@ -455,7 +467,6 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
             else store_slot<P::N>(a, walk.slot(), q * P::N, x, y);
         }
     };
-    float nmean = a.mean[walk.r0], nrstd = a.rstd[walk.r0];
     for (uint32_t r = walk.r0; r < walk.r1; ++r) {
         copies_wait<D - 2>();
         if (P::SHIFT) __syncwarp();
@@ -508,22 +519,23 @@ template <typename K> static cudaError_t allow_shared(K kernel, size_t bytes) {
     return bytes <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
-template <typename T, typename W, int MODE, bool ALL, int NV, int D> static cudaError_t forward_launch(const NormArgs& a, dim3 block, int sms, cudaStream_t st) {
+template <typename T, typename W, int MODE, bool ALL, int NV, int D, int MAXT> static cudaError_t forward_launch(const NormArgs& a, dim3 block, int sms, cudaStream_t st) {
     using P = Part<T, MODE, NV>;
     const size_t smem = (size_t)block.y * D * (block.x / 32) * P::PLACE;
-    const cudaError_t e = allow_shared(norm_forward_kernel<T, W, MODE, ALL, NV, D>, smem);
+    const cudaError_t e = allow_shared(norm_forward_kernel<T, W, MODE, ALL, NV, D, MAXT>, smem);
     if (e != cudaSuccess) return e;
     const uint32_t threads = block.x * block.y, per_sm = threads < 768 ? 768 / threads : 1;
     const uint32_t blocks = (a.rows + block.y - 1) / block.y, cap = (uint32_t)sms * per_sm;
-    norm_forward_kernel<T, W, MODE, ALL, NV, D><<<blocks < cap ? blocks : cap, block, smem, st>>>(a);
+    norm_forward_kernel<T, W, MODE, ALL, NV, D, MAXT><<<blocks < cap ? blocks : cap, block, smem, st>>>(a);
     return cudaGetLastError();
 }
 template <typename T, typename W, int MODE, int NV, int D> static cudaError_t forward_run(const NormArgs& a, int sms, cudaStream_t st) {
     using P = Part<T, MODE, NV>;
     const dim3 block = group_shape((a.H + P::N - 1) / P::N, NV);
     if constexpr (MODE == kAligned)
-        if (a.H == NV * P::N * block.x) return forward_launch<T, W, MODE, true, NV, D>(a, block, sms, st);
-    return forward_launch<T, W, MODE, false, NV, D>(a, block, sms, st);
+        if (a.H == NV * P::N * block.x)
+            return block.x <= 256 ? forward_launch<T, W, MODE, true, NV, D, 256>(a, block, sms, st) : forward_launch<T, W, MODE, true, NV, D, kMaxGroup>(a, block, sms, st);
+    return block.x <= 256 ? forward_launch<T, W, MODE, false, NV, D, 256>(a, block, sms, st) : forward_launch<T, W, MODE, false, NV, D, kMaxGroup>(a, block, sms, st);
 }
 
 // cudaErrorNotSupported: the row does not fit.

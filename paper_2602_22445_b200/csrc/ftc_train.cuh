@@ -22,6 +22,19 @@ template <typename V> __device__ __forceinline__ V warp_sum(V v) {
     return v;
 }
 
+// Two kernels of one call: the second one may be put on the GPU while the first is at work (all of whose blocks are there at once) and
+// waits for its results only where it needs them.
+__device__ __forceinline__ void later_kernel_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_earlier_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+template <typename... A> cudaError_t launch_second(void (*kernel)(A...), dim3 grid, dim3 block, cudaStream_t st, A... args) {
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t how{};
+    how.gridDim = grid; how.blockDim = block; how.stream = st; how.attrs = &early; how.numAttrs = 1;
+    return cudaLaunchKernelEx(&how, kernel, args...);
+}
+
 // ---- the table of tensors: header, entries, one tensor index for each block of FTC_STATE_BLOCK elements ----
 
 constexpr uint64_t kTableMagic = 0x3154424154435446ull;
