@@ -418,22 +418,31 @@ constexpr int kAhead = 4;                                        // blocks whose
 
 // Sum of the squares of 8 numbers. In float32 where that neither overflows nor loses small squares (4 roundings at most one after the
 // other), else in float64.
+__device__ __noinline__ double squares_64(F2 a, F2 b, F2 c, F2 d) {
+    const F2 g[4] = {a, b, c, d};
+    double s = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s += (double)lo(g[i]) * lo(g[i]) + (double)hi(g[i]) * hi(g[i]);
+    return s;
+}
 __device__ __forceinline__ double squares(const F2* g) {
     const F2 s = add(fma(g[0], g[0], mul(g[1], g[1])), fma(g[2], g[2], mul(g[3], g[3])));
     const float f = lo(s) + hi(s);
-    if (f >= 1e-30f && f <= 1e38f) return (double)f;
-    double d = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) d += (double)lo(g[i]) * lo(g[i]) + (double)hi(g[i]) * hi(g[i]);
-    return d;
+    return f >= 1e-30f && f <= 1e38f ? (double)f : squares_64(g[0], g[1], g[2], g[3]);
 }
 
-template <bool WIDE> __device__ __forceinline__ double block_squares(const Raw& x, const TableEntry& t, uint64_t e0, uint32_t lane, uint32_t left) {
+// Any block of any tensor, the narrow way.
+__device__ __noinline__ double block_squares(const TableEntry& t, uint64_t b) {
+    Raw x;
     F2 g[4];
-    numbers<WIDE>(g, x, t.grad_dtype);
+    const uint32_t lane = threadIdx.x & 31;
+    const uint64_t e0 = (b - t.first_block) * FTC_STATE_BLOCK, rest = t.n - e0;
+    const uint32_t left = rest < FTC_STATE_BLOCK ? (uint32_t)rest : FTC_STATE_BLOCK;
+    load_raw<false>(x, t.grad, t.grad_dtype, e0, lane, left);
+    numbers<false>(g, x, t.grad_dtype);
     if (t.status) {
         F2 w[4];
-        const uint32_t live = shares<WIDE>(w, t, e0, lane, left);
+        const uint32_t live = shares<false>(w, t, e0, lane, left);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             g[i] = mul(g[i], w[i]);
@@ -443,52 +452,105 @@ template <bool WIDE> __device__ __forceinline__ double block_squares(const Raw& 
     return squares(g);                                               // elements behind the end were loaded as zeros
 }
 
-__global__ void __launch_bounds__(kWarps * 32) grad_squares_kernel(const void* table, uint32_t n_params, uint64_t n_blocks, uint64_t span, double* slots, uint32_t* ticket) {
+// `blocks` full aligned blocks of elements of one type from `p` (this lane's first) on; record `message` and every `stride`-th after
+// it for those that have one.
+template <uint32_t DTYPE, bool STATUS>
+__device__ __forceinline__ double run_squares(const char* p, uint32_t blocks, const uint32_t* status, uint32_t message, uint32_t stride) {
+    constexpr uint32_t BYTES = FTC_STATE_BLOCK * (DTYPE == FTC_F32 ? 4 : 2);
+    double s = 0;
+    const uint2* st = reinterpret_cast<const uint2*>(status + (uint64_t)message * FTC_STATUS_WORDS);
+    const uint64_t next = (uint64_t)stride * (FTC_STATUS_WORDS / 2);
+    const auto add_one = [&](const Raw& x, uint2 r) {
+        F2 g[4];
+        numbers<true>(g, x, DTYPE);
+        const float share = STATUS ? share_of(r) : 1.f;
+        if (share > 0.f) s = ::fma((double)share * share, squares(g), s);
+    };
+    const auto load_one = [&](Raw& x, int i) { if (DTYPE == FTC_F32) load_32(p + i * BYTES, x.r); else load_16(p + i * BYTES, x.r); };
+    for (; blocks >= kAhead; blocks -= kAhead, p += kAhead * BYTES, st += kAhead * next) {
+        Raw x[kAhead];
+        uint2 r[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) { r[i] = STATUS ? st[i * next] : make_uint2(0u, 1u); load_one(x[i], i); }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) add_one(x[i], r[i]);
+    }
+    for (; blocks; --blocks, p += BYTES, st += next) {
+        Raw x;
+        const uint2 r = STATUS ? *st : make_uint2(0u, 1u);
+        load_one(x, 0);
+        add_one(x, r);
+    }
+    return s;
+}
+
+// The sums of one warp.
+__device__ __forceinline__ void warp_squares(const void* table, uint32_t n_params, uint64_t n_blocks, uint64_t span, uint64_t w, double* slots) {
     const uint32_t lane = threadIdx.x & 31;
-    const uint64_t w = blockIdx.x * (uint64_t)kWarps + (threadIdx.x >> 5);
-    if (w == 0 && lane == 0) *ticket = 0;
     uint64_t b = w * span;
     const uint64_t b1 = b + span < n_blocks ? b + span : n_blocks;
     while (b < b1) {
         const uint32_t ti = table_map(table, n_params)[b];
-        const TableEntry t = table_entries(table)[ti];
-        const uint64_t last = t.first_block + (t.n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK, end = last < b1 ? last : b1;
-        const uint64_t whole = t.wide ? t.first_block + t.n / FTC_STATE_BLOCK : 0, end_wide = whole < end ? whole : end;
-        const bool plain = t.status && t.k % 8 == 0 && t.n <= 0xFFFFFFFFull;    // a lane's eight elements are of one message
+        const TableEntry& t = table_entries(table)[ti];
+        const uint64_t first = t.first_block, n = t.n, last = first + (n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK, end = last < b1 ? last : b1;
+        const uint32_t k = t.k, dtype = t.grad_dtype;
+        // runs: full blocks on wide boundaries; with records, where messages fit a block and hold whole lanes
+        const bool run = t.wide && (!t.status || (k % 8 == 0 && FTC_STATE_BLOCK % k == 0 && n <= 0xFFFFFFFFull));
+        const uint64_t whole = run ? first + n / FTC_STATE_BLOCK : 0, end_run = whole < end ? whole : end;
         double s = 0;
-        for (; b + kAhead <= end_wide; b += kAhead) {
-            Raw x[kAhead];
-            const uint64_t e0 = (b - t.first_block) * FTC_STATE_BLOCK;
-            uint2 st[kAhead];
-            if (plain) {
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) st[i] = record(t, ((uint32_t)e0 + i * FTC_STATE_BLOCK + lane * 8) / t.k);
-            }
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) load_raw<true>(x[i], t.grad, t.grad_dtype, e0 + i * FTC_STATE_BLOCK, lane, FTC_STATE_BLOCK);
-            if (!plain) {
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) s += block_squares<true>(x[i], t, e0 + i * FTC_STATE_BLOCK, lane, FTC_STATE_BLOCK);
-                continue;
-            }
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                F2 g[4];
-                numbers<true>(g, x[i], t.grad_dtype);
-                const float share = share_of(st[i]);
-                if (share > 0.f) s = ::fma((double)share * share, squares(g), s);
-            }
+        if (b < end_run) {
+            const uint64_t e = (b - first) * FTC_STATE_BLOCK + lane * 8;
+            const char* p = static_cast<const char*>(t.grad) + e * (dtype == FTC_F32 ? 4 : 2);
+            const uint32_t blocks = (uint32_t)(end_run - b);
+            if (t.status) {
+                const uint32_t message = (uint32_t)e / k, stride = FTC_STATE_BLOCK / k;
+                s = dtype == FTC_F32 ? run_squares<FTC_F32, true>(p, blocks, t.status, message, stride)
+                  : dtype == FTC_BF16 ? run_squares<FTC_BF16, true>(p, blocks, t.status, message, stride) : run_squares<FTC_F16, true>(p, blocks, t.status, message, stride);
+            } else
+                s = dtype == FTC_F32 ? run_squares<FTC_F32, false>(p, blocks, nullptr, 0, 0)
+                  : dtype == FTC_BF16 ? run_squares<FTC_BF16, false>(p, blocks, nullptr, 0, 0) : run_squares<FTC_F16, false>(p, blocks, nullptr, 0, 0);
+            b = end_run;
         }
-        for (; b < end; ++b) {
-            Raw x;
-            const uint64_t e0 = (b - t.first_block) * FTC_STATE_BLOCK, rest = t.n - e0;
-            const uint32_t left = rest < FTC_STATE_BLOCK ? (uint32_t)rest : FTC_STATE_BLOCK;
-            load_raw<false>(x, t.grad, t.grad_dtype, e0, lane, left);
-            s += block_squares<false>(x, t, e0, lane, left);
-        }
+        for (; b < end; ++b) s += block_squares(t, b);
         s = warp_sum(s);
         if (lane == 0) slots[w + ti] = s;
     }
+}
+
+__global__ void __launch_bounds__(kWarps * 32, 3) grad_squares_kernel(const void* table, uint32_t n_params, uint64_t n_blocks, uint64_t span, double* slots, uint32_t* ticket) {
+    later_kernel_may_start();
+    const uint64_t w = blockIdx.x * (uint64_t)kWarps + (threadIdx.x >> 5);
+    if (w == 0 && (threadIdx.x & 31) == 0) *ticket = 0;
+    warp_squares(table, n_params, n_blocks, span, w, slots);
+}
+
+__device__ __forceinline__ void give_norm(double s, float max_norm, float* norm) {
+    const float r = (float)sqrt(s);
+    norm[0] = r;
+    norm[1] = !isfinite(r) ? __uint_as_float(0x7FC00000u) : r > max_norm ? max_norm / r : 1.f;
+}
+
+// Tables of few blocks: all in one thread block, the sums through the workspace.
+constexpr uint32_t kSoloWarps = 32, kSoloSpan = 16;
+__global__ void __launch_bounds__(kSoloWarps * 32) grad_norm_solo_kernel(const void* table, uint32_t n_params, uint64_t n_blocks, uint64_t span, float max_norm, double* slots,
+                                                                         float* norm, float* norms) {
+    __shared__ double part[kSoloWarps];
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    warp_squares(table, n_params, n_blocks, span, warp, slots);
+    __syncthreads();
+    double all = 0;
+    for (uint32_t ti = warp; ti < n_params; ti += kSoloWarps) {
+        const uint64_t n = table_entries(table)[ti].n, first = table_entries(table)[ti].first_block;
+        const uint32_t w0 = (uint32_t)(first / span), w1 = n ? (uint32_t)((first + (n - 1) / FTC_STATE_BLOCK) / span) + 1 : w0;      // at most kSoloWarps warps
+        const double s = warp_sum(w0 + lane < w1 ? slots[w0 + lane + ti] : 0.0);
+        if (lane == 0 && norms) norms[ti] = (float)sqrt(s);
+        all += s;
+    }
+    if (lane == 0) part[warp] = all;
+    __syncthreads();
+    if (warp) return;
+    all = warp_sum(part[lane]);
+    if (lane == 0) give_norm(all, max_norm, norm);
 }
 
 __device__ __forceinline__ double block_sum(double s, double* part) {          // 128 threads
@@ -506,9 +568,11 @@ __global__ void __launch_bounds__(128) grad_norm_kernel(const void* table, uint3
                                                         uint32_t* ticket, float* norm, float* norms) {
     __shared__ double part[4];
     __shared__ bool mine;
+    if (blockIdx.x >= n_params) wait_for_earlier_kernel();           // the one block of an empty table
     for (uint32_t ti = blockIdx.x; ti < n_params; ti += gridDim.x) {
         const uint64_t n = table_entries(table)[ti].n, first = table_entries(table)[ti].first_block;
         double s = 0;
+        wait_for_earlier_kernel();
         if (n) {
             const uint64_t last = (first + (n - 1) / FTC_STATE_BLOCK) / span;
 #pragma unroll 8
@@ -527,31 +591,31 @@ __global__ void __launch_bounds__(128) grad_norm_kernel(const void* table, uint3
     double s = 0;
     for (uint32_t ti = threadIdx.x; ti < n_params; ti += 128) s += __ldcg(sums + ti);
     s = block_sum(s, part);
-    if (threadIdx.x == 0) {
-        const float r = (float)sqrt(s);
-        norm[0] = r;
-        norm[1] = !isfinite(r) ? __uint_as_float(0x7FC00000u) : r > max_norm ? max_norm / r : 1.f;
-    }
+    if (threadIdx.x == 0) give_norm(s, max_norm, norm);
 }
 
-// Warps that share the blocks: at most those the GPU holds.
+// Warps that share the blocks: at most those the GPU holds; of one thread block where all have a few blocks at most.
 uint32_t grad_norm_warps(uint64_t n_blocks, int sm_count) {
-    const uint64_t cap = (uint64_t)sm_count * 32;
+    if (n_blocks <= kSoloWarps * kSoloSpan) return kSoloWarps;
+    const uint64_t cap = (uint64_t)sm_count * kWarps * 3 * 4;                  // four rounds of thread blocks: who is done early takes the next
     return (uint32_t)(n_blocks < cap ? n_blocks : cap);
 }
 
 cudaError_t launch_grad_norm(const void* table, uint32_t n_params, uint64_t n_blocks, float max_norm, float* norm, float* norms, double* ws, int sm_count,
                              cudaStream_t st) {
-    const uint32_t warps = grad_norm_warps(n_blocks, sm_count), squares_grid = warps ? (warps + kWarps - 1) / kWarps : 1;
-    const uint64_t span = warps ? (n_blocks + warps - 1) / warps : 1;
+    const uint32_t warps = grad_norm_warps(n_blocks, sm_count);
+    const uint64_t span = n_blocks ? (n_blocks + warps - 1) / warps : 1;
     double *slots = ws + 1, *sums = slots + warps + n_params;
     uint32_t* ticket = reinterpret_cast<uint32_t*>(ws);
-    grad_squares_kernel<<<squares_grid, kWarps * 32, 0, st>>>(table, n_params, n_blocks, span, slots, ticket);
+    if (n_blocks <= kSoloWarps * kSoloSpan) {
+        grad_norm_solo_kernel<<<1, kSoloWarps * 32, 0, st>>>(table, n_params, n_blocks, span, max_norm, slots, norm, norms);
+        return cudaGetLastError();
+    }
+    grad_squares_kernel<<<(warps + kWarps - 1) / kWarps, kWarps * 32, 0, st>>>(table, n_params, n_blocks, span, slots, ticket);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    const uint32_t cap = (uint32_t)sm_count * 8, grid = n_params < cap ? (n_params ? n_params : 1) : cap;
-    grad_norm_kernel<<<grid, 128, 0, st>>>(table, n_params, span, max_norm, slots, sums, ticket, norm, norms);
-    return cudaGetLastError();
+    const uint32_t cap = (uint32_t)sm_count * 8;
+    return launch_second(grad_norm_kernel, n_params < cap ? n_params : cap, 128, st, table, n_params, span, max_norm, (const double*)slots, sums, ticket, norm, norms);
 }
 
 }  // namespace ftc
