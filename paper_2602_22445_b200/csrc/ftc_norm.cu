@@ -22,6 +22,59 @@ __device__ __forceinline__ float block_sum(float v, float* scratch) {
     return s;
 }
 
+// Rows of up to 32 elements a thread, from memory to registers and back; weights come from the caches.
+constexpr int kLongest = 32 * 1024;
+template <typename T, typename W, int VB>
+__global__ void __launch_bounds__(1024) norm_forward_wide_kernel(NormArgs a) {
+    using V = Pack<T, VB>;
+    constexpr int N = V::N, NV = 32 / N;
+    __shared__ float scratch[2][32];
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x / 32, v0 = warp * 32 * NV + lane, vecs = a.H / N;
+    const auto sum = [&](float v, int turn) {
+        v = warp_sum(v);
+        if (lane == 0) scratch[turn][warp] = v;
+        __syncthreads();
+        return warp_sum(lane < warps ? scratch[turn][lane] : 0.f);
+    };
+    for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const T* x = static_cast<const T*>(a.x) + r * a.x_stride;
+        T* y = static_cast<T*>(a.y) + r * a.y_stride;
+        V v[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (v0 + i * 32 < vecs) v[i].load(x + (v0 + i * 32) * N); else v[i].clear();
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) s += v[i].get(j);
+        const float mean = sum(s, 0) / a.H;
+        s = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (v0 + i * 32 < vecs) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) { const float d = v[i].get(j) - mean; s = fmaf(d, d, s); }
+            }
+        const float rstd = inverse_root(sum(s, 1) / a.H + a.eps);    // each place is written again behind the other one's barrier
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t c = (v0 + i * 32) * N;
+            if (c >= a.H) continue;
+            float g[N], b[N], o[N];
+            load_weights<W, N>(g, static_cast<const W*>(a.gamma), c, 1.f);
+            load_weights<W, N>(b, static_cast<const W*>(a.beta), c, 0.f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) o[j] = fmaf((v[i].get(j) - mean) * rstd, g[j], b[j]);
+            V::store(y + c, o);
+        }
+        if (threadIdx.x == 0) {
+            if (a.mean_out) a.mean_out[r] = mean;
+            if (a.rstd_out) a.rstd_out[r] = rstd;
+        }
+    }
+}
+
 // A block walks a row three times; rows come back from the caches.
 template <typename T, typename W>
 __global__ void __launch_bounds__(kThreads) norm_forward_long_kernel(NormArgs a) {
@@ -46,25 +99,43 @@ __global__ void __launch_bounds__(kThreads) norm_forward_long_kernel(NormArgs a)
     }
 }
 
-// dx alone.
-template <typename T, typename W>
-__global__ void __launch_bounds__(kThreads) norm_backward_long_kernel(NormArgs a) {
-    __shared__ float scratch[kThreads / 32];
-    const W* gamma = static_cast<const W*>(a.gamma);
-    for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+// dx alone; a block walks a row twice, the second time from the caches.
+template <typename T, typename W, int VB>
+__global__ void __launch_bounds__(1024) norm_backward_long_kernel(NormArgs a) {
+    using V = Pack<T, VB>;
+    constexpr int N = V::N;
+    __shared__ float2 scratch[32];
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x / 32, step = blockDim.x * N;
+    for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const T* x = static_cast<const T*>(a.x) + r * a.x_stride;
         const T* dy = static_cast<const T*>(a.dy) + r * a.dy_stride;
         T* dx = static_cast<T*>(a.dx) + r * a.dx_stride;
         const float mean = a.mean[r], rstd = a.rstd[r];
         float s1 = 0.f, s2 = 0.f;
-        for (uint32_t h = threadIdx.x; h < a.H; h += kThreads) {
-            const float xh = (to_f32(x[h]) - mean) * rstd, u = to_f32(dy[h]) * (gamma ? to_f32(gamma[h]) : 1.f);
-            s1 += u; s2 = fmaf(u, xh, s2);
+#pragma unroll 4
+        for (uint32_t c = threadIdx.x * N; c < a.H; c += step) {     // N divides H
+            V v, d;
+            float g[N];
+            v.load(x + c); d.load(dy + c);
+            load_weights<W, N>(g, static_cast<const W*>(a.gamma), c, 1.f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) { const float u = d.get(j) * g[j]; s1 += u; s2 = fmaf(u, (v.get(j) - mean) * rstd, s2); }
         }
-        const float c1 = block_sum(s1, scratch) / a.H, c2 = block_sum(s2, scratch) / a.H;
-        for (uint32_t h = threadIdx.x; h < a.H; h += kThreads) {
-            const float xh = (to_f32(x[h]) - mean) * rstd, u = to_f32(dy[h]) * (gamma ? to_f32(gamma[h]) : 1.f);
-            dx[h] = from_f32<T>(rstd * (u - c1 - xh * c2));
+        s1 = warp_sum(s1); s2 = warp_sum(s2);
+        __syncthreads();
+        if (lane == 0) scratch[warp] = make_float2(s1, s2);
+        __syncthreads();
+        const float2 part = lane < warps ? scratch[lane] : make_float2(0.f, 0.f);
+        const float c1 = warp_sum(part.x) / a.H, c2 = warp_sum(part.y) / a.H;
+#pragma unroll 4
+        for (uint32_t c = threadIdx.x * N; c < a.H; c += step) {
+            V v, d;
+            float g[N], o[N];
+            v.load(x + c); d.load(dy + c);
+            load_weights<W, N>(g, static_cast<const W*>(a.gamma), c, 1.f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) o[j] = rstd * (fmaf(d.get(j), g[j], -c1) - (v.get(j) - mean) * rstd * c2);
+            V::store(dx + c, o);
         }
     }
 }
@@ -163,6 +234,12 @@ static uint32_t row_vector(const NormArgs& a) {
 template <typename T, typename W> static cudaError_t forward(const NormArgs& a, int sms, cudaStream_t st) {
     const cudaError_t e = forward_rows<T, W>(a, row_vector(a), sms, st);
     if (e != cudaErrorNotSupported) return e;
+    if (a.H <= kLongest) {
+        const uint32_t threads = (a.H + 1023) / 1024 * 32, cap = (uint32_t)sms * (1024 / threads), grid = a.rows < cap ? a.rows : cap;
+        if (row_vector(a) == 16) norm_forward_wide_kernel<T, W, 16><<<grid, threads, 0, st>>>(a);
+        else norm_forward_wide_kernel<T, W, sizeof(T)><<<grid, threads, 0, st>>>(a);
+        return cudaGetLastError();
+    }
     const uint64_t cap = (uint64_t)sms * 8;
     norm_forward_long_kernel<T, W><<<(uint32_t)(a.rows < cap ? a.rows : cap), kThreads, 0, st>>>(a);
     return cudaGetLastError();
@@ -174,14 +251,14 @@ cudaError_t launch_norm_forward(const NormArgs& a, int sms, cudaStream_t st) {
     return a.wdtype == FTC_F32 ? forward<__half, float>(a, sms, st) : forward<__half, __half>(a, sms, st);
 }
 
-// Groups that share the rows in the backward pass: as many as the GPU runs at once, at least 16 rows each where there are rows enough
-// (each group writes and the second kernel reads 8 bytes a column: 16 rows keep that under a sixth of the rows' own 96 bytes and more),
-// fewer where their partial sums would take up more than 2 GiB.
+// Groups that share the rows in the backward pass: as many as the GPU runs at once. Each group writes and the second kernel reads 8 bytes a
+// column: where that comes to more than 8 MB in all, groups have at least 16 rows (which keeps it under a sixth of the rows' own 96 bytes
+// and more), and never partial sums of more than 2 GiB.
 uint32_t norm_backward_groups(uint32_t H, uint64_t rows, int sms) {
     const uint32_t g = group_threads(H), per_sm = g < 512 ? 512 / g : 1;
     uint64_t n = (uint64_t)sms * per_sm;
-    const uint64_t few = rows / 16 > (uint64_t)sms ? rows / 16 : (uint64_t)sms, room = (1ull << 28) / H;
-    if (n > few) n = few;
+    const uint64_t cheap = (1u << 20) / H, few = rows / 16 > (uint64_t)sms ? rows / 16 : (uint64_t)sms, room = (1ull << 28) / H;
+    if (n > few && n > cheap) n = few > cheap ? few : cheap;
     if (n > room) n = room ? room : 1;
     if (n > rows) n = rows;
     if (n == 0) return 0;
@@ -203,8 +280,9 @@ template <typename T, typename W> static cudaError_t backward(const NormArgs& a,
     const cudaError_t e = backward_rows<T, W>(a, row_vector(a), st);
     if (e != cudaErrorNotSupported) return e;
     if (a.slots) { const cudaError_t c = columns<T>(a, st); if (c != cudaSuccess || !a.dx) return c; }
-    const uint64_t cap = (uint64_t)sms * 8;
-    norm_backward_long_kernel<T, W><<<(uint32_t)(a.rows < cap ? a.rows : cap), kThreads, 0, st>>>(a);
+    const uint32_t threads = 512, cap = (uint32_t)sms * 4, grid = a.rows < cap ? a.rows : cap;
+    if (row_vector(a) == 16) norm_backward_long_kernel<T, W, 16><<<grid, threads, 0, st>>>(a);
+    else norm_backward_long_kernel<T, W, sizeof(T)><<<grid, threads, 0, st>>>(a);
     return cudaGetLastError();
 }
 

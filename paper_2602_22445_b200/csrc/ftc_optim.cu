@@ -103,16 +103,21 @@ __device__ __forceinline__ uint2 record(const TableEntry& t, uint64_t message) {
 // 1 / processes included, 0 where the message was not delivered.
 __device__ __forceinline__ float share_of(uint2 s) { return (s.x & 0xFFu) == FTC_ST_OK && s.y ? 1.f / (float)s.y : 0.f; }
 
-// What each of the lane's elements is multiplied with, and which were delivered (bits). One division where the lane's elements are
-// neighbours; elements and messages of more than 32 bits take the long one.
+// The message of element e, and its place in there. Messages of a power of two elements take a shift; elements of more than 32 bits the long
+// division.
+__device__ __forceinline__ uint64_t message_of(const TableEntry& t, uint64_t e, uint32_t& place) {
+    if (t.k_shift != 255) { place = (uint32_t)e & (t.k - 1); return e >> t.k_shift; }
+    const uint64_t q = e <= 0xFFFFFFFFull ? (uint32_t)e / t.k : e / t.k;
+    place = (uint32_t)(e - q * t.k);
+    return q;
+}
+
+// What each of the lane's elements is multiplied with, and which were delivered (bits).
 template <bool WIDE> __device__ __forceinline__ uint32_t shares(F2* w, const TableEntry& t, uint64_t e0, uint32_t lane, uint32_t left) {
-    uint32_t live = 0;
+    uint32_t live = 0, r;
     float f[8];
-    const bool small = e0 + FTC_STATE_BLOCK <= 0xFFFFFFFFull;
-    if (WIDE) {
-        const uint64_t e = e0 + lane * 8;
-        uint64_t q = small ? (uint32_t)e / t.k : e / t.k;
-        uint32_t r = (uint32_t)(e - q * t.k);
+    if (WIDE) {                                                      // neighbours: one division
+        uint64_t q = message_of(t, e0 + lane * 8, r);
         float s = share_of(record(t, q));
         if (t.k - r >= 8) {                                          // one message has all eight
 #pragma unroll
@@ -125,15 +130,27 @@ template <bool WIDE> __device__ __forceinline__ uint32_t shares(F2* w, const Tab
             live |= (s > 0.f ? 1u : 0u) << j;
             if (j < 7 && ++r == t.k) { r = 0; s = share_of(record(t, ++q)); }
         }
+    } else if (t.k >= 3) {                                           // the block's messages, at most 87, over the lanes of the warp
+        const uint64_t q = message_of(t, e0, r);
+        const uint32_t last = (r + left - 1) / t.k, more = 32 / t.k, over = 32 - more * t.k;
+        float s[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) s[i] = lane + i * 32 <= last ? share_of(record(t, q + lane + i * 32)) : 0.f;
+        uint32_t m = (r + lane) / t.k, place = r + lane - m * t.k;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float a = __shfl_sync(0xFFFFFFFFu, s[0], m & 31), b = __shfl_sync(0xFFFFFFFFu, s[1], m & 31), c = __shfl_sync(0xFFFFFFFFu, s[2], m & 31);
+            f[j] = m < 32 ? a : m < 64 ? b : c;
+            if (at<WIDE>(lane, j) >= left) f[j] = 0.f;
+            live |= (f[j] > 0.f ? 1u : 0u) << j;
+            m += more; place += over;
+            if (place >= t.k) { place -= t.k; ++m; }
+        }
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            f[j] = 0.f;
-            if (at<WIDE>(lane, j) < left) {
-                const uint64_t e = e0 + at<WIDE>(lane, j);
-                f[j] = share_of(record(t, small ? (uint32_t)e / t.k : e / t.k));
-                live |= (f[j] > 0.f ? 1u : 0u) << j;
-            }
+            f[j] = at<WIDE>(lane, j) < left ? share_of(record(t, message_of(t, e0 + at<WIDE>(lane, j), r))) : 0.f;
+            live |= (f[j] > 0.f ? 1u : 0u) << j;
         }
     }
 #pragma unroll
@@ -431,18 +448,13 @@ __device__ __forceinline__ double squares(const F2* g) {
     return f >= 1e-30f && f <= 1e38f ? (double)f : squares_64(g[0], g[1], g[2], g[3]);
 }
 
-// Any block of any tensor, the narrow way.
-__device__ __noinline__ double block_squares(const TableEntry& t, uint64_t b) {
-    Raw x;
+// The squares of one block that was loaded, with its records.
+template <bool WIDE> __device__ __forceinline__ double block_squares(const Raw& x, const TableEntry& t, uint64_t e0, uint32_t left) {
     F2 g[4];
-    const uint32_t lane = threadIdx.x & 31;
-    const uint64_t e0 = (b - t.first_block) * FTC_STATE_BLOCK, rest = t.n - e0;
-    const uint32_t left = rest < FTC_STATE_BLOCK ? (uint32_t)rest : FTC_STATE_BLOCK;
-    load_raw<false>(x, t.grad, t.grad_dtype, e0, lane, left);
-    numbers<false>(g, x, t.grad_dtype);
+    numbers<WIDE>(g, x, t.grad_dtype);
     if (t.status) {
         F2 w[4];
-        const uint32_t live = shares<false>(w, t, e0, lane, left);
+        const uint32_t live = shares<WIDE>(w, t, e0, threadIdx.x & 31, left);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             g[i] = mul(g[i], w[i]);
@@ -450,6 +462,23 @@ __device__ __noinline__ double block_squares(const TableEntry& t, uint64_t b) {
         }
     }
     return squares(g);                                               // elements behind the end were loaded as zeros
+}
+// Blocks b .. end - 1 of any tensor, two of them under way.
+template <bool WIDE> __device__ __forceinline__ double walk_squares(const TableEntry& t, uint64_t b, uint64_t end) {
+    const uint32_t lane = threadIdx.x & 31;
+    double s = 0;
+    for (uint64_t e0 = (b - t.first_block) * FTC_STATE_BLOCK; b < end; b += 2, e0 += 2 * FTC_STATE_BLOCK) {
+        Raw x, y;
+        const uint64_t rest = t.n - e0;
+        const bool two = b + 1 < end;
+        const uint32_t left = rest < FTC_STATE_BLOCK ? (uint32_t)rest : FTC_STATE_BLOCK;
+        const uint32_t more = !two ? 0 : rest < 2 * FTC_STATE_BLOCK ? (uint32_t)rest - FTC_STATE_BLOCK : FTC_STATE_BLOCK;
+        load_raw<WIDE>(x, t.grad, t.grad_dtype, e0, lane, left);
+        if (two) load_raw<WIDE>(y, t.grad, t.grad_dtype, e0 + FTC_STATE_BLOCK, lane, more);
+        s += block_squares<WIDE>(x, t, e0, left);
+        if (two) s += block_squares<WIDE>(y, t, e0 + FTC_STATE_BLOCK, more);
+    }
+    return s;
 }
 
 // `blocks` full aligned blocks of elements of one type from `p` (this lane's first) on; record `message` and every `stride`-th after
@@ -475,11 +504,15 @@ __device__ __forceinline__ double run_squares(const char* p, uint32_t blocks, co
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) add_one(x[i], r[i]);
     }
-    for (; blocks; --blocks, p += BYTES, st += next) {
-        Raw x;
-        const uint2 r = STATUS ? *st : make_uint2(0u, 1u);
-        load_one(x, 0);
-        add_one(x, r);
+    if (blocks) {
+        Raw x[kAhead - 1];
+        uint2 r[kAhead - 1];
+#pragma unroll
+        for (int i = 0; i < kAhead - 1; ++i)
+            if (i < (int)blocks) { r[i] = STATUS ? st[i * next] : make_uint2(0u, 1u); load_one(x[i], i); }
+#pragma unroll
+        for (int i = 0; i < kAhead - 1; ++i)
+            if (i < (int)blocks) add_one(x[i], r[i]);
     }
     return s;
 }
@@ -494,6 +527,7 @@ __device__ __forceinline__ void warp_squares(const void* table, uint32_t n_param
         const TableEntry& t = table_entries(table)[ti];
         const uint64_t first = t.first_block, n = t.n, last = first + (n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK, end = last < b1 ? last : b1;
         const uint32_t k = t.k, dtype = t.grad_dtype;
+        const uint64_t full = t.wide ? first + n / FTC_STATE_BLOCK : 0, end_wide = full < end ? full : end;
         // runs: full blocks on wide boundaries; with records, where messages fit a block and hold whole lanes
         const bool run = t.wide && (!t.status || (k % 8 == 0 && FTC_STATE_BLOCK % k == 0 && n <= 0xFFFFFFFFull));
         const uint64_t whole = run ? first + n / FTC_STATE_BLOCK : 0, end_run = whole < end ? whole : end;
@@ -511,7 +545,8 @@ __device__ __forceinline__ void warp_squares(const void* table, uint32_t n_param
                   : dtype == FTC_BF16 ? run_squares<FTC_BF16, false>(p, blocks, nullptr, 0, 0) : run_squares<FTC_F16, false>(p, blocks, nullptr, 0, 0);
             b = end_run;
         }
-        for (; b < end; ++b) s += block_squares(t, b);
+        if (b < end_wide) { s += walk_squares<true>(t, b, end_wide); b = end_wide; }
+        if (b < end) { s += walk_squares<false>(t, b, end); b = end; }
         s = warp_sum(s);
         if (lane == 0) slots[w + ti] = s;
     }
@@ -531,7 +566,7 @@ __device__ __forceinline__ void give_norm(double s, float max_norm, float* norm)
 }
 
 // Tables of few blocks: all in one thread block, the sums through the workspace.
-constexpr uint32_t kSoloWarps = 32, kSoloSpan = 16;
+constexpr uint32_t kSoloWarps = 32, kSoloBlocks = 160;
 __global__ void __launch_bounds__(kSoloWarps * 32) grad_norm_solo_kernel(const void* table, uint32_t n_params, uint64_t n_blocks, uint64_t span, float max_norm, double* slots,
                                                                          float* norm, float* norms) {
     __shared__ double part[kSoloWarps];
@@ -594,20 +629,22 @@ __global__ void __launch_bounds__(128) grad_norm_kernel(const void* table, uint3
     if (threadIdx.x == 0) give_norm(s, max_norm, norm);
 }
 
-// Warps that share the blocks: at most those the GPU holds; of one thread block where all have a few blocks at most.
+// Warps that share the blocks: those that the GPU holds at once; of more than 8 blocks for each, four times as many (8 blocks at least:
+// two rounds of loads), so that who is done early takes the next.
 uint32_t grad_norm_warps(uint64_t n_blocks, int sm_count) {
-    if (n_blocks <= kSoloWarps * kSoloSpan) return kSoloWarps;
-    const uint64_t cap = (uint64_t)sm_count * kWarps * 3 * 4;                  // four rounds of thread blocks: who is done early takes the next
-    return (uint32_t)(n_blocks < cap ? n_blocks : cap);
+    const uint64_t held = (uint64_t)sm_count * kWarps * 3, most = n_blocks / 8 < 4 * held ? n_blocks / 8 : 4 * held;
+    const uint64_t warps = n_blocks <= 8 * held ? (n_blocks < held ? n_blocks : held) : most;
+    return (uint32_t)(warps < kSoloWarps ? kSoloWarps : warps);      // room for either kernel
 }
 
 cudaError_t launch_grad_norm(const void* table, uint32_t n_params, uint64_t n_blocks, float max_norm, float* norm, float* norms, double* ws, int sm_count,
                              cudaStream_t st) {
-    const uint32_t warps = grad_norm_warps(n_blocks, sm_count);
+    const bool solo = n_blocks <= kSoloBlocks && n_params <= 16;
+    const uint32_t warps = solo ? kSoloWarps : grad_norm_warps(n_blocks, sm_count);
     const uint64_t span = n_blocks ? (n_blocks + warps - 1) / warps : 1;
     double *slots = ws + 1, *sums = slots + warps + n_params;
     uint32_t* ticket = reinterpret_cast<uint32_t*>(ws);
-    if (n_blocks <= kSoloWarps * kSoloSpan) {
+    if (solo) {
         grad_norm_solo_kernel<<<1, kSoloWarps * 32, 0, st>>>(table, n_params, n_blocks, span, max_norm, slots, norm, norms);
         return cudaGetLastError();
     }

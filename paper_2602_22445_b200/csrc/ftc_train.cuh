@@ -42,7 +42,7 @@ struct TableHead { uint64_t magic, n_blocks; uint32_t n_params, flags; uint64_t 
 struct TableEntry {
     void* param; float* master; const void* grad; const uint32_t* status;
     uint64_t n, first_block;
-    uint32_t k; uint8_t param_dtype, grad_dtype, wide, pad;
+    uint32_t k; uint8_t param_dtype, grad_dtype, wide, k_shift;       // k_shift: k = 2^k_shift, or 255
     float lr_scale, weight_decay;
 };
 static_assert(sizeof(TableHead) == 32 && sizeof(TableEntry) == 64, "table layout");

@@ -125,7 +125,7 @@ int ftc_param_table_build(const ftc_param_t* h_params, uint32_t n_params, void* 
         const ftc_param_t& t = h_params[i];
         TableEntry& q = en[i];
         q.param = t.param; q.master = t.master; q.grad = t.grad; q.status = t.status; q.n = t.n; q.first_block = at;
-        q.k = t.status ? t.k : 1; q.param_dtype = (uint8_t)t.param_dtype; q.grad_dtype = (uint8_t)t.grad_dtype;
+        q.k = t.status ? t.k : 1; q.k_shift = q.k & (q.k - 1) ? 255 : (uint8_t)__builtin_ctz(q.k); q.param_dtype = (uint8_t)t.param_dtype; q.grad_dtype = (uint8_t)t.grad_dtype;
         q.wide = aligned(t.grad, 8 * size_of(t.grad_dtype)) && aligned(t.param, 8 * size_of(t.param_dtype)) && aligned(t.master, 32);   // 8 elements a load
         q.lr_scale = t.lr_scale; q.weight_decay = t.weight_decay;
         if (t.n && !t.param) h->flags |= 1u;
