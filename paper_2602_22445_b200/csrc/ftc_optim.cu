@@ -201,11 +201,14 @@ __device__ __forceinline__ float fast_inverse(float x) { float r; asm("rcp.appro
 
 
 // What a block needs, as loaded.
-struct BlockIn { Raw gr, pr, mr, vr; float ms, vs; };
+struct BlockIn { Raw gr, pr, mr, vr; float ms, vs; uint2 st; };
+// Do a lane's eight neighbours have one record, found by a shift? It is loaded with the rest then.
+__device__ __forceinline__ bool one_record(const TableEntry& t) { return t.k_shift >= 3 && t.k_shift != 255; }
 
 template <int BITS, bool WIDE>
 __device__ __forceinline__ void adamw_load(BlockIn& in, const AdamArgs& a, const TableEntry& t, uint64_t b, uint32_t lane, uint64_t e0, uint32_t left) {
     Raw &mr = in.mr, &vr = in.vr;
+    if (WIDE && t.status && one_record(t)) in.st = record(t, (e0 + lane * 8) >> t.k_shift);
     load_raw<WIDE>(in.gr, t.grad, t.grad_dtype, e0, lane, left);
     load_raw<WIDE>(in.pr, t.master ? t.master : t.param, t.master ? (uint32_t)FTC_F32 : t.param_dtype, e0, lane, left);
     const uint64_t q = b * FTC_STATE_BLOCK;
@@ -239,7 +242,12 @@ __device__ __forceinline__ void adamw_block(const BlockIn& in, const AdamArgs& a
     numbers<WIDE>(g, gr, t.grad_dtype);
     if (t.status) {
         F2 w[4];
-        live = shares<WIDE>(w, t, e0, lane, left);
+        if (WIDE && one_record(t)) {
+            const float s = share_of(in.st);
+            live = s > 0.f ? 0xFFu : 0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = twice(s);
+        } else live = shares<WIDE>(w, t, e0, lane, left);
 #pragma unroll
         for (int i = 0; i < 4; ++i) g[i] = mul(g[i], w[i]);
     } else live = inside<WIDE>(lane, left);
