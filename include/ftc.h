@@ -347,7 +347,8 @@ FTC_API int ftc_launch_blocks(const ftc_desc_t* desc, uint64_t S, int is_allredu
 typedef struct {
     uint32_t H;         /* elements of a row, 1 .. 2^24 */
     uint32_t P;         /* processes the rows are divided over (backward), 1 .. 2^20; 1: the ordinary weight gradient */
-    uint32_t k;         /* elements of a message (backward): the weight gradients are [ceil(H/k)][P][k]; k = H and P = 1: [H] */
+    uint32_t k;         /* elements of a message (backward), 1 .. 2^24: the weight gradients are [ceil(H/k)][P][k]; k = H and P = 1:
+                           [H]; (H + k) * P at most 2^35 */
     uint32_t dtype;     /* x, y, dy, dx: FTC_F32, FTC_BF16 or FTC_F16 */
     uint32_t wdtype;    /* gamma, beta: FTC_F32 or dtype */
     float    eps;       /* >= 0 */

@@ -99,11 +99,12 @@ __global__ void __launch_bounds__(kThreads) norm_forward_long_kernel(NormArgs a)
     }
 }
 
-// dx alone; a block walks a row twice, the second time from the caches.
-template <typename T, typename W, int VB>
+// dx alone. KEEP: the row stays in registers, four vectors a thread, as loaded; else a block walks it twice, the second time from the
+// caches.
+template <typename T, typename W, int VB, bool KEEP>
 __global__ void __launch_bounds__(1024) norm_backward_long_kernel(NormArgs a) {
     using V = Pack<T, VB>;
-    constexpr int N = V::N;
+    constexpr int N = V::N, NV = KEEP ? 4 : 1;
     __shared__ float2 scratch[32];
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x / 32, step = blockDim.x * N;
     for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
@@ -111,15 +112,28 @@ __global__ void __launch_bounds__(1024) norm_backward_long_kernel(NormArgs a) {
         const T* dy = static_cast<const T*>(a.dy) + r * a.dy_stride;
         T* dx = static_cast<T*>(a.dx) + r * a.dx_stride;
         const float mean = a.mean[r], rstd = a.rstd[r];
+        V v[NV], d[NV];
         float s1 = 0.f, s2 = 0.f;
-#pragma unroll 4
-        for (uint32_t c = threadIdx.x * N; c < a.H; c += step) {     // N divides H
-            V v, d;
+        const auto add = [&](const V& vi, const V& di, uint32_t c) {
             float g[N];
-            v.load(x + c); d.load(dy + c);
             load_weights<W, N>(g, static_cast<const W*>(a.gamma), c, 1.f);
 #pragma unroll
-            for (int j = 0; j < N; ++j) { const float u = d.get(j) * g[j]; s1 += u; s2 = fmaf(u, (v.get(j) - mean) * rstd, s2); }
+            for (int j = 0; j < N; ++j) { const float u = di.get(j) * g[j]; s1 += u; s2 = fmaf(u, (vi.get(j) - mean) * rstd, s2); }
+        };
+        if (KEEP) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const uint32_t c = threadIdx.x * N + i * step;
+                if (c < a.H) { v[i].load(x + c); d[i].load(dy + c); }            // N divides H
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const uint32_t c = threadIdx.x * N + i * step;
+                if (c < a.H) add(v[i], d[i], c);
+            }
+        } else {
+#pragma unroll 4
+            for (uint32_t c = threadIdx.x * N; c < a.H; c += step) { v[0].load(x + c); d[0].load(dy + c); add(v[0], d[0], c); }
         }
         s1 = warp_sum(s1); s2 = warp_sum(s2);
         __syncthreads();
@@ -127,15 +141,22 @@ __global__ void __launch_bounds__(1024) norm_backward_long_kernel(NormArgs a) {
         __syncthreads();
         const float2 part = lane < warps ? scratch[lane] : make_float2(0.f, 0.f);
         const float c1 = warp_sum(part.x) / a.H, c2 = warp_sum(part.y) / a.H;
-#pragma unroll 4
-        for (uint32_t c = threadIdx.x * N; c < a.H; c += step) {
-            V v, d;
+        const auto give = [&](const V& vi, const V& di, uint32_t c) {
             float g[N], o[N];
-            v.load(x + c); d.load(dy + c);
             load_weights<W, N>(g, static_cast<const W*>(a.gamma), c, 1.f);
 #pragma unroll
-            for (int j = 0; j < N; ++j) o[j] = rstd * (fmaf(d.get(j), g[j], -c1) - (v.get(j) - mean) * rstd * c2);
+            for (int j = 0; j < N; ++j) o[j] = rstd * (fmaf(di.get(j), g[j], -c1) - (vi.get(j) - mean) * rstd * c2);
             V::store(dx + c, o);
+        };
+        if (KEEP) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const uint32_t c = threadIdx.x * N + i * step;
+                if (c < a.H) give(v[i], d[i], c);
+            }
+        } else {
+#pragma unroll 4
+            for (uint32_t c = threadIdx.x * N; c < a.H; c += step) { v[0].load(x + c); d[0].load(dy + c); give(v[0], d[0], c); }
         }
     }
 }
@@ -185,39 +206,43 @@ __global__ void __launch_bounds__(kThreads) norm_columns_kernel(NormArgs a) {
     if (walk.any) store_slot<N>(a, walk.slot(), c, dg, db);
 }
 
-// dgamma[s][p][e], dbeta[s][p][e] from the slots: Q warps add the slots of one process for 32 columns, each every Q-th slot, and their
-// sums are added in order.
-template <int Q>
-__global__ void __launch_bounds__(Q == 32 ? 1024 : 256) norm_messages_kernel(NormArgs a, uint32_t tiles) {
+// dgamma[s][p][e], dbeta[s][p][e] from the slots: Q warps add the slots of one process for C columns a lane, each every Q-th slot, and
+// their sums are added in order.
+template <int Q, int C>
+__global__ void __launch_bounds__(Q == 32 ? 1024 : 256) norm_messages_kernel(NormArgs a, uint32_t tiles, uint32_t items) {
     constexpr int WARPS = Q == 32 ? 32 : 8;
     __shared__ float part[2][WARPS][32];
-    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, turn = warp % Q;
-    const uint64_t item = blockIdx.x * (uint64_t)(WARPS / Q) + warp / Q;
-    const uint32_t p = (uint32_t)(item / tiles), h = (uint32_t)(item % tiles) * 32 + lane;
-    float g = 0.f, b = 0.f;
-    const bool wanted = p < a.P && h < a.H;
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, turn = warp % Q, item = blockIdx.x * (WARPS / Q) + warp / Q;
+    const uint32_t p = item / tiles, h0 = (item - p * tiles) * (32 * C) + lane, S = (a.H + a.k - 1) / a.k;
+    float g[C] = {}, b[C] = {};
+    const bool wanted = item < items && h0 < a.H;
     const uint32_t lo = wanted ? first_row(a, p) : 0, hi = wanted ? first_row(a, p + 1) : 0;
     wait_for_earlier_kernel();
     if (lo < hi) {
         const uint32_t last = (hi - 1) / a.rows_per_group;
-#pragma unroll 4
+#pragma unroll(C > 1 ? 1 : 4)
         for (uint32_t grp = lo / a.rows_per_group + turn; grp <= last; grp += Q) {
-            const float* slot = a.slots + ((uint64_t)grp + p) * 2 * a.H + h;
-            g += slot[0];
-            b += slot[a.H];
+            const float* slot = a.slots + ((uint64_t)grp + p) * 2 * a.H + h0;
+#pragma unroll
+            for (int i = 0; i < C; ++i)
+                if (i == 0 || h0 + i * 32 < a.H) { g[i] += slot[i * 32]; b[i] += slot[a.H + i * 32]; }
         }
     }
-    if (Q > 1) {
-        part[0][warp][lane] = g; part[1][warp][lane] = b;
+    if (Q > 1) {                                                     // C = 1
+        part[0][warp][lane] = g[0]; part[1][warp][lane] = b[0];
         __syncthreads();
         if (turn) return;
-        for (int i = 1; i < Q; ++i) { g += part[0][warp + i][lane]; b += part[1][warp + i][lane]; }
+        for (int i = 1; i < Q; ++i) { g[0] += part[0][warp + i][lane]; b[0] += part[1][warp + i][lane]; }
     }
-    const uint32_t S = (a.H + a.k - 1) / a.k, s = h / a.k;
-    if (p >= a.P || s >= S) return;                                  // h beyond H: the last message's fill, zeros
-    const uint64_t o = ((uint64_t)s * a.P + p) * a.k + h % a.k;
-    if (a.dgamma) a.dgamma[o] = g;
-    if (a.dbeta) a.dbeta[o] = b;
+    if (item >= items) return;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        const uint32_t h = h0 + i * 32, s = h / a.k;
+        if (s >= S) return;                                          // h beyond H: the last message's fill, zeros
+        const uint64_t o = ((uint64_t)s * a.P + p) * a.k + (h - s * a.k);
+        if (a.dgamma) a.dgamma[o] = g[i];
+        if (a.dbeta) a.dbeta[o] = b[i];
+    }
 }
 
 static bool on(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
@@ -280,9 +305,15 @@ template <typename T, typename W> static cudaError_t backward(const NormArgs& a,
     const cudaError_t e = backward_rows<T, W>(a, row_vector(a), st);
     if (e != cudaErrorNotSupported) return e;
     if (a.slots) { const cudaError_t c = columns<T>(a, st); if (c != cudaSuccess || !a.dx) return c; }
-    const uint32_t threads = 512, cap = (uint32_t)sms * 4, grid = a.rows < cap ? a.rows : cap;
-    if (row_vector(a) == 16) norm_backward_long_kernel<T, W, 16><<<grid, threads, 0, st>>>(a);
-    else norm_backward_long_kernel<T, W, sizeof(T)><<<grid, threads, 0, st>>>(a);
+    const uint32_t v = row_vector(a), vecs = a.H * (uint32_t)sizeof(T) / 16;
+    if (v == 16 && vecs <= 4 * 1024) {
+        const uint32_t threads = (vecs + 127) / 128 * 32, cap = (uint32_t)sms * (1024 / threads);
+        norm_backward_long_kernel<T, W, 16, true><<<a.rows < cap ? a.rows : cap, threads, 0, st>>>(a);
+    } else {
+        const uint32_t cap = (uint32_t)sms * 4, grid = a.rows < cap ? a.rows : cap;
+        if (v == 16) norm_backward_long_kernel<T, W, 16, false><<<grid, 512, 0, st>>>(a);
+        else norm_backward_long_kernel<T, W, sizeof(T), false><<<grid, 512, 0, st>>>(a);
+    }
     return cudaGetLastError();
 }
 
@@ -297,17 +328,21 @@ cudaError_t launch_norm_backward(const NormArgs& a, int sms, cudaStream_t st) {
     if (!a.slots) return cudaSuccess;
     const uint32_t S = (a.H + a.k - 1) / a.k;
     const uint64_t filled = (uint64_t)S * a.k;                       // columns with the last message's fill
-    const uint32_t tiles = (uint32_t)((filled + 31) / 32);
+    const uint32_t tiles = (uint32_t)((filled + 31) / 32), wide = (uint32_t)((filled + 127) / 128), slots = a.groups / a.P + 1;    // slots of a process, on average
     const uint64_t items = (uint64_t)tiles * a.P;
+    if (items > 0x7FFFFFFFull) return cudaErrorInvalidValue;         // refused before (ftc_train_api.cu)
+    const uint32_t n = (uint32_t)items, nw = wide * a.P;
     if (!a.rows) {                                                   // zeros; no earlier kernel of this call
-        norm_messages_kernel<1><<<(uint32_t)((items + 7) / 8), 256, 0, st>>>(a, tiles);
+        norm_messages_kernel<1, 4><<<(nw + 7) / 8, 256, 0, st>>>(a, wide, nw);
         return cudaGetLastError();
     }
-    const uint32_t slots = a.groups / a.P + 1;                       // of a process, on average
-    if (slots <= 2) return launch_second(norm_messages_kernel<1>, (uint32_t)((items + 7) / 8), 256, st, a, tiles);
-    if (slots <= 12) return launch_second(norm_messages_kernel<4>, (uint32_t)((items + 1) / 2), 256, st, a, tiles);
-    if (slots <= 64) return launch_second(norm_messages_kernel<8>, (uint32_t)items, 256, st, a, tiles);
-    return launch_second(norm_messages_kernel<32>, (uint32_t)items, 1024, st, a, tiles);
+    // A warp for each process and tile where slots are few or warps plenty; four columns a lane where that still leaves every SM its 64
+    // warps (955 processes of 13256 columns, two slots each: 46 us against 96).
+    if (slots <= 2 && nw >= 64u * sms) return launch_second(norm_messages_kernel<1, 4>, (nw + 7) / 8, 256, st, a, wide, nw);
+    if (slots <= 2 || (slots <= 12 && n >= 32u * sms)) return launch_second(norm_messages_kernel<1, 1>, (n + 7) / 8, 256, st, a, tiles, n);
+    if (slots <= 12) return launch_second(norm_messages_kernel<4, 1>, (n + 1) / 2, 256, st, a, tiles, n);
+    if (slots <= 64) return launch_second(norm_messages_kernel<8, 1>, n, 256, st, a, tiles, n);
+    return launch_second(norm_messages_kernel<32, 1>, n, 1024, st, a, tiles, n);
 }
 
 }  // namespace ftc

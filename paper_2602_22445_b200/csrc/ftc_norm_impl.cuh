@@ -185,6 +185,12 @@ __device__ __forceinline__ float2 group_sum(float2 v, Scratch& scratch, uint32_t
     const float other = __shfl_xor_sync(0xFFFFFFFFu, s, 16);
     return upper ? make_float2(other, s) : make_float2(s, other);
 }
+__device__ __forceinline__ void group_sums(float (&v)[1], Scratch& scratch, uint32_t& turn) { v[0] = group_sum(v[0], scratch, turn); }
+__device__ __forceinline__ void group_sums(float (&v)[2], Scratch& scratch, uint32_t& turn) {
+    const float2 s = group_sum(make_float2(v[0], v[1]), scratch, turn);
+    v[0] = s.x; v[1] = s.y;
+}
+
 // 1 / sqrt(x): the approximate one and a step of Newton's method (none at 0, infinity and NaN, where the first is right).
 __device__ __forceinline__ float inverse_root(float x) {
     const float r = rsqrtf(x);
@@ -276,9 +282,9 @@ template <typename T, int MODE, bool ALL, int NV> struct RingRows {
                     if (at + e >= first && at + e < behind) *reinterpret_cast<T*>(place + q * 16u + e) = *reinterpret_cast<const T*>(at + e);
         }
     }
-    // This thread's elements of the present row; zeros behind its end.
-    template <bool WHOLE> __device__ __forceinline__ void read_as(F2* v, const char* place) const {
-        const uint32_t lane = threadIdx.x & 31, mis = SHIFT ? (uint32_t)reinterpret_cast<uintptr_t>(row) & 15u : 0u;
+    // This thread's elements of the row that came from `from`; zeros behind its end.
+    template <bool WHOLE> __device__ __forceinline__ void read_as(F2* v, const char* place, const char* from) const {
+        const uint32_t lane = threadIdx.x & 31, mis = SHIFT ? (uint32_t)reinterpret_cast<uintptr_t>(from) & 15u : 0u;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const uint32_t q = P::first_vector() + i * 32;
@@ -309,7 +315,7 @@ template <typename T, int MODE, bool ALL, int NV> struct RingRows {
             }
         }
     }
-    __device__ __forceinline__ void read(F2* v, const char* place) const { if (ALL || whole) read_as<true>(v, place); else read_as<false>(v, place); }
+    __device__ __forceinline__ void read(F2* v, const char* place, const char* from) const { if (ALL || whole) read_as<true>(v, place, from); else read_as<false>(v, place, from); }
 };
 
 // A thread's results to its columns of a row.
@@ -361,67 +367,105 @@ template <typename T, typename W, int MODE, int NV> __device__ __forceinline__ v
     for (int j = 0; j < P::E / 2; ++j) v[j] = pair(f[2 * j], f[2 * j + 1]);
 }
 
-// blockDim = (G, groups in the block).
-template <typename T, typename W, int MODE, bool ALL, int NV, int D, int MAXT>
-__global__ void __launch_bounds__(MAXT, MAXT <= 256 ? 768 / MAXT : 1) norm_forward_kernel(NormArgs a) {
+// blockDim = (G, groups in the block). A group takes R rows at a time: two rows share the barriers, and one's latencies hide the other's.
+// gamma and beta wait in shared memory, each thread's own where it left them: as registers they would cost a block of three.
+template <typename T, typename W, int MODE, bool ALL, int NV, int R, int D, int MAXT>
+__global__ void __launch_bounds__(MAXT, 768 / MAXT) norm_forward_kernel(NormArgs a) {
     using P = Part<T, MODE, NV>;
     constexpr int H2 = P::E / 2;
     extern __shared__ uint4 ring_memory[];
     __shared__ Scratch scratch;
     uint32_t turn = 0;
     const uint32_t bytes = blockDim.x / 32 * P::PLACE;               // a row in the ring
-    char* ring = reinterpret_cast<char*>(ring_memory) + threadIdx.y * D * bytes + (threadIdx.x >> 5) * P::PLACE;
+    char* ring = reinterpret_cast<char*>(ring_memory) + threadIdx.y * D * R * bytes + (threadIdx.x >> 5) * P::PLACE;
+    float4* weights = reinterpret_cast<float4*>(reinterpret_cast<char*>(ring_memory) + blockDim.y * D * R * bytes) + threadIdx.x;
     const float inv = 1.f / (float)a.H;
-    const uint32_t step = gridDim.x * blockDim.y, r0 = blockIdx.x * blockDim.y + threadIdx.y;
+    const uint32_t step = gridDim.x * blockDim.y * R, r0 = (blockIdx.x * blockDim.y + threadIdx.y) * R;
     RingRows<T, MODE, ALL, NV> in(a.x, a.x_stride, a.rows, a.H, r0, step, D - 1);
+    const uint64_t x_next = a.x_stride * sizeof(T);                  // bytes to the next row
     T* y = static_cast<T*>(a.y) + r0 * a.y_stride;
+    const auto fetch = [&](uint32_t r, char* place, const char* from) {
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            if (r + k < a.rows) in.fetch(place + k * bytes, from + k * x_next);
+        copies_end_batch();
+    };
     uint32_t fetched = r0, put = 0, take = 0;
 #pragma unroll
     for (int d = 0; d < D - 1; ++d) {
-        if (fetched < a.rows) in.fetch(ring + put, in.row + d * in.step);
-        copies_end_batch();
-        fetched += step; put += bytes;                               // rows + grid stay below 2^32
+        fetch(fetched, ring + put, in.row + d * in.step);
+        fetched += step; put += R * bytes;                           // rows + grid stay below 2^32
     }
-    F2 g[H2], b[H2];
-    read_weights<T, W, MODE, NV>(g, a.gamma, 1.f, a.H);
-    read_weights<T, W, MODE, NV>(b, a.beta, 0.f, a.H);
+    if (threadIdx.y == 0) {
+        F2 g[H2], b[H2];
+        read_weights<T, W, MODE, NV>(g, a.gamma, 1.f, a.H);
+        read_weights<T, W, MODE, NV>(b, a.beta, 0.f, a.H);
+#pragma unroll
+        for (int j = 0; j < H2 / 2; ++j) {
+            weights[2 * j * blockDim.x] = make_float4(lo(g[2 * j]), hi(g[2 * j]), lo(g[2 * j + 1]), hi(g[2 * j + 1]));
+            weights[(2 * j + 1) * blockDim.x] = make_float4(lo(b[2 * j]), hi(b[2 * j]), lo(b[2 * j + 1]), hi(b[2 * j + 1]));
+        }
+    }
     clear_scratch(scratch);
     for (uint32_t r = r0; r < a.rows; r += step) {
         copies_wait<D - 2>();
         if (P::SHIFT) __syncwarp();
-        F2 x[H2];
-        in.read(x, ring + take);
-        if (fetched < a.rows) in.fetch(ring + put, in.row + in.ahead);
-        copies_end_batch();
+        F2 x[R][H2];
+        float mean[R], rstd[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) in.read(x[k], ring + take + k * bytes, in.row + k * x_next);
+        fetch(fetched, ring + put, in.row + in.ahead);
         fetched += step;
         put = take;
-        take = take + bytes == D * bytes ? 0 : take + bytes;
+        take = take + R * bytes == D * R * bytes ? 0 : take + R * bytes;
         in.next();
-        F2 s = x[0];
 #pragma unroll
-        for (int j = 1; j < H2; ++j) s = add(s, x[j]);
-        const float mean = group_sum(lo(s) + hi(s), scratch, turn) * inv;
-        s = twice(0.f);
+        for (int k = 0; k < R; ++k) {
+            F2 s = x[k][0];
 #pragma unroll
-        for (int j = 0; j < H2; ++j) x[j] = add(x[j], twice(-mean));
-        if (!ALL && !in.whole) {                                     // nothing behind the row's end
+            for (int j = 1; j < H2; ++j) s = add(s, x[k][j]);
+            mean[k] = lo(s) + hi(s);
+        }
+        group_sums(mean, scratch, turn);
 #pragma unroll
-            for (int j = 0; j < H2; ++j) {
-                const uint32_t c = P::N == 1 ? P::first_vector() + 2 * j * 32 : (P::first_vector() + 2 * j / P::N * 32) * P::N + 2 * j % P::N;
-                if (c + (P::N == 1 ? 32 : 1) >= a.H) x[j] = pair(c < a.H ? lo(x[j]) : 0.f, 0.f);
+        for (int k = 0; k < R; ++k) {
+            mean[k] *= inv;
+#pragma unroll
+            for (int j = 0; j < H2; ++j) x[k][j] = add(x[k][j], twice(-mean[k]));
+            if (!ALL && !in.whole) {                                 // nothing behind the row's end
+#pragma unroll
+                for (int j = 0; j < H2; ++j) {
+                    const uint32_t c = P::N == 1 ? P::first_vector() + 2 * j * 32 : (P::first_vector() + 2 * j / P::N * 32) * P::N + 2 * j % P::N;
+                    if (c + (P::N == 1 ? 32 : 1) >= a.H) x[k][j] = pair(c < a.H ? lo(x[k][j]) : 0.f, 0.f);
+                }
+            }
+            F2 s = mul(x[k][0], x[k][0]);
+#pragma unroll
+            for (int j = 1; j < H2; ++j) s = fma(x[k][j], x[k][j], s);
+            rstd[k] = lo(s) + hi(s);
+        }
+        group_sums(rstd, scratch, turn);
+#pragma unroll
+        for (int k = 0; k < R; ++k) rstd[k] = inverse_root(rstd[k] * inv + a.eps);
+#pragma unroll
+        for (int j = 0; j < H2 / 2; ++j) {
+            const float4 g = weights[2 * j * blockDim.x], b = weights[(2 * j + 1) * blockDim.x];
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                x[k][2 * j] = fma(mul(x[k][2 * j], twice(rstd[k])), pair(g.x, g.y), pair(b.x, b.y));
+                x[k][2 * j + 1] = fma(mul(x[k][2 * j + 1], twice(rstd[k])), pair(g.z, g.w), pair(b.z, b.w));
             }
         }
 #pragma unroll
-        for (int j = 0; j < H2; ++j) s = fma(x[j], x[j], s);
-        const float rstd = inverse_root(group_sum(lo(s) + hi(s), scratch, turn) * inv + a.eps);
-#pragma unroll
-        for (int j = 0; j < H2; ++j) x[j] = fma(mul(x[j], twice(rstd)), g[j], b[j]);
-        write_row<T, MODE, ALL, NV>(y, x, a.H, in.whole);
+        for (int k = 0; k < R; ++k)
+            if (k == 0 || r + k < a.rows) {
+                write_row<T, MODE, ALL, NV>(y + k * a.y_stride, x[k], a.H, in.whole);
+                if (threadIdx.x == 0) {
+                    if (a.mean_out) a.mean_out[r + k] = mean[k];
+                    if (a.rstd_out) a.rstd_out[r + k] = rstd[k];
+                }
+            }
         y += step * a.y_stride;
-        if (threadIdx.x == 0) {
-            if (a.mean_out) a.mean_out[r] = mean;
-            if (a.rstd_out) a.rstd_out[r] = rstd;
-        }
     }
 }
 
@@ -471,8 +515,8 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
         copies_wait<D - 2>();
         if (P::SHIFT) __syncwarp();
         F2 x[H2], dy[H2];
-        xs.read(x, ring + take);
-        ys.read(dy, ring + take + bytes);
+        xs.read(x, ring + take, xs.row);
+        ys.read(dy, ring + take + bytes, ys.row);
         if (r + (D - 1) < walk.r1) { xs.fetch(ring + put, xs.row + xs.ahead); ys.fetch(ring + put + bytes, ys.row + ys.ahead); }
         copies_end_batch();
         put = take;
@@ -515,37 +559,53 @@ static inline dim3 group_shape(uint32_t vecs, uint32_t nv) {
     return dim3(g, g == 32 ? 4 : 1);
 }
 
+// Blocks of the forward kernel that an SM holds: 768 threads, and their shared memory.
+static inline uint32_t forward_per_sm(dim3 block, size_t smem) {
+    const uint32_t threads = block.x * block.y, by_threads = threads < 768 ? 768 / threads : 1, by_memory = (uint32_t)(227 * 1024 / (smem + 1536));
+    return by_threads < by_memory ? by_threads : by_memory ? by_memory : 1;
+}
+
 template <typename K> static cudaError_t allow_shared(K kernel, size_t bytes) {
     return bytes <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
-template <typename T, typename W, int MODE, bool ALL, int NV, int D, int MAXT> static cudaError_t forward_launch(const NormArgs& a, dim3 block, int sms, cudaStream_t st) {
+template <typename T, typename W, int MODE, bool ALL, int NV, int R, int MAXT> static cudaError_t forward_launch(const NormArgs& a, dim3 block, int sms, cudaStream_t st) {
     using P = Part<T, MODE, NV>;
-    const size_t smem = (size_t)block.y * D * (block.x / 32) * P::PLACE;
-    const cudaError_t e = allow_shared(norm_forward_kernel<T, W, MODE, ALL, NV, D, MAXT>, smem);
+    constexpr int D = 2;
+    const size_t smem = (size_t)block.y * D * R * (block.x / 32) * P::PLACE + (size_t)block.x * P::E * 8;
+    const cudaError_t e = allow_shared(norm_forward_kernel<T, W, MODE, ALL, NV, R, D, MAXT>, smem);
     if (e != cudaSuccess) return e;
-    const uint32_t threads = block.x * block.y, per_sm = threads < 768 ? 768 / threads : 1;
-    const uint32_t blocks = (a.rows + block.y - 1) / block.y, cap = (uint32_t)sms * per_sm;
-    norm_forward_kernel<T, W, MODE, ALL, NV, D, MAXT><<<blocks < cap ? blocks : cap, block, smem, st>>>(a);
+    const uint32_t blocks = (a.rows + block.y * R - 1) / (block.y * R), cap = (uint32_t)sms * forward_per_sm(block, smem);
+    norm_forward_kernel<T, W, MODE, ALL, NV, R, D, MAXT><<<blocks < cap ? blocks : cap, block, smem, st>>>(a);
     return cudaGetLastError();
 }
-template <typename T, typename W, int MODE, int NV, int D> static cudaError_t forward_run(const NormArgs& a, int sms, cudaStream_t st) {
+// Two rows at a time where that still leaves every SM its blocks.
+template <typename T, typename W, int MODE, bool ALL, int NV> static cudaError_t forward_shape(const NormArgs& a, dim3 block, int sms, cudaStream_t st) {
+    const bool two = a.rows >= 2u * sms * forward_per_sm(block, 0) * block.y;
+    if (NV == 1 || block.x <= 256)                                   // NV = 1: one warp
+        return two ? forward_launch<T, W, MODE, ALL, NV, 2, 256>(a, block, sms, st) : forward_launch<T, W, MODE, ALL, NV, 1, 256>(a, block, sms, st);
+    if constexpr (NV > 1) {
+        if (two && block.x <= 384) return forward_launch<T, W, MODE, ALL, NV, 2, 384>(a, block, sms, st);
+        return two ? forward_launch<T, W, MODE, ALL, NV, 2, kMaxGroup>(a, block, sms, st) : forward_launch<T, W, MODE, ALL, NV, 1, kMaxGroup>(a, block, sms, st);
+    }
+    return cudaErrorNotSupported;
+}
+template <typename T, typename W, int MODE, int NV> static cudaError_t forward_run(const NormArgs& a, int sms, cudaStream_t st) {
     using P = Part<T, MODE, NV>;
     const dim3 block = group_shape((a.H + P::N - 1) / P::N, NV);
     if constexpr (MODE == kAligned)
-        if (a.H == NV * P::N * block.x)
-            return block.x <= 256 ? forward_launch<T, W, MODE, true, NV, D, 256>(a, block, sms, st) : forward_launch<T, W, MODE, true, NV, D, kMaxGroup>(a, block, sms, st);
-    return block.x <= 256 ? forward_launch<T, W, MODE, false, NV, D, 256>(a, block, sms, st) : forward_launch<T, W, MODE, false, NV, D, kMaxGroup>(a, block, sms, st);
+        if (a.H == NV * P::N * block.x) return forward_shape<T, W, MODE, true, NV>(a, block, sms, st);
+    return forward_shape<T, W, MODE, false, NV>(a, block, sms, st);
 }
 
 // cudaErrorNotSupported: the row does not fit.
 template <typename T, typename W> static cudaError_t forward_rows(const NormArgs& a, uint32_t v, int sms, cudaStream_t st) {
-    constexpr int e = sizeof(T), D = e == 2 ? 4 : 3;
+    constexpr int e = sizeof(T);
     if (a.H > 16 * kMaxGroup) return cudaErrorNotSupported;
-    if (v == 16) return a.H <= 32 * 16 / e ? forward_run<T, W, kAligned, 1, D>(a, sms, st) : forward_run<T, W, kAligned, e, D>(a, sms, st);
+    if (v == 16) return a.H <= 32 * 16 / e ? forward_run<T, W, kAligned, 1>(a, sms, st) : forward_run<T, W, kAligned, e>(a, sms, st);
     if constexpr (e == 2)
-        if (v == 2) return forward_run<T, W, kOdd, 8, D>(a, sms, st);
-    return forward_run<T, W, kWords, 4 * e, D>(a, sms, st);
+        if (v == 2) return forward_run<T, W, kOdd, 8>(a, sms, st);
+    return forward_run<T, W, kWords, 4 * e>(a, sms, st);
 }
 
 template <typename T, typename W, int MODE, bool ALL, int NV, int D> static cudaError_t backward_launch(const NormArgs& a, dim3 block, cudaStream_t st) {

@@ -22,6 +22,7 @@ int check_norm(const ftc_norm_t* d, uint64_t rows) {
     if (!is_float(d->dtype) || (d->wdtype != FTC_F32 && d->wdtype != d->dtype)) return FTC_EUNSUPPORTED;
     if (d->H == 0 || d->H > (1u << 24) || d->P == 0 || d->P > (1u << 20) || d->k == 0 || d->k > (1u << 24) || !(d->eps >= 0.f) || rows > (1ull << 31))
         return FTC_EINVAL;
+    if (((uint64_t)d->H + d->k + 31) / 32 * d->P > 0x7FFFFFFFull) return FTC_EINVAL;
     return FTC_OK;
 }
 
