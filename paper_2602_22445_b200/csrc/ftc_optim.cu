@@ -168,10 +168,19 @@ template <bool WIDE> __device__ __forceinline__ uint32_t inside(uint32_t lane, u
 // Byte j of the words x, and the numbers' low bytes back: a whole number c with |c| < 2^22 stands in the low bits of 3 * 2^22 + c
 // (no conversion instructions, which run at a quarter of the rate).
 constexpr float kWhole = 12582912.f;
-__device__ __forceinline__ F2 bytes_numbers(uint32_t a, uint32_t b, F2 less) {                     // a, b: one byte each
-    return add(pair(__uint_as_float(a | 0x4B000000u), __uint_as_float(b | 0x4B000000u)), less);
+__device__ __forceinline__ F2 bytes_numbers(uint32_t a, uint32_t b, F2 less) {                     // a, b: 2^23 + a byte, as bits
+    return add(pair(__uint_as_float(a), __uint_as_float(b)), less);
 }
-__device__ __forceinline__ uint32_t byte_of(uint32_t w, int j) { return __byte_perm(w, 0u, 0x4440 + j); }
+__device__ __forceinline__ uint32_t byte_of(uint32_t w, int j) { return __byte_perm(w, 0x4B000000u, 0x7440 + j); }
+
+__device__ __forceinline__ float one_above(float x) { float r; asm("set.gt.f32.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(x)); return r; }       // 1 where x > 0, else 0
+
+// Largest size of three numbers; NaN where one of them is.
+__device__ __forceinline__ float largest(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 
 // The whole numbers c nearest to sqrt(x), (c - 1/2)^2 <= x < (c + 1/2)^2, at most `most`, from an approximate root. The root and
 // x may be off by some units in the last place: `far` collects how far the root lies from its whole number, and where that comes
@@ -181,7 +190,7 @@ constexpr float kDoubtM = 2e-5f, kDoubtV = 6.5e-5f;
 __device__ __forceinline__ float fast_root(float x) { float r; asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ F2 likely_roots(F2 x, float& far) {
     const F2 s = pair(fast_root(lo(x)), fast_root(hi(x))), c = add(add(s, twice(kWhole)), twice(-kWhole)), f = fma(c, twice(-1.f), s);
-    far = fmaxf(far, fmaxf(fabsf(lo(f)), fabsf(hi(f))));
+    far = largest(far, lo(f), hi(f));
     return c;
 }
 // The same without doubt: x - c^2 is exact in float32 (a multiple of x's last place, smaller than x), so two comparisons decide.
@@ -260,11 +269,11 @@ __device__ __forceinline__ void adamw_block(const BlockIn& in, const AdamArgs& a
         for (int i = 0; i < 4; ++i) {
             const int j = i * 2 % 4;
             const F2 c = WIDE ? bytes_numbers(byte_of(mr.r[i / 2], j), byte_of(mr.r[i / 2], j + 1), twice(-8388736.f))
-                              : bytes_numbers(mr.r[2 * i] ^ 0x80u, mr.r[2 * i + 1] ^ 0x80u, twice(-8388736.f));
+                              : bytes_numbers(mr.r[2 * i] ^ 0x4B000080u, mr.r[2 * i + 1] ^ 0x4B000080u, twice(-8388736.f));
             const F2 d = WIDE ? bytes_numbers(byte_of(vr.r[i / 2], j), byte_of(vr.r[i / 2], j + 1), twice(-8388608.f))
-                              : bytes_numbers(vr.r[2 * i], vr.r[2 * i + 1], twice(-8388608.f));
+                              : bytes_numbers(vr.r[2 * i] | 0x4B000000u, vr.r[2 * i + 1] | 0x4B000000u, twice(-8388608.f));
             const F2 r = mul(mul(d, d), vk);
-            m[i] = mul(mul(c, pair(fabsf(lo(c)), fabsf(hi(c)))), mk);
+            m[i] = mul(pair(__fmul_rn(lo(c), fabsf(lo(c))), __fmul_rn(hi(c), fabsf(hi(c)))), mk);
             v[i] = mul(r, r);
         }
     }
@@ -296,13 +305,13 @@ __device__ __forceinline__ void adamw_block(const BlockIn& in, const AdamArgs& a
         return;
     }
     if (t.status && !__any_sync(0xFFFFFFFFu, live)) return;
-    uint32_t mm = 0, vm = 0;                                                    // behind the tensor's end all is zero
+    float mm = 0.f, vm = 0.f;                                                   // behind the tensor's end all is zero
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        mm = max(mm, max(__float_as_uint(lo(m[i])) & 0x7FFFFFFFu, __float_as_uint(hi(m[i])) & 0x7FFFFFFFu));
-        vm = max(vm, max(__float_as_uint(lo(v[i])) & 0x7FFFFFFFu, __float_as_uint(hi(v[i])) & 0x7FFFFFFFu));
+        mm = largest(mm, lo(m[i]), hi(m[i]));
+        vm = largest(vm, lo(v[i]), hi(v[i]));
     }
-    ms = warp_max_bits(mm); vs = __fsqrt_rn(warp_max_bits(vm));                 // the root keeps the order: the largest root
+    ms = warp_max_bits(__float_as_uint(mm)); vs = __fsqrt_rn(warp_max_bits(__float_as_uint(vm)));     // the root keeps the order: the largest root
     ms = ms <= 3.402823466e38f ? fmaxf(ms, kTiny) : __uint_as_float(0x7FC00000u);
     vs = vs <= 3.402823466e38f ? fmaxf(vs, kTiny) : __uint_as_float(0x7FC00000u);
     const float inv = 1.f / (lane & 1 ? vs : ms);                               // one division for both
@@ -311,7 +320,7 @@ __device__ __forceinline__ void adamw_block(const BlockIn& in, const AdamArgs& a
     float far_m = 0.f, far_v = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        c[i] = likely_roots(mul(mul(pair(fabsf(lo(m[i])), fabsf(hi(m[i]))), twice(mi)), twice(16129.f)), far_m);
+        c[i] = likely_roots(mul(pair(__fmul_rn(fabsf(lo(m[i])), mi), __fmul_rn(fabsf(hi(m[i])), mi)), twice(16129.f)), far_m);
         d[i] = likely_roots(mul(mul(root[i], twice(vi)), twice(65025.f)), far_v);
     }
     if (!(far_m < 0.5f - kDoubtM && far_v < 0.5f - kDoubtV)) {                  // one lane in a thousand, and NaN
@@ -324,7 +333,7 @@ __device__ __forceinline__ void adamw_block(const BlockIn& in, const AdamArgs& a
     uint32_t cm[8], cv[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const F2 e = pair(lo(v[i]) > 0.f ? fmaxf(lo(d[i]), 1.f) : lo(d[i]), hi(v[i]) > 0.f ? fmaxf(hi(d[i]), 1.f) : hi(d[i]));
+        const F2 e = pair(fmaxf(lo(d[i]), one_above(lo(v[i]))), fmaxf(hi(d[i]), one_above(hi(v[i]))));
         const F2 s = add(pair(copysignf(lo(c[i]), lo(m[i])), copysignf(hi(c[i]), hi(m[i]))), twice(kWhole)), u = add(e, twice(kWhole));
         cm[2 * i] = __float_as_uint(lo(s)); cm[2 * i + 1] = __float_as_uint(hi(s));
         cv[2 * i] = __float_as_uint(lo(u)); cv[2 * i + 1] = __float_as_uint(hi(u));
