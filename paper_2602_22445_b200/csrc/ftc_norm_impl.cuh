@@ -108,6 +108,7 @@ struct RowWalk {
     uint32_t r0, r1, start, end, b, p;
     bool any;                                   // the present process has rows here so far
     __device__ __forceinline__ RowWalk(const NormArgs& args, uint32_t group) : a(args), start(0), end(~0u), b(group), p(0), any(false) {
+        if (a.direct) { p = group; r0 = first_row(a, group); r1 = first_row(a, group + 1); return; }
         r0 = group * a.rows_per_group;
         r1 = a.rows - r0 < a.rows_per_group ? a.rows : r0 + a.rows_per_group;
     }
@@ -121,6 +122,30 @@ struct RowWalk {
     __device__ __forceinline__ bool counts(uint32_t r) const { return r >= start; }
     __device__ __forceinline__ uint64_t slot() const { return (uint64_t)b + p; }
 };
+
+// The sums of one process for N neighbouring columns, to their places in the messages.
+template <int N> __device__ __forceinline__ void store_message(const NormArgs& a, uint32_t p, uint32_t c, const float* dg, const float* db) {
+    if constexpr (N % 4 == 0) {
+        if (a.direct == 2) {                    // messages of whole vectors of four, on 16 bytes
+#pragma unroll
+            for (int j = 0; j < N; j += 4) {
+                const uint32_t s = (c + j) / a.k;
+                const uint64_t o = ((uint64_t)s * a.P + p) * a.k + (c + j - s * a.k);
+                if (a.dgamma) *reinterpret_cast<float4*>(a.dgamma + o) = make_float4(dg[j], dg[j + 1], dg[j + 2], dg[j + 3]);
+                if (a.dbeta) *reinterpret_cast<float4*>(a.dbeta + o) = make_float4(db[j], db[j + 1], db[j + 2], db[j + 3]);
+            }
+            return;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if (c + j >= a.H) continue;
+        const uint32_t s = (c + j) / a.k;
+        const uint64_t o = ((uint64_t)s * a.P + p) * a.k + (c + j - s * a.k);
+        if (a.dgamma) a.dgamma[o] = dg[j];
+        if (a.dbeta) a.dbeta[o] = db[j];
+    }
+}
 
 template <int N> __device__ __forceinline__ void store_slot(const NormArgs& a, uint64_t slot, uint32_t c, const float* dg, const float* db) {
     float* g = a.slots + slot * 2 * a.H + c;
@@ -493,7 +518,9 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
         copies_end_batch();
         put += 2 * bytes;
     }
-    float nmean = a.mean[walk.r0], nrstd = a.rstd[walk.r0];
+    const bool weights = a.slots || a.direct;
+    float nmean = 0.f, nrstd = 0.f;
+    if (walk.r0 < walk.r1) { nmean = a.mean[walk.r0]; nrstd = a.rstd[walk.r0]; }
     if (a.slots) walk.find();
     F2 g[H2], dg[H2], db[H2];
     read_weights<T, W, MODE, NV>(g, a.gamma, 1.f, a.H);
@@ -507,7 +534,8 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
             float x[P::N], y[P::N];
 #pragma unroll
             for (int j = 0; j < P::N; ++j) { x[j] = element(dg, i * P::N + j); y[j] = element(db, i * P::N + j); }
-            if (MODE == kOdd && q == a.H / 2) store_slot<1>(a, walk.slot(), q * 2, x, y);
+            if (a.direct) store_message<P::N>(a, walk.p, q * P::N, x, y);
+            else if (MODE == kOdd && q == a.H / 2) store_slot<1>(a, walk.slot(), q * 2, x, y);
             else store_slot<P::N>(a, walk.slot(), q * P::N, x, y);
         }
     };
@@ -530,7 +558,7 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
             for (int j = 0; j < H2; ++j) dg[j] = db[j] = twice(0.f);
             walk.go_to(r);
         }
-        const bool counts = a.slots && walk.counts(r);
+        const bool counts = weights && walk.counts(r);
         walk.any |= counts;
 #pragma unroll
         for (int j = 0; j < H2; ++j) x[j] = mul(add(x[j], twice(-mean)), twice(rstd));        // behind the row's end dy = 0 adds nothing
@@ -549,7 +577,13 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
         write_row<T, MODE, ALL, NV>(dx, x, a.H, xs.whole);
         dx += a.dx_stride;
     }
-    if (a.slots && walk.any) leave();
+    if (a.direct || (a.slots && walk.any)) leave();
+    if (a.direct)                                                    // the last message's fill
+        for (uint32_t h = a.H + threadIdx.x; h < (a.H + a.k - 1) / a.k * a.k; h += blockDim.x) {
+            const uint64_t o = ((uint64_t)(h / a.k) * a.P + walk.p) * a.k + h % a.k;
+            if (a.dgamma) a.dgamma[o] = 0.f;
+            if (a.dbeta) a.dbeta[o] = 0.f;
+        }
 }
 
 // Threads that hold a row of H elements, 16 each, and rows of a block of 128 threads where a warp is enough for one.

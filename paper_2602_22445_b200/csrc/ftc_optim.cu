@@ -375,9 +375,9 @@ __global__ void __launch_bounds__(kWarps * 32, 4) adamw_kernel(AdamArgs a) {
     else adamw_one<BITS, false>(a, t, b, lane, e0, left < FTC_STATE_BLOCK ? (uint32_t)left : FTC_STATE_BLOCK, scale);
 }
 
+// States in 8 bits, whose arithmetic takes about as long as the memory: a warp takes `span` blocks one after the other, the next one's
+// loads out while it works on the present one.
 constexpr uint32_t kWalkWarps = 8, kWalkBlocks = 2;
-// A warp takes `span` blocks, the next one's loads out while it works on the present one.
-template <int BITS, bool WIDE>
 __global__ void __launch_bounds__(kWalkWarps * 32, kWalkBlocks) adamw_walk_kernel(AdamArgs a, uint64_t span) {
     const uint32_t lane = threadIdx.x & 31;
     uint64_t b = (blockIdx.x * (uint64_t)kWalkWarps + (threadIdx.x >> 5)) * span;
@@ -387,28 +387,28 @@ __global__ void __launch_bounds__(kWalkWarps * 32, kWalkBlocks) adamw_walk_kerne
     while (b < stop) {
         const TableEntry t = table_entries(a.table)[table_map(a.table, a.n_params)[b]];
         const uint64_t last = t.first_block + (t.n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK, end = last < stop ? last : stop;
-        const uint64_t whole = t.wide || !WIDE ? t.first_block + t.n / FTC_STATE_BLOCK : 0, end_ahead = whole < end ? whole : end;
+        const uint64_t whole = t.wide ? t.first_block + t.n / FTC_STATE_BLOCK : 0, end_wide = whole < end ? whole : end;
         uint64_t e0 = (b - t.first_block) * FTC_STATE_BLOCK;
-        if (b < end_ahead) {
+        if (b < end_wide) {
             BlockIn next;
-            adamw_load<BITS, WIDE>(next, a, t, b, lane, e0, FTC_STATE_BLOCK);
-            for (; b < end_ahead; ++b, e0 += FTC_STATE_BLOCK) {
+            adamw_load<8, true>(next, a, t, b, lane, e0, FTC_STATE_BLOCK);
+            for (; b < end_wide; ++b, e0 += FTC_STATE_BLOCK) {
                 const BlockIn in = next;
-                if (b + 1 < end_ahead) adamw_load<BITS, WIDE>(next, a, t, b + 1, lane, e0 + FTC_STATE_BLOCK, FTC_STATE_BLOCK);
-                adamw_block<BITS, WIDE>(in, a, t, b, lane, e0, FTC_STATE_BLOCK, scale);
+                if (b + 1 < end_wide) adamw_load<8, true>(next, a, t, b + 1, lane, e0 + FTC_STATE_BLOCK, FTC_STATE_BLOCK);
+                adamw_block<8, true>(in, a, t, b, lane, e0, FTC_STATE_BLOCK, scale);
             }
         }
         for (; b < end; ++b, e0 += FTC_STATE_BLOCK)
-            adamw_one<BITS, false>(a, t, b, lane, e0, t.n - e0 < FTC_STATE_BLOCK ? (uint32_t)(t.n - e0) : FTC_STATE_BLOCK, scale);
+            adamw_one<8, false>(a, t, b, lane, e0, t.n - e0 < FTC_STATE_BLOCK ? (uint32_t)(t.n - e0) : FTC_STATE_BLOCK, scale);
     }
 }
 
 cudaError_t launch_adamw(const AdamArgs& a, int sms, cudaStream_t st) {
-    const uint64_t warps = (uint64_t)sms * kWalkWarps * kWalkBlocks, span = (a.n_blocks + warps - 1) / warps;
-    const uint32_t walk_grid = sms * kWalkBlocks, threads = kWalkWarps * 32;
-    if (a.bits == 8 && a.n_blocks >= warps * 4 && (a.mostly_wide || 0)) {
-        if (a.mostly_wide) adamw_walk_kernel<8, true><<<walk_grid, threads, 0, st>>>(a, span);
-        else adamw_walk_kernel<8, false><<<walk_grid, threads, 0, st>>>(a, span);
+    // The walk pays from four blocks a warp on (24 layers, 201M elements: 606 us against 725); the narrow way has too much in
+    // registers for it (packed odd tensors: 98 us against 82).
+    const uint64_t warps = (uint64_t)sms * kWalkWarps * kWalkBlocks;
+    if (a.bits == 8 && a.mostly_wide && a.n_blocks >= warps * 4) {
+        adamw_walk_kernel<<<sms * kWalkBlocks, kWalkWarps * 32, 0, st>>>(a, (a.n_blocks + warps - 1) / warps);
         return cudaGetLastError();
     }
     const uint32_t grid = (uint32_t)((a.n_blocks + kWarps - 1) / kWarps);

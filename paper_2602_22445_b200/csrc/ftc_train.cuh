@@ -63,11 +63,13 @@ struct NormArgs {
     const uint64_t* splits;
     float *dgamma, *dbeta, *slots;
     uint64_t x_stride, y_stride, dy_stride, dx_stride;
-    uint32_t rows, H, P, k, dtype, wdtype, groups, rows_per_group;
+    uint32_t rows, H, P, k, dtype, wdtype, groups, rows_per_group, direct;
     float eps;
 };
 cudaError_t launch_norm_forward(const NormArgs& a, int sm_count, cudaStream_t st);
 cudaError_t launch_norm_backward(const NormArgs& a, int sm_count, cudaStream_t st);
+// Does each process's group write its messages itself? 2: in vectors of four.
+uint32_t norm_backward_direct(const NormArgs& a, int sm_count);
 // Groups that share the rows in the backward pass; each leaves its partial sums of the weight gradients in the workspace.
 uint32_t norm_backward_groups(uint32_t H, uint64_t rows, int sm_count);
 

@@ -103,7 +103,9 @@ int ftc_layernorm_backward(const ftc_norm_t* desc, uint64_t rows, const void* d_
     a.dgamma = d_dgamma; a.dbeta = d_dbeta; a.slots = weights ? static_cast<float*>(d_workspace) : nullptr;
     a.rows = (uint32_t)rows; a.x_stride = x_stride; a.dy_stride = dy_stride; a.dx_stride = dx_stride;
     a.H = desc->H; a.P = desc->P; a.k = desc->k; a.dtype = desc->dtype; a.wdtype = desc->wdtype; a.eps = desc->eps;
-    a.groups = norm_backward_groups(desc->H, rows, sms);
+    a.direct = norm_backward_direct(a, sms);
+    if (a.direct) a.slots = nullptr;
+    a.groups = a.direct ? a.P : norm_backward_groups(desc->H, rows, sms);
     a.rows_per_group = a.groups ? (uint32_t)((rows + a.groups - 1) / a.groups) : 0;
     return status(launch_norm_backward(a, sms, static_cast<cudaStream_t>(cuda_stream)));
 }

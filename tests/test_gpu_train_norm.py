@@ -235,3 +235,46 @@ def test_workspace_is_wanted():
         assert B.ftc_layernorm_backward(desc, x, x, None, stat, stat, None, None, out, out, ws, check=False) == B.FTC_EWORKSPACE
     with pytest.raises(B.FtcError):
         B.ftc_layernorm_backward(desc, x, x, None, stat, stat, None, None, out, out, None)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("rows,H,P,k", [(64, 512, 8, 16), (5, 96, 8, 32), (700, 260, 700, 4), (3000, 72, 2999, 7), (4096, 1024, 1024, 32), (2500, 33, 1300, 5), (8, 4099, 1, 4099),
+                                        (600, 8192, 300, 128), (7, 1024, 1, 1000), (40, 24, 5, 24)])
+def test_one_group_for_each_process(rows, H, P, k, dtype):
+    """Many processes, or few rows each: every process's sums go straight to its messages, fill and empty processes included."""
+    rng = np.random.default_rng([rows, H, P, 4])
+    for pad, offset in ((0, 0), (3, 1)):
+        x, xd = make(rng, rows, H, dtype, pad, offset)
+        dy, dyd = make(rng, rows, H, dtype, pad, offset)
+        gamma, gd = vector(rng, H, "float32", 1.0)
+        _, mean, rstd = run_forward(x, gamma, None, 1e-5, "float32")
+        got = run_backward(dy, x, gamma, mean, rstd, P, k)
+        want, off = O.norm_backward(dyd, xd, gd, host(mean), host(rstd), P, k, None)
+        O.assert_within(host(got[0]), want[0], off[0], dtype, "dx")
+        O.assert_within(host(got[1]), want[1], off[1], what="dgamma")
+        O.assert_within(host(got[2]), want[2], off[2], what="dbeta")
+        splits = [p * rows // P for p in range(P + 1)]
+        other = run_backward(dy, x, gamma, mean, rstd, P, k, splits)              # the same shares, given
+        O.assert_within(host(other[1]), want[1], off[1], what="dgamma of splits")
+
+
+@pytest.mark.parametrize("rows,H,P", [(2500, 1025, 3), (3000, 4424, 2), (1800, 6001, 1), (700, 8191, 5), (9000, 200, 16), (40, 12000, 3), (50, 12001, 40), (30, 33000, 2)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_many_rows(rows, H, P, dtype):
+    """Rows enough for every block to walk several, two at a time; rows wider than a group holds."""
+    rng = np.random.default_rng([rows, H, P, 5])
+    x, xd = make(rng, rows, H, dtype)
+    dy, dyd = make(rng, rows, H, dtype)
+    gamma, gd = vector(rng, H, "float32", 1.0)
+    beta, bd = vector(rng, H, "float32", 0.0)
+    got = run_forward(x, gamma, beta, 1e-5, "float32")
+    want, off = O.norm_forward(xd, gd, bd, 1e-5)
+    O.assert_within(host(got[0]), want[0], off[0], dtype, "y")
+    O.assert_within(host(got[1]), want[1], off[1], what="mean")
+    O.assert_within(host(got[2]), want[2], off[2], what="rstd")
+    _, mean, rstd = got
+    got = run_backward(dy, x, gamma, mean, rstd, P, 32)
+    want, off = O.norm_backward(dyd, xd, gd, host(mean), host(rstd), P, 32, None)
+    O.assert_within(host(got[0]), want[0], off[0], dtype, "dx")
+    O.assert_within(host(got[1]), want[1], off[1], what="dgamma")
+    O.assert_within(host(got[2]), want[2], off[2], what="dbeta")
