@@ -518,15 +518,13 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
         copies_end_batch();
         put += 2 * bytes;
     }
-    const bool weights = a.slots || a.direct;
     float nmean = 0.f, nrstd = 0.f;
     if (walk.r0 < walk.r1) { nmean = a.mean[walk.r0]; nrstd = a.rstd[walk.r0]; }
-    if (a.slots) walk.find();
     F2 g[H2], dg[H2], db[H2];
     read_weights<T, W, MODE, NV>(g, a.gamma, 1.f, a.H);
 #pragma unroll
     for (int j = 0; j < H2; ++j) dg[j] = db[j] = twice(0.f);
-    const auto leave = [&]() {
+    const auto leave = [&](bool direct) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const uint32_t q = P::first_vector() + i * 32;
@@ -534,11 +532,13 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
             float x[P::N], y[P::N];
 #pragma unroll
             for (int j = 0; j < P::N; ++j) { x[j] = element(dg, i * P::N + j); y[j] = element(db, i * P::N + j); }
-            if (a.direct) store_message<P::N>(a, walk.p, q * P::N, x, y);
+            if (direct) store_message<P::N>(a, walk.p, q * P::N, x, y);
             else if (MODE == kOdd && q == a.H / 2) store_slot<1>(a, walk.slot(), q * 2, x, y);
             else store_slot<P::N>(a, walk.slot(), q * P::N, x, y);
         }
     };
+    uint32_t weights_from = a.direct ? 0 : ~0u, weights_to = ~0u;    // the rows that count for the present process
+    if (a.slots) { walk.find(); weights_from = walk.start; weights_to = walk.end; }
     for (uint32_t r = walk.r0; r < walk.r1; ++r) {
         copies_wait<D - 2>();
         if (P::SHIFT) __syncwarp();
@@ -552,13 +552,14 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
         xs.next(); ys.next();
         const float mean = nmean, rstd = nrstd;
         if (r + 1 < walk.r1) { nmean = a.mean[r + 1]; nrstd = a.rstd[r + 1]; }
-        if (a.slots && walk.leaves(r)) {
-            if (walk.any) leave();
+        if (r >= weights_to) {
+            if (walk.any) leave(false);
 #pragma unroll
             for (int j = 0; j < H2; ++j) dg[j] = db[j] = twice(0.f);
             walk.go_to(r);
+            weights_from = walk.start; weights_to = walk.end;
         }
-        const bool counts = weights && walk.counts(r);
+        const bool counts = r >= weights_from;
         walk.any |= counts;
 #pragma unroll
         for (int j = 0; j < H2; ++j) x[j] = mul(add(x[j], twice(-mean)), twice(rstd));        // behind the row's end dy = 0 adds nothing
@@ -571,19 +572,21 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
 #pragma unroll
         for (int j = 0; j < H2; ++j) { dy[j] = mul(dy[j], g[j]); s1 = add(s1, dy[j]); s2 = fma(dy[j], x[j], s2); }
         const float2 s = group_sum(make_float2(lo(s1) + hi(s1), lo(s2) + hi(s2)), scratch, turn);
-        const F2 c1 = twice(-s.x * inv), c2 = twice(-s.y * inv);
+        const F2 c1 = twice(-s.x * inv * rstd), c2 = twice(-s.y * inv * rstd);
 #pragma unroll
-        for (int j = 0; j < H2; ++j) x[j] = mul(fma(x[j], c2, add(dy[j], c1)), twice(rstd));
+        for (int j = 0; j < H2; ++j) x[j] = fma(dy[j], twice(rstd), fma(x[j], c2, c1));
         write_row<T, MODE, ALL, NV>(dx, x, a.H, xs.whole);
         dx += a.dx_stride;
     }
-    if (a.direct || (a.slots && walk.any)) leave();
-    if (a.direct)                                                    // the last message's fill
+    if (a.slots && walk.any) leave(false);
+    if (a.direct) {
+        leave(true);                                                 // and the last message's fill
         for (uint32_t h = a.H + threadIdx.x; h < (a.H + a.k - 1) / a.k * a.k; h += blockDim.x) {
             const uint64_t o = ((uint64_t)(h / a.k) * a.P + walk.p) * a.k + h % a.k;
             if (a.dgamma) a.dgamma[o] = 0.f;
             if (a.dbeta) a.dbeta[o] = 0.f;
         }
+    }
 }
 
 // Threads that hold a row of H elements, 16 each, and rows of a block of 128 threads where a warp is enough for one.

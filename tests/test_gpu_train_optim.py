@@ -313,3 +313,40 @@ def test_refusals_on_the_device():
         B.make_param(torch.zeros(299, device="cuda"), g)
     with pytest.raises(ValueError):
         B.make_param(g, g, status=torch.zeros(3, 4, dtype=torch.int32, device="cuda"), k=32)
+
+
+def test_a_tensor_of_more_than_32_bits_of_elements():
+    """2^32 + 1000 elements: offsets, blocks and messages beyond 32 bits (27 GB on the device)."""
+    import torch
+    n = (1 << 32) + 1000
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("40 GB of device memory are wanted")
+    grad, param = torch.zeros(n, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    spots = torch.tensor([0, 255, (1 << 31) + 7, (1 << 32) - 1, 1 << 32, (1 << 32) + 300, n - 1], device="cuda")
+    grad[spots] = torch.tensor([1.0, 2.0, 3.0, 4.0, 5.0, 6.0, 7.0], dtype=torch.bfloat16, device="cuda")
+    table = B.make_param_table([B.make_param(param, grad)])
+    norm = torch.empty(2, device="cuda")
+    ws = torch.empty(B.ftc_grad_norm_workspace_bytes(table), dtype=torch.uint8, device="cuda")
+    B.ftc_grad_norm(table, 1e9, norm, None, ws)
+    assert abs(float(norm[0]) - 140 ** 0.5) <= 4 * O.U * 140 ** 0.5
+    m, v = torch.zeros(table.blocks * 256, dtype=torch.int8, device="cuda"), torch.zeros(table.blocks * 256, dtype=torch.uint8, device="cuda")
+    ms, vs = torch.zeros(table.blocks, device="cuda"), torch.zeros(table.blocks, device="cuda")
+    B.ftc_adamw_step(B.make_adamw(0.5, B1, B2, EPS, 1), table, m, v, ms, vs)
+    assert torch.equal(param[spots].float(), torch.full((7,), -0.5, device="cuda"))      # the first step moves by lr against the sign
+    assert int(torch.count_nonzero(param[:1 << 30])) == 2 and int(torch.count_nonzero(param[-(1 << 30):])) == 4
+    assert int(m[n - 1]) == 127 and int(v[n - 1]) == 255
+    # the same gradients in float32 as messages of 256, some with records of their own beyond element 2^32
+    del m, v, ms, vs, param, grad, table
+    k = 256
+    status = torch.zeros(-(-n // k), 4, dtype=torch.int32, device="cuda")
+    status[:, 1] = 2
+    status[(n - 1) // k, 0] = 2                                                        # the last message was not delivered
+    status[(1 << 32) // k, 1] = 4                                                      # that of element 2^32: four processes
+    grad = torch.zeros(n, device="cuda")
+    grad[spots] = torch.arange(1.0, 8.0, device="cuda")
+    table = B.make_param_table([B.make_param(None, grad, status=status, k=k)])
+    ws = torch.empty(B.ftc_grad_norm_workspace_bytes(table), dtype=torch.uint8, device="cuda")
+    B.ftc_grad_norm(table, 1e9, norm, None, ws)
+    shares = {(n - 1) // k: 0.0, (1 << 32) // k: 0.25}
+    want = sum(((i + 1) * shares.get(s // k, 0.5)) ** 2 for i, s in enumerate(spots.tolist())) ** 0.5
+    assert abs(float(norm[0]) - want) <= 8 * O.U * want
