@@ -377,7 +377,8 @@ FTC_API int ftc_layernorm_forward(const ftc_norm_t* desc, uint64_t rows, const v
  *   d_dgamma, d_dbeta  float32 [ceil(H/k)][P][k] -- the inputs of ceil(H/k) scenarios for ftc_allreduce_batch (FTC_F32, FTC_SUM):
  *                   column h of process p is element h % k of message h / k; the last message is filled up with zeros; NULL: not
  *                   computed
- *   d_workspace     ftc_layernorm_workspace_bytes(desc, rows) bytes (0 when neither weight gradient is wanted), 16-byte aligned
+ *   d_workspace     ftc_layernorm_workspace_bytes(desc, rows) bytes (may be NULL when neither weight gradient is wanted), 16-byte
+ *                   aligned; contents are undefined afterwards; calls that share a workspace must not overlap on the device
  * rows = 0 writes zeros to the weight gradients.
  */
 FTC_API int ftc_layernorm_backward(const ftc_norm_t* desc, uint64_t rows, const void* d_dy, uint64_t dy_stride, const void* d_x,
@@ -425,7 +426,7 @@ FTC_API uint64_t ftc_param_table_blocks(const void* h_table);
  *   d_norm   [2] float32: the norm over all tensors; max_norm / norm where the norm exceeds max_norm, else 1, NaN where the norm is
  *            not finite (which makes ftc_adamw_step do nothing)
  *   d_norms  [n_params] float32: each tensor's norm, or NULL
- *   d_workspace  ftc_grad_norm_workspace_bytes(h_table) bytes, 16-byte aligned
+ *   d_workspace  ftc_grad_norm_workspace_bytes(h_table) bytes, 16-byte aligned; as for ftc_layernorm_backward
  * Squares are added up in float64. max_norm > 0 (infinity: no clipping).
  */
 FTC_API int ftc_grad_norm(const void* h_table, const void* d_table, float max_norm, float* d_norm, float* d_norms,

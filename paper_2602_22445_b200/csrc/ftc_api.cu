@@ -437,9 +437,9 @@ int ftc_launch_blocks(const ftc_desc_t* desc, uint64_t S, int is_allreduce, uint
 const char* ftc_strerror(int code) {
     switch (code) {
     case FTC_OK: return "ok";
-    case FTC_EINVAL: return "invalid argument (P < f+2, k = 0, root >= P, f > 31, max_inop > 32, NULL or misaligned pointer)";
+    case FTC_EINVAL: return "invalid argument (P < f+2, k = 0, root >= P, f > 31, max_inop > 32; NULL or misaligned pointer, size or stride out of range)";
     case FTC_EUNSUPPORTED: return "unsupported dtype/op combination or flag";
-    case FTC_EWORKSPACE: return "workspace missing, misaligned or smaller than ftc_workspace_bytes()";
+    case FTC_EWORKSPACE: return "workspace missing, misaligned or smaller than the call's *_workspace_bytes()";
     case FTC_ECUDA: return "a CUDA call or kernel launch failed";
     case FTC_ETOOLARGE: return "shape too large for the built-in scratch: ceil((P-1)/(f+1)) * k * element size exceeds FTC_NOALLOC_SCRATCH_BYTES";
     }
