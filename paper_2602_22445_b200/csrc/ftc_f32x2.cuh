@@ -14,8 +14,8 @@ __device__ __forceinline__ F2 add(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, 
 __device__ __forceinline__ F2 mul(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
 __device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
 
-// The sum of two products that were rounded before: with plain additions, since the assembler joins a packed product and a packed sum into
-// one multiply-add.
-__device__ __forceinline__ F2 add_apart(F2 a, F2 b) { return pair(__fadd_rn(lo(a), lo(b)), __fadd_rn(hi(a), hi(b))); }
+// The sum of two products that were rounded before. The assembler joins a packed product and a packed sum into one multiply-add, so the
+// sum is a multiply-add itself, with a factor of 1 (twice) that only the host knows.
+__device__ __forceinline__ F2 add_apart(F2 a, F2 b, F2 one) { return fma(a, one, b); }
 
 }  // namespace ftc

@@ -182,6 +182,12 @@ __device__ __forceinline__ float largest(float a, float b, float c) {
     return r;
 }
 
+__device__ __forceinline__ float smallest(float a, float b, float c) {
+    float r;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
 // The whole numbers c nearest to sqrt(x), (c - 1/2)^2 <= x < (c + 1/2)^2, at most `most`, from an approximate root. The root and
 // x may be off by some units in the last place: `far` collects how far the root lies from its whole number, and where that comes
 // too near a half, c may be wrong. With a root good to 2^-23 and an exact x (m) the root is off by 127 * 2^-23 < 1.6e-5; with an x whose
@@ -284,8 +290,8 @@ __device__ __forceinline__ void adamw_block(const BlockIn& in, const AdamArgs& a
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         g[i] = mul(g[i], sc);
-        const F2 mi = add_apart(mul(m[i], twice(a.beta1)), mul(g[i], twice(a.rest1)));
-        const F2 vi = add_apart(mul(v[i], twice(a.beta2)), mul(mul(g[i], g[i]), twice(a.rest2)));
+        const F2 mi = add_apart(mul(m[i], twice(a.beta1)), mul(g[i], twice(a.rest1)), twice(a.one));
+        const F2 vi = add_apart(mul(v[i], twice(a.beta2)), mul(mul(g[i], g[i]), twice(a.rest2)), twice(a.one));
         root[i] = pair(fast_root(lo(vi)), fast_root(hi(vi)));
         const F2 den = add(mul(root[i], twice(a.fix2)), twice(a.eps));
         const F2 pi = fma(mul(mi, pair(fast_inverse(lo(den)), fast_inverse(hi(den)))), rate, mul(p[i], keep));
@@ -330,11 +336,17 @@ __device__ __forceinline__ void adamw_block(const BlockIn& in, const AdamArgs& a
             d[i] = pair(nearest_root(__fsqrt_rn(lo(v[i])) * vi * 65025.f, 255.f), nearest_root(__fsqrt_rn(hi(v[i])) * vi * 65025.f, 255.f));
         }
     }
+    float least = 255.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) least = smallest(least, lo(d[i]), hi(d[i]));
+    if (!(least >= 1.f)) {                                                      // a root above zero has a code above zero
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] = pair(fmaxf(lo(d[i]), one_above(lo(v[i]))), fmaxf(hi(d[i]), one_above(hi(v[i]))));
+    }
     uint32_t cm[8], cv[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const F2 e = pair(fmaxf(lo(d[i]), one_above(lo(v[i]))), fmaxf(hi(d[i]), one_above(hi(v[i]))));
-        const F2 s = add(pair(copysignf(lo(c[i]), lo(m[i])), copysignf(hi(c[i]), hi(m[i]))), twice(kWhole)), u = add(e, twice(kWhole));
+        const F2 s = add(pair(copysignf(lo(c[i]), lo(m[i])), copysignf(hi(c[i]), hi(m[i]))), twice(kWhole)), u = add(d[i], twice(kWhole));
         cm[2 * i] = __float_as_uint(lo(s)); cm[2 * i + 1] = __float_as_uint(hi(s));
         cv[2 * i] = __float_as_uint(lo(u)); cv[2 * i + 1] = __float_as_uint(hi(u));
     }

@@ -76,7 +76,7 @@ uint32_t norm_backward_groups(uint32_t H, uint64_t rows, int sm_count);
 struct AdamArgs {
     const void* table; uint32_t n_params; uint64_t n_blocks;
     void *m, *v; float *m_scale, *v_scale; const float* grad_scale;
-    float lr, beta1, beta2, rest1, rest2, eps, fix1, fix2;
+    float lr, beta1, beta2, rest1, rest2, eps, fix1, fix2, one;         // one = 1
     uint32_t bits, mostly_wide;
 };
 cudaError_t launch_adamw(const AdamArgs& a, int sm_count, cudaStream_t st);

@@ -179,6 +179,7 @@ int ftc_adamw_step(const ftc_adamw_t* hyper, const void* h_table, const void* d_
     a.table = d_table; a.n_params = h->n_params; a.n_blocks = h->n_blocks;
     a.m = d_m; a.v = d_v; a.m_scale = d_m_scale; a.v_scale = d_v_scale; a.grad_scale = d_grad_scale; a.bits = hyper->state_bits; a.mostly_wide = h->flags >> 1 & 1u;
     const double t = (double)hyper->step;
+    a.one = 1.f;
     a.lr = (float)hyper->lr; a.eps = (float)hyper->eps;
     a.beta1 = (float)hyper->beta1; a.beta2 = (float)hyper->beta2; a.rest1 = (float)(1 - hyper->beta1); a.rest2 = (float)(1 - hyper->beta2);
     a.fix1 = (float)(1 / (1 - std::pow(hyper->beta1, t))); a.fix2 = (float)(1 / std::sqrt(1 - std::pow(hyper->beta2, t)));
