@@ -68,7 +68,7 @@ template <typename W, int N> __device__ __forceinline__ void load_weights(float*
         for (int j = 0; j < N; ++j) v[j] = other;
         return;
     }
-    constexpr int BYTES = N * (int)sizeof(W), VB = BYTES >= 16 ? 16 : BYTES == 8 ? 4 : BYTES, M = VB / (int)sizeof(W);
+    constexpr int BYTES = N * (int)sizeof(W), VB = BYTES >= 16 ? 16 : BYTES, M = VB / (int)sizeof(W);
 #pragma unroll
     for (int i = 0; i < N / M; ++i) {
         Pack<W, VB> p;

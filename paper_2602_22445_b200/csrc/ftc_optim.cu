@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(256) adamw_states_kernel(uint64_t blocks, cons
     store_32(vo + i * 8, rv);
 }
 
-cudaError_t launch_adamw_states(uint64_t blocks, const void* m, const void* v, const float* ms, const float* vs, float* mo, float* vo, int, cudaStream_t st) {
+cudaError_t launch_adamw_states(uint64_t blocks, const void* m, const void* v, const float* ms, const float* vs, float* mo, float* vo, cudaStream_t st) {
     adamw_states_kernel<<<(uint32_t)((blocks + 7) / 8), 256, 0, st>>>(blocks, static_cast<const uint8_t*>(m), static_cast<const uint8_t*>(v), ms, vs, mo, vo);
     return cudaGetLastError();
 }
@@ -464,8 +464,6 @@ cudaError_t launch_adamw_states(uint64_t blocks, const void* m, const void* v, c
 // ---- the norm: one pass over the gradients, bound by memory where they are many (202M elements in float32 with a record for each 32:
 // 153-163 us, 5.9 TB/s), by two kernels' beginnings where they are few. Warp w adds up the squares of the blocks [w*span, (w+1)*span) and leaves one sum for each tensor it meets; warp w and
 // tensor t share slot w + t (going on by one block either grows, so no two pairs with blocks in common share a slot)
-
-constexpr int kAhead = 4;                                        // blocks whose loads a warp has out at once
 
 // Sum of the squares of 8 numbers. In float32 where that neither overflows nor loses small squares (4 roundings at most one after the
 // other), else in float64.
@@ -517,9 +515,10 @@ template <bool WIDE> __device__ __forceinline__ double walk_squares(const TableE
 
 // `blocks` full aligned blocks of elements of one type from `p` (this lane's first) on; record `message` and every `stride`-th after
 // it for those that have one.
-template <uint32_t DTYPE, bool STATUS>
+template <uint32_t DTYPE, bool STATUS, bool SOLO>
 __device__ __forceinline__ double run_squares(const char* p, uint32_t blocks, const uint32_t* status, uint32_t message, uint32_t stride) {
     constexpr uint32_t BYTES = FTC_STATE_BLOCK * (DTYPE == FTC_F32 ? 4 : 2);
+    constexpr int AHEAD = DTYPE == FTC_F32 || SOLO ? 4 : 8;           // blocks whose loads are out at once: 4 KB a warp (a lone block of 32 warps: 64 registers)
     double s = 0;
     const uint2* st = reinterpret_cast<const uint2*>(status + (uint64_t)message * FTC_STATUS_WORDS);
     const uint64_t next = (uint64_t)stride * (FTC_STATUS_WORDS / 2);
@@ -530,35 +529,38 @@ __device__ __forceinline__ double run_squares(const char* p, uint32_t blocks, co
         if (share > 0.f) s = ::fma((double)share * share, squares(g), s);
     };
     const auto load_one = [&](Raw& x, int i) { if (DTYPE == FTC_F32) load_32(p + i * BYTES, x.r); else load_16(p + i * BYTES, x.r); };
-    for (; blocks >= kAhead; blocks -= kAhead, p += kAhead * BYTES, st += kAhead * next) {
-        Raw x[kAhead];
-        uint2 r[kAhead];
+    for (; blocks >= AHEAD; blocks -= AHEAD, p += AHEAD * BYTES, st += AHEAD * next) {
+        Raw x[AHEAD];
+        uint2 r[AHEAD];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) { r[i] = STATUS ? st[i * next] : make_uint2(0u, 1u); load_one(x[i], i); }
+        for (int i = 0; i < AHEAD; ++i) { r[i] = STATUS ? st[i * next] : make_uint2(0u, 1u); load_one(x[i], i); }
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) add_one(x[i], r[i]);
+        for (int i = 0; i < AHEAD; ++i) add_one(x[i], r[i]);
     }
     if (blocks) {
-        Raw x[kAhead - 1];
-        uint2 r[kAhead - 1];
+        Raw x[AHEAD - 1];
+        uint2 r[AHEAD - 1];
 #pragma unroll
-        for (int i = 0; i < kAhead - 1; ++i)
-            if (i < (int)blocks) { r[i] = STATUS ? st[i * next] : make_uint2(0u, 1u); load_one(x[i], i); }
+        for (int i = 0; i < AHEAD - 1; ++i) {                       // behind the end the last one again, not added
+            const int at = i < (int)blocks ? i : (int)blocks - 1;
+            r[i] = STATUS ? st[at * next] : make_uint2(0u, 1u);
+            load_one(x[i], at);
+        }
 #pragma unroll
-        for (int i = 0; i < kAhead - 1; ++i)
+        for (int i = 0; i < AHEAD - 1; ++i)
             if (i < (int)blocks) add_one(x[i], r[i]);
     }
     return s;
 }
 
-// The sums of one warp.
-__device__ __forceinline__ void warp_squares(const void* table, uint32_t n_params, uint64_t n_blocks, uint64_t span, uint64_t w, double* slots) {
+// The sums of the warp w, whose first block is of tensor `ti`.
+template <bool SOLO> __device__ __forceinline__ void warp_squares(const TableEntry* entries, uint32_t ti, uint64_t n_blocks, uint64_t span, uint64_t w, double* slots) {
     const uint32_t lane = threadIdx.x & 31;
     uint64_t b = w * span;
     const uint64_t b1 = b + span < n_blocks ? b + span : n_blocks;
-    while (b < b1) {
-        const uint32_t ti = table_map(table, n_params)[b];
-        const TableEntry& t = table_entries(table)[ti];
+    for (; b < b1; ++ti) {
+        const TableEntry& t = entries[ti];
+        if (t.n == 0) continue;
         const uint64_t first = t.first_block, n = t.n, last = first + (n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK, end = last < b1 ? last : b1;
         const uint32_t k = t.k, dtype = t.grad_dtype;
         const uint64_t full = t.wide ? first + n / FTC_STATE_BLOCK : 0, end_wide = full < end ? full : end;
@@ -572,11 +574,11 @@ __device__ __forceinline__ void warp_squares(const void* table, uint32_t n_param
             const uint32_t blocks = (uint32_t)(end_run - b);
             if (t.status) {
                 const uint32_t message = (uint32_t)e / k, stride = FTC_STATE_BLOCK / k;
-                s = dtype == FTC_F32 ? run_squares<FTC_F32, true>(p, blocks, t.status, message, stride)
-                  : dtype == FTC_BF16 ? run_squares<FTC_BF16, true>(p, blocks, t.status, message, stride) : run_squares<FTC_F16, true>(p, blocks, t.status, message, stride);
+                s = dtype == FTC_F32 ? run_squares<FTC_F32, true, SOLO>(p, blocks, t.status, message, stride)
+                  : dtype == FTC_BF16 ? run_squares<FTC_BF16, true, SOLO>(p, blocks, t.status, message, stride) : run_squares<FTC_F16, true, SOLO>(p, blocks, t.status, message, stride);
             } else
-                s = dtype == FTC_F32 ? run_squares<FTC_F32, false>(p, blocks, nullptr, 0, 0)
-                  : dtype == FTC_BF16 ? run_squares<FTC_BF16, false>(p, blocks, nullptr, 0, 0) : run_squares<FTC_F16, false>(p, blocks, nullptr, 0, 0);
+                s = dtype == FTC_F32 ? run_squares<FTC_F32, false, SOLO>(p, blocks, nullptr, 0, 0)
+                  : dtype == FTC_BF16 ? run_squares<FTC_BF16, false, SOLO>(p, blocks, nullptr, 0, 0) : run_squares<FTC_F16, false, SOLO>(p, blocks, nullptr, 0, 0);
             b = end_run;
         }
         if (b < end_wide) { s += walk_squares<true>(t, b, end_wide); b = end_wide; }
@@ -590,7 +592,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) grad_squares_kernel(const void
     later_kernel_may_start();
     const uint64_t w = blockIdx.x * (uint64_t)kWarps + (threadIdx.x >> 5);
     if (w == 0 && (threadIdx.x & 31) == 0) *ticket = 0;
-    warp_squares(table, n_params, n_blocks, span, w, slots);
+    if (w * span < n_blocks) warp_squares<false>(table_entries(table), table_map(table, n_params)[w * span], n_blocks, span, w, slots);
 }
 
 __device__ __forceinline__ void give_norm(double s, float max_norm, float* norm) {
@@ -599,21 +601,25 @@ __device__ __forceinline__ void give_norm(double s, float max_norm, float* norm)
     norm[1] = !isfinite(r) ? __uint_as_float(0x7FC00000u) : r > max_norm ? max_norm / r : 1.f;
 }
 
-// Tables of few blocks: all in one thread block, the sums through the workspace.
-constexpr uint32_t kSoloWarps = 32, kSoloBlocks = 160;
-__global__ void __launch_bounds__(kSoloWarps * 32) grad_norm_solo_kernel(const void* table, uint32_t n_params, uint64_t n_blocks, uint64_t span, float max_norm, double* slots,
+// Tables of few blocks and tensors: all in one thread block, entries and sums in shared memory (132 blocks of 6 tensors: 6.6 us a call, as long as its checks and launch take, against 8.2 by way of the workspace).
+constexpr uint32_t kSoloWarps = 32, kSoloBlocks = 160, kSoloTensors = 16;
+__global__ void __launch_bounds__(kSoloWarps * 32) grad_norm_solo_kernel(const void* table, uint32_t n_params, uint64_t n_blocks, uint64_t span, float max_norm,
                                                                          float* norm, float* norms) {
-    __shared__ double part[kSoloWarps];
+    __shared__ TableEntry entries[kSoloTensors];
+    __shared__ double slots[kSoloWarps + kSoloTensors], part[kSoloWarps];
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    warp_squares(table, n_params, n_blocks, span, warp, slots);
+    const uint32_t ti = warp * span < n_blocks ? table_map(table, n_params)[warp * span] : 0;
+    if (threadIdx.x < n_params * (sizeof(TableEntry) / 4))
+        reinterpret_cast<uint32_t*>(entries)[threadIdx.x] = reinterpret_cast<const uint32_t*>(table_entries(table))[threadIdx.x];
+    __syncthreads();
+    warp_squares<true>(entries, ti, n_blocks, span, warp, slots);
     __syncthreads();
     double all = 0;
-    for (uint32_t ti = warp; ti < n_params; ti += kSoloWarps) {
-        const uint64_t n = table_entries(table)[ti].n, first = table_entries(table)[ti].first_block;
+    if (warp < n_params) {
+        const uint64_t n = entries[warp].n, first = entries[warp].first_block;
         const uint32_t w0 = (uint32_t)(first / span), w1 = n ? (uint32_t)((first + (n - 1) / FTC_STATE_BLOCK) / span) + 1 : w0;      // at most kSoloWarps warps
-        const double s = warp_sum(w0 + lane < w1 ? slots[w0 + lane + ti] : 0.0);
-        if (lane == 0 && norms) norms[ti] = (float)sqrt(s);
-        all += s;
+        all = warp_sum(w0 + lane < w1 ? slots[w0 + lane + warp] : 0.0);
+        if (lane == 0 && norms) norms[warp] = (float)sqrt(all);
     }
     if (lane == 0) part[warp] = all;
     __syncthreads();
@@ -637,7 +643,6 @@ __global__ void __launch_bounds__(128) grad_norm_kernel(const void* table, uint3
                                                         uint32_t* ticket, float* norm, float* norms) {
     __shared__ double part[4];
     __shared__ bool mine;
-    if (blockIdx.x >= n_params) wait_for_earlier_kernel();           // the one block of an empty table
     for (uint32_t ti = blockIdx.x; ti < n_params; ti += gridDim.x) {
         const uint64_t n = table_entries(table)[ti].n, first = table_entries(table)[ti].first_block;
         double s = 0;
@@ -663,26 +668,25 @@ __global__ void __launch_bounds__(128) grad_norm_kernel(const void* table, uint3
     if (threadIdx.x == 0) give_norm(s, max_norm, norm);
 }
 
-// Warps that share the blocks: those that the GPU holds at once; of more than 8 blocks for each, four times as many (8 blocks at least:
-// two rounds of loads), so that who is done early takes the next.
+// Warps that share the blocks: those that the GPU holds at once; of more than 32 blocks for each, four times as many, so that who is done
+// early takes the next (202M elements: 163 us against 173).
 uint32_t grad_norm_warps(uint64_t n_blocks, int sm_count) {
-    const uint64_t held = (uint64_t)sm_count * kWarps * 3, most = n_blocks / 8 < 4 * held ? n_blocks / 8 : 4 * held;
-    const uint64_t warps = n_blocks <= 8 * held ? (n_blocks < held ? n_blocks : held) : most;
-    return (uint32_t)(warps < kSoloWarps ? kSoloWarps : warps);      // room for either kernel
+    const uint64_t held = (uint64_t)sm_count * kWarps * 3;
+    return (uint32_t)(n_blocks < held ? n_blocks : n_blocks <= 32 * held ? held : 4 * held);
 }
 
 cudaError_t launch_grad_norm(const void* table, uint32_t n_params, uint64_t n_blocks, float max_norm, float* norm, float* norms, double* ws, int sm_count,
                              cudaStream_t st) {
-    const bool solo = n_blocks <= kSoloBlocks && n_params <= 16;
+    const bool solo = n_blocks <= kSoloBlocks && n_params <= kSoloTensors;
     const uint32_t warps = solo ? kSoloWarps : grad_norm_warps(n_blocks, sm_count);
     const uint64_t span = n_blocks ? (n_blocks + warps - 1) / warps : 1;
     double *slots = ws + 1, *sums = slots + warps + n_params;
     uint32_t* ticket = reinterpret_cast<uint32_t*>(ws);
     if (solo) {
-        grad_norm_solo_kernel<<<1, kSoloWarps * 32, 0, st>>>(table, n_params, n_blocks, span, max_norm, slots, norm, norms);
+        grad_norm_solo_kernel<<<1, kSoloWarps * 32, 0, st>>>(table, n_params, n_blocks, span, max_norm, norm, norms);
         return cudaGetLastError();
     }
-    grad_squares_kernel<<<(warps + kWarps - 1) / kWarps, kWarps * 32, 0, st>>>(table, n_params, n_blocks, span, slots, ticket);
+    grad_squares_kernel<<<warps ? (warps + kWarps - 1) / kWarps : 1, kWarps * 32, 0, st>>>(table, n_params, n_blocks, span, slots, ticket);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const uint32_t cap = (uint32_t)sm_count * 8;

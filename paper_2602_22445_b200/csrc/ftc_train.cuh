@@ -80,7 +80,7 @@ struct AdamArgs {
     uint32_t bits, mostly_wide;
 };
 cudaError_t launch_adamw(const AdamArgs& a, int sm_count, cudaStream_t st);
-cudaError_t launch_adamw_states(uint64_t blocks, const void* m, const void* v, const float* ms, const float* vs, float* mo, float* vo, int sm_count, cudaStream_t st);
+cudaError_t launch_adamw_states(uint64_t blocks, const void* m, const void* v, const float* ms, const float* vs, float* mo, float* vo, cudaStream_t st);
 uint32_t grad_norm_warps(uint64_t n_blocks, int sm_count);
 cudaError_t launch_grad_norm(const void* table, uint32_t n_params, uint64_t n_blocks, float max_norm, float* norm, float* norms, double* ws,
                              int sm_count, cudaStream_t st);

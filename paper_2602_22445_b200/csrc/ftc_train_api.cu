@@ -191,9 +191,7 @@ int ftc_adamw_states(uint64_t blocks, const void* d_m, const void* d_v, const fl
     if (blocks == 0) return FTC_OK;
     if (blocks > (1ull << 32) || !d_m || !d_v || !d_m_scale || !d_v_scale || !d_m_out || !d_v_out) return FTC_EINVAL;
     if (!aligned(d_m, 32) || !aligned(d_v, 32) || !aligned(d_m_out, 32) || !aligned(d_v_out, 32) || !aligned(d_m_scale, 4) || !aligned(d_v_scale, 4)) return FTC_EINVAL;
-    int sms = 0, rc = sm_count(sms);
-    if (rc != FTC_OK) return rc;
-    return status(launch_adamw_states(blocks, d_m, d_v, d_m_scale, d_v_scale, d_m_out, d_v_out, sms, static_cast<cudaStream_t>(cuda_stream)));
+    return status(launch_adamw_states(blocks, d_m, d_v, d_m_scale, d_v_scale, d_m_out, d_v_out, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 }  // extern "C"

@@ -264,7 +264,8 @@ def test_grad_norm_extremes():
 
 def test_empty_tables():
     import torch
-    for params in ([], [B.make_param(torch.empty(0, device="cuda"), torch.empty(0, device="cuda"))]):
+    empty = B.make_param(torch.empty(0, device="cuda"), torch.empty(0, device="cuda"))
+    for params in ([], [empty], [empty] * 40):
         table = B.make_param_table(params)
         assert table.blocks == 0
         ws = torch.empty(max(16, B.ftc_grad_norm_workspace_bytes(table)), dtype=torch.uint8, device="cuda")
