@@ -130,7 +130,7 @@ def check_codes(codes, scale, values, off, most, least):
 @pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("p,g,master", [("float32", "float32", False), ("bfloat16", "float32", True), ("bfloat16", "bfloat16", False),
                                         ("float16", "float16", True), ("float32", "bfloat16", False), ("float16", "float32", False)])
-@pytest.mark.parametrize("k,offset", [(0, 0), (0, 3), (32, 0), (7, 0), (4, 1), (1000, 16), (1, 0)])
+@pytest.mark.parametrize("k,offset", [(0, 0), (0, 3), (32, 0), (7, 0), (4, 1), (1000, 16), (1, 0), (4, 4), (0, 12), (3, 2), (2, 5)])
 def test_adamw(p, g, master, k, offset, bits):
     job = Job([bits, k, offset], SIZES, p, g, master, k, bits, offset)
     for step in (3, 4):
@@ -224,7 +224,8 @@ def test_many_steps_in_8_bits_follow_32_bits():
 
 
 @pytest.mark.parametrize("sizes", [[1], [256], [3, 0, 5], SIZES, [70001] * 3, [13] * 500, [1 << 20, 1, 300]])
-@pytest.mark.parametrize("g,k,offset", [("float32", 0, 0), ("bfloat16", 0, 1), ("float16", 0, 0), ("float32", 32, 0), ("float32", 7, 3)])
+@pytest.mark.parametrize("g,k,offset", [("float32", 0, 0), ("bfloat16", 0, 1), ("float16", 0, 0), ("float32", 32, 0), ("float32", 7, 3), ("float32", 4, 4),
+                                        ("float32", 0, 20), ("float32", 3, 2), ("float32", 1, 1)])
 def test_grad_norm(sizes, g, k, offset):
     import torch
     job = Job([len(sizes), k], sizes, "float32", g, False, k, 32, offset)
