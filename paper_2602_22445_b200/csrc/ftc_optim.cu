@@ -462,7 +462,7 @@ cudaError_t launch_adamw_states(uint64_t blocks, const void* m, const void* v, c
 }
 
 // ---- the norm: one pass over the gradients, bound by memory where they are many (202M elements in float32 with a record for each 32:
-// 153-163 us, 5.9 TB/s), by two kernels' beginnings where they are few. Warp w adds up the squares of the blocks [w*span, (w+1)*span) and leaves one sum for each tensor it meets; warp w and
+// 156 us, 5.8 TB/s), by two kernels' beginnings where they are few. Warp w adds up the squares of the blocks [w*span, (w+1)*span) and leaves one sum for each tensor it meets; warp w and
 // tensor t share slot w + t (going on by one block either grows, so no two pairs with blocks in common share a slot)
 
 // Sum of the squares of 8 numbers. In float32 where that neither overflows nor loses small squares (4 roundings at most one after the
@@ -480,13 +480,13 @@ __device__ __forceinline__ double squares(const F2* g) {
     return f >= 1e-30f && f <= 1e38f ? (double)f : squares_64(g[0], g[1], g[2], g[3]);
 }
 
-// The squares of one block that was loaded, with its records.
-template <bool WIDE> __device__ __forceinline__ double block_squares(const Raw& x, const TableEntry& t, uint64_t e0, uint32_t left) {
+// Elements e .. end - 1 of any tensor, two pieces of 256 under way.
+__device__ __forceinline__ double piece_squares(const Raw& x, const TableEntry& t, uint64_t e, uint32_t left) {
     F2 g[4];
-    numbers<WIDE>(g, x, t.grad_dtype);
+    numbers<false>(g, x, t.grad_dtype);
     if (t.status) {
         F2 w[4];
-        const uint32_t live = shares<WIDE>(w, t, e0, threadIdx.x & 31, left);
+        const uint32_t live = shares<false>(w, t, e, threadIdx.x & 31, left);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             g[i] = mul(g[i], w[i]);
@@ -495,104 +495,142 @@ template <bool WIDE> __device__ __forceinline__ double block_squares(const Raw& 
     }
     return squares(g);                                               // elements behind the end were loaded as zeros
 }
-// Blocks b .. end - 1 of any tensor, two of them under way.
-template <bool WIDE> __device__ __forceinline__ double walk_squares(const TableEntry& t, uint64_t b, uint64_t end) {
+__device__ __forceinline__ double walk_squares(const TableEntry& t, uint64_t e, uint64_t end) {
     const uint32_t lane = threadIdx.x & 31;
     double s = 0;
-    for (uint64_t e0 = (b - t.first_block) * FTC_STATE_BLOCK; b < end; b += 2, e0 += 2 * FTC_STATE_BLOCK) {
+    for (; e < end; e += 2 * FTC_STATE_BLOCK) {
         Raw x, y;
-        const uint64_t rest = t.n - e0;
-        const bool two = b + 1 < end;
+        const uint64_t rest = end - e;
         const uint32_t left = rest < FTC_STATE_BLOCK ? (uint32_t)rest : FTC_STATE_BLOCK;
-        const uint32_t more = !two ? 0 : rest < 2 * FTC_STATE_BLOCK ? (uint32_t)rest - FTC_STATE_BLOCK : FTC_STATE_BLOCK;
-        load_raw<WIDE>(x, t.grad, t.grad_dtype, e0, lane, left);
-        if (two) load_raw<WIDE>(y, t.grad, t.grad_dtype, e0 + FTC_STATE_BLOCK, lane, more);
-        s += block_squares<WIDE>(x, t, e0, left);
-        if (two) s += block_squares<WIDE>(y, t, e0 + FTC_STATE_BLOCK, more);
+        const uint32_t more = rest <= FTC_STATE_BLOCK ? 0 : rest < 2 * FTC_STATE_BLOCK ? (uint32_t)rest - FTC_STATE_BLOCK : FTC_STATE_BLOCK;
+        load_raw<false>(x, t.grad, t.grad_dtype, e, lane, left);
+        if (more) load_raw<false>(y, t.grad, t.grad_dtype, e + FTC_STATE_BLOCK, lane, more);
+        s += piece_squares(x, t, e, left);
+        if (more) s += piece_squares(y, t, e + FTC_STATE_BLOCK, more);
     }
     return s;
 }
 
-// `blocks` full aligned blocks of elements of one type from `p` (this lane's first) on; record `message` and every `stride`-th after
-// it for those that have one.
-template <uint32_t DTYPE, bool STATUS, bool SOLO>
-__device__ __forceinline__ double run_squares(const char* p, uint32_t blocks, const uint32_t* status, uint32_t message, uint32_t stride) {
-    constexpr uint32_t BYTES = FTC_STATE_BLOCK * (DTYPE == FTC_F32 ? 4 : 2);
-    constexpr int AHEAD = DTYPE == FTC_F32 || SOLO ? 4 : 8;           // blocks whose loads are out at once: 4 KB a warp (a lone block of 32 warps: 64 registers)
-    double s = 0;
-    const uint2* st = reinterpret_cast<const uint2*>(status + (uint64_t)message * FTC_STATUS_WORDS);
-    const uint64_t next = (uint64_t)stride * (FTC_STATUS_WORDS / 2);
-    const auto add_one = [&](const Raw& x, uint2 r) {
-        F2 g[4];
-        numbers<true>(g, x, DTYPE);
-        const float share = STATUS ? share_of(r) : 1.f;
-        if (share > 0.f) s = ::fma((double)share * share, squares(g), s);
-    };
-    const auto load_one = [&](Raw& x, int i) { if (DTYPE == FTC_F32) load_32(p + i * BYTES, x.r); else load_16(p + i * BYTES, x.r); };
-    for (; blocks >= AHEAD; blocks -= AHEAD, p += AHEAD * BYTES, st += AHEAD * next) {
-        Raw x[AHEAD];
-        uint2 r[AHEAD];
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) { r[i] = STATUS ? st[i * next] : make_uint2(0u, 1u); load_one(x[i], i); }
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) add_one(x[i], r[i]);
+// `pieces` times 256 elements of one type; this lane's first eight are e .. e + 7, on a boundary of eight. A lane's eight have
+// no record, one (the records of neighbouring pieces lie a fixed way apart then), or up to two or three (82M elements in float32 with a
+// record for each 7: 104 us; element by element by way of the warp's lanes 262).
+template <uint32_t DTYPE, int RECORDS, bool SOLO> __device__ __forceinline__ double run_squares(const TableEntry& t, uint64_t e, uint32_t pieces) {
+    constexpr uint32_t BYTES = FTC_STATE_BLOCK * (DTYPE == FTC_F32 ? 4 : 2), RECORD = FTC_STATUS_WORDS / 2;
+    constexpr int AHEAD = SOLO ? RECORDS >= 2 ? 2 : 4 : DTYPE == FTC_F32 || RECORDS >= 2 ? 4 : 8;       // pieces whose loads are out at once: 4 KB a warp; fewer in the lone block's 64 registers
+    struct In { Raw x; uint2 a, b, c; uint32_t split; };                // a: for the first `split` elements, b: for the k after them
+    const char* p = static_cast<const char*>(t.grad) + e * (BYTES / FTC_STATE_BLOCK);
+    const uint2* st = nullptr;
+    uint64_t next = 0;
+    uint32_t place = 0, over = 0, k = 0;
+    if (RECORDS) {
+        k = t.k;
+        st = reinterpret_cast<const uint2*>(t.status) + message_of(t, e, place) * RECORD;
+        next = (uint64_t)(FTC_STATE_BLOCK / k) * RECORD;
+        over = FTC_STATE_BLOCK % k;
     }
-    if (blocks) {
-        Raw x[AHEAD - 1];
-        uint2 r[AHEAD - 1];
+    const auto load = [&](In& in, int i) {                           // of the piece i from here
+        if (RECORDS) in.a = st[i * next];
+        if (RECORDS >= 2) {
+            in.split = k - place;
+            in.b = st[in.split < 8 ? RECORD : 0];
+        }
+        if (RECORDS == 3) in.c = st[in.split + k < 8 ? 2 * RECORD : 0];
+        if (DTYPE == FTC_F32) load_32(p + i * BYTES, in.x.r);
+        else load_16(p + i * BYTES, in.x.r);
+    };
+    const auto go_on = [&](int i) {                                  // i pieces; one at a time where a place in the message is kept
+        p += i * BYTES;
+        if (RECORDS) st += i * next;
+        if (RECORDS >= 2) {
+            place += over;
+            if (place >= k) { place -= k; st += RECORD; }
+        }
+    };
+    constexpr bool EACH = RECORDS >= 2;
+    double s = 0;
+    const auto add_one = [&](const In& in) {
+        F2 g[4];
+        numbers<true>(g, in.x, DTYPE);
+        const float a = RECORDS ? share_of(in.a) : 1.f;
+        if (RECORDS >= 2) {
+            const float b = share_of(in.b), c = RECORDS == 3 ? share_of(in.c) : 0.f;
+            const auto shared = [&](float x, uint32_t j) {
+                const float f = j < in.split ? a : RECORDS == 2 || j < in.split + k ? b : c;
+                return f > 0.f ? x * f : 0.f;                        // what was not delivered may be NaN
+            };
+#pragma unroll
+            for (int i = 0; i < 4; ++i) g[i] = pair(shared(lo(g[i]), 2 * i), shared(hi(g[i]), 2 * i + 1));
+            s += squares(g);
+        } else if (a > 0.f) s = ::fma((double)a * a, squares(g), s);
+    };
+    for (; pieces >= AHEAD; pieces -= AHEAD) {
+        In in[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) { load(in[i], EACH ? 0 : i); if (EACH) go_on(1); }
+        if (!EACH) go_on(AHEAD);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) add_one(in[i]);
+    }
+    if (pieces) {
+        In in[AHEAD - 1];
 #pragma unroll
         for (int i = 0; i < AHEAD - 1; ++i) {                       // behind the end the last one again, not added
-            const int at = i < (int)blocks ? i : (int)blocks - 1;
-            r[i] = STATUS ? st[at * next] : make_uint2(0u, 1u);
-            load_one(x[i], at);
+            const bool more = i + 1 < (int)pieces;
+            load(in[i], EACH ? 0 : i < (int)pieces ? i : (int)pieces - 1);
+            if (EACH && more) go_on(1);
         }
 #pragma unroll
         for (int i = 0; i < AHEAD - 1; ++i)
-            if (i < (int)blocks) add_one(x[i], r[i]);
+            if (i < (int)pieces) add_one(in[i]);
     }
     return s;
 }
+template <int RECORDS, bool SOLO> __device__ __forceinline__ double run_squares(const TableEntry& t, uint64_t e, uint32_t pieces) {
+    return t.grad_dtype == FTC_F32 ? run_squares<FTC_F32, RECORDS, SOLO>(t, e, pieces)
+         : t.grad_dtype == FTC_BF16 ? run_squares<FTC_BF16, RECORDS, SOLO>(t, e, pieces) : run_squares<FTC_F16, RECORDS, SOLO>(t, e, pieces);
+}
 
-// The sums of the warp w, whose first block is of tensor `ti`.
-template <bool SOLO> __device__ __forceinline__ void warp_squares(const TableEntry* entries, uint32_t ti, uint64_t n_blocks, uint64_t span, uint64_t w, double* slots) {
+// The sums of the warp w, whose first block is of tensor `ti`. Where a tensor does not begin on a boundary of 8 elements its blocks are
+// taken `h` elements later, on the first such boundary; the tensor's first warp has the h elements before it, its last warp up to a block less
+// (72M bf16 elements packed without padding: 44 us, with loads of single elements 55). MIXED: with the code for two and three records; without
+// it the kernel is smaller and takes 156 us for 202M elements in place of 158.
+template <bool SOLO, bool MIXED> __device__ __forceinline__ void warp_squares(const TableEntry* entries, uint32_t ti, uint64_t n_blocks, uint64_t span, uint64_t w, double* slots) {
     const uint32_t lane = threadIdx.x & 31;
     uint64_t b = w * span;
     const uint64_t b1 = b + span < n_blocks ? b + span : n_blocks;
     for (; b < b1; ++ti) {
         const TableEntry& t = entries[ti];
-        if (t.n == 0) continue;
-        const uint64_t first = t.first_block, n = t.n, last = first + (n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK, end = last < b1 ? last : b1;
-        const uint32_t k = t.k, dtype = t.grad_dtype;
-        const uint64_t full = t.wide ? first + n / FTC_STATE_BLOCK : 0, end_wide = full < end ? full : end;
-        // runs: full blocks on wide boundaries; with records, where messages fit a block and hold whole lanes
-        const bool run = t.wide && (!t.status || (k % 8 == 0 && FTC_STATE_BLOCK % k == 0 && n <= 0xFFFFFFFFull));
-        const uint64_t whole = run ? first + n / FTC_STATE_BLOCK : 0, end_run = whole < end ? whole : end;
+        const uint64_t n = t.n;
+        if (n == 0) continue;
+        const uint64_t first = t.first_block, last = first + (n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK, end = last < b1 ? last : b1;
+        const uint32_t h = (uint32_t)(0 - reinterpret_cast<uintptr_t>(t.grad) / (t.grad_dtype == FTC_F32 ? 4 : 2)) & 7u, k = t.k;
+        uint64_t e = b == first ? 0 : (b - first) * FTC_STATE_BLOCK + h, to = end == last ? n : (end - first) * FTC_STATE_BLOCK + h;
+        b = end;
+        if (to > n) to = n;
         double s = 0;
-        if (b < end_run) {
-            const uint64_t e = (b - first) * FTC_STATE_BLOCK + lane * 8;
-            const char* p = static_cast<const char*>(t.grad) + e * (dtype == FTC_F32 ? 4 : 2);
-            const uint32_t blocks = (uint32_t)(end_run - b);
-            if (t.status) {
-                const uint32_t message = (uint32_t)e / k, stride = FTC_STATE_BLOCK / k;
-                s = dtype == FTC_F32 ? run_squares<FTC_F32, true, SOLO>(p, blocks, t.status, message, stride)
-                  : dtype == FTC_BF16 ? run_squares<FTC_BF16, true, SOLO>(p, blocks, t.status, message, stride) : run_squares<FTC_F16, true, SOLO>(p, blocks, t.status, message, stride);
-            } else
-                s = dtype == FTC_F32 ? run_squares<FTC_F32, false, SOLO>(p, blocks, nullptr, 0, 0)
-                  : dtype == FTC_BF16 ? run_squares<FTC_BF16, false, SOLO>(p, blocks, nullptr, 0, 0) : run_squares<FTC_F16, false, SOLO>(p, blocks, nullptr, 0, 0);
-            b = end_run;
+        if (e == 0 && h) { e = h < to ? h : to; s = walk_squares(t, 0, e); }
+        if (to >= e + FTC_STATE_BLOCK) {
+            const uint64_t mine = e + lane * 8;
+            const uint32_t pieces = (uint32_t)((to - e) / FTC_STATE_BLOCK);
+            bool run = true;
+            if (!t.status) s += run_squares<0, SOLO>(t, mine, pieces);
+            else if (h == 0 && k % 8 == 0 && FTC_STATE_BLOCK % k == 0) s += run_squares<1, SOLO>(t, mine, pieces);
+            else if (MIXED && (k >= 7 || (k == 4 && h % 4 == 0))) s += run_squares<2, SOLO>(t, mine, pieces);          // eight neighbours meet two messages at most
+            else if (MIXED && k >= 4) s += run_squares<3, SOLO>(t, mine, pieces);
+            else run = false;
+            if (run) e += (uint64_t)pieces * FTC_STATE_BLOCK;
         }
-        if (b < end_wide) { s += walk_squares<true>(t, b, end_wide); b = end_wide; }
-        if (b < end) { s += walk_squares<false>(t, b, end); b = end; }
+        if (e < to) s += walk_squares(t, e, to);
         s = warp_sum(s);
         if (lane == 0) slots[w + ti] = s;
     }
 }
 
-__global__ void __launch_bounds__(kWarps * 32, 3) grad_squares_kernel(const void* table, uint32_t n_params, uint64_t n_blocks, uint64_t span, double* slots, uint32_t* ticket) {
+template <bool MIXED> __global__ void __launch_bounds__(kWarps * 32, 3) grad_squares_kernel(const void* table, uint32_t n_params, uint64_t n_blocks, uint64_t span, double* slots, uint32_t* ticket) {
     later_kernel_may_start();
     const uint64_t w = blockIdx.x * (uint64_t)kWarps + (threadIdx.x >> 5);
     if (w == 0 && (threadIdx.x & 31) == 0) *ticket = 0;
-    if (w * span < n_blocks) warp_squares<false>(table_entries(table), table_map(table, n_params)[w * span], n_blocks, span, w, slots);
+    if (w * span < n_blocks) warp_squares<false, MIXED>(table_entries(table), table_map(table, n_params)[w * span], n_blocks, span, w, slots);
 }
 
 __device__ __forceinline__ void give_norm(double s, float max_norm, float* norm) {
@@ -603,7 +641,7 @@ __device__ __forceinline__ void give_norm(double s, float max_norm, float* norm)
 
 // Tables of few blocks and tensors: all in one thread block, entries and sums in shared memory (132 blocks of 6 tensors: 6.6 us a call, as long as its checks and launch take, against 8.2 by way of the workspace).
 constexpr uint32_t kSoloWarps = 32, kSoloBlocks = 160, kSoloTensors = 16;
-__global__ void __launch_bounds__(kSoloWarps * 32) grad_norm_solo_kernel(const void* table, uint32_t n_params, uint64_t n_blocks, uint64_t span, float max_norm,
+template <bool MIXED> __global__ void __launch_bounds__(kSoloWarps * 32) grad_norm_solo_kernel(const void* table, uint32_t n_params, uint64_t n_blocks, uint64_t span, float max_norm,
                                                                          float* norm, float* norms) {
     __shared__ TableEntry entries[kSoloTensors];
     __shared__ double slots[kSoloWarps + kSoloTensors], part[kSoloWarps];
@@ -612,7 +650,7 @@ __global__ void __launch_bounds__(kSoloWarps * 32) grad_norm_solo_kernel(const v
     if (threadIdx.x < n_params * (sizeof(TableEntry) / 4))
         reinterpret_cast<uint32_t*>(entries)[threadIdx.x] = reinterpret_cast<const uint32_t*>(table_entries(table))[threadIdx.x];
     __syncthreads();
-    warp_squares<true>(entries, ti, n_blocks, span, warp, slots);
+    warp_squares<true, MIXED>(entries, ti, n_blocks, span, warp, slots);
     __syncthreads();
     double all = 0;
     if (warp < n_params) {
@@ -675,7 +713,7 @@ uint32_t grad_norm_warps(uint64_t n_blocks, int sm_count) {
     return (uint32_t)(n_blocks < held ? n_blocks : n_blocks <= 32 * held ? held : 4 * held);
 }
 
-cudaError_t launch_grad_norm(const void* table, uint32_t n_params, uint64_t n_blocks, float max_norm, float* norm, float* norms, double* ws, int sm_count,
+cudaError_t launch_grad_norm(const void* table, uint32_t n_params, uint64_t n_blocks, bool mixed, float max_norm, float* norm, float* norms, double* ws, int sm_count,
                              cudaStream_t st) {
     const bool solo = n_blocks <= kSoloBlocks && n_params <= kSoloTensors;
     const uint32_t warps = solo ? kSoloWarps : grad_norm_warps(n_blocks, sm_count);
@@ -683,10 +721,10 @@ cudaError_t launch_grad_norm(const void* table, uint32_t n_params, uint64_t n_bl
     double *slots = ws + 1, *sums = slots + warps + n_params;
     uint32_t* ticket = reinterpret_cast<uint32_t*>(ws);
     if (solo) {
-        grad_norm_solo_kernel<<<1, kSoloWarps * 32, 0, st>>>(table, n_params, n_blocks, span, max_norm, norm, norms);
+        (mixed ? grad_norm_solo_kernel<true> : grad_norm_solo_kernel<false>)<<<1, kSoloWarps * 32, 0, st>>>(table, n_params, n_blocks, span, max_norm, norm, norms);
         return cudaGetLastError();
     }
-    grad_squares_kernel<<<warps ? (warps + kWarps - 1) / kWarps : 1, kWarps * 32, 0, st>>>(table, n_params, n_blocks, span, slots, ticket);
+    (mixed ? grad_squares_kernel<true> : grad_squares_kernel<false>)<<<warps ? (warps + kWarps - 1) / kWarps : 1, kWarps * 32, 0, st>>>(table, n_params, n_blocks, span, slots, ticket);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const uint32_t cap = (uint32_t)sm_count * 8;

@@ -38,7 +38,7 @@ template <typename... A> cudaError_t launch_second(void (*kernel)(A...), dim3 gr
 // ---- the table of tensors: header, entries, one tensor index for each block of FTC_STATE_BLOCK elements ----
 
 constexpr uint64_t kTableMagic = 0x3154424154435446ull;
-struct TableHead { uint64_t magic, n_blocks; uint32_t n_params, flags; uint64_t pad; };     // flags bit 0: some tensor has no weights; 1: most blocks are full ones of aligned tensors
+struct TableHead { uint64_t magic, n_blocks; uint32_t n_params, flags; uint64_t pad; };     // flags bit 0: some tensor has no weights; 1: most blocks are full ones of aligned tensors; 2: neighbours of some tensor's 8 have more than one record
 struct TableEntry {
     void* param; float* master; const void* grad; const uint32_t* status;
     uint64_t n, first_block;
@@ -82,7 +82,7 @@ struct AdamArgs {
 cudaError_t launch_adamw(const AdamArgs& a, int sm_count, cudaStream_t st);
 cudaError_t launch_adamw_states(uint64_t blocks, const void* m, const void* v, const float* ms, const float* vs, float* mo, float* vo, cudaStream_t st);
 uint32_t grad_norm_warps(uint64_t n_blocks, int sm_count);
-cudaError_t launch_grad_norm(const void* table, uint32_t n_params, uint64_t n_blocks, float max_norm, float* norm, float* norms, double* ws,
+cudaError_t launch_grad_norm(const void* table, uint32_t n_params, uint64_t n_blocks, bool mixed, float max_norm, float* norm, float* norms, double* ws,
                              int sm_count, cudaStream_t st);
 
 }  // namespace ftc

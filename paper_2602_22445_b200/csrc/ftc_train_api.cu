@@ -132,6 +132,7 @@ int ftc_param_table_build(const ftc_param_t* h_params, uint32_t n_params, void* 
         q.wide = aligned(t.grad, 8 * size_of(t.grad_dtype)) && aligned(t.param, 8 * size_of(t.param_dtype)) && aligned(t.master, 32);   // 8 elements a load
         q.lr_scale = t.lr_scale; q.weight_decay = t.weight_decay;
         if (t.n && !t.param) h->flags |= 1u;
+        if (t.status && (t.k % 8 || FTC_STATE_BLOCK % t.k || !aligned(t.grad, 8 * size_of(t.grad_dtype)))) h->flags |= 4u;
         if (q.wide) wide += t.n / FTC_STATE_BLOCK;
         for (const uint64_t end = at + (t.n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK; at < end; ++at) map[at] = i;
     }
@@ -159,7 +160,7 @@ int ftc_grad_norm(const void* h_table, const void* d_table, float max_norm, floa
     int sms = 0, rc = sm_count(sms);
     if (rc != FTC_OK) return rc;
     if (!d_workspace || !aligned(d_workspace, 16) || workspace_bytes < grad_norm_doubles(h, sms) * sizeof(double)) return FTC_EWORKSPACE;
-    return status(launch_grad_norm(d_table, h->n_params, h->n_blocks, max_norm, d_norm, d_norms, static_cast<double*>(d_workspace), sms,
+    return status(launch_grad_norm(d_table, h->n_params, h->n_blocks, h->flags >> 2 & 1u, max_norm, d_norm, d_norms, static_cast<double*>(d_workspace), sms,
                                    static_cast<cudaStream_t>(cuda_stream)));
 }
 
