@@ -375,7 +375,7 @@ __device__ __forceinline__ void adamw_one(const AdamArgs& a, const TableEntry& t
 
 // A warp takes one block; 32 warps an SM, no loop: the table's entry and the block's loads are the whole wait, and other warps fill it. 32-bit
 // states run at a copy's speed (101M elements, bf16 weights with a float32 copy, records: 455-470 us, 6.6 TB/s); states in 8 bits take
-// 85 instructions an element the narrow way (packed odd tensors, 17M elements: 82 us, 4.0 TB/s with the read-out), which bounds them.
+// 77 instructions an element the narrow way (packed odd tensors, 17M elements: 70 us, 3.5 TB/s, 58 % of the issue slots), which bounds them.
 // WIDE: full blocks of aligned tensors go the wide way; else all go the narrow one.
 template <int BITS, bool WIDE>
 __global__ void __launch_bounds__(kWarps * 32, 4) adamw_kernel(AdamArgs a) {
@@ -390,8 +390,8 @@ __global__ void __launch_bounds__(kWarps * 32, 4) adamw_kernel(AdamArgs a) {
     else adamw_one<BITS, false>(a, t, b, lane, e0, left < FTC_STATE_BLOCK ? (uint32_t)left : FTC_STATE_BLOCK, scale);
 }
 
-// States in 8 bits, whose arithmetic (66 instructions an element) takes about as long as the memory: 201M elements in 606 us, 5.3 TB/s,
-// 66 % of the issue slots. Prefetch by way of shared memory at 24 or 32 warps an SM spilled and was slower (695, 820 us). A warp takes `span` blocks one after the other, the next one's
+// States in 8 bits, whose arithmetic (63 instructions an element) takes about as long as the memory: 201M elements in 606 us, 5.3 TB/s,
+// 64 % of the issue slots. Prefetch by way of shared memory at 24 or 32 warps an SM spilled and was slower (695, 820 us). A warp takes `span` blocks one after the other, the next one's
 // loads out while it works on the present one.
 constexpr uint32_t kWalkWarps = 8, kWalkBlocks = 2;
 __global__ void __launch_bounds__(kWalkWarps * 32, kWalkBlocks) adamw_walk_kernel(AdamArgs a, uint64_t span) {
@@ -421,7 +421,7 @@ __global__ void __launch_bounds__(kWalkWarps * 32, kWalkBlocks) adamw_walk_kerne
 
 cudaError_t launch_adamw(const AdamArgs& a, int sms, cudaStream_t st) {
     // The walk pays from four blocks a warp on (24 layers, 201M elements: 606 us against 725); the narrow way has too much in
-    // registers for it (packed odd tensors: 98 us against 82).
+    // registers for it (packed odd tensors: 98 us against 82, both at 85 instructions an element).
     const uint64_t warps = (uint64_t)sms * kWalkWarps * kWalkBlocks;
     if (a.bits == 8 && a.mostly_wide && a.n_blocks >= warps * 4) {
         adamw_walk_kernel<<<sms * kWalkBlocks, kWalkWarps * 32, 0, st>>>(a, (a.n_blocks + warps - 1) / warps);
