@@ -245,6 +245,43 @@ def test_grad_norm(sizes, g, k, offset):
     assert torch.equal(alone, norm)
 
 
+@pytest.mark.parametrize("g", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("k,offset", [(0, 0), (0, 3), (32, 0), (32, 8), (32, 3), (8, 4), (7, 0), (9, 5), (5, 2), (6, 0), (4, 1), (4, 4), (3, 0), (300, 1), (1000, 0)])
+def test_grad_norm_of_long_tensors(g, k, offset):
+    """Warps that walk many blocks: few numbers among zeros, few delivered messages among such of NaN, so that one element too many or
+    too few shows. Whole numbers and shares of powers of two: the sums are exact, and the root and its rounding are all that is off."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(100 * k + offset)
+    params, want = [], []
+    for n in (9_000_001, 513, 7_000_007, 2_000_000):
+        grad = torch.empty(n + offset, dtype=getattr(torch, g), device="cuda")[offset:]
+        values = torch.randint(-8, 9, (n,), generator=gen, device="cuda").double()
+        few = 200 if n > 1000 else 2
+        if k:
+            messages = -(-n // k)
+            status = torch.zeros(messages, 4, dtype=torch.int32, device="cuda")
+            status[:, 1] = 1 << torch.randint(0, 3, (messages,), generator=gen, device="cuda")
+            lost = torch.randint(0, few * 8 // k + 2, (messages,), generator=gen, device="cuda") > 0
+            status[:, 0] = lost.int() * 2
+            status[:, 1] *= 1 - (lost & (torch.arange(messages, device="cuda") % 2 == 0)).int()      # half of the lost ones with a count, half without
+            each = lost.repeat_interleave(k)[:n]
+            grad.copy_(torch.where(each, float("nan"), values))
+            share = torch.where(lost, 0.0, 1.0 / status[:, 1].clamp(min=1).double()).repeat_interleave(k)[:n]
+            want.append(((values * share) ** 2).sum())
+        else:
+            status, values = None, values * (torch.randint(0, few, (n,), generator=gen, device="cuda") == 0)
+            grad.copy_(values)
+            want.append((values ** 2).sum())
+        params.append(B.make_param(None, grad, status=status, k=k))
+    table = B.make_param_table(params)
+    ws = torch.empty(B.ftc_grad_norm_workspace_bytes(table), dtype=torch.uint8, device="cuda")
+    norm, norms = torch.empty(2, device="cuda"), torch.empty(4, device="cuda")
+    B.ftc_grad_norm(table, 1e9, norm, norms, ws)
+    want = torch.stack(want)
+    assert torch.allclose(norms.double(), want.sqrt(), rtol=2 * O.U, atol=0)
+    assert abs(float(norm[0]) - float(want.sum().sqrt())) <= 2 * O.U * float(want.sum().sqrt())
+
+
 def test_grad_norm_extremes():
     import torch
     job = Job([1], [3000, 5], "float32", "float32", False, 0, 32)
