@@ -139,6 +139,16 @@ def test_adamw(p, g, master, k, offset, bits):
         job.check(before, step)
 
 
+@pytest.mark.parametrize("p,g,master,k", [("bfloat16", "bfloat16", True, 0), ("float32", "float32", False, 32), ("float16", "float32", True, 7), ("float32", "float16", False, 1000)])
+def test_long_tensors_in_8_bits(p, g, master, k):
+    """More blocks than one for each warp that the GPU holds: warps walk, and fetch a block while they work on another."""
+    job = Job([8, k, 77], [2_500_001, 300, 150_016, 5], p, g, master, k, 8)
+    for step in (1, 5):
+        before = job.weights(), job.states()
+        job.step(step)
+        job.check(before, step)
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_first_step_from_zero_states_and_a_scale(bits):
     import torch
