@@ -392,6 +392,102 @@ template <typename T, typename W, int MODE, int NV> __device__ __forceinline__ v
     for (int j = 0; j < P::E / 2; ++j) v[j] = pair(f[2 * j], f[2 * j + 1]);
 }
 
+// ---- narrow rows (H <= 256): L lanes hold a row, 8 elements each, and a warp 32 / L rows, so that a warp's instructions do not depend on
+// how little of it a row would fill (bf16, 262144 rows of 64: 14.4 us against 61.5 with a warp for each row, 4.7 TB/s; 65536 rows of 97 that
+// begin between words: 16.3 against 37.5). No ring: a warp has ROUNDS such rounds of rows under way in registers, 24 warps an SM (32 with 64
+// registers: bf16 rows of 64 16.4, of 128 32.0 against 28.8). VEC: neighbours in vectors of 16 bytes; else single elements L apart, for rows that begin
+// anywhere. Bound by instructions below 128 columns (the two sums' exchanges), by memory above.
+constexpr uint32_t kNarrow = 256, kNarrowWarps = 8, kNarrowBlocks = 3;
+
+template <typename T, bool VEC, int L> struct NarrowPart {
+    static constexpr int N = VEC ? 16 / (int)sizeof(T) : 1, NV = 8 / N, VB = N * (int)sizeof(T), ROUNDS = VEC && sizeof(T) == 2 ? 4 : 2;
+    static __device__ __forceinline__ uint32_t column(int i) { return (threadIdx.x % L + L * i) * N; }        // of vector i
+    static __device__ __forceinline__ void load(Pack<T, VB> (&x)[NV], const T* row, uint32_t n) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) { if (column(i) < n) x[i].load(row + column(i)); else x[i].clear(); }
+    }
+    static __device__ __forceinline__ void numbers(F2* v, const Pack<T, VB> (&x)[NV]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = pair(x[2 * j / N].get(2 * j % N), x[(2 * j + 1) / N].get((2 * j + 1) % N));
+    }
+    template <typename W> static __device__ __forceinline__ void weights(F2* v, const void* w, float other, uint32_t n) {
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) f[i * N + j] = other;
+            if (column(i) < n) load_weights<W, N>(f + i * N, static_cast<const W*>(w), column(i), other);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = pair(f[2 * j], f[2 * j + 1]);
+    }
+    static __device__ __forceinline__ void store(T* row, const F2* v, uint32_t n) {
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = element(v, j);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (column(i) < n) Pack<T, VB>::store(row + column(i), f + i * N);
+    }
+    static __device__ __forceinline__ F2 inside(F2 v, int j, uint32_t n) {      // pair j; zeros behind the row's end
+        return pair(column(2 * j / N) < n ? lo(v) : 0.f, column((2 * j + 1) / N) < n ? hi(v) : 0.f);
+    }
+    // Sum over the row's lanes of 8 numbers each.
+    static __device__ __forceinline__ float sum(float v) {
+#pragma unroll
+        for (int o = L / 2; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+        return v;
+    }
+};
+__device__ __forceinline__ float sum_of_8(const F2* v) { const F2 s = add(add(v[0], v[1]), add(v[2], v[3])); return lo(s) + hi(s); }
+
+template <typename T, typename W, bool VEC, int L>
+__global__ void __launch_bounds__(kNarrowWarps * 32, kNarrowBlocks) norm_forward_narrow_kernel(NormArgs a) {
+    using P = NarrowPart<T, VEC, L>;
+    constexpr int U = P::ROUNDS, PER = 32 / L;
+    const uint32_t sub = threadIdx.x % 32 / L;
+    const float inv = 1.f / (float)a.H;
+    F2 g[4], b[4];
+    P::template weights<W>(g, a.gamma, 1.f, a.H);
+    P::template weights<W>(b, a.beta, 0.f, a.H);
+    const uint64_t step = (uint64_t)gridDim.x * kNarrowWarps * U * PER;
+    for (uint64_t r = ((uint64_t)blockIdx.x * kNarrowWarps + threadIdx.x / 32) * U * PER + sub; r - sub < a.rows; r += step) {
+        Pack<T, P::VB> in[U][P::NV];
+#pragma unroll
+        for (int u = 0; u < U; ++u) P::load(in[u], static_cast<const T*>(a.x) + (r + u * PER) * a.x_stride, r + u * PER < a.rows ? a.H : 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            F2 x[4], s[4];
+            P::numbers(x, in[u]);
+            const float mean = P::sum(sum_of_8(x)) * inv;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { x[j] = P::inside(add(x[j], twice(-mean)), j, a.H); s[j] = mul(x[j], x[j]); }
+            const float rstd = inverse_root(P::sum(sum_of_8(s)) * inv + a.eps);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = fma(mul(x[j], twice(rstd)), g[j], b[j]);
+            const uint64_t row = r + u * PER;
+            if (row >= a.rows) continue;
+            P::store(static_cast<T*>(a.y) + row * a.y_stride, x, a.H);
+            if (threadIdx.x % L == 0) {
+                if (a.mean_out) a.mean_out[row] = mean;
+                if (a.rstd_out) a.rstd_out[row] = rstd;
+            }
+        }
+    }
+}
+template <typename T, typename W, bool VEC, int L> static cudaError_t forward_narrow(const NormArgs& a, int sms, cudaStream_t st) {
+    const uint64_t each = kNarrowWarps * NarrowPart<T, VEC, L>::ROUNDS * (32 / L), blocks = (a.rows + each - 1) / each, cap = (uint64_t)sms * kNarrowBlocks;
+    norm_forward_narrow_kernel<T, W, VEC, L><<<(uint32_t)(blocks < cap ? blocks : cap), kNarrowWarps * 32, 0, st>>>(a);
+    return cudaGetLastError();
+}
+template <typename T, typename W, bool VEC> static cudaError_t forward_narrow(const NormArgs& a, int sms, cudaStream_t st) {
+    if (a.H <= 32) return forward_narrow<T, W, VEC, 4>(a, sms, st);
+    if (a.H <= 64) return forward_narrow<T, W, VEC, 8>(a, sms, st);
+    if (a.H <= 128) return forward_narrow<T, W, VEC, 16>(a, sms, st);
+    if constexpr (VEC && sizeof(T) == 2) return cudaErrorNotSupported;          // not called
+    else return forward_narrow<T, W, VEC, 32>(a, sms, st);
+}
+
 // blockDim = (G, groups in the block). A group takes R rows at a time: two rows share the barriers, and one's latencies hide the other's.
 // gamma and beta wait in shared memory, each thread's own where it left them: as registers they would cost a block of three.
 // Bound by memory where rows are many (bf16, 32768 rows of 4096: 88 us, 6.1 TB/s, 0.93 of a copy; the instructions take 54 % of the issue
@@ -644,7 +740,11 @@ template <typename T, typename W, int MODE, int NV> static cudaError_t forward_r
 template <typename T, typename W> static cudaError_t forward_rows(const NormArgs& a, uint32_t v, int sms, cudaStream_t st) {
     constexpr int e = sizeof(T);
     if (a.H > 16 * kMaxGroup) return cudaErrorNotSupported;
-    if (v == 16) return a.H <= 32 * 16 / e ? forward_run<T, W, kAligned, 1>(a, sms, st) : forward_run<T, W, kAligned, e>(a, sms, st);
+    // Narrow: bf16, 65536 rows of 256 on 16 bytes take 12.4 us by way of the ring against 15.1, all else is faster without it.
+    if constexpr (e == 2)
+        if (v == 16 && a.H > kNarrow / 2 && a.H <= kNarrow) return forward_run<T, W, kAligned, 1>(a, sms, st);
+    if (a.H <= kNarrow) return v == 16 ? forward_narrow<T, W, true>(a, sms, st) : forward_narrow<T, W, false>(a, sms, st);
+    if (v == 16) return forward_run<T, W, kAligned, e>(a, sms, st);
     if constexpr (e == 2)
         if (v == 2) return forward_run<T, W, kOdd, 8>(a, sms, st);
     return forward_run<T, W, kWords, 4 * e>(a, sms, st);

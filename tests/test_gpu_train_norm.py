@@ -73,6 +73,25 @@ def test_forward(rows, H, dtype, wdtype):
 
 
 @pytest.mark.parametrize("dtype,wdtype", TYPES)
+@pytest.mark.parametrize("H", [2, 24, 32, 40, 57, 64, 72, 97, 128, 130, 136, 193, 248, 256])
+def test_forward_of_narrow_rows(H, dtype, wdtype):
+    """Rows that share a warp: as many as end within its last round, and more than the GPU holds; nothing between the rows is written."""
+    rng = np.random.default_rng([H, 9])
+    for rows, pad, offset in ((1, 0, 0), (75, 8, 8), (75, 1, 1), (40003, 0, 0), (9001, 3, 2)):
+        x, xd = make(rng, rows, H, dtype, pad, offset)
+        gamma, gd = vector(rng, H, wdtype, 1.0, offset)
+        beta, bd = vector(rng, H, wdtype, 0.0, offset)
+        out, _ = make(rng, rows, H, dtype, pad, offset)
+        got = run_forward(x, gamma, beta, 1e-5, wdtype, y=out)
+        want, off = O.norm_forward(xd, gd, bd, 1e-5)
+        O.assert_within(host(got[0]), want[0], off[0], dtype, f"y of {rows} rows")
+        O.assert_within(host(got[1]), want[1], off[1], what="mean")
+        O.assert_within(host(got[2]), want[2], off[2], what="rstd")
+        if pad:
+            assert (out.as_strided((rows - 1, pad), (H + pad, 1), offset + H) == 77.0).all() if rows > 1 else True
+
+
+@pytest.mark.parametrize("dtype,wdtype", TYPES)
 @pytest.mark.parametrize("rows,H", SHAPES)
 def test_backward(rows, H, dtype, wdtype):
     rng = np.random.default_rng([rows, H, 2])
