@@ -111,6 +111,29 @@ def test_backward(rows, H, dtype, wdtype):
         O.assert_within(host(got[2]), want[2], off[2], what=f"dbeta P {P}")
 
 
+@pytest.mark.parametrize("dtype,wdtype", TYPES)
+@pytest.mark.parametrize("H", [2, 24, 32, 40, 57, 64, 72, 97, 128, 136, 201, 256])
+def test_backward_of_narrow_rows(H, dtype, wdtype):
+    """Rows that share a warp: processes that begin and end inside a round of rows, that have none, that write their messages themselves."""
+    rng = np.random.default_rng([H, 11])
+    for rows, P, k, ragged, pad, offset in ((1, 1, H, False, 0, 0), (333, 200, 7, True, 8, 8), (333, 111, 4, False, 1, 1), (20011, 5, 32, True, 0, 0), (9001, 3000, 8, True, 3, 2)):
+        x, xd = make(rng, rows, H, dtype, pad, offset)
+        dy, dyd = make(rng, rows, H, dtype, 2 * pad, offset, 0.3)
+        gamma, gd = vector(rng, H, wdtype, 1.0, offset)
+        _, mean, rstd = run_forward(x, gamma, None, 1e-5, wdtype)
+        splits = np.sort(rng.integers(0, rows + 1, P + 1)) if ragged else None       # some rows are nobody's
+        dx, _ = make(rng, rows, H, dtype, pad, offset)
+        got = run_backward(dy, x, gamma, mean, rstd, P, k, splits, wdtype, dx=dx)
+        want, off = O.norm_backward(dyd, xd, gd, host(mean), host(rstd), P, k, splits)
+        O.assert_within(host(got[0]), want[0], off[0], dtype, f"dx of {rows} rows")
+        O.assert_within(host(got[1]), want[1], off[1], what=f"dgamma of {rows} rows")
+        O.assert_within(host(got[2]), want[2], off[2], what=f"dbeta of {rows} rows")
+        if pad:
+            assert (dx.as_strided((rows - 1, pad), (H + pad, 1), offset + H) == 77.0).all()
+        alone = run_backward(dy, x, gamma, mean, rstd, P, k, splits, wdtype, weights=False)[0]
+        assert (alone == got[0]).all()
+
+
 @pytest.mark.parametrize("rows,H,P,k,splits", [
     (1000, 96, 64, 32, None), (700, 260, 1024, 4, None), (2000, 128, 3, 128, [0, 0, 2000, 2000]), (2000, 128, 4, 32, [100, 100, 900, 1500, 1900]),
     (900, 64, 3, 16, [0, 10, 5000, 6000]), (600, 1032, 600, 8, None), (5000, 40, 2, 64, [0, 1, 5000]), (64, 512, 8, 16, None), (1, 64, 2, 16, [0, 0, 1])])
