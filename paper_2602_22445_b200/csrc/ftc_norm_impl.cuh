@@ -1,7 +1,7 @@
 // Layer norm on rows that fit the registers of a thread block.
 //
-// A group of threads (a warp, or a block of up to 16 warps) holds a row, 16 elements a thread (rows of at most 512 bytes: one vector),
-// as packed pairs. A warp has one contiguous stretch of the row, vector i of lane l its vector 32 i + l: every load and store of a warp
+// A group of threads (a warp, or a block of up to 16 warps) holds a row, 16 elements a thread as packed pairs
+// (16-bit rows of 129 to 256 on 16 bytes: one vector; other rows of up to 256 share a warp, see the narrow rows). A warp has one contiguous stretch of the row, vector i of lane l its vector 32 i + l: every load and store of a warp
 // is one contiguous run, all at fixed offsets, and only the last warp may have vectors that do not exist. Statistics are taken in two
 // steps from the registers (mean, then squared distances), which no common offset of the row can spoil. A group walks many rows with
 // gamma, beta and the column sums in registers.
