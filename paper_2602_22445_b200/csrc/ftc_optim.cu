@@ -194,6 +194,8 @@ __device__ __forceinline__ float smallest(float a, float b, float c) {
 // own root was approximate and whose roundings may fall otherwise (v: 2^-23 + 2 * 2^-24), by 255 * 2^-22 < 6.1e-5.
 constexpr float kDoubtM = 2e-5f, kDoubtV = 6.5e-5f;
 __device__ __forceinline__ float fast_root(float x) { float r; asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+// The same where x may be a subnormal number (second moments of gradients below 1e-18).
+__device__ __forceinline__ float fast_root_of_any(float x) { float r; asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ F2 likely_roots(F2 x, float& far) {
     const F2 s = pair(fast_root(lo(x)), fast_root(hi(x))), c = add(add(s, twice(kWhole)), twice(-kWhole)), f = fma(c, twice(-1.f), s);
     far = largest(far, lo(f), hi(f));
@@ -292,16 +294,26 @@ __device__ __forceinline__ void adamw_block(const BlockIn& in, const AdamArgs& a
         g[i] = mul(g[i], sc);
         const F2 mi = add_apart(mul(m[i], twice(a.beta1)), mul(g[i], twice(a.rest1)), twice(a.one));
         const F2 vi = add_apart(mul(v[i], twice(a.beta2)), mul(mul(g[i], g[i]), twice(a.rest2)), twice(a.one));
-        root[i] = pair(fast_root(lo(vi)), fast_root(hi(vi)));
-        const F2 den = add(mul(root[i], twice(a.fix2)), twice(a.eps));
-        const F2 pi = fma(mul(mi, pair(fast_inverse(lo(den)), fast_inverse(hi(den)))), rate, mul(p[i], keep));
         if (BITS == 8 && some) {                                                // the block's codes need all; in 32 bits the live are stored
             const bool x = live >> (2 * i) & 1u, y = live >> (2 * i + 1) & 1u;
             m[i] = pair(x ? lo(mi) : lo(m[i]), y ? hi(mi) : hi(m[i]));
             v[i] = pair(x ? lo(vi) : lo(v[i]), y ? hi(vi) : hi(v[i]));
-            root[i] = pair(fast_root(lo(v[i])), fast_root(hi(v[i])));
         } else { m[i] = mi; v[i] = vi; }
-        p[i] = pi;
+        root[i] = BITS == 8 ? pair(fast_root(lo(v[i])), fast_root(hi(v[i]))) : pair(fast_root_of_any(lo(v[i])), fast_root_of_any(hi(v[i])));
+    }
+    if (BITS == 8) {                                                            // subnormal numbers among v, or zeros: the rest has done without
+        float least = lo(root[0]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) least = smallest(least, i ? lo(root[i]) : hi(root[0]), hi(root[i]));
+        if (!(least > 0.f)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) root[i] = pair(fast_root_of_any(lo(v[i])), fast_root_of_any(hi(v[i])));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const F2 den = add(mul(root[i], twice(a.fix2)), twice(a.eps));
+        p[i] = fma(mul(m[i], pair(fast_inverse(lo(den)), fast_inverse(hi(den)))), rate, mul(p[i], keep));
     }
     store_numbers<WIDE>(weights, pd, e0, lane, p, live);
     if (t.master) store_numbers<WIDE>(t.param, t.param_dtype, e0, lane, p, live);
