@@ -210,6 +210,16 @@ __device__ __noinline__ float nearest_root(float x, float most) {
     return fminf(fmaxf(c, 0.f), most);                               // at c = 0 the lower comparison says nothing
 }
 
+// The whole number below sqrt(x) or the one above, so that over many u from [0, 1) what they stand for is x on average (FOURTH: x^2, as
+// v goes with the fourth power of its code). x - c^2 is exact as above.
+template <bool FOURTH> __device__ __forceinline__ float dithered_root(float x, float u, float most) {
+    float c = floorf(fast_root(x)), d = __fmaf_rn(-c, c, x), w = c + c + 1.f;
+    if (d < 0.f) { c -= 1.f; w -= 2.f; d += w; }
+    else if (d >= w) { d -= w; c += 1.f; w += 2.f; }
+    const float s = c * c, step = FOURTH ? w * (s + s + w) : w;                // (c+1)^4 - c^4 = ((c+1)^2 - c^2) ((c+1)^2 + c^2)
+    return fminf((FOURTH ? d * (x + s) : d) > u * step ? c + 1.f : c, most);
+}
+
 // Largest of the warp's non-negative values, as bit patterns: infinities above all numbers, NaN above them.
 __device__ __forceinline__ float warp_max_bits(uint32_t v) { return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, v)); }
 
@@ -245,7 +255,7 @@ __device__ __forceinline__ void adamw_load(BlockIn& in, const AdamArgs& a, const
     }
 }
 
-template <int BITS, bool WIDE>
+template <int BITS, bool WIDE, bool DITHER>
 __device__ __forceinline__ void adamw_block(const BlockIn& in, const AdamArgs& a, const TableEntry& t, uint64_t b, uint32_t lane, uint64_t e0, uint32_t left, float scale) {
     const Raw &gr = in.gr, &pr = in.pr;
     Raw mr = in.mr, vr = in.vr;
@@ -338,14 +348,22 @@ __device__ __forceinline__ void adamw_block(const BlockIn& in, const AdamArgs& a
     float far_m = 0.f, far_v = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        c[i] = likely_roots(mul(pair(__fmul_rn(fabsf(lo(m[i])), mi), __fmul_rn(fabsf(hi(m[i])), mi)), twice(16129.f)), far_m);
-        d[i] = likely_roots(mul(mul(root[i], twice(vi)), twice(65025.f)), far_v);
+        const F2 xm = mul(pair(__fmul_rn(fabsf(lo(m[i])), mi), __fmul_rn(fabsf(hi(m[i])), mi)), twice(16129.f)), xv = mul(mul(root[i], twice(vi)), twice(65025.f));
+        if (DITHER) {
+            const uint32_t e = (uint32_t)q + at<WIDE>(lane, 2 * i), f = (uint32_t)q + at<WIDE>(lane, 2 * i + 1);
+            const float u = (float)((e * kDitherPlace + a.phase) >> 8) * 0x1p-24f, w = (float)((f * kDitherPlace + a.phase) >> 8) * 0x1p-24f;
+            c[i] = a.dither & kDitherM ? pair(dithered_root<false>(lo(xm), u, 127.f), dithered_root<false>(hi(xm), w, 127.f)) : likely_roots(xm, far_m);
+            d[i] = a.dither & kDitherV ? pair(dithered_root<true>(lo(xv), u, 255.f), dithered_root<true>(hi(xv), w, 255.f)) : likely_roots(xv, far_v);
+        } else {
+            c[i] = likely_roots(xm, far_m);
+            d[i] = likely_roots(xv, far_v);
+        }
     }
     if (!(far_m < 0.5f - kDoubtM && far_v < 0.5f - kDoubtV)) {                  // one lane in a thousand, and NaN
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            c[i] = pair(nearest_root(fabsf(lo(m[i])) * mi * 16129.f, 127.f), nearest_root(fabsf(hi(m[i])) * mi * 16129.f, 127.f));
-            d[i] = pair(nearest_root(__fsqrt_rn(lo(v[i])) * vi * 65025.f, 255.f), nearest_root(__fsqrt_rn(hi(v[i])) * vi * 65025.f, 255.f));
+            if (!DITHER || !(a.dither & kDitherM)) c[i] = pair(nearest_root(fabsf(lo(m[i])) * mi * 16129.f, 127.f), nearest_root(fabsf(hi(m[i])) * mi * 16129.f, 127.f));
+            if (!DITHER || !(a.dither & kDitherV)) d[i] = pair(nearest_root(__fsqrt_rn(lo(v[i])) * vi * 65025.f, 255.f), nearest_root(__fsqrt_rn(hi(v[i])) * vi * 65025.f, 255.f));
         }
     }
     float least = 255.f;
@@ -378,18 +396,18 @@ __device__ __forceinline__ void adamw_block(const BlockIn& in, const AdamArgs& a
     if (lane == 0) { a.m_scale[b] = ms; a.v_scale[b] = vs; }
 }
 
-template <int BITS, bool WIDE>
+template <int BITS, bool WIDE, bool DITHER>
 __device__ __forceinline__ void adamw_one(const AdamArgs& a, const TableEntry& t, uint64_t b, uint32_t lane, uint64_t e0, uint32_t left, float scale) {
     BlockIn in;
     adamw_load<BITS, WIDE>(in, a, t, b, lane, e0, left);
-    adamw_block<BITS, WIDE>(in, a, t, b, lane, e0, left, scale);
+    adamw_block<BITS, WIDE, DITHER>(in, a, t, b, lane, e0, left, scale);
 }
 
 // A warp takes one block; 32 warps an SM, no loop: the table's entry and the block's loads are the whole wait, and other warps fill it. 32-bit
 // states run at a copy's speed (101M elements, bf16 weights with a float32 copy, records: 455-470 us, 6.6 TB/s); states in 8 bits take
 // 77 instructions an element the narrow way (packed odd tensors, 17M elements: 70 us, 3.5 TB/s, 58 % of the issue slots), which bounds them.
 // WIDE: full blocks of aligned tensors go the wide way; else all go the narrow one.
-template <int BITS, bool WIDE>
+template <int BITS, bool WIDE, bool DITHER>
 __global__ void __launch_bounds__(kWarps * 32, 4) adamw_kernel(AdamArgs a) {
     const uint32_t lane = threadIdx.x & 31;
     const uint64_t b = blockIdx.x * (uint64_t)kWarps + (threadIdx.x >> 5);
@@ -398,15 +416,15 @@ __global__ void __launch_bounds__(kWarps * 32, 4) adamw_kernel(AdamArgs a) {
     const TableEntry t = table_entries(a.table)[table_map(a.table, a.n_params)[b]];
     if (!isfinite(scale)) return;
     const uint64_t e0 = (b - t.first_block) * FTC_STATE_BLOCK, left = t.n - e0;
-    if (WIDE && t.wide && left >= FTC_STATE_BLOCK) adamw_one<BITS, true>(a, t, b, lane, e0, FTC_STATE_BLOCK, scale);
-    else adamw_one<BITS, false>(a, t, b, lane, e0, left < FTC_STATE_BLOCK ? (uint32_t)left : FTC_STATE_BLOCK, scale);
+    if (WIDE && t.wide && left >= FTC_STATE_BLOCK) adamw_one<BITS, true, DITHER>(a, t, b, lane, e0, FTC_STATE_BLOCK, scale);
+    else adamw_one<BITS, false, DITHER>(a, t, b, lane, e0, left < FTC_STATE_BLOCK ? (uint32_t)left : FTC_STATE_BLOCK, scale);
 }
 
 // States in 8 bits, whose arithmetic (63 instructions an element) takes about as long as the memory: 201M elements in 606 us, 5.3 TB/s,
 // 64 % of the issue slots. Prefetch by way of shared memory at 24 or 32 warps an SM spilled and was slower (695, 820 us). A warp takes `span` blocks one after the other, the next one's
 // loads out while it works on the present one.
 constexpr uint32_t kWalkWarps = 8, kWalkBlocks = 2;
-__global__ void __launch_bounds__(kWalkWarps * 32, kWalkBlocks) adamw_walk_kernel(AdamArgs a, uint64_t span) {
+template <bool DITHER> __global__ void __launch_bounds__(kWalkWarps * 32, kWalkBlocks) adamw_walk_kernel(AdamArgs a, uint64_t span) {
     const uint32_t lane = threadIdx.x & 31;
     uint64_t b = (blockIdx.x * (uint64_t)kWalkWarps + (threadIdx.x >> 5)) * span;
     const uint64_t stop = b + span < a.n_blocks ? b + span : a.n_blocks;
@@ -423,11 +441,11 @@ __global__ void __launch_bounds__(kWalkWarps * 32, kWalkBlocks) adamw_walk_kerne
             for (; b < end_wide; ++b, e0 += FTC_STATE_BLOCK) {
                 const BlockIn in = next;
                 if (b + 1 < end_wide) adamw_load<8, true>(next, a, t, b + 1, lane, e0 + FTC_STATE_BLOCK, FTC_STATE_BLOCK);
-                adamw_block<8, true>(in, a, t, b, lane, e0, FTC_STATE_BLOCK, scale);
+                adamw_block<8, true, DITHER>(in, a, t, b, lane, e0, FTC_STATE_BLOCK, scale);
             }
         }
         for (; b < end; ++b, e0 += FTC_STATE_BLOCK)
-            adamw_one<8, false>(a, t, b, lane, e0, t.n - e0 < FTC_STATE_BLOCK ? (uint32_t)(t.n - e0) : FTC_STATE_BLOCK, scale);
+            adamw_one<8, false, DITHER>(a, t, b, lane, e0, t.n - e0 < FTC_STATE_BLOCK ? (uint32_t)(t.n - e0) : FTC_STATE_BLOCK, scale);
     }
 }
 
@@ -436,16 +454,16 @@ cudaError_t launch_adamw(const AdamArgs& a, int sms, cudaStream_t st) {
     // registers for it (packed odd tensors: 98 us against 82, both at 85 instructions an element).
     const uint64_t warps = (uint64_t)sms * kWalkWarps * kWalkBlocks;
     if (a.bits == 8 && a.mostly_wide && a.n_blocks >= warps * 4) {
-        adamw_walk_kernel<<<sms * kWalkBlocks, kWalkWarps * 32, 0, st>>>(a, (a.n_blocks + warps - 1) / warps);
+        (a.dither ? adamw_walk_kernel<true> : adamw_walk_kernel<false>)<<<sms * kWalkBlocks, kWalkWarps * 32, 0, st>>>(a, (a.n_blocks + warps - 1) / warps);
         return cudaGetLastError();
     }
     const uint32_t grid = (uint32_t)((a.n_blocks + kWarps - 1) / kWarps);
     if (a.bits == 32) {
-        if (a.mostly_wide) adamw_kernel<32, true><<<grid, kWarps * 32, 0, st>>>(a);
-        else adamw_kernel<32, false><<<grid, kWarps * 32, 0, st>>>(a);
+        (a.mostly_wide ? adamw_kernel<32, true, false> : adamw_kernel<32, false, false>)<<<grid, kWarps * 32, 0, st>>>(a);
+    } else if (a.dither) {
+        (a.mostly_wide ? adamw_kernel<8, true, true> : adamw_kernel<8, false, true>)<<<grid, kWarps * 32, 0, st>>>(a);
     } else {
-        if (a.mostly_wide) adamw_kernel<8, true><<<grid, kWarps * 32, 0, st>>>(a);
-        else adamw_kernel<8, false><<<grid, kWarps * 32, 0, st>>>(a);
+        (a.mostly_wide ? adamw_kernel<8, true, false> : adamw_kernel<8, false, false>)<<<grid, kWarps * 32, 0, st>>>(a);
     }
     return cudaGetLastError();
 }

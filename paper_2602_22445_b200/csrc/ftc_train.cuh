@@ -77,8 +77,11 @@ struct AdamArgs {
     const void* table; uint32_t n_params; uint64_t n_blocks;
     void *m, *v; float *m_scale, *v_scale; const float* grad_scale;
     float lr, beta1, beta2, rest1, rest2, eps, fix1, fix2, one;         // one = 1
-    uint32_t bits, mostly_wide;
+    uint32_t bits, mostly_wide, dither, phase;                          // phase: step * kDitherStep
 };
+// Codes rounded up or down by u = (place * kDitherPlace + step * kDitherStep) mod 2^32 / 2^32, with the fractions of sqrt(2) and of the golden
+// ratio: over the steps of an element, and over the elements of a step, u takes every part of [0, 1) evenly.
+constexpr uint32_t kDitherM = 1, kDitherV = 2, kDitherPlace = 0x6A09E667u, kDitherStep = 0x9E3779B9u;
 cudaError_t launch_adamw(const AdamArgs& a, int sm_count, cudaStream_t st);
 cudaError_t launch_adamw_states(uint64_t blocks, const void* m, const void* v, const float* ms, const float* vs, float* mo, float* vo, cudaStream_t st);
 uint32_t grad_norm_warps(uint64_t n_blocks, int sm_count);

@@ -57,3 +57,17 @@ def decode(m, v, ms, vs):
     c, d = m.astype(F).reshape(-1, BLOCK), v.astype(F).reshape(-1, BLOCK)
     r = d * d * (vs * (F(1) / F(65025)))[:, None]
     return (c * np.abs(c) * (ms * (F(1) / F(16129)))[:, None]).ravel(), (r * r).ravel()
+
+
+def dither(places, step):
+    """u of each place in the states' arrays."""
+    return (((places.astype(np.uint64) * 0x6A09E667 + step * 0x9E3779B9) & 0xFFFFFFFF) >> 8).astype(np.float64) * 2.0 ** -24
+
+
+def dithered_root(x, u, most, power):
+    """The whole number c with c^2 <= x < (c + 1)^2, or c + 1 where x lies more than u of the way from c to it, by what they stand for (the
+    codes' square, or with power 4 their fourth power)."""
+    x = x.astype(np.float64)
+    c = np.floor(np.sqrt(x))
+    part = (x ** (power / 2) - c ** power) / ((c + 1) ** power - c ** power)
+    return np.minimum(np.where(part > u, c + 1, c), most)
