@@ -190,9 +190,11 @@ __device__ __forceinline__ float smallest(float a, float b, float c) {
 
 // The whole numbers c nearest to sqrt(x), (c - 1/2)^2 <= x < (c + 1/2)^2, at most `most`, from an approximate root. The root and
 // x may be off by some units in the last place: `far` collects how far the root lies from its whole number, and where that comes
-// too near a half, c may be wrong. With a root good to 2^-23 and an exact x (m) the root is off by 127 * 2^-23 < 1.6e-5; with an x whose
-// own root was approximate and whose roundings may fall otherwise (v: 2^-23 + 2 * 2^-24), by 255 * 2^-22 < 6.1e-5.
-constexpr float kDoubtM = 2e-5f, kDoubtV = 6.5e-5f;
+// too near a half, c may be wrong. What counts is the distance from the exact root of the x that plain float32 gives. m has that x: the approximate
+// root, good to 2^-23, is off by 127 * 2^-23 < 1.6e-5. v has it from an approximate root and two products, where plain float32 rounds its root
+// and the same products: 2^-23 + 2^-24 and 4 * 2^-24 apart at most, half of which is left under the next root, which adds its own 2^-23:
+// 255 * 2.75 * 2^-23 < 8.4e-5.
+constexpr float kDoubtM = 2e-5f, kDoubtV = 9e-5f;
 __device__ __forceinline__ float fast_root(float x) { float r; asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 // The same where x may be a subnormal number (second moments of gradients below 1e-18).
 __device__ __forceinline__ float fast_root_of_any(float x) { float r; asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
@@ -359,12 +361,13 @@ __device__ __forceinline__ void adamw_block(const BlockIn& in, const AdamArgs& a
             d[i] = likely_roots(xv, far_v);
         }
     }
-    if (!(far_m < 0.5f - kDoubtM && far_v < 0.5f - kDoubtV)) {                  // one lane in a thousand, and NaN
+    if (!(far_m < 0.5f - kDoubtM)) {                                            // one lane in three thousand, and NaN
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (!DITHER || !(a.dither & kDitherM)) c[i] = pair(nearest_root(fabsf(lo(m[i])) * mi * 16129.f, 127.f), nearest_root(fabsf(hi(m[i])) * mi * 16129.f, 127.f));
-            if (!DITHER || !(a.dither & kDitherV)) d[i] = pair(nearest_root(__fsqrt_rn(lo(v[i])) * vi * 65025.f, 255.f), nearest_root(__fsqrt_rn(hi(v[i])) * vi * 65025.f, 255.f));
-        }
+        for (int i = 0; i < 4; ++i) c[i] = pair(nearest_root(fabsf(lo(m[i])) * mi * 16129.f, 127.f), nearest_root(fabsf(hi(m[i])) * mi * 16129.f, 127.f));
+    }
+    if (!(far_v < 0.5f - kDoubtV)) {                                            // one in seven hundred
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] = pair(nearest_root(__fsqrt_rn(lo(v[i])) * vi * 65025.f, 255.f), nearest_root(__fsqrt_rn(hi(v[i])) * vi * 65025.f, 255.f));
     }
     float least = 255.f;
 #pragma unroll

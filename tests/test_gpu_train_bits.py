@@ -1,4 +1,4 @@
-"""AdamW's states have the bits of the formula in plain float32, and weights move by it: subnormal second moments."""
+"""AdamW's states have the bits of the formula in plain float32, and weights move by it: subnormal second moments, codes beside a tie."""
 import numpy as np
 import pytest
 
@@ -68,3 +68,15 @@ def test_subnormal_and_normal_second_moments_in_one_block(bits):
     job = Run(0.01 * rng.standard_normal(n), bits)
     for step in (1, 2, 3):
         job.step(10.0 ** rng.uniform(-23, -15, n) * rng.choice([-1, 1], n), step, 1e-28)
+
+
+@pytest.mark.parametrize("blocks", [300, 24000])
+def test_codes_beside_a_tie(blocks):
+    """Gradients whose codes of v lie within some units in the last place of a half: the codes are those of plain float32."""
+    rng = np.random.default_rng(blocks)
+    top = 10.0 ** rng.uniform(-3, 1, (blocks, 1))
+    half = rng.integers(60, 255, (blocks, 256)) + 0.5
+    g = top * (half / 255) ** 2 * (1 + rng.uniform(-2e-6, 2e-6, (blocks, 256)))
+    g[:, 0] = top[:, 0]
+    job = Run(np.zeros(blocks * 256), 8)
+    job.step(g.ravel(), 1, 1e-8)
