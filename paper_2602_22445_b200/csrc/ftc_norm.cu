@@ -170,11 +170,11 @@ template <typename T, int VB>
 __global__ void __launch_bounds__(kThreads) norm_columns_kernel(NormArgs a) {
     constexpr int N = VB / (int)sizeof(T), AHEAD = 4;
     using V = Pack<T, VB>;
-    const uint32_t c = (blockIdx.x * kThreads + threadIdx.x) * N;
+    const uint32_t own = (blockIdx.x * kThreads + threadIdx.x) * N, c = own < a.H ? own : a.H - N;         // N divides H
     later_kernel_may_start();
     RowWalk walk(a, blockIdx.y);
-    walk.find();                                                     // by whole warps
-    if (c >= a.H) return;                                            // N divides H
+    walk.find();
+    if (__all_sync(0xFFFFFFFFu, own >= a.H)) return;                 // warps stay whole for the walk
     float dg[N] = {}, db[N] = {};
     for (uint32_t r = walk.r0; r < walk.r1; r += AHEAD) {                // r1 + AHEAD stays below 2^32
         V x[AHEAD], dy[AHEAD];
@@ -190,10 +190,10 @@ __global__ void __launch_bounds__(kThreads) norm_columns_kernel(NormArgs a) {
         for (int i = 0; i < AHEAD; ++i)
             if (r + i < walk.r1) {
                 if (walk.leaves(r + i)) {
-                    if (walk.any) store_slot<N>(a, walk.slot(), c, dg, db);
+                    if (walk.any && own < a.H) store_slot<N>(a, walk.slot(), c, dg, db);
+                    walk.go_to(r + i);
 #pragma unroll
                     for (int j = 0; j < N; ++j) dg[j] = db[j] = 0.f;
-                    walk.go_to(r + i);
                 }
                 if (walk.counts(r + i)) {
                     walk.any = true;
@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(kThreads) norm_columns_kernel(NormArgs a) {
                 }
             }
     }
-    if (walk.any) store_slot<N>(a, walk.slot(), c, dg, db);
+    if (walk.any && own < a.H) store_slot<N>(a, walk.slot(), c, dg, db);
 }
 
 // dgamma[s][p][e], dbeta[s][p][e] from the slots: Q warps add the slots of one process for C columns a lane, each every Q-th slot, and

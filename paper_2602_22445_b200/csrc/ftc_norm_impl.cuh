@@ -101,6 +101,17 @@ __device__ __forceinline__ uint32_t holder(const NormArgs& a, uint32_t r) {
     }
     return lo;
 }
+// The same where process p ends before row r and a million without rows may come before the one that holds it; for a whole warp. Lane l
+// looks 2^l processes ahead; what is left halves each time. (With the search above in its place the kernel for columns spilled.)
+__device__ __forceinline__ uint32_t later_holder(const NormArgs& a, uint32_t p, uint32_t r) {
+    if (!a.splits) return holder(a, r);
+    while (true) {
+        const uint32_t q = p + (1u << (threadIdx.x & 31u));           // P is at most 2^20: the last lanes are beyond it
+        const uint32_t hits = __ballot_sync(0xFFFFFFFFu, q >= a.P || a.splits[q + 1] > r);
+        if (hits & 1u) return p + 1;
+        p += 1u << (__ffs(hits) - 2);
+    }
+}
 
 // The rows of group b, and the process that holds the present one. A warp walks as one.
 struct RowWalk {
@@ -118,7 +129,12 @@ struct RowWalk {
         end = p < a.P ? first_row(a, p + 1) : ~0u;
     }
     __device__ __forceinline__ bool leaves(uint32_t r) const { return r >= end; }
-    __device__ __forceinline__ void go_to(uint32_t r) { while (r >= end) { ++p; bounds(); } any = false; }
+    __device__ __forceinline__ void go_to(uint32_t r) {              // for the whole warp; mostly to the next process
+        ++p;
+        bounds();
+        if (r >= end) { p = later_holder(a, p, r); bounds(); }
+        any = false;
+    }
     __device__ __forceinline__ bool counts(uint32_t r) const { return r >= start; }
     __device__ __forceinline__ uint64_t slot() const { return (uint64_t)b + p; }
 };
@@ -655,9 +671,9 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
         if (r + 1 < walk.r1) { nmean = a.mean[r + 1]; nrstd = a.rstd[r + 1]; }
         if (r >= weights_to) {
             if (walk.any) leave(false);
+            walk.go_to(r);
 #pragma unroll
             for (int j = 0; j < H2; ++j) dg[j] = db[j] = twice(0.f);
-            walk.go_to(r);
             weights_from = walk.start; weights_to = walk.end;
         }
         const bool counts = r >= weights_from;
@@ -753,9 +769,9 @@ template <typename T, typename W, bool VEC, int L> __global__ void __launch_boun
                 walk.any |= from < stop && to > base;
                 if (to >= stop) break;
                 if (walk.any) leave(false);
+                walk.go_to(to);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) dg[j] = db[j] = twice(0.f);
-                walk.go_to(to);
                 from = walk.start; to = walk.end;
             }
             if (!a.dx) continue;
