@@ -137,3 +137,21 @@ def test_weights_follow_those_of_32_bits():
             job.step(step, 0.9, 0.999)
     moved = [(job.param - b).view(8, 256)[:, :100].mean() for job, b in zip((small, big), begin)]
     assert 0.8 < float(moved[0] / moved[1]) < 1.25
+
+
+@pytest.mark.parametrize("beta2", [0.999, 0.99999, 1 - 2.0 ** -24])
+def test_float32_states_over_steps(beta2):
+    """States in 32 bits against the formula in 64: a step adds at most four half units (beta's rounding, two products, a sum) to what is off."""
+    import torch
+    rng = np.random.default_rng(5)
+    n, beta1, steps = 2560, 0.95, 60
+    job = Job(n, 32)
+    m, v = np.zeros(n), np.zeros(n)
+    for step in range(1, steps + 1):
+        g = np.clip(rng.standard_normal(n), -6, 6).astype(F)
+        job.grad.copy_(torch.from_numpy(g))
+        job.step(step, beta1, beta2)
+        m, v = m * beta1 + (1 - beta1) * g.astype(np.float64), v * beta2 + (1 - beta2) * g.astype(np.float64) ** 2
+    got = [t.double().cpu().numpy() for t in job.state]
+    assert (np.abs(got[1] - v) <= 2.0 ** -24 * 4 * (steps + 4) * v).all()
+    assert (np.abs(got[0] - m) <= 2.0 ** -24 * 4 * (steps + 4) * 6).all()        # no gradient is larger than 6

@@ -115,6 +115,21 @@ def test_calls_on_tables_refused():
     assert lib.ftc_adamw_states(1, FAKE, FAKE, FAKE, FAKE, FAKE + 4, FAKE, None) == B.FTC_EINVAL
 
 
+@pytest.mark.parametrize("name", ["beta1", "beta2"])
+@pytest.mark.parametrize("bits", [8, 32])
+def test_betas_that_are_one_in_float32_refused(name, bits):
+    """A state would grow without ever decaying."""
+    _, rc, buf = build(entry())
+    assert rc == B.FTC_OK
+    for beta in (1 - 1e-8, 1 - 2.0 ** -26, np.nextafter(1, 0), 1.0, float("nan")):
+        a = dict(lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, step=1, state_bits=bits, reserved=0) | {name: beta}
+        assert B.load().ftc_adamw_step(C.byref(B.ftc_adamw_t(**a)), buf.ctypes.data, FAKE, FAKE, FAKE, FAKE, FAKE, None, None) == B.FTC_EINVAL, beta
+    _, rc, buf = build(entry(n=0, param=None, grad=None))
+    for beta in (1 - 2.0 ** -24, 0.99999, 0.0):
+        a = dict(lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, step=1, state_bits=bits, reserved=0) | {name: beta}
+        assert B.load().ftc_adamw_step(C.byref(B.ftc_adamw_t(**a)), buf.ctypes.data, FAKE, FAKE, FAKE, FAKE, FAKE, None, None) == B.FTC_OK, beta
+
+
 def test_definitions():
     """The 64-bit gradients against central differences, and the messages' layout."""
     rng = np.random.default_rng(0)
