@@ -435,7 +435,7 @@ FTC_API size_t ftc_grad_norm_workspace_bytes(const void* h_table);
 
 /* One AdamW step (decoupled weight decay). */
 typedef struct {
-    double lr, beta1, beta2, eps;   /* lr >= 0 finite, 0 <= beta < 1 (also as float32: beta is at most 1 - 2^-24), eps >= 1e-30. A beta near 1 and its
+    double lr, beta1, beta2, eps;   /* lr >= 0 finite (also as float32), 0 <= beta < 1 (also as float32: beta is at most 1 - 2^-24), eps >= 1e-30. A beta near 1 and its
                                        state in float32 leave the state within about 1e-7 / (1 - beta) of itself: 0.01 % at 0.999, 1 % at 0.99999 */
     uint64_t step;                  /* 1 for the first step (bias corrections 1 - beta^step) */
     uint32_t state_bits;            /* 32 or 8 */

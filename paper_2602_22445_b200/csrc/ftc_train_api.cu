@@ -173,7 +173,7 @@ int ftc_adamw_step(const ftc_adamw_t* hyper, const void* h_table, const void* d_
                    float* d_v_scale, const float* d_grad_scale, void* cuda_stream) {
     const TableHead* h = head_of(h_table);
     if (!hyper || !h || !d_table || !aligned(d_table, 256) || hyper->reserved || (h->flags & 1u)) return FTC_EINVAL;
-    if (!(hyper->lr >= 0) || !std::isfinite(hyper->lr) || !(hyper->beta1 >= 0 && (float)hyper->beta1 < 1.f) || !(hyper->beta2 >= 0 && (float)hyper->beta2 < 1.f) ||
+    if (!(hyper->lr >= 0) || !std::isfinite((float)hyper->lr) || !(hyper->beta1 >= 0 && (float)hyper->beta1 < 1.f) || !(hyper->beta2 >= 0 && (float)hyper->beta2 < 1.f) ||
         !(hyper->eps >= 1e-30) || !std::isfinite((float)hyper->eps) || hyper->step == 0) return FTC_EINVAL;
     if (hyper->state_bits != 32 && hyper->state_bits != 8) return FTC_EUNSUPPORTED;
     if (h->n_blocks == 0) return FTC_OK;

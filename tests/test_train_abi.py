@@ -130,6 +130,14 @@ def test_betas_that_are_one_in_float32_refused(name, bits):
         assert B.load().ftc_adamw_step(C.byref(B.ftc_adamw_t(**a)), buf.ctypes.data, FAKE, FAKE, FAKE, FAKE, FAKE, None, None) == B.FTC_OK, beta
 
 
+def test_learning_rates_beyond_float32_refused():
+    """An infinite rate times a weight decay of zero would make every weight NaN."""
+    for n, lr, want in ((300, 1e39, B.FTC_EINVAL), (300, 3.5e38, B.FTC_EINVAL), (0, 3.4e38, B.FTC_OK)):
+        buf = build(entry(n=n))[2]
+        hyper = B.ftc_adamw_t(lr, 0.9, 0.99, 1e-8, 1, 32, 0)
+        assert B.load().ftc_adamw_step(C.byref(hyper), buf.ctypes.data, FAKE, FAKE, FAKE, None, None, None, None) == want, lr
+
+
 def test_definitions():
     """The 64-bit gradients against central differences, and the messages' layout."""
     rng = np.random.default_rng(0)
