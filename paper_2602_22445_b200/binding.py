@@ -518,8 +518,9 @@ def _states(table, d_m, d_v, d_m_scale, d_v_scale):
 
 def ftc_adamw_step(hyper, table, d_m, d_v, d_m_scale=None, d_v_scale=None, d_grad_scale=None, stream=None, check=True) -> int:
     bits, states = _states(table, d_m, d_v, d_m_scale, d_v_scale)
-    hyper = ftc_adamw_t.from_buffer_copy(hyper)       # the caller's may be in use by another thread, over states of other bits
-    hyper.state_bits = bits
+    if hyper.state_bits != bits:                      # never the caller's own: another thread may use it over states of other bits
+        hyper = ftc_adamw_t.from_buffer_copy(hyper)
+        hyper.state_bits = bits
     rc = (_lib or load()).ftc_adamw_step(hyper, table.h_ptr, table.d_ptr, *states, _vector_ptr(d_grad_scale, "d_grad_scale", 1),
                                _stream(stream))
     if check and rc != FTC_OK:
