@@ -455,7 +455,7 @@ typedef struct {
  * signed, and stands for c*|c|*s/127^2. v is held through its root r = sqrt(v): s = max r, c nearest to 255*sqrt(r/s) and at
  * least 1 where r > 0; it stands for (c^2*s/255^2)^2. A state whose beta exceeds 31/32 changes too little in a step for the nearest code to follow:
  * its code is the one below or the one above, the upper one where what the state stands for lies more than u of the way from the lower
- * code's value to the upper's, with u = (e*0x6A09E667 + step*0x9E3779B9) mod 2^32 / 2^32 (its upper 24 bits) for element e of d_m and d_v. Over the
+ * code's value to the upper's, with u = (e*0x6A09E667 + step*0x9E3779B9) mod 2^32 / 2^32 (its upper 23 bits) for element e of d_m and d_v. Over the
  * steps u is spread evenly, so the states' mean is kept; it spreads around the 32-bit state by some tenths of its root. With beta up
  * to 31/32, codes are the nearest ones, and a state whose gradients vanish falls no further than about code 2/(1-beta2) of 255 (v; 40 at 0.95: 2.5 % of
  * the block's largest root) and 1/(1-beta1) of 127 (m). The update itself uses the new m and v before they are rounded. A block of which no

@@ -212,15 +212,18 @@ __device__ __noinline__ float nearest_root(float x, float most) {
     return fminf(fmaxf(c, 0.f), most);                               // at c = 0 the lower comparison says nothing
 }
 
-// The whole number below sqrt(x) or the one above, so that over many u from [0, 1) what they stand for is x on average (FOURTH: x^2, as
-// v goes with the fourth power of its code). x - c^2 is exact as above.
-template <bool FOURTH> __device__ __forceinline__ float dithered_root(float x, float u, float most) {
-    float c = floorf(fast_root(x)), d = __fmaf_rn(-c, c, x), w = c + c + 1.f;
-    if (d < 0.f) { c -= 1.f; w -= 2.f; d += w; }
-    else if (d >= w) { d -= w; c += 1.f; w += 2.f; }
-    const float s = c * c, step = FOURTH ? w * (s + s + w) : w;                // (c+1)^4 - c^4 = ((c+1)^2 - c^2) ((c+1)^2 + c^2)
-    return fminf((FOURTH ? d * (x + s) : d) > u * step ? c + 1.f : c, most);
+// The whole number c below sqrt(x) or the one above, so that over many u from [0, 1) what they stand for is x on average (FOURTH: x^2, as
+// v goes with the fourth power of its code): c + 1 where x lies more than u of the way. less_u: -u. A root beside a whole number may give the c
+// below it, or the one above: the way is then a little over 1, or under 0, and the code that number all the same.
+template <bool FOURTH> __device__ __forceinline__ F2 dithered_roots(F2 x, F2 less_u, float most) {
+    const F2 r = pair(fast_root(lo(x)), fast_root(hi(x))), c = add(add(add(r, twice(-0.5f)), twice(kWhole)), twice(-kWhole));
+    const F2 s = mul(c, c), d = fma(s, twice(-1.f), x), w = fma(c, twice(2.f), twice(1.f));             // s exact, w = (c+1)^2 - c^2
+    const F2 more = FOURTH ? fma(less_u, mul(w, fma(s, twice(2.f), w)), mul(d, add(x, s))) : fma(less_u, w, d);   // (c+1)^4 - c^4 = w ((c+1)^2 + c^2)
+    const F2 q = add(c, pair(one_above(lo(more)), one_above(hi(more))));
+    return pair(fminf(lo(q), most), fminf(hi(q), most));
 }
+// -u of place e.
+__device__ __forceinline__ float dither(uint32_t e, uint32_t phase) { return 1.f - __uint_as_float((e * kDitherPlace + phase) >> 9 | 0x3F800000u); }
 
 // Largest of the warp's non-negative values, as bit patterns: infinities above all numbers, NaN above them.
 __device__ __forceinline__ float warp_max_bits(uint32_t v) { return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, v)); }
@@ -352,10 +355,9 @@ __device__ __forceinline__ void adamw_block(const BlockIn& in, const AdamArgs& a
     for (int i = 0; i < 4; ++i) {
         const F2 xm = mul(pair(__fmul_rn(fabsf(lo(m[i])), mi), __fmul_rn(fabsf(hi(m[i])), mi)), twice(16129.f)), xv = mul(mul(root[i], twice(vi)), twice(65025.f));
         if (DITHER) {
-            const uint32_t e = (uint32_t)q + at<WIDE>(lane, 2 * i), f = (uint32_t)q + at<WIDE>(lane, 2 * i + 1);
-            const float u = (float)((e * kDitherPlace + a.phase) >> 8) * 0x1p-24f, w = (float)((f * kDitherPlace + a.phase) >> 8) * 0x1p-24f;
-            c[i] = a.dither & kDitherM ? pair(dithered_root<false>(lo(xm), u, 127.f), dithered_root<false>(hi(xm), w, 127.f)) : likely_roots(xm, far_m);
-            d[i] = a.dither & kDitherV ? pair(dithered_root<true>(lo(xv), u, 255.f), dithered_root<true>(hi(xv), w, 255.f)) : likely_roots(xv, far_v);
+            const F2 u = pair(dither((uint32_t)q + at<WIDE>(lane, 2 * i), a.phase), dither((uint32_t)q + at<WIDE>(lane, 2 * i + 1), a.phase));
+            c[i] = a.dither & kDitherM ? dithered_roots<false>(xm, u, 127.f) : likely_roots(xm, far_m);
+            d[i] = a.dither & kDitherV ? dithered_roots<true>(xv, u, 255.f) : likely_roots(xv, far_v);
         } else {
             c[i] = likely_roots(xm, far_m);
             d[i] = likely_roots(xv, far_v);

@@ -61,7 +61,7 @@ def decode(m, v, ms, vs):
 
 def dither(places, step):
     """u of each place in the states' arrays."""
-    return (((places.astype(np.uint64) * 0x6A09E667 + step * 0x9E3779B9) & 0xFFFFFFFF) >> 8).astype(np.float64) * 2.0 ** -24
+    return (((places.astype(np.uint64) * 0x6A09E667 + step * 0x9E3779B9) & 0xFFFFFFFF) >> 9).astype(np.float64) * 2.0 ** -23
 
 
 def dithered_root(x, u, most, power):
