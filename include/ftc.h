@@ -399,7 +399,7 @@ typedef struct {
                                    [ceil(n/k)][k] of which the first n elements count */
     const uint32_t* status;     /* [ceil(n/k)][FTC_STATUS_WORDS]: the status records of those messages, 16-byte aligned. The gradient
                                    is the sum divided by the processes included in it; a message with another outcome than FTC_ST_OK
-                                   (or nobody included) was not delivered: its elements keep their weights and states and count
+                                   (or nobody included) was not delivered: its elements keep their weights and 32-bit states and count
                                    nothing in the norm. NULL: the gradient is taken as it is */
     uint64_t n;                 /* elements, 0 .. 2^40 */
     uint32_t k;                 /* elements of a message, 1 .. 2^30; read only with status */
@@ -427,7 +427,8 @@ FTC_API uint64_t ftc_param_table_blocks(const void* h_table);
  *            not finite (which makes ftc_adamw_step do nothing)
  *   d_norms  [n_params] float32: each tensor's norm, or NULL
  *   d_workspace  ftc_grad_norm_workspace_bytes(h_table) bytes, 16-byte aligned; as for ftc_layernorm_backward
- * Squares are added up in float64. max_norm > 0 (infinity: no clipping).
+ * Squares of eight elements are added in float32 (in float64 where that would overflow or lose small ones), their sums in float64.
+ * max_norm > 0 (infinity: no clipping).
  */
 FTC_API int ftc_grad_norm(const void* h_table, const void* d_table, float max_norm, float* d_norm, float* d_norms,
                           void* d_workspace, size_t workspace_bytes, void* cuda_stream);
@@ -435,31 +436,36 @@ FTC_API size_t ftc_grad_norm_workspace_bytes(const void* h_table);
 
 /* One AdamW step (decoupled weight decay). */
 typedef struct {
-    double lr, beta1, beta2, eps;   /* lr >= 0 finite (also as float32), 0 <= beta < 1 (also as float32: beta is at most 1 - 2^-24), eps >= 1e-30. A beta near 1 and its
-                                       state in float32 leave the state within about 1e-7 / (1 - beta) of itself: 0.01 % at 0.999, 1 % at 0.99999 */
-    uint64_t step;                  /* 1 for the first step (bias corrections 1 - beta^step) */
+    double lr, beta1, beta2, eps;   /* lr >= 0, 0 <= beta < 1, eps >= 1e-30; lr finite and the betas below 1 as float32 too. A beta near
+                                       1 and its state in float32 leave the state within about 1e-7 / (1 - beta) of itself: 0.01 %
+                                       at 0.999, 1 % at 0.99999 */
+    uint64_t step;                  /* 1 for the first step (bias corrections 1 - beta^step). lr and step are numbers of the call: a captured
+                                       graph replays those that it was captured with */
     uint32_t state_bits;            /* 32 or 8 */
     uint32_t reserved;              /* 0 */
 } ftc_adamw_t;
 
 /*
- * For every element, in float32 with each operation rounded (no fused multiply-add), c1 = 1/(1-beta1^step), c2 = 1/sqrt(1-beta2^step),
- * l = lr * lr_scale:
+ * For every element, in float32, with c1 = 1/(1-beta1^step), c2 = 1/sqrt(1-beta2^step), l = lr * lr_scale:
  *   g = grad * (1 / included) * *d_grad_scale;  m = m*beta1 + g*(1-beta1);  v = v*beta2 + (g*g)*(1-beta2)
  *   p = p * (1 - l*weight_decay) - (m / (sqrt(v)*c2 + eps)) * (l*c1)
+ * Each operation of g, m and v is rounded (no fused multiply-add). The move of p has an approximate root and quotient (2^-23 each) and ends in a
+ * multiply-add: it is good to 16 half units in its last place.
  *   d_m, d_v  states of ftc_param_table_blocks() blocks of FTC_STATE_BLOCK elements: float32, or with state_bits = 8 int8 and
  *             uint8; zero bytes before the first step; 32-byte aligned
- *   d_m_scale, d_v_scale  float32, one for each block (state_bits = 8; else NULL)
+ *   d_m_scale, d_v_scale  float32, one for each block (state_bits = 8; else NULL); zeros before the first step
  *   d_grad_scale  one float32 (d_norm + 1 of ftc_grad_norm), or NULL for 1; where it is not finite the call changes nothing
  * States in 8 bits: with s = max |m| of the block (at least 2^-126), m is held as the whole number c nearest to 127*sqrt(|m|/s),
  * signed, and stands for c*|c|*s/127^2. v is held through its root r = sqrt(v): s = max r, c nearest to 255*sqrt(r/s) and at
- * least 1 where r > 0; it stands for (c^2*s/255^2)^2. A state whose beta exceeds 31/32 changes too little in a step for the nearest code to follow:
- * its code is the one below or the one above, the upper one where what the state stands for lies more than u of the way from the lower
- * code's value to the upper's, with u = (e*0x6A09E667 + step*0x9E3779B9) mod 2^32 / 2^32 (its upper 23 bits) for element e of d_m and d_v. Over the
- * steps u is spread evenly, so the states' mean is kept; it spreads around the 32-bit state by some tenths of its root. With beta up
- * to 31/32, codes are the nearest ones, and a state whose gradients vanish falls no further than about code 2/(1-beta2) of 255 (v; 40 at 0.95: 2.5 % of
- * the block's largest root) and 1/(1-beta1) of 127 (m). The update itself uses the new m and v before they are rounded. A block of which no
- * element's message was delivered stays as it is; a block that meets NaN or an infinity stands for NaN afterwards.
+ * least 1 where r > 0; it stands for (c^2*s/255^2)^2. A state whose beta exceeds 31/32 changes too little in a step for the nearest code
+ * to follow: its code is the one below or the one above, the upper one where what the state stands for lies more than u of the way
+ * from the lower code's value to the upper's, with u = (e*0x6A09E667 + step*0x9E3779B9) mod 2^32 / 2^32 (its upper 23 bits) for
+ * element e of d_m and d_v. Over the steps u is spread evenly, so the states' mean is kept, while single ones spread around the 32-bit
+ * state (v's root by a tenth or two). Steps have to be numbered one after the other for that. With a beta up to 31/32 codes are the
+ * nearest ones, and a state whose gradients vanish falls no further than about code 2/(1-beta2) of 255 (v; 40 at 0.95, 2.5 % of the
+ * block's largest root) and 1/(1-beta1) of 127 (m; 10 at 0.9, 0.6 % of the largest). The update itself uses the new m and v before they
+ * are rounded. A block of which no element's message was delivered stays as it is; in a block of which some were, the others' m and v are
+ * rounded again under the block's new scales. A block whose m or v meets NaN or an infinity has NaN in its place afterwards.
  * param must not be NULL for tensors with n > 0 (FTC_EINVAL).
  */
 FTC_API int ftc_adamw_step(const ftc_adamw_t* hyper, const void* h_table, const void* d_table, void* d_m, void* d_v,

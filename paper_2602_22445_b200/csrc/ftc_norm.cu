@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(kThreads) norm_forward_long_kernel(NormArgs a)
 }
 
 // dx alone, for H > 8192 (f16, 6534 rows of 13256 over 955 processes: columns 78 us, dx 111, messages 46; one kernel for columns and dx
-// would save reading 346 MB again, but no block holds the column sums of such a row). KEEP: the row stays in registers, four vectors a thread, as loaded; else a block walks it twice, the second time from the
+// would save reading 346 MB again. No block holds the column sums of such a row; a cluster of blocks that exchange a row's two sums would). KEEP: the row stays in registers, four vectors a thread, as loaded; else a block walks it twice, the second time from the
 // caches.
 template <typename T, typename W, int VB, bool KEEP>
 __global__ void __launch_bounds__(1024) norm_backward_long_kernel(NormArgs a) {
@@ -310,8 +310,10 @@ cudaError_t launch_norm_forward(const NormArgs& a, int sms, cudaStream_t st) {
 
 // One group for each process, which writes its messages itself (no partial sums, no second kernel): for even shares on rows that fit a
 // group, where a process has few rows (bf16, H = 2048, 64 processes of 4 rows: 9.6 us a call against 12.0), or not many and the processes
-// alone come near what the GPU runs at once (H = 1024, 1024 processes of 16 rows: 21 us against 31). With long walks the last
-// round of groups would leave the GPU half empty (H = 4096, 300 processes of 64 rows: 118 us against 87).
+// alone come near what the GPU runs at once (H = 1024, 1024 processes of 16 rows: 21 us against 29). With long walks the last
+// round of groups would leave the GPU half empty (H = 4096, 300 processes of 64 rows: 118 us against 87). Around the borders, us on the GPU, bf16, this
+// against slots: H = 1024, 64 processes of 4, 8, 12, 16, 24 rows: 4.1, 6.1, 7.9, 9.7, 13.5 against 5.1, 6.4, 9.6, 10.1, 10.3 (a call's two launches add
+// two to five more); H = 4096: 5.8, 8.3, 11.0, 13.5 against 8.4, 9.1, 10.0, 11.0; 256 processes: 7.9, 11.6, 15.4, 21.0, 29.6 against 16.6, 20.4, 24.5, 29.8, 39.1.
 uint32_t norm_backward_direct(const NormArgs& a, int sms) {
     if (a.splits || !(a.dgamma || a.dbeta) || !a.rows || a.H > 16 * kMaxGroup) return 0;
     const uint32_t g = group_threads(a.H), per_sm = g < 512 ? 512 / g : 1;

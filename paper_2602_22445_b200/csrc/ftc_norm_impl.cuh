@@ -412,7 +412,7 @@ template <typename T, typename W, int MODE, int NV> __device__ __forceinline__ v
 // how little of it a row would fill (bf16, 262144 rows of 64: 14.4 us against 61.5 with a warp for each row, 4.7 TB/s; 65536 rows of 97 that
 // begin between words: 16.3 against 37.5). No ring: a warp has ROUNDS such rounds of rows under way in registers, 24 warps an SM (32 with 64
 // registers: bf16 rows of 64 16.4, of 128 32.0 against 28.8). VEC: neighbours in vectors of 16 bytes; else single elements L apart, for rows that begin
-// anywhere. Bound by instructions below 128 columns (the two sums' exchanges), by memory above.
+// anywhere. Bound by instructions below 128 columns (the two sums' exchanges); at 128 the bytes take 0.72 of the time.
 constexpr uint32_t kNarrow = 256, kNarrowWarps = 8, kNarrowBlocks = 3;
 
 template <typename T, bool VEC, int L> struct NarrowPart {
@@ -610,7 +610,7 @@ __global__ void __launch_bounds__(MAXT, 768 / MAXT) norm_forward_kernel(NormArgs
 
 // blockDim = (G, groups in the block); a group of threads walks the rows of one RowWalk. The weight gradients cost no traffic of
 // their own beyond the slots, but 48 registers: 16 warps an SM, each of which waits for a row's chain (ring, two sums over the group, row)
-// half of the time. bf16, 32768 rows of 4096 over 64 processes: 138-144 us with the messages, 5.7 TB/s, 0.87 of a copy; 8191 rows of 2050
+// half of the time. bf16, 32768 rows of 4096 over 64 processes: 135-140 us with the messages, 5.8-6.0 TB/s, 0.88-0.91 of a copy; 8191 rows of 2050
 // over ragged processes: 40 us, of which 10 are beginnings and ends (the holder of the first row, the last slot, the second kernel).
 template <typename T, typename W, int MODE, bool ALL, int NV, int D>
 __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
@@ -708,7 +708,7 @@ __global__ void __launch_bounds__(kMaxGroup) norm_backward_kernel(NormArgs a) {
 
 // Narrow rows (see the forward pass). blockDim = (32, 4); a warp walks the rows of one RowWalk, 32 / L at a time: the lanes of a row that the
 // present process does not hold leave the sums alone, and before the sums are left they are added over the warp's rows. bf16, 262144 rows
-// of 64 over 64 processes: 26.7 us (3.9 TB/s) against 107 with a warp for each row; 65536 of 97 that begin between words: 20.5 against 57.
+// of 64 over 64 processes: 26.7 us (3.9 TB/s) against 107 with a warp for each row; 65536 of 97 that begin between words: 20.5 (24.8 over ragged processes) against 57.
 template <typename T, typename W, bool VEC, int L> __global__ void __launch_bounds__(128, 4) norm_backward_narrow_kernel(NormArgs a) {
     using P = NarrowPart<T, VEC, L>;
     constexpr int U = P::ROUNDS;

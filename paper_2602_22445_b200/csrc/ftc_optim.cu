@@ -410,7 +410,7 @@ __device__ __forceinline__ void adamw_one(const AdamArgs& a, const TableEntry& t
 
 // A warp takes one block; 32 warps an SM, no loop: the table's entry and the block's loads are the whole wait, and other warps fill it. 32-bit
 // states run at a copy's speed (101M elements, bf16 weights with a float32 copy, records: 455-470 us, 6.6 TB/s); states in 8 bits take
-// 77 instructions an element the narrow way (packed odd tensors, 17M elements: 70 us, 3.5 TB/s, 58 % of the issue slots), which bounds them.
+// 79 instructions an element the narrow way (packed odd tensors, 17M elements: 68 us, 3.6 TB/s, 61 % of the issue slots), which bounds them.
 // WIDE: full blocks of aligned tensors go the wide way; else all go the narrow one.
 template <int BITS, bool WIDE, bool DITHER>
 __global__ void __launch_bounds__(kWarps * 32, 4) adamw_kernel(AdamArgs a) {
@@ -425,9 +425,10 @@ __global__ void __launch_bounds__(kWarps * 32, 4) adamw_kernel(AdamArgs a) {
     else adamw_one<BITS, false, DITHER>(a, t, b, lane, e0, left < FTC_STATE_BLOCK ? (uint32_t)left : FTC_STATE_BLOCK, scale);
 }
 
-// States in 8 bits, whose arithmetic (63 instructions an element) takes about as long as the memory: 201M elements in 606 us, 5.3 TB/s,
-// 64 % of the issue slots. Prefetch by way of shared memory at 24 or 32 warps an SM spilled and was slower (695, 820 us). A warp takes `span` blocks one after the other, the next one's
-// loads out while it works on the present one.
+// States in 8 bits, whose arithmetic (63 instructions an element, 74 where v is dithered) takes about as long as the memory: 201M elements in 563 to
+// 635 us, 5.1 to 5.7 TB/s, 64 % of the issue slots; a quarter of them 151 us, dithered 168. Prefetch by way of shared memory at 24 or 32 warps an SM
+// spilled and was slower (695, 820 us when the walk took 606). A warp takes `span` blocks one after the other, the next one's loads out while it works
+// on the present one.
 constexpr uint32_t kWalkWarps = 8, kWalkBlocks = 2;
 template <bool DITHER> __global__ void __launch_bounds__(kWalkWarps * 32, kWalkBlocks) adamw_walk_kernel(AdamArgs a, uint64_t span) {
     const uint32_t lane = threadIdx.x & 31;
@@ -455,8 +456,9 @@ template <bool DITHER> __global__ void __launch_bounds__(kWalkWarps * 32, kWalkB
 }
 
 cudaError_t launch_adamw(const AdamArgs& a, int sms, cudaStream_t st) {
-    // The walk pays from four blocks a warp on (24 layers, 201M elements: 606 us against 725); the narrow way has too much in
-    // registers for it (packed odd tensors: 98 us against 82, both at 85 instructions an element).
+    // The walk pays from about twelve blocks a warp on, where the tensors no longer lie in L2: blocks a warp 4, 8, 16, 29, 331: 8.8, 15.5, 28.6, 53, 563 us
+    // against 8.0, 14.1, 31.0, 55, 614 a block for each warp. The narrow way has too much in registers for it (packed tensors, 4 to 29 blocks a warp:
+    // 13.6 to 81 us against 11.1 to 69).
     const uint64_t warps = (uint64_t)sms * kWalkWarps * kWalkBlocks;
     if (a.bits == 8 && a.mostly_wide && a.n_blocks >= warps * 4) {
         (a.dither ? adamw_walk_kernel<true> : adamw_walk_kernel<false>)<<<sms * kWalkBlocks, kWalkWarps * 32, 0, st>>>(a, (a.n_blocks + warps - 1) / warps);
@@ -674,7 +676,9 @@ __device__ __forceinline__ void give_norm(double s, float max_norm, float* norm)
     norm[1] = !isfinite(r) ? __uint_as_float(0x7FC00000u) : r > max_norm ? max_norm / r : 1.f;
 }
 
-// Tables of few blocks and tensors: all in one thread block, entries and sums in shared memory (132 blocks of 6 tensors: 6.6 us a call, as long as its checks and launch take, against 8.2 by way of the workspace).
+// Tables of few blocks and tensors: all in one thread block, entries and sums in shared memory. One against two kernels by way of the workspace, us on the
+// GPU, 6 tensors in float32 of 64, 132, 160, 320, 640 blocks: 4.1, 5.1, 5.3, 6.1, 7.5 against 5.8, 6.0, 5.8, 5.8, 5.6; with records of 32
+// elements 4.6, 6.2, 6.5, 7.9, 10.3 against 6.2, 5.4, 6.3, 5.9, 6.4. A call among others takes 6.2 us up to about 130 blocks, 8.2 with unaligned tensors or more.
 constexpr uint32_t kSoloWarps = 32, kSoloBlocks = 160, kSoloTensors = 16;
 template <bool MIXED> __global__ void __launch_bounds__(kSoloWarps * 32) grad_norm_solo_kernel(const void* table, uint32_t n_params, uint64_t n_blocks, uint64_t span, float max_norm,
                                                                          float* norm, float* norms) {
