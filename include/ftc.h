@@ -476,6 +476,126 @@ FTC_API int ftc_adamw_step(const ftc_adamw_t* hyper, const void* h_table, const 
 FTC_API int ftc_adamw_states(uint64_t blocks, const void* d_m, const void* d_v, const float* d_m_scale, const float* d_v_scale,
                              float* d_m_out, float* d_v_out, void* cuda_stream);
 
+/*
+ * The two ends of a language model, and the update of its matrices. As above: float32 arithmetic whatever the element types, sums in a
+ * fixed order, status records read as the allreduce leaves them.
+ *
+ * Embedding lookup: rows of a table of V rows of H elements.
+ */
+typedef struct {
+    uint32_t V;          /* rows of the table, 1 .. 2^30 */
+    uint32_t H;          /* elements of a row, 1 .. 2^24; V * H at most 2^40 */
+    uint32_t P;          /* processes the tokens are divided over (backward), 1 .. 2^20 */
+    uint32_t k;          /* elements of a message (backward), 1 .. 2^24: the gradient is [ceil(V*H/k)][P][k]; with P = 1 that is [V][H] (and
+                            the last message's fill) whatever k; (V * H + k) * P at most 2^40 */
+    uint32_t dtype;      /* y, dy: FTC_F32, FTC_BF16 or FTC_F16 */
+    uint32_t wdtype;     /* the table: FTC_F32 or dtype */
+    uint32_t token_bits; /* tokens are int64 or int32: 64 or 32 */
+    float    scale;      /* finite */
+} ftc_embed_t;
+
+/*
+ * y[t] = scale * table[token t], rounded once; zeros where the token is not in 0 .. V-1 (padding, positions without a token).
+ *   d_tokens  [n] of token_bits, n at most 2^31
+ *   d_table   row v at element v * table_stride; d_y: row t at element t * y_stride (strides >= H)
+ * Pointers are aligned to their element size; rows on 16-byte boundaries are the fast case. n = 0 is valid and does nothing.
+ */
+FTC_API int ftc_embedding_forward(const ftc_embed_t* desc, uint64_t n, const void* d_tokens, const void* d_table, uint64_t table_stride,
+                                  void* d_y, uint64_t y_stride, void* cuda_stream);
+
+/*
+ * The table's gradient, for each process: row v of process p is scale * the sum of dy[t] over its tokens t of value v, in the order of
+ * t in runs of FTC_EMBED_RUN (the runs' sums are added in order too).
+ *   d_row_splits  as for ftc_layernorm_backward, of tokens
+ *   d_dtable      float32 [ceil(V*H/k)][P][k], the inputs of ceil(V*H/k) scenarios for ftc_allreduce_batch: element e = v*H + h of
+ *                 process p is element e % k of message e / k; the last message is filled up with zeros. Written whole.
+ *   d_workspace   ftc_embedding_workspace_bytes(desc, n) bytes, 16-byte aligned; as for ftc_layernorm_backward. NULL with n = 0
+ */
+FTC_API int ftc_embedding_backward(const ftc_embed_t* desc, uint64_t n, const void* d_tokens, const void* d_dy, uint64_t dy_stride,
+                                   const uint64_t* d_row_splits, float* d_dtable, void* d_workspace, size_t workspace_bytes,
+                                   void* cuda_stream);
+FTC_API size_t ftc_embedding_workspace_bytes(const ftc_embed_t* desc, uint64_t n);   /* 0 for an invalid descriptor, and for n = 0 */
+#define FTC_EMBED_RUN 32u
+
+/* Log probabilities of given tokens under rows of logits. */
+typedef struct {
+    uint32_t V;          /* logits of a row, 1 .. 2^30 */
+    uint32_t dtype;      /* logits and their gradient: FTC_F32, FTC_BF16 or FTC_F16 */
+    uint32_t token_bits; /* tokens are int64 or int32: 64 or 32 */
+    uint32_t top;        /* the most likely tokens that are listed, 0 .. 32 and at most V */
+    float    scale;      /* z = scale * logit (1 / temperature), 1e-6 .. 1e6 */
+} ftc_logprob_t;
+
+/*
+ * For each row, with z = scale * logits: lse = log(sum(exp(z))), logprob = z[token] - lse, entropy = -sum(p * log p) with p = exp(z - lse),
+ * and the `top` largest logits' log probabilities and tokens, largest first, the lower token first where logits are the same.
+ *   d_logits  [rows] rows of V elements, row r at element r * stride (stride >= V); rows at most 2^31
+ *   d_tokens  [rows] of token_bits, or NULL (with d_logprob NULL). A token outside 0 .. V-1: logprob 0
+ *   d_logprob, d_entropy, d_lse  [rows] float32; each may be NULL
+ *   d_top_logprob [rows][top] float32, d_top_token [rows][top] int32: both given with top > 0, both NULL otherwise
+ * Logits of -infinity are tokens that cannot come: p = 0. A row of nothing else has lse = logprob = top_logprob = -infinity and entropy 0. A row
+ * that holds +infinity or NaN has NaN for logprob (of a token), entropy, lse and top_logprob; its top_token are unspecified.
+ * rows = 0 is valid and does nothing.
+ */
+FTC_API int ftc_token_logprobs(const ftc_logprob_t* desc, uint64_t rows, const void* d_logits, uint64_t stride, const void* d_tokens,
+                               float* d_logprob, float* d_entropy, float* d_lse, float* d_top_logprob, int32_t* d_top_token,
+                               void* cuda_stream);
+
+/*
+ * The gradient of the logits: scale * (dlogprob * ([j = token] - p_j) - dentropy * p_j * (log p_j + entropy)).
+ *   d_lse, d_entropy       [rows], as the forward pass left them (d_entropy may be NULL without d_dentropy)
+ *   d_dlogprob, d_dentropy [rows] float32; either may be NULL: 0. Where the token is outside 0 .. V-1 its dlogprob is not read into the result
+ *   d_dlogits  rows of V elements, row r at element r * dstride; may be d_logits (with the same stride)
+ * Rows with lse = -infinity get zeros.
+ */
+FTC_API int ftc_token_logprobs_backward(const ftc_logprob_t* desc, uint64_t rows, const void* d_logits, uint64_t stride, const void* d_tokens,
+                                        const float* d_lse, const float* d_entropy, const float* d_dlogprob, const float* d_dentropy,
+                                        void* d_dlogits, uint64_t dstride, void* cuda_stream);
+
+/*
+ * Orthogonalised updates of many matrices at once (momentum, then Newton-Schulz products, as the Muon optimiser does). A plan of the
+ * matrices is built on the host and kept by the caller on the host and (a copy) on the device, as the table of tensors is.
+ */
+typedef struct {
+    ftc_param_t tensor;      /* n = rows * cols elements, contiguous, row by row; as in the table of tensors */
+    uint32_t rows, cols;     /* each 1 .. 2^20, the smaller at most 2^14; rows * cols at most 2^31 */
+} ftc_matrix_t;
+
+FTC_API size_t ftc_muon_plan_bytes(const ftc_matrix_t* h_matrices, uint32_t n);      /* 0 for invalid entries */
+/* Checks the entries and writes the plan to h_plan (8-byte aligned host memory). FTC_EINVAL: what ftc_param_table_build refuses, NULL
+ * param, tensor.n other than rows * cols, sizes out of range. */
+FTC_API int ftc_muon_plan_build(const ftc_matrix_t* h_matrices, uint32_t n, void* h_plan, size_t plan_bytes);
+FTC_API uint64_t ftc_muon_plan_blocks(const void* h_plan);                           /* blocks of FTC_STATE_BLOCK elements of momentum */
+FTC_API size_t ftc_muon_workspace_bytes(const void* h_plan, uint32_t products);      /* 0 for anything that is no plan */
+
+typedef struct {
+    double lr, momentum, eps;    /* lr >= 0 and finite, 0 <= momentum < 1, eps >= 1e-30, all of them as float32 */
+    uint32_t steps;              /* Newton-Schulz steps, 1 .. 16 (5 is usual) */
+    uint32_t nesterov;           /* 1 or 0 */
+    uint32_t products;           /* 16: the operands of products are rounded to float16 (of numbers up to 1.3, held times 2^14): the update X is
+                                    good to about 1e-3 of its norm where the momentum is well conditioned. 32: operands are held as two
+                                    float16 numbers each, three products for one: 1e-6 */
+    uint32_t reserved;           /* 0 */
+} ftc_muon_t;
+
+/*
+ * For each matrix, with l = lr * lr_scale:
+ *   g = grad * (1 / included) * *d_grad_scale;  M = M*momentum + g;  U = nesterov ? g + M*momentum : M
+ *   X = U / (|U| + eps) with the root of the sum of squares |U|, transposed if it has more rows than columns; then, `steps` times,
+ *   A = X X^T, X = 3.4445 X + (-4.775 A + 2.0315 A A) X
+ *   p = p * (1 - l*weight_decay) - l * X
+ * X has singular values between 0.68 and 1.21 but where U's are tiny; a matrix's elements then move by about l / sqrt(max(rows, cols))
+ * (lr_scale = 0.2 * sqrt(max(rows, cols)) makes it 0.2 l as with AdamW).
+ *   d_momentum    float32, ftc_muon_plan_blocks() blocks of FTC_STATE_BLOCK elements laid out as AdamW's states; zeros before the first step; 32-byte aligned
+ *   d_grad_scale  as for ftc_adamw_step
+ *   d_workspace   ftc_muon_workspace_bytes(h_plan, products) bytes, 256-byte aligned; as for ftc_layernorm_backward
+ * An element of a message that was not delivered keeps its momentum, which is its U; a matrix of which nothing was delivered (with n > 0) stays as it is.
+ * A matrix that meets NaN or an infinity has NaN in its weights afterwards. d_workspace's first 32-bit word is 0 after the call; were a wait
+ * inside a kernel ever to give up, it is not, and weights of the matrices concerned were left as they are.
+ */
+FTC_API int ftc_muon_step(const ftc_muon_t* hyper, const void* h_plan, const void* d_plan, float* d_momentum, const float* d_grad_scale,
+                          void* d_workspace, size_t workspace_bytes, void* cuda_stream);
+
 FTC_API const char* ftc_strerror(int code);
 FTC_API uint32_t ftc_version(void);
 

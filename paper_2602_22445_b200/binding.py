@@ -46,7 +46,9 @@ EXPORTS = ["ftc_reduce_batch", "ftc_allreduce_batch", "ftc_reduce_batch_noalloc"
            "ftc_kernel_name", "ftc_kernel_variant", "ftc_launch_blocks", "ftc_read_bandwidth_probe", "ftc_strerror", "ftc_version",
            "ftc_layernorm_forward", "ftc_layernorm_backward", "ftc_layernorm_workspace_bytes", "ftc_param_table_bytes",
            "ftc_param_table_build", "ftc_param_table_blocks", "ftc_grad_norm", "ftc_grad_norm_workspace_bytes", "ftc_adamw_step",
-           "ftc_adamw_states"]
+           "ftc_adamw_states", "ftc_embedding_forward", "ftc_embedding_backward", "ftc_embedding_workspace_bytes", "ftc_token_logprobs",
+           "ftc_token_logprobs_backward", "ftc_muon_plan_bytes", "ftc_muon_plan_build", "ftc_muon_plan_blocks", "ftc_muon_workspace_bytes",
+           "ftc_muon_step"]
 FTC_STATE_BLOCK = 256
 
 
@@ -74,6 +76,24 @@ class ftc_param_t(C.Structure):
 class ftc_adamw_t(C.Structure):
     _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_uint64),
                 ("state_bits", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class ftc_embed_t(C.Structure):
+    _fields_ = [("V", C.c_uint32), ("H", C.c_uint32), ("P", C.c_uint32), ("k", C.c_uint32), ("dtype", C.c_uint32), ("wdtype", C.c_uint32),
+                ("token_bits", C.c_uint32), ("scale", C.c_float)]
+
+
+class ftc_logprob_t(C.Structure):
+    _fields_ = [("V", C.c_uint32), ("dtype", C.c_uint32), ("token_bits", C.c_uint32), ("top", C.c_uint32), ("scale", C.c_float)]
+
+
+class ftc_matrix_t(C.Structure):
+    _fields_ = [("tensor", ftc_param_t), ("rows", C.c_uint32), ("cols", C.c_uint32)]
+
+
+class ftc_muon_t(C.Structure):
+    _fields_ = [("lr", C.c_double), ("momentum", C.c_double), ("eps", C.c_double), ("steps", C.c_uint32), ("nesterov", C.c_uint32),
+                ("products", C.c_uint32), ("reserved", C.c_uint32)]
 
 
 class FtcError(RuntimeError):
@@ -149,6 +169,27 @@ def load():
     lib.ftc_adamw_step.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.ftc_adamw_states.restype = C.c_int
     lib.ftc_adamw_states.argtypes = [u64, vp, vp, vp, vp, vp, vp, vp]
+    ep, lp, mp = C.POINTER(ftc_embed_t), C.POINTER(ftc_logprob_t), C.POINTER(ftc_muon_t)
+    lib.ftc_embedding_forward.restype = C.c_int
+    lib.ftc_embedding_forward.argtypes = [ep, u64, vp, vp, u64, vp, u64, vp]
+    lib.ftc_embedding_backward.restype = C.c_int
+    lib.ftc_embedding_backward.argtypes = [ep, u64, vp, vp, u64, vp, vp, vp, sz, vp]
+    lib.ftc_embedding_workspace_bytes.restype = sz
+    lib.ftc_embedding_workspace_bytes.argtypes = [ep, u64]
+    lib.ftc_token_logprobs.restype = C.c_int
+    lib.ftc_token_logprobs.argtypes = [lp, u64, vp, u64, vp, vp, vp, vp, vp, vp, vp]
+    lib.ftc_token_logprobs_backward.restype = C.c_int
+    lib.ftc_token_logprobs_backward.argtypes = [lp, u64, vp, u64, vp, vp, vp, vp, vp, vp, u64, vp]
+    lib.ftc_muon_plan_bytes.restype = sz
+    lib.ftc_muon_plan_bytes.argtypes = [vp, u32]
+    lib.ftc_muon_plan_build.restype = C.c_int
+    lib.ftc_muon_plan_build.argtypes = [vp, u32, vp, sz]
+    lib.ftc_muon_plan_blocks.restype = u64
+    lib.ftc_muon_plan_blocks.argtypes = [vp]
+    lib.ftc_muon_workspace_bytes.restype = sz
+    lib.ftc_muon_workspace_bytes.argtypes = [vp, u32]
+    lib.ftc_muon_step.restype = C.c_int
+    lib.ftc_muon_step.argtypes = [mp, vp, vp, vp, vp, vp, sz, vp]
     lib.ftc_strerror.restype = C.c_char_p
     lib.ftc_strerror.argtypes = [C.c_int]
     lib.ftc_version.restype = u32
@@ -537,4 +578,154 @@ def ftc_adamw_states(table, d_m, d_v, d_m_scale, d_v_scale, d_m_out, d_v_out, st
                                  _stream(stream))
     if check and rc != FTC_OK:
         raise FtcError(rc, "ftc_adamw_states")
+    return rc
+
+
+# ---- the two ends of a language model: embedding, token log probabilities; the orthogonalised update of its matrices ----
+
+def make_embed_desc(V, H, dtype, wdtype=None, P=1, k=None, scale=1.0) -> ftc_embed_t:
+    """A table of V rows of H elements of `wdtype` (default: `dtype`), y and dy of `dtype`; P and k: processes and message length of the
+    gradient (default: one process, [V][H]). The tokens' width is taken from the tensor that a call gets."""
+    dtype = dtype if isinstance(dtype, int) else _float_code(dtype)
+    wdtype = dtype if wdtype is None else wdtype if isinstance(wdtype, int) else _float_code(wdtype)
+    return ftc_embed_t(V, H, P, H if k is None else k, dtype, wdtype, 64, scale)
+
+
+def make_logprob_desc(V, dtype, top=0, scale=1.0) -> ftc_logprob_t:
+    """Rows of V logits of `dtype`, multiplied by `scale`; `top`: how many alternatives are listed (0 .. 32)."""
+    return ftc_logprob_t(V, dtype if isinstance(dtype, int) else _float_code(dtype), 64, top, scale)
+
+
+def _matrix_ptr(t, what, rows, cols, code):
+    """Address and row stride of a [rows][cols] tensor of a floating type whose rows are contiguous."""
+    if t.shape != (rows, cols) or not t.is_cuda or (_FLOAT_CODES.get(t.dtype) != code and _float_code(t.dtype) != code):
+        raise ValueError(f"{what}: a CUDA tensor [{rows}][{cols}] of the descriptor's type is wanted")
+    stride, inner = t.stride()
+    if inner != 1 and cols > 1:
+        raise ValueError(f"{what}: contiguous rows are wanted")
+    return t.data_ptr(), stride if rows > 1 or stride >= cols else cols
+
+
+def _tokens_ptr(desc, t, what="d_tokens"):
+    """The descriptor for these tokens' width (the caller's own is left as it is: another thread may use it over others), their number and
+    address."""
+    size = t.element_size()
+    if not t.is_cuda or not t.is_contiguous() or t.is_floating_point() or size not in (4, 8):
+        raise ValueError(f"{what}: contiguous CUDA whole numbers of 32 or 64 bits are wanted")
+    if desc.token_bits != 8 * size:
+        desc = type(desc).from_buffer_copy(desc)
+        desc.token_bits = 8 * size
+    return desc, t.numel(), t.data_ptr()
+
+
+def ftc_embedding_forward(desc, d_tokens, d_table, d_y, stream=None, check=True) -> int:
+    desc, n, tokens = _tokens_ptr(desc, d_tokens)
+    table, ts = _matrix_ptr(d_table, "d_table", desc.V, desc.H, desc.wdtype)
+    y, ys = _matrix_ptr(d_y, "d_y", n, desc.H, desc.dtype)
+    rc = (_lib or load()).ftc_embedding_forward(desc, n, tokens, table, ts, y, ys, _stream(stream))
+    if rc and check:
+        raise FtcError(rc, "ftc_embedding_forward")
+    return rc
+
+
+def ftc_embedding_workspace_bytes(desc, n) -> int:
+    return load().ftc_embedding_workspace_bytes(C.byref(desc), n)
+
+
+def ftc_embedding_backward(desc, d_tokens, d_dy, d_row_splits, d_dtable, d_workspace, stream=None, check=True) -> int:
+    desc, n, tokens = _tokens_ptr(desc, d_tokens)
+    dy, dys = _matrix_ptr(d_dy, "d_dy", n, desc.H, desc.dtype)
+    if d_row_splits is not None and (d_row_splits.numel() != desc.P + 1 or d_row_splits.element_size() != 8 or d_row_splits.is_floating_point()):
+        raise ValueError("d_row_splits: P + 1 whole numbers of 64 bits are wanted")
+    out = -(-desc.V * desc.H // desc.k) * desc.P * desc.k
+    ws_bytes = 0 if d_workspace is None else d_workspace.numel() * d_workspace.element_size()
+    rc = (_lib or load()).ftc_embedding_backward(desc, n, tokens, dy, dys, _dev_ptr(d_row_splits), _vector_ptr(d_dtable, "d_dtable", out),
+                                                 _dev_ptr(d_workspace), ws_bytes, _stream(stream))
+    if rc and check:
+        raise FtcError(rc, "ftc_embedding_backward")
+    return rc
+
+
+def _given_tokens(desc, d_tokens, rows):
+    if d_tokens is None:
+        return desc, None
+    desc, n, tokens = _tokens_ptr(desc, d_tokens)
+    if n != rows:
+        raise ValueError(f"d_tokens: {rows} tokens are wanted, one for each row")
+    return desc, tokens
+
+
+def ftc_token_logprobs(desc, d_logits, d_tokens, d_logprob, d_entropy=None, d_lse=None, d_top_logprob=None, d_top_token=None, stream=None,
+                       check=True) -> int:
+    rows = d_logits.shape[0]
+    desc, tokens = _given_tokens(desc, d_tokens, rows)
+    x, xs = _matrix_ptr(d_logits, "d_logits", rows, desc.V, desc.dtype)
+    if d_top_token is not None and (d_top_token.numel() != rows * desc.top or d_top_token.element_size() != 4 or d_top_token.is_floating_point()):
+        raise ValueError("d_top_token: `top` whole numbers of 32 bits for each row are wanted")
+    rc = (_lib or load()).ftc_token_logprobs(desc, rows, x, xs, tokens, _vector_ptr(d_logprob, "d_logprob", rows), _vector_ptr(d_entropy, "d_entropy", rows),
+                                             _vector_ptr(d_lse, "d_lse", rows), _vector_ptr(d_top_logprob, "d_top_logprob", rows * desc.top),
+                                             _dev_ptr(d_top_token), _stream(stream))
+    if rc and check:
+        raise FtcError(rc, "ftc_token_logprobs")
+    return rc
+
+
+def ftc_token_logprobs_backward(desc, d_logits, d_tokens, d_lse, d_entropy, d_dlogprob, d_dentropy, d_dlogits, stream=None, check=True) -> int:
+    rows = d_logits.shape[0]
+    desc, tokens = _given_tokens(desc, d_tokens, rows)
+    x, xs = _matrix_ptr(d_logits, "d_logits", rows, desc.V, desc.dtype)
+    d, ds = _matrix_ptr(d_dlogits, "d_dlogits", rows, desc.V, desc.dtype)
+    rc = (_lib or load()).ftc_token_logprobs_backward(desc, rows, x, xs, tokens, _vector_ptr(d_lse, "d_lse", rows), _vector_ptr(d_entropy, "d_entropy", rows),
+                                                      _vector_ptr(d_dlogprob, "d_dlogprob", rows), _vector_ptr(d_dentropy, "d_dentropy", rows), d, ds,
+                                                      _stream(stream))
+    if rc and check:
+        raise FtcError(rc, "ftc_token_logprobs_backward")
+    return rc
+
+
+def make_matrix(param, grad, master=None, status=None, k=0, lr_scale=1.0, weight_decay=0.0):
+    """One matrix of a plan: the arguments of make_param(), `param` with two dimensions. A plan keeps them alive."""
+    if param.dim() != 2:
+        raise ValueError("param: a matrix is wanted")
+    entry, keeps = make_param(param, grad, master, status, k, lr_scale, weight_decay)
+    return ftc_matrix_t(entry, param.shape[0], param.shape[1]), keeps
+
+
+class MuonPlan:
+    """A plan of matrices (ftc_muon_plan_build) on the host and on the device, with the tensors that it points to."""
+
+    def __init__(self, matrices, device="cuda"):
+        torch = _torch()
+        entries = (ftc_matrix_t * max(1, len(matrices)))(*[m[0] for m in matrices])
+        size = load().ftc_muon_plan_bytes(entries, len(matrices))
+        self.host = np.zeros(max(size, 8) // 8, dtype=np.uint64)
+        rc = load().ftc_muon_plan_build(entries, len(matrices), self.host.ctypes.data, size)
+        if rc != FTC_OK:
+            raise FtcError(rc, "ftc_muon_plan_build")
+        self.keeps = [m[1] for m in matrices]
+        self.h_ptr = self.host.ctypes.data
+        self.blocks = load().ftc_muon_plan_blocks(self.h_ptr)
+        self.device = torch.from_numpy(self.host.view(np.int64)).to(device)
+        self.d_ptr = self.device.data_ptr()
+
+
+def make_muon_plan(matrices, device="cuda") -> MuonPlan:
+    """The plan of a list of make_matrix()s. Tensors that move need a new one."""
+    return MuonPlan(matrices, device)
+
+
+def make_muon(lr, momentum=0.95, eps=1e-7, steps=5, nesterov=True, products=16) -> ftc_muon_t:
+    return ftc_muon_t(lr, momentum, eps, steps, int(nesterov), products, 0)
+
+
+def ftc_muon_workspace_bytes(plan, products=32) -> int:
+    return load().ftc_muon_workspace_bytes(plan.h_ptr, products)
+
+
+def ftc_muon_step(hyper, plan, d_momentum, d_grad_scale, d_workspace, stream=None, check=True) -> int:
+    ws_bytes = 0 if d_workspace is None else d_workspace.numel() * d_workspace.element_size()
+    rc = (_lib or load()).ftc_muon_step(hyper, plan.h_ptr, plan.d_ptr, _vector_ptr(d_momentum, "d_momentum", plan.blocks * FTC_STATE_BLOCK),
+                                        _vector_ptr(d_grad_scale, "d_grad_scale", 1), _dev_ptr(d_workspace), ws_bytes, _stream(stream))
+    if rc and check:
+        raise FtcError(rc, "ftc_muon_step")
     return rc

@@ -1,0 +1,371 @@
+// Log probabilities of given tokens, entropy and top alternatives under rows of logits, and the logits' gradient.
+//
+// Forward: one pass over a row. A lane keeps the largest logit m that it has seen, s = sum(2^d) and t = sum(d 2^d) with d = c (x - m),
+// c = scale * log2(e); where a larger one comes, s and t are moved to it. Lanes, warps and blocks are joined the same way; then
+//   lse = scale m + ln s,   entropy = ln s - ln 2 * t / s,   logprob = scale (x[token] - m) - ln s.
+// x - m before the product: logits far from 0 (a row of the type's lowest value) lose nothing.
+// Top alternatives: a warp keeps the best 32 it has seen in its lanes, sorted; an element enters if it beats the last one that counts.
+// Rows are divided over the blocks of a cluster where there are few.
+#include <cooperative_groups.h>
+#include "ftc_lm.cuh"
+
+namespace ftc {
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLeast = -200.f;                                 // 2^-200 is 0 in float32: stands for whatever is smaller
+constexpr uint32_t kNone = 0xFFFFFFFFu;
+
+__device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float max_nan(float a, float b) { float y; asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
+
+// 16 bytes as numbers.
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+    static constexpr int N = 4;
+    static __device__ __forceinline__ void numbers(float* v, uint4 r) {
+        v[0] = __uint_as_float(r.x); v[1] = __uint_as_float(r.y); v[2] = __uint_as_float(r.z); v[3] = __uint_as_float(r.w);
+    }
+    static __device__ __forceinline__ uint4 pack(const float* v) {
+        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    }
+};
+template <> struct Vec<__nv_bfloat16> {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ void numbers(float* v, uint4 r) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+    }
+    static __device__ __forceinline__ uint4 pack(const float* v) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t*>(&h); }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+template <> struct Vec<__half> {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ void numbers(float* v, uint4 r) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i])); v[2 * i] = f.x; v[2 * i + 1] = f.y; }
+    }
+    static __device__ __forceinline__ uint4 pack(const float* v) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t*>(&h); }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+
+struct Sums { float m, s, t; };
+
+__device__ __forceinline__ void move_to(Sums& a, float m, float c) {       // m: at least a.m, or NaN
+    const float d = fmaxf((a.m - m) * c, kLeast), f = exp2_fast(d);          // of two infinities: NaN, which fmaxf leaves out
+    a.t = fmaf(a.s, d, a.t) * f;
+    a.s *= f;
+    a.m = m;
+}
+__device__ __forceinline__ void join(Sums& a, Sums b, float c) {
+    const float m = max_nan(a.m, b.m);
+    move_to(a, m, c);
+    move_to(b, m, c);
+    a.s += b.s; a.t += b.t;
+}
+__device__ __forceinline__ void take(Sums& a, float x, float c) {          // x is at most a.m
+    const float d = fmaxf((x - a.m) * c, kLeast), e = exp2_fast(d);
+    a.s += e;
+    a.t = fmaf(d, e, a.t);
+}
+__device__ __forceinline__ Sums shuffled(const Sums& a, int o) {
+    Sums b;
+    b.m = __shfl_xor_sync(kNone, a.m, o); b.s = __shfl_xor_sync(kNone, a.s, o); b.t = __shfl_xor_sync(kNone, a.t, o);
+    return b;
+}
+
+// The best 32 of a warp, best first, one a lane: a larger word is a better element, equal logits go to the lower index. 0: none.
+__device__ __forceinline__ uint64_t word_of(float x, uint32_t index) {
+    const uint32_t b = __float_as_uint(x + 0.f), o = b & 0x80000000u ? ~b : b | 0x80000000u;     // -0 is 0
+    return (uint64_t)o << 32 | (uint32_t)~index;
+}
+__device__ __forceinline__ float value_of(uint64_t w) {
+    const uint32_t o = (uint32_t)(w >> 32);
+    return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+}
+__device__ __forceinline__ uint32_t index_of(uint64_t w) { return ~(uint32_t)w; }
+__device__ __forceinline__ void insert(uint64_t& best, uint64_t w, uint32_t lane) {
+    const uint32_t at = __popc(__ballot_sync(kNone, best > w));              // sorted: those before it
+    const uint64_t up = __shfl_up_sync(kNone, best, 1);
+    if (lane == at) best = w;
+    else if (lane > at) best = up;
+}
+// The best 32 of two sorted lists, sorted.
+__device__ __forceinline__ uint64_t merged(uint64_t a, uint64_t b, uint32_t lane) {
+    const uint64_t r = __shfl_sync(kNone, b, 31 - lane);
+    uint64_t x = a > r ? a : r;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        const uint64_t y = __shfl_xor_sync(kNone, x, o);
+        x = (lane & o) ? (x < y ? x : y) : (x > y ? x : y);
+    }
+    return x;
+}
+
+// A row's logits for GROUP threads (one warp, or a block of several); blocks of a cluster share it.
+constexpr uint32_t kLogprobThreads = 256;
+
+// Elements begin .. end-1 of a row: single ones up to the first 16-byte boundary, vectors, single ones behind.
+template <typename T, bool TOP> struct Scan {
+    Sums a;
+    uint64_t best;
+    float least;                                                 // what an element has to beat
+    __device__ __forceinline__ void consider(const float* v, int count, float most, uint32_t index, uint32_t n_top, uint32_t lane) {
+        uint32_t lanes = __ballot_sync(kNone, most > least);
+        while (lanes) {
+            const int src = __ffs(lanes) - 1;
+            lanes &= lanes - 1;
+#pragma unroll
+            for (int j = 0; j < count; ++j) {
+                const float x = __shfl_sync(kNone, v[j], src);
+                const uint32_t at = __shfl_sync(kNone, index, src) + j;
+                if (x > least) {
+                    insert(best, word_of(x, at), lane);
+                    const uint64_t w = __shfl_sync(kNone, best, n_top - 1);
+                    least = w ? value_of(w) : -INFINITY;
+                }
+            }
+        }
+    }
+};
+
+template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds__(kLogprobThreads) token_logprobs_kernel(LogprobArgs a, uint32_t parts) {
+    namespace cg = cooperative_groups;
+    constexpr int N = Vec<T>::N;
+    constexpr uint32_t kGroups = kLogprobThreads / GROUP, kWarps = GROUP / 32;
+    __shared__ Sums sums[kLogprobThreads / 32];
+    __shared__ uint64_t lists[kLogprobThreads / 32][32];
+    __shared__ Sums joined;
+    __shared__ uint64_t joined_list[32];
+    const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, in_group = threadIdx.x % GROUP;
+    const uint32_t part = parts > 1 ? cg::this_cluster().block_rank() : 0;
+    const float c = a.scale * kLog2e;
+    // groups beyond the last row go along with it, so that all threads meet at the barriers
+    const uint64_t wanted = (uint64_t)(blockIdx.x / parts) * kGroups + threadIdx.x / GROUP;
+    const uint32_t row = (uint32_t)(wanted < a.rows ? wanted : a.rows - 1);
+    const T* x = static_cast<const T*>(a.logits) + row * a.stride;
+    const uint32_t share = ((a.V + parts - 1) / parts + 63) & ~63u;
+    const uint32_t begin = min(a.V, part * share), end = min(a.V, begin + share);
+    // single elements before the first boundary and behind the last
+    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(x + begin) & 15) / sizeof(T);
+    const uint32_t head = min(end, begin + (off ? N - off : 0)), vecs = (end - head) / N, tail = head + vecs * N;
+
+    Scan<T, TOP> q;
+    q.a = {-INFINITY, 0.f, 0.f};
+    q.best = 0; q.least = -INFINITY;
+    auto single = [&](uint32_t i, bool there) {
+        const float v = there ? to_f32(x[i]) : -INFINITY;
+        const float m = max_nan(q.a.m, v);
+        move_to(q.a, m, c);
+        if (there) take(q.a, v, c);
+        if (TOP) q.consider(&v, 1, v, i, a.top, lane);
+    };
+    if (in_group < 32 && head > begin) single(begin + lane, begin + lane < head);
+    const uint4* xv = reinterpret_cast<const uint4*>(x + head);
+    constexpr uint32_t U = 4;
+    for (uint32_t i0 = in_group - lane; i0 < vecs; i0 += GROUP * U) {
+        uint4 r[U];
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+            const uint32_t i = i0 + u * GROUP + lane;
+            if (i < vecs) r[u] = __ldg(xv + i);
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+            if (i0 + u * GROUP >= vecs) break;                   // the same for the whole warp
+            const uint32_t i = i0 + u * GROUP + lane;
+            float v[N], most = -INFINITY;
+            if (i < vecs) {
+                Vec<T>::numbers(v, r[u]);
+#pragma unroll
+                for (int j = 0; j < N; ++j) most = max_nan(most, v[j]);
+                if (!(most <= q.a.m)) move_to(q.a, max_nan(q.a.m, most), c);
+#pragma unroll
+                for (int j = 0; j < N; ++j) take(q.a, v[j], c);
+            }
+            if (TOP) q.consider(v, N, most, head + i * N, a.top, lane);
+        }
+    }
+    if (in_group >= GROUP - 32 && tail < end) single(tail + lane, tail + lane < end);
+
+    // lanes, warps, blocks
+#pragma unroll
+    for (int o = 16; o; o >>= 1) join(q.a, shuffled(q.a, o), c);
+    if (GROUP > 32 || parts > 1) {
+        if (lane == 0) sums[warp] = q.a;
+        if (TOP) lists[warp][lane] = q.best;
+        __syncthreads();
+        if (warp == 0) {
+            Sums all = sums[0];
+            for (uint32_t w = 1; w < kWarps; ++w) join(all, sums[w], c);
+            q.a = all;
+            if (TOP) for (uint32_t w = 1; w < kWarps; ++w) q.best = merged(q.best, lists[w][lane], lane);
+        }
+        if (parts > 1) {
+            cg::cluster_group cluster = cg::this_cluster();
+            if (warp == 0) {
+                if (lane == 0) joined = q.a;
+                if (TOP) joined_list[lane] = q.best;
+            }
+            cluster.sync();
+            if (part == 0 && warp == 0) {
+                for (uint32_t b = 1; b < parts; ++b) {
+                    join(q.a, *cluster.map_shared_rank(&joined, b), c);
+                    if (TOP) q.best = merged(q.best, cluster.map_shared_rank(joined_list, b)[lane], lane);
+                }
+            }
+            cluster.sync();                                      // a block's shared memory stays until it has been read
+        }
+        if (warp || part) return;
+    }
+    if (wanted >= a.rows) return;
+
+    const bool bad = isnan(q.a.m) || q.a.m == INFINITY, empty = q.a.m == -INFINITY;
+    const float ln_s = logf(q.a.s), nan = __int_as_float(0x7FFFFFFF);
+    const float lse = bad ? nan : empty ? -INFINITY : fmaf(a.scale, q.a.m, ln_s);
+    if (lane == 0) {
+        if (a.lse) a.lse[row] = lse;
+        if (a.entropy) a.entropy[row] = bad ? nan : empty ? 0.f : fmaxf(0.f, ln_s - kLn2 * (q.a.t / q.a.s));
+        if (a.logprob) {
+            const int32_t tok = token_at(a.tokens, a.token_bits, row, a.V);
+            a.logprob[row] = tok < 0 ? 0.f : bad ? nan : empty ? -INFINITY : fmaf(a.scale, to_f32(x[tok]) - q.a.m, -ln_s);
+        }
+    }
+    if (!TOP) return;
+    // fewer logits above -infinity than were asked for: the lowest tokens of the others
+    uint32_t have = __popc(__ballot_sync(kNone, q.best != 0));
+    for (uint32_t i0 = 0; i0 < a.V && have < a.top; i0 += 32) {
+        uint32_t more = __ballot_sync(kNone, i0 + lane < a.V && to_f32(x[min(i0 + lane, a.V - 1)]) == -INFINITY);
+        while (more && have < a.top) {
+            const uint32_t j = __ffs(more) - 1;
+            more &= more - 1;
+            if (lane == have) q.best = word_of(-INFINITY, i0 + j);
+            ++have;
+        }
+    }
+    if (lane < a.top) {
+        const float v = value_of(q.best);
+        a.top_logprob[(uint64_t)row * a.top + lane] = bad ? nan : empty ? -INFINITY : fmaf(a.scale, v - q.a.m, -ln_s);
+        a.top_token[(uint64_t)row * a.top + lane] = q.best ? (int32_t)index_of(q.best) : 0;
+    }
+}
+
+template <typename T, bool TOP> static cudaError_t forward(const LogprobArgs& a, int sms, cudaStream_t st) {
+    if (a.V <= 1024) {                                           // a warp for each row
+        token_logprobs_kernel<T, TOP, 32><<<(a.rows + 7) / 8, kLogprobThreads, 0, st>>>(a, 1);
+        return cudaGetLastError();
+    }
+    uint32_t parts = 1;                                          // blocks of a cluster share a row while there are SMs without one
+    while (parts < 8 && (uint64_t)a.rows * parts * 2 <= (uint64_t)sms * 2 && a.V / (parts * 2) >= 4096) parts *= 2;
+    if ((uint64_t)a.rows * parts > 0x7FFFFFFFull) return cudaErrorInvalidValue;
+    if (parts == 1) {
+        token_logprobs_kernel<T, TOP, kLogprobThreads><<<a.rows, kLogprobThreads, 0, st>>>(a, 1);
+        return cudaGetLastError();
+    }
+    cudaLaunchAttribute shape{};
+    shape.id = cudaLaunchAttributeClusterDimension;
+    shape.val.clusterDim.x = parts; shape.val.clusterDim.y = shape.val.clusterDim.z = 1;
+    cudaLaunchConfig_t how{};
+    how.gridDim = dim3(a.rows * parts); how.blockDim = dim3(kLogprobThreads); how.stream = st; how.attrs = &shape; how.numAttrs = 1;
+    return cudaLaunchKernelEx(&how, token_logprobs_kernel<T, TOP, kLogprobThreads>, a, parts);
+}
+
+cudaError_t launch_token_logprobs(const LogprobArgs& a, int sms, cudaStream_t st) {
+    if (a.dtype == FTC_F32) return a.top ? forward<float, true>(a, sms, st) : forward<float, false>(a, sms, st);
+    if (a.dtype == FTC_BF16) return a.top ? forward<__nv_bfloat16, true>(a, sms, st) : forward<__nv_bfloat16, false>(a, sms, st);
+    return a.top ? forward<__half, true>(a, sms, st) : forward<__half, false>(a, sms, st);
+}
+
+// ---- gradient ----
+//
+// With A = -scale (dlogprob + dentropy (entropy - lse)) and B = -scale * dentropy * scale: p (A + B x), and scale * dlogprob more at the token.
+
+struct RowFactors { float a, b, up, l2; int32_t token; bool zero; };
+
+__device__ __forceinline__ RowFactors factors_of(const LogprobArgs& g, uint32_t row) {
+    RowFactors f;
+    f.token = g.dlogprob ? token_at(g.tokens, g.token_bits, row, g.V) : -1;
+    const float lse = g.lse_in[row], up = f.token >= 0 ? g.dlogprob[row] : 0.f, de = g.dentropy ? g.dentropy[row] : 0.f;
+    f.zero = lse == -INFINITY;
+    f.l2 = lse;
+    f.a = -(up + (g.dentropy ? de * (g.entropy_in[row] - lse) : 0.f)) * g.scale;
+    f.b = -de * g.scale * g.scale;
+    f.up = up * g.scale;
+    return f;
+}
+__device__ __forceinline__ float gradient(const RowFactors& f, float x, float scale) {
+    const float p = exp2_fast(fmaf(x, scale, -f.l2) * kLog2e);
+    return p == 0.f ? 0.f : p * fmaf(f.b, x, f.a);
+}
+
+// Elements a vector at a time (W bytes) where every row of both begins on such a boundary.
+template <typename T, int W> __global__ void __launch_bounds__(256) logprobs_backward_kernel(LogprobArgs g, uint32_t pieces, uint32_t each) {
+    constexpr int N = W / sizeof(T);
+    const uint32_t row = (uint32_t)(blockIdx.x / pieces), piece = blockIdx.x - row * pieces;
+    const RowFactors f = factors_of(g, row);
+    const T* x = static_cast<const T*>(g.logits) + row * g.stride;
+    T* d = static_cast<T*>(g.dlogits) + row * g.dstride;
+    const uint32_t vecs = (g.V + N - 1) / N, begin = piece * each, end = min(vecs, begin + each);
+    constexpr int U = 4;
+    for (uint32_t i0 = begin + threadIdx.x; i0 < end; i0 += 256 * U) {
+        float v[U][N];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t i = i0 + u * 256;
+            if (i >= end) continue;
+            if (W == 16 && (i + 1) * N <= g.V) {
+                const uint4 r = *reinterpret_cast<const uint4*>(x + (uint64_t)i * N);
+                if constexpr (W == 16) Vec<T>::numbers(v[u], r);
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[u][j] = i * N + j < g.V ? to_f32(x[i * N + j]) : 0.f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t i = i0 + u * 256;
+            if (i >= end) continue;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                float y = f.zero ? 0.f : gradient(f, v[u][j], g.scale);
+                if ((int32_t)(i * N + j) == f.token && !f.zero) y += f.up;
+                v[u][j] = y;
+            }
+            if (W == 16 && (i + 1) * N <= g.V) {
+                if constexpr (W == 16) *reinterpret_cast<uint4*>(d + (uint64_t)i * N) = Vec<T>::pack(v[u]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (i * N + j < g.V) d[i * N + j] = from_f32<T>(v[u][j]);
+            }
+        }
+    }
+}
+
+template <typename T> static cudaError_t backward(const LogprobArgs& g, cudaStream_t st) {
+    const uintptr_t all = reinterpret_cast<uintptr_t>(g.logits) | reinterpret_cast<uintptr_t>(g.dlogits) | g.stride * sizeof(T) | g.dstride * sizeof(T);
+    const bool wide = (all & 15) == 0;
+    const uint32_t n = wide ? 16 / sizeof(T) : 1, vecs = (uint32_t)(((uint64_t)g.V + n - 1) / n), each = 256 * 8, pieces = (vecs + each - 1) / each;
+    if ((uint64_t)g.rows * pieces > 0x7FFFFFFFull) return cudaErrorInvalidValue;
+    const uint32_t grid = g.rows * pieces;
+    if (wide) logprobs_backward_kernel<T, 16><<<grid, 256, 0, st>>>(g, pieces, each);
+    else logprobs_backward_kernel<T, sizeof(T)><<<grid, 256, 0, st>>>(g, pieces, each);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_token_logprobs_backward(const LogprobArgs& g, int sms, cudaStream_t st) {
+    if (g.dtype == FTC_F32) return backward<float>(g, st);
+    if (g.dtype == FTC_BF16) return backward<__nv_bfloat16>(g, st);
+    return backward<__half>(g, st);
+}
+
+}  // namespace ftc

@@ -1,0 +1,166 @@
+"""Token log probabilities, entropy, top alternatives and the logits' gradient against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2602_22445_b200 import binding as B
+from tests import lm_oracle as O
+
+pytestmark = pytest.mark.gpu
+DT = {"float32": torch.float32, "bfloat16": torch.bfloat16, "float16": torch.float16}
+INF = float("inf")
+
+
+def logits_of(rng, rows, V, dtype, pad, kind):
+    x = torch.from_numpy(rng.standard_normal((rows, V)) * 4).to(dtype)
+    if kind == "masked":                  # parts, all but one, all of a row
+        x[rng.random((rows, V)) < 0.5] = -INF
+        x[0] = -INF
+        if rows > 1:
+            x[1] = -INF
+            x[1, V // 2] = 3.0
+        if rows > 2:
+            x[2] = torch.finfo(dtype).min
+        if rows > 3:
+            x[3] = torch.finfo(dtype).min
+            x[3, -1] = 1.0
+    if kind == "same":
+        x[:] = 2.5
+    if kind == "far":
+        x += 900 if dtype == torch.float16 else 3000
+    if kind == "rising":                  # every element beats those before it
+        x = torch.linspace(-9, 9, V, dtype=torch.float64).to(dtype).expand(rows, V).clone()
+    room = torch.full((rows, V + pad), INF, dtype=dtype, device="cuda")
+    room[:, :V] = x.cuda()
+    return room[:, :V]
+
+
+def forward(x, tokens, scale, top):
+    rows, V = x.shape
+    desc = B.make_logprob_desc(V, x.dtype, top=top, scale=scale)
+    out = [torch.full((rows,), 77.0, device="cuda") for _ in range(3)]
+    best = torch.full((rows, top), 77.0, device="cuda") if top else None
+    which = torch.full((rows, top), 77, dtype=torch.int32, device="cuda") if top else None
+    B.ftc_token_logprobs(desc, x, tokens, *out, best, which)
+    return desc, out, best, which
+
+
+def tokens_of(rng, rows, V, bits):
+    t = rng.integers(0, V, rows)
+    t[rng.random(rows) < 0.2] = rng.choice([-1, -100, V, 2 ** 31 - 1])
+    return t, torch.from_numpy(t).to(torch.int64 if bits == 64 else torch.int32).cuda()
+
+
+SIZES = [(1, 1, 0, 64), (3, 2, 1, 32), (5, 31, 0, 64), (9, 64, 0, 64), (2, 1000, 3, 32), (40, 1024, 0, 64), (7, 1025, 0, 32), (4, 5003, 5, 64), (1, 16384, 0, 64),
+         (6, 32768, 8, 64), (1, 131072, 0, 32), (300, 2048, 0, 64), (2, 70001, 2, 64)]
+
+
+@pytest.mark.parametrize("name", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("rows,V,pad,bits", SIZES)
+@pytest.mark.parametrize("kind", ["plain", "masked", "same", "far", "rising"])
+def test_forward(name, rows, V, pad, bits, kind):
+    rng = np.random.default_rng(rows + V)
+    x = logits_of(rng, rows, V, DT[name], pad, kind)
+    t, tokens = tokens_of(rng, rows, V, bits)
+    top, scale = min(V, (0, 1, 5, 20, 32)[(rows + len(kind)) % 5]), (1.0, 0.8)[rows % 2]
+    _, (given, entropy, lse), best, which = forward(x, tokens, scale, top)
+    scale = float(np.float32(scale))
+    w_lse, w_given, w_entropy, w_best, w_which, spread = O.logprobs(x.double().cpu().numpy(), t, scale, top)
+    s_off = O.sum_off(spread, V)
+
+    def close(got, want, off):
+        got = got.double().cpu().numpy()
+        same = (got == want) | (np.isnan(got) & np.isnan(want))
+        with np.errstate(invalid="ignore"):
+            assert (same | (abs(got - want) <= off)).all(), abs(got - want).max()
+
+    with np.errstate(invalid="ignore"):
+        size = np.where(np.isfinite(w_lse), abs(w_lse), 0)
+        close(lse, w_lse, s_off + 4 * O.U32 * (size + spread))
+        close(given, w_given, s_off + 4 * O.U32 * np.where(np.isfinite(w_given), abs(w_given), 0) + 4 * O.U32)
+        close(entropy, w_entropy, 4 * s_off * (1 + spread))
+        if top:
+            assert (which.cpu().numpy() == w_which).all()
+            close(best, w_best, s_off[:, None] + 4 * O.U32 * (1 + np.where(np.isfinite(w_best), abs(w_best), 0)))
+
+
+@pytest.mark.parametrize("name", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("rows,V,pad,bits", SIZES)
+@pytest.mark.parametrize("kind", ["plain", "masked", "same", "rising"])
+@pytest.mark.parametrize("what", ["both", "logprob", "entropy", "in place"])
+def test_backward(name, rows, V, pad, bits, kind, what):
+    rng = np.random.default_rng(rows * V)
+    x = logits_of(rng, rows, V, DT[name], pad, kind)
+    if kind == "masked" and rows > 2:
+        x[2] = -INF                       # p of a row at the type's lowest value is beyond what lse can say in float32
+    t, tokens = tokens_of(rng, rows, V, bits)
+    desc, (given, entropy, lse), _, _ = forward(x, tokens, 0.8, 0)
+    up = torch.from_numpy(rng.standard_normal(rows)).float().cuda() if what != "entropy" else None
+    de = torch.from_numpy(rng.standard_normal(rows)).float().cuda() if what != "logprob" else None
+    zero = np.zeros(rows)
+    want, off = O.logprobs_backward(x.double().cpu().numpy(), t, float(np.float32(0.8)), lse.double().cpu().numpy(), entropy.double().cpu().numpy(),
+                                    zero if up is None else up.double().cpu().numpy(), zero if de is None else de.double().cpu().numpy())
+    if what == "in place":
+        d = x
+    else:
+        d = torch.full((rows, V + pad), 7.0, dtype=DT[name], device="cuda")[:, :V]
+    B.ftc_token_logprobs_backward(desc, x, tokens, lse, entropy if de is not None else None, up, de, d)
+    got = d.double().cpu().numpy()
+    off = off + (abs(want) + off) * O.half_step(name) + O.least(name) * O.half_step(name) * 2
+    assert (abs(got - want) <= off).all(), (abs(got - want) / off).max()
+    if pad:
+        assert (d._base[:, V:] == (INF if what == "in place" else 7.0)).all()
+
+
+def test_gradient_against_differences():
+    """The 64-bit forms against each other: the gradient is that of logprob and entropy."""
+    rng = np.random.default_rng(1)
+    x, t = rng.standard_normal((3, 9)) * 2, np.array([4, -1, 8])
+    x[1, 3] = -np.inf
+    up, de = rng.standard_normal(3), rng.standard_normal(3)
+    lse, given, entropy, *_ = O.logprobs(x, t, 0.7)
+    g, _ = O.logprobs_backward(x, t, 0.7, lse, entropy, up, de)
+    for r in range(3):
+        for j in range(9):
+            if not np.isfinite(x[r, j]):
+                assert g[r, j] == 0
+                continue
+            parts = []
+            for h in (1e-5, -1e-5):
+                y = x.copy()
+                y[r, j] += h
+                _, given, entropy, *_ = O.logprobs(y, t, 0.7)
+                parts.append((up * given + de * entropy).sum())
+            assert abs((parts[0] - parts[1]) / 2e-5 - g[r, j]) < 1e-8
+
+
+@pytest.mark.parametrize("V", [100, 5000, 40000])
+@pytest.mark.parametrize("bad", [float("nan"), INF])
+def test_rows_with_nan_or_infinity(V, bad):
+    x = torch.randn(4, V, device="cuda")
+    x[1, V - 1] = bad
+    x[2, 0] = bad
+    tokens = torch.tensor([3, 3, -1, 5], device="cuda")
+    desc, (given, entropy, lse), best, which = forward(x, tokens, 1.0, 4)
+    for r in (1, 2):
+        assert lse[r].isnan() and entropy[r].isnan() and best[r].isnan().all()
+    assert given[1].isnan() and given[2] == 0
+    assert all(torch.isfinite(v[r]).all() for v in (lse, entropy, best) for r in (0, 3))
+    ones = torch.ones(4, device="cuda")
+    d = torch.zeros_like(x)
+    B.ftc_token_logprobs_backward(desc, x, tokens, lse, entropy, ones, ones, d)
+    assert d[1].isnan().all() and d[2].isnan().all() and torch.isfinite(d[0]).all() and torch.isfinite(d[3]).all()
+
+
+def test_some_outputs_only():
+    x = torch.randn(5, 3000, device="cuda")
+    tokens = torch.arange(5, device="cuda")
+    desc, (given, entropy, lse), _, _ = forward(x, tokens, 1.0, 0)
+    a, b = torch.zeros(5, device="cuda"), torch.zeros(5, device="cuda")
+    B.ftc_token_logprobs(desc, x, tokens, a)
+    B.ftc_token_logprobs(desc, x, None, None, None, b)
+    assert torch.equal(a, given) and torch.equal(b, lse)
+    top = B.make_logprob_desc(3000, torch.float32, top=3)
+    v, w = torch.zeros(5, 3, device="cuda"), torch.zeros(5, 3, dtype=torch.int32, device="cuda")
+    B.ftc_token_logprobs(top, x, None, None, None, None, v, w)
+    assert torch.equal(w.long(), x.topk(3, 1).indices)
