@@ -44,7 +44,7 @@ __device__ __forceinline__ int32_t token_at(const void* tokens, uint32_t bits, u
 // ---- the plan of matrices: header, entries, then (n + 1 numbers each) where a matrix's chunks, blocks and tiles begin ----
 
 constexpr uint64_t kPlanMagic = 0x316E4C5054435446ull;
-constexpr uint32_t kMuonChunk = 8192;                            // elements of a block of the momentum kernel
+constexpr uint32_t kMuonChunk = 2048;                            // elements of a block of the momentum kernel
 struct PlanHead { uint64_t magic, n_blocks, x_blocks, a_blocks, diagonals; uint32_t n, chunks, gram_tiles, apply_tiles; uint64_t pad; };
 struct PlanEntry {
     void* param; float* master; const void* grad; const uint32_t* status;
@@ -52,7 +52,7 @@ struct PlanEntry {
     uint32_t k, rows, cols;
     uint8_t param_dtype, grad_dtype, tall, k_shift;
     float lr_scale, weight_decay;
-    uint32_t m, w, mb, nb, kb, pad;                              // X is m x w (m <= w): mb blocks of 128 rows, nb of 64 columns; A: kb of 64 columns
+    uint32_t m, w, mb, nb, kb, wide;                             // X is m x w (m <= w): mb blocks of 128 rows, nb of 64 columns; A: kb of 64 columns. wide: addresses allow eights
 };
 static_assert(sizeof(PlanHead) == 64 && sizeof(PlanEntry) == 120, "plan layout");
 __host__ __device__ inline const PlanEntry* plan_entries(const void* p) {
@@ -67,7 +67,7 @@ struct MuonArgs {
     const void* plan; uint32_t n;
     float* momentum; const float* grad_scale;
     uint32_t* word;                              // first of the workspace: not 0 once a wait has given up
-    double2* sums; uint32_t* live;               // [chunks]: squares of U, messages delivered; [n]: was anything delivered
+    double2* sums; uint32_t* live; float* factor; // [chunks]: squares of U, messages delivered; [n]: was anything delivered, 2^14 / (|U| + eps)
     float *diag_a, *diag_b;
     unsigned char *x[2], *a, *b;                 // blocks of 128 x 64 float16; with two numbers for each, the low ones x_bytes / a_bytes further on
     uint64_t x_bytes, a_bytes;

@@ -59,12 +59,12 @@ bool count_matrices(const ftc_matrix_t* q, uint32_t n, PlanHead& h) {
         if (!t.grad || !t.param) return false;
         if (!aligned(t.param, size_of(t.param_dtype)) || !aligned(t.grad, size_of(t.grad_dtype)) || !aligned(t.master, 4) || !aligned(t.status, 16)) return false;
         if (t.status && (t.k == 0 || t.k > (1u << 30))) return false;
-        const uint64_t mb = (m + 127) / 128, nb = (w + 63) / 64, half = mb / 2;
+        const uint64_t mb = (m + 127) / 128, nb = (w + 63) / 64, mb2 = (mb + 1) / 2;
         h.n_blocks += (t.n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK;
         h.x_blocks += mb * nb; h.a_blocks += mb * 2 * mb; h.diagonals += mb * 128;
         chunks += (t.n + kMuonChunk - 1) / kMuonChunk;
-        gram += half * (half + 1) + (mb % 2 ? half + 1 : 0);
-        apply += mb * ((nb + 3) / 4);
+        gram += mb2 * (mb2 + 1) / 2;
+        apply += mb2 * ((nb + 3) / 4);
         if (h.n_blocks > (1ull << 32) || h.x_blocks > 0x7FFFFFFFull || h.a_blocks > 0x7FFFFFFFull || chunks > 0x7FFFFFFFull || gram > 0x7FFFFFFFull) return false;
     }
     h.chunks = (uint32_t)chunks; h.gram_tiles = (uint32_t)gram; h.apply_tiles = (uint32_t)apply;
@@ -74,14 +74,14 @@ size_t plan_bytes(const PlanHead& h) {
     return sizeof(PlanHead) + (size_t)h.n * sizeof(PlanEntry) + rounded((size_t)kFirsts * (h.n + 1) * 4, 8);
 }
 
-struct MuonLayout { size_t sums, live, diag_a, diag_b, x0, x1, a, b, x_bytes, a_bytes, total; };
+struct MuonLayout { size_t sums, live, factor, diag_a, diag_b, x0, x1, a, b, x_bytes, a_bytes, total; };
 MuonLayout muon_layout(const PlanHead& h, uint32_t products) {
     const size_t block = 128 * 64 * 2, numbers = products == 32 ? 2 : 1;
     MuonLayout l{};
     l.x_bytes = h.x_blocks * block; l.a_bytes = h.a_blocks * block;
     size_t at = 1024;
     auto take = [&](size_t bytes) { const size_t here = at; at = rounded(at + bytes, 256); return here; };
-    l.sums = take((size_t)h.chunks * 16); l.live = take((size_t)h.n * 4);
+    l.sums = take((size_t)h.chunks * 16); l.live = take((size_t)h.n * 4); l.factor = take((size_t)h.n * 4);
     l.diag_a = take(h.diagonals * 4); l.diag_b = take(h.diagonals * 4);
     l.x0 = take(l.x_bytes * numbers); l.x1 = take(l.x_bytes * numbers); l.a = take(l.a_bytes * numbers); l.b = take(l.a_bytes * numbers);
     l.total = at;
@@ -188,11 +188,12 @@ int ftc_muon_plan_build(const ftc_matrix_t* h_matrices, uint32_t n, void* h_plan
         q.mb = (q.m + 127) / 128; q.nb = (q.w + 63) / 64; q.kb = (q.m + 63) / 64;
         q.first_block = blocks; q.x_block = x; q.a_block = a; q.diagonal = diagonal;
         blocks += (t.n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK; x += (uint64_t)q.mb * q.nb; a += (uint64_t)q.mb * 2 * q.mb; diagonal += q.mb * 128;
-        const uint32_t half = q.mb / 2;
+        const uint32_t mb2 = (q.mb + 1) / 2;
+        q.wide = aligned(t.grad, 16);
         first[kChunkFirst][i + 1] = first[kChunkFirst][i] + (uint32_t)((t.n + kMuonChunk - 1) / kMuonChunk);
         first[kBlockFirst][i + 1] = (uint32_t)x;
-        first[kGramFirst][i + 1] = first[kGramFirst][i] + half * (half + 1) + (q.mb % 2 ? half + 1 : 0);
-        first[kApplyFirst][i + 1] = first[kApplyFirst][i] + q.mb * ((q.nb + 3) / 4);
+        first[kGramFirst][i + 1] = first[kGramFirst][i] + mb2 * (mb2 + 1) / 2;
+        first[kApplyFirst][i + 1] = first[kApplyFirst][i] + mb2 * ((q.nb + 3) / 4);
     }
     return FTC_OK;
 }
@@ -223,7 +224,7 @@ int ftc_muon_step(const ftc_muon_t* hyper, const void* h_plan, const void* d_pla
     unsigned char* ws = static_cast<unsigned char*>(d_workspace);
     MuonArgs a{};
     a.plan = d_plan; a.n = h->n; a.momentum = d_momentum; a.grad_scale = d_grad_scale; a.word = reinterpret_cast<uint32_t*>(ws);
-    a.sums = reinterpret_cast<double2*>(ws + l.sums); a.live = reinterpret_cast<uint32_t*>(ws + l.live);
+    a.sums = reinterpret_cast<double2*>(ws + l.sums); a.live = reinterpret_cast<uint32_t*>(ws + l.live); a.factor = reinterpret_cast<float*>(ws + l.factor);
     a.diag_a = reinterpret_cast<float*>(ws + l.diag_a); a.diag_b = reinterpret_cast<float*>(ws + l.diag_b);
     a.x[0] = ws + l.x0; a.x[1] = ws + l.x1; a.a = ws + l.a; a.b = ws + l.b; a.x_bytes = l.x_bytes; a.a_bytes = l.a_bytes;
     a.chunks = h->chunks; a.x_blocks = (uint32_t)h->x_blocks; a.gram_tiles = h->gram_tiles; a.apply_tiles = h->apply_tiles;

@@ -13,6 +13,7 @@
 //
 // Matrices lie in the workspace in blocks of 128 rows x 64 columns (16 KB), their 16-byte pieces in the order that the tensor cores read
 // (piece c of row r at c ^ r % 8): a block is one contiguous copy, whichever way a product reads it, and edges are zeros.
+#include <cooperative_groups.h>
 #include "ftc_lm.cuh"
 
 namespace ftc {
@@ -51,6 +52,30 @@ __device__ __forceinline__ float share_at(const PlanEntry& t, uint64_t i) {
 
 // ---- momentum ----
 
+// Eight neighbouring elements as numbers.
+__device__ __forceinline__ void eight(float* v, const void* p, uint32_t dtype, uint64_t i) {
+    if (dtype == FTC_F32) {
+        const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
+        const float4 a = q[0], b = q[1];
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        return;
+    }
+    const uint4 r = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i);
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (dtype == FTC_BF16) { v[2 * j] = __uint_as_float(w[j] << 16); v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u); }
+        else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j])); v[2 * j] = f.x; v[2 * j + 1] = f.y; }
+    }
+}
+// Shares of eight neighbours; messages of a multiple of 8 elements have one for all.
+__device__ __forceinline__ void eight_shares(float* s, const PlanEntry& t, uint64_t i) {
+    const float one = share_at(t, i);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] = t.status && t.k % 8 ? share_at(t, i + j) : one;
+}
+
+// A block has 2048 elements of one matrix: eight a thread, neighbours where the addresses allow it (t.wide), 256 apart otherwise.
 __global__ void __launch_bounds__(256) muon_momentum_kernel(MuonArgs a) {
     later_kernel_may_start();
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.word = 0;
@@ -58,29 +83,51 @@ __global__ void __launch_bounds__(256) muon_momentum_kernel(MuonArgs a) {
     if (!isfinite(scale)) return;
     const uint32_t* first = plan_first(a.plan, a.n, kChunkFirst);
     const uint32_t which = matrix_of(first, a.n, blockIdx.x);
-    const PlanEntry& t = plan_entries(a.plan)[which];
+    const PlanEntry t = plan_entries(a.plan)[which];
     const uint64_t begin = (uint64_t)(blockIdx.x - first[which]) * kMuonChunk;
     const uint32_t left = (uint32_t)min((uint64_t)kMuonChunk, t.n - begin);
     float* m = a.momentum + t.first_block * FTC_STATE_BLOCK + begin;
+    float old[8], g[8], s[8];
+    const bool wide = t.wide && left == kMuonChunk;
+    if (wide) {
+        eight(old, m, FTC_F32, threadIdx.x * 8);
+        eight(g, t.grad, t.grad_dtype, begin + threadIdx.x * 8);
+        eight_shares(s, t, begin + threadIdx.x * 8);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t e = threadIdx.x + j * 256;
+            const bool there = e < left;
+            old[j] = there ? m[e] : 0.f;
+            g[j] = there ? element(t.grad, t.grad_dtype, begin + e) : 0.f;
+            s[j] = there ? share_at(t, begin + e) : 0.f;
+        }
+    }
     double sum = 0;
     uint32_t live = 0;
-#pragma unroll 8
-    for (uint32_t j = threadIdx.x; j < left; j += 256) {
-        const float s = share_at(t, begin + j), old = m[j];
-        const float g = element(t.grad, t.grad_dtype, begin + j) * s * scale;
-        float now = old, u = old;
-        if (s > 0.f) {
-            now = fmaf(old, a.mu, g);
-            u = a.nesterov ? fmaf(now, a.mu, g) : now;
-            m[j] = now;
-            live = 1;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        float u = old[j];
+        if (s[j] > 0.f) {
+            const float x = g[j] * s[j] * scale;
+            old[j] = fmaf(old[j], a.mu, x);
+            u = a.nesterov ? fmaf(old[j], a.mu, x) : old[j];
+            live |= 1u << j;
         }
         sum = fma((double)u, (double)u, sum);
+    }
+    if (wide) {
+        float4* q = reinterpret_cast<float4*>(m + threadIdx.x * 8);
+        if (live) { q[0] = make_float4(old[0], old[1], old[2], old[3]); q[1] = make_float4(old[4], old[5], old[6], old[7]); }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (live >> j & 1u) m[threadIdx.x + j * 256] = old[j];
     }
     __shared__ double sums[8];
     __shared__ uint32_t lives[8];
     sum = warp_sum(sum);
-    live = __any_sync(0xFFFFFFFFu, live);
+    live = __any_sync(0xFFFFFFFFu, live != 0);
     if (threadIdx.x % 32 == 0) { sums[threadIdx.x / 32] = sum; lives[threadIdx.x / 32] = live; }
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -89,10 +136,30 @@ __global__ void __launch_bounds__(256) muon_momentum_kernel(MuonArgs a) {
     }
 }
 
+// A matrix's factor 2^14 / (|U| + eps), and whether anything of it was delivered: its chunks' sums in a fixed order.
+__global__ void __launch_bounds__(256) muon_norm_kernel(MuonArgs a) {
+    wait_for_earlier_kernel();
+    later_kernel_may_start();
+    const uint32_t* first = plan_first(a.plan, a.n, kChunkFirst) + blockIdx.x;
+    const uint32_t c0 = first[0], c1 = first[1];
+    __shared__ double sums[8], lives[8];
+    double sum = 0, live = 0;
+#pragma unroll 4
+    for (uint32_t c = c0 + threadIdx.x; c < c1; c += 256) { const double2 s = a.sums[c]; sum += s.x; live += s.y; }
+    sum = warp_sum(sum); live = warp_sum(live);
+    if (threadIdx.x % 32 == 0) { sums[threadIdx.x / 32] = sum; lives[threadIdx.x / 32] = live; }
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < 8; ++w) { sum += sums[w]; live += lives[w]; }
+    a.live[blockIdx.x] = live > 0;
+    a.factor[blockIdx.x] = (float)((double)kUp / (sqrt(sum) + (double)a.eps));
+}
+
 // Where the 16-byte piece c of row r lies in a block.
 __device__ __forceinline__ uint32_t piece(uint32_t r, uint32_t c) { return r * 128 + ((c ^ (r & 7)) << 4); }
 
-// One block of 128 x 64 of X.
+// One block of 128 x 64 of X. Elements that are neighbours in memory are loaded by one thread (eight, where the addresses allow it) or by
+// neighbouring threads; a block whose matrix is transposed is turned in shared memory.
 __global__ void __launch_bounds__(256) muon_layout_kernel(MuonArgs a) {
     wait_for_earlier_kernel();
     later_kernel_may_start();
@@ -100,40 +167,70 @@ __global__ void __launch_bounds__(256) muon_layout_kernel(MuonArgs a) {
     if (!isfinite(scale)) return;
     const uint32_t* first = plan_first(a.plan, a.n, kBlockFirst);
     const uint32_t which = matrix_of(first, a.n, blockIdx.x);
-    const PlanEntry& t = plan_entries(a.plan)[which];
+    const PlanEntry t = plan_entries(a.plan)[which];
     const uint32_t at = blockIdx.x - first[which], bi = at / t.nb, bj = at - bi * t.nb;
-    // the norm: all chunks' sums, in the same order in every block
-    __shared__ double sums[8], lives[8];
-    const uint32_t c0 = plan_first(a.plan, a.n, kChunkFirst)[which], c1 = plan_first(a.plan, a.n, kChunkFirst)[which + 1];
-    double sum = 0, live = 0;
-    for (uint32_t c = c0 + threadIdx.x; c < c1; c += 256) { const double2 s = a.sums[c]; sum += s.x; live += s.y; }
-    sum = warp_sum(sum); live = warp_sum(live);
-    if (threadIdx.x % 32 == 0) { sums[threadIdx.x / 32] = sum; lives[threadIdx.x / 32] = live; }
-    __syncthreads();
-    sum = sums[0]; live = lives[0];
-    for (int w = 1; w < 8; ++w) { sum += sums[w]; live += lives[w]; }
-    if (at == 0 && threadIdx.x == 0) a.live[which] = live > 0;
-    const float inv = (float)((double)kUp / (sqrt(sum) + (double)a.eps));
+    const float inv = a.factor[which];
     const float* m = a.momentum + t.first_block * FTC_STATE_BLOCK;
     __shared__ __align__(16) unsigned char tile[2][kBlockBytes];
-#pragma unroll 8
-    for (uint32_t e = threadIdx.x; e < 128 * 64; e += 256) {
-        const uint32_t r = t.tall ? e % 128 : e / 64, c = t.tall ? e / 128 : e % 64;      // neighbours in memory for neighbouring threads
-        const uint32_t i = bi * 128 + r, j = bj * 64 + c;
-        float v = 0.f;
-        if (i < t.m && j < t.w) {
-            const uint64_t q = t.tall ? (uint64_t)j * t.cols + i : (uint64_t)i * t.cols + j;
-            v = m[q];
-            if (a.nesterov) {
-                const float s = share_at(t, q);
-                if (s > 0.f) v = fmaf(v, a.mu, element(t.grad, t.grad_dtype, q) * s * scale);
-            }
-            v *= inv;
-        }
+    auto value = [&](float v, float g, float s) { return (a.nesterov && s > 0.f ? fmaf(v, a.mu, g * s * scale) : v) * inv; };
+    auto put = [&](uint32_t r, uint32_t c, float v) {
         const __half h = __float2half_rn(v);
         const uint32_t to = piece(r, c / 8) + c % 8 * 2;
         *reinterpret_cast<__half*>(tile[0] + to) = h;
         if (a.split) *reinterpret_cast<__half*>(tile[1] + to) = __float2half_rn(v - __half2float(h));
+    };
+    const bool whole = bi * 128 + 128 <= t.m && bj * 64 + 64 <= t.w;
+    if (whole && t.wide && t.cols % 8 == 0) {
+        // runs of 64 neighbours in 128 rows of memory, or of 128 in 64 (transposed)
+        const uint32_t per = t.tall ? 16 : 8;                    // eights of a run
+#pragma unroll
+        for (uint32_t u = 0; u < 2; ++u) {
+            float v[2][8], g[2][8], s[2][8];
+            uint32_t line[2], run[2];
+#pragma unroll
+            for (uint32_t w = 0; w < 2; ++w) {
+                const uint32_t e = threadIdx.x + (2 * u + w) * 256;
+                line[w] = e / per; run[w] = e % per * 8;
+                const uint64_t q = t.tall ? (uint64_t)(bj * 64 + line[w]) * t.cols + bi * 128 + run[w] : (uint64_t)(bi * 128 + line[w]) * t.cols + bj * 64 + run[w];
+                eight(v[w], m, FTC_F32, q);
+                if (a.nesterov) { eight(g[w], t.grad, t.grad_dtype, q); eight_shares(s[w], t, q); }
+            }
+#pragma unroll
+            for (uint32_t w = 0; w < 2; ++w) {
+                if (t.tall) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) put(run[w] + j, line[w], value(v[w][j], g[w][j], s[w][j]));
+                } else {
+                    __half h[8], l[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float x = value(v[w][j], g[w][j], s[w][j]);
+                        h[j] = __float2half_rn(x); l[j] = __float2half_rn(x - __half2float(h[j]));
+                    }
+                    const uint32_t to = piece(line[w], run[w] / 8);
+                    *reinterpret_cast<uint4*>(tile[0] + to) = *reinterpret_cast<const uint4*>(h);
+                    if (a.split) *reinterpret_cast<uint4*>(tile[1] + to) = *reinterpret_cast<const uint4*>(l);
+                }
+            }
+        }
+    } else {
+        for (uint32_t e0 = threadIdx.x; e0 < 128 * 64; e0 += 2048) {
+            float v[8], g[8], s[8];
+#pragma unroll
+            for (uint32_t w = 0; w < 8; ++w) {
+                const uint32_t e = e0 + w * 256, r = t.tall ? e % 128 : e / 64, c = t.tall ? e / 128 : e % 64, i = bi * 128 + r, j = bj * 64 + c;
+                const bool there = i < t.m && j < t.w;
+                const uint64_t q = t.tall ? (uint64_t)j * t.cols + i : (uint64_t)i * t.cols + j;
+                v[w] = there ? m[q] : 0.f;
+                g[w] = there && a.nesterov ? element(t.grad, t.grad_dtype, q) : 0.f;
+                s[w] = there && a.nesterov ? share_at(t, q) : 0.f;
+            }
+#pragma unroll
+            for (uint32_t w = 0; w < 8; ++w) {
+                const uint32_t e = e0 + w * 256, r = t.tall ? e % 128 : e / 64, c = t.tall ? e / 128 : e % 64;
+                put(r, c, value(v[w], g[w], s[w]));
+            }
+        }
     }
     __syncthreads();
     for (uint32_t s = 0; s <= a.split; ++s) {
@@ -145,12 +242,19 @@ __global__ void __launch_bounds__(256) muon_layout_kernel(MuonArgs a) {
 
 // ---- products ----
 //
-// Persistent blocks of eight warps: one thread copies, one issues matrix instructions, four warps read sums out of tensor memory. A tile
-// is 128 x 256, its sum 256 columns of tensor memory; there are two, so that one tile is read out while the next is multiplied. A stage
-// holds 64 of the inner dimension: 16 KB of the left operand, up to 32 of the right one.
+// Persistent pairs of blocks (clusters of two), 12 warps each. A pair has a tile of 256 x 256: a block holds 128 rows of the left operand and
+// half of the right one's columns, one thread of the first block issues the matrix instructions of both, and each block's tensor memory
+// gets its 128 rows of sums, 256 columns; there are two such halves, so that one tile is read out while the next is multiplied. A stage
+// holds 64 of the inner dimension: 16 KB of each operand in each block.
+//   warp 0   copies of its block's operands
+//   warp 1   first block: matrix instructions; second block: tells the first when its copies have landed
+//   warps 4 .. 11   two teams of four read sums out (a warp reads the 32 lanes of tensor memory that its number modulo 4 gives it), the
+//            first team the left 128 columns, the second the right ones, 64 at a time: what the result needs of A or X comes into the
+//            team's shared memory as a block, is replaced there by the result, and goes out as a block; so does its transpose.
 
-constexpr uint32_t kStages = 4, kStageBytes = 48 * 1024, kOutBytes = 4 * 32 * 33 * 4, kProductThreads = 256;
-constexpr uint32_t kProductSmem = kStages * kStageBytes + kOutBytes + 1024 + 256;
+constexpr uint32_t kStages = 5, kStageBytes = 2 * kBlockBytes, kTeamBytes = 2 * kBlockBytes, kProductThreads = 384;
+constexpr uint32_t kProductSmem = kStages * kStageBytes + 2 * kTeamBytes + 1024 + 256;
+static_assert(kProductSmem <= 227 * 1024, "shared memory of a block");
 enum { kGram, kPoly, kApply, kUpdate };
 
 __device__ __forceinline__ uint32_t smem_of(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -158,26 +262,39 @@ __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) { asm vol
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// Arrives at the barrier of the pair's block `rank`.
+__device__ __forceinline__ void bar_arrive_at(uint32_t bar, uint32_t rank) {
+    asm volatile("{\n\t.reg .b32 there;\n\tmapa.shared::cluster.u32 there, %0, %1;\n\tmbarrier.arrive.release.cluster.shared::cluster.b64 _, [there];\n\t}"
+                 ::"r"(bar), "r"(rank) : "memory");
+}
 // Looks at most 2^22 times (each look may sleep for a while): false if the phase did not end.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
     for (uint32_t i = 0; i < 1u << 22; ++i) {
         uint32_t ok;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
         if (ok) return true;
     }
     return false;
 }
+__device__ __forceinline__ bool all_of_team(uint32_t team, bool ok) {
+    uint32_t all;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"((uint32_t)ok), "r"(3 + team) : "memory");
+    return all;
+}
 __device__ __forceinline__ void copy_in(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void commit_to(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void copy_out(void* to, uint32_t from, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(to), "r"(from), "r"(bytes) : "memory");
+}
+// The barriers of both blocks of a pair get to know when all products issued so far are done.
+__device__ __forceinline__ void commit_to_both(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
 __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t how, bool add) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                  ::"r"(d), "l"(a), "l"(b), "r"(how), "r"((uint32_t)add) : "memory");
 }
 __device__ __forceinline__ void read_32(float* v, uint32_t from) {
@@ -196,40 +313,38 @@ __device__ __forceinline__ uint64_t operand(uint32_t address, uint32_t leading, 
     return (uint64_t)((address & 0x3FFFF) >> 4) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
 
-struct Tile { uint32_t which, i, j; };                           // matrix, block of 128 rows, block of 256 columns
+struct Tile { uint32_t which, i, j; };                           // matrix, blocks of 256 rows and of 256 columns
 
-// Tiles on and below the diagonal: rows 2q and 2q + 1 have q + 1 tiles each, the rows before them q (q + 1).
+// Tiles on and below the diagonal: row i has i + 1.
 __device__ __forceinline__ Tile gram_tile(const uint32_t* first, uint32_t n, uint32_t u) {
     Tile t;
     t.which = matrix_of(first, n, u);
     const uint32_t r = u - __ldg(first + t.which);
-    uint32_t q = (uint32_t)((sqrtf(4.f * (float)r + 1.f) - 1.f) * 0.5f);
-    while (q * (q + 1) > r) --q;
-    while ((q + 1) * (q + 2) <= r) ++q;
-    const uint32_t rest = r - q * (q + 1), second = rest >= q + 1;
-    t.i = 2 * q + second;
-    t.j = rest - second * (q + 1);
+    uint32_t i = (uint32_t)((sqrtf(8.f * (float)r + 1.f) - 1.f) * 0.5f);
+    while (i * (i + 1) / 2 > r) --i;
+    while ((i + 1) * (i + 2) / 2 <= r) ++i;
+    t.i = i;
+    t.j = r - i * (i + 1) / 2;
     return t;
 }
 // All tiles, a column's one after the other: they share the right operand.
 __device__ __forceinline__ Tile apply_tile(const uint32_t* first, uint32_t n, uint32_t u, const PlanEntry* e) {
     Tile t;
     t.which = matrix_of(first, n, u);
-    const uint32_t r = u - __ldg(first + t.which), mb = e[t.which].mb;
-    t.j = r / mb;
-    t.i = r - t.j * mb;
+    const uint32_t r = u - __ldg(first + t.which), rows = (e[t.which].mb + 1) / 2;
+    t.j = r / rows;
+    t.i = r - t.j * rows;
     return t;
 }
 
-__device__ __forceinline__ void pack8(unsigned char* to, const float* v) {       // 8 numbers (times 2^14) as float16
+__device__ __forceinline__ uint4 packed(const float* v) {        // 8 numbers (times 2^14) as float16
     uint4 r;
     uint32_t* w = &r.x;
 #pragma unroll
     for (int i = 0; i < 4; ++i) { const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t*>(&h); }
-    *reinterpret_cast<uint4*>(to) = r;
+    return r;
 }
-__device__ __forceinline__ void unpack8(float* v, const unsigned char* from, bool more) {
-    const uint4 r = *reinterpret_cast<const uint4*>(from);
+__device__ __forceinline__ void unpacked(float* v, uint4 r, bool more) {
     const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -237,128 +352,92 @@ __device__ __forceinline__ void unpack8(float* v, const unsigned char* from, boo
         v[2 * i] = more ? v[2 * i] + f.x : f.x; v[2 * i + 1] = more ? v[2 * i + 1] + f.y : f.y;
     }
 }
-// 32 columns of a row in a block, from piece c on; what float16 leaves over goes to `low`.
-__device__ __forceinline__ void put_32(unsigned char* block, unsigned char* low, uint32_t r, uint32_t c, float* v) {
+__device__ __forceinline__ void rest_of(float* v) {              // what float16 leaves over
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        pack8(block + piece(r, c + q), v + 8 * q);
-        if (low) {
-            float rest[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) rest[i] = v[8 * q + i] - __half2float(__float2half_rn(v[8 * q + i]));
-            pack8(low + piece(r, c + q), rest);
-        }
-    }
-}
-__device__ __forceinline__ void get_32(float* v, const unsigned char* block, const unsigned char* low, uint32_t r, uint32_t c) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        unpack8(v + 8 * q, block + piece(r, c + q), false);
-        if (low) unpack8(v + 8 * q, low + piece(r, c + q), true);
-    }
+    for (int i = 0; i < 8; ++i) v[i] -= __half2float(__float2half_rn(v[i]));
 }
 
-// The sums of a tile's row in 32 columns, as entries of A, B or X, or the weights that they move.
-template <int MODE> __device__ __forceinline__ void finish(const MuonArgs& a, const PlanEntry& t, uint32_t which, uint32_t bi, uint32_t r, uint32_t j0, float* v,
-                                                           const unsigned char* x_in, unsigned char* x_out, float* stage) {
-    const uint32_t i = bi * 128 + r, lane = threadIdx.x % 32;
-    if (MODE == kGram || MODE == kPoly) {
-        const uint32_t jb = j0 / 128;                            // block of 128 columns; above the diagonal: the other tile's
-        if (jb > bi) return;
-        const uint64_t here = (t.a_block + (uint64_t)bi * 2 * t.mb + j0 / 64) * kBlockBytes;
-        unsigned char* out = (MODE == kGram ? a.a : a.b) + here;
-        if (MODE == kGram) {
+// The weights of 32 rows (of the team's warp) and 64 columns of X, whose update a lane has: a row of it (v). Turned in shared memory unless
+// the matrix lies transposed, so that neighbouring lanes have neighbouring weights.
+template <typename W> __device__ __forceinline__ void move_weights(const PlanEntry& t, W* weights, uint32_t i0, uint32_t j0, const float* v, float* turn, float down, float move) {
+    const uint32_t lane = threadIdx.x % 32;
+    if (t.tall) {
+        const uint32_t col = i0 + lane;
 #pragma unroll
-            for (int q = 0; q < 32; ++q) {
-                if (j0 + q == i) { a.diag_a[t.diagonal + i] = v[q] * kDown2; v[q] = 0.f; }
-                v[q] *= kDown;
+        for (uint32_t h = 0; h < 2; ++h) {
+            float p[32];
+#pragma unroll
+            for (uint32_t q = 0; q < 32; ++q) {
+                const uint32_t row = j0 + h * 32 + q;
+                p[q] = row < t.rows && col < t.cols ? to_f32(weights[(uint64_t)row * t.cols + col]) : 0.f;
             }
-        } else {
-            float e[32];
-            get_32(e, a.a + here, a.split ? a.a + a.a_bytes + here : nullptr, r, j0 % 64 / 8);
-            const float* d = a.diag_a + t.diagonal;
-            const float di = d[i];
 #pragma unroll
-            for (int q = 0; q < 32; ++q) {
-                const float dj = d[j0 + q];
-                if (j0 + q == i) {
-                    a.diag_b[t.diagonal + i] = fmaf(kQ5, fmaf(v[q], kDown2, di * di), kQ3 * di);
-                    v[q] = 0.f;
-                } else {
-                    v[q] = fmaf(kQ5 * kDown, v[q], e[q] * fmaf(kQ5, di + dj, kQ3));
-                }
+            for (uint32_t q = 0; q < 32; ++q) {
+                const uint32_t row = j0 + h * 32 + q;
+                if (row >= t.rows || col >= t.cols) continue;
+                const uint64_t at = (uint64_t)row * t.cols + col;
+                const float x = fmaf(p[q], down, v[h * 32 + q] * move);
+                weights[at] = from_f32<W>(x);
+                if (t.master) set_element(t.param, t.param_dtype, at, x);
             }
-        }
-        put_32(out, a.split ? out + a.a_bytes : nullptr, r, j0 % 64 / 8, v);
-        if (jb == bi) return;
-        // the same below: element (j, i), neighbours along i in neighbouring lanes
-        unsigned char* mirror = (MODE == kGram ? a.a : a.b) + (t.a_block + (uint64_t)jb * 2 * t.mb + i / 64) * kBlockBytes;
-#pragma unroll
-        for (int q = 0; q < 32; ++q) {
-            const uint32_t row = (j0 + q) % 128, to = piece(row, i % 64 / 8) + i % 8 * 2;
-            const __half h = __float2half_rn(v[q]);
-            *reinterpret_cast<__half*>(mirror + to) = h;
-            if (a.split) *reinterpret_cast<__half*>(mirror + a.a_bytes + to) = __float2half_rn(v[q] - __half2float(h));
         }
         return;
     }
-    const uint64_t here = (t.x_block + (uint64_t)bi * t.nb + j0 / 64) * kBlockBytes;
-    float e[32];
-    get_32(e, x_in + here, a.split ? x_in + a.x_bytes + here : nullptr, r, j0 % 64 / 8);
-    const float keep = kQ1 + a.diag_b[t.diagonal + i];
+    // row r of the warp's 32 at r * 64, its pieces of four numbers at c ^ r % 8
 #pragma unroll
-    for (int q = 0; q < 32; ++q) v[q] = fmaf(v[q], kDown, keep * e[q]);          // times 2^14
-    if (MODE == kApply) {
-        put_32(x_out + here, a.split ? x_out + a.x_bytes + here : nullptr, r, j0 % 64 / 8, v);
-        return;
-    }
-    const float l = a.lr * t.lr_scale, down = 1.f - l * t.weight_decay, move = -l * kDown;
-    void* const weights = t.master ? static_cast<void*>(t.master) : t.param;
-    const uint32_t dtype = t.master ? FTC_F32 : t.param_dtype;
-    if (!t.tall) {                                               // lanes have rows: turned, so that they have neighbouring columns
+    for (uint32_t c = 0; c < 16; ++c) *reinterpret_cast<float4*>(turn + lane * 64 + ((c ^ (lane & 7)) << 2)) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+    __syncwarp();
 #pragma unroll
-        for (int q = 0; q < 32; ++q) stage[lane * 33 + q] = v[q];
-        __syncwarp();
+    for (uint32_t h = 0; h < 2; ++h) {
+        float p[16][2];
 #pragma unroll
-        for (int q = 0; q < 32; ++q) v[q] = stage[q * 33 + lane];
-        __syncwarp();
-    }
-    const uint32_t i0 = i - lane;
-#pragma unroll 8
-    for (int q = 0; q < 32; ++q) {
-        const uint32_t row = t.tall ? j0 + q : i0 + q, col = t.tall ? i : j0 + lane;
-        if (row < t.rows && col < t.cols) {
-            const uint64_t at = (uint64_t)row * t.cols + col;
-            const float p = fmaf(element(weights, dtype, at), down, v[q] * move);
-            set_element(weights, dtype, at, p);
-            if (t.master) set_element(t.param, t.param_dtype, at, p);
-        }
+        for (uint32_t q = 0; q < 16; ++q)
+#pragma unroll
+            for (uint32_t w = 0; w < 2; ++w) {
+                const uint32_t row = i0 + h * 16 + q, col = j0 + w * 32 + lane;
+                p[q][w] = row < t.rows && col < t.cols ? to_f32(weights[(uint64_t)row * t.cols + col]) : 0.f;
+            }
+#pragma unroll
+        for (uint32_t q = 0; q < 16; ++q)
+#pragma unroll
+            for (uint32_t w = 0; w < 2; ++w) {
+                const uint32_t r = h * 16 + q, row = i0 + r, c = w * 32 + lane, col = j0 + c;
+                if (row >= t.rows || col >= t.cols) continue;
+                const uint64_t at = (uint64_t)row * t.cols + col;
+                const float x = fmaf(p[q][w], down, turn[r * 64 + (((c >> 2) ^ (r & 7)) << 2) + (c & 3)] * move);
+                weights[at] = from_f32<W>(x);
+                if (t.master) set_element(t.param, t.param_dtype, at, x);
+            }
     }
 }
 
-template <int MODE> __global__ void __launch_bounds__(kProductThreads, 1) muon_product_kernel(MuonArgs a, uint32_t tiles, uint32_t side) {
+template <int MODE> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) muon_product_kernel(MuonArgs a, uint32_t tiles, uint32_t side) {
+    namespace cg = cooperative_groups;
     extern __shared__ unsigned char raw[];
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    uint32_t rank;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     unsigned char* const smem = raw + (1024 - (smem_of(raw) & 1023)) % 1024;
-    float* const stage_out = reinterpret_cast<float*>(smem + kStages * kStageBytes);
-    uint64_t* const bars = reinterpret_cast<uint64_t*>(smem + kStages * kStageBytes + kOutBytes);    // full, empty, sums full, sums empty, drained
-    uint32_t* const words = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 5);                     // tensor memory, gave up
-    const uint32_t full = smem_of(bars), empty = full + 8 * kStages, sum_full = empty + 8 * kStages, sum_empty = sum_full + 16, drained = sum_empty + 16;
+    uint64_t* const bars = reinterpret_cast<uint64_t*>(smem + kStages * kStageBytes + 2 * kTeamBytes);
+    // full, landed in the second block, empty (each stage); sums full, sums empty (two each); teams' blocks (two); drained
+    const uint32_t full = smem_of(bars), landed = full + 8 * kStages, empty = landed + 8 * kStages, sum_full = empty + 8 * kStages, sum_empty = sum_full + 16,
+                   team_full = sum_empty + 16, drained = team_full + 16;
+    uint32_t* const words = reinterpret_cast<uint32_t*>(bars + 3 * kStages + 7);                     // tensor memory, gave up
     if (threadIdx.x == 0) {
-        for (uint32_t s = 0; s < kStages; ++s) { bar_init(full + 8 * s, 1); bar_init(empty + 8 * s, 1); }
-        for (uint32_t s = 0; s < 2; ++s) { bar_init(sum_full + 8 * s, 1); bar_init(sum_empty + 8 * s, 4); }
+        for (uint32_t s = 0; s < kStages; ++s) { bar_init(full + 8 * s, 1); bar_init(landed + 8 * s, 1); bar_init(empty + 8 * s, 1); }
+        for (uint32_t s = 0; s < 2; ++s) { bar_init(sum_full + 8 * s, 1); bar_init(sum_empty + 8 * s, 16); bar_init(team_full + 8 * s, 1); }
         bar_init(drained, 1);
         words[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_of(words)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_of(words)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
+    cg::this_cluster().sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const uint32_t tmem = words[0];
+    const uint32_t tmem = words[0], pairs = gridDim.x / 2, pair = blockIdx.x / 2;
     wait_for_earlier_kernel();
     later_kernel_may_start();
     const float scale = a.grad_scale ? *a.grad_scale : 1.f;
@@ -367,60 +446,67 @@ template <int MODE> __global__ void __launch_bounds__(kProductThreads, 1) muon_p
     const uint32_t* const first = plan_first(a.plan, a.n, MODE <= kPoly ? kGramFirst : kApplyFirst);
     const uint32_t segments = a.split ? 3 : 1;
     auto tile_of = [&](uint32_t u) { return MODE <= kPoly ? gram_tile(first, a.n, u) : apply_tile(first, a.n, u, entries); };
+    // a tile's steps of 64 and its columns: 256, or 128 where there are no more (in the apply kernels up to 64 of them are nobody's)
+    auto steps_of = [&](const PlanEntry& t) { return segments * (MODE == kGram ? t.nb : t.kb); };
+    auto columns_of = [&](const PlanEntry& t, const Tile& q) { return MODE <= kPoly ? (t.mb > 2 * q.j + 1 ? 256u : 128u) : (t.nb > 4 * q.j + 2 ? 256u : 128u); };
     const unsigned char* const x_in = a.x[side];
     bool ok = true;
 
     if (work && warp == 0 && lane == 0) {                        // copies
         uint32_t it = 0;
-        for (uint32_t u = blockIdx.x; u < tiles && ok; u += gridDim.x) {
+        for (uint32_t u = pair; u < tiles && ok; u += pairs) {
             const Tile tile = tile_of(u);
             const PlanEntry& t = entries[tile.which];
-            const uint32_t steps = MODE == kGram ? t.nb : t.kb;
-            const uint32_t right = MODE <= kPoly ? min(2u, t.mb - 2 * tile.j) : min(4u, t.nb - 4 * tile.j);
-            const uint32_t bytes = kBlockBytes + right * (MODE <= kPoly ? kBlockBytes : kBlockBytes / 2);
+            const uint32_t steps = MODE == kGram ? t.nb : t.kb, left_row = 2 * tile.i + rank, half = columns_of(t, tile) / 2;      // columns of this block
+            const bool has_left = left_row < t.mb;
+            // right operand of a symmetric product: rows half * rank .. of 256; of the others: blocks of 64 columns
+            const uint32_t right_row = 2 * tile.j + (half == 128 ? rank : 0), right_in = half == 128 ? 0 : rank * (kBlockBytes / 2);
+            const uint32_t right_block = 4 * tile.j + rank * (half / 64), right_blocks = MODE <= kPoly ? 0 : min(half / 64, t.nb > right_block ? t.nb - right_block : 0u);
+            const uint32_t bytes = (has_left ? kBlockBytes : 0) + (MODE <= kPoly ? half * 128 : right_blocks * (kBlockBytes / 2));
             for (uint32_t g = 0; g < segments && ok; ++g) {
                 const unsigned char* l = (MODE == kGram ? x_in : MODE == kPoly ? a.a : a.b) + (g == 2 ? (MODE == kGram ? a.x_bytes : a.a_bytes) : 0);
                 const unsigned char* r = (MODE == kPoly ? a.a : x_in) + (g == 1 ? (MODE == kPoly ? a.a_bytes : a.x_bytes) : 0);
+                l += MODE == kGram ? (t.x_block + (uint64_t)left_row * t.nb) * kBlockBytes : (t.a_block + (uint64_t)left_row * 2 * t.mb) * kBlockBytes;
+                r += MODE == kGram ? (t.x_block + (uint64_t)right_row * t.nb) * kBlockBytes + right_in
+                   : MODE == kPoly ? (t.a_block + (uint64_t)right_row * 2 * t.mb) * kBlockBytes + right_in : (t.x_block + right_block) * kBlockBytes;
                 for (uint32_t s = 0; s < steps; ++s, ++it) {
                     const uint32_t slot = it % kStages, to = smem_of(smem) + slot * kStageBytes, bar = full + 8 * slot;
                     if (it >= kStages && !(ok = bar_wait(empty + 8 * slot, (it / kStages - 1) & 1))) break;
                     bar_expect(bar, bytes);
-                    if (MODE == kGram) {
-                        copy_in(to, l + (t.x_block + (uint64_t)tile.i * t.nb + s) * kBlockBytes, kBlockBytes, bar);
-                        for (uint32_t q = 0; q < right; ++q)
-                            copy_in(to + (1 + q) * kBlockBytes, r + (t.x_block + (uint64_t)(2 * tile.j + q) * t.nb + s) * kBlockBytes, kBlockBytes, bar);
-                    } else {
-                        copy_in(to, l + (t.a_block + (uint64_t)tile.i * 2 * t.mb + s) * kBlockBytes, kBlockBytes, bar);
-                        if (MODE == kPoly)
-                            for (uint32_t q = 0; q < right; ++q)
-                                copy_in(to + (1 + q) * kBlockBytes, r + (t.a_block + (uint64_t)(2 * tile.j + q) * 2 * t.mb + s) * kBlockBytes, kBlockBytes, bar);
-                        else                                     // 64 rows of X (half a block), up to four blocks of 64 columns
-                            for (uint32_t q = 0; q < right; ++q)
-                                copy_in(to + kBlockBytes + q * (kBlockBytes / 2),
-                                        r + (t.x_block + (uint64_t)(s / 2) * t.nb + 4 * tile.j + q) * kBlockBytes + s % 2 * (kBlockBytes / 2), kBlockBytes / 2, bar);
-                    }
+                    if (has_left) copy_in(to, l + (uint64_t)s * kBlockBytes, kBlockBytes, bar);
+                    if (MODE <= kPoly) copy_in(to + kBlockBytes, r + (uint64_t)s * kBlockBytes, half * 128, bar);
+                    else                                         // 64 rows of X (half a block)
+                        for (uint32_t q = 0; q < right_blocks; ++q)
+                            copy_in(to + kBlockBytes + q * (kBlockBytes / 2), r + ((uint64_t)(s / 2) * t.nb + q) * kBlockBytes + s % 2 * (kBlockBytes / 2), kBlockBytes / 2, bar);
                 }
             }
         }
         if (!ok) {                                               // copies in flight end before the block does
             words[1] = 1;
-            for (uint32_t s = 0; s < kStages && s < it; ++s) bar_wait(full + 8 * s, ((it - 1 - s) / kStages) & 1);
+            for (uint32_t s = 0; s < kStages && s < it; ++s) { const uint32_t n = it - 1 - s; bar_wait(full + 8 * (n % kStages), (n / kStages) & 1); }
         }
-    } else if (work && warp == 1 && lane == 0) {                 // matrix instructions
+    } else if (work && warp == 1 && lane == 0) {
         uint32_t it = 0, n = 0;
-        for (uint32_t u = blockIdx.x; u < tiles && ok; u += gridDim.x, ++n) {
+        for (uint32_t u = pair; u < tiles && ok; u += pairs, ++n) {
             const Tile tile = tile_of(u);
             const PlanEntry& t = entries[tile.which];
-            const uint32_t steps = segments * (MODE == kGram ? t.nb : t.kb);
-            const uint32_t columns = MODE <= kPoly ? min(2u, t.mb - 2 * tile.j) * 128 : min(4u, t.nb - 4 * tile.j) * 64;
-            // sums in float32, operands float16, the right one along its columns in the apply kernels
-            const uint32_t how = 1u << 4 | (MODE >= kApply ? 1u << 16 : 0u) | columns / 8 << 17 | 128u / 16 << 24;
+            const uint32_t steps = steps_of(t);
+            if (rank) {                                          // the second block's copies
+                for (uint32_t s = 0; s < steps; ++s, ++it) {
+                    const uint32_t slot = it % kStages;
+                    if (!(ok = bar_wait(full + 8 * slot, (it / kStages) & 1))) break;
+                    bar_arrive_at(landed + 8 * slot, 0);
+                }
+                continue;
+            }
+            // sums in float32, operands float16, the right one along its columns in the apply kernels, 256 rows
+            const uint32_t how = 1u << 4 | (MODE >= kApply ? 1u << 16 : 0u) | columns_of(t, tile) / 8 << 17 | 256u / 16 << 24;
             const uint32_t sum = tmem + (n & 1) * 256;
             if (n >= 2 && !(ok = bar_wait(sum_empty + 8 * (n & 1), (n / 2 - 1) & 1))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             for (uint32_t s = 0; s < steps; ++s, ++it) {
                 const uint32_t slot = it % kStages, at = smem_of(smem) + slot * kStageBytes;
-                if (!(ok = bar_wait(full + 8 * slot, (it / kStages) & 1))) break;
+                if (!(ok = bar_wait(full + 8 * slot, (it / kStages) & 1) && bar_wait(landed + 8 * slot, (it / kStages) & 1))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
                 for (uint32_t k = 0; k < 4; ++k) {               // 16 of the inner dimension: 32 bytes along a row, 16 rows of 128 bytes
@@ -428,42 +514,165 @@ template <int MODE> __global__ void __launch_bounds__(kProductThreads, 1) muon_p
                     const uint64_t r = MODE <= kPoly ? operand(at + kBlockBytes + k * 32, 16, 1024) : operand(at + kBlockBytes + k * 2048, kBlockBytes / 2, 1024);
                     multiply(sum, l, r, how, s || k);
                 }
-                commit_to(empty + 8 * slot);
+                commit_to_both(empty + 8 * slot);
             }
-            if (ok) commit_to(sum_full + 8 * (n & 1));
+            if (ok) commit_to_both(sum_full + 8 * (n & 1));
         }
         if (!ok) {
             words[1] = 1;
-            commit_to(drained);                                  // products in flight end before the tensor memory is given back
-            bar_wait(drained, 0);
+            if (!rank) {                                         // products in flight end before the tensor memory is given back
+                asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(drained) : "memory");
+                bar_wait(drained, 0);
+            }
         }
     } else if (work && warp >= 4) {                              // sums
-        const uint32_t quarter = warp - 4, r = quarter * 32 + lane;
-        uint32_t n = 0;
-        for (uint32_t u = blockIdx.x; u < tiles; u += gridDim.x, ++n) {
+        const uint32_t team = (warp - 4) / 4, quarter = warp & 3, r = quarter * 32 + lane;
+        unsigned char* const mine = smem + kStages * kStageBytes + team * kTeamBytes;
+        unsigned char* const other = mine + kBlockBytes;         // the transpose, or the low numbers
+        const uint32_t ready = team_full + 8 * team;
+        const bool leads = quarter == 0 && lane == 0;
+        uint32_t n = 0, blocks = 0;
+        for (uint32_t u = pair; u < tiles && ok; u += pairs, ++n) {
             const Tile tile = tile_of(u);
             const PlanEntry& t = entries[tile.which];
-            ok = __all_sync(0xFFFFFFFFu, bar_wait(sum_full + 8 * (n & 1), (n / 2) & 1));
-            if (!ok) { if (lane == 0) words[1] = 1; break; }
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t columns = MODE <= kPoly ? min(2u, t.mb - 2 * tile.j) * 128 : min(4u, t.nb - 4 * tile.j) * 64;
-            const bool wanted = MODE != kUpdate || a.live[tile.which];
-            for (uint32_t c = 0; c < columns && wanted; c += 32) {
-                float v[32];
-                read_32(v, tmem + (n & 1) * 256 + (quarter * 32 << 16) + c);
-                finish<MODE>(a, t, tile.which, tile.i, r, tile.j * 256 + c, v, x_in, a.x[side ^ 1], stage_out + quarter * 32 * 33);
+            const uint32_t bi = 2 * tile.i + rank, i = bi * 128 + r;
+            // blocks of 64 columns of this team: none above the diagonal, none beyond the edges
+            const uint32_t cb0 = 4 * tile.j + 2 * team, edge = MODE <= kPoly ? 2 * min(t.mb, bi + 1) : t.nb;
+            uint32_t wanted = bi < t.mb && cb0 < edge ? min(2u, edge - cb0) : 0;
+            if (MODE == kUpdate && !a.live[tile.which]) wanted = 0;
+            for (uint32_t b = 0; b < max(wanted, 1u) && ok; ++b, blocks += wanted ? 1 : 0) {
+                const uint32_t cb = cb0 + b, j0 = cb * 64;
+                const uint64_t here = MODE <= kPoly ? (t.a_block + (uint64_t)bi * 2 * t.mb + cb) * kBlockBytes : (t.x_block + (uint64_t)bi * t.nb + cb) * kBlockBytes;
+                if (wanted && leads) {                           // once the last block has left, the next one may come
+                    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    if (MODE == kGram) bar_expect(ready, 0);
+                    else {
+                        const unsigned char* from = (MODE == kPoly ? a.a : x_in) + here;
+                        bar_expect(ready, (a.split ? 2 : 1) * kBlockBytes);
+                        copy_in(smem_of(mine), from, kBlockBytes, ready);
+                        if (a.split) copy_in(smem_of(other), from + (MODE == kPoly ? a.a_bytes : a.x_bytes), kBlockBytes, ready);
+                    }
+                }
+                ok = (b || bar_wait(sum_full + 8 * (n & 1), (n / 2) & 1)) && (!wanted || bar_wait(ready, blocks & 1));
+                ok = all_of_team(team, ok);                      // one goes on only if all do
+                if (!ok || !wanted) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                float v[64];
+                read_32(v, tmem + (n & 1) * 256 + (quarter * 32 << 16) + team * 128 + b * 64);
+                read_32(v + 32, tmem + (n & 1) * 256 + (quarter * 32 << 16) + team * 128 + b * 64 + 32);
+                if (MODE == kGram) {
+#pragma unroll
+                    for (int q = 0; q < 64; ++q) {
+                        if (j0 + q == i) { a.diag_a[t.diagonal + i] = v[q] * kDown2; v[q] = 0.f; }
+                        v[q] *= kDown;
+                    }
+                } else {
+                    const float* d = a.diag_a + t.diagonal;
+                    const float di = MODE == kPoly ? d[i] : 0.f, keep = MODE == kPoly ? 0.f : kQ1 + a.diag_b[t.diagonal + i];
+#pragma unroll
+                    for (uint32_t c = 0; c < 8; ++c) {
+                        float e[8];
+                        unpacked(e, *reinterpret_cast<const uint4*>(mine + piece(r, c)), false);
+                        if (a.split) unpacked(e, *reinterpret_cast<const uint4*>(other + piece(r, c)), true);
+                        if (MODE == kPoly) {
+                            const float4 d0 = *reinterpret_cast<const float4*>(d + j0 + 8 * c), d1 = *reinterpret_cast<const float4*>(d + j0 + 8 * c + 4);
+                            const float dj[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
+#pragma unroll
+                            for (uint32_t q = 0; q < 8; ++q) {
+                                float& x = v[8 * c + q];
+                                if (j0 + 8 * c + q == i) {
+                                    a.diag_b[t.diagonal + i] = fmaf(kQ5, fmaf(x, kDown2, di * di), kQ3 * di);
+                                    x = 0.f;
+                                } else {
+                                    x = fmaf(kQ5 * kDown, x, e[q] * fmaf(kQ5, di + dj[q], kQ3));
+                                }
+                            }
+                        } else {
+#pragma unroll
+                            for (uint32_t q = 0; q < 8; ++q) v[8 * c + q] = fmaf(v[8 * c + q], kDown, keep * e[q]);      // times 2^14
+                        }
+                    }
+                }
+                if (MODE == kUpdate) {
+                    asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory");        // all have read X
+                    const float l = a.lr * t.lr_scale, down = 1.f - l * t.weight_decay, move = -l * kDown;
+                    float* turn = reinterpret_cast<float*>(mine) + quarter * 32 * 64;
+                    if (t.master) move_weights(t, t.master, i - lane, j0, v, turn, down, move);
+                    else if (t.param_dtype == FTC_F32) move_weights(t, static_cast<float*>(t.param), i - lane, j0, v, turn, down, move);
+                    else if (t.param_dtype == FTC_BF16) move_weights(t, static_cast<__nv_bfloat16*>(t.param), i - lane, j0, v, turn, down, move);
+                    else move_weights(t, static_cast<__half*>(t.param), i - lane, j0, v, turn, down, move);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");         // before the next copy into it
+                    asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory");
+                    continue;
+                }
+#pragma unroll
+                for (uint32_t c = 0; c < 8; ++c) {
+                    *reinterpret_cast<uint4*>(mine + piece(r, c)) = packed(v + 8 * c);
+                    if (a.split) {
+                        float x[8];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) x[q] = v[8 * c + q];
+                        rest_of(x);
+                        *reinterpret_cast<uint4*>(other + piece(r, c)) = packed(x);
+                    }
+                }
+                unsigned char* const out = MODE == kGram ? a.a : MODE == kPoly ? a.b : a.x[side ^ 1];
+                const uint64_t low = MODE <= kPoly ? a.a_bytes : a.x_bytes;
+                const bool twice = MODE <= kPoly && cb / 2 < bi;                         // below the diagonal: the transpose too
+                // element (j, i): 64 rows, two blocks of 64 columns, each half a block
+                const uint64_t there = twice ? (t.a_block + (uint64_t)(cb / 2) * 2 * t.mb + 2 * bi) * kBlockBytes + cb % 2 * (kBlockBytes / 2) : 0;
+                auto turned = [&](unsigned char* to, bool lower) {
+                    unsigned char* const half = to + r / 64 * (kBlockBytes / 2);
+#pragma unroll
+                    for (uint32_t q = 0; q < 64; ++q) {
+                        const __half h = __float2half_rn(v[q]);
+                        *reinterpret_cast<__half*>(half + piece(q, r % 64 / 8) + r % 8 * 2) = lower ? __float2half_rn(v[q] - __half2float(h)) : h;
+                    }
+                };
+                if (twice && !a.split) turned(other, false);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory");
+                if (leads) {
+                    copy_out(out + here, smem_of(mine), kBlockBytes);
+                    if (a.split) copy_out(out + low + here, smem_of(other), kBlockBytes);
+                    else if (twice)
+                        for (uint32_t h = 0; h < 2; ++h) copy_out(out + there + h * kBlockBytes, smem_of(other) + h * (kBlockBytes / 2), kBlockBytes / 2);
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                }
+                if (twice && a.split) {                          // both of the transpose's numbers, once theirs have left
+                    if (leads) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory");
+                    turned(mine, false);
+                    turned(other, true);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory");
+                    if (leads) {
+                        for (uint32_t h = 0; h < 2; ++h) {
+                            copy_out(out + there + h * kBlockBytes, smem_of(mine) + h * (kBlockBytes / 2), kBlockBytes / 2);
+                            copy_out(out + low + there + h * kBlockBytes, smem_of(other) + h * (kBlockBytes / 2), kBlockBytes / 2);
+                        }
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
+                }
             }
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) bar_arrive(sum_empty + 8 * (n & 1));
+            if (ok) {                                            // the first block multiplies for both
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive_at(sum_empty + 8 * (n & 1), 0);
+            }
+        }
+        if (leads) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        if (!ok) {
+            if (lane == 0) words[1] = 1;
+            if (leads) bar_wait(ready, blocks & 1);              // a copy that may be in flight
         }
     }
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
+    cg::this_cluster().sync();                                   // neither block's memory goes before the other is done with it
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     if (threadIdx.x == 0 && *reinterpret_cast<volatile uint32_t*>(words + 1)) *a.word = 1;
-    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
 template <int MODE> static cudaError_t product(const MuonArgs& a, uint32_t tiles, uint32_t side, int sms, cudaStream_t st) {
@@ -473,7 +682,8 @@ template <int MODE> static cudaError_t product(const MuonArgs& a, uint32_t tiles
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t how{};
-    how.gridDim = dim3(tiles < (uint32_t)sms ? tiles : (uint32_t)sms); how.blockDim = dim3(kProductThreads); how.dynamicSmemBytes = kProductSmem;
+    const uint32_t most = (uint32_t)sms / 2;
+    how.gridDim = dim3(2 * (tiles < most ? tiles : most)); how.blockDim = dim3(kProductThreads); how.dynamicSmemBytes = kProductSmem;
     how.stream = st; how.attrs = &early; how.numAttrs = 1;
     return cudaLaunchKernelEx(&how, muon_product_kernel<MODE>, a, tiles, side);
 }
@@ -481,6 +691,7 @@ template <int MODE> static cudaError_t product(const MuonArgs& a, uint32_t tiles
 cudaError_t launch_muon(const MuonArgs& a, int sms, cudaStream_t st) {
     muon_momentum_kernel<<<a.chunks, 256, 0, st>>>(a);
     cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) e = launch_second(muon_norm_kernel, a.n, 256, st, a);
     if (e == cudaSuccess) e = launch_second(muon_layout_kernel, a.x_blocks, 256, st, a);
     for (uint32_t s = 0; s < a.steps && e == cudaSuccess; ++s) {
         e = product<kGram>(a, a.gram_tiles, s & 1, sms, st);
