@@ -41,11 +41,12 @@ __device__ __forceinline__ int32_t token_at(const void* tokens, uint32_t bits, u
     return t < V ? (int32_t)t : -1;
 }
 
-// ---- the plan of matrices: header, entries, then (n + 1 numbers each) where a matrix's chunks, blocks and tiles begin ----
+// ---- the plan of matrices: header, entries, then the matrix of each chunk, block and tile ----
 
 constexpr uint64_t kPlanMagic = 0x316E4C5054435446ull;
-constexpr uint32_t kMuonChunk = 2048;                            // elements of a block of the momentum kernel
-struct PlanHead { uint64_t magic, n_blocks, x_blocks, a_blocks, diagonals; uint32_t n, chunks, gram_tiles, apply_tiles; uint64_t pad; };
+constexpr uint32_t kMuonChunk = 4096;                            // elements of a block of the momentum kernel
+enum { kChunks, kBlocks, kGramTiles, kApplyTiles, kItems4 };
+struct PlanHead { uint64_t magic, n_blocks, a_blocks, diagonals; uint32_t items[kItems4], n, pad[3]; };
 struct PlanEntry {
     void* param; float* master; const void* grad; const uint32_t* status;
     uint64_t n, first_block, x_block, a_block, diagonal;         // x_block, a_block: in blocks of 128 x 64 float16; diagonal: in numbers
@@ -53,25 +54,23 @@ struct PlanEntry {
     uint8_t param_dtype, grad_dtype, tall, k_shift;
     float lr_scale, weight_decay;
     uint32_t m, w, mb, nb, kb, wide;                             // X is m x w (m <= w): mb blocks of 128 rows, nb of 64 columns; A: kb of 64 columns. wide: addresses allow eights
+    uint32_t first[kItems4];                                     // where its chunks, blocks, tiles begin
+    uint64_t pad;
 };
-static_assert(sizeof(PlanHead) == 64 && sizeof(PlanEntry) == 120, "plan layout");
+static_assert(sizeof(PlanHead) == 64 && sizeof(PlanEntry) == 144, "plan layout");
 __host__ __device__ inline const PlanEntry* plan_entries(const void* p) {
     return reinterpret_cast<const PlanEntry*>(static_cast<const char*>(p) + sizeof(PlanHead));
 }
-enum { kChunkFirst, kBlockFirst, kGramFirst, kApplyFirst, kFirsts };
-__host__ __device__ inline const uint32_t* plan_first(const void* p, uint32_t n, int which) {
-    return reinterpret_cast<const uint32_t*>(plan_entries(p) + n) + (size_t)which * (n + 1);
-}
 
 struct MuonArgs {
-    const void* plan; uint32_t n;
+    const void* plan; const uint32_t* maps[kItems4]; uint32_t n;
     float* momentum; const float* grad_scale;
     uint32_t* word;                              // first of the workspace: not 0 once a wait has given up
     double2* sums; uint32_t* live; float* factor; // [chunks]: squares of U, messages delivered; [n]: was anything delivered, 2^14 / (|U| + eps)
     float *diag_a, *diag_b;
     unsigned char *x[2], *a, *b;                 // blocks of 128 x 64 float16; with two numbers for each, the low ones x_bytes / a_bytes further on
     uint64_t x_bytes, a_bytes;
-    uint32_t chunks, x_blocks, gram_tiles, apply_tiles, steps, nesterov, split;
+    uint32_t items[kItems4], steps, nesterov, split;
     float lr, mu, eps;
 };
 cudaError_t launch_muon(const MuonArgs& a, int sms, cudaStream_t st);

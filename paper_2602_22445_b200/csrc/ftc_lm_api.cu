@@ -1,4 +1,5 @@
 // extern "C" boundary of the embedding, the token log probabilities and the orthogonalised update: argument checks, workspaces, the plan.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include "ftc_lm.cuh"
@@ -50,7 +51,7 @@ bool count_matrices(const ftc_matrix_t* q, uint32_t n, PlanHead& h) {
     h = PlanHead{};
     if ((!q && n) || n > (1u << 20)) return false;
     h.magic = kPlanMagic; h.n = n;
-    uint64_t chunks = 0, gram = 0, apply = 0;
+    uint64_t chunks = 0, blocks = 0, gram = 0, apply = 0;
     for (uint32_t i = 0; i < n; ++i) {
         const ftc_param_t& t = q[i].tensor;
         const uint64_t rows = q[i].rows, cols = q[i].cols, m = rows < cols ? rows : cols, w = rows < cols ? cols : rows;
@@ -61,27 +62,27 @@ bool count_matrices(const ftc_matrix_t* q, uint32_t n, PlanHead& h) {
         if (t.status && (t.k == 0 || t.k > (1u << 30))) return false;
         const uint64_t mb = (m + 127) / 128, nb = (w + 63) / 64, mb2 = (mb + 1) / 2;
         h.n_blocks += (t.n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK;
-        h.x_blocks += mb * nb; h.a_blocks += mb * 2 * mb; h.diagonals += mb * 128;
+        blocks += mb * nb; h.a_blocks += mb * 2 * mb; h.diagonals += mb * 128;
         chunks += (t.n + kMuonChunk - 1) / kMuonChunk;
         gram += mb2 * (mb2 + 1) / 2;
         apply += mb2 * ((nb + 3) / 4);
-        if (h.n_blocks > (1ull << 32) || h.x_blocks > 0x7FFFFFFFull || h.a_blocks > 0x7FFFFFFFull || chunks > 0x7FFFFFFFull || gram > 0x7FFFFFFFull) return false;
+        if (h.n_blocks > (1ull << 32) || blocks > 0x7FFFFFFFull || h.a_blocks > 0x7FFFFFFFull || chunks > 0x7FFFFFFFull || gram > 0x7FFFFFFFull || apply > 0x7FFFFFFFull) return false;
     }
-    h.chunks = (uint32_t)chunks; h.gram_tiles = (uint32_t)gram; h.apply_tiles = (uint32_t)apply;
+    h.items[kChunks] = (uint32_t)chunks; h.items[kBlocks] = (uint32_t)blocks; h.items[kGramTiles] = (uint32_t)gram; h.items[kApplyTiles] = (uint32_t)apply;
     return true;
 }
 size_t plan_bytes(const PlanHead& h) {
-    return sizeof(PlanHead) + (size_t)h.n * sizeof(PlanEntry) + rounded((size_t)kFirsts * (h.n + 1) * 4, 8);
+    return sizeof(PlanHead) + (size_t)h.n * sizeof(PlanEntry) + rounded(((size_t)h.items[kChunks] + h.items[kBlocks] + h.items[kGramTiles] + h.items[kApplyTiles] + h.n) * 4, 8);
 }
 
 struct MuonLayout { size_t sums, live, factor, diag_a, diag_b, x0, x1, a, b, x_bytes, a_bytes, total; };
 MuonLayout muon_layout(const PlanHead& h, uint32_t products) {
     const size_t block = 128 * 64 * 2, numbers = products == 32 ? 2 : 1;
     MuonLayout l{};
-    l.x_bytes = h.x_blocks * block; l.a_bytes = h.a_blocks * block;
+    l.x_bytes = h.items[kBlocks] * block; l.a_bytes = h.a_blocks * block;
     size_t at = 1024;
     auto take = [&](size_t bytes) { const size_t here = at; at = rounded(at + bytes, 256); return here; };
-    l.sums = take((size_t)h.chunks * 16); l.live = take((size_t)h.n * 4); l.factor = take((size_t)h.n * 4);
+    l.sums = take((size_t)h.items[kChunks] * 16); l.live = take((size_t)h.n * 4); l.factor = take((size_t)h.n * 4);
     l.diag_a = take(h.diagonals * 4); l.diag_b = take(h.diagonals * 4);
     l.x0 = take(l.x_bytes * numbers); l.x1 = take(l.x_bytes * numbers); l.a = take(l.a_bytes * numbers); l.b = take(l.a_bytes * numbers);
     l.total = at;
@@ -174,8 +175,6 @@ int ftc_muon_plan_build(const ftc_matrix_t* h_matrices, uint32_t n, void* h_plan
     std::memset(h_plan, 0, plan_bytes(h));
     *static_cast<PlanHead*>(h_plan) = h;
     PlanEntry* e = const_cast<PlanEntry*>(plan_entries(h_plan));
-    uint32_t* first[kFirsts];
-    for (int w = 0; w < kFirsts; ++w) first[w] = const_cast<uint32_t*>(plan_first(h_plan, n, w));
     uint64_t blocks = 0, x = 0, a = 0, diagonal = 0;
     for (uint32_t i = 0; i < n; ++i) {
         const ftc_param_t& t = h_matrices[i].tensor;
@@ -188,12 +187,25 @@ int ftc_muon_plan_build(const ftc_matrix_t* h_matrices, uint32_t n, void* h_plan
         q.mb = (q.m + 127) / 128; q.nb = (q.w + 63) / 64; q.kb = (q.m + 63) / 64;
         q.first_block = blocks; q.x_block = x; q.a_block = a; q.diagonal = diagonal;
         blocks += (t.n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK; x += (uint64_t)q.mb * q.nb; a += (uint64_t)q.mb * 2 * q.mb; diagonal += q.mb * 128;
-        const uint32_t mb2 = (q.mb + 1) / 2;
         q.wide = aligned(t.grad, 16);
-        first[kChunkFirst][i + 1] = first[kChunkFirst][i] + (uint32_t)((t.n + kMuonChunk - 1) / kMuonChunk);
-        first[kBlockFirst][i + 1] = (uint32_t)x;
-        first[kGramFirst][i + 1] = first[kGramFirst][i] + mb2 * (mb2 + 1) / 2;
-        first[kApplyFirst][i + 1] = first[kApplyFirst][i] + mb2 * ((q.nb + 3) / 4);
+    }
+    // The maps. Tiles of many steps come first, so that the last ones to run are short.
+    uint32_t* map = reinterpret_cast<uint32_t*>(e + n);
+    uint32_t* const order = map + h.items[kChunks] + h.items[kBlocks] + h.items[kGramTiles] + h.items[kApplyTiles];      // room for the sorting
+    for (uint32_t i = 0; i < n; ++i) order[i] = i;
+    for (int w = 0; w < kItems4; ++w) {
+        if (w == kGramTiles) std::sort(order, order + n, [e](uint32_t i, uint32_t j) { return e[i].nb != e[j].nb ? e[i].nb > e[j].nb : i < j; });
+        if (w == kApplyTiles) std::sort(order, order + n, [e](uint32_t i, uint32_t j) { return e[i].kb != e[j].kb ? e[i].kb > e[j].kb : i < j; });
+        uint32_t at = 0;
+        for (uint32_t o = 0; o < n; ++o) {
+            const uint32_t i = order[o];
+            PlanEntry& q = e[i];
+            const uint32_t mb2 = (q.mb + 1) / 2;
+            const uint32_t count = w == kChunks ? (uint32_t)((q.n + kMuonChunk - 1) / kMuonChunk) : w == kBlocks ? q.mb * q.nb : w == kGramTiles ? mb2 * (mb2 + 1) / 2 : mb2 * ((q.nb + 3) / 4);
+            q.first[w] = at;
+            for (const uint32_t end = at + count; at < end; ++at) map[at] = i;
+        }
+        map += at;
     }
     return FTC_OK;
 }
@@ -227,7 +239,8 @@ int ftc_muon_step(const ftc_muon_t* hyper, const void* h_plan, const void* d_pla
     a.sums = reinterpret_cast<double2*>(ws + l.sums); a.live = reinterpret_cast<uint32_t*>(ws + l.live); a.factor = reinterpret_cast<float*>(ws + l.factor);
     a.diag_a = reinterpret_cast<float*>(ws + l.diag_a); a.diag_b = reinterpret_cast<float*>(ws + l.diag_b);
     a.x[0] = ws + l.x0; a.x[1] = ws + l.x1; a.a = ws + l.a; a.b = ws + l.b; a.x_bytes = l.x_bytes; a.a_bytes = l.a_bytes;
-    a.chunks = h->chunks; a.x_blocks = (uint32_t)h->x_blocks; a.gram_tiles = h->gram_tiles; a.apply_tiles = h->apply_tiles;
+    const uint32_t* map = reinterpret_cast<const uint32_t*>(plan_entries(d_plan) + h->n);
+    for (int w = 0; w < kItems4; ++w) { a.items[w] = h->items[w]; a.maps[w] = map; map += h->items[w]; }
     a.steps = hyper->steps; a.nesterov = hyper->nesterov; a.split = hyper->products == 32;
     a.lr = (float)hyper->lr; a.mu = (float)hyper->momentum; a.eps = (float)hyper->eps;
     return status(launch_muon(a, sms, static_cast<cudaStream_t>(cuda_stream)));

@@ -14,6 +14,7 @@
 // Matrices lie in the workspace in blocks of 128 rows x 64 columns (16 KB), their 16-byte pieces in the order that the tensor cores read
 // (piece c of row r at c ^ r % 8): a block is one contiguous copy, whichever way a product reads it, and edges are zeros.
 #include <cooperative_groups.h>
+#include "ftc_f32x2.cuh"
 #include "ftc_lm.cuh"
 
 namespace ftc {
@@ -21,16 +22,6 @@ namespace ftc {
 constexpr float kQ1 = 3.4445f, kQ3 = -4.7750f, kQ5 = 2.0315f;
 constexpr float kUp = 16384.f, kDown = 1.f / 16384.f, kDown2 = kDown * kDown;    // 2^14
 constexpr uint32_t kBlockBytes = 128 * 64 * 2;
-
-// The matrix whose run item u is in: first[i] <= u < first[i + 1].
-__device__ __forceinline__ uint32_t matrix_of(const uint32_t* first, uint32_t n, uint32_t u) {
-    uint32_t lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (__ldg(first + mid) <= u) lo = mid; else hi = mid;
-    }
-    return lo;
-}
 
 __device__ __forceinline__ float element(const void* p, uint32_t dtype, uint64_t i) {
     if (dtype == FTC_F32) return static_cast<const float*>(p)[i];
@@ -75,54 +66,65 @@ __device__ __forceinline__ void eight_shares(float* s, const PlanEntry& t, uint6
     for (int j = 0; j < 8; ++j) s[j] = t.status && t.k % 8 ? share_at(t, i + j) : one;
 }
 
-// A block has 2048 elements of one matrix: eight a thread, neighbours where the addresses allow it (t.wide), 256 apart otherwise.
+// A block has 4096 elements of one matrix: twice eight a thread, neighbours where the addresses allow it (t.wide), 256 apart otherwise; all loads
+// are out before the first is used.
 __global__ void __launch_bounds__(256) muon_momentum_kernel(MuonArgs a) {
     later_kernel_may_start();
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.word = 0;
     const float scale = a.grad_scale ? *a.grad_scale : 1.f;
     if (!isfinite(scale)) return;
-    const uint32_t* first = plan_first(a.plan, a.n, kChunkFirst);
-    const uint32_t which = matrix_of(first, a.n, blockIdx.x);
+    const uint32_t which = a.maps[kChunks][blockIdx.x];
     const PlanEntry t = plan_entries(a.plan)[which];
-    const uint64_t begin = (uint64_t)(blockIdx.x - first[which]) * kMuonChunk;
+    const uint64_t begin = (uint64_t)(blockIdx.x - t.first[kChunks]) * kMuonChunk;
     const uint32_t left = (uint32_t)min((uint64_t)kMuonChunk, t.n - begin);
     float* m = a.momentum + t.first_block * FTC_STATE_BLOCK + begin;
-    float old[8], g[8], s[8];
+    float old[2][8], g[2][8], s[2][8];
     const bool wide = t.wide && left == kMuonChunk;
     if (wide) {
-        eight(old, m, FTC_F32, threadIdx.x * 8);
-        eight(g, t.grad, t.grad_dtype, begin + threadIdx.x * 8);
-        eight_shares(s, t, begin + threadIdx.x * 8);
+#pragma unroll
+        for (uint32_t w = 0; w < 2; ++w) {
+            const uint32_t e = (w * 256 + threadIdx.x) * 8;
+            eight(old[w], m, FTC_F32, e);
+            eight(g[w], t.grad, t.grad_dtype, begin + e);
+            eight_shares(s[w], t, begin + e);
+        }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (uint32_t j = 0; j < 16; ++j) {
             const uint32_t e = threadIdx.x + j * 256;
             const bool there = e < left;
-            old[j] = there ? m[e] : 0.f;
-            g[j] = there ? element(t.grad, t.grad_dtype, begin + e) : 0.f;
-            s[j] = there ? share_at(t, begin + e) : 0.f;
+            old[j / 8][j % 8] = there ? m[e] : 0.f;
+            g[j / 8][j % 8] = there ? element(t.grad, t.grad_dtype, begin + e) : 0.f;
+            s[j / 8][j % 8] = there ? share_at(t, begin + e) : 0.f;
         }
     }
     double sum = 0;
     uint32_t live = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        float u = old[j];
-        if (s[j] > 0.f) {
-            const float x = g[j] * s[j] * scale;
-            old[j] = fmaf(old[j], a.mu, x);
-            u = a.nesterov ? fmaf(old[j], a.mu, x) : old[j];
+    for (uint32_t j = 0; j < 16; ++j) {
+        float& x = old[j / 8][j % 8];
+        float u = x;
+        if (s[j / 8][j % 8] > 0.f) {
+            const float d = g[j / 8][j % 8] * s[j / 8][j % 8] * scale;
+            x = fmaf(x, a.mu, d);
+            u = a.nesterov ? fmaf(x, a.mu, d) : x;
             live |= 1u << j;
         }
-        sum = fma((double)u, (double)u, sum);
+        sum = ::fma((double)u, (double)u, sum);
     }
     if (wide) {
-        float4* q = reinterpret_cast<float4*>(m + threadIdx.x * 8);
-        if (live) { q[0] = make_float4(old[0], old[1], old[2], old[3]); q[1] = make_float4(old[4], old[5], old[6], old[7]); }
+#pragma unroll
+        for (uint32_t w = 0; w < 2; ++w) {
+            float4* q = reinterpret_cast<float4*>(m + (w * 256 + threadIdx.x) * 8);
+            if (live >> (8 * w) & 0xFFu) {
+                q[0] = make_float4(old[w][0], old[w][1], old[w][2], old[w][3]);
+                q[1] = make_float4(old[w][4], old[w][5], old[w][6], old[w][7]);
+            }
+        }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (live >> j & 1u) m[threadIdx.x + j * 256] = old[j];
+        for (uint32_t j = 0; j < 16; ++j)
+            if (live >> j & 1u) m[threadIdx.x + j * 256] = old[j / 8][j % 8];
     }
     __shared__ double sums[8];
     __shared__ uint32_t lives[8];
@@ -140,8 +142,8 @@ __global__ void __launch_bounds__(256) muon_momentum_kernel(MuonArgs a) {
 __global__ void __launch_bounds__(256) muon_norm_kernel(MuonArgs a) {
     wait_for_earlier_kernel();
     later_kernel_may_start();
-    const uint32_t* first = plan_first(a.plan, a.n, kChunkFirst) + blockIdx.x;
-    const uint32_t c0 = first[0], c1 = first[1];
+    const PlanEntry& t = plan_entries(a.plan)[blockIdx.x];
+    const uint32_t c0 = t.first[kChunks], c1 = c0 + (uint32_t)((t.n + kMuonChunk - 1) / kMuonChunk);
     __shared__ double sums[8], lives[8];
     double sum = 0, live = 0;
 #pragma unroll 4
@@ -165,10 +167,9 @@ __global__ void __launch_bounds__(256) muon_layout_kernel(MuonArgs a) {
     later_kernel_may_start();
     const float scale = a.grad_scale ? *a.grad_scale : 1.f;
     if (!isfinite(scale)) return;
-    const uint32_t* first = plan_first(a.plan, a.n, kBlockFirst);
-    const uint32_t which = matrix_of(first, a.n, blockIdx.x);
+    const uint32_t which = a.maps[kBlocks][blockIdx.x];
     const PlanEntry t = plan_entries(a.plan)[which];
-    const uint32_t at = blockIdx.x - first[which], bi = at / t.nb, bj = at - bi * t.nb;
+    const uint32_t at = blockIdx.x - t.first[kBlocks], bi = at / t.nb, bj = at - bi * t.nb;
     const float inv = a.factor[which];
     const float* m = a.momentum + t.first_block * FTC_STATE_BLOCK;
     __shared__ __align__(16) unsigned char tile[2][kBlockBytes];
@@ -182,7 +183,7 @@ __global__ void __launch_bounds__(256) muon_layout_kernel(MuonArgs a) {
     const bool whole = bi * 128 + 128 <= t.m && bj * 64 + 64 <= t.w;
     if (whole && t.wide && t.cols % 8 == 0) {
         // runs of 64 neighbours in 128 rows of memory, or of 128 in 64 (transposed)
-        const uint32_t per = t.tall ? 16 : 8;                    // eights of a run
+        // of the transposed ones neighbouring threads have neighbouring lines, so that they write neighbours in shared memory
 #pragma unroll
         for (uint32_t u = 0; u < 2; ++u) {
             float v[2][8], g[2][8], s[2][8];
@@ -190,7 +191,8 @@ __global__ void __launch_bounds__(256) muon_layout_kernel(MuonArgs a) {
 #pragma unroll
             for (uint32_t w = 0; w < 2; ++w) {
                 const uint32_t e = threadIdx.x + (2 * u + w) * 256;
-                line[w] = e / per; run[w] = e % per * 8;
+                line[w] = t.tall ? threadIdx.x % 64 : e / 8;
+                run[w] = t.tall ? (threadIdx.x / 64 * 4 + 2 * u + w) * 8 : e % 8 * 8;
                 const uint64_t q = t.tall ? (uint64_t)(bj * 64 + line[w]) * t.cols + bi * 128 + run[w] : (uint64_t)(bi * 128 + line[w]) * t.cols + bj * 64 + run[w];
                 eight(v[w], m, FTC_F32, q);
                 if (a.nesterov) { eight(g[w], t.grad, t.grad_dtype, q); eight_shares(s[w], t, q); }
@@ -264,14 +266,14 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
 }
 // Arrives at the barrier of the pair's block `rank`.
 __device__ __forceinline__ void bar_arrive_at(uint32_t bar, uint32_t rank) {
-    asm volatile("{\n\t.reg .b32 there;\n\tmapa.shared::cluster.u32 there, %0, %1;\n\tmbarrier.arrive.release.cluster.shared::cluster.b64 _, [there];\n\t}"
+    asm volatile("{\n\t.reg .b32 there;\n\tmapa.shared::cluster.u32 there, %0, %1;\n\tmbarrier.arrive.shared::cluster.b64 _, [there];\n\t}"
                  ::"r"(bar), "r"(rank) : "memory");
 }
 // Looks at most 2^22 times (each look may sleep for a while): false if the phase did not end.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
     for (uint32_t i = 0; i < 1u << 22; ++i) {
         uint32_t ok;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
         if (ok) return true;
     }
@@ -297,7 +299,7 @@ __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uin
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                  ::"r"(d), "l"(a), "l"(b), "r"(how), "r"((uint32_t)add) : "memory");
 }
-__device__ __forceinline__ void read_32(float* v, uint32_t from) {
+__device__ __forceinline__ void read_32(F2* v, uint32_t from) {
     uint32_t r[32];
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
@@ -305,7 +307,7 @@ __device__ __forceinline__ void read_32(float* v, uint32_t from) {
                  : "r"(from) : "memory");
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < 16; ++i) v[i] = pair(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
 }
 
 // Descriptor of an operand in shared memory: address, the two strides (in bytes) and the swizzle of 128 bytes.
@@ -316,10 +318,10 @@ __device__ __forceinline__ uint64_t operand(uint32_t address, uint32_t leading, 
 struct Tile { uint32_t which, i, j; };                           // matrix, blocks of 256 rows and of 256 columns
 
 // Tiles on and below the diagonal: row i has i + 1.
-__device__ __forceinline__ Tile gram_tile(const uint32_t* first, uint32_t n, uint32_t u) {
+__device__ __forceinline__ Tile gram_tile(const MuonArgs& a, uint32_t u) {
     Tile t;
-    t.which = matrix_of(first, n, u);
-    const uint32_t r = u - __ldg(first + t.which);
+    t.which = __ldg(a.maps[kGramTiles] + u);
+    const uint32_t r = u - plan_entries(a.plan)[t.which].first[kGramTiles];
     uint32_t i = (uint32_t)((sqrtf(8.f * (float)r + 1.f) - 1.f) * 0.5f);
     while (i * (i + 1) / 2 > r) --i;
     while ((i + 1) * (i + 2) / 2 <= r) ++i;
@@ -328,38 +330,22 @@ __device__ __forceinline__ Tile gram_tile(const uint32_t* first, uint32_t n, uin
     return t;
 }
 // All tiles, a column's one after the other: they share the right operand.
-__device__ __forceinline__ Tile apply_tile(const uint32_t* first, uint32_t n, uint32_t u, const PlanEntry* e) {
+__device__ __forceinline__ Tile apply_tile(const MuonArgs& a, uint32_t u) {
     Tile t;
-    t.which = matrix_of(first, n, u);
-    const uint32_t r = u - __ldg(first + t.which), rows = (e[t.which].mb + 1) / 2;
+    t.which = __ldg(a.maps[kApplyTiles] + u);
+    const PlanEntry& e = plan_entries(a.plan)[t.which];
+    const uint32_t r = u - e.first[kApplyTiles], rows = (e.mb + 1) / 2;
     t.j = r / rows;
     t.i = r - t.j * rows;
     return t;
 }
 
-__device__ __forceinline__ uint4 packed(const float* v) {        // 8 numbers (times 2^14) as float16
-    uint4 r;
-    uint32_t* w = &r.x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t*>(&h); }
-    return r;
-}
-__device__ __forceinline__ void unpacked(float* v, uint4 r, bool more) {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-        v[2 * i] = more ? v[2 * i] + f.x : f.x; v[2 * i + 1] = more ? v[2 * i + 1] + f.y : f.y;
-    }
-}
-__device__ __forceinline__ void rest_of(float* v) {              // what float16 leaves over
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] -= __half2float(__float2half_rn(v[i]));
-}
+__device__ __forceinline__ uint32_t half2_of(F2 v) { uint32_t r; asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi(v)), "f"(lo(v))); return r; }
+__device__ __forceinline__ F2 pair_of(uint32_t h) { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h)); return pair(f.x, f.y); }
 
 // The weights of 32 rows (of the team's warp) and 64 columns of X, whose update a lane has: a row of it (v). Turned in shared memory unless
 // the matrix lies transposed, so that neighbouring lanes have neighbouring weights.
-template <typename W> __device__ __forceinline__ void move_weights(const PlanEntry& t, W* weights, uint32_t i0, uint32_t j0, const float* v, float* turn, float down, float move) {
+template <typename W> __device__ __forceinline__ void move_weights(const PlanEntry t, W* weights, uint32_t i0, uint32_t j0, const F2* v, float* turn, float down, float move) {
     const uint32_t lane = threadIdx.x % 32;
     if (t.tall) {
         const uint32_t col = i0 + lane;
@@ -376,7 +362,8 @@ template <typename W> __device__ __forceinline__ void move_weights(const PlanEnt
                 const uint32_t row = j0 + h * 32 + q;
                 if (row >= t.rows || col >= t.cols) continue;
                 const uint64_t at = (uint64_t)row * t.cols + col;
-                const float x = fmaf(p[q], down, v[h * 32 + q] * move);
+                const F2 d = v[(h * 32 + q) / 2];
+                const float x = fmaf(p[q], down, (q & 1 ? hi(d) : lo(d)) * move);
                 weights[at] = from_f32<W>(x);
                 if (t.master) set_element(t.param, t.param_dtype, at, x);
             }
@@ -385,7 +372,7 @@ template <typename W> __device__ __forceinline__ void move_weights(const PlanEnt
     }
     // row r of the warp's 32 at r * 64, its pieces of four numbers at c ^ r % 8
 #pragma unroll
-    for (uint32_t c = 0; c < 16; ++c) *reinterpret_cast<float4*>(turn + lane * 64 + ((c ^ (lane & 7)) << 2)) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+    for (uint32_t c = 0; c < 16; ++c) *reinterpret_cast<float4*>(turn + lane * 64 + ((c ^ (lane & 7)) << 2)) = make_float4(lo(v[2 * c]), hi(v[2 * c]), lo(v[2 * c + 1]), hi(v[2 * c + 1]));
     __syncwarp();
 #pragma unroll
     for (uint32_t h = 0; h < 2; ++h) {
@@ -411,7 +398,7 @@ template <typename W> __device__ __forceinline__ void move_weights(const PlanEnt
     }
 }
 
-template <int MODE> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) muon_product_kernel(MuonArgs a, uint32_t tiles, uint32_t side) {
+template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) muon_product_kernel(MuonArgs a, uint32_t tiles, uint32_t side) {
     namespace cg = cooperative_groups;
     extern __shared__ unsigned char raw[];
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -425,7 +412,7 @@ template <int MODE> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(
     uint32_t* const words = reinterpret_cast<uint32_t*>(bars + 3 * kStages + 7);                     // tensor memory, gave up
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < kStages; ++s) { bar_init(full + 8 * s, 1); bar_init(landed + 8 * s, 1); bar_init(empty + 8 * s, 1); }
-        for (uint32_t s = 0; s < 2; ++s) { bar_init(sum_full + 8 * s, 1); bar_init(sum_empty + 8 * s, 16); bar_init(team_full + 8 * s, 1); }
+        for (uint32_t s = 0; s < 2; ++s) { bar_init(sum_full + 8 * s, 1); bar_init(sum_empty + 8 * s, MODE == kUpdate ? 18 : 16); bar_init(team_full + 8 * s, 1); }
         bar_init(drained, 1);
         words[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -437,15 +424,14 @@ template <int MODE> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     cg::this_cluster().sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const uint32_t tmem = words[0], pairs = gridDim.x / 2, pair = blockIdx.x / 2;
+    const uint32_t tmem = words[0], pairs = gridDim.x / 2, our_pair = blockIdx.x / 2;
     wait_for_earlier_kernel();
     later_kernel_may_start();
     const float scale = a.grad_scale ? *a.grad_scale : 1.f;
     const bool work = isfinite(scale) && *reinterpret_cast<volatile uint32_t*>(a.word) == 0;
     const PlanEntry* const entries = plan_entries(a.plan);
-    const uint32_t* const first = plan_first(a.plan, a.n, MODE <= kPoly ? kGramFirst : kApplyFirst);
-    const uint32_t segments = a.split ? 3 : 1;
-    auto tile_of = [&](uint32_t u) { return MODE <= kPoly ? gram_tile(first, a.n, u) : apply_tile(first, a.n, u, entries); };
+    constexpr uint32_t segments = SPLIT ? 3 : 1;
+    auto tile_of = [&](uint32_t u) { return MODE <= kPoly ? gram_tile(a, u) : apply_tile(a, u); };
     // a tile's steps of 64 and its columns: 256, or 128 where there are no more (in the apply kernels up to 64 of them are nobody's)
     auto steps_of = [&](const PlanEntry& t) { return segments * (MODE == kGram ? t.nb : t.kb); };
     auto columns_of = [&](const PlanEntry& t, const Tile& q) { return MODE <= kPoly ? (t.mb > 2 * q.j + 1 ? 256u : 128u) : (t.nb > 4 * q.j + 2 ? 256u : 128u); };
@@ -454,9 +440,9 @@ template <int MODE> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(
 
     if (work && warp == 0 && lane == 0) {                        // copies
         uint32_t it = 0;
-        for (uint32_t u = pair; u < tiles && ok; u += pairs) {
+        for (uint32_t u = our_pair; u < tiles && ok; u += pairs) {
             const Tile tile = tile_of(u);
-            const PlanEntry& t = entries[tile.which];
+            const PlanEntry t = entries[tile.which];
             const uint32_t steps = MODE == kGram ? t.nb : t.kb, left_row = 2 * tile.i + rank, half = columns_of(t, tile) / 2;      // columns of this block
             const bool has_left = left_row < t.mb;
             // right operand of a symmetric product: rows half * rank .. of 256; of the others: blocks of 64 columns
@@ -487,9 +473,9 @@ template <int MODE> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(
         }
     } else if (work && warp == 1 && lane == 0) {
         uint32_t it = 0, n = 0;
-        for (uint32_t u = pair; u < tiles && ok; u += pairs, ++n) {
+        for (uint32_t u = our_pair; u < tiles && ok; u += pairs, ++n) {
             const Tile tile = tile_of(u);
-            const PlanEntry& t = entries[tile.which];
+            const PlanEntry t = entries[tile.which];
             const uint32_t steps = steps_of(t);
             if (rank) {                                          // the second block's copies
                 for (uint32_t s = 0; s < steps; ++s, ++it) {
@@ -525,6 +511,23 @@ template <int MODE> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(
                 bar_wait(drained, 0);
             }
         }
+    } else if (MODE == kUpdate && work && warp == 3) {           // a tile's weights into L2 while its products are made
+        uint32_t n = 0;
+        for (uint32_t u = our_pair; u < tiles; u += pairs, ++n) {
+            const Tile tile = tile_of(u);
+            const PlanEntry t = entries[tile.which];
+            const uint32_t i0 = (2 * tile.i + rank) * 128, j0 = tile.j * 256, es = t.master || t.param_dtype == FTC_F32 ? 4 : 2;
+            const uint32_t rows = t.tall ? min(256u, t.w - j0) : i0 < t.m ? min(128u, t.m - i0) : 0, cols = t.tall ? (i0 < t.m ? min(128u, t.m - i0) : 0) : min(256u, t.w - j0);
+            const char* const base = static_cast<const char*>(t.master ? static_cast<const void*>(t.master) : t.param) + ((uint64_t)(t.tall ? j0 : i0) * t.cols + (t.tall ? i0 : j0)) * es;
+            const uint32_t lines = (cols * es + 127) / 128;
+            for (uint32_t e = lane; e < rows * lines; e += 32) {
+                const uint32_t row = e / lines;
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(base + (uint64_t)row * t.cols * es + min((e - row * lines) * 128, cols * es - 1)));
+            }
+            // no further ahead than the next tile, and never behind: the sums' next phase waits for this warp too
+            if (!__all_sync(0xFFFFFFFFu, bar_wait(sum_full + 8 * (n & 1), (n / 2) & 1))) break;
+            if (lane == 0) bar_arrive_at(sum_empty + 8 * (n & 1), 0);
+        }
     } else if (work && warp >= 4) {                              // sums
         const uint32_t team = (warp - 4) / 4, quarter = warp & 3, r = quarter * 32 + lane;
         unsigned char* const mine = smem + kStages * kStageBytes + team * kTeamBytes;
@@ -532,9 +535,9 @@ template <int MODE> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(
         const uint32_t ready = team_full + 8 * team;
         const bool leads = quarter == 0 && lane == 0;
         uint32_t n = 0, blocks = 0;
-        for (uint32_t u = pair; u < tiles && ok; u += pairs, ++n) {
+        for (uint32_t u = our_pair; u < tiles && ok; u += pairs, ++n) {
             const Tile tile = tile_of(u);
-            const PlanEntry& t = entries[tile.which];
+            const PlanEntry t = entries[tile.which];
             const uint32_t bi = 2 * tile.i + rank, i = bi * 128 + r;
             // blocks of 64 columns of this team: none above the diagonal, none beyond the edges
             const uint32_t cb0 = 4 * tile.j + 2 * team, edge = MODE <= kPoly ? 2 * min(t.mb, bi + 1) : t.nb;
@@ -548,48 +551,55 @@ template <int MODE> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(
                     if (MODE == kGram) bar_expect(ready, 0);
                     else {
                         const unsigned char* from = (MODE == kPoly ? a.a : x_in) + here;
-                        bar_expect(ready, (a.split ? 2 : 1) * kBlockBytes);
+                        bar_expect(ready, (SPLIT ? 2 : 1) * kBlockBytes);
                         copy_in(smem_of(mine), from, kBlockBytes, ready);
-                        if (a.split) copy_in(smem_of(other), from + (MODE == kPoly ? a.a_bytes : a.x_bytes), kBlockBytes, ready);
+                        if (SPLIT) copy_in(smem_of(other), from + (MODE == kPoly ? a.a_bytes : a.x_bytes), kBlockBytes, ready);
                     }
                 }
                 ok = (b || bar_wait(sum_full + 8 * (n & 1), (n / 2) & 1)) && (!wanted || bar_wait(ready, blocks & 1));
                 ok = all_of_team(team, ok);                      // one goes on only if all do
                 if (!ok || !wanted) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                float v[64];
+                F2 v[32];
                 read_32(v, tmem + (n & 1) * 256 + (quarter * 32 << 16) + team * 128 + b * 64);
-                read_32(v + 32, tmem + (n & 1) * 256 + (quarter * 32 << 16) + team * 128 + b * 64 + 32);
-                if (MODE == kGram) {
+                read_32(v + 16, tmem + (n & 1) * 256 + (quarter * 32 << 16) + team * 128 + b * 64 + 32);
+                // the row's own place on the diagonal, in the block of columns that holds it
+                const bool diagonal = MODE <= kPoly && i / 64 == cb;
+                const uint32_t own = i % 64;
+                float mine_own = 0.f;
+                if (MODE <= kPoly && cb / 2 == bi) {
 #pragma unroll
-                    for (int q = 0; q < 64; ++q) {
-                        if (j0 + q == i) { a.diag_a[t.diagonal + i] = v[q] * kDown2; v[q] = 0.f; }
-                        v[q] *= kDown;
+                    for (uint32_t q = 0; q < 32; ++q) {
+                        if (own == 2 * q) mine_own = lo(v[q]);
+                        if (own == 2 * q + 1) mine_own = hi(v[q]);
                     }
+                    mine_own *= kDown2;
+                }
+                if (MODE == kGram) {
+                    if (diagonal) a.diag_a[t.diagonal + i] = mine_own;
+#pragma unroll
+                    for (int q = 0; q < 32; ++q) v[q] = mul(v[q], twice(kDown));
                 } else {
                     const float* d = a.diag_a + t.diagonal;
-                    const float di = MODE == kPoly ? d[i] : 0.f, keep = MODE == kPoly ? 0.f : kQ1 + a.diag_b[t.diagonal + i];
+                    const float di = MODE == kPoly ? d[i] : 0.f;
+                    const F2 keep = twice(MODE == kPoly ? fmaf(kQ5, di, kQ3) : kQ1 + a.diag_b[t.diagonal + i]);
+                    if (MODE == kPoly && diagonal) a.diag_b[t.diagonal + i] = fmaf(kQ5, fmaf(di, di, mine_own), kQ3 * di);
 #pragma unroll
                     for (uint32_t c = 0; c < 8; ++c) {
-                        float e[8];
-                        unpacked(e, *reinterpret_cast<const uint4*>(mine + piece(r, c)), false);
-                        if (a.split) unpacked(e, *reinterpret_cast<const uint4*>(other + piece(r, c)), true);
+                        const uint4 h = *reinterpret_cast<const uint4*>(mine + piece(r, c));
+                        F2 e[4] = {pair_of(h.x), pair_of(h.y), pair_of(h.z), pair_of(h.w)};
+                        if (SPLIT) {
+                            const uint4 l = *reinterpret_cast<const uint4*>(other + piece(r, c));
+                            e[0] = add(e[0], pair_of(l.x)); e[1] = add(e[1], pair_of(l.y)); e[2] = add(e[2], pair_of(l.z)); e[3] = add(e[3], pair_of(l.w));
+                        }
                         if (MODE == kPoly) {
                             const float4 d0 = *reinterpret_cast<const float4*>(d + j0 + 8 * c), d1 = *reinterpret_cast<const float4*>(d + j0 + 8 * c + 4);
-                            const float dj[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
+                            const F2 dj[4] = {pair(d0.x, d0.y), pair(d0.z, d0.w), pair(d1.x, d1.y), pair(d1.z, d1.w)};
 #pragma unroll
-                            for (uint32_t q = 0; q < 8; ++q) {
-                                float& x = v[8 * c + q];
-                                if (j0 + 8 * c + q == i) {
-                                    a.diag_b[t.diagonal + i] = fmaf(kQ5, fmaf(x, kDown2, di * di), kQ3 * di);
-                                    x = 0.f;
-                                } else {
-                                    x = fmaf(kQ5 * kDown, x, e[q] * fmaf(kQ5, di + dj[q], kQ3));
-                                }
-                            }
+                            for (uint32_t q = 0; q < 4; ++q) v[4 * c + q] = fma(v[4 * c + q], twice(kQ5 * kDown), mul(e[q], fma(dj[q], twice(kQ5), keep)));
                         } else {
 #pragma unroll
-                            for (uint32_t q = 0; q < 8; ++q) v[8 * c + q] = fmaf(v[8 * c + q], kDown, keep * e[q]);      // times 2^14
+                            for (uint32_t q = 0; q < 4; ++q) v[4 * c + q] = fma(v[4 * c + q], twice(kDown), mul(keep, e[q]));   // times 2^14
                         }
                     }
                 }
@@ -605,51 +615,57 @@ template <int MODE> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(
                     asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory");
                     continue;
                 }
+                uint32_t h[32], low_h[SPLIT ? 32 : 1];
+#pragma unroll
+                for (int q = 0; q < 32; ++q) h[q] = half2_of(v[q]);
+                if (SPLIT) {
+#pragma unroll
+                    for (int q = 0; q < 32; ++q) {               // what float16 leaves over
+                        const F2 x = pair_of(h[q]);
+                        low_h[q] = half2_of(pair(lo(v[q]) - lo(x), hi(v[q]) - hi(x)));
+                    }
+                }
 #pragma unroll
                 for (uint32_t c = 0; c < 8; ++c) {
-                    *reinterpret_cast<uint4*>(mine + piece(r, c)) = packed(v + 8 * c);
-                    if (a.split) {
-                        float x[8];
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) x[q] = v[8 * c + q];
-                        rest_of(x);
-                        *reinterpret_cast<uint4*>(other + piece(r, c)) = packed(x);
-                    }
+                    *reinterpret_cast<uint4*>(mine + piece(r, c)) = make_uint4(h[4 * c], h[4 * c + 1], h[4 * c + 2], h[4 * c + 3]);
+                    if (SPLIT) *reinterpret_cast<uint4*>(other + piece(r, c)) = make_uint4(low_h[4 * c], low_h[4 * c + 1], low_h[4 * c + 2], low_h[4 * c + 3]);
+                }
+                if (diagonal) {
+                    *reinterpret_cast<uint16_t*>(mine + piece(r, own / 8) + own % 8 * 2) = 0;
+                    if (SPLIT) *reinterpret_cast<uint16_t*>(other + piece(r, own / 8) + own % 8 * 2) = 0;
                 }
                 unsigned char* const out = MODE == kGram ? a.a : MODE == kPoly ? a.b : a.x[side ^ 1];
                 const uint64_t low = MODE <= kPoly ? a.a_bytes : a.x_bytes;
-                const bool twice = MODE <= kPoly && cb / 2 < bi;                         // below the diagonal: the transpose too
+                const bool both = MODE <= kPoly && cb / 2 < bi;                          // below the diagonal: the transpose too
                 // element (j, i): 64 rows, two blocks of 64 columns, each half a block
-                const uint64_t there = twice ? (t.a_block + (uint64_t)(cb / 2) * 2 * t.mb + 2 * bi) * kBlockBytes + cb % 2 * (kBlockBytes / 2) : 0;
-                auto turned = [&](unsigned char* to, bool lower) {
-                    unsigned char* const half = to + r / 64 * (kBlockBytes / 2);
+                const uint64_t there = both ? (t.a_block + (uint64_t)(cb / 2) * 2 * t.mb + 2 * bi) * kBlockBytes + cb % 2 * (kBlockBytes / 2) : 0;
+                auto turned = [&](unsigned char* to, const uint32_t* w) {
+                    unsigned char* const half = to + r / 64 * (kBlockBytes / 2) + r % 8 * 2;
 #pragma unroll
-                    for (uint32_t q = 0; q < 64; ++q) {
-                        const __half h = __float2half_rn(v[q]);
-                        *reinterpret_cast<__half*>(half + piece(q, r % 64 / 8) + r % 8 * 2) = lower ? __float2half_rn(v[q] - __half2float(h)) : h;
-                    }
+                    for (uint32_t q = 0; q < 64; ++q)
+                        *reinterpret_cast<uint16_t*>(half + piece(q, r % 64 / 8)) = (uint16_t)(q & 1 ? w[q / 2] >> 16 : w[q / 2]);
                 };
-                if (twice && !a.split) turned(other, false);
+                if (both && !SPLIT) turned(other, h);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory");
                 if (leads) {
                     copy_out(out + here, smem_of(mine), kBlockBytes);
-                    if (a.split) copy_out(out + low + here, smem_of(other), kBlockBytes);
-                    else if (twice)
-                        for (uint32_t h = 0; h < 2; ++h) copy_out(out + there + h * kBlockBytes, smem_of(other) + h * (kBlockBytes / 2), kBlockBytes / 2);
+                    if (SPLIT) copy_out(out + low + here, smem_of(other), kBlockBytes);
+                    else if (both)
+                        for (uint32_t q = 0; q < 2; ++q) copy_out(out + there + q * kBlockBytes, smem_of(other) + q * (kBlockBytes / 2), kBlockBytes / 2);
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
-                if (twice && a.split) {                          // both of the transpose's numbers, once theirs have left
+                if (both && SPLIT) {                             // both of the transpose's numbers, once theirs have left
                     if (leads) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory");
-                    turned(mine, false);
-                    turned(other, true);
+                    turned(mine, h);
+                    turned(other, low_h);
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory");
                     if (leads) {
-                        for (uint32_t h = 0; h < 2; ++h) {
-                            copy_out(out + there + h * kBlockBytes, smem_of(mine) + h * (kBlockBytes / 2), kBlockBytes / 2);
-                            copy_out(out + low + there + h * kBlockBytes, smem_of(other) + h * (kBlockBytes / 2), kBlockBytes / 2);
+                        for (uint32_t q = 0; q < 2; ++q) {
+                            copy_out(out + there + q * kBlockBytes, smem_of(mine) + q * (kBlockBytes / 2), kBlockBytes / 2);
+                            copy_out(out + low + there + q * kBlockBytes, smem_of(other) + q * (kBlockBytes / 2), kBlockBytes / 2);
                         }
                         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     }
@@ -675,8 +691,8 @@ template <int MODE> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(
     if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
-template <int MODE> static cudaError_t product(const MuonArgs& a, uint32_t tiles, uint32_t side, int sms, cudaStream_t st) {
-    cudaError_t e = cudaFuncSetAttribute(muon_product_kernel<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
+template <int MODE, bool SPLIT> static cudaError_t product(const MuonArgs& a, uint32_t tiles, uint32_t side, int sms, cudaStream_t st) {
+    cudaError_t e = cudaFuncSetAttribute(muon_product_kernel<MODE, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute early{};
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -685,19 +701,25 @@ template <int MODE> static cudaError_t product(const MuonArgs& a, uint32_t tiles
     const uint32_t most = (uint32_t)sms / 2;
     how.gridDim = dim3(2 * (tiles < most ? tiles : most)); how.blockDim = dim3(kProductThreads); how.dynamicSmemBytes = kProductSmem;
     how.stream = st; how.attrs = &early; how.numAttrs = 1;
-    return cudaLaunchKernelEx(&how, muon_product_kernel<MODE>, a, tiles, side);
+    return cudaLaunchKernelEx(&how, muon_product_kernel<MODE, SPLIT>, a, tiles, side);
+}
+
+template <bool SPLIT> static cudaError_t products(const MuonArgs& a, int sms, cudaStream_t st) {
+    cudaError_t e = cudaSuccess;
+    for (uint32_t s = 0; s < a.steps && e == cudaSuccess; ++s) {
+        e = product<kGram, SPLIT>(a, a.items[kGramTiles], s & 1, sms, st);
+        if (e == cudaSuccess) e = product<kPoly, SPLIT>(a, a.items[kGramTiles], s & 1, sms, st);
+        if (e == cudaSuccess) e = s + 1 < a.steps ? product<kApply, SPLIT>(a, a.items[kApplyTiles], s & 1, sms, st) : product<kUpdate, SPLIT>(a, a.items[kApplyTiles], s & 1, sms, st);
+    }
+    return e;
 }
 
 cudaError_t launch_muon(const MuonArgs& a, int sms, cudaStream_t st) {
-    muon_momentum_kernel<<<a.chunks, 256, 0, st>>>(a);
+    muon_momentum_kernel<<<a.items[kChunks], 256, 0, st>>>(a);
     cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess) e = launch_second(muon_norm_kernel, a.n, 256, st, a);
-    if (e == cudaSuccess) e = launch_second(muon_layout_kernel, a.x_blocks, 256, st, a);
-    for (uint32_t s = 0; s < a.steps && e == cudaSuccess; ++s) {
-        e = product<kGram>(a, a.gram_tiles, s & 1, sms, st);
-        if (e == cudaSuccess) e = product<kPoly>(a, a.gram_tiles, s & 1, sms, st);
-        if (e == cudaSuccess) e = s + 1 < a.steps ? product<kApply>(a, a.apply_tiles, s & 1, sms, st) : product<kUpdate>(a, a.apply_tiles, s & 1, sms, st);
-    }
+    if (e == cudaSuccess) e = launch_second(muon_layout_kernel, a.items[kBlocks], 256, st, a);
+    if (e == cudaSuccess) e = a.split ? products<true>(a, sms, st) : products<false>(a, sms, st);
     return e;
 }
 
