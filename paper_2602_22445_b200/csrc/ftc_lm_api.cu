@@ -187,7 +187,7 @@ int ftc_muon_plan_build(const ftc_matrix_t* h_matrices, uint32_t n, void* h_plan
         q.mb = (q.m + 127) / 128; q.nb = (q.w + 63) / 64; q.kb = (q.m + 63) / 64;
         q.first_block = blocks; q.x_block = x; q.a_block = a; q.diagonal = diagonal;
         blocks += (t.n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK; x += (uint64_t)q.mb * q.nb; a += (uint64_t)q.mb * 2 * q.mb; diagonal += q.mb * 128;
-        q.wide = aligned(t.grad, 16);
+        q.wide = aligned(t.grad, 16) && aligned(t.param, 16) && aligned(t.master, 16);
     }
     // The maps. Tiles of many steps come first, so that the last ones to run are short.
     uint32_t* map = reinterpret_cast<uint32_t*>(e + n);

@@ -242,6 +242,88 @@ __global__ void __launch_bounds__(256) muon_layout_kernel(MuonArgs a) {
     }
 }
 
+// The weights that one block of 128 x 64 of X moves; elements as in the layout.
+__device__ __forceinline__ void store_eight(void* p, uint32_t dtype, uint64_t i, const float* v) {
+    if (dtype == FTC_F32) {
+        float4* q = reinterpret_cast<float4*>(static_cast<float*>(p) + i);
+        q[0] = make_float4(v[0], v[1], v[2], v[3]); q[1] = make_float4(v[4], v[5], v[6], v[7]);
+        return;
+    }
+    uint4 r;
+    uint32_t* w = &r.x;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (dtype == FTC_BF16) { const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]); w[j] = *reinterpret_cast<const uint32_t*>(&h); }
+        else { const __half2 h = __floats2half2_rn(v[2 * j], v[2 * j + 1]); w[j] = *reinterpret_cast<const uint32_t*>(&h); }
+    }
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + i) = r;
+}
+__global__ void __launch_bounds__(256) muon_update_kernel(MuonArgs a) {
+    wait_for_earlier_kernel();
+    const float scale = a.grad_scale ? *a.grad_scale : 1.f;
+    const uint32_t which = a.maps[kBlocks][blockIdx.x];
+    if (!isfinite(scale) || *reinterpret_cast<volatile uint32_t*>(a.word) || !a.live[which]) return;
+    const PlanEntry t = plan_entries(a.plan)[which];
+    const uint32_t at = blockIdx.x - t.first[kBlocks], bi = at / t.nb, bj = at - bi * t.nb;
+    const unsigned char* const x = a.x[a.steps & 1] + (t.x_block + at) * kBlockBytes;
+    const float l = a.lr * t.lr_scale, down = 1.f - l * t.weight_decay, move = -l * kDown;
+    void* const weights = t.master ? static_cast<void*>(t.master) : t.param;
+    const uint32_t dtype = t.master ? FTC_F32 : t.param_dtype;
+    __shared__ __align__(16) unsigned char tile[2][kBlockBytes];
+    const bool whole = bi * 128 + 128 <= t.m && bj * 64 + 64 <= t.w && t.wide && t.cols % 8 == 0;
+    float p[4][8];
+    uint64_t place[4];
+    if (whole) {                                                 // weights first: they come from memory, X from L2 if at all
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) {
+            const uint32_t e = threadIdx.x + u * 256, line = t.tall ? threadIdx.x % 64 : e / 8, run = t.tall ? (threadIdx.x / 64 * 4 + u) * 8 : e % 8 * 8;
+            place[u] = t.tall ? (uint64_t)(bj * 64 + line) * t.cols + bi * 128 + run : (uint64_t)(bi * 128 + line) * t.cols + bj * 64 + run;
+            eight(p[u], weights, dtype, place[u]);
+        }
+    }
+    for (uint32_t s = 0; s <= a.split; ++s) {
+        const uint4* from = reinterpret_cast<const uint4*>(x + s * a.x_bytes);
+        uint4* to = reinterpret_cast<uint4*>(tile[s]);
+#pragma unroll
+        for (uint32_t e = 0; e < kBlockBytes / 16 / 256; ++e) to[threadIdx.x + e * 256] = from[threadIdx.x + e * 256];
+    }
+    __syncthreads();
+    auto update = [&](uint32_t r, uint32_t c) {
+        const uint32_t q = piece(r, c / 8) + c % 8 * 2;
+        float v = __half2float(*reinterpret_cast<const __half*>(tile[0] + q));
+        if (a.split) v += __half2float(*reinterpret_cast<const __half*>(tile[1] + q));
+        return v * move;
+    };
+    if (whole) {
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) {
+            const uint32_t e = threadIdx.x + u * 256, line = t.tall ? threadIdx.x % 64 : e / 8, run = t.tall ? (threadIdx.x / 64 * 4 + u) * 8 : e % 8 * 8;
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) p[u][j] = fmaf(p[u][j], down, t.tall ? update(run + j, line) : update(line, run + j));
+            store_eight(weights, dtype, place[u], p[u]);
+            if (t.master) store_eight(t.param, t.param_dtype, place[u], p[u]);
+        }
+        return;
+    }
+    for (uint32_t e0 = threadIdx.x; e0 < 128 * 64; e0 += 2048) {
+        float v[8];
+#pragma unroll
+        for (uint32_t w = 0; w < 8; ++w) {
+            const uint32_t e = e0 + w * 256, r = t.tall ? e % 128 : e / 64, c = t.tall ? e / 128 : e % 64, i = bi * 128 + r, j = bj * 64 + c;
+            v[w] = i < t.m && j < t.w ? element(weights, dtype, t.tall ? (uint64_t)j * t.cols + i : (uint64_t)i * t.cols + j) : 0.f;
+        }
+#pragma unroll
+        for (uint32_t w = 0; w < 8; ++w) {
+            const uint32_t e = e0 + w * 256, r = t.tall ? e % 128 : e / 64, c = t.tall ? e / 128 : e % 64, i = bi * 128 + r, j = bj * 64 + c;
+            if (i >= t.m || j >= t.w) continue;
+            const uint64_t q = t.tall ? (uint64_t)j * t.cols + i : (uint64_t)i * t.cols + j;
+            const float y = fmaf(v[w], down, update(r, c));
+            set_element(weights, dtype, q, y);
+            if (t.master) set_element(t.param, t.param_dtype, q, y);
+        }
+    }
+}
+
 // ---- products ----
 //
 // Persistent pairs of blocks (clusters of two), 12 warps each. A pair has a tile of 256 x 256: a block holds 128 rows of the left operand and
@@ -255,9 +337,9 @@ __global__ void __launch_bounds__(256) muon_layout_kernel(MuonArgs a) {
 //            team's shared memory as a block, is replaced there by the result, and goes out as a block; so does its transpose.
 
 constexpr uint32_t kStages = 5, kStageBytes = 2 * kBlockBytes, kTeamBytes = 2 * kBlockBytes, kProductThreads = 384;
-constexpr uint32_t kProductSmem = kStages * kStageBytes + 2 * kTeamBytes + 1024 + 256;
+constexpr uint32_t kProductSmem = kStages * kStageBytes + 2 * kTeamBytes + 1024 + 512;
 static_assert(kProductSmem <= 227 * 1024, "shared memory of a block");
-enum { kGram, kPoly, kApply, kUpdate };
+enum { kGram, kPoly, kApply };
 
 __device__ __forceinline__ uint32_t smem_of(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
@@ -279,9 +361,10 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
     }
     return false;
 }
-__device__ __forceinline__ bool all_of_team(uint32_t team, bool ok) {
+// Do both warps of a pair say yes?
+__device__ __forceinline__ bool all_of_pair(uint32_t id, bool ok) {
     uint32_t all;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"((uint32_t)ok), "r"(3 + team) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"((uint32_t)ok), "r"(id) : "memory");
     return all;
 }
 __device__ __forceinline__ void copy_in(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
@@ -299,15 +382,18 @@ __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uin
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                  ::"r"(d), "l"(a), "l"(b), "r"(how), "r"((uint32_t)add) : "memory");
 }
-__device__ __forceinline__ void read_32(F2* v, uint32_t from) {
-    uint32_t r[32];
+// 64 columns of a lane.
+__device__ __forceinline__ void read_64(F2* v, uint32_t from) {
+    uint32_t r[64];
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-                   "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-                 : "r"(from) : "memory");
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(from + 0) : "memory");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+                 : "r"(from + 32) : "memory");
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = pair(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
+    for (int i = 0; i < 32; ++i) v[i] = pair(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
 }
 
 // Descriptor of an operand in shared memory: address, the two strides (in bytes) and the swizzle of 128 bytes.
@@ -343,61 +429,6 @@ __device__ __forceinline__ Tile apply_tile(const MuonArgs& a, uint32_t u) {
 __device__ __forceinline__ uint32_t half2_of(F2 v) { uint32_t r; asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi(v)), "f"(lo(v))); return r; }
 __device__ __forceinline__ F2 pair_of(uint32_t h) { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h)); return pair(f.x, f.y); }
 
-// The weights of 32 rows (of the team's warp) and 64 columns of X, whose update a lane has: a row of it (v). Turned in shared memory unless
-// the matrix lies transposed, so that neighbouring lanes have neighbouring weights.
-template <typename W> __device__ __forceinline__ void move_weights(const PlanEntry t, W* weights, uint32_t i0, uint32_t j0, const F2* v, float* turn, float down, float move) {
-    const uint32_t lane = threadIdx.x % 32;
-    if (t.tall) {
-        const uint32_t col = i0 + lane;
-#pragma unroll
-        for (uint32_t h = 0; h < 2; ++h) {
-            float p[32];
-#pragma unroll
-            for (uint32_t q = 0; q < 32; ++q) {
-                const uint32_t row = j0 + h * 32 + q;
-                p[q] = row < t.rows && col < t.cols ? to_f32(weights[(uint64_t)row * t.cols + col]) : 0.f;
-            }
-#pragma unroll
-            for (uint32_t q = 0; q < 32; ++q) {
-                const uint32_t row = j0 + h * 32 + q;
-                if (row >= t.rows || col >= t.cols) continue;
-                const uint64_t at = (uint64_t)row * t.cols + col;
-                const F2 d = v[(h * 32 + q) / 2];
-                const float x = fmaf(p[q], down, (q & 1 ? hi(d) : lo(d)) * move);
-                weights[at] = from_f32<W>(x);
-                if (t.master) set_element(t.param, t.param_dtype, at, x);
-            }
-        }
-        return;
-    }
-    // row r of the warp's 32 at r * 64, its pieces of four numbers at c ^ r % 8
-#pragma unroll
-    for (uint32_t c = 0; c < 16; ++c) *reinterpret_cast<float4*>(turn + lane * 64 + ((c ^ (lane & 7)) << 2)) = make_float4(lo(v[2 * c]), hi(v[2 * c]), lo(v[2 * c + 1]), hi(v[2 * c + 1]));
-    __syncwarp();
-#pragma unroll
-    for (uint32_t h = 0; h < 2; ++h) {
-        float p[16][2];
-#pragma unroll
-        for (uint32_t q = 0; q < 16; ++q)
-#pragma unroll
-            for (uint32_t w = 0; w < 2; ++w) {
-                const uint32_t row = i0 + h * 16 + q, col = j0 + w * 32 + lane;
-                p[q][w] = row < t.rows && col < t.cols ? to_f32(weights[(uint64_t)row * t.cols + col]) : 0.f;
-            }
-#pragma unroll
-        for (uint32_t q = 0; q < 16; ++q)
-#pragma unroll
-            for (uint32_t w = 0; w < 2; ++w) {
-                const uint32_t r = h * 16 + q, row = i0 + r, c = w * 32 + lane, col = j0 + c;
-                if (row >= t.rows || col >= t.cols) continue;
-                const uint64_t at = (uint64_t)row * t.cols + col;
-                const float x = fmaf(p[q][w], down, turn[r * 64 + (((c >> 2) ^ (r & 7)) << 2) + (c & 3)] * move);
-                weights[at] = from_f32<W>(x);
-                if (t.master) set_element(t.param, t.param_dtype, at, x);
-            }
-    }
-}
-
 template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) muon_product_kernel(MuonArgs a, uint32_t tiles, uint32_t side) {
     namespace cg = cooperative_groups;
     extern __shared__ unsigned char raw[];
@@ -406,13 +437,14 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     unsigned char* const smem = raw + (1024 - (smem_of(raw) & 1023)) % 1024;
     uint64_t* const bars = reinterpret_cast<uint64_t*>(smem + kStages * kStageBytes + 2 * kTeamBytes);
-    // full, landed in the second block, empty (each stage); sums full, sums empty (two each); teams' blocks (two); drained
+    // full, landed in the second block, empty (each stage); sums full, sums empty (two each); drained; warps' rows (two each)
     const uint32_t full = smem_of(bars), landed = full + 8 * kStages, empty = landed + 8 * kStages, sum_full = empty + 8 * kStages, sum_empty = sum_full + 16,
-                   team_full = sum_empty + 16, drained = team_full + 16;
-    uint32_t* const words = reinterpret_cast<uint32_t*>(bars + 3 * kStages + 7);                     // tensor memory, gave up
+                   drained = sum_empty + 16, warp_full = drained + 8;
+    uint32_t* const words = reinterpret_cast<uint32_t*>(bars + 3 * kStages + 21);                    // tensor memory, gave up
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < kStages; ++s) { bar_init(full + 8 * s, 1); bar_init(landed + 8 * s, 1); bar_init(empty + 8 * s, 1); }
-        for (uint32_t s = 0; s < 2; ++s) { bar_init(sum_full + 8 * s, 1); bar_init(sum_empty + 8 * s, MODE == kUpdate ? 18 : 16); bar_init(team_full + 8 * s, 1); }
+        for (uint32_t s = 0; s < 2; ++s) { bar_init(sum_full + 8 * s, 1); bar_init(sum_empty + 8 * s, 16); }
+        for (uint32_t s = 0; s < 16; ++s) bar_init(warp_full + 8 * s, 1);
         bar_init(drained, 1);
         words[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -511,58 +543,58 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                 bar_wait(drained, 0);
             }
         }
-    } else if (MODE == kUpdate && work && warp == 3) {           // a tile's weights into L2 while its products are made
-        uint32_t n = 0;
-        for (uint32_t u = our_pair; u < tiles; u += pairs, ++n) {
-            const Tile tile = tile_of(u);
-            const PlanEntry t = entries[tile.which];
-            const uint32_t i0 = (2 * tile.i + rank) * 128, j0 = tile.j * 256, es = t.master || t.param_dtype == FTC_F32 ? 4 : 2;
-            const uint32_t rows = t.tall ? min(256u, t.w - j0) : i0 < t.m ? min(128u, t.m - i0) : 0, cols = t.tall ? (i0 < t.m ? min(128u, t.m - i0) : 0) : min(256u, t.w - j0);
-            const char* const base = static_cast<const char*>(t.master ? static_cast<const void*>(t.master) : t.param) + ((uint64_t)(t.tall ? j0 : i0) * t.cols + (t.tall ? i0 : j0)) * es;
-            const uint32_t lines = (cols * es + 127) / 128;
-            for (uint32_t e = lane; e < rows * lines; e += 32) {
-                const uint32_t row = e / lines;
-                asm volatile("prefetch.global.L2 [%0];" ::"l"(base + (uint64_t)row * t.cols * es + min((e - row * lines) * 128, cols * es - 1)));
-            }
-            // no further ahead than the next tile, and never behind: the sums' next phase waits for this warp too
-            if (!__all_sync(0xFFFFFFFFu, bar_wait(sum_full + 8 * (n & 1), (n / 2) & 1))) break;
-            if (lane == 0) bar_arrive_at(sum_empty + 8 * (n & 1), 0);
-        }
     } else if (work && warp >= 4) {                              // sums
-        const uint32_t team = (warp - 4) / 4, quarter = warp & 3, r = quarter * 32 + lane;
-        unsigned char* const mine = smem + kStages * kStageBytes + team * kTeamBytes;
-        unsigned char* const other = mine + kBlockBytes;         // the transpose, or the low numbers
-        const uint32_t ready = team_full + 8 * team;
-        const bool leads = quarter == 0 && lane == 0;
-        uint32_t n = 0, blocks = 0;
+        const uint32_t team = (warp - 4) / 4, quarter = warp & 3, pair_id = 1 + team * 2 + quarter / 2, r = quarter * 32 + lane;
+        // a warp's 32 rows of a block of 64 columns (4 KB, the block's rows in order), and what goes with them: the next columns' rows (apply),
+        // its half of the 64 rows' transpose (symmetric), or the low numbers
+        constexpr uint32_t kRows = kBlockBytes / 4;
+        unsigned char* const pair_at = smem + kStages * kStageBytes + (pair_id - 1) * 4 * kRows;
+        unsigned char* const mine = pair_at + (quarter & 1) * kRows;
+        unsigned char* const other = mine + 2 * kRows;
+        const uint32_t ready = warp_full + 16 * (warp - 4);
+        uint32_t n = 0, done[2] = {0, 0};                        // phases of the two barriers
         for (uint32_t u = our_pair; u < tiles && ok; u += pairs, ++n) {
             const Tile tile = tile_of(u);
             const PlanEntry t = entries[tile.which];
             const uint32_t bi = 2 * tile.i + rank, i = bi * 128 + r;
             // blocks of 64 columns of this team: none above the diagonal, none beyond the edges
             const uint32_t cb0 = 4 * tile.j + 2 * team, edge = MODE <= kPoly ? 2 * min(t.mb, bi + 1) : t.nb;
-            uint32_t wanted = bi < t.mb && cb0 < edge ? min(2u, edge - cb0) : 0;
-            if (MODE == kUpdate && !a.live[tile.which]) wanted = 0;
-            for (uint32_t b = 0; b < max(wanted, 1u) && ok; ++b, blocks += wanted ? 1 : 0) {
-                const uint32_t cb = cb0 + b, j0 = cb * 64;
-                const uint64_t here = MODE <= kPoly ? (t.a_block + (uint64_t)bi * 2 * t.mb + cb) * kBlockBytes : (t.x_block + (uint64_t)bi * t.nb + cb) * kBlockBytes;
-                if (wanted && leads) {                           // once the last block has left, the next one may come
-                    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                    if (MODE == kGram) bar_expect(ready, 0);
-                    else {
-                        const unsigned char* from = (MODE == kPoly ? a.a : x_in) + here;
-                        bar_expect(ready, (SPLIT ? 2 : 1) * kBlockBytes);
-                        copy_in(smem_of(mine), from, kBlockBytes, ready);
-                        if (SPLIT) copy_in(smem_of(other), from + (MODE == kPoly ? a.a_bytes : a.x_bytes), kBlockBytes, ready);
-                    }
+            const uint32_t wanted = bi < t.mb && cb0 < edge ? min(2u, edge - cb0) : 0;
+            const uint64_t row_at = (MODE <= kPoly ? t.a_block + (uint64_t)bi * 2 * t.mb : t.x_block + (uint64_t)bi * t.nb) * kBlockBytes + quarter * kRows;
+            const unsigned char* const in = (MODE == kPoly ? a.a : x_in) + row_at;
+            unsigned char* const out = (MODE == kGram ? a.a : MODE == kPoly ? a.b : a.x[side ^ 1]) + row_at;
+            const uint64_t low = MODE <= kPoly ? a.a_bytes : a.x_bytes;
+            auto fetch = [&](uint32_t b, unsigned char* to, uint32_t bar) {              // by one lane
+                const unsigned char* from = in + (uint64_t)(cb0 + b) * kBlockBytes;
+                bar_expect(bar, (SPLIT ? 2 : 1) * kRows);
+                copy_in(smem_of(to), from, kRows, bar);
+                if (SPLIT) copy_in(smem_of(to) + 2 * kRows, from + low, kRows, bar);
+            };
+            if (MODE == kApply && !SPLIT && lane == 0 && wanted) {                        // both of the tile's blocks, once the last ones have left
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                fetch(0, mine, ready);
+                if (wanted > 1) fetch(1, other, ready + 8);
+            }
+            for (uint32_t b = 0; b < max(wanted, 1u) && ok; ++b) {
+                const uint32_t cb = cb0 + b, j0 = cb * 64, which = MODE == kApply && !SPLIT ? b : 0;
+                unsigned char* const here = which ? other : mine;
+                if (wanted && MODE != kApply) {                  // the pair's memory is free once both have seen their stores leave
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    asm volatile("bar.sync %0, 64;" ::"r"(pair_id) : "memory");
+                    if (MODE == kPoly && lane == 0) fetch(b, mine, ready);
                 }
-                ok = (b || bar_wait(sum_full + 8 * (n & 1), (n / 2) & 1)) && (!wanted || bar_wait(ready, blocks & 1));
-                ok = all_of_team(team, ok);                      // one goes on only if all do
+                if (wanted && MODE == kApply && SPLIT && lane == 0) {
+                    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    fetch(b, mine, ready);
+                }
+                ok = (b || bar_wait(sum_full + 8 * (n & 1), (n / 2) & 1)) && (!wanted || MODE == kGram || bar_wait(ready + 8 * which, done[which] & 1));
+                if (MODE == kApply) ok = __all_sync(0xFFFFFFFFu, ok);
+                else ok = all_of_pair(4 + pair_id, ok);          // one goes on only if both do
                 if (!ok || !wanted) break;
+                ++done[which];
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 F2 v[32];
-                read_32(v, tmem + (n & 1) * 256 + (quarter * 32 << 16) + team * 128 + b * 64);
-                read_32(v + 16, tmem + (n & 1) * 256 + (quarter * 32 << 16) + team * 128 + b * 64 + 32);
+                read_64(v, tmem + (n & 1) * 256 + (quarter * 32 << 16) + team * 128 + b * 64);
                 // the row's own place on the diagonal, in the block of columns that holds it
                 const bool diagonal = MODE <= kPoly && i / 64 == cb;
                 const uint32_t own = i % 64;
@@ -586,10 +618,10 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                     if (MODE == kPoly && diagonal) a.diag_b[t.diagonal + i] = fmaf(kQ5, fmaf(di, di, mine_own), kQ3 * di);
 #pragma unroll
                     for (uint32_t c = 0; c < 8; ++c) {
-                        const uint4 h = *reinterpret_cast<const uint4*>(mine + piece(r, c));
+                        const uint4 h = *reinterpret_cast<const uint4*>(here + piece(lane, c));
                         F2 e[4] = {pair_of(h.x), pair_of(h.y), pair_of(h.z), pair_of(h.w)};
                         if (SPLIT) {
-                            const uint4 l = *reinterpret_cast<const uint4*>(other + piece(r, c));
+                            const uint4 l = *reinterpret_cast<const uint4*>(other + piece(lane, c));
                             e[0] = add(e[0], pair_of(l.x)); e[1] = add(e[1], pair_of(l.y)); e[2] = add(e[2], pair_of(l.z)); e[3] = add(e[3], pair_of(l.w));
                         }
                         if (MODE == kPoly) {
@@ -603,18 +635,6 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                         }
                     }
                 }
-                if (MODE == kUpdate) {
-                    asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory");        // all have read X
-                    const float l = a.lr * t.lr_scale, down = 1.f - l * t.weight_decay, move = -l * kDown;
-                    float* turn = reinterpret_cast<float*>(mine) + quarter * 32 * 64;
-                    if (t.master) move_weights(t, t.master, i - lane, j0, v, turn, down, move);
-                    else if (t.param_dtype == FTC_F32) move_weights(t, static_cast<float*>(t.param), i - lane, j0, v, turn, down, move);
-                    else if (t.param_dtype == FTC_BF16) move_weights(t, static_cast<__nv_bfloat16*>(t.param), i - lane, j0, v, turn, down, move);
-                    else move_weights(t, static_cast<__half*>(t.param), i - lane, j0, v, turn, down, move);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");         // before the next copy into it
-                    asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory");
-                    continue;
-                }
                 uint32_t h[32], low_h[SPLIT ? 32 : 1];
 #pragma unroll
                 for (int q = 0; q < 32; ++q) h[q] = half2_of(v[q]);
@@ -627,46 +647,41 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                 }
 #pragma unroll
                 for (uint32_t c = 0; c < 8; ++c) {
-                    *reinterpret_cast<uint4*>(mine + piece(r, c)) = make_uint4(h[4 * c], h[4 * c + 1], h[4 * c + 2], h[4 * c + 3]);
-                    if (SPLIT) *reinterpret_cast<uint4*>(other + piece(r, c)) = make_uint4(low_h[4 * c], low_h[4 * c + 1], low_h[4 * c + 2], low_h[4 * c + 3]);
+                    *reinterpret_cast<uint4*>(here + piece(lane, c)) = make_uint4(h[4 * c], h[4 * c + 1], h[4 * c + 2], h[4 * c + 3]);
+                    if (SPLIT) *reinterpret_cast<uint4*>(other + piece(lane, c)) = make_uint4(low_h[4 * c], low_h[4 * c + 1], low_h[4 * c + 2], low_h[4 * c + 3]);
                 }
                 if (diagonal) {
-                    *reinterpret_cast<uint16_t*>(mine + piece(r, own / 8) + own % 8 * 2) = 0;
-                    if (SPLIT) *reinterpret_cast<uint16_t*>(other + piece(r, own / 8) + own % 8 * 2) = 0;
+                    *reinterpret_cast<uint16_t*>(mine + piece(lane, own / 8) + own % 8 * 2) = 0;
+                    if (SPLIT) *reinterpret_cast<uint16_t*>(other + piece(lane, own / 8) + own % 8 * 2) = 0;
                 }
-                unsigned char* const out = MODE == kGram ? a.a : MODE == kPoly ? a.b : a.x[side ^ 1];
-                const uint64_t low = MODE <= kPoly ? a.a_bytes : a.x_bytes;
                 const bool both = MODE <= kPoly && cb / 2 < bi;                          // below the diagonal: the transpose too
-                // element (j, i): 64 rows, two blocks of 64 columns, each half a block
-                const uint64_t there = both ? (t.a_block + (uint64_t)(cb / 2) * 2 * t.mb + 2 * bi) * kBlockBytes + cb % 2 * (kBlockBytes / 2) : 0;
+                // element (j, i) of the pair's 64 rows i: half a block of 64 rows j
+                unsigned char* const there = (MODE == kGram ? a.a : a.b) + (t.a_block + (uint64_t)(cb / 2) * 2 * t.mb + 2 * bi + quarter / 2) * kBlockBytes + cb % 2 * (kBlockBytes / 2);
                 auto turned = [&](unsigned char* to, const uint32_t* w) {
-                    unsigned char* const half = to + r / 64 * (kBlockBytes / 2) + r % 8 * 2;
 #pragma unroll
                     for (uint32_t q = 0; q < 64; ++q)
-                        *reinterpret_cast<uint16_t*>(half + piece(q, r % 64 / 8)) = (uint16_t)(q & 1 ? w[q / 2] >> 16 : w[q / 2]);
+                        *reinterpret_cast<uint16_t*>(to + r % 8 * 2 + piece(q, r % 64 / 8)) = (uint16_t)(q & 1 ? w[q / 2] >> 16 : w[q / 2]);
                 };
-                if (both && !SPLIT) turned(other, h);
+                if (both && !SPLIT) turned(pair_at + 2 * kRows, h);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory");
-                if (leads) {
-                    copy_out(out + here, smem_of(mine), kBlockBytes);
-                    if (SPLIT) copy_out(out + low + here, smem_of(other), kBlockBytes);
-                    else if (both)
-                        for (uint32_t q = 0; q < 2; ++q) copy_out(out + there + q * kBlockBytes, smem_of(other) + q * (kBlockBytes / 2), kBlockBytes / 2);
+                __syncwarp();
+                if (lane == 0) {
+                    copy_out(out + (uint64_t)cb * kBlockBytes, smem_of(here), kRows);
+                    if (SPLIT) copy_out(out + (uint64_t)cb * kBlockBytes + low, smem_of(other), kRows);
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
-                if (both && SPLIT) {                             // both of the transpose's numbers, once theirs have left
-                    if (leads) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                    asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory");
-                    turned(mine, h);
-                    turned(other, low_h);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory");
-                    if (leads) {
-                        for (uint32_t q = 0; q < 2; ++q) {
-                            copy_out(out + there + q * kBlockBytes, smem_of(mine) + q * (kBlockBytes / 2), kBlockBytes / 2);
-                            copy_out(out + low + there + q * kBlockBytes, smem_of(other) + q * (kBlockBytes / 2), kBlockBytes / 2);
-                        }
+                if (both) {
+                    if (SPLIT) {                                 // both of the transpose's numbers, once theirs have left
+                        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                        asm volatile("bar.sync %0, 64;" ::"r"(pair_id) : "memory");
+                        turned(pair_at, h);
+                        turned(pair_at + 2 * kRows, low_h);
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    }
+                    asm volatile("bar.sync %0, 64;" ::"r"(pair_id) : "memory");
+                    if (lane == 0 && !(quarter & 1)) {
+                        copy_out(there, smem_of(pair_at) + (SPLIT ? 0 : 2 * kRows), 2 * kRows);
+                        if (SPLIT) copy_out(there + low, smem_of(pair_at) + 2 * kRows, 2 * kRows);
                         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     }
                 }
@@ -677,10 +692,10 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                 if (lane == 0) bar_arrive_at(sum_empty + 8 * (n & 1), 0);
             }
         }
-        if (leads) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-        if (!ok) {
-            if (lane == 0) words[1] = 1;
-            if (leads) bar_wait(ready, blocks & 1);              // a copy that may be in flight
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        if (!ok && lane == 0) {
+            words[1] = 1;
+            for (uint32_t w = 0; w < 2; ++w) bar_wait(ready + 8 * w, done[w] & 1);       // copies that may be in flight
         }
     }
     __syncwarp();
@@ -709,7 +724,7 @@ template <bool SPLIT> static cudaError_t products(const MuonArgs& a, int sms, cu
     for (uint32_t s = 0; s < a.steps && e == cudaSuccess; ++s) {
         e = product<kGram, SPLIT>(a, a.items[kGramTiles], s & 1, sms, st);
         if (e == cudaSuccess) e = product<kPoly, SPLIT>(a, a.items[kGramTiles], s & 1, sms, st);
-        if (e == cudaSuccess) e = s + 1 < a.steps ? product<kApply, SPLIT>(a, a.items[kApplyTiles], s & 1, sms, st) : product<kUpdate, SPLIT>(a, a.items[kApplyTiles], s & 1, sms, st);
+        if (e == cudaSuccess) e = product<kApply, SPLIT>(a, a.items[kApplyTiles], s & 1, sms, st);
     }
     return e;
 }
@@ -720,6 +735,7 @@ cudaError_t launch_muon(const MuonArgs& a, int sms, cudaStream_t st) {
     if (e == cudaSuccess) e = launch_second(muon_norm_kernel, a.n, 256, st, a);
     if (e == cudaSuccess) e = launch_second(muon_layout_kernel, a.items[kBlocks], 256, st, a);
     if (e == cudaSuccess) e = a.split ? products<true>(a, sms, st) : products<false>(a, sms, st);
+    if (e == cudaSuccess) e = launch_second(muon_update_kernel, a.items[kBlocks], 256, st, a);
     return e;
 }
 
