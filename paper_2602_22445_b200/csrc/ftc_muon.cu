@@ -4,7 +4,7 @@
 // step follow, each over all matrices at once:
 //   gram   A = X X^T             symmetric: tiles on and below the diagonal, written twice
 //   poly   B = b A + c A A       symmetric too (A A = A A^T)
-//   apply  X = a X + B X         the last one updates the weights instead
+//   apply  X = (a + B) X         with a in B's diagonal
 // Operands are float16, held times 2^14: |X| stays below 1.21 after the first step (the largest value of the quintic on 0 .. 1.21), entries of
 // A below 1.47 and of B below 2.81, so nothing overflows and numbers down to 2^-28 keep their 11 bits (bfloat16 would keep 8). Diagonals,
 // which are the large entries of A and B in late steps, are held apart in float32: with A = D + A', A A = A' A' + D A' + A' D + D D, all but
@@ -23,22 +23,42 @@ constexpr float kQ1 = 3.4445f, kQ3 = -4.7750f, kQ5 = 2.0315f;
 constexpr float kUp = 16384.f, kDown = 1.f / 16384.f, kDown2 = kDown * kDown;    // 2^14
 constexpr uint32_t kBlockBytes = 128 * 64 * 2;
 
-__device__ __forceinline__ float element(const void* p, uint32_t dtype, uint64_t i) {
-    if (dtype == FTC_F32) return static_cast<const float*>(p)[i];
-    if (dtype == FTC_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
-    return __half2float(static_cast<const __half*>(p)[i]);
-}
-__device__ __forceinline__ void set_element(void* p, uint32_t dtype, uint64_t i, float v) {
-    if (dtype == FTC_F32) static_cast<float*>(p)[i] = v;
-    else if (dtype == FTC_BF16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
-    else static_cast<__half*>(p)[i] = __float2half_rn(v);
-}
 // What the gradient is multiplied with: 1 / processes included, 0: not delivered.
 __device__ __forceinline__ float share_at(const PlanEntry& t, uint64_t i) {
     if (!t.status) return 1.f;
     const uint64_t q = t.k_shift != 255 ? i >> t.k_shift : (uint32_t)i / t.k;
     const uint2 s = *reinterpret_cast<const uint2*>(t.status + q * FTC_STATUS_WORDS);
     return (s.x & 0xFFu) == FTC_ST_OK && s.y ? 1.f / (float)s.y : 0.f;
+}
+
+// N elements at at(0), at(1), ... where there(i): all loads out before anything else.
+template <typename T, int N, typename A, typename B> __device__ __forceinline__ void gather_of(float (&v)[N], const T* p, A at, B there) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = there(i) ? to_f32(p[at(i)]) : 0.f;
+}
+template <int N, typename A, typename B> __device__ __forceinline__ void gather(float (&v)[N], const void* p, uint32_t dtype, A at, B there) {
+    if (dtype == FTC_F32) gather_of(v, static_cast<const float*>(p), at, there);
+    else if (dtype == FTC_BF16) gather_of(v, static_cast<const __nv_bfloat16*>(p), at, there);
+    else gather_of(v, static_cast<const __half*>(p), at, there);
+}
+template <typename T, int N, typename A, typename B> __device__ __forceinline__ void scatter_of(const float (&v)[N], T* p, A at, B there) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (there(i)) p[at(i)] = from_f32<T>(v[i]);
+}
+template <int N, typename A, typename B> __device__ __forceinline__ void scatter(const float (&v)[N], void* p, uint32_t dtype, A at, B there) {
+    if (dtype == FTC_F32) scatter_of(v, static_cast<float*>(p), at, there);
+    else if (dtype == FTC_BF16) scatter_of(v, static_cast<__nv_bfloat16*>(p), at, there);
+    else scatter_of(v, static_cast<__half*>(p), at, there);
+}
+template <int N, typename A, typename B> __device__ __forceinline__ void gather_shares(float (&v)[N], const PlanEntry& t, A at, B there) {
+    if (!t.status) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = there(i) ? 1.f : 0.f;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = there(i) ? share_at(t, at(i)) : 0.f;
 }
 
 // ---- momentum ----
@@ -59,6 +79,21 @@ __device__ __forceinline__ void eight(float* v, const void* p, uint32_t dtype, u
         else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j])); v[2 * j] = f.x; v[2 * j + 1] = f.y; }
     }
 }
+__device__ __forceinline__ void store_eight(void* p, uint32_t dtype, uint64_t i, const float* v) {
+    if (dtype == FTC_F32) {
+        float4* q = reinterpret_cast<float4*>(static_cast<float*>(p) + i);
+        q[0] = make_float4(v[0], v[1], v[2], v[3]); q[1] = make_float4(v[4], v[5], v[6], v[7]);
+        return;
+    }
+    uint4 r;
+    uint32_t* w = &r.x;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (dtype == FTC_BF16) { const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]); w[j] = *reinterpret_cast<const uint32_t*>(&h); }
+        else { const __half2 h = __floats2half2_rn(v[2 * j], v[2 * j + 1]); w[j] = *reinterpret_cast<const uint32_t*>(&h); }
+    }
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + i) = r;
+}
 // Shares of eight neighbours; messages of a multiple of 8 elements have one for all.
 __device__ __forceinline__ void eight_shares(float* s, const PlanEntry& t, uint64_t i) {
     const float one = share_at(t, i);
@@ -68,7 +103,7 @@ __device__ __forceinline__ void eight_shares(float* s, const PlanEntry& t, uint6
 
 // A block has 4096 elements of one matrix: twice eight a thread, neighbours where the addresses allow it (t.wide), 256 apart otherwise; all loads
 // are out before the first is used.
-__global__ void __launch_bounds__(256) muon_momentum_kernel(MuonArgs a) {
+__global__ void __launch_bounds__(256, 4) muon_momentum_kernel(MuonArgs a) {
     later_kernel_may_start();
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.word = 0;
     const float scale = a.grad_scale ? *a.grad_scale : 1.f;
@@ -78,53 +113,42 @@ __global__ void __launch_bounds__(256) muon_momentum_kernel(MuonArgs a) {
     const uint64_t begin = (uint64_t)(blockIdx.x - t.first[kChunks]) * kMuonChunk;
     const uint32_t left = (uint32_t)min((uint64_t)kMuonChunk, t.n - begin);
     float* m = a.momentum + t.first_block * FTC_STATE_BLOCK + begin;
-    float old[2][8], g[2][8], s[2][8];
+    float old[16], g[16], s[16];
     const bool wide = t.wide && left == kMuonChunk;
+    auto at = [&](int j) { return (uint32_t)(threadIdx.x + j * 256); };
+    auto there = [&](int j) { return at(j) < left; };
     if (wide) {
 #pragma unroll
         for (uint32_t w = 0; w < 2; ++w) {
             const uint32_t e = (w * 256 + threadIdx.x) * 8;
-            eight(old[w], m, FTC_F32, e);
-            eight(g[w], t.grad, t.grad_dtype, begin + e);
-            eight_shares(s[w], t, begin + e);
+            eight(old + 8 * w, m, FTC_F32, e);
+            eight(g + 8 * w, t.grad, t.grad_dtype, begin + e);
+            eight_shares(s + 8 * w, t, begin + e);
         }
     } else {
-#pragma unroll
-        for (uint32_t j = 0; j < 16; ++j) {
-            const uint32_t e = threadIdx.x + j * 256;
-            const bool there = e < left;
-            old[j / 8][j % 8] = there ? m[e] : 0.f;
-            g[j / 8][j % 8] = there ? element(t.grad, t.grad_dtype, begin + e) : 0.f;
-            s[j / 8][j % 8] = there ? share_at(t, begin + e) : 0.f;
-        }
+        gather(old, m, FTC_F32, at, there);
+        gather(g, t.grad, t.grad_dtype, [&](int j) { return begin + at(j); }, there);
+        gather_shares(s, t, [&](int j) { return begin + at(j); }, there);
     }
     double sum = 0;
     uint32_t live = 0;
 #pragma unroll
     for (uint32_t j = 0; j < 16; ++j) {
-        float& x = old[j / 8][j % 8];
-        float u = x;
-        if (s[j / 8][j % 8] > 0.f) {
-            const float d = g[j / 8][j % 8] * s[j / 8][j % 8] * scale;
-            x = fmaf(x, a.mu, d);
-            u = a.nesterov ? fmaf(x, a.mu, d) : x;
+        float u = old[j];
+        if (s[j] > 0.f) {
+            const float d = g[j] * s[j] * scale;
+            old[j] = fmaf(old[j], a.mu, d);
+            u = a.nesterov ? fmaf(old[j], a.mu, d) : old[j];
             live |= 1u << j;
         }
         sum = ::fma((double)u, (double)u, sum);
     }
     if (wide) {
 #pragma unroll
-        for (uint32_t w = 0; w < 2; ++w) {
-            float4* q = reinterpret_cast<float4*>(m + (w * 256 + threadIdx.x) * 8);
-            if (live >> (8 * w) & 0xFFu) {
-                q[0] = make_float4(old[w][0], old[w][1], old[w][2], old[w][3]);
-                q[1] = make_float4(old[w][4], old[w][5], old[w][6], old[w][7]);
-            }
-        }
+        for (uint32_t w = 0; w < 2; ++w)
+            if (live >> (8 * w) & 0xFFu) store_eight(m, FTC_F32, (w * 256 + threadIdx.x) * 8, old + 8 * w);
     } else {
-#pragma unroll
-        for (uint32_t j = 0; j < 16; ++j)
-            if (live >> j & 1u) m[threadIdx.x + j * 256] = old[j / 8][j % 8];
+        scatter(old, m, FTC_F32, at, [&](int j) { return live >> j & 1u; });
     }
     __shared__ double sums[8];
     __shared__ uint32_t lives[8];
@@ -162,7 +186,7 @@ __device__ __forceinline__ uint32_t piece(uint32_t r, uint32_t c) { return r * 1
 
 // One block of 128 x 64 of X. Elements that are neighbours in memory are loaded by one thread (eight, where the addresses allow it) or by
 // neighbouring threads; a block whose matrix is transposed is turned in shared memory.
-__global__ void __launch_bounds__(256) muon_layout_kernel(MuonArgs a) {
+__global__ void __launch_bounds__(256, 4) muon_layout_kernel(MuonArgs a) {
     wait_for_earlier_kernel();
     later_kernel_may_start();
     const float scale = a.grad_scale ? *a.grad_scale : 1.f;
@@ -173,6 +197,7 @@ __global__ void __launch_bounds__(256) muon_layout_kernel(MuonArgs a) {
     const float inv = a.factor[which];
     const float* m = a.momentum + t.first_block * FTC_STATE_BLOCK;
     __shared__ __align__(16) unsigned char tile[2][kBlockBytes];
+    unsigned char* const out = a.x[0] + (t.x_block + at) * kBlockBytes;
     auto value = [&](float v, float g, float s) { return (a.nesterov && s > 0.f ? fmaf(v, a.mu, g * s * scale) : v) * inv; };
     auto put = [&](uint32_t r, uint32_t c, float v) {
         const __half h = __float2half_rn(v);
@@ -180,10 +205,9 @@ __global__ void __launch_bounds__(256) muon_layout_kernel(MuonArgs a) {
         *reinterpret_cast<__half*>(tile[0] + to) = h;
         if (a.split) *reinterpret_cast<__half*>(tile[1] + to) = __float2half_rn(v - __half2float(h));
     };
-    const bool whole = bi * 128 + 128 <= t.m && bj * 64 + 64 <= t.w;
-    if (whole && t.wide && t.cols % 8 == 0) {
-        // runs of 64 neighbours in 128 rows of memory, or of 128 in 64 (transposed)
-        // of the transposed ones neighbouring threads have neighbouring lines, so that they write neighbours in shared memory
+    if (bi * 128 + 128 <= t.m && bj * 64 + 64 <= t.w && t.wide && t.cols % 8 == 0) {
+        // runs of 64 neighbours in 128 rows of memory: pieces as they are; or of 128 in 64 (transposed): neighbouring threads have neighbouring
+        // lines, so that they write neighbours in shared memory
 #pragma unroll
         for (uint32_t u = 0; u < 2; ++u) {
             float v[2][8], g[2][8], s[2][8];
@@ -203,91 +227,87 @@ __global__ void __launch_bounds__(256) muon_layout_kernel(MuonArgs a) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) put(run[w] + j, line[w], value(v[w][j], g[w][j], s[w][j]));
                 } else {
-                    __half h[8], l[8];
+                    float x[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float x = value(v[w][j], g[w][j], s[w][j]);
-                        h[j] = __float2half_rn(x); l[j] = __float2half_rn(x - __half2float(h[j]));
-                    }
+                    for (int j = 0; j < 8; ++j) x[j] = value(v[w][j], g[w][j], s[w][j]);
                     const uint32_t to = piece(line[w], run[w] / 8);
-                    *reinterpret_cast<uint4*>(tile[0] + to) = *reinterpret_cast<const uint4*>(h);
-                    if (a.split) *reinterpret_cast<uint4*>(tile[1] + to) = *reinterpret_cast<const uint4*>(l);
+                    store_eight(out + to, FTC_F16, 0, x);
+                    if (a.split) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) x[j] -= __half2float(__float2half_rn(x[j]));
+                        store_eight(out + a.x_bytes + to, FTC_F16, 0, x);
+                    }
                 }
             }
         }
+        if (!t.tall) return;
     } else {
         for (uint32_t e0 = threadIdx.x; e0 < 128 * 64; e0 += 2048) {
-            float v[8], g[8], s[8];
+            float v[8], g[8] = {}, s[8] = {};
+            auto row = [&](int w) { const uint32_t e = e0 + w * 256; return t.tall ? e % 128 : e / 64; };
+            auto col = [&](int w) { const uint32_t e = e0 + w * 256; return t.tall ? e / 128 : e % 64; };
+            auto there = [&](int w) { return bi * 128 + row(w) < t.m && bj * 64 + col(w) < t.w; };
+            auto place = [&](int w) {
+                const uint32_t i = bi * 128 + row(w), j = bj * 64 + col(w);
+                return t.tall ? (uint64_t)j * t.cols + i : (uint64_t)i * t.cols + j;
+            };
+            gather(v, m, FTC_F32, place, there);
+            if (a.nesterov) { gather(g, t.grad, t.grad_dtype, place, there); gather_shares(s, t, place, there); }
 #pragma unroll
-            for (uint32_t w = 0; w < 8; ++w) {
-                const uint32_t e = e0 + w * 256, r = t.tall ? e % 128 : e / 64, c = t.tall ? e / 128 : e % 64, i = bi * 128 + r, j = bj * 64 + c;
-                const bool there = i < t.m && j < t.w;
-                const uint64_t q = t.tall ? (uint64_t)j * t.cols + i : (uint64_t)i * t.cols + j;
-                v[w] = there ? m[q] : 0.f;
-                g[w] = there && a.nesterov ? element(t.grad, t.grad_dtype, q) : 0.f;
-                s[w] = there && a.nesterov ? share_at(t, q) : 0.f;
-            }
-#pragma unroll
-            for (uint32_t w = 0; w < 8; ++w) {
-                const uint32_t e = e0 + w * 256, r = t.tall ? e % 128 : e / 64, c = t.tall ? e / 128 : e % 64;
-                put(r, c, value(v[w], g[w], s[w]));
-            }
+            for (int w = 0; w < 8; ++w) put(row(w), col(w), value(v[w], g[w], s[w]));
         }
     }
     __syncthreads();
     for (uint32_t s = 0; s <= a.split; ++s) {
-        uint4* to = reinterpret_cast<uint4*>(a.x[0] + s * a.x_bytes + (t.x_block + at) * kBlockBytes);
+        uint4* to = reinterpret_cast<uint4*>(out + s * a.x_bytes);
         const uint4* from = reinterpret_cast<const uint4*>(tile[s]);
         for (uint32_t e = threadIdx.x; e < kBlockBytes / 16; e += 256) to[e] = from[e];
     }
 }
 
 // The weights that one block of 128 x 64 of X moves; elements as in the layout.
-__device__ __forceinline__ void store_eight(void* p, uint32_t dtype, uint64_t i, const float* v) {
-    if (dtype == FTC_F32) {
-        float4* q = reinterpret_cast<float4*>(static_cast<float*>(p) + i);
-        q[0] = make_float4(v[0], v[1], v[2], v[3]); q[1] = make_float4(v[4], v[5], v[6], v[7]);
-        return;
-    }
-    uint4 r;
-    uint32_t* w = &r.x;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (dtype == FTC_BF16) { const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]); w[j] = *reinterpret_cast<const uint32_t*>(&h); }
-        else { const __half2 h = __floats2half2_rn(v[2 * j], v[2 * j + 1]); w[j] = *reinterpret_cast<const uint32_t*>(&h); }
-    }
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + i) = r;
-}
-__global__ void __launch_bounds__(256) muon_update_kernel(MuonArgs a) {
+__global__ void __launch_bounds__(256, 4) muon_update_kernel(MuonArgs a) {
     wait_for_earlier_kernel();
     const float scale = a.grad_scale ? *a.grad_scale : 1.f;
     const uint32_t which = a.maps[kBlocks][blockIdx.x];
     if (!isfinite(scale) || *reinterpret_cast<volatile uint32_t*>(a.word) || !a.live[which]) return;
     const PlanEntry t = plan_entries(a.plan)[which];
     const uint32_t at = blockIdx.x - t.first[kBlocks], bi = at / t.nb, bj = at - bi * t.nb;
-    const unsigned char* const x = a.x[a.steps & 1] + (t.x_block + at) * kBlockBytes;
+    const unsigned char* const x_at = a.x[a.steps & 1] + (t.x_block + at) * kBlockBytes;
     const float l = a.lr * t.lr_scale, down = 1.f - l * t.weight_decay, move = -l * kDown;
     void* const weights = t.master ? static_cast<void*>(t.master) : t.param;
     const uint32_t dtype = t.master ? FTC_F32 : t.param_dtype;
     __shared__ __align__(16) unsigned char tile[2][kBlockBytes];
     const bool whole = bi * 128 + 128 <= t.m && bj * 64 + 64 <= t.w && t.wide && t.cols % 8 == 0;
-    float p[4][8];
-    uint64_t place[4];
-    if (whole) {                                                 // weights first: they come from memory, X from L2 if at all
+    if (whole && !t.tall) {                                      // pieces as they are
 #pragma unroll
-        for (uint32_t u = 0; u < 4; ++u) {
-            const uint32_t e = threadIdx.x + u * 256, line = t.tall ? threadIdx.x % 64 : e / 8, run = t.tall ? (threadIdx.x / 64 * 4 + u) * 8 : e % 8 * 8;
-            place[u] = t.tall ? (uint64_t)(bj * 64 + line) * t.cols + bi * 128 + run : (uint64_t)(bi * 128 + line) * t.cols + bj * 64 + run;
-            eight(p[u], weights, dtype, place[u]);
+        for (uint32_t h = 0; h < 2; ++h) {
+            float p[2][8], x[2][8], y[2][8];
+            uint64_t place[2];
+#pragma unroll
+            for (uint32_t u = 0; u < 2; ++u) {
+                const uint32_t e = threadIdx.x + (2 * h + u) * 256, line = e / 8, run = e % 8 * 8;
+                place[u] = (uint64_t)(bi * 128 + line) * t.cols + bj * 64 + run;
+                eight(p[u], weights, dtype, place[u]);
+                eight(x[u], x_at + piece(line, run / 8), FTC_F16, 0);
+                if (a.split) eight(y[u], x_at + a.x_bytes + piece(line, run / 8), FTC_F16, 0);
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < 2; ++u) {
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) p[u][j] = fmaf(p[u][j], down, (a.split ? x[u][j] + y[u][j] : x[u][j]) * move);
+                store_eight(weights, dtype, place[u], p[u]);
+                if (t.master) store_eight(t.param, t.param_dtype, place[u], p[u]);
+            }
         }
+        return;
     }
     for (uint32_t s = 0; s <= a.split; ++s) {
-        const uint4* from = reinterpret_cast<const uint4*>(x + s * a.x_bytes);
+        const uint4* from = reinterpret_cast<const uint4*>(x_at + s * a.x_bytes);
         uint4* to = reinterpret_cast<uint4*>(tile[s]);
 #pragma unroll
         for (uint32_t e = 0; e < kBlockBytes / 16 / 256; ++e) to[threadIdx.x + e * 256] = from[threadIdx.x + e * 256];
     }
-    __syncthreads();
     auto update = [&](uint32_t r, uint32_t c) {
         const uint32_t q = piece(r, c / 8) + c % 8 * 2;
         float v = __half2float(*reinterpret_cast<const __half*>(tile[0] + q));
@@ -295,32 +315,36 @@ __global__ void __launch_bounds__(256) muon_update_kernel(MuonArgs a) {
         return v * move;
     };
     if (whole) {
+        const uint32_t line = threadIdx.x % 64, run = threadIdx.x / 64 * 32;
+        const uint64_t place = (uint64_t)(bj * 64 + line) * t.cols + bi * 128 + run;
+        float p[4][8];
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) eight(p[u], weights, dtype, place + u * 8);
+        __syncthreads();
 #pragma unroll
         for (uint32_t u = 0; u < 4; ++u) {
-            const uint32_t e = threadIdx.x + u * 256, line = t.tall ? threadIdx.x % 64 : e / 8, run = t.tall ? (threadIdx.x / 64 * 4 + u) * 8 : e % 8 * 8;
 #pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) p[u][j] = fmaf(p[u][j], down, t.tall ? update(run + j, line) : update(line, run + j));
-            store_eight(weights, dtype, place[u], p[u]);
-            if (t.master) store_eight(t.param, t.param_dtype, place[u], p[u]);
+            for (uint32_t j = 0; j < 8; ++j) p[u][j] = fmaf(p[u][j], down, update(run + u * 8 + j, line));
+            store_eight(weights, dtype, place + u * 8, p[u]);
+            if (t.master) store_eight(t.param, t.param_dtype, place + u * 8, p[u]);
         }
         return;
     }
+    __syncthreads();
     for (uint32_t e0 = threadIdx.x; e0 < 128 * 64; e0 += 2048) {
         float v[8];
+        auto row = [&](int w) { const uint32_t e = e0 + w * 256; return t.tall ? e % 128 : e / 64; };
+        auto col = [&](int w) { const uint32_t e = e0 + w * 256; return t.tall ? e / 128 : e % 64; };
+        auto there = [&](int w) { return bi * 128 + row(w) < t.m && bj * 64 + col(w) < t.w; };
+        auto place = [&](int w) {
+            const uint32_t i = bi * 128 + row(w), j = bj * 64 + col(w);
+            return t.tall ? (uint64_t)j * t.cols + i : (uint64_t)i * t.cols + j;
+        };
+        gather(v, weights, dtype, place, there);
 #pragma unroll
-        for (uint32_t w = 0; w < 8; ++w) {
-            const uint32_t e = e0 + w * 256, r = t.tall ? e % 128 : e / 64, c = t.tall ? e / 128 : e % 64, i = bi * 128 + r, j = bj * 64 + c;
-            v[w] = i < t.m && j < t.w ? element(weights, dtype, t.tall ? (uint64_t)j * t.cols + i : (uint64_t)i * t.cols + j) : 0.f;
-        }
-#pragma unroll
-        for (uint32_t w = 0; w < 8; ++w) {
-            const uint32_t e = e0 + w * 256, r = t.tall ? e % 128 : e / 64, c = t.tall ? e / 128 : e % 64, i = bi * 128 + r, j = bj * 64 + c;
-            if (i >= t.m || j >= t.w) continue;
-            const uint64_t q = t.tall ? (uint64_t)j * t.cols + i : (uint64_t)i * t.cols + j;
-            const float y = fmaf(v[w], down, update(r, c));
-            set_element(weights, dtype, q, y);
-            if (t.master) set_element(t.param, t.param_dtype, q, y);
-        }
+        for (int w = 0; w < 8; ++w) v[w] = fmaf(v[w], down, update(row(w), col(w)));
+        scatter(v, weights, dtype, place, there);
+        if (t.master) scatter(v, t.param, t.param_dtype, place, there);
     }
 }
 
@@ -332,12 +356,12 @@ __global__ void __launch_bounds__(256) muon_update_kernel(MuonArgs a) {
 // holds 64 of the inner dimension: 16 KB of each operand in each block.
 //   warp 0   copies of its block's operands
 //   warp 1   first block: matrix instructions; second block: tells the first when its copies have landed
-//   warps 4 .. 11   two teams of four read sums out (a warp reads the 32 lanes of tensor memory that its number modulo 4 gives it), the
-//            first team the left 128 columns, the second the right ones, 64 at a time: what the result needs of A or X comes into the
-//            team's shared memory as a block, is replaced there by the result, and goes out as a block; so does its transpose.
+//   warps 4 .. 11   read sums out (a warp reads the 32 lanes of tensor memory that its number modulo 4 gives it), the first four those of the
+//            left 128 columns, the others the right ones', 64 at a time, each warp for itself: what the result needs of A comes into shared
+//            memory as 4 KB, is replaced there by the result, and goes out as 4 KB; its transpose in stores of 64 bytes.
 
-constexpr uint32_t kStages = 5, kStageBytes = 2 * kBlockBytes, kTeamBytes = 2 * kBlockBytes, kProductThreads = 384;
-constexpr uint32_t kProductSmem = kStages * kStageBytes + 2 * kTeamBytes + 1024 + 512;
+constexpr uint32_t kStages = 5, kStageBytes = 2 * kBlockBytes, kRows = kBlockBytes / 4, kProductThreads = 384;
+constexpr uint32_t kProductSmem = kStages * kStageBytes + 16 * kRows + 1024 + 512;
 static_assert(kProductSmem <= 227 * 1024, "shared memory of a block");
 enum { kGram, kPoly, kApply };
 
@@ -360,12 +384,6 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
         if (ok) return true;
     }
     return false;
-}
-// Do both warps of a pair say yes?
-__device__ __forceinline__ bool all_of_pair(uint32_t id, bool ok) {
-    uint32_t all;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"((uint32_t)ok), "r"(id) : "memory");
-    return all;
 }
 __device__ __forceinline__ void copy_in(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -436,7 +454,7 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
     uint32_t rank;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     unsigned char* const smem = raw + (1024 - (smem_of(raw) & 1023)) % 1024;
-    uint64_t* const bars = reinterpret_cast<uint64_t*>(smem + kStages * kStageBytes + 2 * kTeamBytes);
+    uint64_t* const bars = reinterpret_cast<uint64_t*>(smem + kStages * kStageBytes + 16 * kRows);
     // full, landed in the second block, empty (each stage); sums full, sums empty (two each); drained; warps' rows (two each)
     const uint32_t full = smem_of(bars), landed = full + 8 * kStages, empty = landed + 8 * kStages, sum_full = empty + 8 * kStages, sum_empty = sum_full + 16,
                    drained = sum_empty + 16, warp_full = drained + 8;
@@ -544,13 +562,10 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
             }
         }
     } else if (work && warp >= 4) {                              // sums
-        const uint32_t team = (warp - 4) / 4, quarter = warp & 3, pair_id = 1 + team * 2 + quarter / 2, r = quarter * 32 + lane;
-        // a warp's 32 rows of a block of 64 columns (4 KB, the block's rows in order), and what goes with them: the next columns' rows (apply),
-        // its half of the 64 rows' transpose (symmetric), or the low numbers
-        constexpr uint32_t kRows = kBlockBytes / 4;
-        unsigned char* const pair_at = smem + kStages * kStageBytes + (pair_id - 1) * 4 * kRows;
-        unsigned char* const mine = pair_at + (quarter & 1) * kRows;
-        unsigned char* const other = mine + 2 * kRows;
+        const uint32_t team = (warp - 4) / 4, quarter = warp & 3, r = quarter * 32 + lane;
+        // a warp's 32 rows of a block of 64 columns (4 KB, the block's rows in order); the low numbers, or the rows of the next 64 columns
+        unsigned char* const mine = smem + kStages * kStageBytes + (warp - 4) * 2 * kRows;
+        unsigned char* const other = mine + kRows;
         const uint32_t ready = warp_full + 16 * (warp - 4);
         uint32_t n = 0, done[2] = {0, 0};                        // phases of the two barriers
         for (uint32_t u = our_pair; u < tiles && ok; u += pairs, ++n) {
@@ -561,35 +576,30 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
             const uint32_t cb0 = 4 * tile.j + 2 * team, edge = MODE <= kPoly ? 2 * min(t.mb, bi + 1) : t.nb;
             const uint32_t wanted = bi < t.mb && cb0 < edge ? min(2u, edge - cb0) : 0;
             const uint64_t row_at = (MODE <= kPoly ? t.a_block + (uint64_t)bi * 2 * t.mb : t.x_block + (uint64_t)bi * t.nb) * kBlockBytes + quarter * kRows;
-            const unsigned char* const in = (MODE == kPoly ? a.a : x_in) + row_at;
             unsigned char* const out = (MODE == kGram ? a.a : MODE == kPoly ? a.b : a.x[side ^ 1]) + row_at;
             const uint64_t low = MODE <= kPoly ? a.a_bytes : a.x_bytes;
-            auto fetch = [&](uint32_t b, unsigned char* to, uint32_t bar) {              // by one lane
-                const unsigned char* from = in + (uint64_t)(cb0 + b) * kBlockBytes;
+            auto fetch = [&](uint32_t b, unsigned char* to, uint32_t bar) {              // A, by one lane
+                const unsigned char* from = a.a + row_at + (uint64_t)(cb0 + b) * kBlockBytes;
                 bar_expect(bar, (SPLIT ? 2 : 1) * kRows);
                 copy_in(smem_of(to), from, kRows, bar);
-                if (SPLIT) copy_in(smem_of(to) + 2 * kRows, from + low, kRows, bar);
+                if (SPLIT) copy_in(smem_of(other), from + low, kRows, bar);
             };
-            if (MODE == kApply && !SPLIT && lane == 0 && wanted) {                        // both of the tile's blocks, once the last ones have left
+            if (!SPLIT && lane == 0 && wanted) {                 // what the last tile left in here has gone
                 asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                fetch(0, mine, ready);
-                if (wanted > 1) fetch(1, other, ready + 8);
+                if (MODE == kPoly) {
+                    fetch(0, mine, ready);
+                    if (wanted > 1) fetch(1, other, ready + 8);
+                }
             }
             for (uint32_t b = 0; b < max(wanted, 1u) && ok; ++b) {
-                const uint32_t cb = cb0 + b, j0 = cb * 64, which = MODE == kApply && !SPLIT ? b : 0;
+                const uint32_t cb = cb0 + b, j0 = cb * 64, which = SPLIT ? 0 : b;
                 unsigned char* const here = which ? other : mine;
-                if (wanted && MODE != kApply) {                  // the pair's memory is free once both have seen their stores leave
-                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                    asm volatile("bar.sync %0, 64;" ::"r"(pair_id) : "memory");
-                    if (MODE == kPoly && lane == 0) fetch(b, mine, ready);
-                }
-                if (wanted && MODE == kApply && SPLIT && lane == 0) {
+                if (SPLIT && wanted && lane == 0) {
                     asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                    fetch(b, mine, ready);
+                    if (MODE == kPoly) fetch(b, mine, ready);
                 }
-                ok = (b || bar_wait(sum_full + 8 * (n & 1), (n / 2) & 1)) && (!wanted || MODE == kGram || bar_wait(ready + 8 * which, done[which] & 1));
-                if (MODE == kApply) ok = __all_sync(0xFFFFFFFFu, ok);
-                else ok = all_of_pair(4 + pair_id, ok);          // one goes on only if both do
+                ok = (b || bar_wait(sum_full + 8 * (n & 1), (n / 2) & 1)) && (!wanted || MODE != kPoly || bar_wait(ready + 8 * which, done[which] & 1));
+                ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok || !wanted) break;
                 ++done[which];
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -607,15 +617,15 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                     }
                     mine_own *= kDown2;
                 }
-                if (MODE == kGram) {
-                    if (diagonal) a.diag_a[t.diagonal + i] = mine_own;
+                if (MODE == kGram && diagonal) a.diag_a[t.diagonal + i] = mine_own;
+                if (MODE != kPoly) {
 #pragma unroll
                     for (int q = 0; q < 32; ++q) v[q] = mul(v[q], twice(kDown));
                 } else {
                     const float* d = a.diag_a + t.diagonal;
-                    const float di = MODE == kPoly ? d[i] : 0.f;
-                    const F2 keep = twice(MODE == kPoly ? fmaf(kQ5, di, kQ3) : kQ1 + a.diag_b[t.diagonal + i]);
-                    if (MODE == kPoly && diagonal) a.diag_b[t.diagonal + i] = fmaf(kQ5, fmaf(di, di, mine_own), kQ3 * di);
+                    const float di = d[i];
+                    const F2 keep = twice(fmaf(kQ5, di, kQ3));
+                    mine_own = (kQ1 + fmaf(kQ5, fmaf(di, di, mine_own), kQ3 * di)) * kUp;
 #pragma unroll
                     for (uint32_t c = 0; c < 8; ++c) {
                         const uint4 h = *reinterpret_cast<const uint4*>(here + piece(lane, c));
@@ -624,15 +634,10 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                             const uint4 l = *reinterpret_cast<const uint4*>(other + piece(lane, c));
                             e[0] = add(e[0], pair_of(l.x)); e[1] = add(e[1], pair_of(l.y)); e[2] = add(e[2], pair_of(l.z)); e[3] = add(e[3], pair_of(l.w));
                         }
-                        if (MODE == kPoly) {
-                            const float4 d0 = *reinterpret_cast<const float4*>(d + j0 + 8 * c), d1 = *reinterpret_cast<const float4*>(d + j0 + 8 * c + 4);
-                            const F2 dj[4] = {pair(d0.x, d0.y), pair(d0.z, d0.w), pair(d1.x, d1.y), pair(d1.z, d1.w)};
+                        const float4 d0 = *reinterpret_cast<const float4*>(d + j0 + 8 * c), d1 = *reinterpret_cast<const float4*>(d + j0 + 8 * c + 4);
+                        const F2 dj[4] = {pair(d0.x, d0.y), pair(d0.z, d0.w), pair(d1.x, d1.y), pair(d1.z, d1.w)};
 #pragma unroll
-                            for (uint32_t q = 0; q < 4; ++q) v[4 * c + q] = fma(v[4 * c + q], twice(kQ5 * kDown), mul(e[q], fma(dj[q], twice(kQ5), keep)));
-                        } else {
-#pragma unroll
-                            for (uint32_t q = 0; q < 4; ++q) v[4 * c + q] = fma(v[4 * c + q], twice(kDown), mul(keep, e[q]));   // times 2^14
-                        }
+                        for (uint32_t q = 0; q < 4; ++q) v[4 * c + q] = fma(v[4 * c + q], twice(kQ5 * kDown), mul(e[q], fma(dj[q], twice(kQ5), keep)));
                     }
                 }
                 uint32_t h[32], low_h[SPLIT ? 32 : 1];
@@ -650,19 +655,11 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                     *reinterpret_cast<uint4*>(here + piece(lane, c)) = make_uint4(h[4 * c], h[4 * c + 1], h[4 * c + 2], h[4 * c + 3]);
                     if (SPLIT) *reinterpret_cast<uint4*>(other + piece(lane, c)) = make_uint4(low_h[4 * c], low_h[4 * c + 1], low_h[4 * c + 2], low_h[4 * c + 3]);
                 }
-                if (diagonal) {
-                    *reinterpret_cast<uint16_t*>(mine + piece(lane, own / 8) + own % 8 * 2) = 0;
-                    if (SPLIT) *reinterpret_cast<uint16_t*>(other + piece(lane, own / 8) + own % 8 * 2) = 0;
+                if (diagonal) {                                  // none in A; that of B with the 3.4445 of X
+                    const __half d = __float2half_rn(MODE == kPoly ? mine_own : 0.f);
+                    *reinterpret_cast<__half*>(here + piece(lane, own / 8) + own % 8 * 2) = d;
+                    if (SPLIT) *reinterpret_cast<__half*>(other + piece(lane, own / 8) + own % 8 * 2) = __float2half_rn(MODE == kPoly ? mine_own - __half2float(d) : 0.f);
                 }
-                const bool both = MODE <= kPoly && cb / 2 < bi;                          // below the diagonal: the transpose too
-                // element (j, i) of the pair's 64 rows i: half a block of 64 rows j
-                unsigned char* const there = (MODE == kGram ? a.a : a.b) + (t.a_block + (uint64_t)(cb / 2) * 2 * t.mb + 2 * bi + quarter / 2) * kBlockBytes + cb % 2 * (kBlockBytes / 2);
-                auto turned = [&](unsigned char* to, const uint32_t* w) {
-#pragma unroll
-                    for (uint32_t q = 0; q < 64; ++q)
-                        *reinterpret_cast<uint16_t*>(to + r % 8 * 2 + piece(q, r % 64 / 8)) = (uint16_t)(q & 1 ? w[q / 2] >> 16 : w[q / 2]);
-                };
-                if (both && !SPLIT) turned(pair_at + 2 * kRows, h);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
@@ -670,19 +667,12 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                     if (SPLIT) copy_out(out + (uint64_t)cb * kBlockBytes + low, smem_of(other), kRows);
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
-                if (both) {
-                    if (SPLIT) {                                 // both of the transpose's numbers, once theirs have left
-                        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                        asm volatile("bar.sync %0, 64;" ::"r"(pair_id) : "memory");
-                        turned(pair_at, h);
-                        turned(pair_at + 2 * kRows, low_h);
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    }
-                    asm volatile("bar.sync %0, 64;" ::"r"(pair_id) : "memory");
-                    if (lane == 0 && !(quarter & 1)) {
-                        copy_out(there, smem_of(pair_at) + (SPLIT ? 0 : 2 * kRows), 2 * kRows);
-                        if (SPLIT) copy_out(there + low, smem_of(pair_at) + 2 * kRows, 2 * kRows);
-                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                if (MODE <= kPoly && cb / 2 < bi) {              // below the diagonal: the transpose too; lanes have neighbours, 64 bytes a store
+                    unsigned char* const there = (MODE == kGram ? a.a : a.b) + (t.a_block + (uint64_t)(cb / 2) * 2 * t.mb + i / 64) * kBlockBytes + cb % 2 * (kBlockBytes / 2) + i % 8 * 2;
+#pragma unroll
+                    for (uint32_t q = 0; q < 64; ++q) {
+                        *reinterpret_cast<uint16_t*>(there + piece(q, i % 64 / 8)) = (uint16_t)(q & 1 ? h[q / 2] >> 16 : h[q / 2]);
+                        if (SPLIT) *reinterpret_cast<uint16_t*>(there + low + piece(q, i % 64 / 8)) = (uint16_t)(q & 1 ? low_h[q / 2] >> 16 : low_h[q / 2]);
                     }
                 }
             }

@@ -117,7 +117,7 @@ def muon(p, m, g, there, lr, lr_scale, decay, mu, nesterov, eps, steps, products
     """Weights, momentum and the update X of one matrix, and how far X may be off (the root of the sum of squares, to first order); `there`: the
     elements that were delivered.
 
-    A step's operands are X and A, B without their diagonals, each entry off by half a step of float16 (u) or, of two float16 numbers, of their
+    A step's operands are X, A without its diagonal and B with 3.4445 on its diagonal, each entry off by half a step of float16 (u) or, of two float16 numbers, of their
     22 bits. X's change grows by the step's slope; A's passes through b + 2 c |A|, then like B's through |X| (largest singular values). The sums
     are float32, 16 products at a time: as many additions in a row as there are sixteens (and a few), each off by 2^-24 of the sum of sizes."""
     m1 = np.where(there, mu * m + g, m)
@@ -139,7 +139,7 @@ def muon(p, m, g, there, lr, lr_scale, decay, mu, nesterov, eps, steps, products
         s = np.linalg.svd(x, compute_uv=False)
         top = s.max()
         q_off = h * norm(q - np.diag(np.diag(q))) + (cols / 16 + 4) * U32 * norm(x) ** 2
-        r_off = h * norm(r - np.diag(np.diag(r))) + q_off * (abs(b) + 2 * c * top ** 2) + c * (rows / 16 + 4) * U32 * norm(q) ** 2
+        r_off = h * norm(r + a * np.eye(rows)) + q_off * (abs(b) + 2 * c * top ** 2) + c * (rows / 16 + 4) * U32 * norm(q) ** 2
         y = a * x + r @ x
         off = _largest_slope(s) * off + r_off * top + (rows / 16 + 4) * U32 * norm(r) * norm(x) + h * norm(y)
         x = y
