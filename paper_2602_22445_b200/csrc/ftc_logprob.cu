@@ -1,12 +1,20 @@
 // Log probabilities of given tokens, entropy and top alternatives under rows of logits, and the logits' gradient.
 //
-// Forward: one pass over a row. A lane keeps the largest logit m that it has seen, s = sum(2^d) and t = sum(d 2^d) with d = c (x - m),
+// Forward: one pass over a row. A lane keeps the largest logit m that it has seen, s = sum(2^d) and t = sum(d 2^d) with d = c x - c m,
 // c = scale * log2(e); where a larger one comes, s and t are moved to it. Lanes, warps and blocks are joined the same way; then
 //   lse = scale m + ln s,   entropy = ln s - ln 2 * t / s,   logprob = scale (x[token] - m) - ln s.
-// x - m before the product: logits far from 0 (a row of the type's lowest value) lose nothing.
-// Top alternatives: a warp keeps the best 32 it has seen in its lanes, sorted; an element enters if it beats the last one that counts.
+// The rounding of c m is the same in all terms and is taken out of ln s and t at the end (up to sizes of 1e8; beyond, see below). Bound by memory and by the 16 powers that an SM
+// makes a cycle (0.7 of what 16-bit logits need); five instructions an element. Logits below -1e30 count as that, so that no infinity meets a
+// zero; a row whose largest c m is beyond 1e8 either way, but not -infinity (all of it masked by the type's lowest value, say) is done again with
+// c (x - m), element by element.
 // Rows are divided over the blocks of a cluster where there are few.
+//
+// Top alternatives: the lanes' largest logits are at hand after the pass. The n-th largest of them is a bound that n elements reach, and about as
+// many do (lanes hold V / 256 elements each): only the lanes that reach it look through their elements again, what reaches the bound is listed
+// and ranked by counting. A list that would be too long (equal logits, rows with few finite ones) is left: then warps keep their best 32 in
+// their lanes, sorted, and take in what beats the last one that counts, as they always do for rows that one warp has to itself.
 #include <cooperative_groups.h>
+#include "ftc_f32x2.cuh"
 #include "ftc_lm.cuh"
 
 namespace ftc {
@@ -58,30 +66,82 @@ template <> struct Vec<__half> {
     }
 };
 
-struct Sums { float m, s, t; };
+struct Sums { float m, cm, s, t, seen; };                        // m: at least kFloor; cm: c * m, rounded up, so that no d is above 0; seen: the largest logit itself
+constexpr float kFloor = -0x1p100f;                              // -1.3e30; its product with c is exact
 
 __device__ __forceinline__ void move_to(Sums& a, float m, float c) {       // m: at least a.m, or NaN
-    const float d = fmaxf((a.m - m) * c, kLeast), f = exp2_fast(d);          // of two infinities: NaN, which fmaxf leaves out
+    const float cm = __fmul_ru(m, c), d = fmaxf(a.cm - cm, kLeast), f = exp2_fast(d);
     a.t = fmaf(a.s, d, a.t) * f;
     a.s *= f;
-    a.m = m;
+    a.m = m; a.cm = cm;
 }
 __device__ __forceinline__ void join(Sums& a, Sums b, float c) {
     const float m = max_nan(a.m, b.m);
     move_to(a, m, c);
     move_to(b, m, c);
     a.s += b.s; a.t += b.t;
-}
-__device__ __forceinline__ void take(Sums& a, float x, float c) {          // x is at most a.m
-    const float d = fmaxf((x - a.m) * c, kLeast), e = exp2_fast(d);
-    a.s += e;
-    a.t = fmaf(d, e, a.t);
+    a.seen = max_nan(a.seen, b.seen);
 }
 __device__ __forceinline__ Sums shuffled(const Sums& a, int o) {
     Sums b;
-    b.m = __shfl_xor_sync(kNone, a.m, o); b.s = __shfl_xor_sync(kNone, a.s, o); b.t = __shfl_xor_sync(kNone, a.t, o);
+    b.m = __shfl_xor_sync(kNone, a.m, o); b.cm = __shfl_xor_sync(kNone, a.cm, o);
+    b.s = __shfl_xor_sync(kNone, a.s, o); b.t = __shfl_xor_sync(kNone, a.t, o); b.seen = __shfl_xor_sync(kNone, a.seen, o);
     return b;
 }
+
+// 16 bytes: the largest of several such, and pairs of numbers of at least kFloor.
+template <typename T> struct Pairs;
+template <> struct Pairs<float> {
+    static constexpr int N = 2;
+    float a, b;
+    __device__ __forceinline__ void start() { a = b = -INFINITY; }
+    __device__ __forceinline__ void most(uint4 r) {
+        a = max_nan(a, max_nan(__uint_as_float(r.x), __uint_as_float(r.y)));
+        b = max_nan(b, max_nan(__uint_as_float(r.z), __uint_as_float(r.w)));
+    }
+    __device__ __forceinline__ float value() const { return max_nan(a, b); }
+    static __device__ __forceinline__ void numbers(F2* v, uint4 r) {
+        v[0] = pair(fmaxf(__uint_as_float(r.x), kFloor), fmaxf(__uint_as_float(r.y), kFloor));
+        v[1] = pair(fmaxf(__uint_as_float(r.z), kFloor), fmaxf(__uint_as_float(r.w), kFloor));
+    }
+};
+__device__ __forceinline__ uint32_t min_u16x2(uint32_t a, uint32_t b) { uint32_t r; asm("min.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r; }
+template <> struct Pairs<__nv_bfloat16> {
+    static constexpr int N = 4;
+    __nv_bfloat162 a;
+    __device__ __forceinline__ void start() { a = __floats2bfloat162_rn(-INFINITY, -INFINITY); }
+    __device__ __forceinline__ void most(uint4 r) {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&r);
+        a = __hmax2_nan(a, __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3])));
+    }
+    __device__ __forceinline__ float value() const { return max_nan(__low2float(a), __high2float(a)); }
+    static __device__ __forceinline__ void numbers(F2* v, uint4 r) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                            // as whole numbers, negative ones grow with their size: 0xF180 is kFloor
+            const uint32_t x = min_u16x2(w[i], 0xF180F180u);
+            v[i] = pair(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u));
+        }
+    }
+};
+template <> struct Pairs<__half> {
+    static constexpr int N = 4;
+    __half2 a;
+    __device__ __forceinline__ void start() { a = __floats2half2_rn(-INFINITY, -INFINITY); }
+    __device__ __forceinline__ void most(uint4 r) {
+        const __half2* h = reinterpret_cast<const __half2*>(&r);
+        a = __hmax2_nan(a, __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3])));
+    }
+    __device__ __forceinline__ float value() const { return max_nan(__low2float(a), __high2float(a)); }
+    static __device__ __forceinline__ void numbers(F2* v, uint4 r) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            v[i] = pair(fmaxf(f.x, kFloor), fmaxf(f.y, kFloor));
+        }
+    }
+};
 
 // The best 32 of a warp, best first, one a lane: a larger word is a better element, equal logits go to the lower index. 0: none.
 __device__ __forceinline__ uint64_t word_of(float x, uint32_t index) {
@@ -111,22 +171,21 @@ __device__ __forceinline__ uint64_t merged(uint64_t a, uint64_t b, uint32_t lane
     return x;
 }
 
-// A row's logits for GROUP threads (one warp, or a block of several); blocks of a cluster share it.
-constexpr uint32_t kLogprobThreads = 256;
+constexpr uint32_t kLogprobThreads = 256, kListed = 256;
 
-// Elements begin .. end-1 of a row: single ones up to the first 16-byte boundary, vectors, single ones behind.
-template <typename T, bool TOP> struct Scan {
-    Sums a;
+// A warp's list, as a row is gone through: what an element has to beat.
+struct Best {
     uint64_t best;
-    float least;                                                 // what an element has to beat
-    __device__ __forceinline__ void consider(const float* v, int count, float most, uint32_t index, uint32_t n_top, uint32_t lane) {
+    float least;
+    __device__ __forceinline__ void start() { best = 0; least = -INFINITY; }
+    // `count` neighbours of each lane, from `index` on, the largest of them `most`. All lanes together.
+    template <typename V> __device__ __forceinline__ void consider(V value, int count, float most, uint32_t index, uint32_t n_top, uint32_t lane) {
         uint32_t lanes = __ballot_sync(kNone, most > least);
         while (lanes) {
             const int src = __ffs(lanes) - 1;
             lanes &= lanes - 1;
-#pragma unroll
             for (int j = 0; j < count; ++j) {
-                const float x = __shfl_sync(kNone, v[j], src);
+                const float x = __shfl_sync(kNone, value(j), src);
                 const uint32_t at = __shfl_sync(kNone, index, src) + j;
                 if (x > least) {
                     insert(best, word_of(x, at), lane);
@@ -138,7 +197,23 @@ template <typename T, bool TOP> struct Scan {
     }
 };
 
-template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds__(kLogprobThreads) token_logprobs_kernel(LogprobArgs a, uint32_t parts) {
+// Elements begin .. end-1 of a row: single ones up to the first 16-byte boundary, vectors, single ones behind.
+template <typename T> struct Stretch {
+    const T* x;
+    uint32_t begin, head, vecs, tail, end;
+    __device__ __forceinline__ Stretch(const T* row, uint32_t b, uint32_t e) : x(row), begin(b), end(e) {
+        constexpr uint32_t N = 16 / sizeof(T);
+        const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(x + begin) & 15) / sizeof(T);
+        head = min(end, begin + (off ? N - off : 0));
+        vecs = (end - head) / N;
+        tail = head + vecs * N;
+    }
+    __device__ __forceinline__ const uint4* vectors() const { return reinterpret_cast<const uint4*>(x + head); }
+    __device__ __forceinline__ uint32_t singles() const { return (head - begin) + (end - tail); }
+    __device__ __forceinline__ uint32_t single(uint32_t i) const { return i < head - begin ? begin + i : tail + (i - (head - begin)); }
+};
+
+template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds__(kLogprobThreads, TOP ? 3 : 4) token_logprobs_kernel(LogprobArgs a, uint32_t parts) {
     namespace cg = cooperative_groups;
     constexpr int N = Vec<T>::N;
     constexpr uint32_t kGroups = kLogprobThreads / GROUP, kWarps = GROUP / 32;
@@ -146,6 +221,10 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
     __shared__ uint64_t lists[kLogprobThreads / 32][32];
     __shared__ Sums joined;
     __shared__ uint64_t joined_list[32];
+    __shared__ __align__(16) float maxima[TOP ? kLogprobThreads : 1];
+    __shared__ uint64_t listed[TOP && GROUP > 32 ? kListed : 1];
+    __shared__ float bound;
+    __shared__ uint32_t count;
     const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, in_group = threadIdx.x % GROUP;
     const uint32_t part = parts > 1 ? cg::this_cluster().block_rank() : 0;
     const float c = a.scale * kLog2e;
@@ -154,73 +233,181 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
     const uint32_t row = (uint32_t)(wanted < a.rows ? wanted : a.rows - 1);
     const T* x = static_cast<const T*>(a.logits) + row * a.stride;
     const uint32_t share = ((a.V + parts - 1) / parts + 63) & ~63u;
-    const uint32_t begin = min(a.V, part * share), end = min(a.V, begin + share);
-    // single elements before the first boundary and behind the last
-    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(x + begin) & 15) / sizeof(T);
-    const uint32_t head = min(end, begin + (off ? N - off : 0)), vecs = (end - head) / N, tail = head + vecs * N;
-
-    Scan<T, TOP> q;
-    q.a = {-INFINITY, 0.f, 0.f};
-    q.best = 0; q.least = -INFINITY;
-    auto single = [&](uint32_t i, bool there) {
-        const float v = there ? to_f32(x[i]) : -INFINITY;
-        const float m = max_nan(q.a.m, v);
-        move_to(q.a, m, c);
-        if (there) take(q.a, v, c);
-        if (TOP) q.consider(&v, 1, v, i, a.top, lane);
-    };
-    if (in_group < 32 && head > begin) single(begin + lane, begin + lane < head);
-    const uint4* xv = reinterpret_cast<const uint4*>(x + head);
+    const uint32_t begin = min(a.V, part * share);
+    const Stretch<T> part_of(x, begin, min(a.V, begin + share));
+    const uint4* xv = part_of.vectors();
+    const uint32_t vecs = part_of.vecs;
+    Sums q = {kFloor, kFloor * c, 0.f, 0.f, -INFINITY};
+    Best best;
+    best.start();
+    F2 s2 = twice(0.f), t2 = twice(0.f);
+    const F2 c2 = twice(c);
+    for (uint32_t i = in_group; i < part_of.singles(); i += GROUP) {
+        const float v = to_f32(x[part_of.single(i)]), m = max_nan(q.m, v);
+        move_to(q, m, c);
+        q.seen = max_nan(q.seen, v);
+        const float d = fmaf(fmaxf(v, kFloor), c, -q.cm), e = exp2_fast(d);
+        q.s += e;
+        q.t = fmaf(d, e, q.t);
+    }
+    if (TOP && GROUP == 32) {                                    // those before the vectors; the ones behind come last, in order
+        const uint32_t n = part_of.head - part_of.begin;
+        const float v = lane < n ? to_f32(x[part_of.begin + lane]) : -INFINITY;
+        best.consider([&](int) { return v; }, 1, v, part_of.begin + lane, a.top, lane);
+    }
     constexpr uint32_t U = 4;
     for (uint32_t i0 = in_group - lane; i0 < vecs; i0 += GROUP * U) {
         uint4 r[U];
+        Pairs<T> most;
+        most.start();
 #pragma unroll
         for (uint32_t u = 0; u < U; ++u) {
             const uint32_t i = i0 + u * GROUP + lane;
             if (i < vecs) r[u] = __ldg(xv + i);
         }
 #pragma unroll
+        for (uint32_t u = 0; u < U; ++u)
+            if (i0 + u * GROUP + lane < vecs) most.most(r[u]);
+        const float m = most.value();
+        q.seen = max_nan(q.seen, m);
+        if (!(m <= q.m)) {
+            q.s += lo(s2) + hi(s2); q.t += lo(t2) + hi(t2);
+            s2 = t2 = twice(0.f);
+            move_to(q, max_nan(q.m, m), c);
+        }
+        const F2 back = twice(-q.cm);
+#pragma unroll
         for (uint32_t u = 0; u < U; ++u) {
-            if (i0 + u * GROUP >= vecs) break;                   // the same for the whole warp
-            const uint32_t i = i0 + u * GROUP + lane;
-            float v[N], most = -INFINITY;
-            if (i < vecs) {
-                Vec<T>::numbers(v, r[u]);
+            if (i0 + u * GROUP + lane >= vecs) continue;
+            F2 v[Pairs<T>::N];
+            Pairs<T>::numbers(v, r[u]);
 #pragma unroll
-                for (int j = 0; j < N; ++j) most = max_nan(most, v[j]);
-                if (!(most <= q.a.m)) move_to(q.a, max_nan(q.a.m, most), c);
-#pragma unroll
-                for (int j = 0; j < N; ++j) take(q.a, v[j], c);
+            for (int j = 0; j < Pairs<T>::N; ++j) {
+                const F2 d = fma(v[j], c2, back), e = pair(exp2_fast(lo(d)), exp2_fast(hi(d)));
+                s2 = add(s2, e);
+                t2 = fma(d, e, t2);
             }
-            if (TOP) q.consider(v, N, most, head + i * N, a.top, lane);
+        }
+        if (TOP && GROUP == 32 && __any_sync(kNone, m > best.least)) {
+#pragma unroll
+            for (uint32_t u = 0; u < U; ++u) {
+                const uint32_t i = i0 + u * GROUP + lane;
+                float v[N], top = -INFINITY;
+                Vec<T>::numbers(v, r[u]);
+                if (i < vecs)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) top = fmaxf(top, v[j]);
+                uint32_t lanes = __ballot_sync(kNone, top > best.least);
+                while (lanes) {
+                    const int src = __ffs(lanes) - 1;
+                    lanes &= lanes - 1;
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        const float y = __shfl_sync(kNone, v[j], src);
+                        if (y > best.least) {
+                            insert(best.best, word_of(y, part_of.head + (i0 + u * GROUP + src) * N + j), lane);
+                            const uint64_t w = __shfl_sync(kNone, best.best, a.top - 1);
+                            best.least = w ? value_of(w) : -INFINITY;
+                        }
+                    }
+                }
+            }
         }
     }
-    if (in_group >= GROUP - 32 && tail < end) single(tail + lane, tail + lane < end);
+    q.s += lo(s2) + hi(s2); q.t += lo(t2) + hi(t2);
+    if (TOP && GROUP == 32) {
+        const uint32_t n = part_of.end - part_of.tail;
+        const float v = lane < n ? to_f32(x[part_of.tail + lane]) : -INFINITY;
+        best.consider([&](int) { return v; }, 1, v, part_of.tail + lane, a.top, lane);
+    }
+    const float lane_most = q.m;
 
     // lanes, warps, blocks
 #pragma unroll
-    for (int o = 16; o; o >>= 1) join(q.a, shuffled(q.a, o), c);
-    if (GROUP > 32 || parts > 1) {
-        if (lane == 0) sums[warp] = q.a;
-        if (TOP) lists[warp][lane] = q.best;
+    for (int o = 16; o; o >>= 1) join(q, shuffled(q, o), c);
+    if (GROUP > 32) {
+        if (lane == 0) sums[warp] = q;
+        if (TOP) {
+            maxima[threadIdx.x] = lane_most;
+            if (threadIdx.x == 0) { bound = INFINITY; count = 0; }
+        }
         __syncthreads();
+        if (TOP) {
+            // the n-th largest of the lanes' largest logits
+            uint32_t ahead = 0;
+#pragma unroll 8
+            for (uint32_t i = 0; i < kLogprobThreads / 4; ++i) {
+                const float4 o = reinterpret_cast<const float4*>(maxima)[i];
+                const float other[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) ahead += other[j] > lane_most || (other[j] == lane_most && 4 * i + j < threadIdx.x);
+            }
+            if (ahead == a.top - 1) bound = lane_most;
+            __syncthreads();
+            const float least = bound;                           // kFloor: fewer lanes than that have seen a logit above it
+            bool whole = least > kFloor;
+            if (whole) {
+                auto list = [&](float v, uint32_t at) {
+                    if (v >= least) {
+                        const uint32_t to = atomicAdd(&count, 1);
+                        if (to < kListed) listed[to] = word_of(v, at);
+                    }
+                };
+                if (threadIdx.x < part_of.singles()) { const uint32_t at = part_of.single(threadIdx.x); list(to_f32(x[at]), at); }
+                uint32_t lanes = __ballot_sync(kNone, lane_most >= least);
+                while (lanes) {
+                    const uint32_t src = __ffs(lanes) - 1;
+                    lanes &= lanes - 1;
+                    for (uint32_t i = warp * 32 + src + lane * GROUP; i < vecs; i += 32 * GROUP) {
+                        float v[N];
+                        Vec<T>::numbers(v, __ldg(xv + i));
+#pragma unroll
+                        for (int j = 0; j < N; ++j) list(v[j], part_of.head + i * N + j);
+                    }
+                }
+            }
+            __syncthreads();
+            const uint32_t n = count;
+            whole = whole && n <= kListed;
+            if (whole) {                                         // ranked: those among the first 32 have their place
+                if (threadIdx.x < 32) lists[0][threadIdx.x] = 0;
+                __syncthreads();
+                if (threadIdx.x < n) {
+                    const uint64_t w = listed[threadIdx.x];
+                    uint32_t before = 0;
+                    for (uint32_t i = 0; i < n; ++i) before += listed[i] > w;
+                    if (before < 32) lists[0][before] = w;
+                }
+                __syncthreads();
+                best.best = lists[0][lane];
+            } else {                                             // one after the other
+                for (uint32_t i0 = begin + warp * 32; i0 < part_of.end; i0 += GROUP) {
+                    const float v = i0 + lane < part_of.end ? to_f32(x[i0 + lane]) : -INFINITY;
+                    best.consider([&](int) { return v; }, 1, v, i0 + lane, a.top, lane);
+                }
+                __syncthreads();
+                lists[warp][lane] = best.best;
+                __syncthreads();
+                if (warp == 0)
+                    for (uint32_t w = 1; w < kWarps; ++w) best.best = merged(best.best, lists[w][lane], lane);
+            }
+        }
         if (warp == 0) {
             Sums all = sums[0];
             for (uint32_t w = 1; w < kWarps; ++w) join(all, sums[w], c);
-            q.a = all;
-            if (TOP) for (uint32_t w = 1; w < kWarps; ++w) q.best = merged(q.best, lists[w][lane], lane);
+            q = all;
         }
         if (parts > 1) {
             cg::cluster_group cluster = cg::this_cluster();
             if (warp == 0) {
-                if (lane == 0) joined = q.a;
-                if (TOP) joined_list[lane] = q.best;
+                if (lane == 0) joined = q;
+                if (TOP) joined_list[lane] = best.best;
             }
             cluster.sync();
             if (part == 0 && warp == 0) {
                 for (uint32_t b = 1; b < parts; ++b) {
-                    join(q.a, *cluster.map_shared_rank(&joined, b), c);
-                    if (TOP) q.best = merged(q.best, cluster.map_shared_rank(joined_list, b)[lane], lane);
+                    join(q, *cluster.map_shared_rank(&joined, b), c);
+                    if (TOP) best.best = merged(best.best, cluster.map_shared_rank(joined_list, b)[lane], lane);
                 }
             }
             cluster.sync();                                      // a block's shared memory stays until it has been read
@@ -229,33 +416,46 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
     }
     if (wanted >= a.rows) return;
 
-    const bool bad = isnan(q.a.m) || q.a.m == INFINITY, empty = q.a.m == -INFINITY;
-    const float ln_s = logf(q.a.s), nan = __int_as_float(0x7FFFFFFF);
-    const float lse = bad ? nan : empty ? -INFINITY : fmaf(a.scale, q.a.m, ln_s);
+    // one warp has the row now
+    float m, ln_s = logf(q.s) - kLn2 * fmaf(q.m, c, -q.cm), mean_d = q.t / q.s - fmaf(q.m, c, -q.cm);      // mean of d, about c m itself
+    m = q.seen;
+    if (fabsf(m * c) > 1e8f && fabsf(m) < INFINITY) {            // nothing but the type's lowest value, or the like: d = c (x - m), which holds anywhere
+        float s = 0.f, t = 0.f;
+#pragma unroll 8
+        for (uint32_t i = lane; i < a.V; i += 32) {
+            const float d = fmaxf((to_f32(x[i]) - m) * c, kLeast), e = exp2_fast(d);
+            s += e;
+            t = fmaf(d, e, t);
+        }
+        s = warp_sum(s); t = warp_sum(t);
+        ln_s = logf(s); mean_d = t / s;
+    }
+    const bool bad = isnan(m) || m == INFINITY, empty = m == -INFINITY;
+    const float nan = __int_as_float(0x7FFFFFFF), lse = bad ? nan : empty ? -INFINITY : fmaf(a.scale, m, ln_s);
     if (lane == 0) {
         if (a.lse) a.lse[row] = lse;
-        if (a.entropy) a.entropy[row] = bad ? nan : empty ? 0.f : fmaxf(0.f, ln_s - kLn2 * (q.a.t / q.a.s));
+        if (a.entropy) a.entropy[row] = bad ? nan : empty ? 0.f : fmaxf(0.f, ln_s - kLn2 * mean_d);
         if (a.logprob) {
             const int32_t tok = token_at(a.tokens, a.token_bits, row, a.V);
-            a.logprob[row] = tok < 0 ? 0.f : bad ? nan : empty ? -INFINITY : fmaf(a.scale, to_f32(x[tok]) - q.a.m, -ln_s);
+            a.logprob[row] = tok < 0 ? 0.f : bad ? nan : empty ? -INFINITY : fmaf(a.scale, to_f32(x[tok]) - m, -ln_s);
         }
     }
     if (!TOP) return;
     // fewer logits above -infinity than were asked for: the lowest tokens of the others
-    uint32_t have = __popc(__ballot_sync(kNone, q.best != 0));
+    uint32_t have = __popc(__ballot_sync(kNone, best.best != 0));
     for (uint32_t i0 = 0; i0 < a.V && have < a.top; i0 += 32) {
         uint32_t more = __ballot_sync(kNone, i0 + lane < a.V && to_f32(x[min(i0 + lane, a.V - 1)]) == -INFINITY);
         while (more && have < a.top) {
             const uint32_t j = __ffs(more) - 1;
             more &= more - 1;
-            if (lane == have) q.best = word_of(-INFINITY, i0 + j);
+            if (lane == have) best.best = word_of(-INFINITY, i0 + j);
             ++have;
         }
     }
     if (lane < a.top) {
-        const float v = value_of(q.best);
-        a.top_logprob[(uint64_t)row * a.top + lane] = bad ? nan : empty ? -INFINITY : fmaf(a.scale, v - q.a.m, -ln_s);
-        a.top_token[(uint64_t)row * a.top + lane] = q.best ? (int32_t)index_of(q.best) : 0;
+        const float v = value_of(best.best);
+        a.top_logprob[(uint64_t)row * a.top + lane] = bad ? nan : empty ? -INFINITY : fmaf(a.scale, v - m, -ln_s);
+        a.top_token[(uint64_t)row * a.top + lane] = best.best ? (int32_t)index_of(best.best) : 0;
     }
 }
 
