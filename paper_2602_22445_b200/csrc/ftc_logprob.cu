@@ -320,7 +320,7 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
         const float v = lane < n ? to_f32(x[part_of.tail + lane]) : -INFINITY;
         best.consider([&](int) { return v; }, 1, v, part_of.tail + lane, a.top, lane);
     }
-    const float lane_most = q.m;
+    const float lane_most = q.seen;
 
     // lanes, warps, blocks
 #pragma unroll
@@ -344,17 +344,17 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
             }
             if (ahead == a.top - 1) bound = lane_most;
             __syncthreads();
-            const float least = bound;                           // kFloor: fewer lanes than that have seen a logit above it
-            bool whole = least > kFloor;
+            const float least = bound;                           // -infinity: fewer lanes than that have seen another
+            bool whole = !isnan(least);
             if (whole) {
                 auto list = [&](float v, uint32_t at) {
-                    if (v >= least) {
+                    if (v >= least && v > -INFINITY) {
                         const uint32_t to = atomicAdd(&count, 1);
                         if (to < kListed) listed[to] = word_of(v, at);
                     }
                 };
                 if (threadIdx.x < part_of.singles()) { const uint32_t at = part_of.single(threadIdx.x); list(to_f32(x[at]), at); }
-                uint32_t lanes = __ballot_sync(kNone, lane_most >= least);
+                uint32_t lanes = __ballot_sync(kNone, lane_most >= least && lane_most > -INFINITY);
                 while (lanes) {
                     const uint32_t src = __ffs(lanes) - 1;
                     lanes &= lanes - 1;
@@ -381,9 +381,20 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
                 __syncthreads();
                 best.best = lists[0][lane];
             } else {                                             // one after the other
-                for (uint32_t i0 = begin + warp * 32; i0 < part_of.end; i0 += GROUP) {
-                    const float v = i0 + lane < part_of.end ? to_f32(x[i0 + lane]) : -INFINITY;
-                    best.consider([&](int) { return v; }, 1, v, i0 + lane, a.top, lane);
+                constexpr uint32_t kAhead = 8;
+                for (uint32_t i0 = begin + warp * 32; i0 < part_of.end; i0 += GROUP * kAhead) {
+                    float v[kAhead], most = -INFINITY;
+#pragma unroll
+                    for (uint32_t k = 0; k < kAhead; ++k) {
+                        const uint32_t i = i0 + k * GROUP + lane;
+                        v[k] = i < part_of.end ? to_f32(x[i]) : -INFINITY;
+                    }
+#pragma unroll
+                    for (uint32_t k = 0; k < kAhead; ++k) most = fmaxf(most, v[k]);
+                    if (!__any_sync(kNone, most > best.least)) continue;
+#pragma unroll
+                    for (uint32_t k = 0; k < kAhead; ++k)
+                        best.consider([&](int) { return v[k]; }, 1, v[k], i0 + k * GROUP + lane, a.top, lane);
                 }
                 __syncthreads();
                 lists[warp][lane] = best.best;
@@ -488,84 +499,127 @@ cudaError_t launch_token_logprobs(const LogprobArgs& a, int sms, cudaStream_t st
 // ---- gradient ----
 //
 // With A = -scale (dlogprob + dentropy (entropy - lse)) and B = -scale * dentropy * scale: p (A + B x), and scale * dlogprob more at the token.
+// Bound by memory; five instructions an element. A row is written in vectors from its own 16-byte boundary on. Where the logits lie
+// otherwise against that boundary (a slice of a padded matrix), a vector is put together from the two that cover it.
 
-struct RowFactors { float a, b, up, l2; int32_t token; bool zero; };
+struct RowFactors { float a, b, up, lse; int32_t token; bool zero; };
 
 __device__ __forceinline__ RowFactors factors_of(const LogprobArgs& g, uint32_t row) {
     RowFactors f;
     f.token = g.dlogprob ? token_at(g.tokens, g.token_bits, row, g.V) : -1;
-    const float lse = g.lse_in[row], up = f.token >= 0 ? g.dlogprob[row] : 0.f, de = g.dentropy ? g.dentropy[row] : 0.f;
-    f.zero = lse == -INFINITY;
-    f.l2 = lse;
-    f.a = -(up + (g.dentropy ? de * (g.entropy_in[row] - lse) : 0.f)) * g.scale;
+    const float given = g.dlogprob ? g.dlogprob[row] : 0.f, up = f.token >= 0 ? given : 0.f, de = g.dentropy ? g.dentropy[row] : 0.f;
+    f.lse = g.lse_in[row];
+    f.zero = f.lse == -INFINITY;
+    f.a = -(up + (g.dentropy ? de * (g.entropy_in[row] - f.lse) : 0.f)) * g.scale;
     f.b = -de * g.scale * g.scale;
     f.up = up * g.scale;
     return f;
 }
 __device__ __forceinline__ float gradient(const RowFactors& f, float x, float scale) {
-    const float p = exp2_fast(fmaf(x, scale, -f.l2) * kLog2e);
-    return p == 0.f ? 0.f : p * fmaf(f.b, x, f.a);
+    const float v = x < kFloor ? kFloor : x;                     // NaN stays
+    return f.zero ? 0.f : exp2_fast(fmaf(v, scale, -f.lse) * kLog2e) * fmaf(f.b, v, f.a);
+}
+// As Pairs' numbers, but NaN stays what it is: the row's lse is NaN then, so no care is needed.
+template <typename T> __device__ __forceinline__ uint4 gradients(const RowFactors& f, uint4 r, float scale) {
+    constexpr int N = Pairs<T>::N;
+    F2 v[N];
+    float y[2 * N];
+    Pairs<T>::numbers(v, r);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const F2 d = mul(fma(v[j], twice(scale), twice(-f.lse)), twice(kLog2e)), e = mul(pair(exp2_fast(lo(d)), exp2_fast(hi(d))), fma(twice(f.b), v[j], twice(f.a)));
+        y[2 * j] = f.zero ? 0.f : lo(e);
+        y[2 * j + 1] = f.zero ? 0.f : hi(e);
+    }
+    return Vec<T>::pack(y);
+}
+// 16 bytes from byte `shift` (1 .. 15) of two vectors on.
+__device__ __forceinline__ uint4 joined_at(uint4 a, uint4 b, uint32_t shift) {
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (shift & 8) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    }
+    if (shift & 4) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    }
+    const uint32_t bits = (shift & 3) * 8;
+    return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
 }
 
-// Elements a vector at a time (W bytes) where every row of both begins on such a boundary.
-template <typename T, int W> __global__ void __launch_bounds__(256) logprobs_backward_kernel(LogprobArgs g, uint32_t pieces, uint32_t each) {
-    constexpr int N = W / sizeof(T);
-    const uint32_t row = (uint32_t)(blockIdx.x / pieces), piece = blockIdx.x - row * pieces;
-    const RowFactors f = factors_of(g, row);
-    const T* x = static_cast<const T*>(g.logits) + row * g.stride;
-    T* d = static_cast<T*>(g.dlogits) + row * g.dstride;
-    const uint32_t vecs = (g.V + N - 1) / N, begin = piece * each, end = min(vecs, begin + each);
-    constexpr int U = 4;
-    for (uint32_t i0 = begin + threadIdx.x; i0 < end; i0 += 256 * U) {
-        float v[U][N];
+// A unit: kPieceVectors vectors of a row for a block, a row for a warp (GROUP = 32).
+constexpr uint32_t kPieceVectors = 2048;
+template <typename T, uint32_t GROUP> __global__ void __launch_bounds__(256, 4) logprobs_backward_kernel(LogprobArgs g, uint32_t pieces, uint64_t units) {
+    constexpr uint32_t N = 16 / sizeof(T), U = 4, kGroups = 256 / GROUP;
+    const uint32_t in_group = threadIdx.x % GROUP;
+    for (uint64_t unit = (uint64_t)blockIdx.x * kGroups + threadIdx.x / GROUP; unit < units; unit += (uint64_t)gridDim.x * kGroups) {
+        const uint32_t row = pieces == 1 ? (uint32_t)unit : (uint32_t)(unit / pieces), piece = pieces == 1 ? 0 : (uint32_t)(unit - (uint64_t)row * pieces);
+        const T* const x = static_cast<const T*>(g.logits) + row * g.stride;
+        T* const d = static_cast<T*>(g.dlogits) + row * g.dstride;
+        const Stretch<T> out(d, 0, g.V);                         // where d has its boundaries
+        const uint32_t end = GROUP == 32 ? out.vecs : min(out.vecs, (piece + 1) * kPieceVectors);
+        const uint32_t shift = (uint32_t)(reinterpret_cast<uintptr_t>(x + out.head) & 15);
+        const uint4* const xv = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(x + out.head) - shift);
+        uint4* const dv = reinterpret_cast<uint4*>(d + out.head);
+        const RowFactors f = factors_of(g, row);
+        const uint32_t at = f.token >= 0 && !f.zero ? (uint32_t)f.token : kNone;
+        for (uint32_t i0 = (GROUP == 32 ? 0 : piece * kPieceVectors) + in_group; i0 < end; i0 += GROUP * U) {
+            uint4 r[U];
+            if (shift) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t i = i0 + u * 256;
-            if (i >= end) continue;
-            if (W == 16 && (i + 1) * N <= g.V) {
-                const uint4 r = *reinterpret_cast<const uint4*>(x + (uint64_t)i * N);
-                if constexpr (W == 16) Vec<T>::numbers(v[u], r);
+                for (uint32_t u = 0; u < U; ++u) {
+                    const uint32_t i = i0 + u * GROUP;
+                    if (i < end) r[u] = joined_at(__ldg(xv + i), __ldg(xv + i + 1), shift);      // the second one holds some of the vector's last element at least
+                }
+            } else if (g.logits == g.dlogits) {
+#pragma unroll
+                for (uint32_t u = 0; u < U; ++u)
+                    if (i0 + u * GROUP < end) r[u] = xv[i0 + u * GROUP];
             } else {
 #pragma unroll
-                for (int j = 0; j < N; ++j) v[u][j] = i * N + j < g.V ? to_f32(x[i * N + j]) : 0.f;
+                for (uint32_t u = 0; u < U; ++u)
+                    if (i0 + u * GROUP < end) r[u] = __ldg(xv + i0 + u * GROUP);
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < U; ++u) {
+                const uint32_t i = i0 + u * GROUP;
+                if (i >= end) continue;
+                dv[i] = gradients<T>(f, r[u], g.scale);
+                if (at - (out.head + i * N) < N) {               // the token is among them
+                    float v[N];
+                    Vec<T>::numbers(v, r[u]);
+#pragma unroll
+                    for (uint32_t j = 0; j < N; ++j)
+                        if (out.head + i * N + j == at) d[at] = from_f32<T>(gradient(f, v[j], g.scale) + f.up);
+                }
             }
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t i = i0 + u * 256;
-            if (i >= end) continue;
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                float y = f.zero ? 0.f : gradient(f, v[u][j], g.scale);
-                if ((int32_t)(i * N + j) == f.token && !f.zero) y += f.up;
-                v[u][j] = y;
+        if (piece == 0)
+            for (uint32_t i = in_group; i < out.singles(); i += GROUP) {
+                const uint32_t e = out.single(i);
+                const float y = gradient(f, to_f32(x[e]), g.scale);
+                d[e] = from_f32<T>(e == at ? y + f.up : y);
             }
-            if (W == 16 && (i + 1) * N <= g.V) {
-                if constexpr (W == 16) *reinterpret_cast<uint4*>(d + (uint64_t)i * N) = Vec<T>::pack(v[u]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (i * N + j < g.V) d[i * N + j] = from_f32<T>(v[u][j]);
-            }
-        }
     }
 }
 
-template <typename T> static cudaError_t backward(const LogprobArgs& g, cudaStream_t st) {
-    const uintptr_t all = reinterpret_cast<uintptr_t>(g.logits) | reinterpret_cast<uintptr_t>(g.dlogits) | g.stride * sizeof(T) | g.dstride * sizeof(T);
-    const bool wide = (all & 15) == 0;
-    const uint32_t n = wide ? 16 / sizeof(T) : 1, vecs = (uint32_t)(((uint64_t)g.V + n - 1) / n), each = 256 * 8, pieces = (vecs + each - 1) / each;
-    if ((uint64_t)g.rows * pieces > 0x7FFFFFFFull) return cudaErrorInvalidValue;
-    const uint32_t grid = g.rows * pieces;
-    if (wide) logprobs_backward_kernel<T, 16><<<grid, 256, 0, st>>>(g, pieces, each);
-    else logprobs_backward_kernel<T, sizeof(T)><<<grid, 256, 0, st>>>(g, pieces, each);
+template <typename T> static cudaError_t backward(const LogprobArgs& g, int sms, cudaStream_t st) {
+    // A warp for rows of up to 256 vectors.
+    const uint32_t vecs = (uint32_t)(((uint64_t)g.V * sizeof(T) + 15) / 16);
+    const bool warps = vecs <= 256;
+    const uint32_t pieces = warps ? 1 : (vecs + kPieceVectors - 1) / kPieceVectors;
+    const uint64_t units = (uint64_t)g.rows * pieces, blocks = warps ? (units + 7) / 8 : units, cap = (uint64_t)sms * 256;
+    const uint32_t grid = (uint32_t)(blocks < cap ? blocks : cap);
+    if (warps) logprobs_backward_kernel<T, 32><<<grid, 256, 0, st>>>(g, pieces, units);
+    else logprobs_backward_kernel<T, 256><<<grid, 256, 0, st>>>(g, pieces, units);
     return cudaGetLastError();
 }
 
 cudaError_t launch_token_logprobs_backward(const LogprobArgs& g, int sms, cudaStream_t st) {
-    if (g.dtype == FTC_F32) return backward<float>(g, st);
-    if (g.dtype == FTC_BF16) return backward<__nv_bfloat16>(g, st);
-    return backward<__half>(g, st);
+    if (g.dtype == FTC_F32) return backward<float>(g, sms, st);
+    if (g.dtype == FTC_BF16) return backward<__nv_bfloat16>(g, sms, st);
+    return backward<__half>(g, sms, st);
 }
 
 }  // namespace ftc
