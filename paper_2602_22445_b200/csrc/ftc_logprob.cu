@@ -9,10 +9,10 @@
 // c (x - m), element by element.
 // Rows are divided over the blocks of a cluster where there are few.
 //
-// Top alternatives: the lanes' largest logits are at hand after the pass. The n-th largest of them is a bound that n elements reach, and about as
-// many do (lanes hold V / 256 elements each): only the lanes that reach it look through their elements again, what reaches the bound is listed
+// Top alternatives: the lanes' largest logits are at hand after the pass. The n-th largest of them (its upper 16 bits, found bit by bit by counting
+// lanes) is a bound that n elements reach, and about as many do (lanes hold V / 256 elements each): only the lanes that reach it look through their elements again, what reaches the bound is listed
 // and ranked by counting. A list that would be too long (equal logits, rows with few finite ones) is left: then warps keep their best 32 in
-// their lanes, sorted, and take in what beats the last one that counts, as they always do for rows that one warp has to itself.
+// their lanes, sorted, and take in what beats the last one that counts.
 #include <cooperative_groups.h>
 #include "ftc_f32x2.cuh"
 #include "ftc_lm.cuh"
@@ -82,11 +82,21 @@ __device__ __forceinline__ void join(Sums& a, Sums b, float c) {
     a.s += b.s; a.t += b.t;
     a.seen = max_nan(a.seen, b.seen);
 }
-__device__ __forceinline__ Sums shuffled(const Sums& a, int o) {
-    Sums b;
-    b.m = __shfl_xor_sync(kNone, a.m, o); b.cm = __shfl_xor_sync(kNone, a.cm, o);
-    b.s = __shfl_xor_sync(kNone, a.s, o); b.t = __shfl_xor_sync(kNone, a.t, o); b.seen = __shfl_xor_sync(kNone, a.seen, o);
-    return b;
+// The sums of the first LANES lanes together.
+template <int LANES> __device__ __forceinline__ Sums joined_lanes(Sums a, float c) {
+    float m = a.m;
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) {
+        m = max_nan(m, __shfl_xor_sync(kNone, m, o));
+        a.seen = max_nan(a.seen, __shfl_xor_sync(kNone, a.seen, o));
+    }
+    move_to(a, m, c);
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) {
+        a.s += __shfl_xor_sync(kNone, a.s, o);
+        a.t += __shfl_xor_sync(kNone, a.t, o);
+    }
+    return a;
 }
 
 // 16 bytes: the largest of several such, and pairs of numbers of at least kFloor.
@@ -171,7 +181,7 @@ __device__ __forceinline__ uint64_t merged(uint64_t a, uint64_t b, uint32_t lane
     return x;
 }
 
-constexpr uint32_t kLogprobThreads = 256, kListed = 256;
+constexpr uint32_t kLogprobThreads = 256, kListed = 256, kWarpListed = 64;
 
 // A warp's list, as a row is gone through: what an element has to beat.
 struct Best {
@@ -221,10 +231,9 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
     __shared__ uint64_t lists[kLogprobThreads / 32][32];
     __shared__ Sums joined;
     __shared__ uint64_t joined_list[32];
-    __shared__ __align__(16) float maxima[TOP ? kLogprobThreads : 1];
-    __shared__ uint64_t listed[TOP && GROUP > 32 ? kListed : 1];
-    __shared__ float bound;
-    __shared__ uint32_t count;
+    constexpr uint32_t kList = GROUP > 32 ? kListed : kWarpListed;
+    __shared__ uint64_t listed_of[TOP ? kGroups : 1][TOP ? kList : 1];
+    __shared__ uint32_t count_of[kGroups];
     const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, in_group = threadIdx.x % GROUP;
     const uint32_t part = parts > 1 ? cg::this_cluster().block_rank() : 0;
     const float c = a.scale * kLog2e;
@@ -240,6 +249,13 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
     Sums q = {kFloor, kFloor * c, 0.f, 0.f, -INFINITY};
     Best best;
     best.start();
+    // the token and its logit, long before they are needed
+    int32_t token = -1;
+    float token_logit = 0.f;
+    if (in_group == 0 && part == 0 && a.logprob) {
+        token = token_at(a.tokens, a.token_bits, row, a.V);
+        if (token >= 0) token_logit = to_f32(x[token]);
+    }
     F2 s2 = twice(0.f), t2 = twice(0.f);
     const F2 c2 = twice(c);
     for (uint32_t i = in_group; i < part_of.singles(); i += GROUP) {
@@ -249,11 +265,6 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
         const float d = fmaf(fmaxf(v, kFloor), c, -q.cm), e = exp2_fast(d);
         q.s += e;
         q.t = fmaf(d, e, q.t);
-    }
-    if (TOP && GROUP == 32) {                                    // those before the vectors; the ones behind come last, in order
-        const uint32_t n = part_of.head - part_of.begin;
-        const float v = lane < n ? to_f32(x[part_of.begin + lane]) : -INFINITY;
-        best.consider([&](int) { return v; }, 1, v, part_of.begin + lane, a.top, lane);
     }
     constexpr uint32_t U = 4;
     for (uint32_t i0 = in_group - lane; i0 < vecs; i0 += GROUP * U) {
@@ -288,126 +299,87 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
                 t2 = fma(d, e, t2);
             }
         }
-        if (TOP && GROUP == 32 && __any_sync(kNone, m > best.least)) {
-#pragma unroll
-            for (uint32_t u = 0; u < U; ++u) {
-                const uint32_t i = i0 + u * GROUP + lane;
-                float v[N], top = -INFINITY;
-                Vec<T>::numbers(v, r[u]);
-                if (i < vecs)
-#pragma unroll
-                    for (int j = 0; j < N; ++j) top = fmaxf(top, v[j]);
-                uint32_t lanes = __ballot_sync(kNone, top > best.least);
-                while (lanes) {
-                    const int src = __ffs(lanes) - 1;
-                    lanes &= lanes - 1;
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const float y = __shfl_sync(kNone, v[j], src);
-                        if (y > best.least) {
-                            insert(best.best, word_of(y, part_of.head + (i0 + u * GROUP + src) * N + j), lane);
-                            const uint64_t w = __shfl_sync(kNone, best.best, a.top - 1);
-                            best.least = w ? value_of(w) : -INFINITY;
-                        }
-                    }
-                }
-            }
-        }
     }
     q.s += lo(s2) + hi(s2); q.t += lo(t2) + hi(t2);
-    if (TOP && GROUP == 32) {
-        const uint32_t n = part_of.end - part_of.tail;
-        const float v = lane < n ? to_f32(x[part_of.tail + lane]) : -INFINITY;
-        best.consider([&](int) { return v; }, 1, v, part_of.tail + lane, a.top, lane);
-    }
     const float lane_most = q.seen;
 
-    // lanes, warps, blocks
+    q = joined_lanes<32>(q, c);
+    if (GROUP > 32 && lane == 0) sums[warp] = q;
+    if (TOP) {
+        uint64_t* const listed = listed_of[threadIdx.x / GROUP];
+        uint32_t* const counted = &count_of[threadIdx.x / GROUP];
+        auto sync = [] { if (GROUP == 32) __syncwarp(); else __syncthreads(); };
+        const uint32_t mine = (uint32_t)(word_of(lane_most, 0) >> 48);           // in order, as whole numbers
+        uint32_t bound = 0;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) join(q, shuffled(q, o), c);
-    if (GROUP > 32) {
-        if (lane == 0) sums[warp] = q;
-        if (TOP) {
-            maxima[threadIdx.x] = lane_most;
-            if (threadIdx.x == 0) { bound = INFINITY; count = 0; }
+        for (int bit = 15; bit >= 0; --bit) {
+            const uint32_t more = bound | 1u << bit;
+            const int reach = GROUP == 32 ? __popc(__ballot_sync(kNone, mine >= more)) : __syncthreads_count(mine >= more);
+            if ((uint32_t)reach >= a.top) bound = more;
         }
-        __syncthreads();
-        if (TOP) {
-            // the n-th largest of the lanes' largest logits
-            uint32_t ahead = 0;
-#pragma unroll 8
-            for (uint32_t i = 0; i < kLogprobThreads / 4; ++i) {
-                const float4 o = reinterpret_cast<const float4*>(maxima)[i];
-                const float other[4] = {o.x, o.y, o.z, o.w};
-#pragma unroll
-                for (uint32_t j = 0; j < 4; ++j) ahead += other[j] > lane_most || (other[j] == lane_most && 4 * i + j < threadIdx.x);
+        if (in_group == 0) *counted = 0;
+        sync();
+        const bool any = bound <= 0x7Fu;                         // fewer lanes than that have seen a logit above -infinity
+        const float least = any ? -INFINITY : value_of((uint64_t)bound << 48 | 0xFFFFFFFFu);
+        auto list = [&](float v, uint32_t at) {
+            if (v >= least && v > -INFINITY) {
+                const uint32_t to = atomicAdd(counted, 1);
+                if (to < kList) listed[to] = word_of(v, at);
             }
-            if (ahead == a.top - 1) bound = lane_most;
-            __syncthreads();
-            const float least = bound;                           // -infinity: fewer lanes than that have seen another
-            bool whole = !isnan(least);
-            if (whole) {
-                auto list = [&](float v, uint32_t at) {
-                    if (v >= least && v > -INFINITY) {
-                        const uint32_t to = atomicAdd(&count, 1);
-                        if (to < kListed) listed[to] = word_of(v, at);
-                    }
-                };
-                if (threadIdx.x < part_of.singles()) { const uint32_t at = part_of.single(threadIdx.x); list(to_f32(x[at]), at); }
-                uint32_t lanes = __ballot_sync(kNone, lane_most >= least && lane_most > -INFINITY);
-                while (lanes) {
-                    const uint32_t src = __ffs(lanes) - 1;
-                    lanes &= lanes - 1;
-                    for (uint32_t i = warp * 32 + src + lane * GROUP; i < vecs; i += 32 * GROUP) {
-                        float v[N];
-                        Vec<T>::numbers(v, __ldg(xv + i));
+        };
+        if (in_group < part_of.singles()) { const uint32_t at = part_of.single(in_group); list(to_f32(x[at]), at); }
+        uint32_t lanes = __ballot_sync(kNone, lane_most >= least && lane_most > -INFINITY);
+        while (lanes) {
+            const uint32_t src = __ffs(lanes) - 1;
+            lanes &= lanes - 1;
+            for (uint32_t i = (in_group - lane) + src + lane * GROUP; i < vecs; i += 32 * GROUP) {
+                float v[N];
+                Vec<T>::numbers(v, __ldg(xv + i));
 #pragma unroll
-                        for (int j = 0; j < N; ++j) list(v[j], part_of.head + i * N + j);
-                    }
-                }
+                for (int j = 0; j < N; ++j) list(v[j], part_of.head + i * N + j);
             }
-            __syncthreads();
-            const uint32_t n = count;
-            whole = whole && n <= kListed;
-            if (whole) {                                         // ranked: those among the first 32 have their place
-                if (threadIdx.x < 32) lists[0][threadIdx.x] = 0;
-                __syncthreads();
-                if (threadIdx.x < n) {
-                    const uint64_t w = listed[threadIdx.x];
-                    uint32_t before = 0;
-                    for (uint32_t i = 0; i < n; ++i) before += listed[i] > w;
-                    if (before < 32) lists[0][before] = w;
+        }
+        sync();
+        const uint32_t n = *counted;
+        uint64_t* const ranked = lists[warp - in_group / 32];
+        if (n <= kList) {                                        // ranked: those among the first 32 have their place
+            if (in_group < 32) ranked[in_group] = 0;
+            sync();
+            for (uint32_t k = in_group; k < n; k += GROUP) {
+                const uint64_t w = listed[k];
+                uint32_t before = 0;
+                for (uint32_t i = 0; i < n; ++i) before += listed[i] > w;
+                if (before < 32) ranked[before] = w;
+            }
+            sync();
+            best.best = ranked[lane];
+        } else {                                                 // one after the other
+            constexpr uint32_t kAhead = 8;
+            for (uint32_t i0 = begin + in_group - lane; i0 < part_of.end; i0 += GROUP * kAhead) {
+                float v[kAhead], most = -INFINITY;
+#pragma unroll
+                for (uint32_t k = 0; k < kAhead; ++k) {
+                    const uint32_t i = i0 + k * GROUP + lane;
+                    v[k] = i < part_of.end ? to_f32(x[i]) : -INFINITY;
                 }
-                __syncthreads();
-                best.best = lists[0][lane];
-            } else {                                             // one after the other
-                constexpr uint32_t kAhead = 8;
-                for (uint32_t i0 = begin + warp * 32; i0 < part_of.end; i0 += GROUP * kAhead) {
-                    float v[kAhead], most = -INFINITY;
 #pragma unroll
-                    for (uint32_t k = 0; k < kAhead; ++k) {
-                        const uint32_t i = i0 + k * GROUP + lane;
-                        v[k] = i < part_of.end ? to_f32(x[i]) : -INFINITY;
-                    }
+                for (uint32_t k = 0; k < kAhead; ++k) most = fmaxf(most, v[k]);
+                if (!__any_sync(kNone, most > best.least)) continue;
 #pragma unroll
-                    for (uint32_t k = 0; k < kAhead; ++k) most = fmaxf(most, v[k]);
-                    if (!__any_sync(kNone, most > best.least)) continue;
-#pragma unroll
-                    for (uint32_t k = 0; k < kAhead; ++k)
-                        best.consider([&](int) { return v[k]; }, 1, v[k], i0 + k * GROUP + lane, a.top, lane);
-                }
-                __syncthreads();
+                for (uint32_t k = 0; k < kAhead; ++k)
+                    best.consider([&](int) { return v[k]; }, 1, v[k], i0 + k * GROUP + lane, a.top, lane);
+            }
+            if (GROUP > 32) {
                 lists[warp][lane] = best.best;
                 __syncthreads();
                 if (warp == 0)
                     for (uint32_t w = 1; w < kWarps; ++w) best.best = merged(best.best, lists[w][lane], lane);
             }
         }
-        if (warp == 0) {
-            Sums all = sums[0];
-            for (uint32_t w = 1; w < kWarps; ++w) join(all, sums[w], c);
-            q = all;
-        }
+    }
+    if (GROUP > 32) {
+        if (!TOP) __syncthreads();
+        if (warp == 0) q = joined_lanes<kWarps>(sums[lane % kWarps], c);
         if (parts > 1) {
             cg::cluster_group cluster = cg::this_cluster();
             if (warp == 0) {
@@ -447,8 +419,7 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
         if (a.lse) a.lse[row] = lse;
         if (a.entropy) a.entropy[row] = bad ? nan : empty ? 0.f : fmaxf(0.f, ln_s - kLn2 * mean_d);
         if (a.logprob) {
-            const int32_t tok = token_at(a.tokens, a.token_bits, row, a.V);
-            a.logprob[row] = tok < 0 ? 0.f : bad ? nan : empty ? -INFINITY : fmaf(a.scale, to_f32(x[tok]) - m, -ln_s);
+            a.logprob[row] = token < 0 ? 0.f : bad ? nan : empty ? -INFINITY : fmaf(a.scale, token_logit - m, -ln_s);
         }
     }
     if (!TOP) return;
