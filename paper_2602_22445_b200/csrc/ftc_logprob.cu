@@ -181,7 +181,7 @@ __device__ __forceinline__ uint64_t merged(uint64_t a, uint64_t b, uint32_t lane
     return x;
 }
 
-constexpr uint32_t kLogprobThreads = 256, kListed = 256, kWarpListed = 64;
+constexpr uint32_t kListed = 256, kWarpListed = 128;
 
 // A warp's list, as a row is gone through: what an element has to beat.
 struct Best {
@@ -223,17 +223,18 @@ template <typename T> struct Stretch {
     __device__ __forceinline__ uint32_t single(uint32_t i) const { return i < head - begin ? begin + i : tail + (i - (head - begin)); }
 };
 
-template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds__(kLogprobThreads, TOP ? 3 : 4) token_logprobs_kernel(LogprobArgs a, uint32_t parts) {
+template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds__(GROUP == 32 ? 256 : GROUP, (TOP ? 768 : 1024) / (GROUP == 32 ? 256 : GROUP)) token_logprobs_kernel(LogprobArgs a, uint32_t parts) {
     namespace cg = cooperative_groups;
     constexpr int N = Vec<T>::N;
-    constexpr uint32_t kGroups = kLogprobThreads / GROUP, kWarps = GROUP / 32;
-    __shared__ Sums sums[kLogprobThreads / 32];
-    __shared__ uint64_t lists[kLogprobThreads / 32][32];
+    constexpr uint32_t kThreads = GROUP == 32 ? 256 : GROUP, kGroups = kThreads / GROUP, kWarps = GROUP / 32;
+    __shared__ Sums sums[kThreads / 32];
+    __shared__ uint64_t lists[kThreads / 32][32];
     __shared__ Sums joined;
     __shared__ uint64_t joined_list[32];
     constexpr uint32_t kList = GROUP > 32 ? kListed : kWarpListed;
     __shared__ uint64_t listed_of[TOP ? kGroups : 1][TOP ? kList : 1];
     __shared__ uint32_t count_of[kGroups];
+    __shared__ uint8_t reaching[TOP ? kThreads / 32 : 1][32];
     const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, in_group = threadIdx.x % GROUP;
     const uint32_t part = parts > 1 ? cg::this_cluster().block_rank() : 0;
     const float c = a.scale * kLog2e;
@@ -328,15 +329,27 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
             }
         };
         if (in_group < part_of.singles()) { const uint32_t at = part_of.single(in_group); list(to_f32(x[at]), at); }
-        uint32_t lanes = __ballot_sync(kNone, lane_most >= least && lane_most > -INFINITY);
-        while (lanes) {
-            const uint32_t src = __ffs(lanes) - 1;
-            lanes &= lanes - 1;
-            for (uint32_t i = (in_group - lane) + src + lane * GROUP; i < vecs; i += 32 * GROUP) {
-                float v[N];
-                Vec<T>::numbers(v, __ldg(xv + i));
+        // the warp's lanes that reach it, and all their vectors one after the other over the warp
+        const uint32_t lanes = __ballot_sync(kNone, lane_most >= least && lane_most > -INFINITY), each = (vecs + GROUP - 1) / GROUP;
+        if (lanes >> lane & 1u) reaching[warp][__popc(lanes & ((1u << lane) - 1))] = (uint8_t)lane;
+        __syncwarp();
+        constexpr uint32_t kAtOnce = 4;
+        for (uint32_t k0 = 0, all = __popc(lanes) * each; k0 < all; k0 += 32 * kAtOnce) {
+            uint4 r[kAtOnce];
+            uint32_t at[kAtOnce];
 #pragma unroll
-                for (int j = 0; j < N; ++j) list(v[j], part_of.head + i * N + j);
+            for (uint32_t u = 0; u < kAtOnce; ++u) {
+                const uint32_t k = k0 + u * 32 + lane, o = k / each;
+                at[u] = k < all ? (in_group - lane) + reaching[warp][o] + (k - o * each) * GROUP : vecs;
+                if (at[u] < vecs) r[u] = __ldg(xv + at[u]);
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < kAtOnce; ++u) {
+                if (at[u] >= vecs) continue;
+                float v[N];
+                Vec<T>::numbers(v, r[u]);
+#pragma unroll
+                for (int j = 0; j < N; ++j) list(v[j], part_of.head + at[u] * N + j);
             }
         }
         sync();
@@ -441,24 +454,30 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
     }
 }
 
-template <typename T, bool TOP> static cudaError_t forward(const LogprobArgs& a, int sms, cudaStream_t st) {
-    if (a.V <= 1024) {                                           // a warp for each row
-        token_logprobs_kernel<T, TOP, 32><<<(a.rows + 7) / 8, kLogprobThreads, 0, st>>>(a, 1);
-        return cudaGetLastError();
-    }
-    uint32_t parts = 1;                                          // blocks of a cluster share a row while there are SMs without one
-    while (parts < 8 && (uint64_t)a.rows * parts * 2 <= (uint64_t)sms * 2 && a.V / (parts * 2) >= 4096) parts *= 2;
-    if ((uint64_t)a.rows * parts > 0x7FFFFFFFull) return cudaErrorInvalidValue;
+constexpr uint32_t kManyRows = 6, kWarpVectors = 512;
+template <typename T, bool TOP, uint32_t GROUP> static cudaError_t forward_of(const LogprobArgs& a, uint32_t parts, cudaStream_t st) {
+    constexpr uint32_t kThreads = GROUP == 32 ? 256 : GROUP, kGroups = kThreads / GROUP;
     if (parts == 1) {
-        token_logprobs_kernel<T, TOP, kLogprobThreads><<<a.rows, kLogprobThreads, 0, st>>>(a, 1);
+        token_logprobs_kernel<T, TOP, GROUP><<<(a.rows + kGroups - 1) / kGroups, kThreads, 0, st>>>(a, 1);
         return cudaGetLastError();
     }
     cudaLaunchAttribute shape{};
     shape.id = cudaLaunchAttributeClusterDimension;
     shape.val.clusterDim.x = parts; shape.val.clusterDim.y = shape.val.clusterDim.z = 1;
     cudaLaunchConfig_t how{};
-    how.gridDim = dim3(a.rows * parts); how.blockDim = dim3(kLogprobThreads); how.stream = st; how.attrs = &shape; how.numAttrs = 1;
-    return cudaLaunchKernelEx(&how, token_logprobs_kernel<T, TOP, kLogprobThreads>, a, parts);
+    how.gridDim = dim3(a.rows * parts); how.blockDim = dim3(kThreads); how.stream = st; how.attrs = &shape; how.numAttrs = 1;
+    return cudaLaunchKernelEx(&how, token_logprobs_kernel<T, TOP, GROUP>, a, parts);
+}
+
+template <typename T, bool TOP> static cudaError_t forward(const LogprobArgs& a, int sms, cudaStream_t st) {
+    const uint32_t vecs = (uint32_t)((uint64_t)a.V * sizeof(T) / 16);
+    if (vecs <= 64 || (vecs <= kWarpVectors && a.rows >= 32u * sms)) return forward_of<T, TOP, 32>(a, 1, st);    // a warp for each row
+    // Blocks of a cluster share a row while there are SMs without one. Many rows: blocks of 128 threads, so that more rows are on their way
+    // while others are joined.
+    uint32_t parts = 1;
+    while (parts < 8 && (uint64_t)a.rows * parts * 2 <= (uint64_t)sms * 2 && a.V / (parts * 2) >= 4096) parts *= 2;
+    if (a.rows >= kManyRows * (uint32_t)sms) return forward_of<T, TOP, 128>(a, 1, st);
+    return forward_of<T, TOP, 256>(a, parts, st);
 }
 
 cudaError_t launch_token_logprobs(const LogprobArgs& a, int sms, cudaStream_t st) {
