@@ -504,8 +504,8 @@ FTC_API int ftc_embedding_forward(const ftc_embed_t* desc, uint64_t n, const voi
                                   void* d_y, uint64_t y_stride, void* cuda_stream);
 
 /*
- * The table's gradient, for each process: row v of process p is scale * the sum of dy[t] over its tokens t of value v, in the order of
- * t in runs of FTC_EMBED_RUN (the runs' sums are added in order too).
+ * The table's gradient, for each process: row v of process p is scale * the sum of dy[t] over its tokens t of value v (in a fixed order:
+ * by stretches of the sorted list of tokens, FTC_EMBED_RUN long, or, of few tokens, of the tokens themselves).
  *   d_row_splits  as for ftc_layernorm_backward, of tokens
  *   d_dtable      float32 [ceil(V*H/k)][P][k], the inputs of ceil(V*H/k) scenarios for ftc_allreduce_batch: element e = v*H + h of
  *                 process p is element e % k of message e / k; the last message is filled up with zeros. Written whole.

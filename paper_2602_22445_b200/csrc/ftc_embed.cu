@@ -9,7 +9,7 @@
 //   2. the sorted list is cut into chunks of 32; a warp sums a chunk's rows of dy for its 256 columns, run by run (a run: one token of one
 //      process), and writes the runs that lie inside the chunk where they belong, sums of the others to the workspace;
 //   3. runs that cross chunks: the first chunk's sum and the following ones' in order, shared out over the warps of a block.
-// Whatever the tokens' distribution, all warps of step 2 have 32 rows to sum. No atomic addition takes part.
+// Whatever the tokens' distribution, all warps of step 2 have 32 rows to sum. No atomic addition takes part. Few tokens are not sorted.
 #include <cooperative_groups.h>
 #include "ftc_lm.cuh"
 
@@ -221,109 +221,147 @@ __global__ void __launch_bounds__(kSortThreads) sort_and_zero_kernel(EmbedArgs a
 
 // ---- backward: sums of runs ----
 
-// Eight columns of a lane, as in the forward pass; those beyond H are not touched.
-template <typename T, bool WIDE> __device__ __forceinline__ void load_columns(float* v, const T* row, uint32_t lane, uint32_t left) {
-    if (WIDE) {
-        if (lane * 8 < left) load8(v, row + lane * 8);
-        else {
+// A lane's columns of a warp's piece: eight neighbours (WIDE, pieces of 256) or two that lie 32 apart (pieces of 64: rows on any address, and
+// more warps for the short rows that odd widths are). Rows are loaded as they are, several ahead, and become numbers when they are added.
+template <typename T, bool WIDE> struct Columns;
+template <typename T> struct Columns<T, true> {
+    static constexpr uint32_t kCols = 8, kPieceCols = 256, kAhead = sizeof(T) == 2 ? 8 : 4;
+    struct Raw { uint4 r[sizeof(T) / 2]; };
+    static __device__ __forceinline__ bool has(uint32_t lane, uint32_t left) { return lane * 8 < left; }
+    static __device__ __forceinline__ void load(Raw& w, const T* row, uint32_t lane, uint32_t left) {
+        if (!has(lane, left)) return;
+        const uint4* p = reinterpret_cast<const uint4*>(row + lane * 8);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = 0.f;
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = lane + j * 32 < left ? to_f32(row[lane + j * 32]) : 0.f;
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) w.r[i] = __ldg(p + i);
     }
-}
-template <bool WIDE> __device__ __forceinline__ void store_columns(float* row, const float* v, uint32_t lane, uint32_t left) {
-    if (WIDE) {
-        if (lane * 8 < left) store8(row + lane * 8, v);
-    } else {
+    static __device__ __forceinline__ void add(float* v, const Raw& w, bool fresh) {
+        float x[8];
+        load8(x, reinterpret_cast<const T*>(w.r));
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (lane + j * 32 < left) row[lane + j * 32] = v[j];
+        for (int i = 0; i < 8; ++i) v[i] = fresh ? x[i] : v[i] + x[i];
     }
-}
+    static __device__ __forceinline__ void add_floats(float* v, const float* row, uint32_t lane, uint32_t left) {
+        if (!has(lane, left)) return;
+        float x[8];
+        load8(x, row + lane * 8);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += x[i];
+    }
+    static __device__ __forceinline__ void store(float* row, const float* v, uint32_t lane, uint32_t left) {
+        if (has(lane, left)) store8(row + lane * 8, v);
+    }
+};
+template <typename T> struct Columns<T, false> {
+    static constexpr uint32_t kCols = 2, kPieceCols = 64, kAhead = 16;
+    struct Raw { T r[2]; };
+    static __device__ __forceinline__ void load(Raw& w, const T* row, uint32_t lane, uint32_t left) {
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i)
+            if (lane + i * 32 < left) w.r[i] = row[lane + i * 32];
+    }
+    static __device__ __forceinline__ void add(float* v, const Raw& w, bool fresh) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) v[i] = fresh ? to_f32(w.r[i]) : v[i] + to_f32(w.r[i]);
+    }
+    static __device__ __forceinline__ void add_floats(float* v, const float* row, uint32_t lane, uint32_t left) {
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i)
+            if (lane + i * 32 < left) v[i] += row[lane + i * 32];
+    }
+    static __device__ __forceinline__ void store(float* row, const float* v, uint32_t lane, uint32_t left) {
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i)
+            if (lane + i * 32 < left) row[lane + i * 32] = v[i];
+    }
+};
 
-// The gradient's row v of process p, columns c .. c+255: where the messages have them.
-template <bool WIDE> __device__ __forceinline__ void store_messages(const EmbedArgs& a, uint32_t v, uint32_t p, uint32_t c, const float* x, uint32_t lane, uint32_t left) {
+// The message of place r (counted from the beginning of a message that a piece begins in): r / k. Pieces are shorter than 4096, and r is below
+// k + 4096: with a k of that at most, r * k stays below 2^32, which makes the multiplication exact.
+__device__ __forceinline__ uint32_t messages_on(const EmbedArgs& a, uint32_t r) { return a.k < 4096 ? __umulhi(r, a.k_inverse) + (a.k == 1 ? r : 0) : r >= a.k; }
+
+// The gradient's row v of process p, columns from c on: where the messages have them.
+template <typename T, bool WIDE> __device__ __forceinline__ void store_messages(const EmbedArgs& a, uint32_t v, uint32_t p, uint32_t c, float* x, uint32_t lane, uint32_t left) {
+    using Cols = Columns<T, WIDE>;
     const uint64_t e = (uint64_t)v * a.H + c;
-    float y[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = x[j] * a.scale;
-    if (a.P == 1) { store_columns<WIDE>(a.dtable + e, y, lane, left); return; }
-    const uint64_t s0 = e / a.k;
-    const uint32_t r0 = (uint32_t)(e - s0 * a.k);                // k and 256 together: no sum passes 32 bits
+    for (uint32_t j = 0; j < Cols::kCols; ++j) x[j] *= a.scale;
+    if (a.P == 1) { Cols::store(a.dtable + e, x, lane, left); return; }
+    const uint64_t s0 = a.k_shift < 32 ? e >> a.k_shift : e / a.k;
+    const uint32_t r0 = (uint32_t)(e - s0 * a.k);
+    float* const out = a.dtable + (s0 * a.P + p) * a.k;
     if (WIDE) {                                                  // k, H and the address allow vectors of four (launch_embedding_backward)
         if (lane * 8 >= left) return;
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const uint32_t r = r0 + lane * 8 + q * 4, s = r / a.k;
-            *reinterpret_cast<float4*>(a.dtable + ((s0 + s) * a.P + p) * a.k + (r - s * a.k)) = make_float4(y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
+        for (uint32_t q = 0; q < 2; ++q) {
+            const uint32_t r = r0 + lane * 8 + q * 4, s = messages_on(a, r);
+            *reinterpret_cast<float4*>(out + (uint64_t)s * a.P * a.k + (r - s * a.k)) = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (uint32_t j = 0; j < Cols::kCols; ++j)
             if (lane + j * 32 < left) {
-                const uint32_t r = r0 + lane + j * 32, s = r / a.k;
-                a.dtable[((s0 + s) * a.P + p) * a.k + (r - s * a.k)] = y[j];
+                const uint32_t r = r0 + lane + j * 32, s = messages_on(a, r);
+                out[(uint64_t)s * a.P * a.k + (r - s * a.k)] = x[j];
             }
     }
 }
 
-template <typename T, bool WIDE> __global__ void __launch_bounds__(128) sum_runs_kernel(EmbedArgs a, uint32_t pieces, uint64_t units) {
+template <typename T, bool WIDE> __global__ void __launch_bounds__(128) sum_runs_kernel(EmbedArgs a, uint32_t pieces, uint32_t units) {
+    using Cols = Columns<T, WIDE>;
     wait_for_earlier_kernel();
     later_kernel_may_start();
-    const uint32_t lane = threadIdx.x % 32;
-    const uint64_t u = (uint64_t)blockIdx.x * 4 + threadIdx.x / 32;
+    const uint32_t lane = threadIdx.x % 32, u = blockIdx.x * 4 + threadIdx.x / 32;
     if (u >= units) return;
-    const uint32_t chunk = (uint32_t)(u / pieces), c = (uint32_t)(u - (uint64_t)chunk * pieces) * kPiece, left = a.H - c;
+    const uint32_t chunk = u / pieces, c = (u - chunk * pieces) * Cols::kPieceCols, left = a.H - c;
     const uint32_t b = chunk * kChunk, i = b + lane, m = min(kChunk, a.n - b);
     const bool there = lane < m;
     const uint32_t key = there ? a.keys[0][i] : a.V, index = there ? a.index[0][i] : 0, process = there ? a.process[i] : 0;
     // does the entry continue the run of the one before it; does the entry behind the chunk continue the last one's
     const uint32_t key_before = i && there ? a.keys[0][i - 1] : 0xFFFFFFFFu, process_before = i && there ? a.process[i - 1] : 0;
+    const uint32_t key_behind = b + m < a.n ? a.keys[0][b + m] : 0xFFFFFFFFu, process_behind = b + m < a.n ? a.process[b + m] : 0;
     const uint32_t goes_on = __ballot_sync(0xFFFFFFFFu, there && key == key_before && process == process_before);
+    const uint32_t live = __popc(__ballot_sync(0xFFFFFFFFu, key < a.V));         // those that count for nobody come last
     const uint32_t last = m - 1, key_last = __shfl_sync(0xFFFFFFFFu, key, last), process_last = __shfl_sync(0xFFFFFFFFu, process, last);
-    const bool leaves = b + m < a.n && a.keys[0][b + m] == key_last && a.process[b + m] == process_last;
-    const T* dy = static_cast<const T*>(a.dy) + c;
-    float sum[8];
-    constexpr uint32_t kAhead = 8;
-    for (uint32_t e0 = 0; e0 < m; e0 += kAhead) {
-        float v[kAhead][8];
+    const bool leaves = key_behind == key_last && process_behind == process_last;
+    const T* const dy = static_cast<const T*>(a.dy) + c;
+    float sum[Cols::kCols];
+    for (uint32_t e0 = 0; e0 < live; e0 += Cols::kAhead) {
+        typename Cols::Raw raw[Cols::kAhead];
 #pragma unroll
-        for (uint32_t j = 0; j < kAhead; ++j) {
-            const uint32_t e = e0 + j, k = __shfl_sync(0xFFFFFFFFu, key, e & 31), row = __shfl_sync(0xFFFFFFFFu, index, e & 31);
-            if (e < m && k < a.V) load_columns<T, WIDE>(v[j], dy + (uint64_t)row * a.dy_stride, lane, left);
+        for (uint32_t j = 0; j < Cols::kAhead; ++j) {
+            const uint32_t row = __shfl_sync(0xFFFFFFFFu, index, (e0 + j) & 31);
+            if (e0 + j < live) Cols::load(raw[j], dy + (uint64_t)row * a.dy_stride, lane, left);
         }
 #pragma unroll
-        for (uint32_t j = 0; j < kAhead; ++j) {
-            const uint32_t e = e0 + j, k = __shfl_sync(0xFFFFFFFFu, key, e & 31), p = __shfl_sync(0xFFFFFFFFu, process, e & 31);
-            if (e >= m || k >= a.V) continue;
-            const bool fresh = e == 0 || !(goes_on >> e & 1u);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) sum[q] = fresh ? v[j][q] : sum[q] + v[j][q];
-            const bool ends = e == last ? true : !(goes_on >> (e + 1) & 1u);
-            if (!ends) continue;
-            const uint32_t here = goes_on & ((2u << e) - 1);     // the run began before this chunk if all its entries up to the first go on
-            const bool from_before = here == (2u << e) - 1, to_next = e == last && leaves;
-            if (from_before) store_columns<WIDE>(a.parts + (uint64_t)chunk * 2 * a.H + c, sum, lane, left);
-            else if (to_next) store_columns<WIDE>(a.parts + ((uint64_t)chunk * 2 + 1) * a.H + c, sum, lane, left);
-            else store_messages<WIDE>(a, k, p, c, sum, lane, left);
+        for (uint32_t j = 0; j < Cols::kAhead; ++j) {
+            const uint32_t e = e0 + j;
+            if (e >= live) break;
+            Cols::add(sum, raw[j], e == 0 || !(goes_on >> e & 1u));
+            if (e != last && (goes_on >> (e + 1) & 1u)) continue;
+            const uint32_t k = __shfl_sync(0xFFFFFFFFu, key, e), p = __shfl_sync(0xFFFFFFFFu, process, e);
+            const uint32_t all = (2u << e) - 1;                  // the run began before this chunk if all its entries up to the first go on
+            if ((goes_on & all) == all) Cols::store(a.parts + (uint64_t)chunk * 2 * a.H + c, sum, lane, left);
+            else if (e == last && leaves) Cols::store(a.parts + ((uint64_t)chunk * 2 + 1) * a.H + c, sum, lane, left);
+            else store_messages<T, WIDE>(a, k, p, c, sum, lane, left);
         }
     }
 }
 
-// Runs that begin in one chunk and end in a later one: a block for each chunk's last run and 256 columns.
+// Runs that begin in one chunk and end in a later one: a block for each chunk's last run. A warp takes a piece of the columns; where a run is
+// long, the block's warps share its chunks, and the sums of the eight parts are added in order.
 template <bool WIDE> __global__ void __launch_bounds__(256) join_runs_kernel(EmbedArgs a, uint32_t pieces) {
+    using Cols = Columns<float, WIDE>;
+    constexpr uint32_t kLong = 16;                               // chunks
     wait_for_earlier_kernel();
-    const uint32_t chunk = (uint32_t)(blockIdx.x / pieces), c = (blockIdx.x - chunk * pieces) * kPiece, left = a.H - c;
-    const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const uint32_t next = (chunk + 1) * kChunk, key = a.keys[0][next], process = a.process[next];
-    if (key >= a.V || a.keys[0][next - 1] != key || a.process[next - 1] != process) return;          // nothing leaves this chunk
-    if (chunk && a.keys[0][next - kChunk - 1] == key && a.process[next - kChunk - 1] == process) return;   // began further before
+    const uint32_t chunk = blockIdx.x, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const uint32_t next = (chunk + 1) * kChunk;
+    const uint32_t key = a.keys[0][next], process = a.process[next], key_here = a.keys[0][next - 1], process_here = a.process[next - 1];
+    const uint32_t key_first = chunk ? a.keys[0][next - kChunk - 1] : 0xFFFFFFFFu, process_first = chunk ? a.process[next - kChunk - 1] : 0;
+    if (key >= a.V || key_here != key || process_here != process) return;        // nothing leaves this chunk
+    if (key_first == key && process_first == process) return;                    // began further before
     // the run's last chunk: the first one behind whose end another run begins
     __shared__ uint32_t found;
-    __shared__ float sums[8][kPiece];
+    __shared__ float sums[8][Cols::kCols][32];
     const uint32_t chunks = (a.n + kChunk - 1) / kChunk;
     uint32_t to = chunk + 1;
     for (;;) {                                                   // 256 chunks at a time; the list ends, and so does this
@@ -338,47 +376,122 @@ template <bool WIDE> __global__ void __launch_bounds__(256) join_runs_kernel(Emb
         if (f != 0xFFFFFFFFu) { to = f; break; }
         to += 256;
     }
-    // warp w has an eighth of the chunks behind the first, in order
-    const uint32_t n = to - chunk, each = (n + 7) / 8, q0 = chunk + 1 + warp * each, q1 = min(to + 1, q0 + each);
-    float sum[8], v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sum[j] = 0.f;
-    if (warp == 0) load_columns<float, WIDE>(sum, a.parts + ((uint64_t)chunk * 2 + 1) * a.H + c, lane, left);
-#pragma unroll 4
-    for (uint32_t q = q0; q < q1; ++q) {
-        load_columns<float, WIDE>(v, a.parts + (uint64_t)q * 2 * a.H + c, lane, left);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum[j] += v[j];
+    const uint32_t n = to - chunk;
+    const float* const parts = a.parts;
+    const uint64_t step = 2 * (uint64_t)a.H;
+    if (n <= kLong) {
+        for (uint32_t piece = warp; piece < pieces; piece += 8) {
+            const uint32_t c = piece * Cols::kPieceCols, left = a.H - c;
+            float sum[Cols::kCols] = {};
+            Cols::add_floats(sum, parts + (uint64_t)chunk * step + a.H + c, lane, left);
+#pragma unroll 8
+            for (uint32_t q = 1; q <= n; ++q) Cols::add_floats(sum, parts + (chunk + q) * step + c, lane, left);
+            store_messages<float, WIDE>(a, key, process, c, sum, lane, left);
+        }
+        return;
     }
+    const uint32_t each = (n + 7) / 8, q0 = 1 + warp * each, q1 = min(n + 1, q0 + each);
+    for (uint32_t piece = 0; piece < pieces; ++piece) {
+        const uint32_t c = piece * Cols::kPieceCols, left = a.H - c;
+        float sum[Cols::kCols] = {};
+        if (warp == 0) Cols::add_floats(sum, parts + (uint64_t)chunk * step + a.H + c, lane, left);
+#pragma unroll 8
+        for (uint32_t q = q0; q < q1; ++q) Cols::add_floats(sum, parts + (chunk + q) * step + c, lane, left);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sums[warp][j * 32 + lane] = sum[j];
+        for (uint32_t j = 0; j < Cols::kCols; ++j) sums[warp][j][lane] = sum[j];
+        __syncthreads();
+        if (warp == piece % 8) {                                 // another warp each time
+#pragma unroll
+            for (uint32_t j = 0; j < Cols::kCols; ++j) {
+                sum[j] = sums[0][j][lane];
+                for (uint32_t w = 1; w < 8; ++w) sum[j] += sums[w][j][lane];
+            }
+            store_messages<float, WIDE>(a, key, process, c, sum, lane, left);
+        }
+        __syncthreads();
+    }
+}
+
+// Few tokens (kFew at most) need no sorting: a block for each token and piece of its columns, which goes on if the token is the first of its value
+// in its process. Its eight warps look through an eighth of the process's tokens each and sum what they find, eight rows ahead.
+constexpr uint32_t kFew = 1024;
+template <typename T, bool WIDE> __global__ void __launch_bounds__(256) sum_few_kernel(EmbedArgs a) {
+    using Cols = Columns<T, WIDE>;
+    const uint32_t t = blockIdx.y, c = blockIdx.x * Cols::kPieceCols, left = a.H - c, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int32_t token = token_at(a.tokens, a.token_bits, t, a.V), p = process_of(a, t);
+    // the process's tokens
+    uint32_t first = 0, end = a.n;
+    if (p >= 0 && a.splits) {
+        first = (uint32_t)min((uint64_t)a.n, a.splits[p]); end = (uint32_t)min((uint64_t)a.n, a.splits[p + 1]);
+    } else if (p >= 0 && a.P > 1) {
+        first = (uint32_t)((uint64_t)p * a.n / a.P); end = (uint32_t)(((uint64_t)p + 1) * a.n / a.P);
+    }
+    const uint32_t each = ((end - first + 7) / 8 + 31) & ~31u, i0 = first + warp * each, i1 = min(end, i0 + each);      // i0 may lie behind the end
+    uint32_t found[kFew / 256] = {};                             // bits of this warp's tokens that are the same
+    bool earlier = false;
+#pragma unroll
+    for (uint32_t w = 0; w < kFew / 256; ++w) {
+        const uint32_t i = i0 + w * 32 + lane;
+        const bool same = i < i1 && token_at(a.tokens, a.token_bits, i, a.V) == token;
+        found[w] = __ballot_sync(0xFFFFFFFFu, same);
+        earlier |= same && i < t;
+    }
+    const bool none = __syncthreads_or(earlier || token < 0 || p < 0);
+    wait_for_earlier_kernel();                                   // the zeros
+    if (none) return;
+    const T* const dy = static_cast<const T*>(a.dy) + c;
+    float sum[Cols::kCols] = {};
+#pragma unroll
+    for (uint32_t w = 0; w < kFew / 256; ++w) {
+        uint32_t bits = found[w];
+        while (bits) {
+            typename Cols::Raw raw[Cols::kAhead];
+            uint32_t rest = bits;
+#pragma unroll
+            for (uint32_t j = 0; j < Cols::kAhead; ++j) {
+                if (rest) Cols::load(raw[j], dy + (uint64_t)(i0 + w * 32 + __ffs(rest) - 1) * a.dy_stride, lane, left);
+                rest &= rest - 1;
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < Cols::kAhead; ++j) {
+                if (bits) Cols::add(sum, raw[j], false);
+                bits &= bits - 1;
+            }
+        }
+    }
+    __shared__ float sums[8][Cols::kCols][32];
+#pragma unroll
+    for (uint32_t j = 0; j < Cols::kCols; ++j) sums[warp][j][lane] = sum[j];
     __syncthreads();
     if (warp) return;
-    for (uint32_t w = 1; w < 8 && (w * each) < n; ++w) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum[j] += sums[w][j * 32 + lane];
-    }
-    store_messages<WIDE>(a, key, process, c, sum, lane, left);
+    for (uint32_t j = 0; j < Cols::kCols; ++j)
+        for (uint32_t w = 1; w < 8; ++w) sum[j] += sums[w][j][lane];
+    store_messages<T, WIDE>(a, (uint32_t)token, (uint32_t)p, c, sum, lane, left);
 }
 
-template <typename T, bool WIDE> static cudaError_t sums(const EmbedArgs& a, cudaStream_t st) {
-    const uint32_t pieces = (a.H + kPiece - 1) / kPiece, chunks = (a.n + kChunk - 1) / kChunk;
+template <typename T, bool WIDE> static cudaError_t sums(const EmbedArgs& a, bool few, cudaStream_t st) {
+    const uint32_t cols = Columns<T, WIDE>::kPieceCols, pieces = (a.H + cols - 1) / cols, chunks = (a.n + kChunk - 1) / kChunk;
+    if (few) return launch_second(sum_few_kernel<T, WIDE>, dim3(pieces, a.n), 256, st, a);
     const uint64_t units = (uint64_t)chunks * pieces;
-    if ((units + 3) / 4 > 0x7FFFFFFFull) return cudaErrorInvalidValue;
-    cudaError_t e = launch_second(sum_runs_kernel<T, WIDE>, (uint32_t)((units + 3) / 4), 128, st, a, pieces, units);
+    if (units > 0x7FFFFFFFull) return cudaErrorInvalidValue;     // refused before (ftc_lm_api.cu)
+    cudaError_t e = launch_second(sum_runs_kernel<T, WIDE>, (uint32_t)((units + 3) / 4), 128, st, a, pieces, (uint32_t)units);
     if (e != cudaSuccess || chunks < 2) return e;
-    if ((uint64_t)(chunks - 1) * pieces > 0x7FFFFFFFull) return cudaErrorInvalidValue;
-    return launch_second(join_runs_kernel<WIDE>, (chunks - 1) * pieces, 256, st, a, pieces);
+    return launch_second(join_runs_kernel<WIDE>, chunks - 1, 256, st, a, pieces);
 }
 
-cudaError_t launch_embedding_backward(const EmbedArgs& a, int sms, cudaStream_t st) {
+cudaError_t launch_embedding_backward(const EmbedArgs& args, int sms, cudaStream_t st) {
+    EmbedArgs a = args;
+    a.k_shift = a.k & (a.k - 1) ? 32 : (uint32_t)__builtin_ctz(a.k);
+    a.k_inverse = (uint32_t)(((1ull << 32) + a.k - 1) / a.k);
+    const bool few = a.n <= kFew;
     // One block sorts up to a tile; a cluster of eight beyond.
     const uint32_t C = a.n > kTile ? 8 : 1;
     const uint64_t quads = (a.out_floats / 4 + kSortThreads - 1) / kSortThreads;
     uint32_t fill = (uint32_t)sms * 2;
     if (quads < fill) fill = (uint32_t)quads + 1;
-    uint32_t passes = 0;                                         // no tokens: zeros only
-    if (a.n) for (passes = 1; passes < 4 && a.V >> (8 * passes); ++passes) {}
+    uint32_t passes = 0;                                         // few or no tokens: zeros only
+    if (!few) for (passes = 1; passes < 4 && a.V >> (8 * passes); ++passes) {}
     cudaLaunchAttribute shape{};
     shape.id = cudaLaunchAttributeClusterDimension;
     shape.val.clusterDim.x = C; shape.val.clusterDim.y = shape.val.clusterDim.z = 1;
@@ -388,9 +501,9 @@ cudaError_t launch_embedding_backward(const EmbedArgs& a, int sms, cudaStream_t 
     if (e != cudaSuccess || !a.n) return e;
     const uint64_t es = a.dtype == FTC_F32 ? 4 : 2;
     const bool wide = a.H % 8 == 0 && (a.k % 4 == 0 || a.P == 1) && on16(a.dy, a.dy_stride * es) && on16(a.dtable, 0);
-    if (a.dtype == FTC_F32) return wide ? sums<float, true>(a, st) : sums<float, false>(a, st);
-    if (a.dtype == FTC_BF16) return wide ? sums<__nv_bfloat16, true>(a, st) : sums<__nv_bfloat16, false>(a, st);
-    return wide ? sums<__half, true>(a, st) : sums<__half, false>(a, st);
+    if (a.dtype == FTC_F32) return wide ? sums<float, true>(a, few, st) : sums<float, false>(a, few, st);
+    if (a.dtype == FTC_BF16) return wide ? sums<__nv_bfloat16, true>(a, few, st) : sums<__nv_bfloat16, false>(a, few, st);
+    return wide ? sums<__half, true>(a, few, st) : sums<__half, false>(a, few, st);
 }
 
 }  // namespace ftc

@@ -12,7 +12,7 @@ struct EmbedArgs {
     uint32_t *keys[2], *index[2], *process;      // the sorted tokens and their positions (two sides of the passes), their processes
     float* parts;                                // [chunks][2][H]: sums of runs that leave their chunk
     uint64_t table_stride, y_stride, dy_stride, out_floats;
-    uint32_t n, V, H, P, k, dtype, wdtype, token_bits;
+    uint32_t n, V, H, P, k, dtype, wdtype, token_bits, k_shift, k_inverse;       // k = 2^k_shift, or 32; ceil(2^32 / k), as 32 bits
     float scale;
 };
 cudaError_t launch_embedding_forward(const EmbedArgs& a, int sms, cudaStream_t st);

@@ -117,6 +117,7 @@ int ftc_embedding_backward(const ftc_embed_t* desc, uint64_t n, const void* d_to
     if (rc != FTC_OK) return rc;
     if (!d_dtable || !aligned(d_dtable, 4) || !aligned(d_row_splits, 8)) return FTC_EINVAL;
     if (n && (!d_tokens || !d_dy || dy_stride < desc->H || dy_stride > kFar || !aligned(d_tokens, desc->token_bits / 8) || !aligned(d_dy, size_of(desc->dtype)))) return FTC_EINVAL;
+    if ((n + FTC_EMBED_RUN - 1) / FTC_EMBED_RUN * ((desc->H + 63) / 64) > 0x7FFFFFFFull) return FTC_ETOOLARGE;
     if (n && (!d_workspace || !aligned(d_workspace, 16) || workspace_bytes < embed_workspace(desc, n))) return FTC_EWORKSPACE;
     if ((rc = sm_count(sms)) != FTC_OK) return rc;
     EmbedArgs a{};
