@@ -3,9 +3,9 @@
 // Forward: y[t] = scale * table[token t]. A warp takes a piece of a row, 8 elements a lane; bound by memory.
 //
 // Backward: the gradient of a table of V rows is dense (it is what the allreduce's messages hold), almost all of it zeros, so its bytes
-// are mostly those of writing zeros. Three kernels:
+// are mostly those of writing zeros. The kernels:
 //   1. one cluster sorts the tokens (a stable radix sort by value, 8 bits a pass, so that equal tokens keep their order, and with it
-//      the order of processes); all other blocks write zeros to the whole gradient meanwhile;
+//      the order of processes); the rest of the GPU writes zeros to the whole gradient meanwhile, a kernel of its own;
 //   2. the sorted list is cut into chunks of 32; a warp sums a chunk's rows of dy for its 256 columns, run by run (a run: one token of one
 //      process), and writes the runs that lie inside the chunk where they belong, sums of the others to the workspace;
 //   3. runs that cross chunks: the first chunk's sum and the following ones' in order, shared out over the warps of a block.
@@ -102,6 +102,26 @@ cudaError_t launch_embedding_forward(const EmbedArgs& a, int sms, cudaStream_t s
 
 // ---- backward: the tokens sorted, zeros written ----
 
+// Zeros, 32 KB a block in stores of 32 bytes: many short blocks, one after the other through memory (7.3 TB/s; blocks that stride through all of
+// it made 5.5, copies out of zeroed shared memory 4.2). The sorting goes on meanwhile: one thread waits for it.
+constexpr uint32_t kZeroThreads = 256, kZeroFloats = 8192;
+__global__ void __launch_bounds__(kZeroThreads) zero_kernel(float* out, uint64_t n, uint32_t sorting) {
+    later_kernel_may_start();
+    const uint64_t ahead = min(n, (uint64_t)((32 - (reinterpret_cast<uintptr_t>(out) & 31)) & 31) / 4), eights = (n - ahead) / 8, behind = ahead + eights * 8;
+    float* const p = out + ahead;
+    const uint64_t i0 = (uint64_t)blockIdx.x * (kZeroFloats / 8) + threadIdx.x;
+#pragma unroll
+    for (uint32_t j = 0; j < kZeroFloats / 8 / kZeroThreads; ++j) {
+        const uint64_t i = i0 + j * kZeroThreads;
+        if (i < eights) asm volatile("st.global.v8.b32 [%0], {%1,%1,%1,%1,%1,%1,%1,%1};" ::"l"(p + i * 8), "r"(0) : "memory");
+    }
+    if (blockIdx.x == 0) {
+        if (threadIdx.x < ahead) out[threadIdx.x] = 0.f;
+        if (behind + threadIdx.x < n) out[behind + threadIdx.x] = 0.f;
+        if (sorting) wait_for_earlier_kernel();
+    }
+}
+
 // The process that holds token t: the one whose rows splits[p] .. splits[p+1]-1 (or even shares) it is among; -1: none.
 __device__ int32_t process_of(const EmbedArgs& a, uint32_t t) {
     if (!a.splits) return a.P == 1 ? 0 : (int32_t)((((uint64_t)t + 1) * a.P - 1) / a.n);
@@ -114,29 +134,17 @@ __device__ int32_t process_of(const EmbedArgs& a, uint32_t t) {
     return (int32_t)lo;
 }
 
-// The first cluster sorts (token, position) by token in `passes` passes of 8 bits; tokens that count for nobody have the value V and
-// come last. All blocks of the other clusters write zeros.
+// One cluster sorts (token, position) by token in `passes` passes of 8 bits; tokens that count for nobody have the value V and come last.
 //
 // A block of the cluster has one stretch of the list, in each pass. It counts its digits, reads all blocks' counts, and gives every entry
 // its place: entries with smaller digits, then those of earlier blocks, of earlier tiles, of earlier warps, of earlier rounds and lanes.
-__global__ void __launch_bounds__(kSortThreads) sort_and_zero_kernel(EmbedArgs a, uint32_t passes) {
+__global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(EmbedArgs a, uint32_t passes) {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t C = cluster.num_blocks(), rank = cluster.block_rank(), tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
     later_kernel_may_start();
-    if (blockIdx.x >= C) {                                       // zeros, 16 bytes a thread and store
-        const uint64_t quads = a.out_floats / 4, step = (uint64_t)(gridDim.x - C) * kSortThreads;
-        const uint64_t i0 = (uint64_t)(blockIdx.x - C) * kSortThreads + tid;
-        if ((reinterpret_cast<uintptr_t>(a.dtable) & 15) == 0) {
-            float4* out = reinterpret_cast<float4*>(a.dtable);
-            for (uint64_t i = i0; i < quads; i += step) out[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (i0 < a.out_floats % 4) a.dtable[quads * 4 + i0] = 0.f;
-        } else {
-            for (uint64_t i = i0; i < a.out_floats; i += step) a.dtable[i] = 0.f;
-        }
-        return;
-    }
-    __shared__ uint32_t counts[2][256], base[256], per_warp[kSortWarps][256], sums[8];
+    __shared__ uint32_t counts[2][256], base[256], sums[8];
+    __shared__ __align__(128) uint32_t per_warp[kSortWarps][256];
     const uint32_t each = ((a.n + C - 1) / C + 31) & ~31u;       // n is at most 2^31: no sum here passes 32 bits
     const uint32_t begin = min(a.n, rank * each), end = min(a.n, begin + each);
     for (uint32_t pass = 0; pass < passes; ++pass) {
@@ -413,11 +421,12 @@ template <bool WIDE> __global__ void __launch_bounds__(256) join_runs_kernel(Emb
 }
 
 // Few tokens (kFew at most) need no sorting: a block for each token and piece of its columns, which goes on if the token is the first of its value
-// in its process. Its eight warps look through an eighth of the process's tokens each and sum what they find, eight rows ahead.
+// in its process (or for some of its pieces). Its eight warps look through an eighth of the process's tokens each and sum what they find, eight
+// rows ahead.
 constexpr uint32_t kFew = 1024;
-template <typename T, bool WIDE> __global__ void __launch_bounds__(256) sum_few_kernel(EmbedArgs a) {
+template <typename T, bool WIDE> __global__ void __launch_bounds__(256) sum_few_kernel(EmbedArgs a, uint32_t pieces) {
     using Cols = Columns<T, WIDE>;
-    const uint32_t t = blockIdx.y, c = blockIdx.x * Cols::kPieceCols, left = a.H - c, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const uint32_t t = blockIdx.y, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int32_t token = token_at(a.tokens, a.token_bits, t, a.V), p = process_of(a, t);
     // the process's tokens
     uint32_t first = 0, end = a.n;
@@ -439,40 +448,48 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256) sum_few_
     const bool none = __syncthreads_or(earlier || token < 0 || p < 0);
     wait_for_earlier_kernel();                                   // the zeros
     if (none) return;
-    const T* const dy = static_cast<const T*>(a.dy) + c;
-    float sum[Cols::kCols] = {};
+    __shared__ float sums[8][Cols::kCols][32];
+    for (uint32_t piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+        const uint32_t c = piece * Cols::kPieceCols, left = a.H - c;
+        const T* const dy = static_cast<const T*>(a.dy) + c;
+        float sum[Cols::kCols] = {};
 #pragma unroll
-    for (uint32_t w = 0; w < kFew / 256; ++w) {
-        uint32_t bits = found[w];
-        while (bits) {
-            typename Cols::Raw raw[Cols::kAhead];
-            uint32_t rest = bits;
+        for (uint32_t w = 0; w < kFew / 256; ++w) {
+            uint32_t bits = found[w];
+            while (bits) {
+                typename Cols::Raw raw[Cols::kAhead];
+                uint32_t rest = bits;
 #pragma unroll
-            for (uint32_t j = 0; j < Cols::kAhead; ++j) {
-                if (rest) Cols::load(raw[j], dy + (uint64_t)(i0 + w * 32 + __ffs(rest) - 1) * a.dy_stride, lane, left);
-                rest &= rest - 1;
-            }
+                for (uint32_t j = 0; j < Cols::kAhead; ++j) {
+                    if (rest) Cols::load(raw[j], dy + (uint64_t)(i0 + w * 32 + __ffs(rest) - 1) * a.dy_stride, lane, left);
+                    rest &= rest - 1;
+                }
 #pragma unroll
-            for (uint32_t j = 0; j < Cols::kAhead; ++j) {
-                if (bits) Cols::add(sum, raw[j], false);
-                bits &= bits - 1;
+                for (uint32_t j = 0; j < Cols::kAhead; ++j) {
+                    if (bits) Cols::add(sum, raw[j], false);
+                    bits &= bits - 1;
+                }
             }
         }
+#pragma unroll
+        for (uint32_t j = 0; j < Cols::kCols; ++j) sums[warp][j][lane] = sum[j];
+        __syncthreads();
+        if (warp == 0) {
+#pragma unroll
+            for (uint32_t j = 0; j < Cols::kCols; ++j)
+                for (uint32_t w = 1; w < 8; ++w) sum[j] += sums[w][j][lane];
+            store_messages<T, WIDE>(a, (uint32_t)token, (uint32_t)p, c, sum, lane, left);
+        }
+        __syncthreads();
     }
-    __shared__ float sums[8][Cols::kCols][32];
-#pragma unroll
-    for (uint32_t j = 0; j < Cols::kCols; ++j) sums[warp][j][lane] = sum[j];
-    __syncthreads();
-    if (warp) return;
-#pragma unroll
-    for (uint32_t j = 0; j < Cols::kCols; ++j)
-        for (uint32_t w = 1; w < 8; ++w) sum[j] += sums[w][j][lane];
-    store_messages<T, WIDE>(a, (uint32_t)token, (uint32_t)p, c, sum, lane, left);
 }
 
-template <typename T, bool WIDE> static cudaError_t sums(const EmbedArgs& a, bool few, cudaStream_t st) {
+template <typename T, bool WIDE> static cudaError_t sums(const EmbedArgs& a, bool few, int sms, cudaStream_t st) {
     const uint32_t cols = Columns<T, WIDE>::kPieceCols, pieces = (a.H + cols - 1) / cols, chunks = (a.n + kChunk - 1) / kChunk;
-    if (few) return launch_second(sum_few_kernel<T, WIDE>, dim3(pieces, a.n), 256, st, a);
+    if (few) {                                                   // no more blocks than the GPU has room for, once there is one for each token
+        const uint32_t most = ((uint32_t)sms * 8 + a.n - 1) / a.n;
+        return launch_second(sum_few_kernel<T, WIDE>, dim3(pieces < most ? pieces : most, a.n), 256, st, a, pieces);
+    }
     const uint64_t units = (uint64_t)chunks * pieces;
     if (units > 0x7FFFFFFFull) return cudaErrorInvalidValue;     // refused before (ftc_lm_api.cu)
     cudaError_t e = launch_second(sum_runs_kernel<T, WIDE>, (uint32_t)((units + 3) / 4), 128, st, a, pieces, (uint32_t)units);
@@ -485,25 +502,29 @@ cudaError_t launch_embedding_backward(const EmbedArgs& args, int sms, cudaStream
     a.k_shift = a.k & (a.k - 1) ? 32 : (uint32_t)__builtin_ctz(a.k);
     a.k_inverse = (uint32_t)(((1ull << 32) + a.k - 1) / a.k);
     const bool few = a.n <= kFew;
-    // One block sorts up to a tile; a cluster of eight beyond.
-    const uint32_t C = a.n > kTile ? 8 : 1;
-    const uint64_t quads = (a.out_floats / 4 + kSortThreads - 1) / kSortThreads;
-    uint32_t fill = (uint32_t)sms * 2;
-    if (quads < fill) fill = (uint32_t)quads + 1;
-    uint32_t passes = 0;                                         // few or no tokens: zeros only
-    if (!few) for (passes = 1; passes < 4 && a.V >> (8 * passes); ++passes) {}
-    cudaLaunchAttribute shape{};
-    shape.id = cudaLaunchAttributeClusterDimension;
-    shape.val.clusterDim.x = C; shape.val.clusterDim.y = shape.val.clusterDim.z = 1;
-    cudaLaunchConfig_t how{};
-    how.gridDim = dim3(C + (fill + C - 1) / C * C); how.blockDim = dim3(kSortThreads); how.stream = st; how.attrs = &shape; how.numAttrs = 1;
-    cudaError_t e = cudaLaunchKernelEx(&how, sort_and_zero_kernel, a, passes);
+    const uint32_t zeros = (uint32_t)((a.out_floats + kZeroFloats - 1) / kZeroFloats);
+    cudaError_t e;
+    if (few) {
+        zero_kernel<<<zeros, kZeroThreads, 0, st>>>(a.dtable, a.out_floats, 0);
+        e = cudaGetLastError();
+    } else {
+        // One block sorts up to a tile; a cluster of eight beyond.
+        uint32_t passes = 1;
+        while (passes < 4 && a.V >> (8 * passes)) ++passes;
+        cudaLaunchAttribute shape{};
+        shape.id = cudaLaunchAttributeClusterDimension;
+        shape.val.clusterDim.x = a.n > kTile ? 8 : 1; shape.val.clusterDim.y = shape.val.clusterDim.z = 1;
+        cudaLaunchConfig_t how{};
+        how.gridDim = dim3(shape.val.clusterDim.x); how.blockDim = dim3(kSortThreads); how.stream = st; how.attrs = &shape; how.numAttrs = 1;
+        e = cudaLaunchKernelEx(&how, sort_tokens_kernel, a, passes);
+        if (e == cudaSuccess) e = launch_second(zero_kernel, zeros, kZeroThreads, st, a.dtable, a.out_floats, 1u);
+    }
     if (e != cudaSuccess || !a.n) return e;
     const uint64_t es = a.dtype == FTC_F32 ? 4 : 2;
     const bool wide = a.H % 8 == 0 && (a.k % 4 == 0 || a.P == 1) && on16(a.dy, a.dy_stride * es) && on16(a.dtable, 0);
-    if (a.dtype == FTC_F32) return wide ? sums<float, true>(a, few, st) : sums<float, false>(a, few, st);
-    if (a.dtype == FTC_BF16) return wide ? sums<__nv_bfloat16, true>(a, few, st) : sums<__nv_bfloat16, false>(a, few, st);
-    return wide ? sums<__half, true>(a, few, st) : sums<__half, false>(a, few, st);
+    if (a.dtype == FTC_F32) return wide ? sums<float, true>(a, few, sms, st) : sums<float, false>(a, few, sms, st);
+    if (a.dtype == FTC_BF16) return wide ? sums<__nv_bfloat16, true>(a, few, sms, st) : sums<__nv_bfloat16, false>(a, few, sms, st);
+    return wide ? sums<__half, true>(a, few, sms, st) : sums<__half, false>(a, few, sms, st);
 }
 
 }  // namespace ftc
