@@ -18,6 +18,8 @@ namespace ftc {
 constexpr uint32_t kChunk = FTC_EMBED_RUN;                       // entries of the sorted list that a warp sums
 constexpr uint32_t kPiece = 256;                                 // columns of a warp
 constexpr uint32_t kSortThreads = 1024, kSortWarps = kSortThreads / 32, kItems = 4, kTile = kSortThreads * kItems;
+constexpr uint32_t kCuts = 1024;                                 // splits that are kept in shared memory
+constexpr uint32_t kHeldBytes = kTile * 8;
 
 // ---- eight neighbouring elements ----
 
@@ -123,15 +125,18 @@ __global__ void __launch_bounds__(kZeroThreads) zero_kernel(float* out, uint64_t
 }
 
 // The process that holds token t: the one whose rows splits[p] .. splits[p+1]-1 (or even shares) it is among; -1: none.
-__device__ int32_t process_of(const EmbedArgs& a, uint32_t t) {
-    if (!a.splits) return a.P == 1 ? 0 : (int32_t)((((uint64_t)t + 1) * a.P - 1) / a.n);
-    if (t < a.splits[0] || t >= a.splits[a.P]) return -1;
-    uint32_t lo = 0, hi = a.P;                                   // splits[lo] <= t < splits[hi]
+template <typename S> __device__ __forceinline__ int32_t process_among(const S* splits, uint32_t P, uint32_t t) {
+    if (t < splits[0] || t >= splits[P]) return -1;
+    uint32_t lo = 0, hi = P;                                     // splits[lo] <= t < splits[hi]
     while (hi - lo > 1) {
         const uint32_t mid = (lo + hi) / 2;
-        if (a.splits[mid] <= t) lo = mid; else hi = mid;
+        if (splits[mid] <= t) lo = mid; else hi = mid;
     }
     return (int32_t)lo;
+}
+__device__ __forceinline__ int32_t process_of(const EmbedArgs& a, uint32_t t) {
+    if (!a.splits) return a.P == 1 ? 0 : (int32_t)((((uint64_t)t + 1) * a.P - 1) / a.n);
+    return process_among(a.splits, a.P, t);
 }
 
 // One cluster sorts (token, position) by token in `passes` passes of 8 bits; tokens that count for nobody have the value V and come last.
@@ -143,33 +148,27 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(EmbedArgs a, 
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t C = cluster.num_blocks(), rank = cluster.block_rank(), tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
     later_kernel_may_start();
+    extern __shared__ __align__(16) unsigned char held_raw[];
     __shared__ uint32_t counts[2][256], base[256], sums[8];
     __shared__ __align__(128) uint32_t per_warp[kSortWarps][256];
     const uint32_t each = ((a.n + C - 1) / C + 31) & ~31u;       // n is at most 2^31: no sum here passes 32 bits
     const uint32_t begin = min(a.n, rank * each), end = min(a.n, begin + each);
-    for (uint32_t pass = 0; pass < passes; ++pass) {
-        const uint32_t shift = pass * 8, side = (passes - 1 - pass) & 1;
-        uint32_t* const count = counts[pass & 1];
-        const uint32_t* const from_key = a.keys[side ^ 1];
-        const uint32_t* const from_index = a.index[side ^ 1];
-        auto key_at = [&](uint32_t i) -> uint32_t {
-            if (pass) return __ldcg(from_key + i);
-            int32_t t = token_at(a.tokens, a.token_bits, i, a.V);
-            if (a.splits && (i < a.splits[0] || i >= a.splits[a.P])) t = -1;
-            return t < 0 ? a.V : (uint32_t)t;
-        };
-        if (tid < 256) count[tid] = 0;
-        __syncthreads();
-        for (uint32_t i0 = begin + warp * 32; i0 < end; i0 += kSortThreads) {
-            const uint32_t i = i0 + lane, digit = i < end ? key_at(i) >> shift & 255u : 256u;
-            const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit);
-            if (digit < 256 && lane == (uint32_t)__ffs(same) - 1) atomicAdd(&count[digit], __popc(same));
-        }
-        cluster.sync();
-        if (tid < 256) {                                         // places of the smaller digits and of the earlier blocks' same ones
+    __shared__ uint32_t cuts[kCuts + 1];
+    const bool near = a.splits && a.P <= kCuts;
+    if (near) for (uint32_t p = tid; p <= a.P; p += kSortThreads) cuts[p] = (uint32_t)min((uint64_t)a.n, a.splits[p]);
+    __syncthreads();
+    auto process_at = [&](uint32_t i) { return (uint32_t)(near ? process_among(cuts, a.P, i) : process_of(a, i)); };
+    auto token_key = [&](uint32_t i) -> uint32_t {
+        int32_t t = token_at(a.tokens, a.token_bits, i, a.V);
+        if (a.splits && (near ? i < cuts[0] || i >= cuts[a.P] : i < a.splits[0] || i >= a.splits[a.P])) t = -1;
+        return t < 0 ? a.V : (uint32_t)t;
+    };
+    // Places of the smaller digits and of the earlier blocks' same ones, from all blocks' counts.
+    auto places = [&](const uint32_t* count) {
+        if (tid < 256) {
             uint32_t total = 0, before = 0;
             for (uint32_t b = 0; b < C; ++b) {
-                const uint32_t c = cluster.map_shared_rank(count, b)[tid];
+                const uint32_t c = cluster.map_shared_rank(const_cast<uint32_t*>(count), b)[tid];
                 if (b < rank) before += c;
                 total += c;
             }
@@ -185,6 +184,86 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(EmbedArgs a, 
             base[tid] = run - total + before;
         }
         __syncthreads();
+    };
+    if (each <= kTile) {
+        // A block's entries stay in registers and, between passes, in the blocks' shared memory.
+        uint32_t* const held = reinterpret_cast<uint32_t*>(held_raw);            // keys, then positions
+        uint32_t key[kItems], index[kItems], place[kItems];
+#pragma unroll
+        for (uint32_t j = 0; j < kItems; ++j) {
+            index[j] = begin + warp * (32 * kItems) + j * 32 + lane;
+            key[j] = index[j] < end ? token_key(index[j]) : 0xFFFFFFFFu;
+        }
+        for (uint32_t pass = 0; pass < passes; ++pass) {
+            const uint32_t shift = pass * 8;
+            uint32_t* const count = counts[pass & 1];
+            auto there = [&](uint32_t j) { return begin + warp * (32 * kItems) + j * 32 + lane < end; };
+            for (uint32_t d = lane; d < 256; d += 32) per_warp[warp][d] = 0;
+            __syncwarp();
+#pragma unroll
+            for (uint32_t j = 0; j < kItems; ++j) {
+                const uint32_t digit = there(j) ? key[j] >> shift & 255u : 256u;
+                const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit), before = __popc(same & ((1u << lane) - 1));
+                place[j] = digit < 256 ? per_warp[warp][digit] + before : 0;
+                __syncwarp();
+                if (digit < 256 && before == 0) per_warp[warp][digit] += __popc(same);
+                __syncwarp();
+            }
+            __syncthreads();
+            {                                                    // four threads a digit, eight warps each
+                const uint32_t d = tid / 4, w0 = tid % 4 * 8;
+                uint32_t c[8], all = 0;
+#pragma unroll
+                for (uint32_t w = 0; w < 8; ++w) { c[w] = per_warp[w0 + w][d]; all += c[w]; }
+                uint32_t run = all;
+#pragma unroll
+                for (int o = 1; o < 4; o <<= 1) {
+                    const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, run, o, 4);
+                    if (tid % 4 >= (uint32_t)o) run += up;
+                }
+                if (tid % 4 == 3) count[d] = run;
+                run -= all;
+#pragma unroll
+                for (uint32_t w = 0; w < 8; ++w) { per_warp[w0 + w][d] = run; run += c[w]; }
+            }
+            cluster.sync();
+            places(count);
+#pragma unroll
+            for (uint32_t j = 0; j < kItems; ++j) {
+                if (!there(j)) continue;
+                const uint32_t d = key[j] >> shift & 255u, to = base[d] + per_warp[warp][d] + place[j];
+                if (pass + 1 == passes) {
+                    a.keys[0][to] = key[j]; a.index[0][to] = index[j]; a.process[to] = process_at(index[j]);
+                } else {
+                    const uint32_t b = to / each;
+                    uint32_t* const h = cluster.map_shared_rank(held, b);
+                    h[to - b * each] = key[j]; h[kTile + to - b * each] = index[j];
+                }
+            }
+            if (pass + 1 == passes) break;
+            cluster.sync();
+#pragma unroll
+            for (uint32_t j = 0; j < kItems; ++j)
+                if (there(j)) { const uint32_t i = warp * (32 * kItems) + j * 32 + lane; key[j] = held[i]; index[j] = held[kTile + i]; }
+        }
+        cluster.sync();                                          // a block's shared memory stays until all have read it
+        return;
+    }
+    for (uint32_t pass = 0; pass < passes; ++pass) {
+        const uint32_t shift = pass * 8, side = (passes - 1 - pass) & 1;
+        uint32_t* const count = counts[pass & 1];
+        const uint32_t* const from_key = a.keys[side ^ 1];
+        const uint32_t* const from_index = a.index[side ^ 1];
+        auto key_at = [&](uint32_t i) -> uint32_t { return pass ? __ldcg(from_key + i) : token_key(i); };
+        if (tid < 256) count[tid] = 0;
+        __syncthreads();
+        for (uint32_t i0 = begin + warp * 32; i0 < end; i0 += kSortThreads) {
+            const uint32_t i = i0 + lane, digit = i < end ? key_at(i) >> shift & 255u : 256u;
+            const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit);
+            if (digit < 256 && lane == (uint32_t)__ffs(same) - 1) atomicAdd(&count[digit], __popc(same));
+        }
+        cluster.sync();
+        places(count);
         for (uint32_t t0 = begin; t0 < end; t0 += kTile) {
             for (uint32_t d = lane; d < 256; d += 32) per_warp[warp][d] = 0;
             __syncwarp();
@@ -218,7 +297,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(EmbedArgs a, 
                     const uint32_t to = per_warp[warp][key[j] >> shift & 255u] + place[j], index = pass ? __ldcg(from_index + i) : i;
                     a.keys[side][to] = key[j];
                     a.index[side][to] = index;
-                    if (pass + 1 == passes) a.process[to] = (uint32_t)process_of(a, index);
+                    if (pass + 1 == passes) a.process[to] = process_at(index);
                 }
             }
             __syncthreads();
@@ -515,8 +594,9 @@ cudaError_t launch_embedding_backward(const EmbedArgs& args, int sms, cudaStream
         shape.id = cudaLaunchAttributeClusterDimension;
         shape.val.clusterDim.x = a.n > kTile ? 8 : 1; shape.val.clusterDim.y = shape.val.clusterDim.z = 1;
         cudaLaunchConfig_t how{};
-        how.gridDim = dim3(shape.val.clusterDim.x); how.blockDim = dim3(kSortThreads); how.stream = st; how.attrs = &shape; how.numAttrs = 1;
-        e = cudaLaunchKernelEx(&how, sort_tokens_kernel, a, passes);
+        how.gridDim = dim3(shape.val.clusterDim.x); how.blockDim = dim3(kSortThreads); how.dynamicSmemBytes = kHeldBytes; how.stream = st; how.attrs = &shape; how.numAttrs = 1;
+        e = cudaFuncSetAttribute(sort_tokens_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldBytes);
+        if (e == cudaSuccess) e = cudaLaunchKernelEx(&how, sort_tokens_kernel, a, passes);
         if (e == cudaSuccess) e = launch_second(zero_kernel, zeros, kZeroThreads, st, a.dtable, a.out_floats, 1u);
     }
     if (e != cudaSuccess || !a.n) return e;
