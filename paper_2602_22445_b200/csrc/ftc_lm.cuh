@@ -45,8 +45,10 @@ __device__ __forceinline__ int32_t token_at(const void* tokens, uint32_t bits, u
 
 constexpr uint64_t kPlanMagic = 0x316E4C5054435446ull;
 constexpr uint32_t kMuonChunk = 4096;                            // elements of a block of the momentum kernel
-enum { kChunks, kBlocks, kGramTiles, kApplyTiles, kItems4 };
-struct PlanHead { uint64_t magic, n_blocks, a_blocks, diagonals; uint32_t items[kItems4], n, pad[3]; };
+enum { kChunks, kBlocks, kGramTiles, kApplyTiles, kSmall, kLists };    // kSmall: matrices that one block takes through all steps
+// A matrix of at most 128 x 256.
+__host__ __device__ inline bool plan_small(uint64_t m, uint64_t w) { return m <= 128 && w <= 256; }
+struct PlanHead { uint64_t magic, n_blocks, a_blocks, diagonals; uint32_t items[kLists], n, pad[2]; };
 struct PlanEntry {
     void* param; float* master; const void* grad; const uint32_t* status;
     uint64_t n, first_block, x_block, a_block, diagonal;         // x_block, a_block: in blocks of 128 x 64 float16; diagonal: in numbers
@@ -54,8 +56,8 @@ struct PlanEntry {
     uint8_t param_dtype, grad_dtype, tall, k_shift;
     float lr_scale, weight_decay;
     uint32_t m, w, mb, nb, kb, wide;                             // X is m x w (m <= w): mb blocks of 128 rows, nb of 64 columns; A: kb of 64 columns. wide: addresses allow eights
-    uint32_t first[kItems4];                                     // where its chunks, blocks, tiles begin
-    uint64_t pad;
+    uint32_t first[kLists];                                      // where its chunks, blocks, tiles begin
+    uint32_t pad;
 };
 static_assert(sizeof(PlanHead) == 64 && sizeof(PlanEntry) == 144, "plan layout");
 __host__ __device__ inline const PlanEntry* plan_entries(const void* p) {
@@ -63,14 +65,14 @@ __host__ __device__ inline const PlanEntry* plan_entries(const void* p) {
 }
 
 struct MuonArgs {
-    const void* plan; const uint32_t* maps[kItems4]; uint32_t n;
+    const void* plan; const uint32_t* maps[kLists]; uint32_t n;
     float* momentum; const float* grad_scale;
     uint32_t* word;                              // first of the workspace: not 0 once a wait has given up
     double2* sums; uint32_t* live; float* factor; // [chunks]: squares of U, messages delivered; [n]: was anything delivered, 2^14 / (|U| + eps)
     float* diag_a;
     unsigned char *x[2], *a, *b;                 // blocks of 128 x 64 float16; with two numbers for each, the low ones x_bytes / a_bytes further on
     uint64_t x_bytes, a_bytes;
-    uint32_t items[kItems4], steps, nesterov, split;
+    uint32_t items[kLists], steps, nesterov, split;
     float lr, mu, eps;
 };
 cudaError_t launch_muon(const MuonArgs& a, int sms, cudaStream_t st);

@@ -64,15 +64,15 @@ bool count_matrices(const ftc_matrix_t* q, uint32_t n, PlanHead& h) {
         h.n_blocks += (t.n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK;
         blocks += mb * nb; h.a_blocks += mb * 2 * mb; h.diagonals += mb * 128;
         chunks += (t.n + kMuonChunk - 1) / kMuonChunk;
-        gram += mb2 * (mb2 + 1) / 2;
-        apply += mb2 * ((nb + 3) / 4);
+        if (plan_small(m, w)) ++h.items[kSmall];
+        else { gram += mb2 * (mb2 + 1) / 2; apply += mb2 * ((nb + 3) / 4); }
         if (h.n_blocks > (1ull << 32) || blocks > 0x7FFFFFFFull || h.a_blocks > 0x7FFFFFFFull || chunks > 0x7FFFFFFFull || gram > 0x7FFFFFFFull || apply > 0x7FFFFFFFull) return false;
     }
     h.items[kChunks] = (uint32_t)chunks; h.items[kBlocks] = (uint32_t)blocks; h.items[kGramTiles] = (uint32_t)gram; h.items[kApplyTiles] = (uint32_t)apply;
     return true;
 }
 size_t plan_bytes(const PlanHead& h) {
-    return sizeof(PlanHead) + (size_t)h.n * sizeof(PlanEntry) + rounded(((size_t)h.items[kChunks] + h.items[kBlocks] + h.items[kGramTiles] + h.items[kApplyTiles] + h.n) * 4, 8);
+    return sizeof(PlanHead) + (size_t)h.n * sizeof(PlanEntry) + rounded(((size_t)h.items[kChunks] + h.items[kBlocks] + h.items[kGramTiles] + h.items[kApplyTiles] + h.items[kSmall] + h.n) * 4, 8);
 }
 
 struct MuonLayout { size_t sums, live, factor, diag_a, x0, x1, a, b, x_bytes, a_bytes, total; };
@@ -192,9 +192,9 @@ int ftc_muon_plan_build(const ftc_matrix_t* h_matrices, uint32_t n, void* h_plan
     }
     // The maps. Tiles of many steps come first, so that the last ones to run are short.
     uint32_t* map = reinterpret_cast<uint32_t*>(e + n);
-    uint32_t* const order = map + h.items[kChunks] + h.items[kBlocks] + h.items[kGramTiles] + h.items[kApplyTiles];      // room for the sorting
+    uint32_t* const order = map + h.items[kChunks] + h.items[kBlocks] + h.items[kGramTiles] + h.items[kApplyTiles] + h.items[kSmall];      // room for the sorting
     for (uint32_t i = 0; i < n; ++i) order[i] = i;
-    for (int w = 0; w < kItems4; ++w) {
+    for (int w = 0; w < kLists; ++w) {
         if (w == kGramTiles) std::sort(order, order + n, [e](uint32_t i, uint32_t j) { return e[i].nb != e[j].nb ? e[i].nb > e[j].nb : i < j; });
         if (w == kApplyTiles) std::sort(order, order + n, [e](uint32_t i, uint32_t j) { return e[i].kb != e[j].kb ? e[i].kb > e[j].kb : i < j; });
         uint32_t at = 0;
@@ -202,7 +202,7 @@ int ftc_muon_plan_build(const ftc_matrix_t* h_matrices, uint32_t n, void* h_plan
             const uint32_t i = order[o];
             PlanEntry& q = e[i];
             const uint32_t mb2 = (q.mb + 1) / 2;
-            const uint32_t count = w == kChunks ? (uint32_t)((q.n + kMuonChunk - 1) / kMuonChunk) : w == kBlocks ? q.mb * q.nb : w == kGramTiles ? mb2 * (mb2 + 1) / 2 : mb2 * ((q.nb + 3) / 4);
+            const uint32_t count = w == kChunks ? (uint32_t)((q.n + kMuonChunk - 1) / kMuonChunk) : w == kBlocks ? q.mb * q.nb : w == kSmall ? plan_small(q.m, q.w) : plan_small(q.m, q.w) ? 0 : w == kGramTiles ? mb2 * (mb2 + 1) / 2 : mb2 * ((q.nb + 3) / 4);
             q.first[w] = at;
             for (const uint32_t end = at + count; at < end; ++at) map[at] = i;
         }
@@ -241,7 +241,7 @@ int ftc_muon_step(const ftc_muon_t* hyper, const void* h_plan, const void* d_pla
     a.diag_a = reinterpret_cast<float*>(ws + l.diag_a);
     a.x[0] = ws + l.x0; a.x[1] = ws + l.x1; a.a = ws + l.a; a.b = ws + l.b; a.x_bytes = l.x_bytes; a.a_bytes = l.a_bytes;
     const uint32_t* map = reinterpret_cast<const uint32_t*>(plan_entries(d_plan) + h->n);
-    for (int w = 0; w < kItems4; ++w) { a.items[w] = h->items[w]; a.maps[w] = map; map += h->items[w]; }
+    for (int w = 0; w < kLists; ++w) { a.items[w] = h->items[w]; a.maps[w] = map; map += h->items[w]; }
     a.steps = hyper->steps; a.nesterov = hyper->nesterov; a.split = hyper->products == 32;
     a.lr = (float)hyper->lr; a.mu = (float)hyper->momentum; a.eps = (float)hyper->eps;
     return status(launch_muon(a, sms, static_cast<cudaStream_t>(cuda_stream)));

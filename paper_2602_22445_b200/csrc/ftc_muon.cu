@@ -696,6 +696,185 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
     if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
+// ---- small matrices ----
+//
+// A matrix of at most 128 x 256 (either way) goes through all its steps in one block's shared memory: X (64 KB, twice that with `split`) and A,
+// which B replaces, each product's sum in tensor memory, read out by eight warps. A chain of launches costs 10 us a product at any size (12 matrices
+// of 64 x 64 and 64 x 256: 164 us a call in all, so 49).
+
+constexpr uint32_t kSmallThreads = 256, kSmallColumns = 4;                       // columns in blocks of 64
+constexpr uint32_t kSmallSmem = 2 * (kSmallColumns + 2) * kBlockBytes + 1024 + 1024;
+
+__device__ __forceinline__ void multiply_alone(uint32_t d, uint64_t a, uint64_t b, uint32_t how, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(how), "r"((uint32_t)add) : "memory");
+}
+
+template <bool SPLIT> __global__ void __launch_bounds__(kSmallThreads, 1) muon_small_kernel(MuonArgs a) {
+    extern __shared__ unsigned char raw[];
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, quarter = warp & 3, half = warp >> 2, r = quarter * 32 + lane;
+    unsigned char* const x = raw + (1024 - (smem_of(raw) & 1023)) % 1024;        // X's blocks, its low numbers', A's, its low numbers'
+    constexpr uint32_t kLowX = kSmallColumns * kBlockBytes, kLowA = 2 * kBlockBytes;
+    unsigned char* const m = x + 2 * kLowX;
+    float* const diag = reinterpret_cast<float*>(m + 2 * kLowA);                 // 128
+    const uint32_t bar = smem_of(diag + 128);                                    // copies; products
+    uint32_t* const words = reinterpret_cast<uint32_t*>(diag + 132);
+    if (threadIdx.x == 0) {
+        bar_init(bar, 1); bar_init(bar + 8, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 256;" ::"r"(smem_of(words)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = words[0];
+    wait_for_earlier_kernel();
+    later_kernel_may_start();
+    const float scale = a.grad_scale ? *a.grad_scale : 1.f;
+    bool ok = true;
+    uint32_t copied = 0, multiplied = 0;
+    const uint32_t count = isfinite(scale) && *reinterpret_cast<volatile uint32_t*>(a.word) == 0 ? a.items[kSmall] : 0;
+    // The block's products of `steps` blocks of 64 of the inner dimension; everybody waits for them.
+    auto product = [&](const unsigned char* left, uint32_t left_low, const unsigned char* right, uint32_t right_low, uint32_t steps, uint32_t columns, bool along) {
+        if (threadIdx.x == 0) {
+            const uint32_t how = 1u << 4 | (along ? 1u << 16 : 0u) | columns / 8 << 17 | 128u / 16 << 24;
+            for (uint32_t g = 0; g < (SPLIT ? 3 : 1); ++g)
+                for (uint32_t s = 0; s < steps; ++s)
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k) {
+                        const uint32_t l = smem_of(left) + (g == 2 ? left_low : 0) + s * kBlockBytes + k * 32, q = smem_of(right) + (g == 1 ? right_low : 0);
+                        multiply_alone(tmem, operand(l, 16, 1024), along ? operand(q + s * (kBlockBytes / 2) + k * 2048, kBlockBytes, 1024) : operand(q + s * kBlockBytes + k * 32, 16, 1024),
+                                       how, g || s || k);
+                    }
+            asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar + 8) : "memory");
+        }
+        __syncwarp();
+        ok = !__syncthreads_or(!bar_wait(bar + 8, multiplied++ & 1));
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    };
+    // 64 columns of the sum as 16-bit numbers into a block.
+    auto put = [&](unsigned char* block, uint32_t low, const F2* v, float own_value, bool own) {
+#pragma unroll
+        for (uint32_t c = 0; c < 8; ++c) {
+            uint32_t h[4], l[4];
+#pragma unroll
+            for (uint32_t q = 0; q < 4; ++q) {
+                const F2 e = v[4 * c + q];
+                h[q] = half2_of(e);
+                if (SPLIT) { const F2 y = pair_of(h[q]); l[q] = half2_of(pair(lo(e) - lo(y), hi(e) - hi(y))); }
+            }
+            *reinterpret_cast<uint4*>(block + piece(r, c)) = make_uint4(h[0], h[1], h[2], h[3]);
+            if (SPLIT) *reinterpret_cast<uint4*>(block + low + piece(r, c)) = make_uint4(l[0], l[1], l[2], l[3]);
+        }
+        if (own) {                                               // the row's place on the diagonal
+            const uint32_t at = piece(r, r % 64 / 8) + r % 8 * 2;
+            const __half h = __float2half_rn(own_value);
+            *reinterpret_cast<__half*>(block + at) = h;
+            if (SPLIT) *reinterpret_cast<__half*>(block + low + at) = __float2half_rn(own_value - __half2float(h));
+        }
+    };
+    auto own_of = [&](const F2* v) {
+        float y = 0.f;
+#pragma unroll
+        for (uint32_t q = 0; q < 32; ++q) {
+            if (r % 64 == 2 * q) y = lo(v[q]);
+            if (r % 64 == 2 * q + 1) y = hi(v[q]);
+        }
+        return y * kDown2;
+    };
+    auto written = [] {                                          // by threads, read by products and copies next
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncthreads();
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    };
+    for (uint32_t u = blockIdx.x; u < count && ok; u += gridDim.x) {
+        const PlanEntry t = plan_entries(a.plan)[a.maps[kSmall][u]];
+        const uint32_t bytes = t.nb * kBlockBytes;
+        if (threadIdx.x == 0) {
+            const unsigned char* from = a.x[0] + t.x_block * kBlockBytes;
+            bar_expect(bar, (SPLIT ? 2 : 1) * bytes);
+            copy_in(smem_of(x), from, bytes, bar);
+            if (SPLIT) copy_in(smem_of(x) + kLowX, from + a.x_bytes, bytes, bar);
+        }
+        ok = !__syncthreads_or(!bar_wait(bar, copied++ & 1));
+        const bool own = r / 64 == half;
+        for (uint32_t s = 0; s < a.steps && ok; ++s) {
+            F2 v[32];
+            product(x, kLowX, x, kLowX, t.nb, 128, false);
+            if (!ok) break;
+            read_64(v, tmem + (quarter * 32 << 16) + half * 64);
+            if (own) diag[r] = own_of(v);
+#pragma unroll
+            for (int q = 0; q < 32; ++q) v[q] = mul(v[q], twice(kDown));
+            put(m + half * kBlockBytes, kLowA, v, 0.f, own);
+            written();
+            product(m, kLowA, m, kLowA, t.kb, 128, false);
+            if (!ok) break;
+            read_64(v, tmem + (quarter * 32 << 16) + half * 64);
+            const float di = diag[r], more = own ? own_of(v) : 0.f;
+            const F2 keep = twice(fmaf(kQ5, di, kQ3));
+            unsigned char* const block = m + half * kBlockBytes;
+#pragma unroll
+            for (uint32_t c = 0; c < 8; ++c) {
+                const uint4 h = *reinterpret_cast<const uint4*>(block + piece(r, c));
+                F2 e[4] = {pair_of(h.x), pair_of(h.y), pair_of(h.z), pair_of(h.w)};
+                if (SPLIT) {
+                    const uint4 l = *reinterpret_cast<const uint4*>(block + kLowA + piece(r, c));
+                    e[0] = add(e[0], pair_of(l.x)); e[1] = add(e[1], pair_of(l.y)); e[2] = add(e[2], pair_of(l.z)); e[3] = add(e[3], pair_of(l.w));
+                }
+                const float4 d0 = *reinterpret_cast<const float4*>(diag + half * 64 + 8 * c), d1 = *reinterpret_cast<const float4*>(diag + half * 64 + 8 * c + 4);
+                const F2 dj[4] = {pair(d0.x, d0.y), pair(d0.z, d0.w), pair(d1.x, d1.y), pair(d1.z, d1.w)};
+#pragma unroll
+                for (uint32_t q = 0; q < 4; ++q) v[4 * c + q] = fma(v[4 * c + q], twice(kQ5 * kDown), mul(e[q], fma(dj[q], twice(kQ5), keep)));
+            }
+            put(block, kLowA, v, (kQ1 + fmaf(kQ5, fmaf(di, di, more), kQ3 * di)) * kUp, own);
+            written();
+            product(m, kLowA, x, kLowX, t.kb, t.nb * 64, true);
+            if (!ok) break;
+            for (uint32_t q = half; q < t.nb; q += 2) {
+                read_64(v, tmem + (quarter * 32 << 16) + q * 64);
+#pragma unroll
+                for (int p = 0; p < 32; ++p) v[p] = mul(v[p], twice(kDown));
+                put(x + q * kBlockBytes, kLowX, v, 0.f, false);
+            }
+            written();
+        }
+        if (threadIdx.x == 0 && ok) {
+            unsigned char* to = a.x[a.steps & 1] + t.x_block * kBlockBytes;
+            copy_out(to, smem_of(x), bytes);
+            if (SPLIT) copy_out(to + a.x_bytes, smem_of(x) + kLowX, bytes);
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        }
+    }
+    if (threadIdx.x == 0 && !ok) {                               // a wait has given up: once more, for what may still be on its way
+        *a.word = 1;
+        bar_wait(bar, (copied - 1) & 1);
+        if (multiplied) bar_wait(bar + 8, (multiplied - 1) & 1);
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 256;" ::"r"(tmem) : "memory");
+}
+
+template <bool SPLIT> static cudaError_t small(const MuonArgs& a, int sms, cudaStream_t st) {
+    cudaError_t e = cudaFuncSetAttribute(muon_small_kernel<SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t how{};
+    how.gridDim = dim3(a.items[kSmall] < (uint32_t)sms ? a.items[kSmall] : (uint32_t)sms); how.blockDim = dim3(kSmallThreads); how.dynamicSmemBytes = kSmallSmem;
+    how.stream = st; how.attrs = &early; how.numAttrs = 1;
+    return cudaLaunchKernelEx(&how, muon_small_kernel<SPLIT>, a);
+}
+
 template <int MODE, bool SPLIT> static cudaError_t product(const MuonArgs& a, uint32_t tiles, uint32_t side, int sms, cudaStream_t st) {
     cudaError_t e = cudaFuncSetAttribute(muon_product_kernel<MODE, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
     if (e != cudaSuccess) return e;
@@ -724,7 +903,8 @@ cudaError_t launch_muon(const MuonArgs& a, int sms, cudaStream_t st) {
     cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess) e = launch_second(muon_norm_kernel, a.n, 256, st, a);
     if (e == cudaSuccess) e = launch_second(muon_layout_kernel, a.items[kBlocks], 256, st, a);
-    if (e == cudaSuccess) e = a.split ? products<true>(a, sms, st) : products<false>(a, sms, st);
+    if (e == cudaSuccess && a.items[kSmall]) e = a.split ? small<true>(a, sms, st) : small<false>(a, sms, st);
+    if (e == cudaSuccess && a.items[kGramTiles]) e = a.split ? products<true>(a, sms, st) : products<false>(a, sms, st);
     if (e == cudaSuccess) e = launch_second(muon_update_kernel, a.items[kBlocks], 256, st, a);
     return e;
 }
