@@ -483,6 +483,8 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
     constexpr uint32_t segments = SPLIT ? 3 : 1;
     auto tile_of = [&](uint32_t u) { return MODE <= kPoly ? gram_tile(a, u) : apply_tile(a, u); };
     // a tile's steps of 64 and its columns: 256, or 128 where there are no more (in the apply kernels up to 64 of them are nobody's)
+    // a tile on the diagonal: the left operand is the right one too
+    auto one_of = [&](const PlanEntry& t, const Tile& q, uint32_t g) { return MODE <= kPoly && g == 0 && q.i == q.j && t.mb > 2 * q.j + 1; };
     auto steps_of = [&](const PlanEntry& t) { return segments * (MODE == kGram ? t.nb : t.kb); };
     auto columns_of = [&](const PlanEntry& t, const Tile& q) { return MODE <= kPoly ? (t.mb > 2 * q.j + 1 ? 256u : 128u) : (t.nb > 4 * q.j + 2 ? 256u : 128u); };
     const unsigned char* const x_in = a.x[side];
@@ -498,8 +500,9 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
             // right operand of a symmetric product: rows half * rank .. of 256; of the others: blocks of 64 columns
             const uint32_t right_row = 2 * tile.j + (half == 128 ? rank : 0), right_in = half == 128 ? 0 : rank * (kBlockBytes / 2);
             const uint32_t right_block = 4 * tile.j + rank * (half / 64), right_blocks = MODE <= kPoly ? 0 : min(half / 64, t.nb > right_block ? t.nb - right_block : 0u);
-            const uint32_t bytes = (has_left ? kBlockBytes : 0) + (MODE <= kPoly ? half * 128 : right_blocks * (kBlockBytes / 2));
             for (uint32_t g = 0; g < segments && ok; ++g) {
+                const bool one = one_of(t, tile, g);
+                const uint32_t bytes = (has_left ? kBlockBytes : 0) + (one ? 0 : MODE <= kPoly ? half * 128 : right_blocks * (kBlockBytes / 2));
                 const unsigned char* l = (MODE == kGram ? x_in : MODE == kPoly ? a.a : a.b) + (g == 2 ? (MODE == kGram ? a.x_bytes : a.a_bytes) : 0);
                 const unsigned char* r = (MODE == kPoly ? a.a : x_in) + (g == 1 ? (MODE == kPoly ? a.a_bytes : a.x_bytes) : 0);
                 l += MODE == kGram ? (t.x_block + (uint64_t)left_row * t.nb) * kBlockBytes : (t.a_block + (uint64_t)left_row * 2 * t.mb) * kBlockBytes;
@@ -510,6 +513,7 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                     if (it >= kStages && !(ok = bar_wait(empty + 8 * slot, (it / kStages - 1) & 1))) break;
                     bar_expect(bar, bytes);
                     if (has_left) copy_in(to, l + (uint64_t)s * kBlockBytes, kBlockBytes, bar);
+                    if (one) continue;
                     if (MODE <= kPoly) copy_in(to + kBlockBytes, r + (uint64_t)s * kBlockBytes, half * 128, bar);
                     else                                         // 64 rows of X (half a block)
                         for (uint32_t q = 0; q < right_blocks; ++q)
@@ -544,10 +548,11 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                 const uint32_t slot = it % kStages, at = smem_of(smem) + slot * kStageBytes;
                 if (!(ok = bar_wait(full + 8 * slot, (it / kStages) & 1) && bar_wait(landed + 8 * slot, (it / kStages) & 1))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t right = one_of(t, tile, s < (MODE == kGram ? t.nb : t.kb) ? 0 : 1) ? 0 : kBlockBytes;
 #pragma unroll
                 for (uint32_t k = 0; k < 4; ++k) {               // 16 of the inner dimension: 32 bytes along a row, 16 rows of 128 bytes
                     const uint64_t l = operand(at + k * 32, 16, 1024);
-                    const uint64_t r = MODE <= kPoly ? operand(at + kBlockBytes + k * 32, 16, 1024) : operand(at + kBlockBytes + k * 2048, kBlockBytes / 2, 1024);
+                    const uint64_t r = MODE <= kPoly ? operand(at + right + k * 32, 16, 1024) : operand(at + kBlockBytes + k * 2048, kBlockBytes / 2, 1024);
                     multiply(sum, l, r, how, s || k);
                 }
                 commit_to_both(empty + 8 * slot);
