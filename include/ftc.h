@@ -574,7 +574,7 @@ typedef struct {
     uint32_t nesterov;           /* 1 or 0 */
     uint32_t products;           /* 16: the operands of products are rounded to float16 (of numbers up to 1.3, held times 2^14): the update X is
                                     good to about 1e-3 of its norm where the momentum is well conditioned. 32: operands are held as two
-                                    float16 numbers each, three products for one: 1e-6 */
+                                    float16 numbers each, three products for one: 1e-6, or 2e-5 where sums have thousands of terms */
     uint32_t reserved;           /* 0 */
 } ftc_muon_t;
 
@@ -591,7 +591,7 @@ typedef struct {
  *   d_workspace   ftc_muon_workspace_bytes(h_plan, products) bytes, 256-byte aligned; as for ftc_layernorm_backward
  * An element of a message that was not delivered keeps its momentum, which is its U; a matrix of which nothing was delivered (with n > 0) stays as it is.
  * A matrix that meets NaN or an infinity has NaN in its weights afterwards. d_workspace's first 32-bit word is 0 after the call; were a wait
- * inside a kernel ever to give up, it is not, and weights of the matrices concerned were left as they are.
+ * inside a kernel ever to give up, it is not, and no weights were changed.
  */
 FTC_API int ftc_muon_step(const ftc_muon_t* hyper, const void* h_plan, const void* d_plan, float* d_momentum, const float* d_grad_scale,
                           void* d_workspace, size_t workspace_bytes, void* cuda_stream);
