@@ -178,6 +178,7 @@ __global__ void __launch_bounds__(256) muon_norm_kernel(MuonArgs a) {
     if (threadIdx.x) return;
     for (int w = 1; w < 8; ++w) { sum += sums[w]; live += lives[w]; }
     a.live[blockIdx.x] = live > 0;
+    for (uint32_t k = 0; k < 3; ++k) a.written[k * a.n + blockIdx.x] = 0;
     a.factor[blockIdx.x] = (float)((double)kUp / (sqrt(sum) + (double)a.eps));
 }
 
@@ -354,6 +355,8 @@ __global__ void __launch_bounds__(256, 4) muon_update_kernel(MuonArgs a) {
 // half of the right one's columns, one thread of the first block issues the matrix instructions of both, and each block's tensor memory
 // gets its 128 rows of sums, 256 columns; there are two such halves, so that one tile is read out while the next is multiplied. A stage
 // holds 64 of the inner dimension: 16 KB of each operand in each block.
+// All products of all steps are one launch. A pair takes every so many-th tile of their list; a tile waits until the product before it of its own
+// matrix has been written, which with many matrices it long has been: no product's last tiles keep the GPU waiting, and none pays for a launch.
 //   warp 0   copies of its block's operands
 //   warp 1   first block: matrix instructions; second block: tells the first when its copies have landed
 //   warps 4 .. 11   read sums out (a warp reads the 32 lanes of tensor memory that its number modulo 4 gives it), the first four those of the
@@ -364,6 +367,7 @@ constexpr uint32_t kStages = 5, kStageBytes = 2 * kBlockBytes, kRows = kBlockByt
 constexpr uint32_t kProductSmem = kStages * kStageBytes + 16 * kRows + 1024 + 512;
 static_assert(kProductSmem <= 227 * 1024, "shared memory of a block");
 enum { kGram, kPoly, kApply };
+template <int M> struct Mode { static constexpr int value = M; };
 
 __device__ __forceinline__ uint32_t smem_of(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
@@ -419,13 +423,29 @@ __device__ __forceinline__ uint64_t operand(uint32_t address, uint32_t leading, 
     return (uint64_t)((address & 0x3FFFF) >> 4) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
 
-struct Tile { uint32_t which, i, j; };                           // matrix, blocks of 256 rows and of 256 columns
+struct Tile { uint32_t step, mode, which, i, j; };               // step, product, matrix, blocks of 256 rows and of 256 columns
 
-// Tiles on and below the diagonal: row i has i + 1.
-__device__ __forceinline__ Tile gram_tile(const MuonArgs& a, uint32_t u) {
+// Tile u of a call: step by step, gram, poly and apply of all matrices; of a symmetric product the tiles on and below the diagonal (row i has i + 1), of
+// the others a column's tiles one after the other: they share the right operand.
+__device__ __forceinline__ Tile tile_at(const MuonArgs& a, uint32_t u) {
     Tile t;
-    t.which = __ldg(a.maps[kGramTiles] + u);
-    const uint32_t r = u - plan_entries(a.plan)[t.which].first[kGramTiles];
+    const uint32_t gram = a.items[kGramTiles], all = 2 * gram + a.items[kApplyTiles];
+    t.step = u / all;
+    uint32_t r = u - t.step * all;
+    t.mode = r < gram ? kGram : r < 2 * gram ? kPoly : kApply;
+    if (t.mode == kApply) {
+        r -= 2 * gram;
+        t.which = __ldg(a.maps[kApplyTiles] + r);
+        const PlanEntry& e = plan_entries(a.plan)[t.which];
+        const uint32_t rows = (e.mb + 1) / 2;
+        r -= e.first[kApplyTiles];
+        t.j = r / rows;
+        t.i = r - t.j * rows;
+        return t;
+    }
+    if (t.mode == kPoly) r -= gram;
+    t.which = __ldg(a.maps[kGramTiles] + r);
+    r -= plan_entries(a.plan)[t.which].first[kGramTiles];
     uint32_t i = (uint32_t)((sqrtf(8.f * (float)r + 1.f) - 1.f) * 0.5f);
     while (i * (i + 1) / 2 > r) --i;
     while ((i + 1) * (i + 2) / 2 <= r) ++i;
@@ -433,21 +453,28 @@ __device__ __forceinline__ Tile gram_tile(const MuonArgs& a, uint32_t u) {
     t.j = r - i * (i + 1) / 2;
     return t;
 }
-// All tiles, a column's one after the other: they share the right operand.
-__device__ __forceinline__ Tile apply_tile(const MuonArgs& a, uint32_t u) {
-    Tile t;
-    t.which = __ldg(a.maps[kApplyTiles] + u);
-    const PlanEntry& e = plan_entries(a.plan)[t.which];
-    const uint32_t r = u - e.first[kApplyTiles], rows = (e.mb + 1) / 2;
-    t.j = r / rows;
-    t.i = r - t.j * rows;
-    return t;
+
+// What a tile reads is there once all tiles of its matrix's product before have been written: 16 warps count each of them.
+__device__ __forceinline__ bool wait_for_product(const MuonArgs& a, const Tile& q, const PlanEntry& t) {
+    const uint32_t rows = (t.mb + 1) / 2, gram = rows * (rows + 1) / 2, apply = rows * ((t.nb + 3) / 4);
+    const uint32_t target = q.mode == kGram ? q.step * apply * 16 : (q.step + 1) * gram * 16;
+    const uint32_t* const count = a.written + (q.mode == kGram ? 2 : q.mode - 1) * a.n + q.which;
+    for (uint32_t i = 0; i < 1u << 23; ++i) {
+        uint32_t now;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(now) : "l"(count) : "memory");
+        if (now >= target) {
+            asm volatile("fence.proxy.async;" ::: "memory");     // and for the copies that follow
+            return true;
+        }
+        __nanosleep(64);
+    }
+    return false;
 }
 
 __device__ __forceinline__ uint32_t half2_of(F2 v) { uint32_t r; asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi(v)), "f"(lo(v))); return r; }
 __device__ __forceinline__ F2 pair_of(uint32_t h) { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h)); return pair(f.x, f.y); }
 
-template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) muon_product_kernel(MuonArgs a, uint32_t tiles, uint32_t side) {
+template <bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1) muon_products_kernel(MuonArgs a) {
     namespace cg = cooperative_groups;
     extern __shared__ unsigned char raw[];
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -475,46 +502,46 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
     cg::this_cluster().sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = words[0], pairs = gridDim.x / 2, our_pair = blockIdx.x / 2;
-    wait_for_earlier_kernel();
-    later_kernel_may_start();
     const float scale = a.grad_scale ? *a.grad_scale : 1.f;
     const bool work = isfinite(scale) && *reinterpret_cast<volatile uint32_t*>(a.word) == 0;
     const PlanEntry* const entries = plan_entries(a.plan);
+    const uint32_t tiles = a.steps * (2 * a.items[kGramTiles] + a.items[kApplyTiles]);
     constexpr uint32_t segments = SPLIT ? 3 : 1;
-    auto tile_of = [&](uint32_t u) { return MODE <= kPoly ? gram_tile(a, u) : apply_tile(a, u); };
-    // a tile's steps of 64 and its columns: 256, or 128 where there are no more (in the apply kernels up to 64 of them are nobody's)
     // a tile on the diagonal: the left operand is the right one too
-    auto one_of = [&](const PlanEntry& t, const Tile& q, uint32_t g) { return MODE <= kPoly && g == 0 && q.i == q.j && t.mb > 2 * q.j + 1; };
-    auto steps_of = [&](const PlanEntry& t) { return segments * (MODE == kGram ? t.nb : t.kb); };
-    auto columns_of = [&](const PlanEntry& t, const Tile& q) { return MODE <= kPoly ? (t.mb > 2 * q.j + 1 ? 256u : 128u) : (t.nb > 4 * q.j + 2 ? 256u : 128u); };
-    const unsigned char* const x_in = a.x[side];
+    auto one_of = [&](const PlanEntry& t, const Tile& q, uint32_t g) { return q.mode <= kPoly && g == 0 && q.i == q.j && t.mb > 2 * q.j + 1; };
+    auto inner_of = [&](const PlanEntry& t, const Tile& q) { return q.mode == kGram ? t.nb : t.kb; };             // blocks of 64
+    // a tile's columns: 256, or 128 where there are no more (of an apply tile up to 64 of them are nobody's)
+    auto columns_of = [&](const PlanEntry& t, const Tile& q) { return (q.mode <= kPoly ? t.mb > 2 * q.j + 1 : t.nb > 4 * q.j + 2) ? 256u : 128u; };
     bool ok = true;
 
     if (work && warp == 0 && lane == 0) {                        // copies
         uint32_t it = 0;
         for (uint32_t u = our_pair; u < tiles && ok; u += pairs) {
-            const Tile tile = tile_of(u);
+            const Tile tile = tile_at(a, u);
             const PlanEntry t = entries[tile.which];
-            const uint32_t steps = MODE == kGram ? t.nb : t.kb, left_row = 2 * tile.i + rank, half = columns_of(t, tile) / 2;      // columns of this block
+            if (!(ok = wait_for_product(a, tile, t))) break;
+            const bool sym = tile.mode <= kPoly, gram = tile.mode == kGram;
+            const unsigned char* const x_in = a.x[tile.step & 1];
+            const uint32_t steps = inner_of(t, tile), left_row = 2 * tile.i + rank, half = columns_of(t, tile) / 2;      // columns of this block
             const bool has_left = left_row < t.mb;
             // right operand of a symmetric product: rows half * rank .. of 256; of the others: blocks of 64 columns
             const uint32_t right_row = 2 * tile.j + (half == 128 ? rank : 0), right_in = half == 128 ? 0 : rank * (kBlockBytes / 2);
-            const uint32_t right_block = 4 * tile.j + rank * (half / 64), right_blocks = MODE <= kPoly ? 0 : min(half / 64, t.nb > right_block ? t.nb - right_block : 0u);
+            const uint32_t right_block = 4 * tile.j + rank * (half / 64), right_blocks = sym ? 0 : min(half / 64, t.nb > right_block ? t.nb - right_block : 0u);
             for (uint32_t g = 0; g < segments && ok; ++g) {
                 const bool one = one_of(t, tile, g);
-                const uint32_t bytes = (has_left ? kBlockBytes : 0) + (one ? 0 : MODE <= kPoly ? half * 128 : right_blocks * (kBlockBytes / 2));
-                const unsigned char* l = (MODE == kGram ? x_in : MODE == kPoly ? a.a : a.b) + (g == 2 ? (MODE == kGram ? a.x_bytes : a.a_bytes) : 0);
-                const unsigned char* r = (MODE == kPoly ? a.a : x_in) + (g == 1 ? (MODE == kPoly ? a.a_bytes : a.x_bytes) : 0);
-                l += MODE == kGram ? (t.x_block + (uint64_t)left_row * t.nb) * kBlockBytes : (t.a_block + (uint64_t)left_row * 2 * t.mb) * kBlockBytes;
-                r += MODE == kGram ? (t.x_block + (uint64_t)right_row * t.nb) * kBlockBytes + right_in
-                   : MODE == kPoly ? (t.a_block + (uint64_t)right_row * 2 * t.mb) * kBlockBytes + right_in : (t.x_block + right_block) * kBlockBytes;
+                const uint32_t bytes = (has_left ? kBlockBytes : 0) + (one ? 0 : sym ? half * 128 : right_blocks * (kBlockBytes / 2));
+                const unsigned char* l = (gram ? x_in : (tile.mode == kPoly) ? a.a : a.b) + (g == 2 ? (gram ? a.x_bytes : a.a_bytes) : 0);
+                const unsigned char* r = ((tile.mode == kPoly) ? a.a : x_in) + (g == 1 ? ((tile.mode == kPoly) ? a.a_bytes : a.x_bytes) : 0);
+                l += gram ? (t.x_block + (uint64_t)left_row * t.nb) * kBlockBytes : (t.a_block + (uint64_t)left_row * 2 * t.mb) * kBlockBytes;
+                r += gram ? (t.x_block + (uint64_t)right_row * t.nb) * kBlockBytes + right_in
+                   : (tile.mode == kPoly) ? (t.a_block + (uint64_t)right_row * 2 * t.mb) * kBlockBytes + right_in : (t.x_block + right_block) * kBlockBytes;
                 for (uint32_t s = 0; s < steps; ++s, ++it) {
                     const uint32_t slot = it % kStages, to = smem_of(smem) + slot * kStageBytes, bar = full + 8 * slot;
                     if (it >= kStages && !(ok = bar_wait(empty + 8 * slot, (it / kStages - 1) & 1))) break;
                     bar_expect(bar, bytes);
                     if (has_left) copy_in(to, l + (uint64_t)s * kBlockBytes, kBlockBytes, bar);
                     if (one) continue;
-                    if (MODE <= kPoly) copy_in(to + kBlockBytes, r + (uint64_t)s * kBlockBytes, half * 128, bar);
+                    if (sym) copy_in(to + kBlockBytes, r + (uint64_t)s * kBlockBytes, half * 128, bar);
                     else                                         // 64 rows of X (half a block)
                         for (uint32_t q = 0; q < right_blocks; ++q)
                             copy_in(to + kBlockBytes + q * (kBlockBytes / 2), r + ((uint64_t)(s / 2) * t.nb + q) * kBlockBytes + s % 2 * (kBlockBytes / 2), kBlockBytes / 2, bar);
@@ -528,9 +555,9 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
     } else if (work && warp == 1 && lane == 0) {
         uint32_t it = 0, n = 0;
         for (uint32_t u = our_pair; u < tiles && ok; u += pairs, ++n) {
-            const Tile tile = tile_of(u);
+            const Tile tile = tile_at(a, u);
             const PlanEntry t = entries[tile.which];
-            const uint32_t steps = steps_of(t);
+            const uint32_t inner = inner_of(t, tile), steps = segments * inner;
             if (rank) {                                          // the second block's copies
                 for (uint32_t s = 0; s < steps; ++s, ++it) {
                     const uint32_t slot = it % kStages;
@@ -539,8 +566,10 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                 }
                 continue;
             }
+            const bool sym = tile.mode <= kPoly;
+            const uint32_t along = sym ? 32 : 2048, leading = sym ? 16 : kBlockBytes / 2;
             // sums in float32, operands float16, the right one along its columns in the apply kernels, 256 rows
-            const uint32_t how = 1u << 4 | (MODE >= kApply ? 1u << 16 : 0u) | columns_of(t, tile) / 8 << 17 | 256u / 16 << 24;
+            const uint32_t how = 1u << 4 | (!sym ? 1u << 16 : 0u) | columns_of(t, tile) / 8 << 17 | 256u / 16 << 24;
             const uint32_t sum = tmem + (n & 1) * 256;
             if (n >= 2 && !(ok = bar_wait(sum_empty + 8 * (n & 1), (n / 2 - 1) & 1))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -548,11 +577,10 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                 const uint32_t slot = it % kStages, at = smem_of(smem) + slot * kStageBytes;
                 if (!(ok = bar_wait(full + 8 * slot, (it / kStages) & 1) && bar_wait(landed + 8 * slot, (it / kStages) & 1))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t right = one_of(t, tile, s < (MODE == kGram ? t.nb : t.kb) ? 0 : 1) ? 0 : kBlockBytes;
+                const uint32_t right = at + (one_of(t, tile, s < inner ? 0 : 1) ? 0 : kBlockBytes);
 #pragma unroll
                 for (uint32_t k = 0; k < 4; ++k) {               // 16 of the inner dimension: 32 bytes along a row, 16 rows of 128 bytes
-                    const uint64_t l = operand(at + k * 32, 16, 1024);
-                    const uint64_t r = MODE <= kPoly ? operand(at + right + k * 32, 16, 1024) : operand(at + kBlockBytes + k * 2048, kBlockBytes / 2, 1024);
+                    const uint64_t l = operand(at + k * 32, 16, 1024), r = operand(right + k * along, leading, 1024);
                     multiply(sum, l, r, how, s || k);
                 }
                 commit_to_both(empty + 8 * slot);
@@ -573,15 +601,15 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
         unsigned char* const other = mine + kRows;
         const uint32_t ready = warp_full + 16 * (warp - 4);
         uint32_t n = 0, done[2] = {0, 0};                        // phases of the two barriers
-        for (uint32_t u = our_pair; u < tiles && ok; u += pairs, ++n) {
-            const Tile tile = tile_of(u);
-            const PlanEntry t = entries[tile.which];
+        // One tile's part of this warp, for each of the three products.
+        auto finish = [&](auto mode, const Tile& tile, const PlanEntry& t) {
+            constexpr int MODE = decltype(mode)::value;
             const uint32_t bi = 2 * tile.i + rank, i = bi * 128 + r;
             // blocks of 64 columns of this team: none above the diagonal, none beyond the edges
             const uint32_t cb0 = 4 * tile.j + 2 * team, edge = MODE <= kPoly ? 2 * min(t.mb, bi + 1) : t.nb;
             const uint32_t wanted = bi < t.mb && cb0 < edge ? min(2u, edge - cb0) : 0;
             const uint64_t row_at = (MODE <= kPoly ? t.a_block + (uint64_t)bi * 2 * t.mb : t.x_block + (uint64_t)bi * t.nb) * kBlockBytes + quarter * kRows;
-            unsigned char* const out = (MODE == kGram ? a.a : MODE == kPoly ? a.b : a.x[side ^ 1]) + row_at;
+            unsigned char* const out = (MODE == kGram ? a.a : MODE == kPoly ? a.b : a.x[tile.step & 1 ^ 1]) + row_at;
             const uint64_t low = MODE <= kPoly ? a.a_bytes : a.x_bytes;
             auto fetch = [&](uint32_t b, unsigned char* to, uint32_t bar) {              // A, by one lane
                 const unsigned char* from = a.a + row_at + (uint64_t)(cb0 + b) * kBlockBytes;
@@ -589,24 +617,24 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                 copy_in(smem_of(to), from, kRows, bar);
                 if (SPLIT) copy_in(smem_of(other), from + low, kRows, bar);
             };
-            if (!SPLIT && lane == 0 && wanted) {                 // what the last tile left in here has gone
-                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                if (MODE == kPoly) {
-                    fetch(0, mine, ready);
-                    if (wanted > 1) fetch(1, other, ready + 8);
-                }
+            if (MODE == kPoly && wanted && lane == 0) ok = wait_for_product(a, tile, t);
+            if (MODE == kPoly) ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
+            if (!ok) return;
+            if (!SPLIT && MODE == kPoly && lane == 0 && wanted) {
+                fetch(0, mine, ready);
+                if (wanted > 1) fetch(1, other, ready + 8);
             }
             for (uint32_t b = 0; b < max(wanted, 1u) && ok; ++b) {
                 const uint32_t cb = cb0 + b, j0 = cb * 64, which = SPLIT ? 0 : b;
                 unsigned char* const here = which ? other : mine;
-                if (SPLIT && wanted && lane == 0) {
+                if (SPLIT && wanted && lane == 0) {              // what the last block left in here has gone
                     asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     if (MODE == kPoly) fetch(b, mine, ready);
                 }
                 ok = (b || bar_wait(sum_full + 8 * (n & 1), (n / 2) & 1)) && (!wanted || MODE != kPoly || bar_wait(ready + 8 * which, done[which] & 1));
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok || !wanted) break;
-                ++done[which];
+                if (MODE == kPoly) ++done[which];
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 F2 v[32];
                 read_64(v, tmem + (n & 1) * 256 + (quarter * 32 << 16) + team * 128 + b * 64);
@@ -628,7 +656,7 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                     for (int q = 0; q < 32; ++q) v[q] = mul(v[q], twice(kDown));
                 } else {
                     const float* d = a.diag_a + t.diagonal;
-                    const float di = d[i];
+                    const float di = __ldcg(d + i);
                     const F2 keep = twice(fmaf(kQ5, di, kQ3));
                     mine_own = (kQ1 + fmaf(kQ5, fmaf(di, di, mine_own), kQ3 * di)) * kUp;
 #pragma unroll
@@ -639,7 +667,7 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                             const uint4 l = *reinterpret_cast<const uint4*>(other + piece(lane, c));
                             e[0] = add(e[0], pair_of(l.x)); e[1] = add(e[1], pair_of(l.y)); e[2] = add(e[2], pair_of(l.z)); e[3] = add(e[3], pair_of(l.w));
                         }
-                        const float4 d0 = *reinterpret_cast<const float4*>(d + j0 + 8 * c), d1 = *reinterpret_cast<const float4*>(d + j0 + 8 * c + 4);
+                        const float4 d0 = __ldcg(reinterpret_cast<const float4*>(d + j0 + 8 * c)), d1 = __ldcg(reinterpret_cast<const float4*>(d + j0 + 8 * c + 4));
                         const F2 dj[4] = {pair(d0.x, d0.y), pair(d0.z, d0.w), pair(d1.x, d1.y), pair(d1.z, d1.w)};
 #pragma unroll
                         for (uint32_t q = 0; q < 4; ++q) v[4 * c + q] = fma(v[4 * c + q], twice(kQ5 * kDown), mul(e[q], fma(dj[q], twice(kQ5), keep)));
@@ -681,11 +709,25 @@ template <int MODE, bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __laun
                     }
                 }
             }
-            if (ok) {                                            // the first block multiplies for both
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) bar_arrive_at(sum_empty + 8 * (n & 1), 0);
+            if (!ok) return;
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            if (MODE <= kPoly) asm volatile("fence.proxy.async;" ::: "memory");          // the transpose is read by copies
+            __syncwarp();
+            if (lane == 0) {
+                bar_arrive_at(sum_empty + 8 * (n & 1), 0);       // the first block multiplies for both
+                // all that this warp wrote is in place: the stores of its lanes before the barrier above, the copies after this wait
+                asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+                asm volatile("fence.acq_rel.gpu;" ::: "memory");
+                asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(a.written + MODE * a.n + tile.which) : "memory");
             }
+            __syncwarp();
+        };
+        for (uint32_t u = our_pair; u < tiles && ok; u += pairs, ++n) {
+            const Tile tile = tile_at(a, u);
+            const PlanEntry t = entries[tile.which];
+            if (tile.mode == kGram) finish(Mode<kGram>(), tile, t);
+            else if (tile.mode == kPoly) finish(Mode<kPoly>(), tile, t);
+            else finish(Mode<kApply>(), tile, t);
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
         if (!ok && lane == 0) {
@@ -880,27 +922,22 @@ template <bool SPLIT> static cudaError_t small(const MuonArgs& a, int sms, cudaS
     return cudaLaunchKernelEx(&how, muon_small_kernel<SPLIT>, a);
 }
 
-template <int MODE, bool SPLIT> static cudaError_t product(const MuonArgs& a, uint32_t tiles, uint32_t side, int sms, cudaStream_t st) {
-    cudaError_t e = cudaFuncSetAttribute(muon_product_kernel<MODE, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
+// All steps' products in one cooperative launch: as many pairs as the GPU holds at once, since tiles wait for those of other pairs.
+template <bool SPLIT> static cudaError_t products(const MuonArgs& a, cudaStream_t st) {
+    cudaError_t e = cudaFuncSetAttribute(muon_products_kernel<SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
     if (e != cudaSuccess) return e;
-    cudaLaunchAttribute early{};
-    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchAttribute how_at_once{};
+    how_at_once.id = cudaLaunchAttributeCooperative;
+    how_at_once.val.cooperative = 1;
     cudaLaunchConfig_t how{};
-    const uint32_t most = (uint32_t)sms / 2;
-    how.gridDim = dim3(2 * (tiles < most ? tiles : most)); how.blockDim = dim3(kProductThreads); how.dynamicSmemBytes = kProductSmem;
-    how.stream = st; how.attrs = &early; how.numAttrs = 1;
-    return cudaLaunchKernelEx(&how, muon_product_kernel<MODE, SPLIT>, a, tiles, side);
-}
-
-template <bool SPLIT> static cudaError_t products(const MuonArgs& a, int sms, cudaStream_t st) {
-    cudaError_t e = cudaSuccess;
-    for (uint32_t s = 0; s < a.steps && e == cudaSuccess; ++s) {
-        e = product<kGram, SPLIT>(a, a.items[kGramTiles], s & 1, sms, st);
-        if (e == cudaSuccess) e = product<kPoly, SPLIT>(a, a.items[kGramTiles], s & 1, sms, st);
-        if (e == cudaSuccess) e = product<kApply, SPLIT>(a, a.items[kApplyTiles], s & 1, sms, st);
-    }
-    return e;
+    how.gridDim = dim3(2); how.blockDim = dim3(kProductThreads); how.dynamicSmemBytes = kProductSmem; how.stream = st;
+    int most = 0;
+    if ((e = cudaOccupancyMaxActiveClusters(&most, muon_products_kernel<SPLIT>, &how)) != cudaSuccess) return e;
+    const uint32_t busiest = a.items[kGramTiles] > a.items[kApplyTiles] ? a.items[kGramTiles] : a.items[kApplyTiles];      // no more pairs than a product has tiles
+    if (most < 1) return cudaErrorInvalidConfiguration;
+    how.gridDim = dim3(2 * (busiest < (uint32_t)most ? busiest : (uint32_t)most));
+    how.attrs = &how_at_once; how.numAttrs = 1;
+    return cudaLaunchKernelEx(&how, muon_products_kernel<SPLIT>, a);
 }
 
 cudaError_t launch_muon(const MuonArgs& a, int sms, cudaStream_t st) {
@@ -909,7 +946,7 @@ cudaError_t launch_muon(const MuonArgs& a, int sms, cudaStream_t st) {
     if (e == cudaSuccess) e = launch_second(muon_norm_kernel, a.n, 256, st, a);
     if (e == cudaSuccess) e = launch_second(muon_layout_kernel, a.items[kBlocks], 256, st, a);
     if (e == cudaSuccess && a.items[kSmall]) e = a.split ? small<true>(a, sms, st) : small<false>(a, sms, st);
-    if (e == cudaSuccess && a.items[kGramTiles]) e = a.split ? products<true>(a, sms, st) : products<false>(a, sms, st);
+    if (e == cudaSuccess && a.items[kGramTiles]) e = a.split ? products<true>(a, st) : products<false>(a, st);
     if (e == cudaSuccess) e = launch_second(muon_update_kernel, a.items[kBlocks], 256, st, a);
     return e;
 }
