@@ -46,9 +46,9 @@ __device__ __forceinline__ int32_t token_at(const void* tokens, uint32_t bits, u
 constexpr uint64_t kPlanMagic = 0x316E4C5054435446ull;
 constexpr uint32_t kMuonChunk = 4096;                            // elements of a block of the momentum kernel
 enum { kChunks, kBlocks, kGramTiles, kApplyTiles, kSmall, kLists };    // kSmall: matrices that one block takes through all steps
-// A matrix of at most 128 x 256.
-__host__ __device__ inline bool plan_small(uint64_t m, uint64_t w) { return m <= 128 && w <= 256; }
-struct PlanHead { uint64_t magic, n_blocks, a_blocks, diagonals; uint32_t items[kLists], n, pad[2]; };
+// Matrices of at most 128 x 256 are small; of at most 128 x 512 where operands are one number each. The latter come last in the lists.
+inline uint32_t plan_size(uint64_t m, uint64_t w) { return m <= 128 && w <= 256 ? 0 : m <= 128 && w <= 512 ? 1 : 2; }
+struct PlanHead { uint64_t magic, n_blocks, a_blocks, diagonals; uint32_t items[kLists], n, middle, gram_middle, apply_middle, pad; };     // ..middle: matrices and tiles of size 1, the lists' last
 struct PlanEntry {
     void* param; float* master; const void* grad; const uint32_t* status;
     uint64_t n, first_block, x_block, a_block, diagonal;         // x_block, a_block: in blocks of 128 x 64 float16; diagonal: in numbers
@@ -59,7 +59,7 @@ struct PlanEntry {
     uint32_t first[kLists];                                      // where its chunks, blocks, tiles begin
     uint32_t pad;
 };
-static_assert(sizeof(PlanHead) == 64 && sizeof(PlanEntry) == 144, "plan layout");
+static_assert(sizeof(PlanHead) == 72 && sizeof(PlanEntry) == 144, "plan layout");
 __host__ __device__ inline const PlanEntry* plan_entries(const void* p) {
     return reinterpret_cast<const PlanEntry*>(static_cast<const char*>(p) + sizeof(PlanHead));
 }

@@ -64,8 +64,10 @@ bool count_matrices(const ftc_matrix_t* q, uint32_t n, PlanHead& h) {
         h.n_blocks += (t.n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK;
         blocks += mb * nb; h.a_blocks += mb * 2 * mb; h.diagonals += mb * 128;
         chunks += (t.n + kMuonChunk - 1) / kMuonChunk;
-        if (plan_small(m, w)) ++h.items[kSmall];
-        else { gram += mb2 * (mb2 + 1) / 2; apply += mb2 * ((nb + 3) / 4); }
+        const uint32_t size = plan_size(m, w);
+        if (size < 2) ++h.items[kSmall];
+        if (size > 0) { gram += mb2 * (mb2 + 1) / 2; apply += mb2 * ((nb + 3) / 4); }
+        if (size == 1) { ++h.middle; h.gram_middle += (uint32_t)(mb2 * (mb2 + 1) / 2); h.apply_middle += (uint32_t)(mb2 * ((nb + 3) / 4)); }
         if (h.n_blocks > (1ull << 32) || blocks > 0x7FFFFFFFull || h.a_blocks > 0x7FFFFFFFull || chunks > 0x7FFFFFFFull || 16 * (2 * gram + apply) > 0x7FFFFFFFull) return false;   // tiles of 16 steps
     }
     h.items[kChunks] = (uint32_t)chunks; h.items[kBlocks] = (uint32_t)blocks; h.items[kGramTiles] = (uint32_t)gram; h.items[kApplyTiles] = (uint32_t)apply;
@@ -190,19 +192,24 @@ int ftc_muon_plan_build(const ftc_matrix_t* h_matrices, uint32_t n, void* h_plan
         blocks += (t.n + FTC_STATE_BLOCK - 1) / FTC_STATE_BLOCK; x += (uint64_t)q.mb * q.nb; a += (uint64_t)q.mb * 2 * q.mb; diagonal += q.mb * 128;
         q.wide = aligned(t.grad, 16) && aligned(t.param, 16) && aligned(t.master, 16);
     }
-    // The maps. Tiles of many steps come first, so that the last ones to run are short.
+    // The maps.
     uint32_t* map = reinterpret_cast<uint32_t*>(e + n);
     uint32_t* const order = map + h.items[kChunks] + h.items[kBlocks] + h.items[kGramTiles] + h.items[kApplyTiles] + h.items[kSmall];      // room for the sorting
     for (uint32_t i = 0; i < n; ++i) order[i] = i;
     for (int w = 0; w < kLists; ++w) {
-        if (w == kGramTiles) std::sort(order, order + n, [e](uint32_t i, uint32_t j) { return e[i].nb != e[j].nb ? e[i].nb > e[j].nb : i < j; });
-        if (w == kApplyTiles) std::sort(order, order + n, [e](uint32_t i, uint32_t j) { return e[i].kb != e[j].kb ? e[i].kb > e[j].kb : i < j; });
+        // chunks and blocks as the caller has them; tiles and small matrices: middle sizes last, those of many steps first
+        if (w >= kGramTiles)
+            std::sort(order, order + n, [e, w](uint32_t i, uint32_t j) {
+                const bool late = plan_size(e[i].m, e[i].w) == 1, late_j = plan_size(e[j].m, e[j].w) == 1;
+                const uint32_t s = w == kGramTiles ? e[i].nb : e[i].kb, s_j = w == kGramTiles ? e[j].nb : e[j].kb;
+                return late != late_j ? late_j : s != s_j ? s > s_j : i < j;
+            });
         uint32_t at = 0;
         for (uint32_t o = 0; o < n; ++o) {
             const uint32_t i = order[o];
             PlanEntry& q = e[i];
             const uint32_t mb2 = (q.mb + 1) / 2;
-            const uint32_t count = w == kChunks ? (uint32_t)((q.n + kMuonChunk - 1) / kMuonChunk) : w == kBlocks ? q.mb * q.nb : w == kSmall ? plan_small(q.m, q.w) : plan_small(q.m, q.w) ? 0 : w == kGramTiles ? mb2 * (mb2 + 1) / 2 : mb2 * ((q.nb + 3) / 4);
+            const uint32_t count = w == kChunks ? (uint32_t)((q.n + kMuonChunk - 1) / kMuonChunk) : w == kBlocks ? q.mb * q.nb : w == kSmall ? plan_size(q.m, q.w) < 2 : plan_size(q.m, q.w) == 0 ? 0 : w == kGramTiles ? mb2 * (mb2 + 1) / 2 : mb2 * ((q.nb + 3) / 4);
             q.first[w] = at;
             for (const uint32_t end = at + count; at < end; ++at) map[at] = i;
         }
@@ -242,6 +249,8 @@ int ftc_muon_step(const ftc_muon_t* hyper, const void* h_plan, const void* d_pla
     a.x[0] = ws + l.x0; a.x[1] = ws + l.x1; a.a = ws + l.a; a.b = ws + l.b; a.x_bytes = l.x_bytes; a.a_bytes = l.a_bytes;
     const uint32_t* map = reinterpret_cast<const uint32_t*>(plan_entries(d_plan) + h->n);
     for (int w = 0; w < kLists; ++w) { a.items[w] = h->items[w]; a.maps[w] = map; map += h->items[w]; }
+    if (hyper->products == 16) { a.items[kGramTiles] -= h->gram_middle; a.items[kApplyTiles] -= h->apply_middle; }
+    else a.items[kSmall] -= h->middle;
     a.steps = hyper->steps; a.nesterov = hyper->nesterov; a.split = hyper->products == 32;
     a.lr = (float)hyper->lr; a.mu = (float)hyper->momentum; a.eps = (float)hyper->eps;
     return status(launch_muon(a, sms, static_cast<cudaStream_t>(cuda_stream)));

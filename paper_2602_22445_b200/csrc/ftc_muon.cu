@@ -745,12 +745,12 @@ template <bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
 
 // ---- small matrices ----
 //
-// A matrix of at most 128 x 256 (either way) goes through all its steps in one block's shared memory: X (64 KB, twice that with `split`) and A,
+// A matrix of at most 128 x 512 (128 x 256 with `split`; either way) goes through all its steps in one block's shared memory: X (up to 128 KB) and A,
 // which B replaces, each product's sum in tensor memory, read out by eight warps. A chain of launches costs 10 us a product at any size (12 matrices
 // of 64 x 64 and 64 x 256: 164 us a call in all, so 49).
 
-constexpr uint32_t kSmallThreads = 256, kSmallColumns = 4;                       // columns in blocks of 64
-constexpr uint32_t kSmallSmem = 2 * (kSmallColumns + 2) * kBlockBytes + 1024 + 1024;
+constexpr uint32_t kSmallThreads = 256, kSmallBlocks = 8;                        // X's
+constexpr uint32_t kSmallSmem = (kSmallBlocks + 4) * kBlockBytes + 1024 + 1024;
 
 __device__ __forceinline__ void multiply_alone(uint32_t d, uint64_t a, uint64_t b, uint32_t how, bool add) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
@@ -761,8 +761,8 @@ template <bool SPLIT> __global__ void __launch_bounds__(kSmallThreads, 1) muon_s
     extern __shared__ unsigned char raw[];
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, quarter = warp & 3, half = warp >> 2, r = quarter * 32 + lane;
     unsigned char* const x = raw + (1024 - (smem_of(raw) & 1023)) % 1024;        // X's blocks, its low numbers', A's, its low numbers'
-    constexpr uint32_t kLowX = kSmallColumns * kBlockBytes, kLowA = 2 * kBlockBytes;
-    unsigned char* const m = x + 2 * kLowX;
+    constexpr uint32_t kLowX = kSmallBlocks / 2 * kBlockBytes, kLowA = 2 * kBlockBytes;
+    unsigned char* const m = x + kSmallBlocks * kBlockBytes;
     float* const diag = reinterpret_cast<float*>(m + 2 * kLowA);                 // 128
     const uint32_t bar = smem_of(diag + 128);                                    // copies; products
     uint32_t* const words = reinterpret_cast<uint32_t*>(diag + 132);
@@ -771,7 +771,7 @@ template <bool SPLIT> __global__ void __launch_bounds__(kSmallThreads, 1) muon_s
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 256;" ::"r"(smem_of(words)) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_of(words)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -787,15 +787,17 @@ template <bool SPLIT> __global__ void __launch_bounds__(kSmallThreads, 1) muon_s
     // The block's products of `steps` blocks of 64 of the inner dimension; everybody waits for them.
     auto product = [&](const unsigned char* left, uint32_t left_low, const unsigned char* right, uint32_t right_low, uint32_t steps, uint32_t columns, bool along) {
         if (threadIdx.x == 0) {
-            const uint32_t how = 1u << 4 | (along ? 1u << 16 : 0u) | columns / 8 << 17 | 128u / 16 << 24;
-            for (uint32_t g = 0; g < (SPLIT ? 3 : 1); ++g)
-                for (uint32_t s = 0; s < steps; ++s)
+            for (uint32_t c = 0; c < columns; c += 256) {        // right operands of at most 256 columns
+                const uint32_t how = 1u << 4 | (along ? 1u << 16 : 0u) | min(256u, columns - c) / 8 << 17 | 128u / 16 << 24;
+                for (uint32_t g = 0; g < (SPLIT ? 3 : 1); ++g)
+                    for (uint32_t s = 0; s < steps; ++s)
 #pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k) {
-                        const uint32_t l = smem_of(left) + (g == 2 ? left_low : 0) + s * kBlockBytes + k * 32, q = smem_of(right) + (g == 1 ? right_low : 0);
-                        multiply_alone(tmem, operand(l, 16, 1024), along ? operand(q + s * (kBlockBytes / 2) + k * 2048, kBlockBytes, 1024) : operand(q + s * kBlockBytes + k * 32, 16, 1024),
-                                       how, g || s || k);
-                    }
+                        for (uint32_t k = 0; k < 4; ++k) {
+                            const uint32_t l = smem_of(left) + (g == 2 ? left_low : 0) + s * kBlockBytes + k * 32, q = smem_of(right) + (g == 1 ? right_low : 0) + c / 64 * kBlockBytes;
+                            multiply_alone(tmem + c, operand(l, 16, 1024), along ? operand(q + s * (kBlockBytes / 2) + k * 2048, kBlockBytes, 1024) : operand(q + s * kBlockBytes + k * 32, 16, 1024),
+                                           how, g || s || k);
+                        }
+            }
             asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar + 8) : "memory");
         }
         __syncwarp();
@@ -907,7 +909,7 @@ template <bool SPLIT> __global__ void __launch_bounds__(kSmallThreads, 1) muon_s
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 256;" ::"r"(tmem) : "memory");
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
 template <bool SPLIT> static cudaError_t small(const MuonArgs& a, int sms, cudaStream_t st) {

@@ -75,7 +75,8 @@ def check(matrices, views, products, lr=0.1, scale=1.0, steps=5, nesterov=True):
             assert l * off < 0.5 * np.linalg.norm(l * x)          # the bound says something
 
 
-SHAPES = [(1, 1), (1, 7), (9, 1), (8, 8), (16, 64), (64, 16), (63, 65), (100, 130), (128, 128), (129, 127), (130, 300), (256, 256), (300, 70), (257, 513), (640, 200)]
+SHAPES = [(1, 1), (1, 7), (9, 1), (8, 8), (16, 64), (64, 16), (63, 65), (100, 130), (128, 128), (129, 127), (130, 300), (256, 256), (300, 70), (257, 513), (640, 200),
+          (100, 256), (128, 257), (512, 90), (70, 449), (128, 512), (128, 513), (513, 128)]
 
 
 @pytest.mark.parametrize("products", [16, 32])
@@ -92,7 +93,7 @@ def test_one_matrix(products, rows, cols):
 @pytest.mark.parametrize("g,k,lost", [("bfloat16", 0, 0), ("float16", 0, 0), ("float32", 32, 0.05), ("float32", 7, 0.3), ("float32", 1, 0.1)])
 def test_many(products, p, master, g, k, lost):
     rng = np.random.default_rng(k + 5)
-    made = [make(rng, r, c, p, g, master, k, lost, lr_scale=s, decay=0.05) for r, c, s in ((70, 50, 1.0), (33, 200, 0.5), (128, 384, 2.0), (5, 3, 1.0), (200, 131, 1.0))]
+    made = [make(rng, r, c, p, g, master, k, lost, lr_scale=s, decay=0.05) for r, c, s in ((70, 50, 1.0), (33, 200, 0.5), (128, 384, 2.0), (5, 3, 1.0), (200, 131, 1.0), (310, 90, 1.0))]
     entries, matrices = [m[0] for m in made], [m[1] for m in made]
     _, views = step(entries, matrices, products, scale=0.5)
     check(matrices, views, products, scale=0.5)
