@@ -46,7 +46,7 @@ def test_forward(x, w, n, V, H, pad, bits):
 
 CASES = [  # n, V, H, P, k, kind
     (1, 1, 1, 1, 1, "all"), (1, 300, 8, 1, 8, "all"), (31, 5, 256, 1, 256, "some"), (32, 5, 256, 4, 32, "some"), (33, 5, 256, 4, 32, "some"),
-    (700, 3, 40, 3, 8, "one"), (2500, 300, 24, 7, 4, "some"), (2500, 70000, 8, 1, 8, "some"), (900, 20, 301, 5, 7, "one"), (64, 1000, 33, 64, 5, "some"),
+    (700, 3, 40, 3, 8, "one"), (2500, 300, 24, 7, 4, "some"), (2500, 70000, 8, 1, 8, "some"), (900, 20, 301, 5, 7, "one"), (64, 1000, 33, 64, 5, "some"), (1025, 40, 72, 1, 8, "some"), (2048, 30, 40, 3, 8, "one"), (2049, 30, 40, 3, 8, "one"), (2047, 700, 37, 2, 5, "some"),
     (4096, 257, 16, 2, 16, "some"), (4097, 256, 16, 2, 16, "one"), (9001, 255, 520, 1, 520, "one"), (300, 65, 1032, 2, 12, "one"), (50, 17, 13, 3, 1000, "some"),
     (40000, 400, 8, 6, 4, "one"),
 ]
