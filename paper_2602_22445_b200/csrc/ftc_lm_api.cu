@@ -156,6 +156,7 @@ int ftc_token_logprobs_backward(const ftc_logprob_t* desc, uint64_t rows, const 
     if (rc != FTC_OK || rows == 0) return rc;
     if (!d_logits || !d_dlogits || !d_lse || stride < desc->V || dstride < desc->V || stride > kFar || dstride > kFar || (d_dlogprob && !d_tokens) || (d_dentropy && !d_entropy))
         return FTC_EINVAL;
+    if (d_logits == d_dlogits && stride != dstride) return FTC_EINVAL;
     const uint32_t e = size_of(desc->dtype);
     if (!aligned(d_logits, e) || !aligned(d_dlogits, e) || !aligned(d_tokens, desc->token_bits / 8) || !aligned(d_lse, 4) || !aligned(d_entropy, 4) || !aligned(d_dlogprob, 4) ||
         !aligned(d_dentropy, 4)) return FTC_EINVAL;

@@ -436,8 +436,8 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
         }
     }
     if (!TOP) return;
-    // fewer logits above -infinity than were asked for: the lowest tokens of the others
-    uint32_t have = __popc(__ballot_sync(kNone, best.best != 0));
+    // fewer logits above -infinity than were asked for: the lowest tokens of the others (of a row with NaN or infinity nothing is looked for)
+    uint32_t have = bad ? a.top : __popc(__ballot_sync(kNone, best.best != 0));
     for (uint32_t i0 = 0; i0 < a.V && have < a.top; i0 += 32) {
         uint32_t more = __ballot_sync(kNone, i0 + lane < a.V && to_f32(x[min(i0 + lane, a.V - 1)]) == -INFINITY);
         while (more && have < a.top) {

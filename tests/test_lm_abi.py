@@ -61,7 +61,7 @@ def logp_forward(d, rows=4, x=FAKE, xs=64, tokens=FAKE, out=FAKE, entropy=FAKE, 
     return B.load().ftc_token_logprobs(C.byref(d) if d else None, rows, x, xs, tokens, out, entropy, lse, tv, ti, None)
 
 
-def logp_backward(d, rows=4, x=FAKE, xs=64, tokens=FAKE, lse=FAKE, entropy=FAKE, up=FAKE, de=FAKE, dx=FAKE, ds=64):
+def logp_backward(d, rows=4, x=FAKE, xs=64, tokens=FAKE, lse=FAKE, entropy=FAKE, up=FAKE, de=FAKE, dx=2 * FAKE, ds=64):
     return B.load().ftc_token_logprobs_backward(C.byref(d) if d else None, rows, x, xs, tokens, lse, entropy, up, de, dx, ds, None)
 
 
@@ -83,6 +83,7 @@ def test_logprob_arguments_refused():
     for bad in (dict(x=None), dict(dx=None), dict(lse=None), dict(xs=49), dict(ds=49), dict(tokens=None), dict(entropy=None), dict(dx=FAKE + 1), dict(up=FAKE + 2), dict(de=FAKE + 2),
                 dict(lse=FAKE + 1)):
         assert logp_backward(d, **bad) == B.FTC_EINVAL, bad
+    assert logp_backward(d, dx=FAKE, ds=65) == B.FTC_EINVAL                                  # in place, rows elsewhere
     assert logp_forward(d, rows=0, x=None) == B.FTC_OK and logp_backward(d, rows=0, x=None) == B.FTC_OK
     assert logp_forward(d, tokens=None, out=None, entropy=None, lse=None) == B.FTC_OK        # nothing asked for
 
