@@ -185,8 +185,14 @@ __global__ void __launch_bounds__(256) muon_norm_kernel(MuonArgs a) {
 // Where the 16-byte piece c of row r lies in a block.
 __device__ __forceinline__ uint32_t piece(uint32_t r, uint32_t c) { return r * 128 + ((c ^ (r & 7)) << 4); }
 
+// A transposed block is turned in shared memory as float32, 64 lines of 128 with a gap of 4 behind each and behind every eighth: whole lines are
+// written and read by neighbouring threads in 16 bytes each, columns by neighbouring threads in neighbouring words or eight lines apart.
+constexpr uint32_t kTurnBytes = (64 * 132 + 32) * 4;
+__device__ __forceinline__ uint32_t turn_line(uint32_t line) { return line * 132 + line / 8 * 4; }
+static_assert(kTurnBytes >= 2 * kBlockBytes, "a block's two numbers take the same memory");
+
 // One block of 128 x 64 of X. Elements that are neighbours in memory are loaded by one thread (eight, where the addresses allow it) or by
-// neighbouring threads; a block whose matrix is transposed is turned in shared memory.
+// neighbouring threads; a block whose matrix is transposed is turned in shared memory (24 of 4096 x 1024: 233 us when threads took a line each, 160 so).
 __global__ void __launch_bounds__(256, 4) muon_layout_kernel(MuonArgs a) {
     wait_for_earlier_kernel();
     later_kernel_may_start();
@@ -197,18 +203,26 @@ __global__ void __launch_bounds__(256, 4) muon_layout_kernel(MuonArgs a) {
     const uint32_t at = blockIdx.x - t.first[kBlocks], bi = at / t.nb, bj = at - bi * t.nb;
     const float inv = a.factor[which];
     const float* m = a.momentum + t.first_block * FTC_STATE_BLOCK;
-    __shared__ __align__(16) unsigned char tile[2][kBlockBytes];
+    __shared__ __align__(16) unsigned char room[kTurnBytes];
     unsigned char* const out = a.x[0] + (t.x_block + at) * kBlockBytes;
     auto value = [&](float v, float g, float s) { return (a.nesterov && s > 0.f ? fmaf(v, a.mu, g * s * scale) : v) * inv; };
     auto put = [&](uint32_t r, uint32_t c, float v) {
         const __half h = __float2half_rn(v);
         const uint32_t to = piece(r, c / 8) + c % 8 * 2;
-        *reinterpret_cast<__half*>(tile[0] + to) = h;
-        if (a.split) *reinterpret_cast<__half*>(tile[1] + to) = __float2half_rn(v - __half2float(h));
+        *reinterpret_cast<__half*>(room + to) = h;
+        if (a.split) *reinterpret_cast<__half*>(room + kBlockBytes + to) = __float2half_rn(v - __half2float(h));
+    };
+    auto put_eight = [&](unsigned char* to, uint64_t low, float* x) {
+        store_eight(to, FTC_F16, 0, x);
+        if (a.split) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] -= __half2float(__float2half_rn(x[j]));
+            store_eight(to + low, FTC_F16, 0, x);
+        }
     };
     if (bi * 128 + 128 <= t.m && bj * 64 + 64 <= t.w && t.wide && t.cols % 8 == 0) {
-        // runs of 64 neighbours in 128 rows of memory: pieces as they are; or of 128 in 64 (transposed): neighbouring threads have neighbouring
-        // lines, so that they write neighbours in shared memory
+        // runs of 64 neighbours in 128 lines of memory, or of 128 in 64 (transposed)
+        float* const turn = reinterpret_cast<float*>(room);
 #pragma unroll
         for (uint32_t u = 0; u < 2; ++u) {
             float v[2][8], g[2][8], s[2][8];
@@ -216,32 +230,32 @@ __global__ void __launch_bounds__(256, 4) muon_layout_kernel(MuonArgs a) {
 #pragma unroll
             for (uint32_t w = 0; w < 2; ++w) {
                 const uint32_t e = threadIdx.x + (2 * u + w) * 256;
-                line[w] = t.tall ? threadIdx.x % 64 : e / 8;
-                run[w] = t.tall ? (threadIdx.x / 64 * 4 + 2 * u + w) * 8 : e % 8 * 8;
+                line[w] = t.tall ? e / 16 : e / 8;
+                run[w] = t.tall ? e % 16 * 8 : e % 8 * 8;
                 const uint64_t q = t.tall ? (uint64_t)(bj * 64 + line[w]) * t.cols + bi * 128 + run[w] : (uint64_t)(bi * 128 + line[w]) * t.cols + bj * 64 + run[w];
                 eight(v[w], m, FTC_F32, q);
                 if (a.nesterov) { eight(g[w], t.grad, t.grad_dtype, q); eight_shares(s[w], t, q); }
             }
 #pragma unroll
             for (uint32_t w = 0; w < 2; ++w) {
-                if (t.tall) {
+                float x[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) put(run[w] + j, line[w], value(v[w][j], g[w][j], s[w][j]));
-                } else {
-                    float x[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = value(v[w][j], g[w][j], s[w][j]);
-                    const uint32_t to = piece(line[w], run[w] / 8);
-                    store_eight(out + to, FTC_F16, 0, x);
-                    if (a.split) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) x[j] -= __half2float(__float2half_rn(x[j]));
-                        store_eight(out + a.x_bytes + to, FTC_F16, 0, x);
-                    }
-                }
+                for (int j = 0; j < 8; ++j) x[j] = value(v[w][j], g[w][j], s[w][j]);
+                if (t.tall) store_eight(turn + turn_line(line[w]) + run[w], FTC_F32, 0, x);
+                else put_eight(out + piece(line[w], run[w] / 8), a.x_bytes, x);
             }
         }
         if (!t.tall) return;
+        float x[4][8];
+        const uint32_t r = threadIdx.x % 128, c0 = threadIdx.x / 128;
+        __syncthreads();
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u)
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) x[u][j] = turn[turn_line((c0 + 2 * u) * 8 + j) + r];
+        __syncthreads();
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) put_eight(room + piece(r, c0 + 2 * u), kBlockBytes, x[u]);
     } else {
         for (uint32_t e0 = threadIdx.x; e0 < 128 * 64; e0 += 2048) {
             float v[8], g[8] = {}, s[8] = {};
@@ -261,7 +275,7 @@ __global__ void __launch_bounds__(256, 4) muon_layout_kernel(MuonArgs a) {
     __syncthreads();
     for (uint32_t s = 0; s <= a.split; ++s) {
         uint4* to = reinterpret_cast<uint4*>(out + s * a.x_bytes);
-        const uint4* from = reinterpret_cast<const uint4*>(tile[s]);
+        const uint4* from = reinterpret_cast<const uint4*>(room + s * kBlockBytes);
         for (uint32_t e = threadIdx.x; e < kBlockBytes / 16; e += 256) to[e] = from[e];
     }
 }
@@ -278,7 +292,7 @@ __global__ void __launch_bounds__(256, 4) muon_update_kernel(MuonArgs a) {
     const float l = a.lr * t.lr_scale, down = 1.f - l * t.weight_decay, move = -l * kDown;
     void* const weights = t.master ? static_cast<void*>(t.master) : t.param;
     const uint32_t dtype = t.master ? FTC_F32 : t.param_dtype;
-    __shared__ __align__(16) unsigned char tile[2][kBlockBytes];
+    __shared__ __align__(16) unsigned char room[kTurnBytes];
     const bool whole = bi * 128 + 128 <= t.m && bj * 64 + 64 <= t.w && t.wide && t.cols % 8 == 0;
     if (whole && !t.tall) {                                      // pieces as they are
 #pragma unroll
@@ -303,34 +317,46 @@ __global__ void __launch_bounds__(256, 4) muon_update_kernel(MuonArgs a) {
         }
         return;
     }
+    if (whole) {                                                 // turned
+        float* const turn = reinterpret_cast<float*>(room);
+        float p[4][8];
+        const uint32_t line = threadIdx.x / 16, run = threadIdx.x % 16 * 8;      // and every 16th line after
+        const uint64_t place = (uint64_t)(bj * 64 + line) * t.cols + bi * 128 + run, on = (uint64_t)16 * t.cols;
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) eight(p[u], weights, dtype, place + u * on);
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) {
+            const uint32_t e = threadIdx.x + u * 256, r = e / 8, c = (e & 7) ^ (r & 7);      // a row's pieces as they lie: neighbours in memory
+            float x[8], y[8];
+            eight(x, x_at + e * 16, FTC_F16, 0);
+            if (a.split) eight(y, x_at + a.x_bytes + e * 16, FTC_F16, 0);
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) turn[turn_line(c * 8 + j) + r] = a.split ? x[j] + y[j] : x[j];
+        }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) {
+            float x[8];
+            eight(x, turn + turn_line(line + u * 16) + run, FTC_F32, 0);
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) p[u][j] = fmaf(p[u][j], down, x[j] * move);
+            store_eight(weights, dtype, place + u * on, p[u]);
+            if (t.master) store_eight(t.param, t.param_dtype, place + u * on, p[u]);
+        }
+        return;
+    }
     for (uint32_t s = 0; s <= a.split; ++s) {
         const uint4* from = reinterpret_cast<const uint4*>(x_at + s * a.x_bytes);
-        uint4* to = reinterpret_cast<uint4*>(tile[s]);
+        uint4* to = reinterpret_cast<uint4*>(room + s * kBlockBytes);
 #pragma unroll
         for (uint32_t e = 0; e < kBlockBytes / 16 / 256; ++e) to[threadIdx.x + e * 256] = from[threadIdx.x + e * 256];
     }
     auto update = [&](uint32_t r, uint32_t c) {
         const uint32_t q = piece(r, c / 8) + c % 8 * 2;
-        float v = __half2float(*reinterpret_cast<const __half*>(tile[0] + q));
-        if (a.split) v += __half2float(*reinterpret_cast<const __half*>(tile[1] + q));
+        float v = __half2float(*reinterpret_cast<const __half*>(room + q));
+        if (a.split) v += __half2float(*reinterpret_cast<const __half*>(room + kBlockBytes + q));
         return v * move;
     };
-    if (whole) {
-        const uint32_t line = threadIdx.x % 64, run = threadIdx.x / 64 * 32;
-        const uint64_t place = (uint64_t)(bj * 64 + line) * t.cols + bi * 128 + run;
-        float p[4][8];
-#pragma unroll
-        for (uint32_t u = 0; u < 4; ++u) eight(p[u], weights, dtype, place + u * 8);
-        __syncthreads();
-#pragma unroll
-        for (uint32_t u = 0; u < 4; ++u) {
-#pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) p[u][j] = fmaf(p[u][j], down, update(run + u * 8 + j, line));
-            store_eight(weights, dtype, place + u * 8, p[u]);
-            if (t.master) store_eight(t.param, t.param_dtype, place + u * 8, p[u]);
-        }
-        return;
-    }
     __syncthreads();
     for (uint32_t e0 = threadIdx.x; e0 < 128 * 64; e0 += 2048) {
         float v[8];
