@@ -529,7 +529,7 @@ typedef struct {
 /*
  * For each row, with z = scale * logits: lse = log(sum(exp(z))), logprob = z[token] - lse, entropy = -sum(p * log p) with p = exp(z - lse),
  * and the `top` largest logits' log probabilities and tokens, largest first, the lower token first where logits are the same.
- *   d_logits  [rows] rows of V elements, row r at element r * stride (stride >= V); rows at most 2^31
+ *   d_logits  [rows] rows of V elements, row r at element r * stride (stride >= V); fewer than 2^31 rows
  *   d_tokens  [rows] of token_bits, or NULL (with d_logprob NULL). A token outside 0 .. V-1: logprob 0
  *   d_logprob, d_entropy, d_lse  [rows] float32; each may be NULL
  *   d_top_logprob [rows][top] float32, d_top_token [rows][top] int32: both given with top > 0, both NULL otherwise
