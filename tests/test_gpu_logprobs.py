@@ -142,3 +142,91 @@ def test_some_outputs_only():
     v, w = torch.zeros(5, 3, device="cuda"), torch.zeros(5, 3, dtype=torch.int32, device="cuda")
     B.ftc_token_logprobs(top, x, None, None, None, None, v, w)
     assert torch.equal(w.long(), x.topk(3, 1).indices)
+
+
+@pytest.mark.parametrize("name", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("V", [90, 40000])
+@pytest.mark.parametrize("scale", [1e-6, 1e4, 1e6])
+def test_masked_logits_at_the_ends_of_the_scale(name, V, scale):
+    """-infinity is p = 0 however large the factors of the entropy's gradient are."""
+    rng = np.random.default_rng(V)
+    x = torch.from_numpy(rng.standard_normal((3, V)) / scale).float().clamp(-60000, 60000).to(DT[name])
+    x[rng.random((3, V)) < 0.5] = -INF
+    x[:, 1] = 0
+    x = x.cuda()
+    t = np.array([1, -1, 1])
+    tokens = torch.from_numpy(t).cuda()
+    desc, (_, entropy, lse), _, _ = forward(x, tokens, scale, 0)
+    up, de = torch.tensor([1.0, -2.0, 0.0], device="cuda"), torch.tensor([1e3, -1e3, 1e3], device="cuda")
+    d = torch.full((3, V), 7.0, dtype=DT[name], device="cuda")
+    B.ftc_token_logprobs_backward(desc, x, tokens, lse, entropy, up, de, d)
+    want, off = O.logprobs_backward(x.double().cpu().numpy(), t, float(np.float32(scale)), lse.double().cpu().numpy(), entropy.double().cpu().numpy(),
+                                    up.double().cpu().numpy(), de.double().cpu().numpy())
+    got = d.double().cpu().numpy()
+    if name == "float16":                 # gradients of up to 1e3 * scale: beyond what the type holds
+        most = torch.finfo(torch.float16).max
+        assert np.isfinite(got[abs(want) + off < most]).all() and not np.isnan(got).any()
+        sure = abs(want) + off < most
+        got, want, off = got[sure], want[sure], off[sure]
+    off = off + (abs(want) + off) * O.half_step(name) + O.least(name) * O.half_step(name) * 2
+    assert (abs(got - want) <= off).all(), (abs(got - want) / off).max()
+
+
+def softmax_gradient(x, t, scale, up, de):
+    """The definition from the logits alone, in 64 bits."""
+    z = scale * x
+    m = z.max(1, keepdims=True)
+    s = np.exp(z - m).sum(1, keepdims=True)
+    p = np.exp(z - m) / s
+    logp = np.where(p > 0, z - m - np.log(s), 0)
+    entropy = -(p * logp).sum(1, keepdims=True)
+    g = -p * (up[:, None] + de[:, None] * (logp + entropy))
+    g[np.arange(len(t)), t] += up
+    return scale * g
+
+
+@pytest.mark.parametrize("name", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("V", [3, 90, 2048, 40001])
+@pytest.mark.parametrize("kind", ["lowest", "far", "far up"])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_rows_whose_lse_says_nothing_of_their_p(name, V, kind, in_place):
+    """All of a row masked with the type's lowest value, or logits so far from zero that lse in float32 is too coarse: p comes from the logits."""
+    rng = np.random.default_rng(V)
+    low = torch.finfo(DT[name]).min
+    x = torch.from_numpy(rng.standard_normal((3, V)) * 2).to(DT[name])
+    if kind == "lowest":
+        x[1] = low
+    else:
+        x[1] = (x[1].double() * 64 + (60000 if kind == "far up" else -60000)).to(DT[name])
+    room = torch.full((3, V + 3), 7.0, dtype=DT[name], device="cuda")
+    room[:, :V] = x.cuda()
+    x = room[:, :V]
+    t = np.array([V - 1, V // 2, 0])
+    tokens = torch.from_numpy(t).cuda()
+    desc, (_, entropy, lse), _, _ = forward(x, tokens, 0.5, 0)
+    up, de = torch.tensor([1.0, -2.0, 0.5], device="cuda"), torch.tensor([1.0, 3.0, -2.0], device="cuda")
+    exact = x.double().cpu().numpy()
+    want = softmax_gradient(exact, t, 0.5, up.double().cpu().numpy(), de.double().cpu().numpy())
+    d = x if in_place else torch.full((3, V), 7.0, dtype=DT[name], device="cuda")
+    B.ftc_token_logprobs_backward(desc, x, tokens, lse, entropy, up, de, d)
+    got = d.double().cpu().numpy()
+    # a term's exponent carries three roundings of z - max (64 at most where p counts) and the power 2^-22, s and ln s V additions, the entropy that
+    # is given its own 4 sum_off (1 + spread); |log p + entropy| stays below 64 + ln V where p counts
+    spread = np.log(V) + 8
+    off = 0.5 * (2 + 3 * (64 + spread)) * (64 * 4 * O.U32 + 2.0 ** -22 + O.sum_off(spread, V)) + 0.5 * 3 * 4 * O.sum_off(spread, V) * (1 + spread)
+    off = off + (abs(want) + off) * O.half_step(name) + O.least(name) * O.half_step(name) * 2
+    assert (abs(got - want) <= off).all(), (abs(got - want) / off).max()
+    assert (room[:, V:] == 7.0).all()
+
+
+@pytest.mark.parametrize("V", [70, 50000])
+def test_empty_and_broken_rows_with_large_factors(V):
+    x = torch.randn(3, V, device="cuda")
+    x[0] = -INF
+    x[1, V // 2] = float("nan")
+    tokens = torch.tensor([0, 1, 2], device="cuda")
+    desc, (_, entropy, lse), _, _ = forward(x, tokens, 1e6, 0)
+    d = torch.full_like(x, 7.0)
+    many = torch.full((3,), 1e3, device="cuda")
+    B.ftc_token_logprobs_backward(desc, x, tokens, lse, entropy, many, many, d)
+    assert (d[0] == 0).all() and d[1].isnan().all() and torch.isfinite(d[2]).all()
