@@ -4,7 +4,7 @@
 // c = scale * log2(e); where a larger one comes, s and t are moved to it. Lanes, warps and blocks are joined the same way; then
 //   lse = scale m + ln s,   entropy = ln s - ln 2 * t / s,   logprob = scale (x[token] - m) - ln s.
 // The rounding of c m is the same in all terms and is taken out of ln s and t at the end (up to sizes of 1e8; beyond, see below). Bound by memory and by the 16 powers that an SM
-// makes a cycle (0.7 of what 16-bit logits need); five instructions an element. Logits below -1e30 count as that, so that no infinity meets a
+// makes a cycle (0.7 of what 16-bit logits need); seven instructions an element (8192 rows of 65536). Logits below -1e30 count as that, so that no infinity meets a
 // zero; a row whose largest c m is beyond 1e8 either way, but not -infinity (all of it masked by the type's lowest value, say) is done again with
 // c (x - m), element by element.
 // Rows are divided over the blocks of a cluster where there are few. 8192 rows of 65536 in bf16: 199 us, 5.4 TB/s; 8 rows of 131072: 10 us.
@@ -489,7 +489,7 @@ cudaError_t launch_token_logprobs(const LogprobArgs& a, int sms, cudaStream_t st
 // ---- gradient ----
 //
 // With A = -scale (dlogprob + dentropy (entropy - lse)) and B = -scale * dentropy * scale: p (A + B x), and scale * dlogprob more at the token.
-// Bound by memory (8192 rows of 65536 in bf16: 331 us, 6.5 TB/s); five instructions an element. A row is written in vectors
+// Bound by memory (8192 rows of 65536 in bf16: 331 us, 6.5 TB/s); twelve instructions an element. A row is written in vectors
 // from its own 16-byte boundary on. Where the logits lie otherwise against that boundary (a slice of a padded matrix), a vector is put together from the two that cover it.
 
 // far: lse is so large that z - lse, from lse in float32, would leave p fewer than ten bits (or all of the row is the type's lowest value), or B takes the
