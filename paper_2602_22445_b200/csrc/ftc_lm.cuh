@@ -69,7 +69,7 @@ struct MuonArgs {
     float* momentum; const float* grad_scale;
     uint32_t* word;                              // first of the workspace: not 0 once a wait has given up
     double2* sums; uint32_t* live; float* factor; // [chunks]: squares of U, messages delivered; [n]: was anything delivered, 2^14 / (|U| + eps)
-    float* diag_a; uint32_t* written;            // [3][n]: warps' parts of tiles that have been written, by product
+    float *diag_a, *diag_b; uint32_t* written;            // [3][n]: warps' parts of tiles that have been written, by product
     unsigned char *x[2], *a, *b;                 // blocks of 128 x 64 float16; with two numbers for each, the low ones x_bytes / a_bytes further on
     uint64_t x_bytes, a_bytes;
     uint32_t items[kLists], steps, nesterov, split;

@@ -77,7 +77,7 @@ size_t plan_bytes(const PlanHead& h) {
     return sizeof(PlanHead) + (size_t)h.n * sizeof(PlanEntry) + rounded(((size_t)h.items[kChunks] + h.items[kBlocks] + h.items[kGramTiles] + h.items[kApplyTiles] + h.items[kSmall] + h.n) * 4, 8);
 }
 
-struct MuonLayout { size_t sums, live, factor, written, diag_a, x0, x1, a, b, x_bytes, a_bytes, total; };
+struct MuonLayout { size_t sums, live, factor, written, diag_a, diag_b, x0, x1, a, b, x_bytes, a_bytes, total; };
 MuonLayout muon_layout(const PlanHead& h, uint32_t products) {
     const size_t block = 128 * 64 * 2, numbers = products == 32 ? 2 : 1;
     MuonLayout l{};
@@ -85,7 +85,7 @@ MuonLayout muon_layout(const PlanHead& h, uint32_t products) {
     size_t at = 1024;
     auto take = [&](size_t bytes) { const size_t here = at; at = rounded(at + bytes, 256); return here; };
     l.sums = take((size_t)h.items[kChunks] * 16); l.live = take((size_t)h.n * 4); l.factor = take((size_t)h.n * 4); l.written = take((size_t)h.n * 12);
-    l.diag_a = take(h.diagonals * 4);
+    l.diag_a = take(h.diagonals * 4); l.diag_b = take(h.diagonals * 4);
     l.x0 = take(l.x_bytes * numbers); l.x1 = take(l.x_bytes * numbers); l.a = take(l.a_bytes * numbers); l.b = take(l.a_bytes * numbers);
     l.total = at;
     return l;
@@ -246,7 +246,7 @@ int ftc_muon_step(const ftc_muon_t* hyper, const void* h_plan, const void* d_pla
     MuonArgs a{};
     a.plan = d_plan; a.n = h->n; a.momentum = d_momentum; a.grad_scale = d_grad_scale; a.word = reinterpret_cast<uint32_t*>(ws);
     a.sums = reinterpret_cast<double2*>(ws + l.sums); a.live = reinterpret_cast<uint32_t*>(ws + l.live); a.factor = reinterpret_cast<float*>(ws + l.factor); a.written = reinterpret_cast<uint32_t*>(ws + l.written);
-    a.diag_a = reinterpret_cast<float*>(ws + l.diag_a);
+    a.diag_a = reinterpret_cast<float*>(ws + l.diag_a); a.diag_b = reinterpret_cast<float*>(ws + l.diag_b);
     a.x[0] = ws + l.x0; a.x[1] = ws + l.x1; a.a = ws + l.a; a.b = ws + l.b; a.x_bytes = l.x_bytes; a.a_bytes = l.a_bytes;
     const uint32_t* map = reinterpret_cast<const uint32_t*>(plan_entries(d_plan) + h->n);
     for (int w = 0; w < kLists; ++w) { a.items[w] = h->items[w]; a.maps[w] = map; map += h->items[w]; }

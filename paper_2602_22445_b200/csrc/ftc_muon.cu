@@ -4,12 +4,14 @@
 // step follow, each over all matrices at once:
 //   gram   A = X X^T             symmetric: tiles on and below the diagonal, written twice
 //   poly   B = b A + c A A       symmetric too (A A = A A^T)
-//   apply  X = (a + B) X         with a in B's diagonal
+//   apply  X = (a + B) X
 // Operands are float16, held times 2^14: |X| stays below 1.21 after the first step (the largest value of the quintic on 0 .. 1.21), entries of
 // A below 1.47 and of B below 2.81, so nothing overflows and numbers down to 2^-28 keep their 11 bits (bfloat16 would keep 8). Diagonals,
 // which are the large entries of A and B in late steps, are held apart in float32: with A = D + A', A A = A' A' + D A' + A' D + D D, all but
-// the first by elements. Sums are float32 throughout, in tensor memory.
-// With `split` every operand is two float16 numbers, the second one what the first leaves over: hi hi + hi lo + lo hi in one sum.
+// the first by elements; with B = E + B', X = B' X + (a + E) X, the second by elements too (E rounded with the rest: an error larger by 1.35 to 1.9).
+// Sums are float32 throughout, in tensor memory.
+// With `split` every operand is two float16 numbers, the second one what the first leaves over: hi hi + hi lo + lo hi in one sum; a + E, up to
+// 3.45, is B's diagonal then (22 bits of it, as of all else).
 //
 // Matrices lie in the workspace in blocks of 128 rows x 64 columns (16 KB), their 16-byte pieces in the order that the tensor cores read
 // (piece c of row r at c ^ r % 8): a block is one contiguous copy, whichever way a product reads it, and edges are zeros.
@@ -387,7 +389,7 @@ __global__ void __launch_bounds__(256, 4) muon_update_kernel(MuonArgs a) {
 //   warp 0   copies of its block's operands
 //   warp 1   first block: matrix instructions; second block: tells the first when its copies have landed
 //   warps 4 .. 11   read sums out (a warp reads the 32 lanes of tensor memory that its number modulo 4 gives it), the first four those of the
-//            left 128 columns, the others the right ones', 64 at a time, each warp for itself: what the result needs of A comes into shared
+//            left 128 columns, the others the right ones', 64 at a time, each warp for itself: what the result needs of A or X comes into shared
 //            memory as 4 KB, is replaced there by the result, and goes out as 4 KB; its transpose in stores of 64 bytes.
 // A step of 64 takes 0.47 us a pair (4096 x 4096), where the tensor cores alone would take 0.3: copies out of L2 bound it. 0.54 with 24 of
 // 1024 x 4096 (five steps: 1.6 ms, 1.05 PFLOP/s with symmetric products counted half), where a tile's beginning and end count; finding the next tile
@@ -634,6 +636,7 @@ template <bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
         // One tile's part of this warp, for each of the three products.
         auto finish = [&](auto mode, const Tile& tile, const PlanEntry& t) {
             constexpr int MODE = decltype(mode)::value;
+            constexpr bool NEEDS = MODE == kPoly || (MODE == kApply && !SPLIT);          // what a diagonal multiplies: A, or X itself
             const uint32_t bi = 2 * tile.i + rank, i = bi * 128 + r;
             // blocks of 64 columns of this team: none above the diagonal, none beyond the edges
             const uint32_t cb0 = 4 * tile.j + 2 * team, edge = MODE <= kPoly ? 2 * min(t.mb, bi + 1) : t.nb;
@@ -641,16 +644,16 @@ template <bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
             const uint64_t row_at = (MODE <= kPoly ? t.a_block + (uint64_t)bi * 2 * t.mb : t.x_block + (uint64_t)bi * t.nb) * kBlockBytes + quarter * kRows;
             unsigned char* const out = (MODE == kGram ? a.a : MODE == kPoly ? a.b : a.x[tile.step & 1 ^ 1]) + row_at;
             const uint64_t low = MODE <= kPoly ? a.a_bytes : a.x_bytes;
-            auto fetch = [&](uint32_t b, unsigned char* to, uint32_t bar) {              // A, by one lane
-                const unsigned char* from = a.a + row_at + (uint64_t)(cb0 + b) * kBlockBytes;
+            auto fetch = [&](uint32_t b, unsigned char* to, uint32_t bar) {              // by one lane
+                const unsigned char* from = (MODE == kPoly ? a.a : a.x[tile.step & 1]) + row_at + (uint64_t)(cb0 + b) * kBlockBytes;
                 bar_expect(bar, (SPLIT ? 2 : 1) * kRows);
                 copy_in(smem_of(to), from, kRows, bar);
                 if (SPLIT) copy_in(smem_of(other), from + low, kRows, bar);
             };
-            if (MODE == kPoly && wanted && lane == 0) ok = wait_for_product(a, tile, t);
-            if (MODE == kPoly) ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
+            if (NEEDS && wanted && lane == 0) ok = wait_for_product(a, tile, t);
+            if (NEEDS) ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
             if (!ok) return;
-            if (!SPLIT && MODE == kPoly && lane == 0 && wanted) {
+            if (!SPLIT && NEEDS && lane == 0 && wanted) {
                 fetch(0, mine, ready);
                 if (wanted > 1) fetch(1, other, ready + 8);
             }
@@ -661,10 +664,10 @@ template <bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
                     asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     if (MODE == kPoly) fetch(b, mine, ready);
                 }
-                ok = (b || bar_wait(sum_full + 8 * (n & 1), (n / 2) & 1)) && (!wanted || MODE != kPoly || bar_wait(ready + 8 * which, done[which] & 1));
+                ok = (b || bar_wait(sum_full + 8 * (n & 1), (n / 2) & 1)) && (!wanted || !NEEDS || bar_wait(ready + 8 * which, done[which] & 1));
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok || !wanted) break;
-                if (MODE == kPoly) ++done[which];
+                if (NEEDS) ++done[which];
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 F2 v[32];
                 read_64(v, tmem + (n & 1) * 256 + (quarter * 32 << 16) + team * 128 + b * 64);
@@ -681,14 +684,25 @@ template <bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
                     mine_own *= kDown2;
                 }
                 if (MODE == kGram && diagonal) a.diag_a[t.diagonal + i] = mine_own;
-                if (MODE != kPoly) {
+                if (!NEEDS) {
 #pragma unroll
                     for (int q = 0; q < 32; ++q) v[q] = mul(v[q], twice(kDown));
+                } else if (MODE == kApply) {
+                    const F2 keep = twice(kQ1 + __ldcg(a.diag_b + t.diagonal + i));
+#pragma unroll
+                    for (uint32_t c = 0; c < 8; ++c) {
+                        const uint4 h = *reinterpret_cast<const uint4*>(here + piece(lane, c));
+                        const F2 e[4] = {pair_of(h.x), pair_of(h.y), pair_of(h.z), pair_of(h.w)};
+#pragma unroll
+                        for (uint32_t q = 0; q < 4; ++q) v[4 * c + q] = fma(v[4 * c + q], twice(kDown), mul(e[q], keep));
+                    }
                 } else {
                     const float* d = a.diag_a + t.diagonal;
                     const float di = __ldcg(d + i);
                     const F2 keep = twice(fmaf(kQ5, di, kQ3));
-                    mine_own = (kQ1 + fmaf(kQ5, fmaf(di, di, mine_own), kQ3 * di)) * kUp;
+                    const float e_own = fmaf(kQ5, fmaf(di, di, mine_own), kQ3 * di);
+                    if (!SPLIT && diagonal) a.diag_b[t.diagonal + i] = e_own;
+                    mine_own = SPLIT ? (kQ1 + e_own) * kUp : 0.f;
 #pragma unroll
                     for (uint32_t c = 0; c < 8; ++c) {
                         const uint4 h = *reinterpret_cast<const uint4*>(here + piece(lane, c));
@@ -718,7 +732,7 @@ template <bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
                     *reinterpret_cast<uint4*>(here + piece(lane, c)) = make_uint4(h[4 * c], h[4 * c + 1], h[4 * c + 2], h[4 * c + 3]);
                     if (SPLIT) *reinterpret_cast<uint4*>(other + piece(lane, c)) = make_uint4(low_h[4 * c], low_h[4 * c + 1], low_h[4 * c + 2], low_h[4 * c + 3]);
                 }
-                if (diagonal) {                                  // none in A; that of B with the 3.4445 of X
+                if (diagonal) {                                  // none in A; in B with `split` alone, with the 3.4445 of X
                     const __half d = __float2half_rn(MODE == kPoly ? mine_own : 0.f);
                     *reinterpret_cast<__half*>(here + piece(lane, own / 8) + own % 8 * 2) = d;
                     if (SPLIT) *reinterpret_cast<__half*>(other + piece(lane, own / 8) + own % 8 * 2) = __float2half_rn(MODE == kPoly ? mine_own - __half2float(d) : 0.f);
@@ -780,7 +794,7 @@ template <bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
 // of 64 x 64 and 64 x 256 in 32-bit products: 164 us a call in all, so 63: five steps of three dependent products, 46 us, which latency bounds).
 
 constexpr uint32_t kSmallThreads = 256, kSmallBlocks = 8;                        // X's
-constexpr uint32_t kSmallSmem = (kSmallBlocks + 4) * kBlockBytes + 1024 + 1024;
+constexpr uint32_t kSmallSmem = (kSmallBlocks + 4) * kBlockBytes + 1024 + 1536;
 
 __device__ __forceinline__ void multiply_alone(uint32_t d, uint64_t a, uint64_t b, uint32_t how, bool add) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
@@ -793,9 +807,9 @@ template <bool SPLIT> __global__ void __launch_bounds__(kSmallThreads, 1) muon_s
     unsigned char* const x = raw + (1024 - (smem_of(raw) & 1023)) % 1024;        // X's blocks, its low numbers', A's, its low numbers'
     constexpr uint32_t kLowX = kSmallBlocks / 2 * kBlockBytes, kLowA = 2 * kBlockBytes;
     unsigned char* const m = x + kSmallBlocks * kBlockBytes;
-    float* const diag = reinterpret_cast<float*>(m + 2 * kLowA);                 // 128
-    const uint32_t bar = smem_of(diag + 128);                                    // copies; products
-    uint32_t* const words = reinterpret_cast<uint32_t*>(diag + 132);
+    float* const diag = reinterpret_cast<float*>(m + 2 * kLowA);                 // A's 128, B's 128 (with `split` in B)
+    const uint32_t bar = smem_of(diag + 256);                                    // copies; products
+    uint32_t* const words = reinterpret_cast<uint32_t*>(diag + 260);
     if (threadIdx.x == 0) {
         bar_init(bar, 1); bar_init(bar + 8, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -910,14 +924,27 @@ template <bool SPLIT> __global__ void __launch_bounds__(kSmallThreads, 1) muon_s
 #pragma unroll
                 for (uint32_t q = 0; q < 4; ++q) v[4 * c + q] = fma(v[4 * c + q], twice(kQ5 * kDown), mul(e[q], fma(dj[q], twice(kQ5), keep)));
             }
-            put(block, kLowA, v, (kQ1 + fmaf(kQ5, fmaf(di, di, more), kQ3 * di)) * kUp, own);
+            const float e_own = fmaf(kQ5, fmaf(di, di, more), kQ3 * di);
+            if (!SPLIT && own) diag[128 + r] = e_own;
+            put(block, kLowA, v, SPLIT ? (kQ1 + e_own) * kUp : 0.f, own);
             written();
             product(m, kLowA, x, kLowX, t.kb, t.nb * 64, true);
             if (!ok) break;
             for (uint32_t q = half; q < t.nb; q += 2) {
                 read_64(v, tmem + (quarter * 32 << 16) + q * 64);
+                if (SPLIT) {
 #pragma unroll
-                for (int p = 0; p < 32; ++p) v[p] = mul(v[p], twice(kDown));
+                    for (int p = 0; p < 32; ++p) v[p] = mul(v[p], twice(kDown));
+                } else {
+                    const F2 keep_x = twice(kQ1 + diag[128 + r]);
+#pragma unroll
+                    for (uint32_t c = 0; c < 8; ++c) {
+                        const uint4 h = *reinterpret_cast<const uint4*>(x + q * kBlockBytes + piece(r, c));
+                        const F2 e[4] = {pair_of(h.x), pair_of(h.y), pair_of(h.z), pair_of(h.w)};
+#pragma unroll
+                        for (uint32_t p = 0; p < 4; ++p) v[4 * c + p] = fma(v[4 * c + p], twice(kDown), mul(e[p], keep_x));
+                    }
+                }
                 put(x + q * kBlockBytes, kLowX, v, 0.f, false);
             }
             written();
