@@ -533,8 +533,9 @@ typedef struct {
  *   d_tokens  [rows] of token_bits, or NULL (with d_logprob NULL). A token outside 0 .. V-1: logprob 0
  *   d_logprob, d_entropy, d_lse  [rows] float32; each may be NULL
  *   d_top_logprob [rows][top] float32, d_top_token [rows][top] int32: both given with top > 0, both NULL otherwise
- * Logits of -infinity are tokens that cannot come: p = 0. A row of nothing else has lse = logprob = top_logprob = -infinity and entropy 0. A row
- * that holds +infinity or NaN has NaN for logprob (of a token), entropy, lse and top_logprob; its top_token are unspecified.
+ * Logits of -infinity are tokens that cannot come: p = 0. A row of nothing else has lse = logprob = top_logprob = -infinity and entropy 0. Any other
+ * row's lse is held within float32's finite numbers (scale * logits may leave them; the rest is right all the same). A row that holds +infinity
+ * or NaN has NaN for logprob (of a token), entropy, lse and top_logprob; its top_token are unspecified.
  * rows = 0 is valid and does nothing.
  */
 FTC_API int ftc_token_logprobs(const ftc_logprob_t* desc, uint64_t rows, const void* d_logits, uint64_t stride, const void* d_tokens,

@@ -21,6 +21,7 @@ namespace ftc {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kLeast = -200.f;                                 // 2^-200 is 0 in float32: stands for whatever is smaller
+constexpr float kMost = 3.40282346638528859812e38f;              // float32's largest number
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 
 __device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
@@ -427,7 +428,8 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
         ln_s = logf(s); mean_d = t / s;
     }
     const bool bad = isnan(m) || m == INFINITY, empty = m == -INFINITY;
-    const float nan = __int_as_float(0x7FFFFFFF), lse = bad ? nan : empty ? -INFINITY : fmaf(a.scale, m, ln_s);
+    // scale * m may leave float32: the largest number stands for it then, so that an lse of -infinity is that of an empty row and no other
+    const float nan = __int_as_float(0x7FFFFFFF), lse = bad ? nan : empty ? -INFINITY : fminf(fmaxf(fmaf(a.scale, m, ln_s), -kMost), kMost);
     if (lane == 0) {
         if (a.lse) a.lse[row] = lse;
         if (a.entropy) a.entropy[row] = bad ? nan : empty ? 0.f : fmaxf(0.f, ln_s - kLn2 * mean_d);
