@@ -547,7 +547,8 @@ FTC_API int ftc_token_logprobs(const ftc_logprob_t* desc, uint64_t rows, const v
  *   d_lse, d_entropy       [rows], as the forward pass left them (d_entropy may be NULL without d_dentropy)
  *   d_dlogprob, d_dentropy [rows] float32; either may be NULL: 0. Where the token is outside 0 .. V-1 its dlogprob is not read into the result
  *   d_dlogits  rows of V elements, row r at element r * dstride; may be d_logits (with the same stride)
- * Rows with lse = -infinity get zeros. Where lse is finite but its size (2^14 or more) leaves p too few bits, p is found from the logits again.
+ * Rows with lse = -infinity get zeros. Where lse is finite but its size (2^7 or more in float32, 2^11 in float16, 2^14 in bfloat16) leaves p too few bits,
+ * p is found from the logits again, in two more passes over the row.
  */
 FTC_API int ftc_token_logprobs_backward(const ftc_logprob_t* desc, uint64_t rows, const void* d_logits, uint64_t stride, const void* d_tokens,
                                         const float* d_lse, const float* d_entropy, const float* d_dlogprob, const float* d_dentropy,

@@ -490,29 +490,32 @@ cudaError_t launch_token_logprobs(const LogprobArgs& a, int sms, cudaStream_t st
 
 // ---- gradient ----
 //
-// With A = -scale (dlogprob + dentropy (entropy - lse)) and B = -scale * dentropy * scale: p (A + B x), and scale * dlogprob more at the token.
+// With A = -scale (dlogprob + dentropy * entropy), B = -scale * dentropy and l = scale x - lse, rounded once: p (A + B l), and scale * dlogprob more at
+// the token. (A + B' x with lse in A would cancel: lse's size over 2^24 of an error.)
 // Bound by memory (8192 rows of 65536 in bf16: 331 us, 6.5 TB/s); twelve instructions an element. A row is written in vectors
 // from its own 16-byte boundary on. Where the logits lie otherwise against that boundary (a slice of a padded matrix), a vector is put together from the two that cover it.
 
-// far: lse is so large that z - lse, from lse in float32, would leave p fewer than ten bits (or all of the row is the type's lowest value), or B takes the
-// 2^100 that stands for an infinity out of float32.
+// far: lse in float32 is too coarse for the type: half its step, which is p's relative error, is 2^-18 below 2^7 (float32), 2^-14 below 2^11 (float16,
+// whose half step is 2^-11), 2^-11 below 2^14 (bfloat16, 2^-8); or B takes the 2^100 that stands for an infinity out of float32.
+template <typename T> constexpr float kFarLse = sizeof(T) == 4 ? 0x1p7f : 0x1p14f;
+template <> constexpr float kFarLse<__half> = 0x1p11f;
 struct RowFactors { float a, b, up, lse; int32_t token; bool zero, far; };
 
-__device__ __forceinline__ RowFactors factors_of(const LogprobArgs& g, uint32_t row) {
+template <typename T> __device__ __forceinline__ RowFactors factors_of(const LogprobArgs& g, uint32_t row) {
     RowFactors f;
     f.token = g.dlogprob ? token_at(g.tokens, g.token_bits, row, g.V) : -1;
     const float given = g.dlogprob ? g.dlogprob[row] : 0.f, up = f.token >= 0 ? given : 0.f, de = g.dentropy ? g.dentropy[row] : 0.f;
     f.lse = g.lse_in[row];
     f.zero = f.lse == -INFINITY;
-    f.a = -(up + (g.dentropy ? de * (g.entropy_in[row] - f.lse) : 0.f)) * g.scale;
-    f.b = -de * g.scale * g.scale;
+    f.a = -(g.dentropy ? fmaf(de, g.entropy_in[row], up) : up) * g.scale;
+    f.b = -de * g.scale;
     f.up = up * g.scale;
-    f.far = fabsf(f.lse) < INFINITY && (fabsf(f.lse) >= 0x1p14f || fabsf(f.b) >= 0x1p26f);
+    f.far = fabsf(f.lse) < INFINITY && (fabsf(f.lse) >= kFarLse<T> || fabsf(f.b * g.scale) >= 0x1p26f);
     return f;
 }
 __device__ __forceinline__ float gradient(const RowFactors& f, float x, float scale) {
-    const float v = x < kFloor ? kFloor : x;                     // NaN stays
-    return f.zero ? 0.f : exp2_fast(fmaf(v, scale, -f.lse) * kLog2e) * fmaf(f.b, v, f.a);
+    const float v = x < kFloor ? kFloor : x, l = fmaf(v, scale, -f.lse);         // NaN stays
+    return f.zero ? 0.f : exp2_fast(l * kLog2e) * fmaf(f.b, l, f.a);
 }
 // As Pairs' numbers, but NaN stays what it is: the row's lse is NaN then, so no care is needed.
 template <typename T> __device__ __forceinline__ uint4 gradients(const RowFactors& f, uint4 r, float scale) {
@@ -522,7 +525,7 @@ template <typename T> __device__ __forceinline__ uint4 gradients(const RowFactor
     Pairs<T>::numbers(v, r);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-        const F2 d = mul(fma(v[j], twice(scale), twice(-f.lse)), twice(kLog2e)), e = mul(pair(exp2_fast(lo(d)), exp2_fast(hi(d))), fma(twice(f.b), v[j], twice(f.a)));
+        const F2 l = fma(v[j], twice(scale), twice(-f.lse)), d = mul(l, twice(kLog2e)), e = mul(pair(exp2_fast(lo(d)), exp2_fast(hi(d))), fma(twice(f.b), l, twice(f.a)));
         y[2 * j] = f.zero ? 0.f : lo(e);
         y[2 * j + 1] = f.zero ? 0.f : hi(e);
     }
@@ -544,7 +547,8 @@ __device__ __forceinline__ uint4 joined_at(uint4 a, uint4 b, uint32_t shift) {
 }
 
 // A far row by one group of threads: its largest logit and sum once more, then scale (dlogprob ([j = token] - p) - dentropy p (log p + entropy)) with
-// log p = c (x - m) ln 2 - ln s. A thread reads and writes the same elements.
+// log p = c (x - m) ln 2 - ln s. A thread reads and writes the same elements. One block has such a row, in three passes: 4096 rows of 65536 in float32
+// take 1045 us so, and 322 if none is far (64 of 131072: 134 and 11). Logits whose lse is that large are rare, and exact gradients worth more.
 template <typename T, uint32_t GROUP> __device__ __forceinline__ void far_row(const LogprobArgs& g, uint32_t row, const RowFactors& f, const T* x, T* d) {
     __shared__ float parts[2][8];
     const uint32_t in_group = threadIdx.x % GROUP, warp = threadIdx.x / 32;
@@ -594,7 +598,7 @@ template <typename T, uint32_t GROUP> __global__ void __launch_bounds__(256, 5) 
         const uint32_t shift = (uint32_t)(reinterpret_cast<uintptr_t>(x + out.head) & 15);
         const uint4* const xv = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(x + out.head) - shift);
         uint4* const dv = reinterpret_cast<uint4*>(d + out.head);
-        const RowFactors f = factors_of(g, row);
+        const RowFactors f = factors_of<T>(g, row);
         const uint32_t stores = f.far ? 0 : end;                 // the loads do not wait for it
         const uint32_t at = f.token >= 0 && !f.zero ? (uint32_t)f.token : kNone;
         for (uint32_t i0 = (GROUP == 32 ? 0 : piece * each) + in_group; i0 < end; i0 += GROUP * U) {

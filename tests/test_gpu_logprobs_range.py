@@ -93,3 +93,29 @@ def test_rows_whose_lse_leaves_float32(name, V, kind, scale):
     got = d.double().cpu().numpy()
     sure = abs(want) + off < torch.finfo(DT[name]).max
     assert np.isfinite(got[sure]).all() and (abs(got - want) <= off)[sure].all(), np.nanmax((abs(got - want) / off)[sure])
+
+
+@pytest.mark.parametrize("name", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("V", [90, 3001, 40001])
+@pytest.mark.parametrize("shift", [0, 100, 300, 3000, 15000, -3000])
+def test_gradient_of_logits_far_from_zero(name, V, shift):
+    """As near to the definition as the type allows, wherever the logits lie: p is good to 2^-17 in float32 and to a quarter of the type's half step in
+    16 bits."""
+    rng = np.random.default_rng(V + abs(shift))
+    x = torch.from_numpy(rng.standard_normal((3, V)) * 3 + shift).to(DT[name]).cuda()
+    t = np.array([0, V // 2, V - 1])
+    tokens = torch.from_numpy(t).cuda()
+    desc, (_, entropy, lse), _, _ = forward(x, tokens, 1.0)
+    up, de = np.array([1.0, -2.0, 0.5]), np.array([0.0, 3.0, -2.0])
+    d = torch.full((3, V), 7.0, dtype=DT[name], device="cuda")
+    B.ftc_token_logprobs_backward(desc, x, tokens, lse, entropy, torch.from_numpy(up).float().cuda(), torch.from_numpy(de).float().cuda(), d)
+    want, p, logp, ent, spread = softmax_gradient(x.double().cpu().numpy(), t, 1.0, up, de)
+    # an error e of log p moves p (up + de (log p + entropy)) by e p (|up| + |de| (|log p| + entropy + 1)): e is half a step of lse (2^-18 below 2^7,
+    # 2^-14 below 2^11, 2^-11 below 2^14, where it is found from the logits), the forward pass's own, and three roundings of |log p|
+    e = {"float32": 2.0 ** -18, "float16": 2.0 ** -14, "bfloat16": 2.0 ** -11}[name]
+    e = e + 4 * O.U32 * (1 + abs(logp)) + O.sum_off(spread, V)
+    off = p * (abs(up)[:, None] + abs(de)[:, None] * (abs(logp) + ent + 1)) * e + p * abs(de)[:, None] * 4 * O.sum_off(spread, V) * (1 + spread)
+    off[np.arange(3), t] += abs(up) * 4 * O.U32
+    off = off + (abs(want) + off) * O.half_step(name) + O.least(name) * O.half_step(name) * 2
+    got = d.double().cpu().numpy()
+    assert (abs(got - want) <= off).all(), (abs(got - want) / off).max()
