@@ -535,7 +535,7 @@ template <bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = words[0], pairs = gridDim.x / 2, our_pair = blockIdx.x / 2;
     const float scale = a.grad_scale ? *a.grad_scale : 1.f;
-    const bool work = isfinite(scale) && *reinterpret_cast<volatile uint32_t*>(a.word) == 0;
+    const bool work = isfinite(scale);                           // not by the word: another pair may be setting it, and threads would disagree
     const PlanEntry* const entries = plan_entries(a.plan);
     const uint32_t tiles = a.steps * (2 * a.items[kGramTiles] + a.items[kApplyTiles]);
     constexpr uint32_t segments = SPLIT ? 3 : 1;
@@ -827,7 +827,7 @@ template <bool SPLIT> __global__ void __launch_bounds__(kSmallThreads, 1) muon_s
     const float scale = a.grad_scale ? *a.grad_scale : 1.f;
     bool ok = true;
     uint32_t copied = 0, multiplied = 0;
-    const uint32_t count = isfinite(scale) && *reinterpret_cast<volatile uint32_t*>(a.word) == 0 ? a.items[kSmall] : 0;
+    const uint32_t count = isfinite(scale) ? a.items[kSmall] : 0;                // not by the word: another block may be setting it, and threads would part at a barrier
     // The block's products of `steps` blocks of 64 of the inner dimension; everybody waits for them.
     auto product = [&](const unsigned char* left, uint32_t left_low, const unsigned char* right, uint32_t right_low, uint32_t steps, uint32_t columns, bool along) {
         if (threadIdx.x == 0) {
