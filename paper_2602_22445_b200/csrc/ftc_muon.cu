@@ -10,8 +10,9 @@
 // which are the large entries of A and B in late steps, are held apart in float32: with A = D + A', A A = A' A' + D A' + A' D + D D, all but
 // the first by elements; with B = E + B', X = B' X + (a + E) X, the second by elements too (E rounded with the rest: an error larger by 1.35 to 1.9).
 // Sums are float32 throughout, in tensor memory.
-// With `split` every operand is two float16 numbers, the second one what the first leaves over: hi hi + hi lo + lo hi in one sum; a + E, up to
-// 3.45, is B's diagonal then (22 bits of it, as of all else).
+// With `split` every operand is two float16 numbers, the second one what the first leaves over: hi lo + lo hi + hi hi in one sum, in this order: the
+// tensor cores cut the sum to float32 every 16 products, of which the small ones' cuts count nothing while the large ones are not in it yet
+// (hi hi first: 1.3 to 4 times the error). a + E, up to 3.45, is B's diagonal then (22 bits of it, as of all else).
 //
 // Matrices lie in the workspace in blocks of 128 rows x 64 columns (16 KB), their 16-byte pieces in the order that the tensor cores read
 // (piece c of row r at c ^ r % 8): a block is one contiguous copy, whichever way a product reads it, and edges are zeros.
@@ -539,8 +540,8 @@ template <bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
     const PlanEntry* const entries = plan_entries(a.plan);
     const uint32_t tiles = a.steps * (2 * a.items[kGramTiles] + a.items[kApplyTiles]);
     constexpr uint32_t segments = SPLIT ? 3 : 1;
-    // a tile on the diagonal: the left operand is the right one too
-    auto one_of = [&](const PlanEntry& t, const Tile& q, uint32_t g) { return q.mode <= kPoly && g == 0 && q.i == q.j && t.mb > 2 * q.j + 1; };
+    // a tile on the diagonal: the left operand is the right one too (hi hi, the last segment)
+    auto one_of = [&](const PlanEntry& t, const Tile& q, uint32_t g) { return q.mode <= kPoly && g + 1 == segments && q.i == q.j && t.mb > 2 * q.j + 1; };
     auto inner_of = [&](const PlanEntry& t, const Tile& q) { return q.mode == kGram ? t.nb : t.kb; };             // blocks of 64
     // a tile's columns: 256, or 128 where there are no more (of an apply tile up to 64 of them are nobody's)
     auto columns_of = [&](const PlanEntry& t, const Tile& q) { return (q.mode <= kPoly ? t.mb > 2 * q.j + 1 : t.nb > 4 * q.j + 2) ? 256u : 128u; };
@@ -562,8 +563,8 @@ template <bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
             for (uint32_t g = 0; g < segments && ok; ++g) {
                 const bool one = one_of(t, tile, g);
                 const uint32_t bytes = (has_left ? kBlockBytes : 0) + (one ? 0 : sym ? half * 128 : right_blocks * (kBlockBytes / 2));
-                const unsigned char* l = (gram ? x_in : (tile.mode == kPoly) ? a.a : a.b) + (g == 2 ? (gram ? a.x_bytes : a.a_bytes) : 0);
-                const unsigned char* r = ((tile.mode == kPoly) ? a.a : x_in) + (g == 1 ? ((tile.mode == kPoly) ? a.a_bytes : a.x_bytes) : 0);
+                const unsigned char* l = (gram ? x_in : (tile.mode == kPoly) ? a.a : a.b) + (SPLIT && g == 1 ? (gram ? a.x_bytes : a.a_bytes) : 0);
+                const unsigned char* r = ((tile.mode == kPoly) ? a.a : x_in) + (SPLIT && g == 0 ? ((tile.mode == kPoly) ? a.a_bytes : a.x_bytes) : 0);
                 l += gram ? (t.x_block + (uint64_t)left_row * t.nb) * kBlockBytes : (t.a_block + (uint64_t)left_row * 2 * t.mb) * kBlockBytes;
                 r += gram ? (t.x_block + (uint64_t)right_row * t.nb) * kBlockBytes + right_in
                    : (tile.mode == kPoly) ? (t.a_block + (uint64_t)right_row * 2 * t.mb) * kBlockBytes + right_in : (t.x_block + right_block) * kBlockBytes;
@@ -609,7 +610,7 @@ template <bool SPLIT> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds_
                 const uint32_t slot = it % kStages, at = smem_of(smem) + slot * kStageBytes;
                 if (!(ok = bar_wait(full + 8 * slot, (it / kStages) & 1) && bar_wait(landed + 8 * slot, (it / kStages) & 1))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t right = at + (one_of(t, tile, s < inner ? 0 : 1) ? 0 : kBlockBytes);
+                const uint32_t right = at + (one_of(t, tile, s < (segments - 1) * inner ? 0 : segments - 1) ? 0 : kBlockBytes);
 #pragma unroll
                 for (uint32_t k = 0; k < 4; ++k) {               // 16 of the inner dimension: 32 bytes along a row, 16 rows of 128 bytes
                     const uint64_t l = operand(at + k * 32, 16, 1024), r = operand(right + k * along, leading, 1024);
@@ -837,7 +838,7 @@ template <bool SPLIT> __global__ void __launch_bounds__(kSmallThreads, 1) muon_s
                     for (uint32_t s = 0; s < steps; ++s)
 #pragma unroll
                         for (uint32_t k = 0; k < 4; ++k) {
-                            const uint32_t l = smem_of(left) + (g == 2 ? left_low : 0) + s * kBlockBytes + k * 32, q = smem_of(right) + (g == 1 ? right_low : 0) + c / 64 * kBlockBytes;
+                            const uint32_t l = smem_of(left) + (SPLIT && g == 1 ? left_low : 0) + s * kBlockBytes + k * 32, q = smem_of(right) + (SPLIT && g == 0 ? right_low : 0) + c / 64 * kBlockBytes;
                             multiply_alone(tmem + c, operand(l, 16, 1024), along ? operand(q + s * (kBlockBytes / 2) + k * 2048, kBlockBytes, 1024) : operand(q + s * kBlockBytes + k * 32, 16, 1024),
                                            how, g || s || k);
                         }
