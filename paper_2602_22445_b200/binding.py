@@ -714,7 +714,8 @@ def make_muon_plan(matrices, device="cuda") -> MuonPlan:
     return MuonPlan(matrices, device)
 
 
-def make_muon(lr, momentum=0.95, eps=1e-7, steps=5, nesterov=True, products=16) -> ftc_muon_t:
+def make_muon(lr, momentum=0.95, eps=1e-7, steps=5, nesterov=True, products=32) -> ftc_muon_t:
+    """`products`: 32, or 16 for updates that may be off by a thousandth (weights in 16 bits), at half the time."""
     return ftc_muon_t(lr, momentum, eps, steps, int(nesterov), products, 0)
 
 
