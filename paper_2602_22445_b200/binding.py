@@ -475,7 +475,7 @@ def ftc_layernorm_backward(desc, d_dy, d_x, d_gamma, d_mean, d_rstd, d_row_split
     x, xs = _rows_ptr(desc, d_x, "d_x", rows)
     dx, dxs = _rows_ptr(desc, d_dx, "d_dx", rows)
     n = -(-desc.H // desc.k) * desc.P * desc.k
-    if d_row_splits is not None and (d_row_splits.numel() != desc.P + 1 or d_row_splits.element_size() != 8 or d_row_splits.is_floating_point()):
+    if d_row_splits is not None and (d_row_splits.numel() != desc.P + 1 or _whole_bytes(d_row_splits) != 8):
         raise ValueError("d_row_splits: P + 1 whole numbers of 64 bits are wanted")
     ws_bytes = 0 if d_workspace is None else d_workspace.numel() * d_workspace.element_size()
     rc = (_lib or load()).ftc_layernorm_backward(desc, rows, dy, dys, x, xs, _vector_ptr(d_gamma, "d_gamma", desc.H, desc.wdtype),
@@ -606,11 +606,23 @@ def _matrix_ptr(t, what, rows, cols, code):
     return t.data_ptr(), stride if rows > 1 or stride >= cols else cols
 
 
+_WHOLE = {}
+
+
+def _whole_bytes(t) -> int:
+    """The size of its elements if they are whole numbers of 32 or 64 bits, else 0 (complex and quantised ones are no floating point numbers
+    either). Types are looked up as they were met."""
+    size = _WHOLE.get(t.dtype)
+    if size is None:
+        size = _WHOLE[t.dtype] = {"int32": 4, "uint32": 4, "int64": 8, "uint64": 8}.get(str(t.dtype).rsplit(".", 1)[-1], 0)
+    return size
+
+
 def _tokens_ptr(desc, t, what="d_tokens"):
     """The descriptor for these tokens' width (the caller's own is left as it is: another thread may use it over others), their number and
     address."""
-    size = t.element_size()
-    if not t.is_cuda or not t.is_contiguous() or t.is_floating_point() or size not in (4, 8):
+    size = _whole_bytes(t)
+    if not size or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{what}: contiguous CUDA whole numbers of 32 or 64 bits are wanted")
     if desc.token_bits != 8 * size:
         desc = type(desc).from_buffer_copy(desc)
@@ -635,7 +647,7 @@ def ftc_embedding_workspace_bytes(desc, n) -> int:
 def ftc_embedding_backward(desc, d_tokens, d_dy, d_row_splits, d_dtable, d_workspace, stream=None, check=True) -> int:
     desc, n, tokens = _tokens_ptr(desc, d_tokens)
     dy, dys = _matrix_ptr(d_dy, "d_dy", n, desc.H, desc.dtype)
-    if d_row_splits is not None and (d_row_splits.numel() != desc.P + 1 or d_row_splits.element_size() != 8 or d_row_splits.is_floating_point()):
+    if d_row_splits is not None and (d_row_splits.numel() != desc.P + 1 or _whole_bytes(d_row_splits) != 8):
         raise ValueError("d_row_splits: P + 1 whole numbers of 64 bits are wanted")
     out = -(-desc.V * desc.H // desc.k) * desc.P * desc.k
     ws_bytes = 0 if d_workspace is None else d_workspace.numel() * d_workspace.element_size()
@@ -660,7 +672,7 @@ def ftc_token_logprobs(desc, d_logits, d_tokens, d_logprob, d_entropy=None, d_ls
     rows = d_logits.shape[0]
     desc, tokens = _given_tokens(desc, d_tokens, rows)
     x, xs = _matrix_ptr(d_logits, "d_logits", rows, desc.V, desc.dtype)
-    if d_top_token is not None and (d_top_token.numel() != rows * desc.top or d_top_token.element_size() != 4 or d_top_token.is_floating_point()):
+    if d_top_token is not None and (d_top_token.numel() != rows * desc.top or _whole_bytes(d_top_token) != 4):
         raise ValueError("d_top_token: `top` whole numbers of 32 bits for each row are wanted")
     rc = (_lib or load()).ftc_token_logprobs(desc, rows, x, xs, tokens, _vector_ptr(d_logprob, "d_logprob", rows), _vector_ptr(d_entropy, "d_entropy", rows),
                                              _vector_ptr(d_lse, "d_lse", rows), _vector_ptr(d_top_logprob, "d_top_logprob", rows * desc.top),
