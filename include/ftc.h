@@ -593,8 +593,10 @@ typedef struct {
  *   d_grad_scale  as for ftc_adamw_step
  *   d_workspace   ftc_muon_workspace_bytes(h_plan, products) bytes, 256-byte aligned; as for ftc_layernorm_backward
  * An element of a message that was not delivered keeps its momentum, which is its U; a matrix of which nothing was delivered (with n > 0) stays as it is.
- * A matrix that meets NaN or an infinity has NaN in its weights afterwards. d_workspace's first 32-bit word is 0 after the call; were a wait
- * inside a kernel ever to give up, it is not, and no weights were changed.
+ * A matrix that meets NaN or an infinity has NaN in its weights afterwards. d_workspace's first 32-bit word is 0 once the call's work is done; were a
+ * wait inside a kernel ever to give up, it is not, and no weights were changed, but d_momentum has moved: the step is not to be called again
+ * with the same gradients unless d_momentum is put back. FTC_ECUDA: the GPU cannot run the kernels (nothing was changed), or a launch failed on the
+ * way (d_momentum may have moved).
  */
 FTC_API int ftc_muon_step(const ftc_muon_t* hyper, const void* h_plan, const void* d_plan, float* d_momentum, const float* d_grad_scale,
                           void* d_workspace, size_t workspace_bytes, void* cuda_stream);

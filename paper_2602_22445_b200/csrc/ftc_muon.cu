@@ -971,8 +971,6 @@ template <bool SPLIT> __global__ void __launch_bounds__(kSmallThreads, 1) muon_s
 }
 
 template <bool SPLIT> static cudaError_t small(const MuonArgs& a, int sms, cudaStream_t st) {
-    cudaError_t e = cudaFuncSetAttribute(muon_small_kernel<SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem);
-    if (e != cudaSuccess) return e;
     cudaLaunchAttribute early{};
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early.val.programmaticStreamSerializationAllowed = 1;
@@ -983,32 +981,43 @@ template <bool SPLIT> static cudaError_t small(const MuonArgs& a, int sms, cudaS
 }
 
 // All steps' products in one cooperative launch: as many pairs as the GPU holds at once, since tiles wait for those of other pairs.
-template <bool SPLIT> static cudaError_t products(const MuonArgs& a, cudaStream_t st) {
-    cudaError_t e = cudaFuncSetAttribute(muon_products_kernel<SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem);
-    if (e != cudaSuccess) return e;
-    cudaLaunchAttribute how_at_once{};
-    how_at_once.id = cudaLaunchAttributeCooperative;
-    how_at_once.val.cooperative = 1;
-    cudaLaunchConfig_t how{};
-    how.gridDim = dim3(2); how.blockDim = dim3(kProductThreads); how.dynamicSmemBytes = kProductSmem; how.stream = st;
-    int most = 0;
-    if ((e = cudaOccupancyMaxActiveClusters(&most, muon_products_kernel<SPLIT>, &how)) != cudaSuccess) return e;
+template <bool SPLIT> static cudaError_t products(const MuonArgs& a, int most, cudaStream_t st) {
     const uint32_t busiest = a.items[kGramTiles] > a.items[kApplyTiles] ? a.items[kGramTiles] : a.items[kApplyTiles];      // no more pairs than a product has tiles
-    if (most < 1) return cudaErrorInvalidConfiguration;
-    how.gridDim = dim3(2 * (busiest < (uint32_t)most ? busiest : (uint32_t)most));
-    how.attrs = &how_at_once; how.numAttrs = 1;
+    cudaLaunchAttribute at_once{};
+    at_once.id = cudaLaunchAttributeCooperative;
+    at_once.val.cooperative = 1;
+    cudaLaunchConfig_t how{};
+    how.gridDim = dim3(2 * (busiest < (uint32_t)most ? busiest : (uint32_t)most)); how.blockDim = dim3(kProductThreads); how.dynamicSmemBytes = kProductSmem;
+    how.stream = st; how.attrs = &at_once; how.numAttrs = 1;
     return cudaLaunchKernelEx(&how, muon_products_kernel<SPLIT>, a);
 }
 
-cudaError_t launch_muon(const MuonArgs& a, int sms, cudaStream_t st) {
+// Whether the GPU can run the kernels that take most of its shared memory; `most`: how many pairs of blocks it holds at once.
+template <bool SPLIT> static cudaError_t ready(const MuonArgs& a, int& most) {
+    cudaError_t e = cudaSuccess;
+    if (a.items[kSmall]) e = cudaFuncSetAttribute(muon_small_kernel<SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem);
+    if (e != cudaSuccess || !a.items[kGramTiles]) return e;
+    if ((e = cudaFuncSetAttribute(muon_products_kernel<SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem)) != cudaSuccess) return e;
+    cudaLaunchConfig_t how{};
+    how.gridDim = dim3(2); how.blockDim = dim3(kProductThreads); how.dynamicSmemBytes = kProductSmem;
+    if ((e = cudaOccupancyMaxActiveClusters(&most, muon_products_kernel<SPLIT>, &how)) != cudaSuccess) return e;
+    return most < 1 ? cudaErrorInvalidConfiguration : cudaSuccess;
+}
+
+template <bool SPLIT> static cudaError_t step(const MuonArgs& a, int sms, cudaStream_t st) {
+    int most = 0;
+    cudaError_t e = ready<SPLIT>(a, most);                       // before the momentum moves: it moves in place, and once
+    if (e != cudaSuccess) return e;
     muon_momentum_kernel<<<a.items[kChunks], 256, 0, st>>>(a);
-    cudaError_t e = cudaGetLastError();
+    e = cudaGetLastError();
     if (e == cudaSuccess) e = launch_second(muon_norm_kernel, a.n, 256, st, a);
     if (e == cudaSuccess) e = launch_second(muon_layout_kernel, a.items[kBlocks], 256, st, a);
-    if (e == cudaSuccess && a.items[kSmall]) e = a.split ? small<true>(a, sms, st) : small<false>(a, sms, st);
-    if (e == cudaSuccess && a.items[kGramTiles]) e = a.split ? products<true>(a, st) : products<false>(a, st);
+    if (e == cudaSuccess && a.items[kSmall]) e = small<SPLIT>(a, sms, st);
+    if (e == cudaSuccess && a.items[kGramTiles]) e = products<SPLIT>(a, most, st);
     if (e == cudaSuccess) e = launch_second(muon_update_kernel, a.items[kBlocks], 256, st, a);
     return e;
 }
+
+cudaError_t launch_muon(const MuonArgs& a, int sms, cudaStream_t st) { return a.split ? step<true>(a, sms, st) : step<false>(a, sms, st); }
 
 }  // namespace ftc

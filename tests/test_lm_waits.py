@@ -19,3 +19,11 @@ def test_kernels_that_give_up_do_not_go_by_who_has():
     assert setting == {"muon_products_kernel", "muon_small_kernel"}
     for name in setting:
         assert len(re.findall(r"a\.word", bodies[name])) == 1, name
+
+
+def test_what_can_be_refused_is_asked_before_the_momentum_moves():
+    """The momentum moves in place in the first kernel, so an error after it would count the gradient twice where the call is made again."""
+    text = open(SOURCE).read()
+    host = text[text.index("muon_small_kernel<SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize"):]
+    first = host.index("muon_momentum_kernel<<<")
+    assert max(host.rindex(name) for name in ("cudaFuncSetAttribute", "cudaOccupancyMaxActiveClusters", "ready<SPLIT>(a")) < first
