@@ -126,6 +126,7 @@ def main(steps=200):
     for i in range(steps):
         loss, _ = job.train_step()
         if i % 20 == 0 or i == steps - 1:
+            B.check_muon(job.muon_ws)
             included = job.status[:, 1]
             print(f"step {i:4d}  loss {float(loss):8.4f}  gradient norm {float(job.norm[0]):7.4f}  processes in the sum {int(included.min())}..{int(included.max())} of {job.P}")
     return float(loss)

@@ -742,3 +742,11 @@ def ftc_muon_step(hyper, plan, d_momentum, d_grad_scale, d_workspace, stream=Non
     if rc and check:
         raise FtcError(rc, "ftc_muon_step")
     return rc
+
+
+def check_muon(d_workspace) -> None:
+    """Waits for the current stream and raises FtcError where a wait inside the last ftc_muon_step() with this workspace gave up: its weights have not
+    moved then, its momentum has. A step itself does not wait for the device and cannot say so."""
+    word = d_workspace.view(-1)[:max(1, 4 // d_workspace.element_size())].view(_torch().int32)
+    if int(word[0]):
+        raise FtcError(FTC_ECUDA, "ftc_muon_step gave up on a wait")

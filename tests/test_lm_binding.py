@@ -30,3 +30,16 @@ def test_tokens_that_are_no_whole_numbers_are_refused(monkeypatch, dtype, size):
                  lambda: B.ftc_token_logprobs(prob, rows, good, None, d_top_logprob=top, d_top_token=Tensor((3, 2), dtype, size), stream=1)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("size", [16, 4096])
+def test_a_wait_that_gave_up_is_told(size):
+    import torch
+    for dtype in (torch.uint8, torch.int16, torch.float32, torch.int64):
+        ws = torch.zeros(size, dtype=dtype)
+        B.check_muon(ws)
+        ws.view(torch.uint8)[4] = 9           # behind the word
+        B.check_muon(ws)
+        ws.view(torch.uint8)[0] = 1
+        with pytest.raises(B.FtcError):
+            B.check_muon(ws)
