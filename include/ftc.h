@@ -576,8 +576,8 @@ typedef struct {
     uint32_t nesterov;           /* 1 or 0 */
     uint32_t products;           /* 16: the operands of products are rounded to float16 (of numbers up to 1.3, held times 2^14): the update X is
                                     good to 1e-3 of its norm where the momentum is well conditioned (6e-4 for wide ones). 32: operands are
-                                    held as two float16 numbers each, three products for one: 2e-6 with sums of 256 terms, 1e-5 with 2048,
-                                    3e-5 with 4096 */
+                                    held as two float16 numbers each, three products for one: 2e-6 with sums of 256 terms, 5e-6 with 1000,
+                                    1.5e-5 with 2000, 3e-5 with 4096 */
     uint32_t reserved;           /* 0 */
 } ftc_muon_t;
 

@@ -7,7 +7,7 @@
 // makes a cycle (0.7 of what 16-bit logits need); seven instructions an element (8192 rows of 65536). Logits below -1e30 count as that, so that no infinity meets a
 // zero; a row whose largest c m is beyond 1e8 either way, but not -infinity (all of it masked by the type's lowest value, say) is done again with
 // c (x - m), element by element.
-// Rows are divided over the blocks of a cluster where there are few. 8192 rows of 65536 in bf16: 199 us, 5.4 TB/s; 8 rows of 131072: 10 us.
+// Rows are divided over the blocks of a cluster where there are few. 8192 rows of 65536 in bf16: 195 to 207 us by box, 5.2 to 5.5 TB/s; 8 rows of 131072: 10 us.
 //
 // Top alternatives: the lanes' largest logits are at hand after the pass. The n-th largest of them (its upper 16 bits, found bit by bit by counting
 // lanes) is a bound that n elements reach, and about as many do (lanes hold V / 256 elements each): only the lanes that reach it look through their elements again, what reaches the bound is listed
@@ -492,7 +492,7 @@ cudaError_t launch_token_logprobs(const LogprobArgs& a, int sms, cudaStream_t st
 //
 // With A = -scale (dlogprob + dentropy * entropy), B = -scale * dentropy and l = scale x - lse, rounded once: p (A + B l), and scale * dlogprob more at
 // the token. (A + B' x with lse in A would cancel: lse's size over 2^24 of an error.)
-// Bound by memory (8192 rows of 65536 in bf16: 331 us, 6.5 TB/s); twelve instructions an element. A row is written in vectors
+// Bound by memory (8192 rows of 65536 in bf16: 330 to 342 us by box, 6.3 to 6.5 TB/s); twelve instructions an element. A row is written in vectors
 // from its own 16-byte boundary on. Where the logits lie otherwise against that boundary (a slice of a padded matrix), a vector is put together from the two that cover it.
 
 // far: lse in float32 is too coarse for the type: half its step, which is p's relative error, is 2^-18 below 2^7 (float32), 2^-14 below 2^11 (float16,
