@@ -428,13 +428,14 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
         ln_s = logf(s); mean_d = t / s;
     }
     const bool bad = isnan(m) || m == INFINITY, empty = m == -INFINITY;
+    auto below = [&](float v) { return fmaf(2.f * a.scale, 0.5f * v - 0.5f * m, -ln_s); };      // scale (v - m) - ln s; v - m itself may leave float32
     // scale * m may leave float32: the largest number stands for it then, so that an lse of -infinity is that of an empty row and no other
     const float nan = __int_as_float(0x7FFFFFFF), lse = bad ? nan : empty ? -INFINITY : fminf(fmaxf(fmaf(a.scale, m, ln_s), -kMost), kMost);
     if (lane == 0) {
         if (a.lse) a.lse[row] = lse;
         if (a.entropy) a.entropy[row] = bad ? nan : empty ? 0.f : fmaxf(0.f, ln_s - kLn2 * mean_d);
         if (a.logprob) {
-            a.logprob[row] = token < 0 ? 0.f : bad ? nan : empty ? -INFINITY : fmaf(a.scale, token_logit - m, -ln_s);
+            a.logprob[row] = token < 0 ? 0.f : bad ? nan : empty ? -INFINITY : below(token_logit);
         }
     }
     if (!TOP) return;
@@ -451,7 +452,7 @@ template <typename T, bool TOP, uint32_t GROUP> __global__ void __launch_bounds_
     }
     if (lane < a.top) {
         const float v = value_of(best.best);
-        a.top_logprob[(uint64_t)row * a.top + lane] = bad ? nan : empty ? -INFINITY : fmaf(a.scale, v - m, -ln_s);
+        a.top_logprob[(uint64_t)row * a.top + lane] = bad ? nan : empty ? -INFINITY : below(v);
         a.top_token[(uint64_t)row * a.top + lane] = best.best ? (int32_t)index_of(best.best) : 0;
     }
 }

@@ -119,3 +119,21 @@ def test_gradient_of_logits_far_from_zero(name, V, shift):
     off = off + (abs(want) + off) * O.half_step(name) + O.least(name) * O.half_step(name) * 2
     got = d.double().cpu().numpy()
     assert (abs(got - want) <= off).all(), (abs(got - want) / off).max()
+
+
+@pytest.mark.parametrize("name", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("V", [4, 90, 40001])
+@pytest.mark.parametrize("scale", [0.4, 1e-3, 1e-6])
+def test_tokens_further_below_the_largest_than_float32_reaches(name, V, scale):
+    """x[token] - max leaves float32 where the type's lowest value meets the largest one; times a small scale it does not."""
+    rng = np.random.default_rng(V)
+    x = edge_rows(rng, V, DT[name], "both")
+    x[3] = torch.finfo(DT[name]).min
+    x[3, 1] = torch.finfo(DT[name]).max / 2
+    t = np.array([0, 0, V - 1, V // 2])
+    _, (given, entropy, lse), best, which = forward(x, torch.from_numpy(t).cuda(), scale, 4)
+    w_lse, w_given, w_entropy, w_best, w_which, spread = O.logprobs(x.double().cpu().numpy(), t, float(np.float32(scale)), 4)
+    s_off = O.sum_off(spread, V)
+    for got, want, off in ((given, w_given, s_off), (best, w_best, s_off[:, None]), (lse, w_lse, s_off)):
+        assert (abs(got.double().cpu().numpy() - want) <= off + 4 * O.U32 * (1 + abs(want))).all()
+    assert (which.cpu().numpy() == w_which).all() and (abs(entropy.double().cpu().numpy() - w_entropy) <= 4 * s_off * (1 + spread)).all()
